@@ -45,7 +45,9 @@ typedef enum {
 } sol_status;
 
 typedef enum { SOL_F32 = 0, SOL_BF16 = 1 } sol_dtype;  /* bf16 = bf16 storage, fp32 accumulate */
-typedef enum { SOL_ACT_NONE = 0, SOL_ACT_RELU = 1 } sol_act;
+/* GELU: z * Phi(z), the normal distribution function; GELU_TANH: its form with tanh, z * (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2;
+ * SILU: z / (1 + exp(-z)).  These three belong to sol_linear_fused and sol_linear_backward; every other call takes NONE and RELU. */
+typedef enum { SOL_ACT_NONE = 0, SOL_ACT_RELU = 1, SOL_ACT_GELU = 2, SOL_ACT_GELU_TANH = 3, SOL_ACT_SILU = 4 } sol_act;
 typedef enum { SOL_POOL_NONE = 0, SOL_POOL_MAX = 1, SOL_POOL_AVG = 2 } sol_pool_kind;
 typedef enum { SOL_LAYER_CONV = 0, SOL_LAYER_POOL = 1, SOL_LAYER_GAP = 2, SOL_LAYER_LINEAR = 3, SOL_LAYER_DWCONV = 4,
                SOL_LAYER_CONCAT = 5 } sol_layer_kind;
@@ -201,6 +203,58 @@ sol_status sol_dwconv2d_fused(const sol_tensor_desc *xd, const void *x, const so
  * cd = {out_f, in_f, 1,1,1,1,0,0}); bias device fp32 [out_f] or NULL. */
 sol_status sol_linear(int m, int in_f, int out_f, sol_dtype dt, const void *x, const void *w_packed,
                       const float *bias, int act, void *y, void *hip_stream);
+
+/* Dropout: element (row, col) of a [rows][cols] tensor is kept if a 16-bit random number is at least t = p * 65536, rounded to the nearest
+ * integer (ties to even), and is then multiplied by 65536 / (65536 - t); otherwise it is 0, whatever it was.  The mask is never stored: the numbers come from
+ * Philox4x32-10 with the key (low word, high word of seed) and the counter (col / 8, row, call, *step), whose four output words give, low half
+ * first, the numbers of the 8 columns of a group.  The same description therefore draws the same mask in the forward pass, in the backward
+ * pass and in any other kernel, on tensors of any pitch.
+ *   p      0 .. 1; 0 keeps everything
+ *   call   which dropout of the model this is
+ *   step   NULL (0), or a device word that the kernel reads when it runs: a captured graph draws a new mask with every replay
+ *          behind which the caller has changed it */
+typedef struct { float p; uint64_t seed; uint32_t call; const uint32_t *step; } sol_dropout_desc;
+
+/* y = dropout(x) + residual over rows x cols elements; residual may be NULL, y may be x or residual itself.  Its backward pass is the
+ * same call on the gradient, without a residual (the residual's gradient is the incoming one). */
+sol_status sol_dropout(int rows, int cols, sol_dtype dt, const void *x, const sol_dropout_desc *drop, const void *residual, void *y,
+                       void *hip_stream);
+
+/* The linear layer with its neighbours in the product's epilogue, and its backward pass (training, and serving from one row up):
+ *   forward   z = x W^T + bias          y = dropout(act(z)) + residual
+ *   backward  dz = act'(z) * dropout(dy)    dx = dz W    dW = dz^T x    db = sum over the rows of dz
+ * (the residual's gradient is dy itself).  Unlike the convolutions' epilogue, the residual is added behind the activation. */
+typedef struct {
+    int m, in_f, out_f;         /* x [m][in_f], y [m][out_f]; at most 2^20 features each */
+    int dtype;                  /* sol_dtype of x, W, residual, y, preact, dy and dx */
+    int act;                    /* sol_act */
+    int ldx, ldy, ldr;          /* elements between consecutive rows of x, of y (backward: of dy) and of residual: 0 = dense, or the number of
+                                   features or more, at most 2^21; elements between the rows are neither read into a result nor written */
+} sol_linear_desc;
+
+/* Device scratch that sol_linear_fused needs, often 0: a copy of x when its rows do not start at multiples of 16 bytes or do not end on one, and
+ * partial sums when there are too few rows to fill the GPU.  sol_linear_backward: dz, partial sums of dW and db, and such a copy. */
+size_t sol_linear_fused_workspace_bytes(const sol_linear_desc *ld);
+size_t sol_linear_backward_workspace_bytes(const sol_linear_desc *ld);
+
+/*   w_packed   [out_f][in_f] as for sol_linear;  bias: device fp32 [out_f] or NULL;  drop: NULL or p = 0 for none
+ *   residual   NULL or [m][out_f]
+ *   preact     NULL, or dense [m][out_f] that receives z, rounded to dtype (y is computed from z before that rounding)
+ *   y may be residual itself (same pitch); otherwise outputs must not overlap inputs.
+ * Sums are fp32.  An infinite z gives the activation's limit, a NaN a NaN (RELU: 0).  m = 0 does nothing. */
+sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void *w_packed, const float *bias,
+                            const sol_dropout_desc *drop, const void *residual, void *y, void *preact, void *workspace,
+                            size_t workspace_bytes, void *hip_stream);
+
+/*   dy         [m][out_f] with pitch ldy;  x, w_packed, drop: those of the forward call
+ *   preact     z as sol_linear_fused stored it; may be NULL with SOL_ACT_NONE
+ *   dx         NULL, or dense [m][in_f];  db: NULL, or device fp32 [out_f]
+ *   dw         NULL, or dense [out_f][in_f] (not packed) of dw_dtype: the layer's dtype or SOL_F32
+ * For bf16, dz is rounded to bf16 before it is multiplied (both products run on the bf16 matrix instructions); db sums it unrounded.
+ * With m = 0, dw and db become zeros.  Every sum runs in an order that depends on the sizes alone. */
+sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const void *x, const void *w_packed, const void *preact,
+                               const sol_dropout_desc *drop, void *dx, void *dw, int dw_dtype, float *db, void *workspace,
+                               size_t workspace_bytes, void *hip_stream);
 
 /* Stand-alone pooling over NHWC x (max with optional int32 argmax as above, or average).
  * Padding acts as -inf for max and as 0 for average.  Requires pad < kernel. */

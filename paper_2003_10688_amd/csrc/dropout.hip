@@ -1,0 +1,142 @@
+// Memory-bound passes beside the linear layer's products: dropout, the gradient in front of the products (activation's slope and dropout's
+// mask in one pass, with the column sums that are the bias gradient), partial sums put together, rows copied to an aligned pitch.
+#include "linear_ops.h"
+
+namespace sol {
+
+// y = dropout(x) + residual.  One group of 8 columns per thread and step: one call of the generator.
+template <typename T>
+__global__ void __launch_bounds__(256) dropout_kernel(const T *x, const T *res, T *y, int cols, uint32_t groups, FastDiv dg, uint32_t total, const DropArgs d) {
+    const uint32_t step = drop_step(d);
+    for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < total; i += gridDim.x * 256u) {
+        uint32_t row, g;
+        dg.divmod(i, row, g);
+        const size_t at = (size_t)row * cols + g * 8;
+        const int nv = min(8, cols - (int)g * 8);
+        float v[8], r[8];
+        load8_any<T>(x + at, v, nv);
+        if (res) load8_any<T>(res + at, r, nv);
+        if (d.t) drop8(d, step, row, g, v);
+        if (res) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] += r[e];
+        }
+        store8_any<T>(y + at, v, nv);
+    }
+}
+
+sol_status launch_dropout(const void *x, const void *res, void *y, int rows, int cols, int dt, const DropArgs &d, hipStream_t st) {
+    const uint32_t groups = (uint32_t)ceil_div(cols, 8), total = (uint32_t)rows * groups;
+    const dim3 grid((unsigned)min((total + 255u) / 256u, 256u * 32u));
+    if (dt == SOL_BF16)
+        hipLaunchKernelGGL(dropout_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t *)x, (const bf16_t *)res, (bf16_t *)y, cols, groups, FastDiv(groups), total, d);
+    else
+        hipLaunchKernelGGL(dropout_kernel<float>, grid, dim3(256), 0, st, (const float *)x, (const float *)res, (float *)y, cols, groups, FastDiv(groups), total, d);
+    SOL_HIP(hipGetLastError());
+    return SOL_OK;
+}
+
+// dz = act'(z) * dropout(dy), and sums of its columns in 32 bits before it is rounded.  A workgroup takes 256 columns of a chunk of rows: 32 groups of 8
+// columns x 8 rows at a time.
+constexpr int DZ_ROWS = 8;
+template <typename T>
+__global__ void __launch_bounds__(256) linear_dz_kernel(const T *__restrict__ dy, long lddy, const T *__restrict__ z, T *__restrict__ dz, long ldz, int rows, int cols,
+                                                        int rows_per_chunk, int act, const DropArgs d, float *__restrict__ part) {
+    __shared__ float red[DZ_ROWS][256 + 4];
+    const int gl = threadIdx.x & 31, rl = threadIdx.x >> 5, n = (blockIdx.x * 32 + gl) * 8, nv = min(8, cols - n);
+    const int r0 = blockIdx.y * rows_per_chunk, r1 = min(rows, r0 + rows_per_chunk);
+    const uint32_t step = drop_step(d);
+    float sum[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) sum[e] = 0.f;
+    if (nv > 0 || (dz && n < ldz)) {
+        for (int r = r0 + rl; r < r1; r += DZ_ROWS) {
+            float v[8], s[8];
+            load8_any<T>(dy + r * lddy + n, v, nv);
+            if (act != SOL_ACT_NONE) load8_any<T>(z + (size_t)r * cols + n, s, nv);
+            if (d.t) drop8(d, step, (uint32_t)r, (uint32_t)n >> 3, v);
+            switch (act) {
+#define SOL_ACT_CASE(A) case A: { _Pragma("unroll") for (int e = 0; e < 8; e++) v[e] *= act_slope(A, s[e]); break; }
+                SOL_ACT_CASE(SOL_ACT_RELU)
+                SOL_ACT_CASE(SOL_ACT_GELU)
+                SOL_ACT_CASE(SOL_ACT_GELU_TANH)
+                SOL_ACT_CASE(SOL_ACT_SILU)
+#undef SOL_ACT_CASE
+                default: break;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                v[e] = e < nv ? v[e] : 0.f;         // the columns behind the last are zeros in dz: the products' reduction runs over them
+                sum[e] += v[e];
+            }
+            if (dz) store8_any<T>(dz + r * ldz + n, v, 8);
+        }
+    }
+    if (!part) return;
+#pragma unroll
+    for (int e = 0; e < 8; e++) red[rl][gl * 8 + e] = sum[e];
+    __syncthreads();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
+    float t = 0.f;
+#pragma unroll
+    for (int r = 0; r < DZ_ROWS; r++) t += red[r][threadIdx.x];
+    part[(size_t)blockIdx.y * cols + c] = t;
+}
+
+static int dz_rows_per_chunk(int rows, int cols) {
+    const int want = max(1, 1024 / ceil_div(cols, 256));         // four workgroups per CU
+    return (int)round_up((size_t)max(1, ceil_div(rows, want)), DZ_ROWS);
+}
+int linear_dz_chunks(int rows, int cols) { return rows > 0 ? ceil_div(rows, dz_rows_per_chunk(rows, cols)) : 0; }
+
+sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, float *db,
+                            hipStream_t st) {
+    const int rpc = dz_rows_per_chunk(rows, cols), chunks = linear_dz_chunks(rows, cols);
+    float *p = !db ? nullptr : chunks == 1 ? db : part;
+    const dim3 grid(ceil_div(dz ? (int)ldz : cols, 256), chunks);
+    if (dt == SOL_BF16)
+        hipLaunchKernelGGL(linear_dz_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t *)dy, lddy, (const bf16_t *)z, (bf16_t *)dz, ldz, rows, cols, rpc, act, d, p);
+    else
+        hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(256), 0, st, (const float *)dy, lddy, (const float *)z, (float *)dz, ldz, rows, cols, rpc, act, d, p);
+    SOL_HIP(hipGetLastError());
+    return db && chunks != 1 ? launch_sum_parts(part, chunks, cols, db, SOL_F32, st) : SOL_OK;
+}
+
+// out[i] = part[0][i] + part[1][i] + ..., in this order
+template <typename T> __global__ void __launch_bounds__(256) sum_parts_kernel(const float *__restrict__ part, int nsplit, long n, T *__restrict__ out) {
+    for (long i = blockIdx.x * 256l + threadIdx.x; i < n; i += gridDim.x * 256l) {
+        float s = 0.f;
+        for (int k = 0; k < nsplit; k++) s += part[k * n + i];
+        Elem<T>::store(out + i, s);
+    }
+}
+
+sol_status launch_sum_parts(const float *part, int nsplit, long n, void *out, int out_dt, hipStream_t st) {
+    const dim3 grid((unsigned)min((n + 255) / 256, 8192l));
+    if (out_dt == SOL_BF16) hipLaunchKernelGGL(sum_parts_kernel<bf16_t>, grid, dim3(256), 0, st, part, nsplit, n, (bf16_t *)out);
+    else hipLaunchKernelGGL(sum_parts_kernel<float>, grid, dim3(256), 0, st, part, nsplit, n, (float *)out);
+    SOL_HIP(hipGetLastError());
+    return SOL_OK;
+}
+
+template <typename T> __global__ void __launch_bounds__(256) pad_rows_kernel(const T *__restrict__ x, long ld, T *__restrict__ out, long ldo, int cols, FastDiv dg, uint32_t total) {
+    for (uint32_t i = blockIdx.x * 256u + threadIdx.x; i < total; i += gridDim.x * 256u) {
+        uint32_t row, g;
+        dg.divmod(i, row, g);
+        float v[8];
+        load8_any<T>(x + row * ld + g * 8, v, min(8, cols - (int)g * 8));       // zeros where there are none
+        store8_any<T>(out + row * ldo + g * 8, v, 8);
+    }
+}
+
+sol_status launch_pad_rows(const void *x, long ld, void *out, long ldo, int rows, int cols, int dt, hipStream_t st) {
+    const uint32_t groups = (uint32_t)(ldo / 8), total = (uint32_t)rows * groups;
+    const dim3 grid((unsigned)min((total + 255u) / 256u, 256u * 32u));
+    if (dt == SOL_BF16) hipLaunchKernelGGL(pad_rows_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t *)x, ld, (bf16_t *)out, ldo, cols, FastDiv(groups), total);
+    else hipLaunchKernelGGL(pad_rows_kernel<float>, grid, dim3(256), 0, st, (const float *)x, ld, (float *)out, ldo, cols, FastDiv(groups), total);
+    SOL_HIP(hipGetLastError());
+    return SOL_OK;
+}
+
+}  // namespace sol

@@ -1,0 +1,224 @@
+// C entry points of the linear layer with its epilogue, its backward pass, and dropout: checks of the arguments, plans, workspaces.
+#include <math.h>
+
+#include "linear_ops.h"
+
+namespace sol {
+namespace {
+
+#define SOL_TRY(call) \
+    do { \
+        const sol_status s_ = (call); \
+        if (s_ != SOL_OK) return s_; \
+    } while (0)
+
+constexpr int MAX_FEATURES = 1 << 20, MAX_PITCH = 1 << 21;
+
+sol_status check_drop(const sol_dropout_desc *d, DropArgs *out) {
+    *out = DropArgs{0, 0, 0, nullptr, 0, 1.f};
+    if (!d) return SOL_OK;
+    SOL_REQUIRE(d->p >= 0.f && d->p <= 1.f, SOL_ERR_SHAPE, "dropout probability %g is not in 0 .. 1", (double)d->p);       // refuses a NaN too
+    SOL_REQUIRE((reinterpret_cast<uintptr_t>(d->step) & 3u) == 0, SOL_ERR_ALIGN, "dropout's step word must be 4-byte aligned");
+    const int t = (int)lrint((double)d->p * 65536.0);
+    *out = DropArgs{(uint32_t)d->seed, (uint32_t)(d->seed >> 32), d->call, d->step, (uint32_t)t, t < 65536 ? (float)(65536.0 / (65536 - t)) : 0.f};
+    return SOL_OK;
+}
+
+sol_status check_pitch(const char *what, int rows, int cols, int *ld) {
+    if (*ld == 0) *ld = cols;
+    SOL_REQUIRE(*ld >= cols, SOL_ERR_SHAPE, "pitch %d of %s is less than its %d columns", *ld, what, cols);
+    SOL_REQUIRE(*ld <= MAX_PITCH, SOL_ERR_UNSUPPORTED, "pitch %d of %s is more than 2^21", *ld, what);
+    SOL_REQUIRE((double)rows * *ld < 2147483648.0, SOL_ERR_UNSUPPORTED, "%s spans 2^31 elements or more", what);
+    return SOL_OK;
+}
+
+// *l: the description with every pitch filled in
+sol_status check_linear(const sol_linear_desc *ld, sol_linear_desc *l) {
+    SOL_REQUIRE(ld, SOL_ERR_NULL, "linear descriptor is NULL");
+    *l = *ld;
+    SOL_REQUIRE(l->dtype == SOL_F32 || l->dtype == SOL_BF16, SOL_ERR_DTYPE, "linear: unknown dtype %d", l->dtype);
+    SOL_REQUIRE(l->m >= 0 && l->in_f > 0 && l->out_f > 0, SOL_ERR_SHAPE, "bad linear shape m=%d in=%d out=%d", l->m, l->in_f, l->out_f);
+    SOL_REQUIRE(l->in_f <= MAX_FEATURES && l->out_f <= MAX_FEATURES, SOL_ERR_UNSUPPORTED, "more than 2^20 features: in=%d out=%d", l->in_f, l->out_f);
+    SOL_REQUIRE((double)l->in_f * l->out_f < 1073741824.0, SOL_ERR_UNSUPPORTED, "weight too large");
+    SOL_REQUIRE(l->act >= SOL_ACT_NONE && l->act <= SOL_ACT_SILU, SOL_ERR_SHAPE, "bad activation %d", l->act);
+    SOL_TRY(check_pitch("x", l->m, l->in_f, &l->ldx));
+    SOL_TRY(check_pitch("y", l->m, l->out_f, &l->ldy));
+    return check_pitch("residual", l->m, l->out_f, &l->ldr);
+}
+
+int pack_pitch(int n, int dt) { return (int)round_up((size_t)n, dt == SOL_BF16 ? 64 : 32); }
+// rows that DMA can take as they are: they start and end at multiples of 16 bytes
+bool rows_aligned(int ld, int cols, int dt) { return (ld * dtype_size(dt)) % 16 == 0 && (cols * dtype_size(dt)) % 16 == 0; }
+bool cut_needed(int k, int dt) { return (k * dtype_size(dt)) % 64 != 0; }
+
+// Parts of a reduction of K, so that a product of few tiles fills the GPU: about one workgroup per CU, each with eight stages or more.
+int split_of(int M, int N, int K, int dt) {
+    const long tiles = (long)ceil_div(M, 64) * ceil_div(N, 64), stages = ceil_div(K, 64 / (int)dtype_size(dt));
+    if (tiles >= 192) return 1;
+    return (int)max(1l, min(min(256 / tiles, stages / 8), 16l));
+}
+
+struct ForwardPlan {
+    size_t xpad, bytes;
+    bool pad;
+};
+ForwardPlan forward_plan(const sol_linear_desc &l) {
+    ForwardPlan p{};
+    p.pad = !rows_aligned(l.ldx, l.in_f, l.dtype);
+    if (p.pad) p.bytes = (size_t)l.m * pack_pitch(l.in_f, l.dtype) * dtype_size(l.dtype);
+    return p;
+}
+
+struct BackwardPlan {
+    size_t dz, part, xpad, sums, bytes;     // offsets
+    bool pad;
+    int dw_split, dx_split;
+};
+BackwardPlan backward_plan(const sol_linear_desc &l) {
+    BackwardPlan p{};
+    const size_t es = dtype_size(l.dtype);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at = round_up(at + bytes, 256); return here; };
+    p.dz = take((size_t)l.m * pack_pitch(l.out_f, l.dtype) * es);
+    p.part = take((size_t)linear_dz_chunks(l.m, l.out_f) * l.out_f * 4);
+    p.pad = !rows_aligned(l.ldx, l.in_f, l.dtype);
+    p.xpad = take(p.pad ? (size_t)l.m * pack_pitch(l.in_f, l.dtype) * es : 0);
+    p.dw_split = split_of(l.out_f, l.in_f, l.m, l.dtype);
+    p.dx_split = split_of(l.m, l.in_f, l.out_f, l.dtype);
+    const size_t dw = p.dw_split > 1 ? (size_t)p.dw_split * l.out_f * l.in_f * 4 : 0, dx = p.dx_split > 1 ? (size_t)p.dx_split * l.m * l.in_f * 4 : 0;
+    p.sums = take(dw > dx ? dw : dx);
+    p.bytes = at;
+    return p;
+}
+
+sol_status check_workspace(const void *workspace, size_t have, size_t need) {
+    SOL_REQUIRE(have >= need, SOL_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", have, need);
+    SOL_REQUIRE(workspace || need == 0, SOL_ERR_NULL, "workspace is NULL");
+    SOL_REQUIRE(aligned16(workspace), SOL_ERR_ALIGN, "workspace must be 16-byte aligned");
+    return SOL_OK;
+}
+
+// extent of [rows][cols] with pitch ld
+size_t span(int rows, long ld, int cols, int dt) { return ((size_t)(rows - 1) * ld + cols) * dtype_size(dt); }
+
+}  // namespace
+}  // namespace sol
+
+using namespace sol;
+
+extern "C" {
+
+size_t sol_linear_fused_workspace_bytes(const sol_linear_desc *ld) {
+    sol_linear_desc l;
+    return check_linear(ld, &l) == SOL_OK && l.m > 0 ? forward_plan(l).bytes : 0;
+}
+
+size_t sol_linear_backward_workspace_bytes(const sol_linear_desc *ld) {
+    sol_linear_desc l;
+    return check_linear(ld, &l) == SOL_OK && l.m > 0 ? backward_plan(l).bytes : 0;
+}
+
+sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void *w_packed, const float *bias, const sol_dropout_desc *drop, const void *residual, void *y,
+                            void *preact, void *workspace, size_t workspace_bytes, void *stream) {
+    sol_linear_desc l;
+    DropArgs d;
+    SOL_TRY(check_linear(ld, &l));
+    SOL_TRY(check_drop(drop, &d));
+    if (l.m == 0) return SOL_OK;
+    SOL_REQUIRE(x && w_packed && y, SOL_ERR_NULL, "x, w_packed and y must not be NULL");
+    SOL_REQUIRE(aligned16(x) && aligned16(w_packed) && aligned16(bias) && aligned16(residual) && aligned16(y) && aligned16(preact), SOL_ERR_ALIGN,
+                "device pointers must be 16-byte aligned");
+    SOL_REQUIRE(y != x && y != w_packed && preact != x && preact != w_packed && (!preact || (preact != y && preact != residual)), SOL_ERR_UNSUPPORTED,
+                "linear: outputs must not alias inputs or each other");
+    SOL_REQUIRE(y != residual || l.ldy == l.ldr, SOL_ERR_UNSUPPORTED, "linear: y in the residual's place needs its pitch");
+    const ForwardPlan p = forward_plan(l);
+    SOL_TRY(check_workspace(workspace, workspace_bytes, p.bytes));
+    hipStream_t st = (hipStream_t)stream;
+    const int kp = pack_pitch(l.in_f, l.dtype);
+
+    GemmArgs a{};
+    a.a = x; a.lda = l.ldx; a.a_bytes = span(l.m, l.ldx, l.in_f, l.dtype); a.a_cut = cut_needed(l.in_f, l.dtype);
+    if (p.pad) {
+        SOL_TRY(launch_pad_rows(x, l.ldx, workspace, kp, l.m, l.in_f, l.dtype, st));
+        a.a = workspace; a.lda = kp; a.a_bytes = span(l.m, kp, kp, l.dtype); a.a_cut = 0;
+    }
+    a.b = w_packed; a.ldb = kp; a.b_bytes = span(l.out_f, kp, kp, l.dtype);
+    a.M = l.m; a.N = l.out_f; a.K = l.in_f; a.nsplit = 1;
+    a.epi = LinearEpi{bias, residual, y, preact, l.ldr, l.ldy, l.act, d};
+    return launch_linear_gemm(a, l.dtype, GEMM_FORWARD, st);
+}
+
+sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const void *x, const void *w_packed, const void *preact, const sol_dropout_desc *drop, void *dx, void *dw,
+                               int dw_dtype, float *db, void *workspace, size_t workspace_bytes, void *stream) {
+    sol_linear_desc l;
+    DropArgs d;
+    SOL_TRY(check_linear(ld, &l));
+    SOL_TRY(check_drop(drop, &d));
+    SOL_REQUIRE(!dw || dw_dtype == l.dtype || dw_dtype == SOL_F32, SOL_ERR_DTYPE, "dw is of the layer's dtype or fp32, not %d", dw_dtype);
+    SOL_REQUIRE(aligned16(dy) && aligned16(x) && aligned16(w_packed) && aligned16(preact) && aligned16(dx) && aligned16(dw) && aligned16(db), SOL_ERR_ALIGN,
+                "device pointers must be 16-byte aligned");
+    hipStream_t st = (hipStream_t)stream;
+    if (l.m == 0) {
+        if (dw) SOL_TRY(launch_sum_parts(nullptr, 0, (long)l.out_f * l.in_f, dw, dw_dtype, st));
+        return db ? launch_sum_parts(nullptr, 0, l.out_f, db, SOL_F32, st) : SOL_OK;
+    }
+    SOL_REQUIRE(dy && (x || !dw) && (w_packed || !dx), SOL_ERR_NULL, "dy, x (for dw) and w_packed (for dx) must not be NULL");
+    SOL_REQUIRE(preact || l.act == SOL_ACT_NONE, SOL_ERR_NULL, "preact must not be NULL with an activation");
+    const void *const outs[3] = {dx, dw, db}, *const ins[4] = {dy, x, w_packed, preact};
+    for (int i = 0; i < 3; i++) {
+        for (const void *in : ins) SOL_REQUIRE(!outs[i] || outs[i] != in, SOL_ERR_UNSUPPORTED, "linear backward: outputs must not alias inputs");
+        for (int j = 0; j < i; j++) SOL_REQUIRE(!outs[i] || outs[i] != outs[j], SOL_ERR_UNSUPPORTED, "linear backward: outputs must not alias each other");
+    }
+    const BackwardPlan p = backward_plan(l);
+    SOL_TRY(check_workspace(workspace, workspace_bytes, p.bytes));
+    unsigned char *ws = static_cast<unsigned char *>(workspace);
+
+    // dz is dy itself where neither an activation nor dropout lies between them
+    const bool own_dz = (dx || dw) && (l.act != SOL_ACT_NONE || d.t || !rows_aligned(l.ldy, l.out_f, l.dtype));
+    const long ldz = own_dz ? pack_pitch(l.out_f, l.dtype) : l.ldy;
+    const void *dz = own_dz ? ws + p.dz : dy;
+    const size_t dz_bytes = own_dz ? span(l.m, ldz, (int)ldz, l.dtype) : span(l.m, ldz, l.out_f, l.dtype);
+    if (own_dz || db)
+        SOL_TRY(launch_linear_dz(dy, l.ldy, preact, own_dz ? ws + p.dz : nullptr, ldz, l.m, l.out_f, l.act, d, l.dtype, reinterpret_cast<float *>(ws + p.part), db, st));
+    const int kp = pack_pitch(l.in_f, l.dtype);
+    if (dx) {
+        GemmArgs a{};
+        a.a = dz; a.lda = ldz; a.a_bytes = dz_bytes; a.a_cut = !own_dz && cut_needed(l.out_f, l.dtype);
+        a.b = w_packed; a.ldb = kp; a.b_bytes = span(l.out_f, kp, kp, l.dtype);
+        a.M = l.m; a.N = l.in_f; a.K = l.out_f; a.nsplit = p.dx_split;
+        a.part = reinterpret_cast<float *>(ws + p.sums);
+        a.out = dx; a.ldo = l.in_f; a.out_dt = l.dtype;
+        SOL_TRY(launch_linear_gemm(a, l.dtype, GEMM_DX, st));
+        if (p.dx_split > 1) SOL_TRY(launch_sum_parts(a.part, p.dx_split, (long)l.m * l.in_f, dx, l.dtype, st));
+    }
+    if (dw) {
+        GemmArgs a{};
+        a.a = dz; a.lda = ldz; a.a_bytes = dz_bytes;
+        a.b = x; a.ldb = l.ldx; a.b_bytes = span(l.m, l.ldx, l.in_f, l.dtype);
+        if (p.pad) {
+            SOL_TRY(launch_pad_rows(x, l.ldx, ws + p.xpad, kp, l.m, l.in_f, l.dtype, st));
+            a.b = ws + p.xpad; a.ldb = kp; a.b_bytes = span(l.m, kp, kp, l.dtype);
+        }
+        a.M = l.out_f; a.N = l.in_f; a.K = l.m; a.nsplit = p.dw_split;
+        a.part = reinterpret_cast<float *>(ws + p.sums);
+        a.out = dw; a.ldo = l.in_f; a.out_dt = dw_dtype;
+        SOL_TRY(launch_linear_gemm(a, l.dtype, GEMM_DW, st));
+        if (p.dw_split > 1) SOL_TRY(launch_sum_parts(a.part, p.dw_split, (long)l.out_f * l.in_f, dw, dw_dtype, st));
+    }
+    return SOL_OK;
+}
+
+sol_status sol_dropout(int rows, int cols, sol_dtype dt, const void *x, const sol_dropout_desc *drop, const void *residual, void *y, void *stream) {
+    SOL_REQUIRE(dt == SOL_F32 || dt == SOL_BF16, SOL_ERR_DTYPE, "dropout: unknown dtype %d", (int)dt);
+    SOL_REQUIRE(rows >= 0 && cols > 0, SOL_ERR_SHAPE, "bad dropout shape [%d,%d]", rows, cols);
+    SOL_REQUIRE((double)rows * cols < 2147483648.0, SOL_ERR_UNSUPPORTED, "dropout: 2^31 elements or more");
+    SOL_REQUIRE(drop, SOL_ERR_NULL, "dropout descriptor is NULL");
+    DropArgs d;
+    SOL_TRY(check_drop(drop, &d));
+    if (rows == 0) return SOL_OK;
+    SOL_REQUIRE(x && y, SOL_ERR_NULL, "x and y must not be NULL");
+    SOL_REQUIRE(aligned16(x) && aligned16(residual) && aligned16(y), SOL_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    return launch_dropout(x, residual, y, rows, cols, dt, d, (hipStream_t)stream);
+}
+
+}  // extern "C"

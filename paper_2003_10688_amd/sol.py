@@ -15,7 +15,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("SOL_MI355_LIB") or os.path.join(_HERE, "libsol_mi355.so")
 
 F32, BF16 = 0, 1
-ACT_NONE, ACT_RELU = 0, 1
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)      # the last three: sol_linear_fused and sol_linear_backward
 POOL_NONE, POOL_MAX, POOL_AVG = 0, 1, 2
 LAYER_CONV, LAYER_POOL, LAYER_GAP, LAYER_LINEAR, LAYER_DWCONV, LAYER_CONCAT = 0, 1, 2, 3, 4, 5
 NET_TRAINING, NET_KEEP_ACTIVATIONS = 1, 2
@@ -41,6 +41,24 @@ class ConvDesc(C.Structure):
 class Layer(C.Structure):
     _fields_ = [("kind", C.c_int), ("conv", ConvDesc), ("has_bn", C.c_int), ("act", C.c_int),
                 ("pool", PoolDesc), ("out_features", C.c_int), ("src", C.c_int), ("res", C.c_int), ("pre_bn", C.c_int)]
+
+
+class LinearDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("m", "in_f", "out_f", "dtype", "act", "ldx", "ldy", "ldr")]
+
+
+class Dropout(C.Structure):
+    """p: probability of dropping an element; seed: 64 bits; call: which dropout of the model this is; step: None, or a device int32
+    tensor of one element that the kernels read when they run (a captured graph draws a new mask when it has changed)."""
+    _fields_ = [("p", C.c_float), ("seed", C.c_uint64), ("call", C.c_uint32), ("step", C.c_void_p)]
+
+    def __init__(self, p, seed, call=0, step=None):
+        if step is not None:
+            if not step.is_cuda or step.dtype != torch.int32 or step.numel() != 1:
+                raise ValueError("dropout's step is a device int32 tensor of one element")
+            self.step_tensor = step
+            step = step.data_ptr()
+        super().__init__(p, seed & 0xFFFFFFFFFFFFFFFF, call, step)
 
 
 class SolError(RuntimeError):
@@ -83,6 +101,11 @@ def lib():
         # the calls that a program repeats: with their argument types known, plain integers are marshalled without wrapper objects
         vp, sz, i = C.c_void_p, C.c_size_t, C.c_int
         L.sol_conv2d_fused.argtypes = [C.POINTER(TensorDesc), vp, C.POINTER(ConvDesc), vp, vp, vp, vp, i, C.POINTER(PoolDesc), vp, vp, vp, vp]
+        for f in (L.sol_linear_fused_workspace_bytes, L.sol_linear_backward_workspace_bytes):
+            f.restype, f.argtypes = sz, [C.POINTER(LinearDesc)]
+        L.sol_linear_fused.argtypes = [C.POINTER(LinearDesc), vp, vp, vp, C.POINTER(Dropout), vp, vp, vp, vp, sz, vp]
+        L.sol_linear_backward.argtypes = [C.POINTER(LinearDesc), vp, vp, vp, vp, C.POINTER(Dropout), vp, vp, i, vp, vp, sz, vp]
+        L.sol_dropout.argtypes = [i, i, i, vp, C.POINTER(Dropout), vp, vp, vp]
         L.sol_network_forward.argtypes = [vp, vp, vp, vp, sz, vp]
         L.sol_network_backward.argtypes = [vp, vp, vp, vp, vp, sz, vp]
         L.sol_network_sgd_step.argtypes = [vp, C.c_float, C.c_float, vp]
@@ -281,6 +304,100 @@ def sol_linear(x, w_packed, bias, out_f, act=ACT_NONE, stream=None):
     y = torch.empty((m, out_f), dtype=x.dtype, device=x.device)
     _check(lib().sol_linear(C.c_int(m), C.c_int(in_f), C.c_int(out_f), C.c_int(dtype_of(x)), _ptr(x), _ptr(w_packed),
                             _ptr(bias), C.c_int(act), _ptr(y), _stream(stream)))
+    return y
+
+
+def _rows(t, cols, what, like=None):
+    """Address and pitch of a [rows][cols] device tensor whose rows are contiguous; `like`: what it has to match in rows, type and device."""
+    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{what}: rows of {cols} neighbouring elements are wanted, not a tensor of shape {tuple(t.shape)} and strides {t.stride()}")
+    if not t.is_cuda or t.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"{what}: a float32 or bfloat16 GPU tensor is wanted, not {t.dtype} on {t.device}")
+    if like is not None and (t.shape[0] != like.shape[0] or t.dtype != like.dtype or t.device != like.device):
+        raise ValueError(f"{what}: {t.shape[0]} rows of {t.dtype} on {t.device} do not go with {like.shape[0]} of {like.dtype} on {like.device}")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else cols
+
+
+def _dense(t, shape, what, like, dtype=None):
+    """Address of an optional dense device tensor of this shape, on `like`'s device and of its type (or dtype)."""
+    if t is None:
+        return 0
+    if tuple(t.shape) != shape or not t.is_contiguous() or t.dtype != (dtype or like.dtype) or t.device != like.device:
+        raise ValueError(f"{what}: a contiguous {dtype or like.dtype} tensor of shape {shape} on {like.device} is wanted, not {tuple(t.shape)} of {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _packed(w, in_f, out_f, x):
+    """Address of packed linear weights, checked for their size."""
+    block = 64 if x.dtype == torch.bfloat16 else 32
+    if w.device != x.device or not w.is_contiguous() or w.numel() * w.element_size() != out_f * ((in_f + block - 1) // block * block) * x.element_size():
+        raise ValueError(f"w_packed: [{out_f}][{in_f}] packed for {x.dtype} on {x.device} is wanted")
+    return w.data_ptr()
+
+
+def _scratch(workspace, need, x):
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    if workspace.device != x.device or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the operands' device is wanted")
+    return workspace
+
+
+def _on_current(x):
+    if x.get_device() != torch.cuda.current_device():
+        raise ValueError(f"tensors on {x.device}, but the current device is cuda:{torch.cuda.current_device()}: call under torch.cuda.device({x.get_device()})")
+
+
+def sol_linear_fused(x, w_packed, out_f, bias=None, act=ACT_NONE, drop=None, residual=None, want_preact=False, out=None, workspace=None, stream=None):
+    """y = dropout(act(z)) + residual, z = x W^T + bias.  x [m][in] with rows of any pitch; residual, out: [m][out_f] likewise (out may be residual);
+    drop: a Dropout.  Returns (y, z or None)."""
+    m, in_f = x.shape
+    xa, ldx = _rows(x, in_f, "x")
+    _on_current(x)
+    ra, ldr = _rows(residual, out_f, "residual", x) if residual is not None else (0, 0)
+    y = torch.empty((m, out_f), dtype=x.dtype, device=x.device) if out is None else out
+    ya, ldy = _rows(y, out_f, "out", x)
+    z = torch.empty((m, out_f), dtype=x.dtype, device=x.device) if want_preact else None
+    ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldy, ldr)
+    need = lib().sol_linear_fused_workspace_bytes(ld)
+    ws = _scratch(workspace, need, x)
+    _check(lib().sol_linear_fused(ld, xa, _packed(w_packed, in_f, out_f, x), _dense(bias, (out_f,), "bias", x, torch.float32), drop, ra, ya,
+                                  _addr(z), _addr(ws), ws.numel() * ws.element_size() if ws is not None else 0, _stream_handle(stream)))
+    return y, z
+
+
+def sol_linear_backward(dy, x, w_packed, preact=None, act=ACT_NONE, drop=None, need_dx=True, need_dw=True, need_db=True, dw_dtype=None, workspace=None,
+                        stream=None):
+    """Gradients of sol_linear_fused: dy [m][out] and x [m][in] with rows of any pitch; preact: the z that the forward call returned (not needed with
+    ACT_NONE); drop: the forward call's.  Returns (dx, dW [out][in] of x's type or dw_dtype, db in fp32), None for what is not needed.
+    The residual's gradient is dy."""
+    m, in_f = x.shape
+    out_f = dy.shape[1]
+    xa, ldx = _rows(x, in_f, "x")
+    _on_current(x)
+    ga, ldg = _rows(dy, out_f, "dy", x)
+    wdt = x.dtype if dw_dtype is None else dw_dtype
+    if wdt not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"dw_dtype: float32 or the layer's type is wanted, not {wdt}")
+    dx = torch.empty((m, in_f), dtype=x.dtype, device=x.device) if need_dx else None
+    dw = torch.empty((out_f, in_f), dtype=wdt, device=x.device) if need_dw else None
+    db = torch.empty(out_f, dtype=torch.float32, device=x.device) if need_db else None
+    ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldg, 0)
+    ws = _scratch(workspace, lib().sol_linear_backward_workspace_bytes(ld), x)
+    _check(lib().sol_linear_backward(ld, ga, xa, _packed(w_packed, in_f, out_f, x), _dense(preact, (m, out_f), "preact", x), drop, _addr(dx), _addr(dw),
+                                     BF16 if wdt == torch.bfloat16 else F32, _addr(db), _addr(ws), ws.numel() * ws.element_size() if ws is not None else 0, _stream_handle(stream)))
+    return dx, dw, db
+
+
+def sol_dropout(x, drop, residual=None, out=None, stream=None):
+    """y = dropout(x) + residual; x: contiguous, its last dimension the columns, all before it the rows; out may be x or residual.  Returns y."""
+    cols = x.shape[-1]
+    if x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda or not x.is_contiguous():
+        raise ValueError(f"x: a contiguous float32 or bfloat16 GPU tensor is wanted, not {x.dtype} on {x.device}")
+    _on_current(x)
+    y = torch.empty_like(x) if out is None else out
+    _check(lib().sol_dropout(x.numel() // cols if cols else 0, cols, dtype_of(x), x.data_ptr(), drop, _dense(residual, tuple(x.shape), "residual", x),
+                             _dense(y, tuple(x.shape), "out", x), _stream_handle(stream)))
     return y
 
 

@@ -1,0 +1,366 @@
+"""The linear layer with its epilogue, its backward pass, and dropout, through the public entry points against the 64-bit oracle.
+
+Two kinds of checks.  Whole numbers: inputs are small integers and dropout's factor is 2 (p = 1/2), so that every product and every sum below 2^24 is exact
+in fp32 whatever its order, and the outputs have to be EQUAL (for bf16 after one rounding of the exact value); this catches a single product
+too many or too few.  Real numbers: tolerances are counted in roundings (`half` = half a step of the output type, U = 2^-24 for a sum's additions).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import linear_ops as lo
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"f32": 2.0**-24, "bf16": 2.0**-8}      # half a step, relative
+U = 2.0**-24
+TDT = {"f32": torch.float32, "bf16": torch.bfloat16}
+DROP = (0.5, 0x123456789ABCDEF, 3, 41)          # p, seed, call, step
+
+
+@pytest.fixture(scope="module")
+def sol():
+    from paper_2003_10688_amd import sol as s
+
+    s.lib()
+    return s
+
+
+def dev(a, dt="f32", pitch=0, fill=float("nan")):
+    """Device tensor of a 2-d array; pitch: so many more columns per row, which hold `fill`."""
+    t = torch.from_numpy(np.ascontiguousarray(a, np.float32)).to("cuda:0", TDT[dt])
+    if not pitch:
+        return t
+    wide = torch.full((a.shape[0], a.shape[1] + pitch), fill, dtype=TDT[dt], device="cuda:0")
+    wide[:, :a.shape[1]] = t
+    return wide[:, :a.shape[1]]
+
+
+def host(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def pack(w, dt):
+    block = 64 if dt == "bf16" else 32
+    p = torch.zeros((w.shape[0], -(-w.shape[1] // block) * block), dtype=TDT[dt], device="cuda:0")
+    p[:, :w.shape[1]] = dev(w, dt)
+    return p
+
+
+def grid(a, dt):
+    """Values that dt holds exactly."""
+    return a if dt == "f32" and a.dtype == np.float32 else host(torch.from_numpy(np.asarray(a, np.float32)).to(TDT[dt]))
+
+
+def dropper(sol, drop):
+    if drop is None:
+        return None
+    p, seed, call, step = drop
+    return sol.Dropout(p, seed, call, torch.tensor([step], dtype=torch.int32, device="cuda:0"))
+
+
+def act_id(sol, name):
+    return {n: i for i, n in enumerate(lo.ACTS)}[name]
+
+
+SHAPES = [
+    # rows, in, out                    what it reaches
+    (1, 1, 1),
+    (1, 8, 8), (3, 5, 7),
+    (2, 64, 64), (16, 100, 33),
+    (17, 2048, 1000),                  # a classifier
+    (65, 72, 130), (64, 96, 513),      # tiles of 64 with remainders
+    (129, 250, 65), (200, 1531, 257),  # odd rows
+    (33, 4096, 40),                    # a long reduction, few tiles
+    (777, 33, 1030),                   # tiles of 128 and more
+    (2050, 40, 1700),
+    (2600, 72, 5130),                  # the largest tiles, with remainders
+    (5121, 136, 2570),
+]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n_in,n_out", SHAPES)
+def test_whole_numbers(sol, dt, rows, n_in, n_out):
+    """Forward and backward, equal to the last bit: every product and sum is a whole number below 2^24."""
+    rng = np.random.default_rng([rows, n_in, n_out])
+    ints = lambda *s: rng.integers(-2, 3, s).astype(np.float32)  # noqa: E731
+    x, w, b, r, g = ints(rows, n_in), ints(n_out, n_in), ints(n_out), ints(rows, n_out), ints(rows, n_out)
+    pitch = (rows * 7 + n_in) % 3 * 8 + (5 if rows % 2 else 0)
+    xd, wd = dev(x, dt, pitch), pack(w, dt)
+    for act, drop, res in (("none", None, None), ("relu", DROP, r), ("relu", None, None), ("none", DROP, r)):
+        y, z = sol.sol_linear_fused(xd, wd, n_out, bias=dev(b[None])[0], act=act_id(sol, act), drop=dropper(sol, drop),
+                                    residual=dev(res, dt, pitch) if res is not None else None, want_preact=True)
+        want, wz = lo.linear_fused(x, w, b, act, drop, res)
+        assert np.array_equal(host(z), grid(wz, dt)) and np.array_equal(host(y), grid(want, dt))
+        zq = grid(wz, dt)
+        dx, dw, db = sol.sol_linear_backward(dev(g, dt, pitch), xd, wd, preact=z, act=act_id(sol, act), drop=dropper(sol, drop))
+        wdx, wdw, wdb, _ = lo.linear_fused_bwd(g, x, w, zq, act, drop)
+        assert np.array_equal(host(dx), grid(wdx, dt)) and np.array_equal(host(dw), grid(wdw, dt)) and np.array_equal(host(db), wdb)
+        if dt == "bf16":
+            _, dw32, _ = sol.sol_linear_backward(dev(g, dt), xd, wd, preact=z, act=act_id(sol, act), drop=dropper(sol, drop), need_dx=False, need_db=False, dw_dtype=torch.float32)
+            assert np.array_equal(host(dw32), wdw)
+
+
+def close(got, want, tol, what):
+    bad = np.abs(got - want) - tol
+    assert np.all(np.isfinite(got)) and bad.max() <= 0, f"{what}: off by {np.abs(got - want).flat[bad.argmax()]:.3g}, {tol.flat[bad.argmax()]:.3g} allowed, at {np.unravel_index(bad.argmax(), bad.shape)}"
+
+
+# Roundings of an activation in fp32 (exp2 and the reciprocal: 1 ulp each; the tail's fit 1.5e-7; about ten operations): relative to |z| and slope's size
+ACT_ERR = 3e-6
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("act", lo.ACTS)
+@pytest.mark.parametrize("rows,n_in,n_out,p", [(5, 40, 24, 0.1), (130, 777, 201, 0.25), (300, 512, 1100, 0.0), (2600, 64, 5130, 0.1)])
+def test_real_numbers(sol, dt, act, rows, n_in, n_out, p):
+    rng = np.random.default_rng([rows, n_in, n_out, len(act)])
+    x, w = grid(rng.standard_normal((rows, n_in)), dt), grid(rng.standard_normal((n_out, n_in)) * (2 / np.sqrt(n_in)), dt)
+    b, r, g = rng.standard_normal(n_out).astype(np.float32), grid(rng.standard_normal((rows, n_out)), dt), grid(rng.standard_normal((rows, n_out)), dt)
+    drop = (p, 99 + (7 << 40), 1, 0) if p else None
+    y, z = sol.sol_linear_fused(dev(x, dt), pack(w, dt), n_out, bias=dev(b[None])[0], act=act_id(sol, act), drop=dropper(sol, drop), residual=dev(r, dt), want_preact=True)
+    want, wz = lo.linear_fused(x, w, b, act, drop, r)
+    half, scale = HALF[dt], 1 / (1 - p) * 1.001
+    # a sum of n products: at most n + 1 additions, each off by U of the partial sum, which is at most the sum of magnitudes
+    zerr = (n_in + 2) * U * (np.abs(x) @ np.abs(w).T + np.abs(b))
+    close(host(z), wz, half * np.abs(wz) * 1.01 + zerr, "z")
+    # |act'| <= 1.13; then dropout's factor, the residual's addition and the output's rounding
+    close(host(y), want, half * np.abs(want) * 1.01 + scale * (1.13 * zerr + ACT_ERR * np.abs(wz)) + 4 * U * (np.abs(want) + np.abs(r)), "y")
+
+    zq = host(z)
+    dx, dw, db = sol.sol_linear_backward(dev(g, dt), dev(x, dt), pack(w, dt), preact=z, act=act_id(sol, act), drop=dropper(sol, drop))
+    wdx, wdw, wdb, wdz = lo.linear_fused_bwd(g, x, w, zq, act, drop)
+    gz = lo.dropout(np.abs(g), *drop) if drop else np.abs(g)
+    edz = ACT_ERR * 2 * gz                                    # of dz before it is rounded: slopes are at most 1.13
+    rdz = half * np.abs(wdz) * 1.01 + edz if dt == "bf16" else edz      # bf16: as the products take it
+    close(host(dx), wdx, half * np.abs(wdx) * 1.01 + rdz @ np.abs(w) + (n_out + 2) * U * (np.abs(wdz) @ np.abs(w)), "dx")
+    close(host(dw), wdw, half * np.abs(wdw) * 1.01 + rdz.T @ np.abs(x) + (rows + 20) * U * (np.abs(wdz).T @ np.abs(x)), "dW")
+    close(host(db), wdb, edz.sum(0) + (rows + 20) * U * np.abs(wdz).sum(0), "db")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,p", [(1, 1, 0.5), (1, 2048, 0.1), (3, 7, 0.25), (64, 2048, 0.5), (129, 1001, 0.1), (5, 13, 1.0), (5, 13, 0.0), (1000, 257, 0.999)])
+def test_dropout(sol, dt, rows, cols, p):
+    rng = np.random.default_rng([rows, cols])
+    x, r = grid(rng.standard_normal((rows, cols)), dt), grid(rng.standard_normal((rows, cols)), dt)
+    drop = (p, 2**63 + 12345, 2**32 - 1, -2)                  # the step word's bits are what counts
+    t = (p, 2**63 + 12345, 2**32 - 1, 2**32 - 2)
+    for res in (None, r):
+        want = lo.dropout(x, *t) + (0 if res is None else res)
+        got = host(sol.sol_dropout(dev(x, dt), dropper(sol, drop), residual=None if res is None else dev(res, dt)))
+        # the factor and the product round once each, the sum and the output once each
+        close(got, want, HALF[dt] * np.abs(want) * 1.01 + 4 * U * (np.abs(lo.dropout(x, *t)) + np.abs(want)), "y")
+        if res is None:
+            assert np.array_equal(got == 0, (want == 0))
+    a = dev(x, dt)
+    b = a.clone()
+    want = sol.sol_dropout(a, dropper(sol, drop), residual=dev(r, dt))
+    assert torch.equal(sol.sol_dropout(b, dropper(sol, drop), residual=dev(r, dt), out=b), want) and torch.equal(b, want)   # in place
+
+
+def test_dropout_masks_agree(sol):
+    """The product's epilogue, its backward pass and the pass on its own drop the same elements, whatever the pitches."""
+    rows, n_in, n_out = 77, 64, 203
+    x, w = torch.ones((rows, n_in), device="cuda:0", dtype=torch.bfloat16), pack(np.ones((n_out, n_in)), "bf16")
+    d = dropper(sol, (0.3, 5, 9, 1))
+    y, _ = sol.sol_linear_fused(x, w, n_out, drop=d, out=torch.empty((rows, n_out + 5), device="cuda:0", dtype=torch.bfloat16)[:, :n_out])
+    alone = sol.sol_dropout(torch.ones((rows, n_out), device="cuda:0"), d)
+    assert torch.equal(y != 0, alone != 0)
+    _, dw, db = sol.sol_linear_backward(torch.ones((rows, n_out), device="cuda:0", dtype=torch.bfloat16), x, w, drop=d, need_dx=False, dw_dtype=torch.float32)
+    kept = (alone != 0).float().sum(0)
+    scale = 65536 / (65536 - round(0.3 * 65536))
+    # dz = the factor, rounded to bf16, in every kept place
+    assert torch.equal(dw[:, 0], kept * float(torch.tensor(scale).to(torch.bfloat16))) and torch.allclose(db, kept * scale, rtol=77 * U)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(1, 72, 24), (70, 40, 90), (70, 41, 90), (300, 200, 700)])
+def test_what_lies_between_rows(sol, dt, rows, n_in, n_out):
+    """Gaps of NaN beside x, dy and the residual do not reach a result, and the gaps of y stay as they were."""
+    rng = np.random.default_rng(rows)
+    x, w, r = rng.integers(-2, 3, (rows, n_in)), rng.integers(-2, 3, (n_out, n_in)), rng.integers(-2, 3, (rows, n_out))
+    for pitch in (3, 8, 64):
+        out = torch.full((rows, n_out + pitch), 7.0, dtype=TDT[dt], device="cuda:0")
+        sol.sol_linear_fused(dev(x, dt, pitch), pack(w, dt), n_out, residual=dev(r, dt, pitch), out=out[:, :n_out])
+        assert np.array_equal(host(out[:, :n_out]), grid(lo.linear_fused(x, w, residual=r)[0], dt)) and torch.all(out[:, n_out:] == 7)
+        dx, dw, db = sol.sol_linear_backward(dev(r, dt, pitch), dev(x, dt, pitch), pack(w, dt))
+        want = lo.linear_fused_bwd(r, x, w, None)
+        assert np.array_equal(host(dx), grid(want[0], dt)) and np.array_equal(host(dw), grid(want[1], dt)) and np.array_equal(host(db), want[2])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(9, 40, 30), (140, 72, 200)])
+def test_rows_that_are_not_finite(sol, dt, rows, n_in, n_out):
+    """An infinity or a NaN in one row of x stays in that row of y and dx; dropped places are 0 even there; activations take their limits."""
+    rng = np.random.default_rng(2)
+    x, w = rng.integers(1, 3, (rows, n_in)).astype(np.float32), rng.integers(1, 3, (n_out, n_in)).astype(np.float32)
+    x[2, 3], x[4, 0], x[5, n_in - 1] = np.inf, np.nan, -np.inf
+    for act in lo.ACTS:
+        y, z = sol.sol_linear_fused(dev(x, dt), pack(w, dt), n_out, act=act_id(sol, act), want_preact=True)
+        y, z = host(y), host(z)
+        fine = np.delete(np.arange(rows), [2, 4, 5])
+        assert np.all(np.isfinite(y[fine])) and np.all(z[2] == np.inf) and np.all(z[5] == -np.inf) and np.all(np.isnan(z[4]))
+        assert np.all(y[2] == np.inf) and (np.all(y[4] == 0) if act == "relu" else np.all(np.isnan(y[4])))
+        assert np.all(y[5] == -np.inf) if act == "none" else np.all(np.abs(y[5]) < 1e-30)
+        g = np.ones((rows, n_out), np.float32)
+        zt = dev(np.where(np.isnan(z), 0, z), dt)
+        dx, _, db = sol.sol_linear_backward(dev(g, dt), dev(np.where(np.isfinite(x), x, 0), dt), pack(w, dt), preact=zt, act=act_id(sol, act))
+        assert np.all(np.isfinite(host(dx))) and np.all(np.isfinite(host(db)))          # slopes of infinite z are 0 and 1
+        assert np.all(host(dx)[5] == (host(dx)[0] if act == "none" else 0))
+    d = dropper(sol, DROP)
+    y, _ = sol.sol_linear_fused(dev(x, dt), pack(w, dt), n_out, drop=d)
+    kept = lo.dropout_kept(rows, n_out, *DROP)
+    assert np.all(host(y)[~kept] == 0) and np.all(np.isnan(host(y)[4][kept[4]]))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_equal_rows_equal_bits_and_repeats(sol, dt):
+    """A call repeated gives the same bits, for every output."""
+    rng = np.random.default_rng(8)
+    x, w, g = dev(rng.standard_normal((333, 520)), dt), pack(rng.standard_normal((410, 520)), dt), dev(rng.standard_normal((333, 410)), dt)
+    d = dropper(sol, (0.1, 3, 0, 0))
+    first = None
+    for _ in range(3):
+        y, z = sol.sol_linear_fused(x, w, 410, act=sol.ACT_GELU, drop=d, want_preact=True)
+        got = (y, z) + sol.sol_linear_backward(g, x, w, preact=z, act=sol.ACT_GELU, drop=d)
+        assert first is None or all(torch.equal(a, b) for a, b in zip(first, got))
+        first = got
+
+
+def block_forward(sol, x, w1, b1, w2, b2, hidden, d1, d2):
+    """A feed-forward block with a residual: x + dropout(W2 dropout(gelu(W1 x + b1)) + b2)."""
+    h, z = sol.sol_linear_fused(x, w1, hidden, bias=b1, act=sol.ACT_GELU, drop=d1, want_preact=True)
+    y, _ = sol.sol_linear_fused(h, w2, x.shape[1], bias=b2, drop=d2, residual=x)
+    return y, h, z
+
+
+def block_backward(sol, g, x, h, z, w1, w2, d1, d2):
+    dh, dw2, db2 = sol.sol_linear_backward(g, h, w2, drop=d2)
+    dx, dw1, db1 = sol.sol_linear_backward(dh, x, w1, preact=z, act=sol.ACT_GELU, drop=d1)
+    return dx + g, dw1, db1, dw2, db2
+
+
+def block_inputs(dt, rows, width, hidden, seed=1):
+    rng = np.random.default_rng(seed)
+    a = {"x": rng.standard_normal((rows, width)), "w1": rng.standard_normal((hidden, width)) / np.sqrt(width), "w2": rng.standard_normal((width, hidden)) / np.sqrt(hidden),
+         "g": rng.standard_normal((rows, width))}
+    a = {k: grid(v, dt) for k, v in a.items()}
+    a["b1"], a["b2"] = rng.standard_normal(hidden).astype(np.float32), rng.standard_normal(width).astype(np.float32)
+    return a
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,width,hidden", [(50, 96, 384), (257, 200, 801)])
+def test_block_against_the_oracle(sol, dt, rows, width, hidden):
+    """The operators as they are used together.  Each step adds its own roundings; relative 2-norms: bf16 rounds h, y, dh, dz and the outputs (five times
+    2^-8 / sqrt(3) at most, added up), fp32 sums of up to 801 products."""
+    a = block_inputs(dt, rows, width, hidden)
+    s1, s2 = (0.1, 77, 0, 6), (0.2, 77, 1, 6)
+    h, z = lo.linear_fused(a["x"], a["w1"], a["b1"], "gelu", s1)
+    y, _ = lo.linear_fused(h, a["w2"], a["b2"], "none", s2, a["x"])
+    dh, dw2, db2, _ = lo.linear_fused_bwd(a["g"], h, a["w2"], None, "none", s2)
+    dx, dw1, db1, _ = lo.linear_fused_bwd(dh, a["x"], a["w1"], z, "gelu", s1)
+    x, w1, w2, g = dev(a["x"], dt), pack(a["w1"], dt), pack(a["w2"], dt), dev(a["g"], dt)
+    d1, d2 = dropper(sol, s1), dropper(sol, s2)
+    gy, gh, gz = block_forward(sol, x, w1, dev(a["b1"][None])[0], w2, dev(a["b2"][None])[0], hidden, d1, d2)
+    got = (gy,) + block_backward(sol, g, x, gh, gz, w1, w2, d1, d2)
+    tol = 5 * HALF["bf16"] / np.sqrt(3) if dt == "bf16" else 1e-5
+    for name, v, want in zip(("y", "dx", "dw1", "db1", "dw2", "db2"), got, (y, dx + a["g"], dw1, db1, dw2, db2)):
+        assert np.linalg.norm(host(v) - want) <= tol * np.linalg.norm(want), name
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "gelu_tanh", "silu"])
+def test_gradients_are_differences(sol, act):
+    """Directional derivatives in fp32 by central differences of the kernels' own forward pass."""
+    rng = np.random.default_rng(4)
+    rows, n_in, n_out = 40, 36, 52
+    x, w, b, g = rng.standard_normal((rows, n_in)), rng.standard_normal((n_out, n_in)) / 6, rng.standard_normal(n_out), rng.standard_normal((rows, n_out))
+    d, act = dropper(sol, (0.25, 11, 0, 0)), act_id(sol, act)
+    out = lambda x_, w_, b_: host(sol.sol_linear_fused(dev(x_), pack(w_, "f32"), n_out, bias=dev(b_[None])[0], act=act, drop=d)[0])  # noqa: E731
+    z = sol.sol_linear_fused(dev(x), pack(w, "f32"), n_out, bias=dev(b[None])[0], act=act, want_preact=True)[1]
+    grads = [host(t) for t in sol.sol_linear_backward(dev(g), dev(x), pack(w, "f32"), preact=z, act=act, drop=d)]
+    for i, t in enumerate((x, w, b)):
+        u = rng.standard_normal(t.shape)
+        h = 2.0**-7
+        up, down = [x, w, b], [x, w, b]
+        up[i], down[i] = t + h * u, t - h * u
+        slope = float(((out(*up) - out(*down)) * g).sum()) / (2 * h)
+        want = float((grads[i] * u).sum())
+        # h^2 / 6 of a third derivative of order one along a step of unit size per element, and fp32 roundings over 2h
+        assert abs(slope - want) <= 1e-3 * np.linalg.norm(grads[i]) * np.linalg.norm(u), (i, slope, want)
+
+
+def test_another_stream_and_caller_workspace(sol):
+    rng = np.random.default_rng(6)
+    x, w, g = dev(rng.standard_normal((100, 77)), "bf16"), pack(rng.standard_normal((90, 77)), "bf16"), dev(rng.standard_normal((100, 90)), "bf16")
+    d = dropper(sol, (0.1, 3, 0, 0))
+    y, z = sol.sol_linear_fused(x, w, 90, act=sol.ACT_SILU, drop=d, want_preact=True)
+    want = (y, z) + sol.sol_linear_backward(g, x, w, preact=z, act=sol.ACT_SILU, drop=d) + (sol.sol_dropout(g, d),)
+    torch.cuda.synchronize()
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device="cuda:0")
+    st = torch.cuda.Stream()
+    y, z2 = sol.sol_linear_fused(x, w, 90, act=sol.ACT_SILU, drop=d, want_preact=True, workspace=ws, stream=st)
+    got = (y, z2) + sol.sol_linear_backward(g, x, w, preact=z2, act=sol.ACT_SILU, drop=d, workspace=ws, stream=st) + (sol.sol_dropout(g, d, stream=st),)
+    st.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    with pytest.raises(sol.SolError) as e:
+        sol.sol_linear_backward(g, x, w, preact=z, act=sol.ACT_SILU, workspace=ws[:1024])
+    assert e.value.status == 5
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_captured_and_replayed(sol, dt):
+    """A captured training step of the block; the step word changes between the replays, and so do the masks."""
+    a = block_inputs(dt, 130, 72, 288, seed=5)
+    x, w1, w2, g = dev(a["x"], dt), pack(a["w1"], dt), pack(a["w2"], dt), dev(a["g"], dt)
+    b1, b2 = dev(a["b1"][None])[0], dev(a["b2"][None])[0]
+    step = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    d1, d2 = sol.Dropout(0.1, 5, 0, step), sol.Dropout(0.2, 5, 1, step)
+
+    def run():
+        y, h, z = block_forward(sol, x, w1, b1, w2, b2, 288, d1, d2)
+        return (y,) + block_backward(sol, g, x, h, z, w1, w2, d1, d2)
+
+    run()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = run()
+    last = None
+    for i in (0, 3, 3, 9):
+        step.fill_(i)
+        want = [t.clone() for t in run()]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(want, out)), i
+        assert last is None or torch.equal(last[1], want[0]) == (last[0] == i)
+        last = (i, want[0])
+
+
+def test_no_rows(sol):
+    x = torch.empty((0, 24), device="cuda:0")
+    w = pack(np.ones((16, 24)), "f32")
+    y, z = sol.sol_linear_fused(x, w, 16, want_preact=True)
+    assert y.shape == (0, 16) and z.shape == (0, 16)
+    dx, dw, db = sol.sol_linear_backward(torch.empty((0, 16), device="cuda:0"), x, w)
+    assert dx.shape == (0, 24) and not dw.any() and not db.any()
+    assert sol.sol_dropout(torch.empty((0, 16), device="cuda:0"), sol.Dropout(0.5, 1)).shape == (0, 16)
+
+
+def test_refusals_of_the_binding(sol):
+    x, w = torch.zeros((4, 32), device="cuda:0"), pack(np.ones((8, 32)), "f32")
+    bad = [lambda: sol.sol_linear_fused(x.t(), w, 8), lambda: sol.sol_linear_fused(x.double(), w, 8), lambda: sol.sol_linear_fused(x, w[:7], 8),
+           lambda: sol.sol_linear_fused(x, w, 8, bias=torch.zeros(7, device="cuda:0")), lambda: sol.sol_linear_fused(x, w, 8, bias=torch.zeros(8, device="cuda:0", dtype=torch.bfloat16)),
+           lambda: sol.sol_linear_fused(x, w, 8, residual=torch.zeros((3, 8), device="cuda:0")), lambda: sol.sol_linear_fused(x, w, 8, out=torch.zeros((4, 8), device="cuda:0", dtype=torch.bfloat16)),
+           lambda: sol.sol_linear_backward(torch.zeros((5, 8), device="cuda:0"), x, w), lambda: sol.sol_linear_backward(torch.zeros((4, 8), device="cuda:0"), x, w, dw_dtype=torch.float16),
+           lambda: sol.sol_linear_backward(torch.zeros((4, 8), device="cuda:0"), x, w, preact=torch.zeros((4, 9), device="cuda:0")),
+           lambda: sol.sol_dropout(x.t(), sol.Dropout(0.5, 1)), lambda: sol.sol_dropout(x, sol.Dropout(0.5, 1), residual=torch.zeros(4, device="cuda:0")),
+           lambda: sol.sol_dropout(x.half(), sol.Dropout(0.5, 1))]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} was not refused")
+    with pytest.raises(sol.SolError) as e:
+        sol.sol_linear_backward(torch.zeros((4, 8), device="cuda:0"), x, w, act=sol.ACT_GELU)     # no preact
+    assert e.value.status == 1

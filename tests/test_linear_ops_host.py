@@ -1,0 +1,160 @@
+"""The linear layer's operators and dropout without a GPU: the oracle's own pins (published numbers, differences), and every refusal of the C ABI and
+of the binding, which come before anything is launched."""
+import ctypes as C
+import os
+
+import numpy as np
+import pytest
+
+from oracle import linear_ops as lo
+
+FAKE, NULL = 0x1000, 0          # never dereferenced: validation fails first
+
+
+@pytest.fixture(scope="module")
+def sol():
+    from paper_2003_10688_amd import sol as s
+
+    if not os.path.exists(s.LIB_PATH):
+        from paper_2003_10688_amd import build
+
+        build.build(verbose=False)
+    s.lib()
+    return s
+
+
+def test_philox_known_answers():
+    """The generator's published test vectors (10 rounds)."""
+    got = lo.philox4x32(np.array([[0, 0, 0, 0]]), (0, 0))[0]
+    assert [int(v) for v in got] == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
+    f = 0xFFFFFFFF
+    got = lo.philox4x32(np.array([[f, f, f, f]]), (f, f))[0]
+    assert [int(v) for v in got] == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
+    got = lo.philox4x32(np.array([[0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344]]), (0xA4093822, 0x299F31D0))[0]
+    assert [int(v) for v in got] == [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1]
+
+
+@pytest.mark.parametrize("p", [0.1, 0.5, 0.9])
+def test_kept_share_and_independence(p):
+    """Shares of 2^20 elements within five standard deviations; other calls, steps and seeds give other masks."""
+    a = lo.dropout_kept(1024, 1024, p, 7)
+    sd = np.sqrt(p * (1 - p) / a.size)
+    assert abs(a.mean() - (1 - p)) <= 5 * sd + 2.0**-17
+    for other in (lo.dropout_kept(1024, 1024, p, 7, call=1), lo.dropout_kept(1024, 1024, p, 7, step=1), lo.dropout_kept(1024, 1024, p, 7 + (1 << 32))):
+        same = (a == other).mean()                       # of two independent masks: p^2 + (1 - p)^2
+        q = p * p + (1 - p) ** 2
+        assert abs(same - q) <= 5 * np.sqrt(q * (1 - q) / a.size) + 2.0**-16
+
+
+@pytest.mark.parametrize("name", lo.ACTS)
+def test_slopes_are_differences(name):
+    z = np.linspace(-6, 6, 241) + 0.0125                 # not at ReLU's corner
+    h = 1e-5
+    assert np.allclose(lo.slope(name, z), (lo.act(name, z + h) - lo.act(name, z - h)) / (2 * h), atol=1e-9)
+
+
+@pytest.mark.parametrize("name", lo.ACTS)
+def test_oracle_gradients_are_differences(name):
+    rng = np.random.default_rng(3)
+    x, w, b, r, g = rng.standard_normal((5, 7)), rng.standard_normal((11, 7)), rng.standard_normal(11), rng.standard_normal((5, 11)), rng.standard_normal((5, 11))
+    drop = (0.3, 1234567890123, 5, 2)
+    loss = lambda x_, w_, b_: float((lo.linear_fused(x_, w_, b_, name, drop, r)[0] * g).sum())  # noqa: E731
+    z = lo.linear_fused(x, w, b, name, drop, r)[1]
+    for t, grad, at in ((x, 0, 0), (w, 1, 1), (b, 2, 2)):
+        want = lo.linear_fused_bwd(g, x, w, z, name, drop)[grad]
+        for idx in list(np.ndindex(t.shape))[::5]:
+            h = 1e-6
+            up, down = t.copy(), t.copy()
+            up[idx] += h
+            down[idx] -= h
+            args = lambda v: [v if i == at else a for i, a in enumerate((x, w, b))]  # noqa: E731
+            assert abs((loss(*args(up)) - loss(*args(down))) / (2 * h) - want[idx]) <= 1e-6
+
+
+def desc(sol, m=4, i=16, o=8, dtype=0, act=0, ldx=0, ldy=0, ldr=0):
+    return sol.LinearDesc(m, i, o, dtype, act, ldx, ldy, ldr)
+
+
+def forward(sol, ld, x=FAKE, w=FAKE, bias=NULL, drop=None, res=NULL, y=FAKE + 0x1000, pre=NULL, ws=NULL, nbytes=0):
+    return sol.lib().sol_linear_fused(ld, x, w if w != FAKE else 0x9000, bias, drop, res, y, pre, ws, nbytes, NULL)
+
+
+def backward(sol, ld, dy=FAKE, x=0x3000, w=0x9000, pre=0x5000, drop=None, dx=0x6000, dw=0x7000, dw_dt=0, db=0x8000, ws=0xA000, nbytes=1 << 40):
+    return sol.lib().sol_linear_backward(ld, dy, x, w, pre, drop, dx, dw, dw_dt, db, ws, nbytes, NULL)
+
+
+def test_forward_refusals(sol):
+    L = sol.lib()
+    assert forward(sol, None) == 1 and b"descriptor" in L.sol_last_error()
+    assert forward(sol, desc(sol), x=NULL) == 1 and forward(sol, desc(sol), y=NULL) == 1
+    assert L.sol_linear_fused(desc(sol), FAKE, NULL, NULL, None, NULL, 0x2000, NULL, NULL, 0, NULL) == 1
+    for bad in (dict(m=-1), dict(i=0), dict(o=0), dict(act=5), dict(act=-1), dict(ldx=15), dict(ldy=7), dict(ldr=7), dict(ldx=-16)):
+        assert forward(sol, desc(sol, **bad)) == 2, bad
+    assert forward(sol, desc(sol, dtype=2)) == 3
+    for bad in (dict(i=(1 << 20) + 1), dict(o=(1 << 20) + 1), dict(i=1 << 16, o=1 << 16), dict(ldx=(1 << 21) + 1), dict(m=1 << 20, ldx=1 << 11), dict(m=1 << 28)):
+        assert forward(sol, desc(sol, **bad)) == 6, bad
+    for bad in (dict(x=FAKE + 4), dict(w=0x9008), dict(bias=FAKE + 4), dict(res=FAKE + 2), dict(y=FAKE + 8), dict(pre=FAKE + 1)):
+        assert forward(sol, desc(sol), **bad) == 4, bad
+    assert forward(sol, desc(sol), y=FAKE) == 6                              # y on x
+    assert forward(sol, desc(sol), pre=FAKE + 0x1000) == 6                   # z on y
+    assert forward(sol, desc(sol, ldr=16), res=FAKE + 0x1000) == 6           # y on the residual, another pitch
+    odd = desc(sol, i=17)
+    need = L.sol_linear_fused_workspace_bytes(odd)
+    assert need >= 4 * 17 * 4
+    assert forward(sol, odd) == 5 and forward(sol, odd, ws=0xB000, nbytes=need - 1) == 5
+    assert forward(sol, odd, ws=NULL, nbytes=need) == 1 and forward(sol, odd, ws=0xB004, nbytes=need) == 4
+    assert L.sol_linear_fused_workspace_bytes(desc(sol)) == 0 and L.sol_linear_fused_workspace_bytes(desc(sol, m=-1)) == 0
+    assert forward(sol, desc(sol, m=0), x=NULL, y=NULL) == 0                 # nothing to do
+
+
+def test_backward_refusals(sol):
+    L = sol.lib()
+    assert backward(sol, None) == 1 and backward(sol, desc(sol), dy=NULL) == 1
+    assert backward(sol, desc(sol), x=NULL) == 1 and backward(sol, desc(sol), w=NULL) == 1
+    assert backward(sol, desc(sol, act=2), pre=NULL) == 1
+    assert backward(sol, desc(sol), dw_dt=1) == 3                            # a bf16 gradient of fp32 weights
+    assert backward(sol, desc(sol, act=9)) == 2 and backward(sol, desc(sol, ldy=3)) == 2
+    for bad in (dict(dy=FAKE + 4), dict(x=0x3002), dict(w=0x9004), dict(pre=0x5004), dict(dx=0x6008), dict(dw=0x7004), dict(db=0x8004), dict(ws=0xA008)):
+        assert backward(sol, desc(sol), **bad) == 4, bad
+    for bad in (dict(dx=FAKE), dict(dw=0x9000), dict(dx=0x5000), dict(dx=0x3000), dict(dw=0x6000), dict(db=0x7000)):
+        assert backward(sol, desc(sol), **bad) == 6, bad
+    need = L.sol_linear_backward_workspace_bytes(desc(sol, act=2))
+    assert need >= 4 * 8 * 4 and backward(sol, desc(sol, act=2), nbytes=need - 1) == 5
+    assert backward(sol, desc(sol, act=2), ws=NULL, nbytes=need) == 1
+
+
+def test_dropout_refusals(sol):
+    L = sol.lib()
+    ok = sol.Dropout(0.5, 1)
+    call = lambda rows=4, cols=8, dt=0, x=FAKE, d=ok, res=NULL, y=FAKE: L.sol_dropout(rows, cols, dt, x, d, res, y, NULL)  # noqa: E731
+    assert call(rows=-1) == 2 and call(cols=0) == 2 and call(dt=3) == 3 and call(rows=1 << 20, cols=1 << 12) == 6
+    assert call(d=None) == 1 and call(x=NULL) == 1 and call(y=NULL) == 1
+    assert call(x=FAKE + 4) == 4 and call(res=FAKE + 2) == 4 and call(y=FAKE + 8) == 4
+    for p in (-0.1, 1.5, float("nan"), float("inf")):
+        assert call(d=sol.Dropout(p, 1)) == 2, p
+        assert forward(sol, desc(sol), drop=sol.Dropout(p, 1)) == 2 and backward(sol, desc(sol), drop=sol.Dropout(p, 1)) == 2
+    bad = sol.Dropout(0.5, 1)
+    bad.step = 0x1002
+    assert call(d=bad) == 4
+    assert call(rows=0, x=NULL, y=NULL) == 0
+
+
+def test_other_calls_refuse_the_new_activations(sol):
+    xd, cd = sol.TensorDesc(1, 8, 8, 16, sol.F32), sol.ConvDesc(8, 16, 3, 3, 1, 1, 1, 1)
+    for act in (sol.ACT_GELU, sol.ACT_GELU_TANH, sol.ACT_SILU):
+        assert sol.lib().sol_conv2d_fused(xd, FAKE, cd, FAKE, NULL, NULL, NULL, act, None, FAKE, NULL, NULL, NULL) == 2
+        assert sol.lib().sol_linear(4, 16, 8, 0, C.c_void_p(FAKE), C.c_void_p(FAKE), C.c_void_p(0), act, C.c_void_p(FAKE), C.c_void_p(0)) == 2
+
+
+def test_binding_refuses_what_is_not_on_the_gpu(sol):
+    import torch
+
+    x, w = torch.zeros(4, 32), torch.zeros(8, 32)
+    with pytest.raises(ValueError):
+        sol.sol_linear_fused(x, w, 8)
+    with pytest.raises(ValueError):
+        sol.sol_linear_backward(torch.zeros(4, 8), x, w)
+    with pytest.raises(ValueError):
+        sol.sol_dropout(x, sol.Dropout(0.5, 1))
+    with pytest.raises(ValueError):
+        sol.Dropout(0.5, 1, step=torch.zeros(1, dtype=torch.int32))
