@@ -49,13 +49,13 @@ sol_status check_linear(const sol_linear_desc *ld, sol_linear_desc *l) {
 int pack_pitch(int n, int dt) { return (int)round_up((size_t)n, dt == SOL_BF16 ? 64 : 32); }
 // rows that DMA can take as they are: they start and end at multiples of 16 bytes
 bool rows_aligned(int ld, int cols, int dt) { return (ld * dtype_size(dt)) % 16 == 0 && (cols * dtype_size(dt)) % 16 == 0; }
-bool cut_needed(int k, int dt) { return (k * dtype_size(dt)) % 64 != 0; }
+bool cut_needed(int k, int dt) { return (k * dtype_size(dt)) % 128 != 0; }
 
-// Parts of a reduction of K, so that a product of few tiles fills the GPU: about one workgroup per CU, each with eight stages or more.
+// Parts of a reduction of K, so that a product of few tiles fills the GPU: about one workgroup per CU, each with four stages or more.
 int split_of(int M, int N, int K, int dt) {
-    const long tiles = (long)ceil_div(M, 64) * ceil_div(N, 64), stages = ceil_div(K, 64 / (int)dtype_size(dt));
+    const long tiles = (long)ceil_div(M, 64) * ceil_div(N, 64), stages = ceil_div(K, 128 / (int)dtype_size(dt));
     if (tiles >= 192) return 1;
-    return (int)max(1l, min(min(256 / tiles, stages / 8), 16l));
+    return (int)max(1l, min(min(256 / tiles, stages / 4), 16l));
 }
 
 struct ForwardPlan {

@@ -4,9 +4,9 @@
 //   dx       = dz W        A = dz [m][out]  along k    B = W  [out][in]  across k
 //   dW       = dz^T x      A = dz [m][out]  across k   B = x  [m][in]    across k
 //
-// One kernel for the three.  Four waves share a tile of rows x columns; stages of 64 bytes of reduction per row (32 bf16, 16 fp32)
-// travel memory -> LDS by DMA through a ring of NS stages, each wave multiplies its quarter with 32x32 matrix instructions.
-// An operand along k lies in LDS as rows of 64 bytes, read as 16-byte fragments; one across k lies as it is in memory, rows of
+// Four waves share a tile of rows x columns; stages of 128 bytes of reduction per row (64 bf16, 32 fp32) travel memory -> LDS by DMA
+// through a ring, each wave multiplies its quarter with 32x32 matrix instructions.
+// An operand along k lies in LDS as rows of 128 bytes, read as 16-byte fragments; one across k lies as it is in memory, rows of
 // columns, and is transposed on the way to registers (ds_read_b64_tr_b16 for bf16, four 4-byte reads for fp32), so no transposed copy of W, dz or x is
 // ever made.  Slots are permuted on the global side of the DMA so that neither kind of read meets a bank twice.
 //
@@ -20,6 +20,9 @@ namespace sol {
 using namespace lds_pipe;
 
 typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+
+// All but the last N LDS reads have landed (they land in order; the counter has four bits, and waiting for more than needed is right too).
+template <int N> __device__ __forceinline__ void wait_lds() { wait_lgkmcnt<(N < 15 ? N : 15)>(); }
 
 // One fragment: 16 bytes of reduction of one row or column per lane.  bf16 across k arrives in two halves.
 template <typename T, bool ACROSS> struct Frag;
@@ -54,10 +57,12 @@ template <> struct Frag<float, true> {
     static constexpr int READS = 4;
 };
 
-// Where one operand's tile lies: BR rows (or columns) of the product, 64 bytes of reduction.
+constexpr int ROWB = 128;       // bytes of reduction of a stage: whole cache lines (with 64 every line came from L2 twice: 200 against 100 million requests)
+
+// Where BR rows (or columns) of an operand lie in LDS and in memory, one stage of them.
 template <typename T, bool ACROSS, int BR> struct Tile {
-    static constexpr int ES = (int)sizeof(T), BK = 64 / ES, RB = ACROSS ? BR * ES : 64;     // bytes of a row in LDS
-    static constexpr int BYTES = BR * 64, SEGS = BYTES / 1024;                              // DMA instructions of 64 lanes x 16 bytes
+    static constexpr int ES = (int)sizeof(T), BK = ROWB / ES, RB = ACROSS ? BR * ES : ROWB;     // bytes of a row in LDS
+    static constexpr int BYTES = BR * ROWB, SEGS = BYTES / 1024;                                // DMA instructions of 64 lanes x 16 bytes
 
     // permutation of the 16-byte slots of a row across k: transposing reads take 64 bytes of four neighbouring rows at once, 4-byte reads
     // 128 bytes of rows k and k + 4
@@ -71,15 +76,17 @@ template <typename T, bool ACROSS, int BR> struct Tile {
             const int at = seg * 1024 + lane * 16, k = at / RB, slot = (at % RB) / 16;
             return (unsigned)k * pitch + (unsigned)((slot ^ permute(k)) << 4);
         } else {
-            const int row = seg * 16 + (lane >> 2);
-            return (unsigned)row * pitch + (unsigned)(((lane & 3) ^ swz<64>(row)) << 4);
+            const int row = seg * 8 + (lane >> 3);
+            return (unsigned)row * pitch + (unsigned)(((lane & 7) ^ swz<ROWB>(row)) << 4);
         }
     }
+    // along k: whether what that instruction brings of the last stage lies behind `bytes` of it
+    static __device__ __forceinline__ bool behind(int seg, int lane, int bytes) { return (((lane & 7) ^ swz<ROWB>(seg * 8 + (lane >> 3))) << 4) >= bytes; }
     // LDS offset of this lane's fragment of the first k-step for the 32-wide block `blk`
     static __device__ __forceinline__ unsigned frag(int blk, int lane) {
         const int lr = lane & 31, lh = lane >> 5;
         if constexpr (!ACROSS) {
-            return (unsigned)((blk * 32 + lr) * 64 + ((lh ^ swz<64>(lr)) << 4));
+            return (unsigned)((blk * 32 + lr) * ROWB + ((lh ^ swz<ROWB>(lr)) << 4));
         } else if constexpr (ES == 2) {
             const int s = lane & 15, k = 8 * lh + (s >> 2), slot = blk * 4 + ((lane >> 4) & 1) * 2 + ((s & 3) >> 1);
             return (unsigned)(k * RB + ((slot ^ permute(k)) << 4) + (s & 1) * 8);
@@ -90,78 +97,162 @@ template <typename T, bool ACROSS, int BR> struct Tile {
     }
 };
 
+// N blocks of 32 rows of an operand, one k-step, from LDS to registers.  base[]: Tile::frag of the blocks (along k: of the first).
+template <typename T, bool ACROSS, int BR, int N> struct Frags {
+    using TL = Tile<T, ACROSS, BR>;
+    static constexpr int NB = ACROSS ? N : 1, READS = N * Frag<T, ACROSS>::READS;
+    Frag<T, ACROSS> f[N];
+    static __device__ __forceinline__ void bases(unsigned (&base)[NB], unsigned lds, int blk, int lane) {
+#pragma unroll
+        for (int i = 0; i < NB; i++) base[i] = lds + TL::frag(blk + i, lane);
+    }
+    template <int Q> __device__ __forceinline__ void read(const unsigned (&base)[NB], unsigned off) {      // k-step Q of the stage at byte offset off
+        if constexpr (!ACROSS) {
+            const unsigned at = xor_add(base[0], Q << 5, off);
+            static_for<N>([&](auto I) { constexpr int i = decltype(I)::value; f[i].template read<i * 32 * ROWB, ROWB>(at); });
+        } else {
+            static_for<N>([&](auto I) { constexpr int i = decltype(I)::value; f[i].template read<Q *(TL::BK / 4) * TL::RB, TL::RB>(base[i] + off); });
+        }
+    }
+    __device__ __forceinline__ void land() { static_for<N>([&](auto I) { f[decltype(I)::value].land(); }); }
+};
+
+// An operand's corner moves along the reduction as a scalar, and so does the number of bytes left behind it: what lies behind the last row, or behind the
+// last stage, is out of range and arrives as zeros.
+struct Cursor {
+    const unsigned char *p;
+    long left;
+    size_t step;
+    __device__ __forceinline__ void init(const void *base, size_t bytes, size_t at, size_t stage) {
+        p = static_cast<const unsigned char *>(base) + at;
+        left = (long)bytes - (long)at;
+        step = stage;
+    }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t next(bool real) {
+        const unsigned n = real && left > 0 ? (unsigned)min(left, 0xfffffff0L) : 0u;
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(p), 0, (int)n, 0x00020000);
+        p += step;
+        left -= (long)step;
+        return r;
+    }
+};
+
+// Tile order.  Workgroups go to the eight XCDs in turn; each XCD takes a contiguous run of a sequence that walks the columns of eight rows of
+// tiles, so that what runs on it at one time is a block of about eight by eight tiles and shares its operands in that L2.
+__device__ __forceinline__ bool pick_tile(const GemmArgs &a, int &split, int &tp, int &tc) {
+    const int ntiles = a.ntp * a.ntc, per = (ntiles + 7) >> 3;
+    split = (int)blockIdx.x / (per * 8);
+    const int bid = (int)blockIdx.x - split * per * 8, t = (bid & 7) * per + (bid >> 3);
+    if (t >= ntiles) return false;
+    const int g = t / (8 * a.ntc), in = t - g * 8 * a.ntc, rows = min(8, a.ntp - g * 8);
+    tp = g * 8 + in % rows;
+    tc = in / rows;
+    return true;
+}
+
+// Results of 32 rows x 32 * TC columns of a wave.  They go through a strip of LDS of its own, so that a lane has 8 neighbouring columns of one row
+// (one call of dropout's generator) and a store writes whole lines.
+template <typename T, GemmKind KIND, int TC> struct Writer {
+    static constexpr int ERS = TC * 32 + 4, LPR = TC * 4, RPS = 64 / LPR;       // floats of a strip's row; lanes per row, rows per pass
+    static constexpr int BYTES = 32 * ERS * 4;
+    float *strip;
+    int lane, split, n, nv;
+    float bias8[8];
+    uint32_t step;
+    __device__ __forceinline__ void init(const GemmArgs &a, unsigned char *lds, int wave, int lane_, int split_, int c0) {
+        strip = reinterpret_cast<float *>(lds + wave * BYTES);
+        lane = lane_; split = split_;
+        n = c0 + (lane % LPR) * 8;
+        nv = min(8, a.N - n);
+        if constexpr (KIND == GEMM_FORWARD) {
+            load_bias8(a.epi.bias, n, nv, bias8);
+            step = drop_step(a.epi.drop);
+        }
+    }
+    template <typename F> __device__ __forceinline__ void write(const GemmArgs &a, int m0, F &&block) {      // block(i): accumulators of column block i
+        const int lr = lane & 31, lh = lane >> 5, ecol = (lane % LPR) * 8;
+        static_for<TC>([&](auto I) {
+            const f32x16_t &v = block(I);
+#pragma unroll
+            for (int e = 0; e < 4; e++)
+                *reinterpret_cast<float4 *>(strip + lr * ERS + decltype(I)::value * 32 + 8 * e + 4 * lh) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
+        });
+        wave_lds_fence();
+#pragma unroll 1
+        for (int r = lane / LPR; r < 32; r += RPS) {
+            const int m = m0 + r;
+            if (m >= a.M || nv <= 0) continue;
+            const float4 lo = *reinterpret_cast<const float4 *>(strip + r * ERS + ecol), hi = *reinterpret_cast<const float4 *>(strip + r * ERS + ecol + 4);
+            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+            if (a.nsplit > 1) store8_any<float>(a.part + ((size_t)split * a.M + m) * a.N + n, v, nv);
+            else if constexpr (KIND == GEMM_FORWARD) finish8<T>(a.epi, step, m, n, a.N, nv, v, bias8);
+            else if (a.out_dt == SOL_F32) store8_any<float>(static_cast<float *>(a.out) + m * a.ldo + n, v, nv);
+            else store8_any<T>(static_cast<T *>(a.out) + m * a.ldo + n, v, nv);
+        }
+        wave_lds_fence();
+    }
+};
+
+// ---- tiles of 64 x 64 to 128 x 128: a ring of NS whole stages --------------------------------------------------------------------
 // KIND: GEMM_FORWARD (A, B along k), GEMM_DX (B across), GEMM_DW (both across).  WP x WC = 4 waves of TP x TC blocks of 32 x 32.
 template <typename T, GemmKind KIND, int WP, int WC, int TP, int TC, int NS, int PERCU>
-__global__ void __launch_bounds__(256, PERCU) linear_gemm_kernel(const GemmArgs a) {
+__global__ void __launch_bounds__(256, PERCU) linear_tile_kernel(const GemmArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool AX = KIND == GEMM_DW, BX = KIND != GEMM_FORWARD;
-    constexpr int NW = 4, ES = (int)sizeof(T), BP = WP * TP * 32, BC = WC * TC * 32, BK = 64 / ES;
+    constexpr int NW = 4, ES = (int)sizeof(T), BP = WP * TP * 32, BC = WC * TC * 32, BK = ROWB / ES;
     using TA = Tile<T, AX, BP>;
     using TB = Tile<T, BX, BC>;
-    using FA = Frag<T, AX>;
-    using FB = Frag<T, BX>;
+    using FA = Frags<T, AX, BP, TP>;
+    using FB = Frags<T, BX, BC, TC>;
+    using W = Writer<T, KIND, TC>;
     constexpr int STAGE = TA::BYTES + TB::BYTES, XL = TA::SEGS / NW, WL = TB::SEGS / NW, L = XL + WL;
-    constexpr int READS = TP * FA::READS + TC * FB::READS;     // LDS instructions of a k-step
-    constexpr int ERS = TC * 32 + 4;                           // floats of a row in the epilogue's strips
-    static_assert(WP * WC == NW && TA::SEGS % NW == 0 && TB::SEGS % NW == 0, "waves");
-    static_assert(NW * 32 * ERS * 4 <= NS * STAGE && NS >= 3 && (NS - 2) * L < 64, "strips in the ring; vmcnt");
+    constexpr int READS = FA::READS + FB::READS;               // LDS instructions of a k-step
+    static_assert(WP * WC == NW && TA::SEGS % (2 * NW) == 0 && TB::SEGS % NW == 0, "waves");
+    static_assert(NW * W::BYTES <= NS * STAGE && NS >= 2 && (NS - 1) * L < 64, "strips in the ring; vmcnt");
     __shared__ __align__(1024) unsigned char lds[NS * STAGE];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wc = wave / WP;
-
-    // Tile order.  Workgroups go to the eight XCDs in turn; each XCD takes a contiguous run of a sequence that walks the columns of eight rows
-    // of tiles, so that what runs on it at one time is a block of about eight by eight tiles and shares its operands in that L2.
-    const int ntiles = a.ntp * a.ntc, per = (ntiles + 7) >> 3;
-    const int split = (int)blockIdx.x / (per * 8), bid = (int)blockIdx.x - split * per * 8;
-    const int t = (bid & 7) * per + (bid >> 3);
-    if ((bid >> 3) >= per || t >= ntiles) return;
-    const int g = t / (8 * a.ntc), in = t - g * 8 * a.ntc, rows = min(8, a.ntp - g * 8);
-    const int p0 = (g * 8 + in % rows) * BP, c0 = (in / rows) * BC;
-
+    int split, tp, tc;
+    if (!pick_tile(a, split, tp, tc)) return;
+    const int p0 = tp * BP, c0 = tc * BC;
     const int nk = (a.K + BK - 1) / BK, s0 = split * a.steps, s1 = min(nk, s0 + a.steps);   // this part's stages
 
-    // The operands' corners move along the reduction as scalars, and so does the number of bytes left behind them: what lies behind the last
-    // row, or behind the last stage, is out of range and arrives as zeros.
     const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES);
-    const size_t astep = AX ? (size_t)BK * apitch : 64, bstep = BX ? (size_t)BK * bpitch : 64;
-    const size_t a0 = (AX ? (size_t)p0 * ES : (size_t)p0 * apitch) + s0 * astep, b0 = (BX ? (size_t)c0 * ES : (size_t)c0 * bpitch) + s0 * bstep;
-    const unsigned char *ap = static_cast<const unsigned char *>(a.a) + a0, *bp = static_cast<const unsigned char *>(a.b) + b0;
-    long aleft = (long)a.a_bytes - (long)a0, bleft = (long)a.b_bytes - (long)b0;
-
-    unsigned ao[XL], bo[WL];
+    const size_t astep = AX ? (size_t)BK * apitch : ROWB, bstep = BX ? (size_t)BK * bpitch : ROWB;
+    Cursor ca, cb;
+    ca.init(a.a, a.a_bytes, (AX ? (size_t)p0 * ES : (size_t)p0 * apitch) + s0 * astep, astep);
+    cb.init(a.b, a.b_bytes, (BX ? (size_t)c0 * ES : (size_t)c0 * bpitch) + s0 * bstep, bstep);
+    unsigned ao[XL], bo[WL], cut[2] = {0u, 0u};                // cut: what lies behind K in the last stage (odd and even instructions)
 #pragma unroll
     for (int i = 0; i < XL; i++) ao[i] = TA::offset(wave * XL + i, lane, apitch);
 #pragma unroll
     for (int i = 0; i < WL; i++) bo[i] = TB::offset(wave * WL + i, lane, bpitch);
-    // A along k whose rows do not end with zeros: the slots of the last stage that lie behind K (the row permutation is the same for every i)
-    unsigned cut = 0;
-    if constexpr (!AX) cut = a.a_cut && (nk - 1) * 64 + (((lane & 3) ^ swz<64>(lane >> 2)) << 4) >= a.K * ES ? 0xffffffffu : 0u;
-
-    int left = s1 - s0, at = s0;                               // stages not yet requested; the next one
+    if constexpr (!AX) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) cut[i] = a.a_cut && TA::behind(wave * XL + i, lane, a.K * ES - (nk - 1) * ROWB) ? 0xffffffffu : 0u;
+    }
+    int at = s0;                                               // the next stage to request
     __amdgpu_buffer_rsrc_t ar, br;
-    unsigned acut = 0;
-    auto next_stage = [&]() {                                  // resources of the next stage to request
-        const bool real = left > 0;
-        const unsigned an = real && aleft > 0 ? (unsigned)min(aleft, 0xfffffff0L) : 0u, bn = real && bleft > 0 ? (unsigned)min(bleft, 0xfffffff0L) : 0u;
-        ar = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(ap), 0, (int)an, 0x00020000);
-        br = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(bp), 0, (int)bn, 0x00020000);
-        if constexpr (!AX) acut = at == nk - 1 ? cut : 0u;
-        ap += astep; bp += bstep; aleft -= (long)astep; bleft -= (long)bstep;
-        --left; ++at;
+    bool last = false;
+    auto next_stage = [&]() {
+        ar = ca.next(at < s1);
+        br = cb.next(at < s1);
+        last = at == nk - 1;
+        ++at;
     };
-    auto request = [&](auto I, int buf) {                      // the I-th DMA of this wave for that stage
+    auto request = [&](auto I, unsigned off) {                 // the I-th DMA of this wave for that stage
         constexpr int i = decltype(I)::value;
-        unsigned char *la = lds + buf * STAGE, *lb = la + TA::BYTES;
+        unsigned char *la = lds + off, *lb = la + TA::BYTES;
         if constexpr (i < XL)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (__attribute__((address_space(3))) void *)(la + (wave * XL + i) * 1024), 16, ao[i] | acut, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ar, (__attribute__((address_space(3))) void *)(la + (wave * XL + i) * 1024), 16, !AX ? ao[i] | (last ? cut[i & 1] : 0u) : ao[i], 0, 0, 0);
         else
             __builtin_amdgcn_raw_ptr_buffer_load_lds(br, (__attribute__((address_space(3))) void *)(lb + (wave * WL + i - XL) * 1024), 16, bo[i - XL], 0, 0, 0);
     };
 #pragma unroll
     for (int s = 0; s < NS; s++) {
         next_stage();
-        static_for<L>([&](auto I) { request(I, s); });
+        static_for<L>([&](auto I) { request(I, (unsigned)(s * STAGE)); });
     }
 
     f32x16_t acc[TC][TP];
@@ -172,144 +263,269 @@ __global__ void __launch_bounds__(256, PERCU) linear_gemm_kernel(const GemmArgs 
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
 
-    unsigned fa0[TP], fb0[TC];
-#pragma unroll
-    for (int j = 0; j < TP; j++) fa0[j] = lds_addr(lds) + TA::frag(wp * TP + j, lane);
-#pragma unroll
-    for (int i = 0; i < TC; i++) fb0[i] = lds_addr(lds) + TA::BYTES + TB::frag(wc * TC + i, lane);
-
-    FA fa[2][TP];
-    FB fb[2][TC];
-    auto read_step = [&](auto Q, unsigned sb) {                // fragments of k-step Q (0, 1) of the stage at byte offset sb
-        constexpr int q = decltype(Q)::value;
-        if constexpr (!BX) {
-            const unsigned w = xor_add(fb0[0], q << 5, sb);
-            static_for<TC>([&](auto I) { constexpr int i = decltype(I)::value; fb[q][i].template read<i * 2048, 64>(w); });
-        } else {
-            static_for<TC>([&](auto I) { constexpr int i = decltype(I)::value; fb[q][i].template read<q *(BK / 2) * TB::RB, TB::RB>(fb0[i] + sb); });
-        }
-        if constexpr (!AX) {
-            const unsigned x = xor_add(fa0[0], q << 5, sb);
-            static_for<TP>([&](auto J) { constexpr int j = decltype(J)::value; fa[q][j].template read<j * 2048, 64>(x); });
-        } else {
-            static_for<TP>([&](auto J) { constexpr int j = decltype(J)::value; fa[q][j].template read<q *(BK / 2) * TA::RB, TA::RB>(fa0[j] + sb); });
-        }
-    };
-    auto land = [&](auto Q) {
-        constexpr int q = decltype(Q)::value;
-        static_for<TC>([&](auto I) { fb[q][decltype(I)::value].land(); });
-        static_for<TP>([&](auto J) { fa[q][decltype(J)::value].land(); });
-    };
-    auto multiply = [&](auto Q, auto &&between) {
-        constexpr int q = decltype(Q)::value;
+    unsigned abase[FA::NB], bbase[FB::NB];
+    FA::bases(abase, lds_addr(lds), wp * TP, lane);
+    FB::bases(bbase, lds_addr(lds) + TA::BYTES, wc * TC, lane);
+    FA fa[2];
+    FB fb[2];
+    auto multiply = [&](auto S, auto &&between) {
+        constexpr int set = decltype(S)::value;
         static_for<TC * TP>([&](auto U) {
             constexpr int u = decltype(U)::value, i = u / TP, j = u % TP;
-            Mma<T>::run(acc[i][j], fb[q][i].get(), fa[q][j].get());
+            Mma<T>::run(acc[i][j], fb[set].f[i].get(), fa[set].f[j].get());
             between(U);
         });
+        __builtin_amdgcn_sched_barrier(0);
     };
-    constexpr std::integral_constant<int, 0> Q0{};
-    constexpr std::integral_constant<int, 1> Q1{};
 
     wait_vmcnt<(NS - 1) * L>();                                // the first stage has landed
     __builtin_amdgcn_s_barrier();
-    read_step(Q0, 0u);
-
+    fb[0].template read<0>(bbase, 0u);
+    fa[0].template read<0>(abase, 0u);
     unsigned sb = 0;
-    int buf = 0;
     for (int s = s0; s < s1; s++) {
         const unsigned sbn = sb + STAGE == NS * STAGE ? 0u : sb + STAGE;
-        read_step(Q1, sb);
-        wait_lgkmcnt<(READS < 15 ? READS : 0)>();              // the first k-step's fragments are here
-        land(Q0);
-        multiply(Q0, [](auto) {});
+        static_for<3>([&](auto Q) {                            // k-steps 0 .. 2, the next one's fragments on their way
+            constexpr int q = decltype(Q)::value, set = q & 1;
+            fb[set ^ 1].template read<q + 1>(bbase, sb);
+            fa[set ^ 1].template read<q + 1>(abase, sb);
+            wait_lds<READS>();
+            fb[set].land();
+            fa[set].land();
+            multiply(std::integral_constant<int, set>{}, [](auto) {});
+        });
         wait_lgkmcnt<0>();                                     // all of this stage is in registers
-        land(Q1);
+        fb[1].land();
+        fa[1].land();
         wait_vmcnt<(NS - 2) * L>();                            // the next stage has landed
         __builtin_amdgcn_s_barrier();                          // ... for every wave, and nobody reads this one any more: it can be refilled
-        read_step(Q0, sbn);
+        fb[0].template read<0>(bbase, sbn);
+        fa[0].template read<0>(abase, sbn);
         next_stage();
-        multiply(Q1, [&](auto U) {
-            constexpr int u = decltype(U)::value;
-            if constexpr (u < L) request(U, buf);
-            if constexpr (u == TC * TP - 1 && L > TC * TP)
-                static_for<(L > TC * TP ? L - TC * TP : 0)>([&](auto V) { request(std::integral_constant<int, TC * TP + decltype(V)::value>{}, buf); });
+        multiply(std::integral_constant<int, 1>{}, [&](auto U) {
+            constexpr int u = decltype(U)::value, per = (L + TC * TP - 1) / (TC * TP);
+            static_for<per>([&](auto V) {
+                constexpr int i = u * per + decltype(V)::value;
+                if constexpr (i < L) request(std::integral_constant<int, i>{}, sb);
+            });
         });
-        buf = buf + 1 == NS ? 0 : buf + 1;
         sb = sbn;
     }
     wait_lgkmcnt<0>();                                         // the fragments requested behind the last stage
-    land(Q0);
+    fb[0].land();
+    fa[0].land();
     wait_vmcnt<0>();                                           // ... and its DMAs, zeros into dead slots
-    __builtin_amdgcn_s_barrier();                              // the ring becomes the epilogue's strips
+    __builtin_amdgcn_s_barrier();                              // the ring becomes the strips
 
-    // Epilogue: a wave takes 32 rows at a time through a strip of LDS of its own, so that a lane has 8 neighbouring columns of one row
-    // (one call of dropout's generator) and a store writes whole lines.
-    constexpr int LPR = TC * 4, RPS = 64 / LPR;
-    float *strip = reinterpret_cast<float *>(lds) + wave * (32 * ERS);
-    const int lr = lane & 31, lh = lane >> 5, erow = lane / LPR, ecol = (lane % LPR) * 8;
-    const int n = c0 + wc * TC * 32 + ecol, nv = min(8, a.N - n);
-    float bias8[8];
-    uint32_t step = 0;
-    if constexpr (KIND == GEMM_FORWARD) {
-        load_bias8(a.epi.bias, n, nv, bias8);
-        step = drop_step(a.epi.drop);
-    }
+    W w;
+    w.init(a, lds, wave, lane, split, c0 + wc * TC * 32);
     static_for<TP>([&](auto J) {
         constexpr int j = decltype(J)::value;
-#pragma unroll
-        for (int i = 0; i < TC; i++)
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                *reinterpret_cast<float4 *>(strip + lr * ERS + i * 32 + 8 * e + 4 * lh) = make_float4(acc[i][j][4 * e], acc[i][j][4 * e + 1], acc[i][j][4 * e + 2], acc[i][j][4 * e + 3]);
-        wave_lds_fence();
-#pragma unroll 1
-        for (int r = erow; r < 32; r += RPS) {
-            const int m = p0 + (wp * TP + j) * 32 + r;
-            if (m >= a.M || nv <= 0) continue;
-            const float4 lo = *reinterpret_cast<const float4 *>(strip + r * ERS + ecol), hi = *reinterpret_cast<const float4 *>(strip + r * ERS + ecol + 4);
-            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            if (a.nsplit > 1) store8_any<float>(a.part + ((size_t)split * a.M + m) * a.N + n, v, nv);
-            else if constexpr (KIND == GEMM_FORWARD) finish8<T>(a.epi, step, m, n, a.N, nv, v, bias8);
-            else if (a.out_dt == SOL_F32) store8_any<float>(static_cast<float *>(a.out) + m * a.ldo + n, v, nv);
-            else store8_any<T>(static_cast<T *>(a.out) + m * a.ldo + n, v, nv);
-        }
-        wave_lds_fence();
+        w.write(a, p0 + (wp * TP + j) * 32, [&](auto I) -> const f32x16_t & { return acc[decltype(I)::value][j]; });
     });
 #endif
 }
 
-template <typename T, GemmKind KIND, int WP, int WC, int TP, int TC, int NS, int PERCU> static sol_status launch_tile(GemmArgs a, hipStream_t st) {
-    a.ntp = ceil_div(a.M, WP * TP * 32);
-    a.ntc = ceil_div(a.N, WC * TC * 32);
-    const int nk = ceil_div(a.K, 64 / (int)sizeof(T));
+// ---- tiles of 256 x 128 ----------------------------------------------------------------------------------------------------------
+// Two workgroups per CU leave 80 KB of LDS each, and a stage of whole lines has 48.  So the ring counts not stages but units of 16 KB, 128 rows or columns each,
+// five of them: a stage is B, A0 (rows 0 .. 127) and A1 (rows 128 .. 255).  A wave takes its fragments of B into registers once and multiplies A0, then A1, with
+// them; when A0 is done its slot and B's are refilled, and when A1 is done its own.  Every unit is requested one stage (32 matrix instructions per wave) before it is needed.
+template <typename T, GemmKind KIND>
+__global__ void __launch_bounds__(256, 2) linear_big_kernel(const GemmArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr bool AX = KIND == GEMM_DW, BX = KIND != GEMM_FORWARD;
+    constexpr int NW = 4, ES = (int)sizeof(T), BK = ROWB / ES, UNIT = 16384, UL = UNIT / 1024 / NW;      // UL: DMA instructions of a wave per unit
+    using TA = Tile<T, AX, 128>;
+    using TB = Tile<T, BX, 128>;
+    using FA = Frags<T, AX, 128, 2>;
+    using FB = Frags<T, BX, 128, 2>;
+    using W = Writer<T, KIND, 2>;
+    static_assert(NW * W::BYTES <= 5 * UNIT, "strips in the ring");
+    __shared__ __align__(1024) unsigned char lds[5 * UNIT];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave & 1, wc = wave >> 1;
+    int split, tp, tc;
+    if (!pick_tile(a, split, tp, tc)) return;
+    const int p0 = tp * 256, c0 = tc * 128;
+    const int nk = (a.K + BK - 1) / BK, s0 = split * a.steps, s1 = min(nk, s0 + a.steps);   // this part's stages
+
+    const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES);
+    const size_t astep = AX ? (size_t)BK * apitch : ROWB, bstep = BX ? (size_t)BK * bpitch : ROWB;
+    const size_t acorner = (AX ? (size_t)p0 * ES : (size_t)p0 * apitch) + s0 * astep;
+    Cursor ca[2], cb;
+    ca[0].init(a.a, a.a_bytes, acorner, astep);
+    ca[1].init(a.a, a.a_bytes, acorner + (AX ? (size_t)128 * ES : (size_t)128 * apitch), astep);
+    cb.init(a.b, a.b_bytes, (BX ? (size_t)c0 * ES : (size_t)c0 * bpitch) + s0 * bstep, bstep);
+    unsigned ao[UL], bo[UL], cut[2] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < UL; i++) {
+        ao[i] = TA::offset(wave * UL + i, lane, apitch);
+        bo[i] = TB::offset(wave * UL + i, lane, bpitch);
+    }
+    if constexpr (!AX) {
+#pragma unroll
+        for (int i = 0; i < 2; i++) cut[i] = a.a_cut && TA::behind(wave * UL + i, lane, a.K * ES - (nk - 1) * ROWB) ? 0xffffffffu : 0u;
+    }
+    auto request_a = [&](const __amdgpu_buffer_rsrc_t &r, auto I, unsigned off, bool last) {
+        constexpr int i = decltype(I)::value;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, !AX ? ao[i] | (last ? cut[i & 1] : 0u) : ao[i], 0, 0, 0);
+    };
+    auto request_b = [&](const __amdgpu_buffer_rsrc_t &r, auto I, unsigned off) {
+        constexpr int i = decltype(I)::value;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, bo[i], 0, 0, 0);
+    };
+
+    unsigned o0 = 0, o1 = UNIT, o2 = 2 * UNIT, o3 = 3 * UNIT, o4 = 4 * UNIT;      // slots of this stage's B, A0, A1 and of the next one's B, A0
+    {
+        __amdgpu_buffer_rsrc_t r = cb.next(s0 < s1);
+        static_for<UL>([&](auto I) { request_b(r, I, o0); });
+        r = ca[0].next(s0 < s1);
+        static_for<UL>([&](auto I) { request_a(r, I, o1, s0 == nk - 1); });
+        r = ca[1].next(s0 < s1);
+        static_for<UL>([&](auto I) { request_a(r, I, o2, s0 == nk - 1); });
+        r = cb.next(s0 + 1 < s1);
+        static_for<UL>([&](auto I) { request_b(r, I, o3); });
+        r = ca[0].next(s0 + 1 < s1);
+        static_for<UL>([&](auto I) { request_a(r, I, o4, s0 + 1 == nk - 1); });
+    }
+
+    f32x16_t acc[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
+
+    unsigned abase[FA::NB], bbase[FB::NB];
+    FA::bases(abase, lds_addr(lds), wp * 2, lane);
+    FB::bases(bbase, lds_addr(lds), wc * 2, lane);
+    FA fa[2];
+    FB fb[4];
+    auto multiply = [&](auto H, auto Q, auto &&between) {       // four products of half H, k-step Q
+        constexpr int h = decltype(H)::value, q = decltype(Q)::value;
+        static_for<4>([&](auto U) {
+            constexpr int u = decltype(U)::value, i = u / 2, j = u % 2;
+            Mma<T>::run(acc[i][h * 2 + j], fb[q].f[i].get(), fa[q & 1].f[j].get());
+            between(U);
+        });
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    constexpr std::integral_constant<int, 0> C0{};
+    constexpr std::integral_constant<int, 1> C1{};
+    constexpr std::integral_constant<int, 3> C3{};
+    auto nothing = [](auto) {};
+
+    wait_vmcnt<3 * UL>();                                       // B and A0 of the first stage have landed
+    __builtin_amdgcn_s_barrier();
+    static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value>(bbase, o0); });
+    wait_lgkmcnt<0>();
+    static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
+    fa[0].template read<0>(abase, o1);
+
+    for (int s = s0; s < s1; s++) {
+        // ---- A0
+        static_for<3>([&](auto Q) {
+            constexpr int q = decltype(Q)::value;
+            fa[(q + 1) & 1].template read<q + 1>(abase, o1);
+            wait_lds<FA::READS>();
+            if constexpr (q == 0) fb[3].land();
+            fa[q & 1].land();
+            multiply(C0, Q, nothing);
+        });
+        wait_lgkmcnt<0>();                                      // all of A0 is in registers
+        fa[1].land();
+        wait_vmcnt<UL>();                                       // A1 and the next stage's B have landed
+        __builtin_amdgcn_s_barrier();                           // ... for every wave, and nobody reads A0 and B any more
+        fa[0].template read<0>(abase, o2);
+        {
+            const __amdgpu_buffer_rsrc_t r1 = ca[1].next(s + 1 < s1), rb = cb.next(s + 2 < s1);
+            multiply(C0, C3, [&](auto U) {
+                request_a(r1, U, o0, s + 1 == nk - 1);
+                request_b(rb, U, o1);
+            });
+        }
+        // ---- A1; behind each k-step's last products its fragments of B make room for the next stage's
+        static_for<3>([&](auto Q) {
+            constexpr int q = decltype(Q)::value;
+            fa[(q + 1) & 1].template read<q + 1>(abase, o2);
+            wait_lds<FA::READS + (q ? FB::READS : 0)>();
+            fa[q & 1].land();
+            if constexpr (q == 2) fb[0].land();
+            multiply(C1, Q, nothing);
+            fb[q].template read<q>(bbase, o3);
+        });
+        wait_lds<FB::READS>();                              // all of A1 is in registers
+        fa[1].land();
+        fb[1].land();
+        wait_vmcnt<2 * UL>();                                   // the next stage's A0 has landed
+        __builtin_amdgcn_s_barrier();
+        {
+            const __amdgpu_buffer_rsrc_t r0 = ca[0].next(s + 2 < s1);
+            fa[0].template read<0>(abase, o4);
+            multiply(C1, C3, [&](auto U) { request_a(r0, U, o2, s + 2 == nk - 1); });
+        }
+        fb[3].template read<3>(bbase, o3);
+        wait_lds<FA::READS + FB::READS>();
+        fb[2].land();
+        const unsigned t0 = o0, t1 = o1, t2 = o2;
+        o0 = o3; o1 = o4; o2 = t0; o3 = t1; o4 = t2;
+    }
+    wait_lgkmcnt<0>();                                          // the fragments requested behind the last stage
+    fa[0].land();
+    fb[3].land();
+    wait_vmcnt<0>();                                            // ... and its DMAs, zeros into dead slots
+    __builtin_amdgcn_s_barrier();                               // the ring becomes the strips
+
+    W w;
+    w.init(a, lds, wave, lane, split, c0 + wc * 64);
+    static_for<4>([&](auto J) {
+        constexpr int j = decltype(J)::value;
+        w.write(a, p0 + (j >> 1) * 128 + wp * 64 + (j & 1) * 32, [&](auto I) -> const f32x16_t & { return acc[decltype(I)::value][j]; });
+    });
+#endif
+}
+
+static long tiles_of(GemmArgs &a, int dt, int bp, int bc) {     // fills in the tile counts; workgroups of the launch
+    a.ntp = ceil_div(a.M, bp);
+    a.ntc = ceil_div(a.N, bc);
     a.nsplit = a.nsplit < 1 ? 1 : a.nsplit;
-    a.steps = ceil_div(nk, a.nsplit);
-    const long blocks = (long)ceil_div(a.ntp * a.ntc, 8) * 8 * a.nsplit;
-    hipLaunchKernelGGL((linear_gemm_kernel<T, KIND, WP, WC, TP, TC, NS, PERCU>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+    a.steps = ceil_div(ceil_div(a.K, ROWB / (int)dtype_size(dt)), a.nsplit);
+    return (long)ceil_div(a.ntp * a.ntc, 8) * 8 * a.nsplit;
+}
+
+template <typename T, GemmKind KIND, int WP, int WC, int TP, int TC, int NS, int PERCU> static sol_status launch_tile(GemmArgs a, int dt, hipStream_t st) {
+    const long blocks = tiles_of(a, dt, WP * TP * 32, WC * TC * 32);
+    hipLaunchKernelGGL((linear_tile_kernel<T, KIND, WP, WC, TP, TC, NS, PERCU>), dim3((unsigned)blocks), dim3(256), 0, st, a);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
 
-template <typename T, GemmKind KIND> static sol_status launch_kind(const GemmArgs &a, hipStream_t st) {
+template <typename T, GemmKind KIND> static sol_status launch_kind(GemmArgs a, int dt, hipStream_t st) {
     const long big = (long)ceil_div(a.M, 256) * ceil_div(a.N, 128) * a.nsplit, mid = (long)ceil_div(a.M, 128) * ceil_div(a.N, 128) * a.nsplit;
-    if (big >= 400) return launch_tile<T, KIND, 2, 2, 4, 2, 3, 2>(a, st);
-    if (mid >= 200) return launch_tile<T, KIND, 2, 2, 2, 2, 4, 2>(a, st);
-    return launch_tile<T, KIND, 2, 2, 1, 1, 5, 3>(a, st);
+    if (big >= 400) {
+        const long blocks = tiles_of(a, dt, 256, 128);
+        hipLaunchKernelGGL((linear_big_kernel<T, KIND>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+        SOL_HIP(hipGetLastError());
+        return SOL_OK;
+    }
+    if (mid >= 200) return launch_tile<T, KIND, 2, 2, 2, 2, 2, 2>(a, dt, st);
+    return launch_tile<T, KIND, 2, 2, 1, 1, 3, 3>(a, dt, st);
 }
 
 sol_status launch_linear_gemm(GemmArgs a, int dt, GemmKind kind, hipStream_t st) {
     if (dt == SOL_BF16) {
         switch (kind) {
-            case GEMM_FORWARD: return launch_kind<bf16_t, GEMM_FORWARD>(a, st);
-            case GEMM_DX: return launch_kind<bf16_t, GEMM_DX>(a, st);
-            default: return launch_kind<bf16_t, GEMM_DW>(a, st);
+            case GEMM_FORWARD: return launch_kind<bf16_t, GEMM_FORWARD>(a, dt, st);
+            case GEMM_DX: return launch_kind<bf16_t, GEMM_DX>(a, dt, st);
+            default: return launch_kind<bf16_t, GEMM_DW>(a, dt, st);
         }
     }
     switch (kind) {
-        case GEMM_FORWARD: return launch_kind<float, GEMM_FORWARD>(a, st);
-        case GEMM_DX: return launch_kind<float, GEMM_DX>(a, st);
-        default: return launch_kind<float, GEMM_DW>(a, st);
+        case GEMM_FORWARD: return launch_kind<float, GEMM_FORWARD>(a, dt, st);
+        case GEMM_DX: return launch_kind<float, GEMM_DX>(a, dt, st);
+        default: return launch_kind<float, GEMM_DW>(a, dt, st);
     }
 }
 

@@ -193,7 +193,7 @@ __device__ __forceinline__ void load_bias8(const float *bias, int n, int nv, flo
 // ---- launchers --------------------------------------------------------------------------------------------------------------------
 // D[p][c] = sum_k A(p, k) B(c, k) for p < M, c < N, k < K.  An operand is stored along k ([p][k], ld elements between its rows) or across
 // it ([k][p]).  Base addresses and pitches are multiples of 16 bytes; an operand stored along k ends its rows with zeros up to a multiple of
-// 64 bytes, or has K a multiple of 16 bytes' worth of elements and a_cut set.
+// 128 bytes, or has K a multiple of 16 bytes' worth of elements and a_cut set.
 struct GemmArgs {
     const void *a, *b;
     long lda, ldb;
