@@ -98,8 +98,7 @@ sol_status check_workspace(const void *workspace, size_t have, size_t need) {
     return SOL_OK;
 }
 
-// extent of [rows][cols] with pitch ld
-size_t span(int rows, long ld, int cols, int dt) { return ((size_t)(rows - 1) * ld + cols) * dtype_size(dt); }
+int row_bytes(int cols, int dt) { return cols * (int)dtype_size(dt); }
 
 }  // namespace
 }  // namespace sol
@@ -137,12 +136,12 @@ sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void
     const int kp = pack_pitch(l.in_f, l.dtype);
 
     GemmArgs a{};
-    a.a = x; a.lda = l.ldx; a.a_bytes = span(l.m, l.ldx, l.in_f, l.dtype); a.a_cut = cut_needed(l.in_f, l.dtype);
+    a.a = x; a.lda = l.ldx; a.a_row = row_bytes(l.in_f, l.dtype); a.a_cut = cut_needed(l.in_f, l.dtype);
     if (p.pad) {
         SOL_TRY(launch_pad_rows(x, l.ldx, workspace, kp, l.m, l.in_f, l.dtype, st));
-        a.a = workspace; a.lda = kp; a.a_bytes = span(l.m, kp, kp, l.dtype); a.a_cut = 0;
+        a.a = workspace; a.lda = kp; a.a_row = row_bytes(kp, l.dtype); a.a_cut = 0;
     }
-    a.b = w_packed; a.ldb = kp; a.b_bytes = span(l.out_f, kp, kp, l.dtype);
+    a.b = w_packed; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
     a.M = l.m; a.N = l.out_f; a.K = l.in_f; a.nsplit = 1;
     a.epi = LinearEpi{bias, residual, y, preact, l.ldr, l.ldy, l.act, d};
     return launch_linear_gemm(a, l.dtype, GEMM_FORWARD, st);
@@ -177,14 +176,14 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
     const bool own_dz = (dx || dw) && (l.act != SOL_ACT_NONE || d.t || !rows_aligned(l.ldy, l.out_f, l.dtype));
     const long ldz = own_dz ? pack_pitch(l.out_f, l.dtype) : l.ldy;
     const void *dz = own_dz ? ws + p.dz : dy;
-    const size_t dz_bytes = own_dz ? span(l.m, ldz, (int)ldz, l.dtype) : span(l.m, ldz, l.out_f, l.dtype);
+    const int dz_row = row_bytes(own_dz ? (int)ldz : l.out_f, l.dtype);
     if (own_dz || db)
         SOL_TRY(launch_linear_dz(dy, l.ldy, preact, own_dz ? ws + p.dz : nullptr, ldz, l.m, l.out_f, l.act, d, l.dtype, reinterpret_cast<float *>(ws + p.part), db, st));
     const int kp = pack_pitch(l.in_f, l.dtype);
     if (dx) {
         GemmArgs a{};
-        a.a = dz; a.lda = ldz; a.a_bytes = dz_bytes; a.a_cut = !own_dz && cut_needed(l.out_f, l.dtype);
-        a.b = w_packed; a.ldb = kp; a.b_bytes = span(l.out_f, kp, kp, l.dtype);
+        a.a = dz; a.lda = ldz; a.a_row = dz_row; a.a_cut = !own_dz && cut_needed(l.out_f, l.dtype);
+        a.b = w_packed; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
         a.M = l.m; a.N = l.in_f; a.K = l.out_f; a.nsplit = p.dx_split;
         a.part = reinterpret_cast<float *>(ws + p.sums);
         a.out = dx; a.ldo = l.in_f; a.out_dt = l.dtype;
@@ -193,11 +192,11 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
     }
     if (dw) {
         GemmArgs a{};
-        a.a = dz; a.lda = ldz; a.a_bytes = dz_bytes;
-        a.b = x; a.ldb = l.ldx; a.b_bytes = span(l.m, l.ldx, l.in_f, l.dtype);
+        a.a = dz; a.lda = ldz; a.a_row = dz_row;
+        a.b = x; a.ldb = l.ldx; a.b_row = row_bytes(l.in_f, l.dtype);
         if (p.pad) {
             SOL_TRY(launch_pad_rows(x, l.ldx, ws + p.xpad, kp, l.m, l.in_f, l.dtype, st));
-            a.b = ws + p.xpad; a.ldb = kp; a.b_bytes = span(l.m, kp, kp, l.dtype);
+            a.b = ws + p.xpad; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
         }
         a.M = l.out_f; a.N = l.in_f; a.K = l.m; a.nsplit = p.dw_split;
         a.part = reinterpret_cast<float *>(ws + p.sums);

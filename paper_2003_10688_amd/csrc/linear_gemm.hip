@@ -117,22 +117,41 @@ template <typename T, bool ACROSS, int BR, int N> struct Frags {
     __device__ __forceinline__ void land() { static_for<N>([&](auto I) { f[decltype(I)::value].land(); }); }
 };
 
-// An operand's corner moves along the reduction as a scalar, and so does the number of bytes left behind it: what lies behind the last row, or behind the
-// last stage, is out of range and arrives as zeros.
-struct Cursor {
+// An operand's corner moves along the reduction as a scalar; what lies behind the tensor, or behind the part's last stage, is out of range of the resource and
+// arrives as zeros.  Along k: rows from `rows` on.  Across k: rows of k from `left` on, and what lies behind row_bytes of the last one.
+template <bool ACROSS, int BK> struct Cursor;
+template <int BK> struct Cursor<false, BK> {
     const unsigned char *p;
-    long left;
-    size_t step;
-    __device__ __forceinline__ void init(const void *base, size_t bytes, size_t at, size_t stage) {
-        p = static_cast<const unsigned char *>(base) + at;
-        left = (long)bytes - (long)at;
-        step = stage;
+    unsigned num;
+    int left;
+    __device__ __forceinline__ void init(const void *base, unsigned pitch, int es, int first, int limit, int, int s0, int s1, int) {
+        p = static_cast<const unsigned char *>(base) + (size_t)first * pitch + (size_t)s0 * ROWB;
+        num = (unsigned)max(0, min(256, limit - first)) * pitch;       // a row ends in memory where the pitch ends, or its last stage is cut
+        left = s1 - s0;
     }
-    __device__ __forceinline__ __amdgpu_buffer_rsrc_t next(bool real) {
-        const unsigned n = real && left > 0 ? (unsigned)min(left, 0xfffffff0L) : 0u;
-        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(p), 0, (int)n, 0x00020000);
-        p += step;
-        left -= (long)step;
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t next() {
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(p), 0, left > 0 ? (int)num : 0, 0x00020000);
+        p += ROWB;
+        --left;
+        return r;
+    }
+};
+template <int BK> struct Cursor<true, BK> {
+    const unsigned char *p;
+    unsigned pitch, lack;
+    int left;
+    __device__ __forceinline__ void init(const void *base, unsigned pitch_, int es, int first, int, int row_bytes, int s0, int s1, int K) {
+        pitch = pitch_;
+        p = static_cast<const unsigned char *>(base) + (size_t)first * es + (size_t)s0 * BK * pitch;
+        const int row = row_bytes - first * es;
+        lack = pitch - (unsigned)row;
+        left = row > 0 ? min(K, s1 * BK) - s0 * BK : 0;
+    }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t next() {
+        const int rows = min(left, BK);
+        const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(p), 0, rows > 0 ? (int)((unsigned)rows * pitch - lack) : 0, 0x00020000);
+        p += (size_t)BK * pitch;
+        left -= BK;
         return r;
     }
 };
@@ -219,10 +238,10 @@ __global__ void __launch_bounds__(256, PERCU) linear_tile_kernel(const GemmArgs 
     const int nk = (a.K + BK - 1) / BK, s0 = split * a.steps, s1 = min(nk, s0 + a.steps);   // this part's stages
 
     const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES);
-    const size_t astep = AX ? (size_t)BK * apitch : ROWB, bstep = BX ? (size_t)BK * bpitch : ROWB;
-    Cursor ca, cb;
-    ca.init(a.a, a.a_bytes, (AX ? (size_t)p0 * ES : (size_t)p0 * apitch) + s0 * astep, astep);
-    cb.init(a.b, a.b_bytes, (BX ? (size_t)c0 * ES : (size_t)c0 * bpitch) + s0 * bstep, bstep);
+    Cursor<AX, BK> ca;
+    Cursor<BX, BK> cb;
+    ca.init(a.a, apitch, ES, p0, a.M, a.a_row, s0, s1, a.K);
+    cb.init(a.b, bpitch, ES, c0, a.N, a.b_row, s0, s1, a.K);
     unsigned ao[XL], bo[WL], cut[2] = {0u, 0u};                // cut: what lies behind K in the last stage (odd and even instructions)
 #pragma unroll
     for (int i = 0; i < XL; i++) ao[i] = TA::offset(wave * XL + i, lane, apitch);
@@ -236,8 +255,8 @@ __global__ void __launch_bounds__(256, PERCU) linear_tile_kernel(const GemmArgs 
     __amdgpu_buffer_rsrc_t ar, br;
     bool last = false;
     auto next_stage = [&]() {
-        ar = ca.next(at < s1);
-        br = cb.next(at < s1);
+        ar = ca.next();
+        br = cb.next();
         last = at == nk - 1;
         ++at;
     };
@@ -340,7 +359,7 @@ __global__ void __launch_bounds__(256, 2) linear_big_kernel(const GemmArgs a) {
     using FA = Frags<T, AX, 128, 2>;
     using FB = Frags<T, BX, 128, 2>;
     using W = Writer<T, KIND, 2>;
-    static_assert(NW * W::BYTES <= 5 * UNIT, "strips in the ring");
+    static_assert(NW * W::BYTES <= 5 * UNIT && UL == 4, "strips in the ring; requests per unit");
     __shared__ __align__(1024) unsigned char lds[5 * UNIT];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -351,12 +370,11 @@ __global__ void __launch_bounds__(256, 2) linear_big_kernel(const GemmArgs a) {
     const int nk = (a.K + BK - 1) / BK, s0 = split * a.steps, s1 = min(nk, s0 + a.steps);   // this part's stages
 
     const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES);
-    const size_t astep = AX ? (size_t)BK * apitch : ROWB, bstep = BX ? (size_t)BK * bpitch : ROWB;
-    const size_t acorner = (AX ? (size_t)p0 * ES : (size_t)p0 * apitch) + s0 * astep;
-    Cursor ca[2], cb;
-    ca[0].init(a.a, a.a_bytes, acorner, astep);
-    ca[1].init(a.a, a.a_bytes, acorner + (AX ? (size_t)128 * ES : (size_t)128 * apitch), astep);
-    cb.init(a.b, a.b_bytes, (BX ? (size_t)c0 * ES : (size_t)c0 * bpitch) + s0 * bstep, bstep);
+    Cursor<AX, BK> ca[2];
+    Cursor<BX, BK> cb;
+    ca[0].init(a.a, apitch, ES, p0, a.M, a.a_row, s0, s1, a.K);
+    ca[1].init(a.a, apitch, ES, p0 + 128, a.M, a.a_row, s0, s1, a.K);
+    cb.init(a.b, bpitch, ES, c0, a.N, a.b_row, s0, s1, a.K);
     unsigned ao[UL], bo[UL], cut[2] = {0u, 0u};
 #pragma unroll
     for (int i = 0; i < UL; i++) {
@@ -377,17 +395,16 @@ __global__ void __launch_bounds__(256, 2) linear_big_kernel(const GemmArgs a) {
     };
 
     unsigned o0 = 0, o1 = UNIT, o2 = 2 * UNIT, o3 = 3 * UNIT, o4 = 4 * UNIT;      // slots of this stage's B, A0, A1 and of the next one's B, A0
+    __amdgpu_buffer_rsrc_t r0;                                  // of the A0 whose requests are spread over two halves
     {
-        __amdgpu_buffer_rsrc_t r = cb.next(s0 < s1);
-        static_for<UL>([&](auto I) { request_b(r, I, o0); });
-        r = ca[0].next(s0 < s1);
-        static_for<UL>([&](auto I) { request_a(r, I, o1, s0 == nk - 1); });
-        r = ca[1].next(s0 < s1);
-        static_for<UL>([&](auto I) { request_a(r, I, o2, s0 == nk - 1); });
-        r = cb.next(s0 + 1 < s1);
-        static_for<UL>([&](auto I) { request_b(r, I, o3); });
-        r = ca[0].next(s0 + 1 < s1);
-        static_for<UL>([&](auto I) { request_a(r, I, o4, s0 + 1 == nk - 1); });
+        const __amdgpu_buffer_rsrc_t rb = cb.next(), r1 = ca[1].next(), rn = cb.next();
+        r0 = ca[0].next();
+        static_for<UL>([&](auto I) { request_b(rb, I, o0); });
+        static_for<UL>([&](auto I) { request_a(r0, I, o1, s0 == nk - 1); });
+        static_for<UL>([&](auto I) { request_a(r1, I, o2, s0 == nk - 1); });
+        static_for<UL>([&](auto I) { request_b(rn, I, o3); });
+        r0 = ca[0].next();
+        static_for<UL / 2>([&](auto I) { request_a(r0, I, o4, s0 + 1 == nk - 1); });
     }
 
     f32x16_t acc[2][4];
@@ -401,81 +418,222 @@ __global__ void __launch_bounds__(256, 2) linear_big_kernel(const GemmArgs a) {
     unsigned abase[FA::NB], bbase[FB::NB];
     FA::bases(abase, lds_addr(lds), wp * 2, lane);
     FB::bases(bbase, lds_addr(lds), wc * 2, lane);
-    FA fa[2];
+    FA fa[4];                                                   // of the four k-steps of a half: two are on their way while one is multiplied
     FB fb[4];
     auto multiply = [&](auto H, auto Q, auto &&between) {       // four products of half H, k-step Q
         constexpr int h = decltype(H)::value, q = decltype(Q)::value;
         static_for<4>([&](auto U) {
             constexpr int u = decltype(U)::value, i = u / 2, j = u % 2;
-            Mma<T>::run(acc[i][h * 2 + j], fb[q].f[i].get(), fa[q & 1].f[j].get());
+            Mma<T>::run(acc[i][h * 2 + j], fb[q].f[i].get(), fa[q].f[j].get());
             between(U);
         });
         __builtin_amdgcn_sched_barrier(0);
     };
     constexpr std::integral_constant<int, 0> C0{};
     constexpr std::integral_constant<int, 1> C1{};
+    constexpr std::integral_constant<int, 2> C2{};
     constexpr std::integral_constant<int, 3> C3{};
-    auto nothing = [](auto) {};
 
-    wait_vmcnt<3 * UL>();                                       // B and A0 of the first stage have landed
+    wait_vmcnt<2 * UL + UL / 2>();                              // B and A0 of the first stage have landed
     __builtin_amdgcn_s_barrier();
     static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value>(bbase, o0); });
+    fa[0].template read<0>(abase, o1);
+    fa[1].template read<1>(abase, o1);
     wait_lgkmcnt<0>();
     static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
-    fa[0].template read<0>(abase, o1);
+    fa[0].land();
+    fa[1].land();
 
+    // The counts of the waits: LDS reads and DMAs land in the order in which they were issued, and each wait names how many were issued behind what it waits for.
     for (int s = s0; s < s1; s++) {
-        // ---- A0
-        static_for<3>([&](auto Q) {
-            constexpr int q = decltype(Q)::value;
-            fa[(q + 1) & 1].template read<q + 1>(abase, o1);
-            wait_lds<FA::READS>();
-            if constexpr (q == 0) fb[3].land();
-            fa[q & 1].land();
-            multiply(C0, Q, nothing);
-        });
-        wait_lgkmcnt<0>();                                      // all of A0 is in registers
-        fa[1].land();
-        wait_vmcnt<UL>();                                       // A1 and the next stage's B have landed
-        __builtin_amdgcn_s_barrier();                           // ... for every wave, and nobody reads A0 and B any more
-        fa[0].template read<0>(abase, o2);
-        {
-            const __amdgpu_buffer_rsrc_t r1 = ca[1].next(s + 1 < s1), rb = cb.next(s + 2 < s1);
-            multiply(C0, C3, [&](auto U) {
-                request_a(r1, U, o0, s + 1 == nk - 1);
-                request_b(rb, U, o1);
-            });
-        }
-        // ---- A1; behind each k-step's last products its fragments of B make room for the next stage's
-        static_for<3>([&](auto Q) {
-            constexpr int q = decltype(Q)::value;
-            fa[(q + 1) & 1].template read<q + 1>(abase, o2);
-            wait_lds<FA::READS + (q ? FB::READS : 0)>();
-            fa[q & 1].land();
-            if constexpr (q == 2) fb[0].land();
-            multiply(C1, Q, nothing);
-            fb[q].template read<q>(bbase, o3);
-        });
-        wait_lds<FB::READS>();                              // all of A1 is in registers
-        fa[1].land();
+        // ---- A0 times B; the second half of the next stage's A0 is requested
+        const bool next_last = s + 1 == nk - 1, third_last = s + 2 == nk - 1;
+        fa[2].template read<2>(abase, o1);
+        wait_lds<2 * FA::READS + 2 * FB::READS>();
+        fa[0].land();
         fb[1].land();
+        multiply(C0, C0, [&](auto U) { if constexpr (U == 3) request_a(r0, C2, o4, next_last); });
+        fa[3].template read<3>(abase, o1);
+        wait_lds<2 * FA::READS + FB::READS>();
+        fa[1].land();
+        fb[2].land();
+        multiply(C0, C1, [&](auto U) { if constexpr (U == 3) request_a(r0, C3, o4, next_last); });
+        wait_lgkmcnt<0>();                                      // all of A0 and B is in registers
+        fa[2].land();
+        fa[3].land();
+        fb[3].land();
+        wait_vmcnt<UL>();                                       // A1 and the next stage's B have landed
+        __builtin_amdgcn_s_barrier();                           // ... for every wave, and nobody reads A0 and B any more: A1 and B of later stages take their slots
+        fa[0].template read<0>(abase, o2);
+        const __amdgpu_buffer_rsrc_t r1 = ca[1].next(), rb = cb.next();
+        multiply(C0, C2, [&](auto U) { if constexpr (U & 1) request_a(r1, std::integral_constant<int, U / 2>{}, o0, next_last); });
+        fa[1].template read<1>(abase, o2);
+        multiply(C0, C3, [&](auto U) { if constexpr (U & 1) request_a(r1, std::integral_constant<int, 2 + U / 2>{}, o0, next_last); });
+        // ---- A1 times B; behind each k-step's last products its fragments of B make room for the next stage's
+        fa[2].template read<2>(abase, o2);
+        wait_lds<2 * FA::READS>();
+        fa[0].land();
+        multiply(C1, C0, [&](auto U) { if constexpr (U & 1) request_b(rb, std::integral_constant<int, U / 2>{}, o1); });
+        fb[0].template read<0>(bbase, o3);
+        fa[3].template read<3>(abase, o2);
+        wait_lds<2 * FA::READS + FB::READS>();
+        fa[1].land();
+        multiply(C1, C1, [&](auto U) { if constexpr (U & 1) request_b(rb, std::integral_constant<int, 2 + U / 2>{}, o1); });
+        fb[1].template read<1>(bbase, o3);
+        wait_lds<FB::READS>();                                  // all of A1 is in registers
+        fa[2].land();
+        fa[3].land();
+        fb[0].land();
         wait_vmcnt<2 * UL>();                                   // the next stage's A0 has landed
         __builtin_amdgcn_s_barrier();
-        {
-            const __amdgpu_buffer_rsrc_t r0 = ca[0].next(s + 2 < s1);
-            fa[0].template read<0>(abase, o4);
-            multiply(C1, C3, [&](auto U) { request_a(r0, U, o2, s + 2 == nk - 1); });
-        }
+        fa[0].template read<0>(abase, o4);
+        r0 = ca[0].next();
+        multiply(C1, C2, [&](auto U) { if constexpr (U == 3) request_a(r0, C0, o2, third_last); });
+        fb[2].template read<2>(bbase, o3);
+        fa[1].template read<1>(abase, o4);
+        multiply(C1, C3, [&](auto U) { if constexpr (U == 3) request_a(r0, C1, o2, third_last); });
         fb[3].template read<3>(bbase, o3);
-        wait_lds<FA::READS + FB::READS>();
-        fb[2].land();
         const unsigned t0 = o0, t1 = o1, t2 = o2;
         o0 = o3; o1 = o4; o2 = t0; o3 = t1; o4 = t2;
     }
     wait_lgkmcnt<0>();                                          // the fragments requested behind the last stage
     fa[0].land();
-    fb[3].land();
+    fa[1].land();
+    static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
     wait_vmcnt<0>();                                            // ... and its DMAs, zeros into dead slots
+    __builtin_amdgcn_s_barrier();                               // the ring becomes the strips
+
+    W w;
+    w.init(a, lds, wave, lane, split, c0 + wc * 64);
+    static_for<4>([&](auto J) {
+        constexpr int j = decltype(J)::value;
+        w.write(a, p0 + (j >> 1) * 128 + wp * 64 + (j & 1) * 32, [&](auto I) -> const f32x16_t & { return acc[decltype(I)::value][j]; });
+    });
+#endif
+}
+
+// ---- tiles of 256 x 256 ----------------------------------------------------------------------------------------------------------
+// Eight waves in two groups of four; wave w and wave w + 4 share a SIMD.  While one group multiplies (16 matrix instructions a wave), the other reads its next
+// fragments from LDS and requests later units; a barrier, and they change places.  The matrix units always have one group's products, and neither
+// LDS reads nor the issue of DMAs (a full queue holds the wave that issues) ever stand between two products.
+// A stage (64 bf16 of k) is four units of 16 KB: A0, A1 (rows 0 .. 127, 128 .. 255), B0, B1 (columns).  A wave has 64 rows of each half and 64 columns: it multiplies A0
+// with B, then A1 with the fragments of B that it still has in registers.  The ring has ten units; A0, A1 of stage s + 2 and B0 of s + 3 take the places of B0, B1
+// and A0 of stage s, and B1 of s + 3 that of A1.
+template <typename T, GemmKind KIND>
+__global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr bool AX = KIND == GEMM_DW, BX = KIND != GEMM_FORWARD;
+    constexpr int NW = 8, ES = (int)sizeof(T), BK = ROWB / ES, UNIT = 16384, UL = UNIT / 1024 / NW, NU = 10;
+    using TA = Tile<T, AX, 128>;
+    using TB = Tile<T, BX, 128>;
+    using FA = Frags<T, AX, 128, 2>;
+    using FB = Frags<T, BX, 128, 2>;
+    using W = Writer<T, KIND, 2>;
+    static_assert(NW * W::BYTES <= NU * UNIT && UL == 2, "strips in the ring; requests per unit");
+    __shared__ __align__(1024) unsigned char lds[NU * UNIT];
+
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave & 1, wc = wave >> 1, grp = wave >> 2;
+    int split, tp, tc;
+    if (!pick_tile(a, split, tp, tc)) return;
+    const int p0 = tp * 256, c0 = tc * 256;
+    const int nk = (a.K + BK - 1) / BK, s0 = split * a.steps, s1 = min(nk, s0 + a.steps);   // this part's stages
+
+    const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES);
+    Cursor<AX, BK> ca[2];
+    Cursor<BX, BK> cb[2];
+#pragma unroll
+    for (int h = 0; h < 2; h++) {
+        ca[h].init(a.a, apitch, ES, p0 + h * 128, a.M, a.a_row, s0, s1, a.K);
+        cb[h].init(a.b, bpitch, ES, c0 + h * 128, a.N, a.b_row, s0, s1, a.K);
+    }
+    unsigned ao[UL], bo[UL], cut[UL] = {0u, 0u};
+#pragma unroll
+    for (int i = 0; i < UL; i++) {
+        ao[i] = TA::offset(wave * UL + i, lane, apitch);
+        bo[i] = TB::offset(wave * UL + i, lane, bpitch);
+        if constexpr (!AX) cut[i] = a.a_cut && TA::behind(wave * UL + i, lane, a.K * ES - (nk - 1) * ROWB) ? 0xffffffffu : 0u;
+    }
+    auto request_a = [&](int h, unsigned off, bool last) {
+        const __amdgpu_buffer_rsrc_t r = ca[h].next();
+#pragma unroll
+        for (int i = 0; i < UL; i++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, !AX ? ao[i] | (last ? cut[i] : 0u) : ao[i], 0, 0, 0);
+    };
+    auto request_b = [&](int h, unsigned off) {
+        const __amdgpu_buffer_rsrc_t r = cb[h].next();
+#pragma unroll
+        for (int i = 0; i < UL; i++)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, bo[i], 0, 0, 0);
+    };
+    request_b(0, 0 * UNIT);
+    request_b(1, 1 * UNIT);
+    request_a(0, 2 * UNIT, s0 == nk - 1);
+    request_a(1, 3 * UNIT, s0 == nk - 1);
+    request_b(0, 4 * UNIT);
+    request_b(1, 5 * UNIT);
+    request_a(0, 6 * UNIT, s0 + 1 == nk - 1);
+    request_a(1, 7 * UNIT, s0 + 1 == nk - 1);
+    request_b(0, 8 * UNIT);
+
+    f32x16_t acc[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; i++)
+#pragma unroll
+        for (int j = 0; j < 4; j++)
+#pragma unroll
+            for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
+
+    unsigned abase[FA::NB], bbase[FB::NB];
+    FA::bases(abase, lds_addr(lds), wp * 2, lane);
+    FB::bases(bbase, lds_addr(lds), (wc & 1) * 2, lane);
+    FA fa[4];
+    FB fb[4];
+    auto multiply = [&](auto H) {
+        constexpr int h = decltype(H)::value;
+        __builtin_amdgcn_s_setprio(1);
+        static_for<16>([&](auto U) {
+            constexpr int u = decltype(U)::value, q = u / 4, i = u / 2 % 2, j = u % 2;
+            Mma<T>::run(acc[i][h * 2 + j], fb[q].f[i].get(), fa[q].f[j].get());
+        });
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // Between two changes each group does one thing; the requests of both that the next reader needs have landed at every second change.
+    auto change = [&](bool landed_too) {
+        if (landed_too) wait_vmcnt<6 * UL>();
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    wait_vmcnt<6 * UL>();                                       // B and A0 of the first stage
+    __builtin_amdgcn_s_barrier();
+    if (grp) change(false);                                     // the second group runs one change behind
+
+    unsigned pos = 0;                                           // slot of B0 of this stage; B1, A0, A1 follow
+    auto slot = [&](unsigned k) { const unsigned p = pos + k * UNIT; return p >= NU * UNIT ? p - NU * UNIT : p; };
+    for (int s = s0; s < s1; s++) {
+        const unsigned ob = slot(wc >> 1), oa0 = slot(2), oa1 = slot(3);
+        static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value>(bbase, ob); });
+        static_for<4>([&](auto Q) { fa[decltype(Q)::value].template read<decltype(Q)::value>(abase, oa0); });
+        request_b(1, slot(9));                                  // of stage s + 2, where A1 of stage s - 1 was
+        wait_lgkmcnt<0>();
+        static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); fa[decltype(Q)::value].land(); });
+        change(grp == 1);
+        multiply(std::integral_constant<int, 0>{});
+        change(grp == 0);
+        static_for<4>([&](auto Q) { fa[decltype(Q)::value].template read<decltype(Q)::value>(abase, oa1); });
+        request_a(0, slot(0), s + 2 == nk - 1);                 // of stage s + 2
+        request_a(1, slot(1), s + 2 == nk - 1);
+        request_b(0, oa0);                                      // of stage s + 3
+        wait_lgkmcnt<0>();
+        static_for<4>([&](auto Q) { fa[decltype(Q)::value].land(); });
+        change(grp == 1);
+        multiply(std::integral_constant<int, 1>{});
+        change(grp == 0);
+        pos = slot(4);
+    }
+    if (!grp) change(false);
+    wait_vmcnt<0>();                                            // the DMAs behind the last stage, zeros into dead slots
     __builtin_amdgcn_s_barrier();                               // the ring becomes the strips
 
     W w;
@@ -504,6 +662,13 @@ template <typename T, GemmKind KIND, int WP, int WC, int TP, int TC, int NS, int
 
 template <typename T, GemmKind KIND> static sol_status launch_kind(GemmArgs a, int dt, hipStream_t st) {
     const long big = (long)ceil_div(a.M, 256) * ceil_div(a.N, 128) * a.nsplit, mid = (long)ceil_div(a.M, 128) * ceil_div(a.N, 128) * a.nsplit;
+    const long huge = (long)ceil_div(a.M, 256) * ceil_div(a.N, 256) * a.nsplit;
+    if (huge >= 200) {
+        const long blocks = tiles_of(a, dt, 256, 256);
+        hipLaunchKernelGGL((linear_huge_kernel<T, KIND>), dim3((unsigned)blocks), dim3(512), 0, st, a);
+        SOL_HIP(hipGetLastError());
+        return SOL_OK;
+    }
     if (big >= 400) {
         const long blocks = tiles_of(a, dt, 256, 128);
         hipLaunchKernelGGL((linear_big_kernel<T, KIND>), dim3((unsigned)blocks), dim3(256), 0, st, a);

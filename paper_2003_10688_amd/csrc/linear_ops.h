@@ -197,7 +197,7 @@ __device__ __forceinline__ void load_bias8(const float *bias, int n, int nv, flo
 struct GemmArgs {
     const void *a, *b;
     long lda, ldb;
-    size_t a_bytes, b_bytes;    // from the base to the last byte that may be read
+    int a_row, b_row;           // bytes of a row that may be read (the pitch where it is this library's own buffer)
     int a_cut;                  // A, stored along k: elements >= K of a row are not zeros and have to be masked
     int M, N, K;
     int nsplit;                 // > 1: the reduction in so many parts; part s goes to `part` + s * M * N (fp32, dense), nothing else is written
