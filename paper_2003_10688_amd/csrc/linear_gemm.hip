@@ -533,7 +533,7 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
     __shared__ __align__(1024) unsigned char lds[NU * UNIT];
 
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave & 1, wc = wave >> 1, grp = wave >> 2;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave & 1, wc = wave >> 1;
     int split, tp, tc;
     if (!pick_tile(a, split, tp, tc)) return;
     const int p0 = tp * 256, c0 = tc * 256;
@@ -554,27 +554,24 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
         bo[i] = TB::offset(wave * UL + i, lane, bpitch);
         if constexpr (!AX) cut[i] = a.a_cut && TA::behind(wave * UL + i, lane, a.K * ES - (nk - 1) * ROWB) ? 0xffffffffu : 0u;
     }
-    auto request_a = [&](int h, unsigned off, bool last) {
-        const __amdgpu_buffer_rsrc_t r = ca[h].next();
-#pragma unroll
-        for (int i = 0; i < UL; i++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, !AX ? ao[i] | (last ? cut[i] : 0u) : ao[i], 0, 0, 0);
+    auto request_a = [&](const __amdgpu_buffer_rsrc_t &r, auto I, unsigned off, bool last) {
+        constexpr int i = decltype(I)::value;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, !AX ? ao[i] | (last ? cut[i] : 0u) : ao[i], 0, 0, 0);
     };
-    auto request_b = [&](int h, unsigned off) {
-        const __amdgpu_buffer_rsrc_t r = cb[h].next();
-#pragma unroll
-        for (int i = 0; i < UL; i++)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, bo[i], 0, 0, 0);
+    auto request_b = [&](const __amdgpu_buffer_rsrc_t &r, auto I, unsigned off) {
+        constexpr int i = decltype(I)::value;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, bo[i], 0, 0, 0);
     };
-    request_b(0, 0 * UNIT);
-    request_b(1, 1 * UNIT);
-    request_a(0, 2 * UNIT, s0 == nk - 1);
-    request_a(1, 3 * UNIT, s0 == nk - 1);
-    request_b(0, 4 * UNIT);
-    request_b(1, 5 * UNIT);
-    request_a(0, 6 * UNIT, s0 + 1 == nk - 1);
-    request_a(1, 7 * UNIT, s0 + 1 == nk - 1);
-    request_b(0, 8 * UNIT);
+#pragma unroll
+    for (int u = 0; u < NU; u++) {                              // unit u: stage u / 4, B0, B1, A0, A1 in turn
+        if (u % 4 < 2) {
+            const __amdgpu_buffer_rsrc_t r = cb[u % 4].next();
+            static_for<UL>([&](auto I) { request_b(r, I, u * UNIT); });
+        } else {
+            const __amdgpu_buffer_rsrc_t r = ca[u % 4 - 2].next();
+            static_for<UL>([&](auto I) { request_a(r, I, u * UNIT, s0 + u / 4 == nk - 1); });
+        }
+    }
 
     f32x16_t acc[2][4];
 #pragma unroll
@@ -587,53 +584,92 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
     unsigned abase[FA::NB], bbase[FB::NB];
     FA::bases(abase, lds_addr(lds), wp * 2, lane);
     FB::bases(bbase, lds_addr(lds), (wc & 1) * 2, lane);
-    FA fa[4];
+    FA fa[4];                                                   // of the four k-steps of a half: two are on their way while one is multiplied
     FB fb[4];
-    auto multiply = [&](auto H) {
-        constexpr int h = decltype(H)::value;
-        __builtin_amdgcn_s_setprio(1);
-        static_for<16>([&](auto U) {
-            constexpr int u = decltype(U)::value, q = u / 4, i = u / 2 % 2, j = u % 2;
+    auto multiply = [&](auto H, auto Q, auto &&between) {       // four products of half H, k-step Q
+        constexpr int h = decltype(H)::value, q = decltype(Q)::value;
+        static_for<4>([&](auto U) {
+            constexpr int u = decltype(U)::value, i = u / 2, j = u % 2;
             Mma<T>::run(acc[i][h * 2 + j], fb[q].f[i].get(), fa[q].f[j].get());
+            between(U);
         });
-        __builtin_amdgcn_s_setprio(0);
         __builtin_amdgcn_sched_barrier(0);
     };
-    // Between two changes each group does one thing; the requests of both that the next reader needs have landed at every second change.
-    auto change = [&](bool landed_too) {
-        if (landed_too) wait_vmcnt<6 * UL>();
-        __builtin_amdgcn_s_barrier();
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    wait_vmcnt<6 * UL>();                                       // B and A0 of the first stage
-    __builtin_amdgcn_s_barrier();
-    if (grp) change(false);                                     // the second group runs one change behind
+    constexpr std::integral_constant<int, 0> C0{};
+    constexpr std::integral_constant<int, 1> C1{};
+    constexpr std::integral_constant<int, 2> C2{};
+    constexpr std::integral_constant<int, 3> C3{};
+    auto nothing = [](auto) {};
 
-    unsigned pos = 0;                                           // slot of B0 of this stage; B1, A0, A1 follow
+    unsigned pos = 0;                                           // slot of B0 of this stage; B1, A0, A1 and the next stage's follow
     auto slot = [&](unsigned k) { const unsigned p = pos + k * UNIT; return p >= NU * UNIT ? p - NU * UNIT : p; };
+    wait_vmcnt<7 * UL>();                                       // B and A0 of the first stage have landed
+    __builtin_amdgcn_s_barrier();
+    static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value>(bbase, slot(wc >> 1)); });
+    fa[0].template read<0>(abase, slot(2));
+    fa[1].template read<1>(abase, slot(2));
+    wait_lgkmcnt<0>();
+    static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
+    fa[0].land();
+    fa[1].land();
+
+    // The counts of the waits: LDS reads and DMAs land in the order in which they were issued, and each wait names how many were issued behind what it waits for.
     for (int s = s0; s < s1; s++) {
-        const unsigned ob = slot(wc >> 1), oa0 = slot(2), oa1 = slot(3);
-        static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value>(bbase, ob); });
-        static_for<4>([&](auto Q) { fa[decltype(Q)::value].template read<decltype(Q)::value>(abase, oa0); });
-        request_b(1, slot(9));                                  // of stage s + 2, where A1 of stage s - 1 was
-        wait_lgkmcnt<0>();
-        static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); fa[decltype(Q)::value].land(); });
-        change(grp == 1);
-        multiply(std::integral_constant<int, 0>{});
-        change(grp == 0);
-        static_for<4>([&](auto Q) { fa[decltype(Q)::value].template read<decltype(Q)::value>(abase, oa1); });
-        request_a(0, slot(0), s + 2 == nk - 1);                 // of stage s + 2
-        request_a(1, slot(1), s + 2 == nk - 1);
-        request_b(0, oa0);                                      // of stage s + 3
-        wait_lgkmcnt<0>();
-        static_for<4>([&](auto Q) { fa[decltype(Q)::value].land(); });
-        change(grp == 1);
-        multiply(std::integral_constant<int, 1>{});
-        change(grp == 0);
+        const unsigned oa0 = slot(2), oa1 = slot(3), obn = slot(4 + (wc >> 1)), oan = slot(6);
+        // ---- A0 times B
+        fa[2].template read<2>(abase, oa0);
+        wait_lds<2 * FA::READS + 2 * FB::READS>();
+        fa[0].land();
+        fb[1].land();
+        multiply(C0, C0, nothing);
+        fa[3].template read<3>(abase, oa0);
+        wait_lds<2 * FA::READS + FB::READS>();
+        fa[1].land();
+        fb[2].land();
+        multiply(C0, C1, nothing);
+        wait_lgkmcnt<0>();                                      // all of A0 and B is in registers
+        fa[2].land();
+        fa[3].land();
+        fb[3].land();
+        wait_vmcnt<4 * UL>();                                   // A1 and the next stage's B have landed
+        __builtin_amdgcn_s_barrier();                           // ... for every wave, and nobody reads A0 and B any more: units of later stages take their slots
+        fa[0].template read<0>(abase, oa1);
+        const bool last = s + 2 == nk - 1;
+        const __amdgpu_buffer_rsrc_t r0 = ca[0].next(), r1 = ca[1].next(), rb0 = cb[0].next();
+        multiply(C0, C2, [&](auto U) { if constexpr (U & 1) request_a(r0, std::integral_constant<int, U / 2>{}, slot(0), last); });
+        fa[1].template read<1>(abase, oa1);
+        multiply(C0, C3, [&](auto U) { if constexpr (U == 1) request_a(r1, C0, slot(1), last); });
+        // ---- A1 times B; behind each k-step's last products its fragments of B make room for the next stage's
+        fa[2].template read<2>(abase, oa1);
+        wait_lds<2 * FA::READS>();
+        fa[0].land();
+        multiply(C1, C0, [&](auto U) { if constexpr (U == 1) request_a(r1, C1, slot(1), last); if constexpr (U == 3) request_b(rb0, C0, slot(2)); });
+        fb[0].template read<0>(bbase, obn);
+        fa[3].template read<3>(abase, oa1);
+        wait_lds<2 * FA::READS + FB::READS>();
+        fa[1].land();
+        multiply(C1, C1, [&](auto U) { if constexpr (U == 1) request_b(rb0, C1, slot(2)); });
+        fb[1].template read<1>(bbase, obn);
+        wait_lds<FB::READS>();                                  // all of A1 is in registers
+        fa[2].land();
+        fa[3].land();
+        fb[0].land();
+        wait_vmcnt<6 * UL>();                                   // the next stage's A0 has landed
+        __builtin_amdgcn_s_barrier();
+        fa[0].template read<0>(abase, oan);
+        const __amdgpu_buffer_rsrc_t rb1 = cb[1].next();
+        multiply(C1, C2, [&](auto U) { if constexpr (U == 1) request_b(rb1, C0, oa1); });
+        fb[2].template read<2>(bbase, obn);
+        fa[1].template read<1>(abase, oan);
+        multiply(C1, C3, [&](auto U) { if constexpr (U == 1) request_b(rb1, C1, oa1); });
+        fb[3].template read<3>(bbase, obn);
         pos = slot(4);
     }
-    if (!grp) change(false);
-    wait_vmcnt<0>();                                            // the DMAs behind the last stage, zeros into dead slots
+    wait_lgkmcnt<0>();                                          // the fragments requested behind the last stage
+    fa[0].land();
+    fa[1].land();
+    static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
+    wait_vmcnt<0>();                                            // ... and its DMAs, zeros into dead slots
     __builtin_amdgcn_s_barrier();                               // the ring becomes the strips
 
     W w;
