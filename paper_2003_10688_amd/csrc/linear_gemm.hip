@@ -164,8 +164,10 @@ __device__ __forceinline__ bool pick_tile(const GemmArgs &a, int &split, int &tp
     const int bid = (int)blockIdx.x - split * per * 8, t = (bid & 7) * per + (bid >> 3);
     if (t >= ntiles) return false;
     const int g = t / (8 * a.ntc), in = t - g * 8 * a.ntc, rows = min(8, a.ntp - g * 8);
-    tp = g * 8 + in % rows;
-    tc = in / rows;
+    // divisions run on the vector units: back to scalars, or every resource derived from them would be taken for different ones per lane
+    tp = __builtin_amdgcn_readfirstlane(g * 8 + in % rows);
+    tc = __builtin_amdgcn_readfirstlane(in / rows);
+    split = __builtin_amdgcn_readfirstlane(split);
     return true;
 }
 
@@ -513,12 +515,46 @@ __global__ void __launch_bounds__(256, 2) linear_big_kernel(const GemmArgs a) {
 }
 
 // ---- tiles of 256 x 256 ----------------------------------------------------------------------------------------------------------
-// Eight waves in two groups of four; wave w and wave w + 4 share a SIMD.  While one group multiplies (16 matrix instructions a wave), the other reads its next
-// fragments from LDS and requests later units; a barrier, and they change places.  The matrix units always have one group's products, and neither
-// LDS reads nor the issue of DMAs (a full queue holds the wave that issues) ever stand between two products.
-// A stage (64 bf16 of k) is four units of 16 KB: A0, A1 (rows 0 .. 127, 128 .. 255), B0, B1 (columns).  A wave has 64 rows of each half and 64 columns: it multiplies A0
-// with B, then A1 with the fragments of B that it still has in registers.  The ring has ten units; A0, A1 of stage s + 2 and B0 of s + 3 take the places of B0, B1
-// and A0 of stage s, and B1 of s + 3 that of A1.
+// One workgroup of eight waves per CU: a row or column fetched once serves 256 of the other operand, 32 bytes a clock at the full rate of the matrix units, where the path
+// from L2 to LDS gives 58 (with two workgroups of 256 x 128 it was 48, and their waves stood behind their own requests).
+// A stage is four units of 16 KB: B0, B1 (columns 0 .. 127, 128 .. 255), A0, A1 (rows).  A wave has 64 rows of each half of A and 64 columns: it takes its fragments of B into
+// registers once, multiplies A0, then A1, with them, and behind each k-step's last products reads the next stage's over them.  The ring has ten units; A0, A1 of
+// stage s + 2 and B0 of s + 3 take the places of B0, B1 and A0 of stage s, and B1 of s + 3 that of A1, so every unit is requested one and a half stages (48 matrix instructions of a wave)
+// before it is needed.
+// The two waves of a SIMD issue one instruction each at a time, and everything that is not a product has to fit beside the products: resources and lane offsets are
+// constants of the loop (a scalar offset moves along the reduction, and the range check includes it), and the loop is unrolled over the five stages after which the ring repeats.
+template <int OFF> __device__ __forceinline__ unsigned add_const(unsigned v) {     // opaque: or sixty sums would be kept in registers across the loop
+    unsigned d;
+    asm volatile("v_add_u32_e32 %0, %1, %2" : "=v"(d) : "n"(OFF), "v"(v));
+    return d;
+}
+
+// Fragments of one k-step of a unit at a constant place.  at[]: along k, the first block's place for each of the four k-steps; across, each block's for the first.
+template <typename T, bool ACROSS> struct UnitFrags {
+    using TL = Tile<T, ACROSS, 128>;
+    static constexpr int NB = ACROSS ? 2 : 4, READS = 2 * Frag<T, ACROSS>::READS;
+    Frag<T, ACROSS> f[2];
+    static __device__ __forceinline__ void places(unsigned (&at)[NB], unsigned lds, int blk, int lane) {
+#pragma unroll
+        for (int i = 0; i < NB; i++) at[i] = ACROSS ? lds + TL::frag(blk + i, lane) : lds + (TL::frag(blk, lane) ^ (unsigned)(i << 5));
+    }
+    template <int Q, int OFF> __device__ __forceinline__ void read(const unsigned (&at)[NB]) {
+        static_for<2>([&](auto I) {
+            constexpr int i = decltype(I)::value, off = ACROSS ? Q *(TL::BK / 4) * TL::RB : i * 32 * ROWB, room = 65536 - (ACROSS ? 4 * TL::RB : 0);
+            if constexpr (OFF + off < room) f[i].template read<OFF + off, TL::RB>(at[ACROSS ? i : Q]);
+            else f[i].template read<off, TL::RB>(add_const<OFF>(at[ACROSS ? i : Q]));
+        });
+    }
+    __device__ __forceinline__ void land() { f[0].land(); f[1].land(); }
+};
+
+// Bytes from the corner of a unit (its first row, or column, is `first` of `limit`) to the end of what may be read
+__device__ __forceinline__ unsigned unit_bytes(bool across, int es, int first, int limit, int K, unsigned pitch, int row_bytes) {
+    if (across) return row_bytes > first * es ? (unsigned)(K - 1) * pitch + (unsigned)(row_bytes - first * es) : 0u;
+    const int rows = min(128, limit - first);
+    return rows > 0 ? (unsigned)(rows - 1) * pitch + (unsigned)row_bytes : 0u;
+}
+
 template <typename T, GemmKind KIND>
 __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -526,8 +562,8 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
     constexpr int NW = 8, ES = (int)sizeof(T), BK = ROWB / ES, UNIT = 16384, UL = UNIT / 1024 / NW, NU = 10;
     using TA = Tile<T, AX, 128>;
     using TB = Tile<T, BX, 128>;
-    using FA = Frags<T, AX, 128, 2>;
-    using FB = Frags<T, BX, 128, 2>;
+    using FA = UnitFrags<T, AX>;
+    using FB = UnitFrags<T, BX>;
     using W = Writer<T, KIND, 2>;
     static_assert(NW * W::BYTES <= NU * UNIT && UL == 2, "strips in the ring; requests per unit");
     __shared__ __align__(1024) unsigned char lds[NU * UNIT];
@@ -536,41 +572,49 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave & 1, wc = wave >> 1;
     int split, tp, tc;
     if (!pick_tile(a, split, tp, tc)) return;
-    const int p0 = tp * 256, c0 = tc * 256;
-    const int nk = (a.K + BK - 1) / BK, s0 = split * a.steps, s1 = min(nk, s0 + a.steps);   // this part's stages
+    const int p0 = tp * 256, c0 = tc * 256, nk = (a.K + BK - 1) / BK;
 
-    const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES);
-    Cursor<AX, BK> ca[2];
-    Cursor<BX, BK> cb[2];
+    const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES), astep = AX ? BK * apitch : ROWB, bstep = BX ? BK * bpitch : ROWB;
+    __amdgpu_buffer_rsrc_t ra[2], rb[2];
 #pragma unroll
     for (int h = 0; h < 2; h++) {
-        ca[h].init(a.a, apitch, ES, p0 + h * 128, a.M, a.a_row, s0, s1, a.K);
-        cb[h].init(a.b, bpitch, ES, c0 + h * 128, a.N, a.b_row, s0, s1, a.K);
+        const int p = p0 + h * 128, c = c0 + h * 128;
+        ra[h] = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(static_cast<const unsigned char *>(a.a) + (size_t)p * (AX ? ES : apitch)), 0,
+                                                  (int)unit_bytes(AX, ES, p, a.M, a.K, apitch, a.a_row), 0x00020000);
+        rb[h] = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(static_cast<const unsigned char *>(a.b) + (size_t)c * (BX ? ES : bpitch)), 0,
+                                                  (int)unit_bytes(BX, ES, c, a.N, a.K, bpitch, a.b_row), 0x00020000);
     }
-    unsigned ao[UL], bo[UL], cut[UL] = {0u, 0u};
+    unsigned ao[UL], bo[UL];
 #pragma unroll
     for (int i = 0; i < UL; i++) {
         ao[i] = TA::offset(wave * UL + i, lane, apitch);
         bo[i] = TB::offset(wave * UL + i, lane, bpitch);
-        if constexpr (!AX) cut[i] = a.a_cut && TA::behind(wave * UL + i, lane, a.K * ES - (nk - 1) * ROWB) ? 0xffffffffu : 0u;
     }
-    auto request_a = [&](const __amdgpu_buffer_rsrc_t &r, auto I, unsigned off, bool last) {
-        constexpr int i = decltype(I)::value;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, !AX ? ao[i] | (last ? cut[i] : 0u) : ao[i], 0, 0, 0);
+    // A along k whose rows do not end with zeros: from the last stage on, the slots behind K are out of range
+    auto cut_last = [&](int stage) {
+        if constexpr (!AX) {
+            if (stage == nk - 1 && a.a_cut) {
+#pragma unroll
+                for (int i = 0; i < UL; i++) ao[i] |= TA::behind(wave * UL + i, lane, a.K * ES - (nk - 1) * ROWB) ? 0xffffffffu : 0u;
+            }
+        }
     };
-    auto request_b = [&](const __amdgpu_buffer_rsrc_t &r, auto I, unsigned off) {
+    unsigned char *const mine = lds + wave * UL * 1024;         // where this wave's part of a unit goes
+    auto request_a = [&](int h, auto I, int unit, unsigned soff) {
         constexpr int i = decltype(I)::value;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, bo[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra[h], (__attribute__((address_space(3))) void *)(mine + unit * UNIT + i * 1024), 16, ao[i], soff, 0, 0);
+    };
+    auto request_b = [&](int h, auto I, int unit, unsigned soff) {
+        constexpr int i = decltype(I)::value;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb[h], (__attribute__((address_space(3))) void *)(mine + unit * UNIT + i * 1024), 16, bo[i], soff, 0, 0);
     };
 #pragma unroll
-    for (int u = 0; u < NU; u++) {                              // unit u: stage u / 4, B0, B1, A0, A1 in turn
-        if (u % 4 < 2) {
-            const __amdgpu_buffer_rsrc_t r = cb[u % 4].next();
-            static_for<UL>([&](auto I) { request_b(r, I, u * UNIT); });
-        } else {
-            const __amdgpu_buffer_rsrc_t r = ca[u % 4 - 2].next();
-            static_for<UL>([&](auto I) { request_a(r, I, u * UNIT, s0 + u / 4 == nk - 1); });
-        }
+    for (int u = 0; u < NU - 1; u++) {                          // unit u: stage u / 4, B0, B1, A0, A1 in turn
+        if (u % 4 == 2) cut_last(u / 4);
+        static_for<UL>([&](auto I) {
+            if (u % 4 < 2) request_b(u % 4, I, u, (unsigned)(u / 4) * bstep);
+            else request_a(u % 4 - 2, I, u, (unsigned)(u / 4) * astep);
+        });
     }
 
     f32x16_t acc[2][4];
@@ -581,17 +625,17 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
 #pragma unroll
             for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
 
-    unsigned abase[FA::NB], bbase[FB::NB];
-    FA::bases(abase, lds_addr(lds), wp * 2, lane);
-    FB::bases(bbase, lds_addr(lds), (wc & 1) * 2, lane);
+    unsigned aat[FA::NB], bat[FB::NB];
+    FA::places(aat, lds_addr(lds), wp * 2, lane);
+    FB::places(bat, lds_addr(lds) + (wc >> 1) * UNIT, (wc & 1) * 2, lane);       // B1 lies behind B0, except where the ring's end is between them: never, units go in twos
     FA fa[4];                                                   // of the four k-steps of a half: two are on their way while one is multiplied
     FB fb[4];
-    auto multiply = [&](auto H, auto Q, auto &&between) {       // four products of half H, k-step Q
+    auto multiply = [&](auto H, auto Q, auto &&request) {       // four products of half H, k-step Q, and a request among them
         constexpr int h = decltype(H)::value, q = decltype(Q)::value;
         static_for<4>([&](auto U) {
             constexpr int u = decltype(U)::value, i = u / 2, j = u % 2;
             Mma<T>::run(acc[i][h * 2 + j], fb[q].f[i].get(), fa[q].f[j].get());
-            between(U);
+            if constexpr (u == 1) request();
         });
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -599,77 +643,89 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
     constexpr std::integral_constant<int, 1> C1{};
     constexpr std::integral_constant<int, 2> C2{};
     constexpr std::integral_constant<int, 3> C3{};
-    auto nothing = [](auto) {};
 
-    unsigned pos = 0;                                           // slot of B0 of this stage; B1, A0, A1 and the next stage's follow
-    auto slot = [&](unsigned k) { const unsigned p = pos + k * UNIT; return p >= NU * UNIT ? p - NU * UNIT : p; };
-    wait_vmcnt<7 * UL>();                                       // B and A0 of the first stage have landed
+    wait_vmcnt<6 * UL>();                                       // B and A0 of the first stage have landed
     __builtin_amdgcn_s_barrier();
-    static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value>(bbase, slot(wc >> 1)); });
-    fa[0].template read<0>(abase, slot(2));
-    fa[1].template read<1>(abase, slot(2));
+    static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value, 0>(bat); });
+    fa[0].template read<0, 2 * UNIT>(aat);
+    fa[1].template read<1, 2 * UNIT>(aat);
     wait_lgkmcnt<0>();
     static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
     fa[0].land();
     fa[1].land();
 
     // The counts of the waits: LDS reads and DMAs land in the order in which they were issued, and each wait names how many were issued behind what it waits for.
-    for (int s = s0; s < s1; s++) {
-        const unsigned oa0 = slot(2), oa1 = slot(3), obn = slot(4 + (wc >> 1)), oan = slot(6);
+    // One request per k-step and wave: a request holds its wave while the queue is full, and two at a time from eight waves fill it.
+    unsigned asoff = 2 * astep, bsoff = 2 * bstep;              // of stage s + 2
+    auto stage = [&](auto P, int s) {
+        constexpr int p = decltype(P)::value;
+        constexpr auto at = [](int k) { return (p * 4 + k) % NU; };      // unit k from this stage's B0 on
+        constexpr int A0 = at(2) * UNIT, A1 = at(3) * UNIT, BN = at(4) * UNIT, AN = at(6) * UNIT;
         // ---- A0 times B
-        fa[2].template read<2>(abase, oa0);
+        fa[2].template read<2, A0>(aat);
         wait_lds<2 * FA::READS + 2 * FB::READS>();
         fa[0].land();
         fb[1].land();
-        multiply(C0, C0, nothing);
-        fa[3].template read<3>(abase, oa0);
+        multiply(C0, C0, [&] { request_b(1, C0, at(9), bsoff); });
+        fa[3].template read<3, A0>(aat);
         wait_lds<2 * FA::READS + FB::READS>();
         fa[1].land();
         fb[2].land();
-        multiply(C0, C1, nothing);
+        multiply(C0, C1, [&] { request_b(1, C1, at(9), bsoff); });
         wait_lgkmcnt<0>();                                      // all of A0 and B is in registers
         fa[2].land();
         fa[3].land();
         fb[3].land();
         wait_vmcnt<4 * UL>();                                   // A1 and the next stage's B have landed
         __builtin_amdgcn_s_barrier();                           // ... for every wave, and nobody reads A0 and B any more: units of later stages take their slots
-        fa[0].template read<0>(abase, oa1);
-        const bool last = s + 2 == nk - 1;
-        const __amdgpu_buffer_rsrc_t r0 = ca[0].next(), r1 = ca[1].next(), rb0 = cb[0].next();
-        multiply(C0, C2, [&](auto U) { if constexpr (U & 1) request_a(r0, std::integral_constant<int, U / 2>{}, slot(0), last); });
-        fa[1].template read<1>(abase, oa1);
-        multiply(C0, C3, [&](auto U) { if constexpr (U == 1) request_a(r1, C0, slot(1), last); });
+        fa[0].template read<0, A1>(aat);
+        cut_last(s + 2);
+        multiply(C0, C2, [&] { request_a(0, C0, at(0), asoff); });
+        fa[1].template read<1, A1>(aat);
+        multiply(C0, C3, [&] { request_a(0, C1, at(0), asoff); });
         // ---- A1 times B; behind each k-step's last products its fragments of B make room for the next stage's
-        fa[2].template read<2>(abase, oa1);
+        fa[2].template read<2, A1>(aat);
         wait_lds<2 * FA::READS>();
         fa[0].land();
-        multiply(C1, C0, [&](auto U) { if constexpr (U == 1) request_a(r1, C1, slot(1), last); if constexpr (U == 3) request_b(rb0, C0, slot(2)); });
-        fb[0].template read<0>(bbase, obn);
-        fa[3].template read<3>(abase, oa1);
+        multiply(C1, C0, [&] { request_a(1, C0, at(1), asoff); });
+        fb[0].template read<0, BN>(bat);
+        fa[3].template read<3, A1>(aat);
         wait_lds<2 * FA::READS + FB::READS>();
         fa[1].land();
-        multiply(C1, C1, [&](auto U) { if constexpr (U == 1) request_b(rb0, C1, slot(2)); });
-        fb[1].template read<1>(bbase, obn);
+        multiply(C1, C1, [&] { request_a(1, C1, at(1), asoff); });
+        fb[1].template read<1, BN>(bat);
         wait_lds<FB::READS>();                                  // all of A1 is in registers
         fa[2].land();
         fa[3].land();
         fb[0].land();
-        wait_vmcnt<6 * UL>();                                   // the next stage's A0 has landed
+        wait_vmcnt<5 * UL>();                                   // the next stage's A0 has landed
         __builtin_amdgcn_s_barrier();
-        fa[0].template read<0>(abase, oan);
-        const __amdgpu_buffer_rsrc_t rb1 = cb[1].next();
-        multiply(C1, C2, [&](auto U) { if constexpr (U == 1) request_b(rb1, C0, oa1); });
-        fb[2].template read<2>(bbase, obn);
-        fa[1].template read<1>(abase, oan);
-        multiply(C1, C3, [&](auto U) { if constexpr (U == 1) request_b(rb1, C1, oa1); });
-        fb[3].template read<3>(bbase, obn);
-        pos = slot(4);
+        fa[0].template read<0, AN>(aat);
+        asoff += astep;
+        bsoff += bstep;
+        multiply(C1, C2, [&] { request_b(0, C0, at(2), bsoff); });
+        fb[2].template read<2, BN>(bat);
+        fa[1].template read<1, AN>(aat);
+        multiply(C1, C3, [&] { request_b(0, C1, at(2), bsoff); });
+        fb[3].template read<3, BN>(bat);
+    };
+    for (int s = 0;;) {
+        stage(C0, s);
+        if (++s >= nk) break;
+        stage(C1, s);
+        if (++s >= nk) break;
+        stage(C2, s);
+        if (++s >= nk) break;
+        stage(C3, s);
+        if (++s >= nk) break;
+        stage(std::integral_constant<int, 4>{}, s);
+        if (++s >= nk) break;
     }
     wait_lgkmcnt<0>();                                          // the fragments requested behind the last stage
     fa[0].land();
     fa[1].land();
     static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
-    wait_vmcnt<0>();                                            // ... and its DMAs, zeros into dead slots
+    wait_vmcnt<0>();                                            // ... and its DMAs into dead slots
     __builtin_amdgcn_s_barrier();                               // the ring becomes the strips
 
     W w;
@@ -699,7 +755,9 @@ template <typename T, GemmKind KIND, int WP, int WC, int TP, int TC, int NS, int
 template <typename T, GemmKind KIND> static sol_status launch_kind(GemmArgs a, int dt, hipStream_t st) {
     const long big = (long)ceil_div(a.M, 256) * ceil_div(a.N, 128) * a.nsplit, mid = (long)ceil_div(a.M, 128) * ceil_div(a.N, 128) * a.nsplit;
     const long huge = (long)ceil_div(a.M, 256) * ceil_div(a.N, 256) * a.nsplit;
-    if (huge >= 200) {
+    const double abytes = KIND == GEMM_DW ? ((double)a.K + 256) * a.lda * sizeof(T) : 256.0 * a.lda * sizeof(T);
+    const double bbytes = KIND != GEMM_FORWARD ? ((double)a.K + 256) * a.ldb * sizeof(T) : 256.0 * a.ldb * sizeof(T);
+    if (huge >= 200 && a.nsplit <= 1 && abytes < 4294967296.0 && bbytes < 4294967296.0) {       // 32-bit offsets along the reduction
         const long blocks = tiles_of(a, dt, 256, 256);
         hipLaunchKernelGGL((linear_huge_kernel<T, KIND>), dim3((unsigned)blocks), dim3(512), 0, st, a);
         SOL_HIP(hipGetLastError());
