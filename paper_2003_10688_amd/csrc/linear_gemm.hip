@@ -4,15 +4,14 @@
 //   dx       = dz W        A = dz [m][out]  along k    B = W  [out][in]  across k
 //   dW       = dz^T x      A = dz [m][out]  across k   B = x  [m][in]    across k
 //
-// Four waves share a tile of rows x columns; stages of 128 bytes of reduction per row (64 bf16, 32 fp32) travel memory -> LDS by DMA
-// through a ring, each wave multiplies its quarter with 32x32 matrix instructions.
-// An operand along k lies in LDS as rows of 128 bytes, read as 16-byte fragments; one across k lies as it is in memory, rows of
-// columns, and is transposed on the way to registers (ds_read_b64_tr_b16 for bf16, four 4-byte reads for fp32), so no transposed copy of W, dz or x is
-// ever made.  Slots are permuted on the global side of the DMA so that neither kind of read meets a bank twice.
+// The waves of a workgroup share a tile of rows x columns; stages of 128 bytes of reduction per row (64 bf16, 32 fp32) travel memory -> LDS by DMA through a
+// ring, and each wave multiplies its part with 16x16 matrix instructions.
+// An operand along k lies in LDS as rows of 128 bytes, read as 16-byte fragments; one across k lies as it is in memory, rows of columns, and is transposed on the
+// way to registers (ds_read_b64_tr_b16 for bf16, four 4-byte reads for fp32), so no transposed copy of W, dz or x is ever made.  Slots are permuted on the global
+// side of the DMA so that neither kind of read meets a bank twice.
 //
-// Why two workgroups of four waves per CU, and not one of eight on a tile twice as large: every wave of a workgroup waits at the
-// same barrier, starts up and writes its results at the same time, and nothing multiplies meanwhile; two workgroups drift apart, and one's
-// epilogue (activation, dropout's generator: up to 15 % of the products' time on the vector units) runs beside the other's products.
+// Why 16x16x32 and not 32x32x16: large products run at the card's power limit, not at its clock, and on values as they occur a loop of nothing but 16x16x32
+// instructions sustains 2.00 PFLOP/s where 32x32x16 sustains 1.76 (on zeros both reach 2.4): an accumulator is read and written half as often.
 #include "linear_ops.h"
 
 namespace sol {
@@ -24,7 +23,7 @@ typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
 // All but the last N LDS reads have landed (they land in order; the counter has four bits, and waiting for more than needed is right too).
 template <int N> __device__ __forceinline__ void wait_lds() { wait_lgkmcnt<(N < 15 ? N : 15)>(); }
 
-// One fragment: 16 bytes of reduction of one row or column per lane.  bf16 across k arrives in two halves.
+// One fragment: 64 bytes of reduction of 16 rows or columns, 16 bytes per lane: row lane % 16, elements from 16 bytes' worth times lane / 16 on.  bf16 across k arrives in two halves.
 template <typename T, bool ACROSS> struct Frag;
 template <typename T> struct Frag<T, false> {
     u32x4_t v;
@@ -64,11 +63,11 @@ template <typename T, bool ACROSS, int BR> struct Tile {
     static constexpr int ES = (int)sizeof(T), BK = ROWB / ES, RB = ACROSS ? BR * ES : ROWB;     // bytes of a row in LDS
     static constexpr int BYTES = BR * ROWB, SEGS = BYTES / 1024;                                // DMA instructions of 64 lanes x 16 bytes
 
-    // permutation of the 16-byte slots of a row across k: transposing reads take 64 bytes of four neighbouring rows at once, 4-byte reads
-    // 128 bytes of rows k and k + 4
+    // Permutation of the 16-byte slots of a row across k.  32 lanes of a transposing read take 32 bytes of each of rows k .. k + 3 and k + 8 .. k + 11, those of a 4-byte read
+    // 64 bytes of rows k and k + 4 (of 64 lanes: k + 8, k + 12 too).
     static __device__ __forceinline__ int permute(int k) {
-        if constexpr (ES == 2) return RB >= 256 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
-        else return RB >= 256 ? ((k >> 2) & 1) << 3 : 0;
+        if constexpr (ES == 2) return (RB >= 256 ? (k & 3) << 2 : (k >> 1 & 1) << 2) | (k >> 3 & 1) << 1;
+        else return (k >> 2 & 3) << 2;
     }
     // byte offset, from the tile's corner in memory, of what this lane's part of DMA instruction `seg` brings
     static __device__ __forceinline__ unsigned offset(int seg, int lane, unsigned pitch) {
@@ -82,56 +81,135 @@ template <typename T, bool ACROSS, int BR> struct Tile {
     }
     // along k: whether what that instruction brings of the last stage lies behind `bytes` of it
     static __device__ __forceinline__ bool behind(int seg, int lane, int bytes) { return (((lane & 7) ^ swz<ROWB>(seg * 8 + (lane >> 3))) << 4) >= bytes; }
-    // LDS offset of this lane's fragment of the first k-step for the 32-wide block `blk`
+    // LDS offset of this lane's fragment of the first 64 bytes of k for the block of 16 rows `blk`.  Along k the blocks are 2048 bytes apart and the second 64 bytes are at this ^ 64; across,
+    // they are BK / 2 rows further.
     static __device__ __forceinline__ unsigned frag(int blk, int lane) {
-        const int lr = lane & 31, lh = lane >> 5;
+        const int r = lane & 15, g = lane >> 4;
         if constexpr (!ACROSS) {
-            return (unsigned)((blk * 32 + lr) * ROWB + ((lh ^ swz<ROWB>(lr)) << 4));
+            return (unsigned)((blk * 16 + r) * ROWB + ((g ^ swz<ROWB>(r)) << 4));
         } else if constexpr (ES == 2) {
-            const int s = lane & 15, k = 8 * lh + (s >> 2), slot = blk * 4 + ((lane >> 4) & 1) * 2 + ((s & 3) >> 1);
-            return (unsigned)(k * RB + ((slot ^ permute(k)) << 4) + (s & 1) * 8);
+            const int k = 8 * g + (r >> 2), slot = blk * 2 + ((r & 3) >> 1);
+            return (unsigned)(k * RB + ((slot ^ permute(k)) << 4) + (r & 1) * 8);
         } else {
-            const int k = 4 * lh, slot = blk * 8 + (lr >> 2);
-            return (unsigned)(k * RB + ((slot ^ permute(k)) << 4) + (lr & 3) * 4);
+            const int k = 4 * g, slot = blk * 4 + (r >> 2);
+            return (unsigned)(k * RB + ((slot ^ permute(k)) << 4) + (r & 3) * 4);
         }
     }
 };
 
-// N blocks of 32 rows of an operand, one k-step, from LDS to registers.  base[]: Tile::frag of the blocks (along k: of the first).
-template <typename T, bool ACROSS, int BR, int N> struct Frags {
+template <int OFF> __device__ __forceinline__ unsigned add_const(unsigned v) {     // opaque: or dozens of sums would be kept in registers across the loop
+    unsigned d;
+    asm volatile("v_add_u32_e32 %0, %1, %2" : "=v"(d) : "n"(OFF), "v"(v));
+    return d;
+}
+template <int OFF> __device__ __forceinline__ unsigned s_add_const(unsigned v) {   // likewise for scalars
+    unsigned d;
+    asm volatile("s_add_i32 %0, %1, %2" : "=s"(d) : "s"(v), "n"(OFF) : "scc");
+    return d;
+}
+
+// Where a wave's N blocks of 16 rows lie in a tile's part of LDS: along k, the first block for either half of the stage; across, every block.
+template <typename T, bool ACROSS, int BR, int N> struct Places {
     using TL = Tile<T, ACROSS, BR>;
-    static constexpr int NB = ACROSS ? N : 1, READS = N * Frag<T, ACROSS>::READS;
-    Frag<T, ACROSS> f[N];
-    static __device__ __forceinline__ void bases(unsigned (&base)[NB], unsigned lds, int blk, int lane) {
+    using F = Frag<T, ACROSS>;
+    unsigned at[ACROSS ? N : 2];
+    __device__ __forceinline__ void init(unsigned lds, int blk, int lane) {
+        if constexpr (ACROSS) {
 #pragma unroll
-        for (int i = 0; i < NB; i++) base[i] = lds + TL::frag(blk + i, lane);
-    }
-    template <int Q> __device__ __forceinline__ void read(const unsigned (&base)[NB], unsigned off) {      // k-step Q of the stage at byte offset off
-        if constexpr (!ACROSS) {
-            const unsigned at = xor_add(base[0], Q << 5, off);
-            static_for<N>([&](auto I) { constexpr int i = decltype(I)::value; f[i].template read<i * 32 * ROWB, ROWB>(at); });
+            for (int i = 0; i < N; i++) at[i] = lds + TL::frag(blk + i, lane);
         } else {
-            static_for<N>([&](auto I) { constexpr int i = decltype(I)::value; f[i].template read<Q *(TL::BK / 4) * TL::RB, TL::RB>(base[i] + off); });
+            at[0] = lds + TL::frag(blk, lane);
+            at[1] = lds + (TL::frag(blk, lane) ^ 64u);
         }
     }
-    __device__ __forceinline__ void land() { static_for<N>([&](auto I) { f[decltype(I)::value].land(); }); }
+    // fragment of block I, half K of the stage, at byte offset OFF (a constant) + off
+    template <int I, int K, int OFF> __device__ __forceinline__ void read(F &f, unsigned off) const {
+        constexpr int in = ACROSS ? K *(TL::BK / 2) * TL::RB : I * 16 * ROWB, room = 65536 - (ACROSS ? 4 * TL::RB : 0);
+        const unsigned base = at[ACROSS ? I : K] + off;
+        if constexpr (OFF + in < room) f.template read<OFF + in, TL::RB>(base);
+        else f.template read<in, TL::RB>(add_const<OFF>(base));
+    }
 };
 
+// Tile order.  Workgroups go to the eight XCDs in turn; each XCD takes a contiguous run of a sequence that walks the columns of eight rows of
+// tiles, so that what runs on it at one time is a block of about eight by four tiles and shares its operands in that L2.
+__device__ __forceinline__ bool pick_tile(const GemmArgs &a, int &split, int &tp, int &tc) {
+    const int ntiles = a.ntp * a.ntc, per = (ntiles + 7) >> 3;
+    split = (int)blockIdx.x / (per * 8);
+    const int bid = (int)blockIdx.x - split * per * 8, t = (bid & 7) * per + (bid >> 3);
+    if (t >= ntiles) return false;
+    const int g = t / (8 * a.ntc), in = t - g * 8 * a.ntc, rows = min(8, a.ntp - g * 8);
+    // divisions run on the vector units: back to scalars, or every resource derived from them would be taken for different ones per lane
+    tp = __builtin_amdgcn_readfirstlane(g * 8 + in % rows);
+    tc = __builtin_amdgcn_readfirstlane(in / rows);
+    split = __builtin_amdgcn_readfirstlane(split);
+    return true;
+}
+
+// Results of a wave, RP blocks of 16 rows by RC (even) of 16 columns, from accumulators to memory.  A lane has 4 neighbouring columns of one row of each block; an exchange
+// between rows of 16 lanes over two blocks leaves it with 8 neighbouring columns (one call of dropout's generator), and a store with 64 contiguous bytes of 16 rows.
+__device__ __forceinline__ void rows8(const f32x4_t &x, const f32x4_t &y, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x[e]), __float_as_uint(y[e]), false, false);
+        v[e] = __uint_as_float(r[0]);
+        v[4 + e] = __uint_as_float(r[1]);
+    }
+}
+template <typename T, GemmKind KIND, int RP, int RC>
+__device__ __forceinline__ void write_results(const GemmArgs &a, int split, const f32x4_t (&acc)[RP][RC], int p0, int c0, int lane) {
+    static_assert(RP % 2 == 0 && RC % 2 == 0, "two blocks at a time");
+    const int lrow = lane & 15, lcol = (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
+    if (KIND == GEMM_FORWARD && a.nsplit <= 1) {
+        const uint32_t step = drop_step(a.epi.drop);
+#pragma unroll 1
+        for (int u = 0; u < RP * RC / 4; u++) {                 // one copy of the epilogue's code: 32 rows x 32 columns at a time
+            f32x4_t b[2][2];
+            static_for<RP * RC / 4>([&](auto U) {
+                constexpr int j = decltype(U)::value % (RP / 2) * 2, i = decltype(U)::value / (RP / 2) * 2;
+                if (u == decltype(U)::value) {
+                    b[0][0] = acc[j][i]; b[0][1] = acc[j][i + 1]; b[1][0] = acc[j + 1][i]; b[1][1] = acc[j + 1][i + 1];
+                }
+            });
+            const int m = p0 + u % (RP / 2) * 32 + lrow, n = c0 + u / (RP / 2) * 32 + lcol, nv = min(8, a.N - n);
+            float v[2][8], bias8[8];
+            rows8(b[0][0], b[0][1], v[0]);
+            rows8(b[1][0], b[1][1], v[1]);
+            load_bias8(a.epi.bias, n, nv, bias8);
+            finish_rows<T>(a.epi, step, m, n, a.M, a.N, nv, v, bias8);
+        }
+    } else {
+        static_for<RP * RC / 2>([&](auto U) {
+            constexpr int j = decltype(U)::value % RP, i = decltype(U)::value / RP * 2;
+            const int m = p0 + j * 16 + lrow, n = c0 + i * 16 + lcol, nv = min(8, a.N - n);
+            float v[8];
+            rows8(acc[j][i], acc[j][i + 1], v);
+            if (m >= a.M || nv <= 0) return;
+            if (a.nsplit > 1) store8_any<float>(a.part + ((size_t)split * a.M + m) * a.N + n, v, nv);
+            else if (a.out_dt == SOL_F32) store8_any<float>(static_cast<float *>(a.out) + (size_t)m * a.ldo + n, v, nv);
+            else store8_any<T>(static_cast<T *>(a.out) + (size_t)m * a.ldo + n, v, nv);
+        });
+    }
+}
+
+// ---- tiles of 64 x 64 to 128 x 128: a ring of NS whole stages --------------------------------------------------------------------
 // An operand's corner moves along the reduction as a scalar; what lies behind the tensor, or behind the part's last stage, is out of range of the resource and
-// arrives as zeros.  Along k: rows from `rows` on.  Across k: rows of k from `left` on, and what lies behind row_bytes of the last one.
+// arrives as zeros.  Along k: rows from `limit` on.  Across k: rows of k from `left` on, and what lies behind row_bytes of the last one.
 template <bool ACROSS, int BK> struct Cursor;
 template <int BK> struct Cursor<false, BK> {
     const unsigned char *p;
     unsigned num;
     int left;
-    __device__ __forceinline__ void init(const void *base, unsigned pitch, int es, int first, int limit, int, int s0, int s1, int) {
+    __device__ __forceinline__ void init(const void *base, unsigned pitch, int es, int first, int limit, int row_bytes, int s0, int s1, int) {
         p = static_cast<const unsigned char *>(base) + (size_t)first * pitch + (size_t)s0 * ROWB;
-        num = (unsigned)max(0, min(256, limit - first)) * pitch;       // a row ends in memory where the pitch ends, or its last stage is cut
+        const int rows = min(128, limit - first);
+        num = rows > 0 ? (unsigned)(rows - 1) * pitch + (unsigned)row_bytes - (unsigned)s0 * ROWB : 0u;
         left = s1 - s0;
     }
     __device__ __forceinline__ __amdgpu_buffer_rsrc_t next() {
         const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char *>(p), 0, left > 0 ? (int)num : 0, 0x00020000);
         p += ROWB;
+        num -= ROWB;
         --left;
         return r;
     }
@@ -156,80 +234,18 @@ template <int BK> struct Cursor<true, BK> {
     }
 };
 
-// Tile order.  Workgroups go to the eight XCDs in turn; each XCD takes a contiguous run of a sequence that walks the columns of eight rows of
-// tiles, so that what runs on it at one time is a block of about eight by eight tiles and shares its operands in that L2.
-__device__ __forceinline__ bool pick_tile(const GemmArgs &a, int &split, int &tp, int &tc) {
-    const int ntiles = a.ntp * a.ntc, per = (ntiles + 7) >> 3;
-    split = (int)blockIdx.x / (per * 8);
-    const int bid = (int)blockIdx.x - split * per * 8, t = (bid & 7) * per + (bid >> 3);
-    if (t >= ntiles) return false;
-    const int g = t / (8 * a.ntc), in = t - g * 8 * a.ntc, rows = min(8, a.ntp - g * 8);
-    // divisions run on the vector units: back to scalars, or every resource derived from them would be taken for different ones per lane
-    tp = __builtin_amdgcn_readfirstlane(g * 8 + in % rows);
-    tc = __builtin_amdgcn_readfirstlane(in / rows);
-    split = __builtin_amdgcn_readfirstlane(split);
-    return true;
-}
-
-// Results of 32 rows x 32 * TC columns of a wave.  They go through a strip of LDS of its own, so that a lane has 8 neighbouring columns of one row
-// (one call of dropout's generator) and a store writes whole lines.
-template <typename T, GemmKind KIND, int TC> struct Writer {
-    static constexpr int ERS = TC * 32 + 4, LPR = TC * 4, RPS = 64 / LPR;       // floats of a strip's row; lanes per row, rows per pass
-    static constexpr int BYTES = 32 * ERS * 4;
-    float *strip;
-    int lane, split, n, nv;
-    float bias8[8];
-    uint32_t step;
-    __device__ __forceinline__ void init(const GemmArgs &a, unsigned char *lds, int wave, int lane_, int split_, int c0) {
-        strip = reinterpret_cast<float *>(lds + wave * BYTES);
-        lane = lane_; split = split_;
-        n = c0 + (lane % LPR) * 8;
-        nv = min(8, a.N - n);
-        if constexpr (KIND == GEMM_FORWARD) {
-            load_bias8(a.epi.bias, n, nv, bias8);
-            step = drop_step(a.epi.drop);
-        }
-    }
-    template <typename F> __device__ __forceinline__ void write(const GemmArgs &a, int m0, F &&block) {      // block(i): accumulators of column block i
-        const int lr = lane & 31, lh = lane >> 5, ecol = (lane % LPR) * 8;
-        static_for<TC>([&](auto I) {
-            const f32x16_t &v = block(I);
-#pragma unroll
-            for (int e = 0; e < 4; e++)
-                *reinterpret_cast<float4 *>(strip + lr * ERS + decltype(I)::value * 32 + 8 * e + 4 * lh) = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-        });
-        wave_lds_fence();
-#pragma unroll 1
-        for (int r = lane / LPR; r < 32; r += RPS) {
-            const int m = m0 + r;
-            if (m >= a.M || nv <= 0) continue;
-            const float4 lo = *reinterpret_cast<const float4 *>(strip + r * ERS + ecol), hi = *reinterpret_cast<const float4 *>(strip + r * ERS + ecol + 4);
-            float v[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-            if (a.nsplit > 1) store8_any<float>(a.part + ((size_t)split * a.M + m) * a.N + n, v, nv);
-            else if constexpr (KIND == GEMM_FORWARD) finish8<T>(a.epi, step, m, n, a.N, nv, v, bias8);
-            else if (a.out_dt == SOL_F32) store8_any<float>(static_cast<float *>(a.out) + m * a.ldo + n, v, nv);
-            else store8_any<T>(static_cast<T *>(a.out) + m * a.ldo + n, v, nv);
-        }
-        wave_lds_fence();
-    }
-};
-
-// ---- tiles of 64 x 64 to 128 x 128: a ring of NS whole stages --------------------------------------------------------------------
-// KIND: GEMM_FORWARD (A, B along k), GEMM_DX (B across), GEMM_DW (both across).  WP x WC = 4 waves of TP x TC blocks of 32 x 32.
-template <typename T, GemmKind KIND, int WP, int WC, int TP, int TC, int NS, int PERCU>
+// KIND: GEMM_FORWARD (A, B along k), GEMM_DX (B across), GEMM_DW (both across).  WP x WC = 4 waves of RP x RC blocks of 16 x 16.
+template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int PERCU>
 __global__ void __launch_bounds__(256, PERCU) linear_tile_kernel(const GemmArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool AX = KIND == GEMM_DW, BX = KIND != GEMM_FORWARD;
-    constexpr int NW = 4, ES = (int)sizeof(T), BP = WP * TP * 32, BC = WC * TC * 32, BK = ROWB / ES;
+    constexpr int NW = 4, ES = (int)sizeof(T), BP = WP * RP * 16, BC = WC * RC * 16, BK = ROWB / ES;
     using TA = Tile<T, AX, BP>;
     using TB = Tile<T, BX, BC>;
-    using FA = Frags<T, AX, BP, TP>;
-    using FB = Frags<T, BX, BC, TC>;
-    using W = Writer<T, KIND, TC>;
     constexpr int STAGE = TA::BYTES + TB::BYTES, XL = TA::SEGS / NW, WL = TB::SEGS / NW, L = XL + WL;
-    constexpr int READS = FA::READS + FB::READS;               // LDS instructions of a k-step
-    static_assert(WP * WC == NW && TA::SEGS % (2 * NW) == 0 && TB::SEGS % NW == 0, "waves");
-    static_assert(NW * W::BYTES <= NS * STAGE && NS >= 2 && (NS - 1) * L < 64, "strips in the ring; vmcnt");
+    constexpr int READS = RP * Frag<T, AX>::READS + RC * Frag<T, BX>::READS;       // LDS instructions of half a stage
+    static_assert(WP * WC == NW && TA::SEGS % (2 * NW) == 0 && TB::SEGS % NW == 0 && BP <= 128, "waves; rows that a cursor covers");
+    static_assert(NS >= 2 && (NS - 1) * L < 64 && NS * STAGE <= 160 * 1024 / PERCU, "vmcnt; LDS");
     __shared__ __align__(1024) unsigned char lds[NS * STAGE];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -276,55 +292,58 @@ __global__ void __launch_bounds__(256, PERCU) linear_tile_kernel(const GemmArgs 
         static_for<L>([&](auto I) { request(I, (unsigned)(s * STAGE)); });
     }
 
-    f32x16_t acc[TC][TP];
+    f32x4_t acc[RP][RC];
 #pragma unroll
-    for (int i = 0; i < TC; i++)
+    for (int j = 0; j < RP; j++)
 #pragma unroll
-        for (int j = 0; j < TP; j++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
+        for (int i = 0; i < RC; i++) acc[j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-    unsigned abase[FA::NB], bbase[FB::NB];
-    FA::bases(abase, lds_addr(lds), wp * TP, lane);
-    FB::bases(bbase, lds_addr(lds) + TA::BYTES, wc * TC, lane);
-    FA fa[2];
-    FB fb[2];
-    auto multiply = [&](auto S, auto &&between) {
-        constexpr int set = decltype(S)::value;
-        static_for<TC * TP>([&](auto U) {
-            constexpr int u = decltype(U)::value, i = u / TP, j = u % TP;
-            Mma<T>::run(acc[i][j], fb[set].f[i].get(), fa[set].f[j].get());
+    Places<T, AX, BP, RP> pa;
+    Places<T, BX, BC, RC> pb;
+    pa.init(lds_addr(lds), wp * RP, lane);
+    pb.init(lds_addr(lds) + TA::BYTES, wc * RC, lane);
+    Frag<T, AX> fa[2][RP];
+    Frag<T, BX> fb[2][RC];
+    auto read_half = [&](auto K, unsigned off) {
+        constexpr int k = decltype(K)::value;
+        static_for<RC>([&](auto I) { pb.template read<decltype(I)::value, k, 0>(fb[k][decltype(I)::value], off); });
+        static_for<RP>([&](auto J) { pa.template read<decltype(J)::value, k, 0>(fa[k][decltype(J)::value], off); });
+    };
+    auto land = [&](auto K) {
+        constexpr int k = decltype(K)::value;
+        static_for<RC>([&](auto I) { fb[k][decltype(I)::value].land(); });
+        static_for<RP>([&](auto J) { fa[k][decltype(J)::value].land(); });
+    };
+    auto multiply = [&](auto K, auto &&between) {
+        constexpr int k = decltype(K)::value;
+        static_for<RP * RC>([&](auto U) {
+            constexpr int u = decltype(U)::value, j = u / RC, i = u % RC;
+            Mma16<T>::run(acc[j][i], fb[k][i].get(), fa[k][j].get());
             between(U);
         });
         __builtin_amdgcn_sched_barrier(0);
     };
+    constexpr std::integral_constant<int, 0> K0{};
+    constexpr std::integral_constant<int, 1> K1{};
 
     wait_vmcnt<(NS - 1) * L>();                                // the first stage has landed
     __builtin_amdgcn_s_barrier();
-    fb[0].template read<0>(bbase, 0u);
-    fa[0].template read<0>(abase, 0u);
+    read_half(K0, 0u);
     unsigned sb = 0;
     for (int s = s0; s < s1; s++) {
         const unsigned sbn = sb + STAGE == NS * STAGE ? 0u : sb + STAGE;
-        static_for<3>([&](auto Q) {                            // k-steps 0 .. 2, the next one's fragments on their way
-            constexpr int q = decltype(Q)::value, set = q & 1;
-            fb[set ^ 1].template read<q + 1>(bbase, sb);
-            fa[set ^ 1].template read<q + 1>(abase, sb);
-            wait_lds<READS>();
-            fb[set].land();
-            fa[set].land();
-            multiply(std::integral_constant<int, set>{}, [](auto) {});
-        });
+        read_half(K1, sb);
+        wait_lds<READS>();
+        land(K0);
+        multiply(K0, [](auto) {});
         wait_lgkmcnt<0>();                                     // all of this stage is in registers
-        fb[1].land();
-        fa[1].land();
+        land(K1);
         wait_vmcnt<(NS - 2) * L>();                            // the next stage has landed
         __builtin_amdgcn_s_barrier();                          // ... for every wave, and nobody reads this one any more: it can be refilled
-        fb[0].template read<0>(bbase, sbn);
-        fa[0].template read<0>(abase, sbn);
+        read_half(K0, sbn);
         next_stage();
-        multiply(std::integral_constant<int, 1>{}, [&](auto U) {
-            constexpr int u = decltype(U)::value, per = (L + TC * TP - 1) / (TC * TP);
+        multiply(K1, [&](auto U) {
+            constexpr int u = decltype(U)::value, per = (L + RP * RC - 1) / (RP * RC);
             static_for<per>([&](auto V) {
                 constexpr int i = u * per + decltype(V)::value;
                 if constexpr (i < L) request(std::integral_constant<int, i>{}, sb);
@@ -333,220 +352,20 @@ __global__ void __launch_bounds__(256, PERCU) linear_tile_kernel(const GemmArgs 
         sb = sbn;
     }
     wait_lgkmcnt<0>();                                         // the fragments requested behind the last stage
-    fb[0].land();
-    fa[0].land();
+    land(K0);
     wait_vmcnt<0>();                                           // ... and its DMAs, zeros into dead slots
-    __builtin_amdgcn_s_barrier();                              // the ring becomes the strips
-
-    W w;
-    w.init(a, lds, wave, lane, split, c0 + wc * TC * 32);
-    static_for<TP>([&](auto J) {
-        constexpr int j = decltype(J)::value;
-        w.write(a, p0 + (wp * TP + j) * 32, [&](auto I) -> const f32x16_t & { return acc[decltype(I)::value][j]; });
-    });
-#endif
-}
-
-// ---- tiles of 256 x 128 ----------------------------------------------------------------------------------------------------------
-// Two workgroups per CU leave 80 KB of LDS each, and a stage of whole lines has 48.  So the ring counts not stages but units of 16 KB, 128 rows or columns each,
-// five of them: a stage is B, A0 (rows 0 .. 127) and A1 (rows 128 .. 255).  A wave takes its fragments of B into registers once and multiplies A0, then A1, with
-// them; when A0 is done its slot and B's are refilled, and when A1 is done its own.  Every unit is requested one stage (32 matrix instructions per wave) before it is needed.
-template <typename T, GemmKind KIND>
-__global__ void __launch_bounds__(256, 2) linear_big_kernel(const GemmArgs a) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    constexpr bool AX = KIND == GEMM_DW, BX = KIND != GEMM_FORWARD;
-    constexpr int NW = 4, ES = (int)sizeof(T), BK = ROWB / ES, UNIT = 16384, UL = UNIT / 1024 / NW;      // UL: DMA instructions of a wave per unit
-    using TA = Tile<T, AX, 128>;
-    using TB = Tile<T, BX, 128>;
-    using FA = Frags<T, AX, 128, 2>;
-    using FB = Frags<T, BX, 128, 2>;
-    using W = Writer<T, KIND, 2>;
-    static_assert(NW * W::BYTES <= 5 * UNIT && UL == 4, "strips in the ring; requests per unit");
-    __shared__ __align__(1024) unsigned char lds[5 * UNIT];
-
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave & 1, wc = wave >> 1;
-    int split, tp, tc;
-    if (!pick_tile(a, split, tp, tc)) return;
-    const int p0 = tp * 256, c0 = tc * 128;
-    const int nk = (a.K + BK - 1) / BK, s0 = split * a.steps, s1 = min(nk, s0 + a.steps);   // this part's stages
-
-    const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES);
-    Cursor<AX, BK> ca[2];
-    Cursor<BX, BK> cb;
-    ca[0].init(a.a, apitch, ES, p0, a.M, a.a_row, s0, s1, a.K);
-    ca[1].init(a.a, apitch, ES, p0 + 128, a.M, a.a_row, s0, s1, a.K);
-    cb.init(a.b, bpitch, ES, c0, a.N, a.b_row, s0, s1, a.K);
-    unsigned ao[UL], bo[UL], cut[2] = {0u, 0u};
-#pragma unroll
-    for (int i = 0; i < UL; i++) {
-        ao[i] = TA::offset(wave * UL + i, lane, apitch);
-        bo[i] = TB::offset(wave * UL + i, lane, bpitch);
-    }
-    if constexpr (!AX) {
-#pragma unroll
-        for (int i = 0; i < 2; i++) cut[i] = a.a_cut && TA::behind(wave * UL + i, lane, a.K * ES - (nk - 1) * ROWB) ? 0xffffffffu : 0u;
-    }
-    auto request_a = [&](const __amdgpu_buffer_rsrc_t &r, auto I, unsigned off, bool last) {
-        constexpr int i = decltype(I)::value;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, !AX ? ao[i] | (last ? cut[i & 1] : 0u) : ao[i], 0, 0, 0);
-    };
-    auto request_b = [&](const __amdgpu_buffer_rsrc_t &r, auto I, unsigned off) {
-        constexpr int i = decltype(I)::value;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + off + (wave * UL + i) * 1024), 16, bo[i], 0, 0, 0);
-    };
-
-    unsigned o0 = 0, o1 = UNIT, o2 = 2 * UNIT, o3 = 3 * UNIT, o4 = 4 * UNIT;      // slots of this stage's B, A0, A1 and of the next one's B, A0
-    __amdgpu_buffer_rsrc_t r0;                                  // of the A0 whose requests are spread over two halves
-    {
-        const __amdgpu_buffer_rsrc_t rb = cb.next(), r1 = ca[1].next(), rn = cb.next();
-        r0 = ca[0].next();
-        static_for<UL>([&](auto I) { request_b(rb, I, o0); });
-        static_for<UL>([&](auto I) { request_a(r0, I, o1, s0 == nk - 1); });
-        static_for<UL>([&](auto I) { request_a(r1, I, o2, s0 == nk - 1); });
-        static_for<UL>([&](auto I) { request_b(rn, I, o3); });
-        r0 = ca[0].next();
-        static_for<UL / 2>([&](auto I) { request_a(r0, I, o4, s0 + 1 == nk - 1); });
-    }
-
-    f32x16_t acc[2][4];
-#pragma unroll
-    for (int i = 0; i < 2; i++)
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-#pragma unroll
-            for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
-
-    unsigned abase[FA::NB], bbase[FB::NB];
-    FA::bases(abase, lds_addr(lds), wp * 2, lane);
-    FB::bases(bbase, lds_addr(lds), wc * 2, lane);
-    FA fa[4];                                                   // of the four k-steps of a half: two are on their way while one is multiplied
-    FB fb[4];
-    auto multiply = [&](auto H, auto Q, auto &&between) {       // four products of half H, k-step Q
-        constexpr int h = decltype(H)::value, q = decltype(Q)::value;
-        static_for<4>([&](auto U) {
-            constexpr int u = decltype(U)::value, i = u / 2, j = u % 2;
-            Mma<T>::run(acc[i][h * 2 + j], fb[q].f[i].get(), fa[q].f[j].get());
-            between(U);
-        });
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    constexpr std::integral_constant<int, 0> C0{};
-    constexpr std::integral_constant<int, 1> C1{};
-    constexpr std::integral_constant<int, 2> C2{};
-    constexpr std::integral_constant<int, 3> C3{};
-
-    wait_vmcnt<2 * UL + UL / 2>();                              // B and A0 of the first stage have landed
-    __builtin_amdgcn_s_barrier();
-    static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value>(bbase, o0); });
-    fa[0].template read<0>(abase, o1);
-    fa[1].template read<1>(abase, o1);
-    wait_lgkmcnt<0>();
-    static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
-    fa[0].land();
-    fa[1].land();
-
-    // The counts of the waits: LDS reads and DMAs land in the order in which they were issued, and each wait names how many were issued behind what it waits for.
-    for (int s = s0; s < s1; s++) {
-        // ---- A0 times B; the second half of the next stage's A0 is requested
-        const bool next_last = s + 1 == nk - 1, third_last = s + 2 == nk - 1;
-        fa[2].template read<2>(abase, o1);
-        wait_lds<2 * FA::READS + 2 * FB::READS>();
-        fa[0].land();
-        fb[1].land();
-        multiply(C0, C0, [&](auto U) { if constexpr (U == 3) request_a(r0, C2, o4, next_last); });
-        fa[3].template read<3>(abase, o1);
-        wait_lds<2 * FA::READS + FB::READS>();
-        fa[1].land();
-        fb[2].land();
-        multiply(C0, C1, [&](auto U) { if constexpr (U == 3) request_a(r0, C3, o4, next_last); });
-        wait_lgkmcnt<0>();                                      // all of A0 and B is in registers
-        fa[2].land();
-        fa[3].land();
-        fb[3].land();
-        wait_vmcnt<UL>();                                       // A1 and the next stage's B have landed
-        __builtin_amdgcn_s_barrier();                           // ... for every wave, and nobody reads A0 and B any more: A1 and B of later stages take their slots
-        fa[0].template read<0>(abase, o2);
-        const __amdgpu_buffer_rsrc_t r1 = ca[1].next(), rb = cb.next();
-        multiply(C0, C2, [&](auto U) { if constexpr (U & 1) request_a(r1, std::integral_constant<int, U / 2>{}, o0, next_last); });
-        fa[1].template read<1>(abase, o2);
-        multiply(C0, C3, [&](auto U) { if constexpr (U & 1) request_a(r1, std::integral_constant<int, 2 + U / 2>{}, o0, next_last); });
-        // ---- A1 times B; behind each k-step's last products its fragments of B make room for the next stage's
-        fa[2].template read<2>(abase, o2);
-        wait_lds<2 * FA::READS>();
-        fa[0].land();
-        multiply(C1, C0, [&](auto U) { if constexpr (U & 1) request_b(rb, std::integral_constant<int, U / 2>{}, o1); });
-        fb[0].template read<0>(bbase, o3);
-        fa[3].template read<3>(abase, o2);
-        wait_lds<2 * FA::READS + FB::READS>();
-        fa[1].land();
-        multiply(C1, C1, [&](auto U) { if constexpr (U & 1) request_b(rb, std::integral_constant<int, 2 + U / 2>{}, o1); });
-        fb[1].template read<1>(bbase, o3);
-        wait_lds<FB::READS>();                                  // all of A1 is in registers
-        fa[2].land();
-        fa[3].land();
-        fb[0].land();
-        wait_vmcnt<2 * UL>();                                   // the next stage's A0 has landed
-        __builtin_amdgcn_s_barrier();
-        fa[0].template read<0>(abase, o4);
-        r0 = ca[0].next();
-        multiply(C1, C2, [&](auto U) { if constexpr (U == 3) request_a(r0, C0, o2, third_last); });
-        fb[2].template read<2>(bbase, o3);
-        fa[1].template read<1>(abase, o4);
-        multiply(C1, C3, [&](auto U) { if constexpr (U == 3) request_a(r0, C1, o2, third_last); });
-        fb[3].template read<3>(bbase, o3);
-        const unsigned t0 = o0, t1 = o1, t2 = o2;
-        o0 = o3; o1 = o4; o2 = t0; o3 = t1; o4 = t2;
-    }
-    wait_lgkmcnt<0>();                                          // the fragments requested behind the last stage
-    fa[0].land();
-    fa[1].land();
-    static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
-    wait_vmcnt<0>();                                            // ... and its DMAs, zeros into dead slots
-    __builtin_amdgcn_s_barrier();                               // the ring becomes the strips
-
-    W w;
-    w.init(a, lds, wave, lane, split, c0 + wc * 64);
-    static_for<4>([&](auto J) {
-        constexpr int j = decltype(J)::value;
-        w.write(a, p0 + (j >> 1) * 128 + wp * 64 + (j & 1) * 32, [&](auto I) -> const f32x16_t & { return acc[decltype(I)::value][j]; });
-    });
+    write_results<T, KIND, RP, RC>(a, split, acc, p0 + wp * RP * 16, c0 + wc * RC * 16, lane);
 #endif
 }
 
 // ---- tiles of 256 x 256 ----------------------------------------------------------------------------------------------------------
 // One workgroup of eight waves per CU: a row or column fetched once serves 256 of the other operand, 32 bytes a clock at the full rate of the matrix units, where the path
-// from L2 to LDS gives 58 (with two workgroups of 256 x 128 it was 48, and their waves stood behind their own requests).
-// A stage is four units of 16 KB: B0, B1 (columns 0 .. 127, 128 .. 255), A0, A1 (rows).  A wave has 64 rows of each half of A and 64 columns: it takes its fragments of B into
-// registers once, multiplies A0, then A1, with them, and behind each k-step's last products reads the next stage's over them.  The ring has ten units; A0, A1 of
-// stage s + 2 and B0 of s + 3 take the places of B0, B1 and A0 of stage s, and B1 of s + 3 that of A1, so every unit is requested one and a half stages (48 matrix instructions of a wave)
-// before it is needed.
+// from L2 to LDS gives 58.  A stage is four units of 16 KB: B0, B1 (columns 0 .. 127, 128 .. 255), A0, A1 (rows).  A wave has 64 rows of each half of A and 64 columns: it takes
+// its fragments of B into registers once, multiplies A0, then A1, with them, and reads the next stage's over them behind the last products that need them.  The ring has ten
+// units; A0, A1 of stage s + 2 and B0 of s + 3 take the places of B0, B1 and A0 of stage s, and B1 of s + 3 that of A1, so every unit is requested one and a half stages (96 matrix
+// instructions of a wave) before it is needed.
 // The two waves of a SIMD issue one instruction each at a time, and everything that is not a product has to fit beside the products: resources and lane offsets are
 // constants of the loop (a scalar offset moves along the reduction, and the range check includes it), and the loop is unrolled over the five stages after which the ring repeats.
-template <int OFF> __device__ __forceinline__ unsigned add_const(unsigned v) {     // opaque: or sixty sums would be kept in registers across the loop
-    unsigned d;
-    asm volatile("v_add_u32_e32 %0, %1, %2" : "=v"(d) : "n"(OFF), "v"(v));
-    return d;
-}
-
-// Fragments of one k-step of a unit at a constant place.  at[]: along k, the first block's place for each of the four k-steps; across, each block's for the first.
-template <typename T, bool ACROSS> struct UnitFrags {
-    using TL = Tile<T, ACROSS, 128>;
-    static constexpr int NB = ACROSS ? 2 : 4, READS = 2 * Frag<T, ACROSS>::READS;
-    Frag<T, ACROSS> f[2];
-    static __device__ __forceinline__ void places(unsigned (&at)[NB], unsigned lds, int blk, int lane) {
-#pragma unroll
-        for (int i = 0; i < NB; i++) at[i] = ACROSS ? lds + TL::frag(blk + i, lane) : lds + (TL::frag(blk, lane) ^ (unsigned)(i << 5));
-    }
-    template <int Q, int OFF> __device__ __forceinline__ void read(const unsigned (&at)[NB]) {
-        static_for<2>([&](auto I) {
-            constexpr int i = decltype(I)::value, off = ACROSS ? Q *(TL::BK / 4) * TL::RB : i * 32 * ROWB, room = 65536 - (ACROSS ? 4 * TL::RB : 0);
-            if constexpr (OFF + off < room) f[i].template read<OFF + off, TL::RB>(at[ACROSS ? i : Q]);
-            else f[i].template read<off, TL::RB>(add_const<OFF>(at[ACROSS ? i : Q]));
-        });
-    }
-    __device__ __forceinline__ void land() { f[0].land(); f[1].land(); }
-};
 
 // Bytes from the corner of a unit (its first row, or column, is `first` of `limit`) to the end of what may be read
 __device__ __forceinline__ unsigned unit_bytes(bool across, int es, int first, int limit, int K, unsigned pitch, int row_bytes) {
@@ -562,10 +381,8 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
     constexpr int NW = 8, ES = (int)sizeof(T), BK = ROWB / ES, UNIT = 16384, UL = UNIT / 1024 / NW, NU = 10;
     using TA = Tile<T, AX, 128>;
     using TB = Tile<T, BX, 128>;
-    using FA = UnitFrags<T, AX>;
-    using FB = UnitFrags<T, BX>;
-    using W = Writer<T, KIND, 2>;
-    static_assert(NW * W::BYTES <= NU * UNIT && UL == 2, "strips in the ring; requests per unit");
+    constexpr int RA = 2 * Frag<T, AX>::READS, RBK = 4 * Frag<T, BX>::READS;       // LDS instructions of a step's fragments of A, of half a stage's of B
+    static_assert(UL == 2, "requests per unit");
     __shared__ __align__(1024) unsigned char lds[NU * UNIT];
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -599,43 +416,55 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
             }
         }
     };
-    unsigned char *const mine = lds + wave * UL * 1024;         // where this wave's part of a unit goes
-    auto request_a = [&](int h, auto I, int unit, unsigned soff) {
-        constexpr int i = decltype(I)::value;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra[h], (__attribute__((address_space(3))) void *)(mine + unit * UNIT + i * 1024), 16, ao[i], soff, 0, 0);
+    const unsigned mine = lds_addr(lds) + wave * UL * 1024;     // where this wave's part of a unit goes
+    auto request_a = [&](auto H, auto I, auto U, unsigned soff) {
+        constexpr int h = decltype(H)::value, i = decltype(I)::value, at = decltype(U)::value * UNIT + i * 1024;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra[h], (__attribute__((address_space(3))) void *)(size_t)s_add_const<at>(mine), 16, ao[i], soff, 0, 0);
     };
-    auto request_b = [&](int h, auto I, int unit, unsigned soff) {
-        constexpr int i = decltype(I)::value;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb[h], (__attribute__((address_space(3))) void *)(mine + unit * UNIT + i * 1024), 16, bo[i], soff, 0, 0);
+    auto request_b = [&](auto H, auto I, auto U, unsigned soff) {
+        constexpr int h = decltype(H)::value, i = decltype(I)::value, at = decltype(U)::value * UNIT + i * 1024;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb[h], (__attribute__((address_space(3))) void *)(size_t)s_add_const<at>(mine), 16, bo[i], soff, 0, 0);
     };
-#pragma unroll
-    for (int u = 0; u < NU - 1; u++) {                          // unit u: stage u / 4, B0, B1, A0, A1 in turn
-        if (u % 4 == 2) cut_last(u / 4);
+    static_for<NU - 1>([&](auto U) {                            // unit u: stage u / 4, B0, B1, A0, A1 in turn
+        constexpr int u = decltype(U)::value;
+        if constexpr (u % 4 == 2) cut_last(u / 4);
         static_for<UL>([&](auto I) {
-            if (u % 4 < 2) request_b(u % 4, I, u, (unsigned)(u / 4) * bstep);
-            else request_a(u % 4 - 2, I, u, (unsigned)(u / 4) * astep);
+            if constexpr (u % 4 < 2) request_b(std::integral_constant<int, u % 4>{}, I, U, (unsigned)(u / 4) * bstep);
+            else request_a(std::integral_constant<int, u % 4 - 2>{}, I, U, (unsigned)(u / 4) * astep);
         });
-    }
+    });
 
-    f32x16_t acc[2][4];
+    f32x4_t acc[2][4][4];                                       // [half of A][block of rows][block of columns]
 #pragma unroll
-    for (int i = 0; i < 2; i++)
+    for (int h = 0; h < 2; h++)
 #pragma unroll
         for (int j = 0; j < 4; j++)
 #pragma unroll
-            for (int e = 0; e < 16; e++) acc[i][j][e] = 0.f;
+            for (int i = 0; i < 4; i++) acc[h][j][i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 
-    unsigned aat[FA::NB], bat[FB::NB];
-    FA::places(aat, lds_addr(lds), wp * 2, lane);
-    FB::places(bat, lds_addr(lds) + (wc >> 1) * UNIT, (wc & 1) * 2, lane);       // B1 lies behind B0, except where the ring's end is between them: never, units go in twos
-    FA fa[4];                                                   // of the four k-steps of a half: two are on their way while one is multiplied
-    FB fb[4];
-    auto multiply = [&](auto H, auto Q, auto &&request) {       // four products of half H, k-step Q, and a request among them
+    Places<T, AX, 128, 4> pa;
+    Places<T, BX, 128, 4> pb;
+    pa.init(lds_addr(lds), wp * 4, lane);
+    pb.init(lds_addr(lds) + (wc >> 1) * UNIT, (wc & 1) * 4, lane);       // B1 lies behind B0: units go in twos
+    // A half stage of 64 rows is done in four steps of two blocks: step q has blocks q % 2 * 2 and + 1, half q / 2 of the stage's k.  Two steps' fragments are on their way while one is multiplied.
+    Frag<T, AX> fa[4][2];
+    Frag<T, BX> fb[2][4];
+    auto read_a = [&](auto Q, auto OFF) {
+        constexpr int q = decltype(Q)::value;
+        static_for<2>([&](auto J) { pa.template read<(q & 1) * 2 + decltype(J)::value, q / 2, decltype(OFF)::value>(fa[q][decltype(J)::value], 0u); });
+    };
+    auto read_b = [&](auto K, auto OFF) {
+        constexpr int k = decltype(K)::value;
+        static_for<4>([&](auto I) { pb.template read<decltype(I)::value, k, decltype(OFF)::value>(fb[k][decltype(I)::value], 0u); });
+    };
+    auto land_a = [&](auto Q) { static_for<2>([&](auto J) { fa[decltype(Q)::value][decltype(J)::value].land(); }); };
+    auto land_b = [&](auto K) { static_for<4>([&](auto I) { fb[decltype(K)::value][decltype(I)::value].land(); }); };
+    auto multiply = [&](auto H, auto Q, auto &&request) {       // eight products of half H, step Q, and a request among them
         constexpr int h = decltype(H)::value, q = decltype(Q)::value;
-        static_for<4>([&](auto U) {
-            constexpr int u = decltype(U)::value, i = u / 2, j = u % 2;
-            Mma<T>::run(acc[i][h * 2 + j], fb[q].f[i].get(), fa[q].f[j].get());
-            if constexpr (u == 1) request();
+        static_for<8>([&](auto U) {
+            constexpr int u = decltype(U)::value, j = u / 4, i = u % 4;
+            Mma16<T>::run(acc[h][(q & 1) * 2 + j][i], fb[q / 2][i].get(), fa[q][j].get());
+            if constexpr (u == 3) request();
         });
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -643,71 +472,77 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
     constexpr std::integral_constant<int, 1> C1{};
     constexpr std::integral_constant<int, 2> C2{};
     constexpr std::integral_constant<int, 3> C3{};
+    constexpr std::integral_constant<int, 2 * UNIT> FIRST_A0{};
 
     wait_vmcnt<6 * UL>();                                       // B and A0 of the first stage have landed
     __builtin_amdgcn_s_barrier();
-    static_for<4>([&](auto Q) { fb[decltype(Q)::value].template read<decltype(Q)::value, 0>(bat); });
-    fa[0].template read<0, 2 * UNIT>(aat);
-    fa[1].template read<1, 2 * UNIT>(aat);
+    read_b(C0, C0);
+    read_b(C1, C0);
+    read_a(C0, FIRST_A0);
+    read_a(C1, FIRST_A0);
     wait_lgkmcnt<0>();
-    static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
-    fa[0].land();
-    fa[1].land();
+    land_b(C0);
+    land_b(C1);
+    land_a(C0);
+    land_a(C1);
 
     // The counts of the waits: LDS reads and DMAs land in the order in which they were issued, and each wait names how many were issued behind what it waits for.
-    // One request per k-step and wave: a request holds its wave while the queue is full, and two at a time from eight waves fill it.
+    // One request per step and wave: a request holds its wave while the queue is full, and two at a time from eight waves fill it.
     unsigned asoff = 2 * astep, bsoff = 2 * bstep;              // of stage s + 2
     auto stage = [&](auto P, int s) {
         constexpr int p = decltype(P)::value;
         constexpr auto at = [](int k) { return (p * 4 + k) % NU; };      // unit k from this stage's B0 on
-        constexpr int A0 = at(2) * UNIT, A1 = at(3) * UNIT, BN = at(4) * UNIT, AN = at(6) * UNIT;
+        constexpr std::integral_constant<int, at(2) * UNIT> A0{};
+        constexpr std::integral_constant<int, at(3) * UNIT> A1{};
+        constexpr std::integral_constant<int, at(4) * UNIT> BN{};
+        constexpr std::integral_constant<int, at(6) * UNIT> AN{};
+        constexpr std::integral_constant<int, at(0)> U0{};
+        constexpr std::integral_constant<int, at(1)> U1{};
+        constexpr std::integral_constant<int, at(2)> U2{};
+        constexpr std::integral_constant<int, at(9)> U9{};
         // ---- A0 times B
-        fa[2].template read<2, A0>(aat);
-        wait_lds<2 * FA::READS + 2 * FB::READS>();
-        fa[0].land();
-        fb[1].land();
-        multiply(C0, C0, [&] { request_b(1, C0, at(9), bsoff); });
-        fa[3].template read<3, A0>(aat);
-        wait_lds<2 * FA::READS + FB::READS>();
-        fa[1].land();
-        fb[2].land();
-        multiply(C0, C1, [&] { request_b(1, C1, at(9), bsoff); });
+        read_a(C2, A0);
+        wait_lds<2 * RA + RBK>();
+        land_a(C0);
+        land_b(C0);
+        multiply(C0, C0, [&] { request_b(C1, C0, U9, bsoff); });
+        read_a(C3, A0);
+        wait_lds<2 * RA + RBK>();
+        land_a(C1);
+        multiply(C0, C1, [&] { request_b(C1, C1, U9, bsoff); });
         wait_lgkmcnt<0>();                                      // all of A0 and B is in registers
-        fa[2].land();
-        fa[3].land();
-        fb[3].land();
+        land_a(C2);
+        land_a(C3);
+        land_b(C1);
         wait_vmcnt<4 * UL>();                                   // A1 and the next stage's B have landed
         __builtin_amdgcn_s_barrier();                           // ... for every wave, and nobody reads A0 and B any more: units of later stages take their slots
-        fa[0].template read<0, A1>(aat);
+        read_a(C0, A1);
         cut_last(s + 2);
-        multiply(C0, C2, [&] { request_a(0, C0, at(0), asoff); });
-        fa[1].template read<1, A1>(aat);
-        multiply(C0, C3, [&] { request_a(0, C1, at(0), asoff); });
-        // ---- A1 times B; behind each k-step's last products its fragments of B make room for the next stage's
-        fa[2].template read<2, A1>(aat);
-        wait_lds<2 * FA::READS>();
-        fa[0].land();
-        multiply(C1, C0, [&] { request_a(1, C0, at(1), asoff); });
-        fb[0].template read<0, BN>(bat);
-        fa[3].template read<3, A1>(aat);
-        wait_lds<2 * FA::READS + FB::READS>();
-        fa[1].land();
-        multiply(C1, C1, [&] { request_a(1, C1, at(1), asoff); });
-        fb[1].template read<1, BN>(bat);
-        wait_lds<FB::READS>();                                  // all of A1 is in registers
-        fa[2].land();
-        fa[3].land();
-        fb[0].land();
+        multiply(C0, C2, [&] { request_a(C0, C0, U0, asoff); });
+        read_a(C1, A1);
+        multiply(C0, C3, [&] { request_a(C0, C1, U0, asoff); });
+        // ---- A1 times B; behind the last products with half of B's fragments the next stage's take their registers
+        read_a(C2, A1);
+        wait_lds<2 * RA>();
+        land_a(C0);
+        multiply(C1, C0, [&] { request_a(C1, C0, U1, asoff); });
+        read_a(C3, A1);
+        wait_lds<2 * RA>();
+        land_a(C1);
+        multiply(C1, C1, [&] { request_a(C1, C1, U1, asoff); });
+        read_b(C0, BN);
+        wait_lds<RBK>();                                        // all of A1 is in registers
+        land_a(C2);
+        land_a(C3);
         wait_vmcnt<5 * UL>();                                   // the next stage's A0 has landed
         __builtin_amdgcn_s_barrier();
-        fa[0].template read<0, AN>(aat);
+        read_a(C0, AN);
         asoff += astep;
         bsoff += bstep;
-        multiply(C1, C2, [&] { request_b(0, C0, at(2), bsoff); });
-        fb[2].template read<2, BN>(bat);
-        fa[1].template read<1, AN>(aat);
-        multiply(C1, C3, [&] { request_b(0, C1, at(2), bsoff); });
-        fb[3].template read<3, BN>(bat);
+        multiply(C1, C2, [&] { request_b(C0, C0, U2, bsoff); });
+        read_a(C1, AN);
+        multiply(C1, C3, [&] { request_b(C0, C1, U2, bsoff); });
+        read_b(C1, BN);
     };
     for (int s = 0;;) {
         stage(C0, s);
@@ -722,18 +557,13 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
         if (++s >= nk) break;
     }
     wait_lgkmcnt<0>();                                          // the fragments requested behind the last stage
-    fa[0].land();
-    fa[1].land();
-    static_for<4>([&](auto Q) { fb[decltype(Q)::value].land(); });
+    land_a(C0);
+    land_a(C1);
+    land_b(C0);
+    land_b(C1);
     wait_vmcnt<0>();                                            // ... and its DMAs into dead slots
-    __builtin_amdgcn_s_barrier();                               // the ring becomes the strips
-
-    W w;
-    w.init(a, lds, wave, lane, split, c0 + wc * 64);
-    static_for<4>([&](auto J) {
-        constexpr int j = decltype(J)::value;
-        w.write(a, p0 + (j >> 1) * 128 + wp * 64 + (j & 1) * 32, [&](auto I) -> const f32x16_t & { return acc[decltype(I)::value][j]; });
-    });
+#pragma unroll
+    for (int h = 0; h < 2; h++) write_results<T, KIND, 4, 4>(a, 0, acc[h], p0 + h * 128 + wp * 64, c0 + wc * 64, lane);
 #endif
 }
 
@@ -745,32 +575,25 @@ static long tiles_of(GemmArgs &a, int dt, int bp, int bc) {     // fills in the 
     return (long)ceil_div(a.ntp * a.ntc, 8) * 8 * a.nsplit;
 }
 
-template <typename T, GemmKind KIND, int WP, int WC, int TP, int TC, int NS, int PERCU> static sol_status launch_tile(GemmArgs a, int dt, hipStream_t st) {
-    const long blocks = tiles_of(a, dt, WP * TP * 32, WC * TC * 32);
-    hipLaunchKernelGGL((linear_tile_kernel<T, KIND, WP, WC, TP, TC, NS, PERCU>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int PERCU> static sol_status launch_tile(GemmArgs a, int dt, hipStream_t st) {
+    const long blocks = tiles_of(a, dt, WP * RP * 16, WC * RC * 16);
+    hipLaunchKernelGGL((linear_tile_kernel<T, KIND, WP, WC, RP, RC, NS, PERCU>), dim3((unsigned)blocks), dim3(256), 0, st, a);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
 
 template <typename T, GemmKind KIND> static sol_status launch_kind(GemmArgs a, int dt, hipStream_t st) {
-    const long big = (long)ceil_div(a.M, 256) * ceil_div(a.N, 128) * a.nsplit, mid = (long)ceil_div(a.M, 128) * ceil_div(a.N, 128) * a.nsplit;
-    const long huge = (long)ceil_div(a.M, 256) * ceil_div(a.N, 256) * a.nsplit;
-    const double abytes = KIND == GEMM_DW ? ((double)a.K + 256) * a.lda * sizeof(T) : 256.0 * a.lda * sizeof(T);
-    const double bbytes = KIND != GEMM_FORWARD ? ((double)a.K + 256) * a.ldb * sizeof(T) : 256.0 * a.ldb * sizeof(T);
-    if (huge >= 200 && a.nsplit <= 1 && abytes < 4294967296.0 && bbytes < 4294967296.0) {       // 32-bit offsets along the reduction
+    const long huge = (long)ceil_div(a.M, 256) * ceil_div(a.N, 256), mid = (long)ceil_div(a.M, 128) * ceil_div(a.N, 128) * (a.nsplit < 1 ? 1 : a.nsplit);
+    // 32-bit offsets along the reduction
+    const double abytes = (KIND == GEMM_DW ? a.K + 256.0 : 256.0) * a.lda * sizeof(T), bbytes = (KIND != GEMM_FORWARD ? a.K + 256.0 : 256.0) * a.ldb * sizeof(T);
+    if (huge >= 200 && a.nsplit <= 1 && abytes < 4294967296.0 && bbytes < 4294967296.0) {
         const long blocks = tiles_of(a, dt, 256, 256);
         hipLaunchKernelGGL((linear_huge_kernel<T, KIND>), dim3((unsigned)blocks), dim3(512), 0, st, a);
         SOL_HIP(hipGetLastError());
         return SOL_OK;
     }
-    if (big >= 400) {
-        const long blocks = tiles_of(a, dt, 256, 128);
-        hipLaunchKernelGGL((linear_big_kernel<T, KIND>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-        SOL_HIP(hipGetLastError());
-        return SOL_OK;
-    }
-    if (mid >= 200) return launch_tile<T, KIND, 2, 2, 2, 2, 2, 2>(a, dt, st);
-    return launch_tile<T, KIND, 2, 2, 1, 1, 3, 3>(a, dt, st);
+    if (mid >= 200) return launch_tile<T, KIND, 2, 2, 4, 4, 2, 2>(a, dt, st);
+    return launch_tile<T, KIND, 2, 2, 2, 2, 3, 3>(a, dt, st);
 }
 
 sol_status launch_linear_gemm(GemmArgs a, int dt, GemmKind kind, hipStream_t st) {

@@ -20,12 +20,20 @@ struct DropArgs {
 
 struct Philox4 { uint32_t w[4]; };
 
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {       // one instruction
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+#else
+    return a ^ b ^ c;
+#endif
+}
+
 __device__ __forceinline__ Philox4 philox(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
 #pragma unroll
     for (int r = 0; r < 10; r++) {
         const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
+        c0 = xor3((uint32_t)(b >> 32), c1, k0);
+        c2 = xor3((uint32_t)(a >> 32), c3, k1);
         c1 = (uint32_t)b;
         c3 = (uint32_t)a;
         k0 += 0x9E3779B9u;
@@ -185,9 +193,52 @@ __device__ __forceinline__ void finish8(const LinearEpi &e, uint32_t step, int m
     }
     store8_any<T>(static_cast<T *>(e.y) + m * e.ldy + n, v, nv);
 }
+// n is a multiple of 8 and the bias 16-byte aligned
 __device__ __forceinline__ void load_bias8(const float *bias, int n, int nv, float b[8]) {
+    if (bias && nv >= 8) {
+        const float4 lo = *reinterpret_cast<const float4 *>(bias + n), hi = *reinterpret_cast<const float4 *>(bias + n + 4);
+        b[0] = lo.x; b[1] = lo.y; b[2] = lo.z; b[3] = lo.w; b[4] = hi.x; b[5] = hi.y; b[6] = hi.z; b[7] = hi.w;
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; e++) b[e] = bias && e < nv ? bias[n + e] : 0.f;
+        for (int e = 0; e < 8; e++) b[e] = bias && e < nv ? bias[n + e] : 0.f;
+    }
+}
+
+// The same for rows m and m + 16 at once: their arithmetic is independent and fills the waits of one another.
+template <typename T>
+__device__ __forceinline__ void finish_rows(const LinearEpi &e, uint32_t step, int m, int n, int M, int N, int nv, float (&v)[2][8], const float (&bias8)[8]) {
+    const int nv0 = m < M ? nv : 0, nv1 = m + 16 < M ? nv : 0;
+    const size_t zat = (size_t)m * N + n, yat = (size_t)m * e.ldy + n;
+#pragma unroll
+    for (int c = 0; c < 8; c++) { v[0][c] += bias8[c]; v[1][c] += bias8[c]; }
+    if (e.pre) {
+        if (nv0 > 0) store8_any<T>(static_cast<T *>(e.pre) + zat, v[0], nv0);
+        if (nv1 > 0) store8_any<T>(static_cast<T *>(e.pre) + zat + (size_t)16 * N, v[1], nv1);
+    }
+    if (e.act != SOL_ACT_NONE) {
+        switch (e.act) {
+#define SOL_ACT_CASE(A) case A: { _Pragma("unroll") for (int i = 0; i < 16; i++) v[i >> 3][i & 7] = act_forward(A, v[i >> 3][i & 7]); break; }
+            SOL_ACT_CASE(SOL_ACT_RELU)
+            SOL_ACT_CASE(SOL_ACT_GELU)
+            SOL_ACT_CASE(SOL_ACT_GELU_TANH)
+            SOL_ACT_CASE(SOL_ACT_SILU)
+#undef SOL_ACT_CASE
+        }
+    }
+    if (e.drop.t) {
+        drop8(e.drop, step, (uint32_t)m, (uint32_t)n >> 3, v[0]);
+        drop8(e.drop, step, (uint32_t)m + 16, (uint32_t)n >> 3, v[1]);
+    }
+    if (e.res) {
+        const size_t rat = (size_t)m * e.ldr + n;
+        float r[2][8];
+        load8_any<T>(static_cast<const T *>(e.res) + rat, r[0], nv0);
+        load8_any<T>(static_cast<const T *>(e.res) + rat + 16 * e.ldr, r[1], nv1);
+#pragma unroll
+        for (int c = 0; c < 8; c++) { v[0][c] += r[0][c]; v[1][c] += r[1][c]; }
+    }
+    if (nv0 > 0) store8_any<T>(static_cast<T *>(e.y) + yat, v[0], nv0);
+    if (nv1 > 0) store8_any<T>(static_cast<T *>(e.y) + yat + 16 * e.ldy, v[1], nv1);
 }
 
 // ---- launchers --------------------------------------------------------------------------------------------------------------------
