@@ -7,7 +7,7 @@
 // memory into registers, sixteen steps in flight per wave (the kernel is latency-bound: for 2048 inputs that is
 // the whole reduction in one round trip) -- x is tiny and
 // L2-resident -- and the eight partial accumulators are added through LDS in a fixed order behind one barrier.
-#include "conv_common.h"
+#include "linear_ops.h"
 
 namespace sol {
 
@@ -109,8 +109,9 @@ sol_status launch_linear(const ConvArgs &a, int dt, hipStream_t st) {
 // rows 49.8 -> 30.2, 1 row 36.3 -> 18.2.  With 64 rows the rows of x are twice the bytes of the weights on the way into a CU.
 // Weights packed so that a workgroup's stream is one contiguous run: 28.1 instead of 30.2 us with 1 row, 38.4 instead of 35.6
 // with 64 (so the pitch of the rows is not what bounds it).
-template <typename T, int PB, int CB, int NS>
-__global__ void __launch_bounds__(512) linear_stream_kernel(const ConvArgs a, int nrt, int nft) {
+// FUSED: the epilogue of sol_linear_fused (activation, dropout, residual, z) in the place of scale, shift and ReLU.
+template <typename T, int PB, int CB, int NS, bool FUSED>
+__global__ void __launch_bounds__(512) linear_stream_kernel(const ConvArgs a, const LinearEpi epi, int nrt, int nft) {
 #if defined(__HIP_DEVICE_COMPILE__)
     using namespace lds_pipe;
     constexpr int ES = (int)sizeof(T), BP = PB * 16, BC = CB * 16, NW = 8;
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const ConvArgs a, in
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lslot = lane & 7, lrow = lane >> 3;
-    const unsigned xbytes = (unsigned)a.P * a.C * ES, wbytes = (unsigned)a.Cout * a.Kp * ES;
+    const unsigned xbytes = ((unsigned)(a.P - 1) * a.ldx + a.C) * ES, wbytes = (unsigned)a.Cout * a.Kp * ES;
     const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.x), 0, (int)xbytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.w), 0, (int)wbytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t xnull = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.x), 0, 0, 0x00020000);
@@ -139,7 +140,7 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const ConvArgs a, in
 #pragma unroll
     for (int i = 0; i < XL; i++) {
         const int row = i * 8 + lrow;
-        xo[i] = m0 + row < a.P ? (unsigned)(m0 + row) * a.C * ES + ((lslot ^ swz<ROWB>(row)) << 4) : 0xffffffffu;
+        xo[i] = m0 + row < a.P ? (unsigned)(m0 + row) * a.ldx * ES + ((lslot ^ swz<ROWB>(row)) << 4) : 0xffffffffu;
     }
 #pragma unroll
     for (int i = 0; i < WL; i++) {
@@ -227,6 +228,24 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const ConvArgs a, in
             *reinterpret_cast<float4 *>(&red[wave * PB * CB + j * CB + i][lg * LSTR + lr * 4]) = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
     __syncthreads();
 
+    if constexpr (FUSED) {
+        const uint32_t step = drop_step(epi.drop);
+        for (int it = tid; it < BP * (BC / 8); it += NW * 64) {   // eight features of one row per thread, the waves' sums added in order
+            const int cg = it % (BC / 8), row = it / (BC / 8), o = n0 + cg * 8, m = m0 + row, nv = min(8, a.Cout - o);
+            if (nv <= 0 || m >= a.P) continue;
+            const int blk = (row >> 4) * CB + (cg >> 1), at = (cg & 1) * 2 * LSTR + (row & 15) * 4;
+            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bias8[8];
+            load_bias8(epi.bias, o, nv, bias8);
+#pragma unroll
+            for (int w = 0; w < NW; w++) {
+                const float4 p = *reinterpret_cast<const float4 *>(&red[w * PB * CB + blk][at]), q = *reinterpret_cast<const float4 *>(&red[w * PB * CB + blk][at + LSTR]);
+                v[0] += p.x; v[1] += p.y; v[2] += p.z; v[3] += p.w;
+                v[4] += q.x; v[5] += q.y; v[6] += q.z; v[7] += q.w;
+            }
+            finish8<T>(epi, step, m, o, a.Cout, nv, v, bias8);
+        }
+        return;
+    }
     T *__restrict__ yg = static_cast<T *>(a.y);
     const T *__restrict__ resg = static_cast<const T *>(a.res);
     for (int it = tid; it < BP * (BC / 4); it += NW * 64) {   // four features of one row per thread, the waves' sums added in order
@@ -285,14 +304,14 @@ bool linear_stream_applies(const ConvArgs &a, int dt) {
     return linear_kernel_applies(a, dt) && a.P <= 128 && !ring_kernel_is_better(a, dt) && a.C * (int)es >= (dt == SOL_BF16 ? 4096 : 2048) && (double)a.P * a.C * es < 2147483648.0 && (double)a.Cout * a.Kp * es < 2147483648.0;
 }
 
-template <typename T> static sol_status launch_stream_typed(const ConvArgs &a, hipStream_t st) {
+template <typename T, bool FUSED> static sol_status launch_stream_typed(const ConvArgs &a, const LinearEpi &epi, hipStream_t st) {
     const int pb = a.P <= 16 ? 1 : a.P <= 32 ? 2 : 4, nrt = ceil_div(a.P, pb * 16);
     // 32 features per workgroup, or 16 when that takes fewer row loads in the rounds that 256 workgroups of one per CU make
     const int n32 = ceil_div(a.Cout, 32), n16 = ceil_div(a.Cout, 16);
     const bool wide = (long)ceil_div(n32 * nrt, 256) * (pb * 16 + 32) <= (long)ceil_div(n16 * nrt, 256) * (pb * 16 + 16);
     const int nft = wide ? n32 : n16;
     const dim3 grid(ceil_div(nft, 8) * 8 * nrt), block(512);
-#define STREAM(PB, CB, NS) hipLaunchKernelGGL((linear_stream_kernel<T, PB, CB, NS>), grid, block, 0, st, a, nrt, nft)
+#define STREAM(PB, CB, NS) hipLaunchKernelGGL((linear_stream_kernel<T, PB, CB, NS, FUSED>), grid, block, 0, st, a, epi, nrt, nft)
     if (wide) {
         if (pb == 1) STREAM(1, 2, 4);
         else if (pb == 2) STREAM(2, 2, 4);
@@ -308,7 +327,19 @@ template <typename T> static sol_status launch_stream_typed(const ConvArgs &a, h
 }
 
 sol_status launch_linear_stream(const ConvArgs &a, int dt, hipStream_t st) {
-    return dt == SOL_BF16 ? launch_stream_typed<bf16_t>(a, st) : launch_stream_typed<float>(a, st);
+    return dt == SOL_BF16 ? launch_stream_typed<bf16_t, false>(a, LinearEpi{}, st) : launch_stream_typed<float, false>(a, LinearEpi{}, st);
+}
+
+// The same with the epilogue of sol_linear_fused.  Rows of x and of the packed weights are whole fragments of 16 bytes.
+bool linear_rows_applies(const GemmArgs &g, int dt) {
+    const double es = (double)dtype_size(dt);
+    return g.M <= 128 && g.K * (int)es >= 2048 && (double)g.M * g.lda * es < 2147483648.0 && (double)g.N * g.ldb * es < 2147483648.0;
+}
+sol_status launch_linear_rows(const GemmArgs &g, int dt, hipStream_t st) {
+    ConvArgs a{};
+    a.x = g.a; a.w = g.b;
+    a.P = g.M; a.C = g.K; a.ldx = (int)g.lda; a.Cout = g.N; a.Kp = (int)g.ldb;
+    return dt == SOL_BF16 ? launch_stream_typed<bf16_t, true>(a, g.epi, st) : launch_stream_typed<float, true>(a, g.epi, st);
 }
 
 }  // namespace sol

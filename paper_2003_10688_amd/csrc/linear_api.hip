@@ -144,6 +144,7 @@ sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void
     a.b = w_packed; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
     a.M = l.m; a.N = l.out_f; a.K = l.in_f; a.nsplit = 1;
     a.epi = LinearEpi{bias, residual, y, preact, l.ldr, l.ldy, l.act, d};
+    if (linear_rows_applies(a, l.dtype)) return launch_linear_rows(a, l.dtype, st);
     return launch_linear_gemm(a, l.dtype, GEMM_FORWARD, st);
 }
 

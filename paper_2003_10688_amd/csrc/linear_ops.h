@@ -259,6 +259,8 @@ struct GemmArgs {
 };
 enum GemmKind { GEMM_FORWARD, GEMM_DX, GEMM_DW };
 sol_status launch_linear_gemm(GemmArgs a, int dt, GemmKind kind, hipStream_t st);
+bool linear_rows_applies(const GemmArgs &a, int dt);            // forward, up to 128 rows, weights streamed (linear.hip)
+sol_status launch_linear_rows(const GemmArgs &a, int dt, hipStream_t st);
 // copies [rows][cols] (pitch ld, any alignment) to dense rows of ldo elements, the rest of each row zeros
 sol_status launch_pad_rows(const void *x, long ld, void *out, long ldo, int rows, int cols, int dt, hipStream_t st);
 sol_status launch_dropout(const void *x, const void *res, void *y, int rows, int cols, int dt, const DropArgs &d, hipStream_t st);

@@ -76,6 +76,7 @@ SHAPES = [
     (2050, 40, 1700),
     (2600, 72, 5130),                  # the largest tiles, with remainders
     (5121, 136, 2570),
+    (1, 2048, 10), (16, 2056, 33), (32, 1032, 520), (65, 2088, 72), (128, 2048, 4100), (9, 4096, 8200), (64, 1031, 515),    # weights streamed past few rows, with remainders of all three
     (5121, 200, 3300), (5121, 3300, 150), (150, 3300, 5121), (264, 2056, 8200),     # more of them than the GPU has compute units, in each of the three products
 ]
 
