@@ -84,38 +84,41 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const T *__restrict__ dy
     part[(size_t)blockIdx.y * cols + c] = t;
 }
 
+// Four workgroups per CU, but 64 rows or more in each: up to 64 rows have one chunk, whose sums are db themselves.
 static int dz_rows_per_chunk(int rows, int cols) {
-    const int want = max(1, 1024 / ceil_div(cols, 256));         // four workgroups per CU
-    return (int)round_up((size_t)max(1, ceil_div(rows, want)), DZ_ROWS);
+    const int want = max(1, 1024 / ceil_div(cols, 256));
+    return (int)round_up((size_t)max(64, ceil_div(rows, want)), DZ_ROWS);
 }
 int linear_dz_chunks(int rows, int cols) { return rows > 0 ? ceil_div(rows, dz_rows_per_chunk(rows, cols)) : 0; }
 
-sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, float *db,
-                            hipStream_t st) {
-    const int rpc = dz_rows_per_chunk(rows, cols), chunks = linear_dz_chunks(rows, cols);
-    float *p = !db ? nullptr : chunks == 1 ? db : part;
-    const dim3 grid(ceil_div(dz ? (int)ldz : cols, 256), chunks);
+sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, hipStream_t st) {
+    const int rpc = dz_rows_per_chunk(rows, cols);
+    const dim3 grid(ceil_div(dz ? (int)ldz : cols, 256), linear_dz_chunks(rows, cols));
     if (dt == SOL_BF16)
-        hipLaunchKernelGGL(linear_dz_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t *)dy, lddy, (const bf16_t *)z, (bf16_t *)dz, ldz, rows, cols, rpc, act, d, p);
+        hipLaunchKernelGGL(linear_dz_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t *)dy, lddy, (const bf16_t *)z, (bf16_t *)dz, ldz, rows, cols, rpc, act, d, part);
     else
-        hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(256), 0, st, (const float *)dy, lddy, (const float *)z, (float *)dz, ldz, rows, cols, rpc, act, d, p);
+        hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(256), 0, st, (const float *)dy, lddy, (const float *)z, (float *)dz, ldz, rows, cols, rpc, act, d, part);
     SOL_HIP(hipGetLastError());
-    return db && chunks != 1 ? launch_sum_parts(part, chunks, cols, db, SOL_F32, st) : SOL_OK;
+    return SOL_OK;
 }
 
-// out[i] = part[0][i] + part[1][i] + ..., in this order
-template <typename T> __global__ void __launch_bounds__(256) sum_parts_kernel(const float *__restrict__ part, int nsplit, long n, T *__restrict__ out) {
-    for (long i = blockIdx.x * 256l + threadIdx.x; i < n; i += gridDim.x * 256l) {
+__global__ void __launch_bounds__(256) sums_kernel(const SumJobs jobs) {
+    const int b = (int)blockIdx.x, k = b >= jobs.first[2] ? 2 : b >= jobs.first[1] ? 1 : 0;
+    const SumJobs::Job &j = jobs.job[k];
+    const long stride = (long)(jobs.first[k + 1] - jobs.first[k]) * 256;
+    for (long i = (b - jobs.first[k]) * 256l + threadIdx.x; i < j.n; i += stride) {
         float s = 0.f;
-        for (int k = 0; k < nsplit; k++) s += part[k * n + i];
-        Elem<T>::store(out + i, s);
+        for (int p = 0; p < j.nsplit; p++) s += j.part[p * j.n + i];
+        if (j.out_dt == SOL_BF16) Elem<bf16_t>::store(static_cast<bf16_t *>(j.out) + i, s);
+        else static_cast<float *>(j.out)[i] = s;
     }
 }
 
-sol_status launch_sum_parts(const float *part, int nsplit, long n, void *out, int out_dt, hipStream_t st) {
-    const dim3 grid((unsigned)min((n + 255) / 256, 8192l));
-    if (out_dt == SOL_BF16) hipLaunchKernelGGL(sum_parts_kernel<bf16_t>, grid, dim3(256), 0, st, part, nsplit, n, (bf16_t *)out);
-    else hipLaunchKernelGGL(sum_parts_kernel<float>, grid, dim3(256), 0, st, part, nsplit, n, (float *)out);
+sol_status launch_sums(SumJobs jobs, hipStream_t st) {
+    jobs.first[0] = 0;
+    for (int k = 0; k < 3; k++) jobs.first[k + 1] = jobs.first[k] + (k < jobs.count ? (int)min((jobs.job[k].n + 255) / 256, 8192l) : 0);
+    if (jobs.first[3] == 0) return SOL_OK;
+    hipLaunchKernelGGL(sums_kernel, dim3((unsigned)jobs.first[3]), dim3(256), 0, st, jobs);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }

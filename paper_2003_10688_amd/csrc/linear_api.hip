@@ -51,13 +51,6 @@ int pack_pitch(int n, int dt) { return (int)round_up((size_t)n, dt == SOL_BF16 ?
 bool rows_aligned(int ld, int cols, int dt) { return (ld * dtype_size(dt)) % 16 == 0 && (cols * dtype_size(dt)) % 16 == 0; }
 bool cut_needed(int k, int dt) { return (k * dtype_size(dt)) % 128 != 0; }
 
-// Parts of a reduction of K, so that a product of few tiles fills the GPU: about one workgroup per CU, each with four stages or more.
-int split_of(int M, int N, int K, int dt) {
-    const long tiles = (long)ceil_div(M, 64) * ceil_div(N, 64), stages = ceil_div(K, 128 / (int)dtype_size(dt));
-    if (tiles >= 192) return 1;
-    return (int)max(1l, min(min(256 / tiles, stages / 4), 16l));
-}
-
 struct ForwardPlan {
     size_t xpad, bytes;
     bool pad;
@@ -70,9 +63,9 @@ ForwardPlan forward_plan(const sol_linear_desc &l) {
 }
 
 struct BackwardPlan {
-    size_t dz, part, xpad, sums, bytes;     // offsets
+    size_t dz, part, xpad, dw_sums, dx_sums, bytes;     // offsets
     bool pad;
-    int dw_split, dx_split;
+    GemmPlan dw, dx;
 };
 BackwardPlan backward_plan(const sol_linear_desc &l) {
     BackwardPlan p{};
@@ -83,10 +76,10 @@ BackwardPlan backward_plan(const sol_linear_desc &l) {
     p.part = take((size_t)linear_dz_chunks(l.m, l.out_f) * l.out_f * 4);
     p.pad = !rows_aligned(l.ldx, l.in_f, l.dtype);
     p.xpad = take(p.pad ? (size_t)l.m * pack_pitch(l.in_f, l.dtype) * es : 0);
-    p.dw_split = split_of(l.out_f, l.in_f, l.m, l.dtype);
-    p.dx_split = split_of(l.m, l.in_f, l.out_f, l.dtype);
-    const size_t dw = p.dw_split > 1 ? (size_t)p.dw_split * l.out_f * l.in_f * 4 : 0, dx = p.dx_split > 1 ? (size_t)p.dx_split * l.m * l.in_f * 4 : 0;
-    p.sums = take(dw > dx ? dw : dx);
+    p.dw = plan_gemm(l.out_f, l.in_f, l.m, l.dtype, true);
+    p.dx = plan_gemm(l.m, l.in_f, l.out_f, l.dtype, true);
+    p.dw_sums = take(p.dw.split > 1 ? (size_t)p.dw.split * l.out_f * l.in_f * 4 : 0);
+    p.dx_sums = take(p.dx.split > 1 ? (size_t)p.dx.split * l.m * l.in_f * 4 : 0);
     p.bytes = at;
     return p;
 }
@@ -142,7 +135,7 @@ sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void
         a.a = workspace; a.lda = kp; a.a_row = row_bytes(kp, l.dtype); a.a_cut = 0;
     }
     a.b = w_packed; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
-    a.M = l.m; a.N = l.out_f; a.K = l.in_f; a.nsplit = 1;
+    a.M = l.m; a.N = l.out_f; a.K = l.in_f; a.plan = plan_gemm(l.m, l.out_f, l.in_f, l.dtype, false);
     a.epi = LinearEpi{bias, residual, y, preact, l.ldr, l.ldy, l.act, d};
     if (linear_rows_applies(a, l.dtype)) return launch_linear_rows(a, l.dtype, st);
     return launch_linear_gemm(a, l.dtype, GEMM_FORWARD, st);
@@ -158,9 +151,11 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
     SOL_REQUIRE(aligned16(dy) && aligned16(x) && aligned16(w_packed) && aligned16(preact) && aligned16(dx) && aligned16(dw) && aligned16(db), SOL_ERR_ALIGN,
                 "device pointers must be 16-byte aligned");
     hipStream_t st = (hipStream_t)stream;
+    SumJobs sums{};
     if (l.m == 0) {
-        if (dw) SOL_TRY(launch_sum_parts(nullptr, 0, (long)l.out_f * l.in_f, dw, dw_dtype, st));
-        return db ? launch_sum_parts(nullptr, 0, l.out_f, db, SOL_F32, st) : SOL_OK;
+        if (dw) sums.add(nullptr, 0, (long)l.out_f * l.in_f, dw, dw_dtype);
+        if (db) sums.add(nullptr, 0, l.out_f, db, SOL_F32);
+        return launch_sums(sums, st);
     }
     SOL_REQUIRE(dy && (x || !dw) && (w_packed || !dx), SOL_ERR_NULL, "dy, x (for dw) and w_packed (for dx) must not be NULL");
     SOL_REQUIRE(preact || l.act == SOL_ACT_NONE, SOL_ERR_NULL, "preact must not be NULL with an activation");
@@ -178,34 +173,38 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
     const long ldz = own_dz ? pack_pitch(l.out_f, l.dtype) : l.ldy;
     const void *dz = own_dz ? ws + p.dz : dy;
     const int dz_row = row_bytes(own_dz ? (int)ldz : l.out_f, l.dtype);
-    if (own_dz || db)
-        SOL_TRY(launch_linear_dz(dy, l.ldy, preact, own_dz ? ws + p.dz : nullptr, ldz, l.m, l.out_f, l.act, d, l.dtype, reinterpret_cast<float *>(ws + p.part), db, st));
+    if (own_dz || db) {
+        const int chunks = linear_dz_chunks(l.m, l.out_f);
+        float *part = !db ? nullptr : chunks == 1 ? db : reinterpret_cast<float *>(ws + p.part);
+        SOL_TRY(launch_linear_dz(dy, l.ldy, preact, own_dz ? ws + p.dz : nullptr, ldz, l.m, l.out_f, l.act, d, l.dtype, part, st));
+        if (db && chunks > 1) sums.add(part, chunks, l.out_f, db, SOL_F32);
+    }
     const int kp = pack_pitch(l.in_f, l.dtype);
+    GemmArgs ax{}, aw{};
     if (dx) {
-        GemmArgs a{};
-        a.a = dz; a.lda = ldz; a.a_row = dz_row; a.a_cut = !own_dz && cut_needed(l.out_f, l.dtype);
-        a.b = w_packed; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
-        a.M = l.m; a.N = l.in_f; a.K = l.out_f; a.nsplit = p.dx_split;
-        a.part = reinterpret_cast<float *>(ws + p.sums);
-        a.out = dx; a.ldo = l.in_f; a.out_dt = l.dtype;
-        SOL_TRY(launch_linear_gemm(a, l.dtype, GEMM_DX, st));
-        if (p.dx_split > 1) SOL_TRY(launch_sum_parts(a.part, p.dx_split, (long)l.m * l.in_f, dx, l.dtype, st));
+        ax.a = dz; ax.lda = ldz; ax.a_row = dz_row; ax.a_cut = !own_dz && cut_needed(l.out_f, l.dtype);
+        ax.b = w_packed; ax.ldb = kp; ax.b_row = row_bytes(kp, l.dtype);
+        ax.M = l.m; ax.N = l.in_f; ax.K = l.out_f; ax.plan = p.dx;
+        ax.part = reinterpret_cast<float *>(ws + p.dx_sums);
+        ax.out = dx; ax.ldo = l.in_f; ax.out_dt = l.dtype;
+        if (p.dx.split > 1) sums.add(ax.part, p.dx.split, (long)l.m * l.in_f, dx, l.dtype);
     }
     if (dw) {
-        GemmArgs a{};
-        a.a = dz; a.lda = ldz; a.a_row = dz_row;
-        a.b = x; a.ldb = l.ldx; a.b_row = row_bytes(l.in_f, l.dtype);
+        aw.a = dz; aw.lda = ldz; aw.a_row = dz_row;
+        aw.b = x; aw.ldb = l.ldx; aw.b_row = row_bytes(l.in_f, l.dtype);
         if (p.pad) {
             SOL_TRY(launch_pad_rows(x, l.ldx, ws + p.xpad, kp, l.m, l.in_f, l.dtype, st));
-            a.b = ws + p.xpad; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
+            aw.b = ws + p.xpad; aw.ldb = kp; aw.b_row = row_bytes(kp, l.dtype);
         }
-        a.M = l.out_f; a.N = l.in_f; a.K = l.m; a.nsplit = p.dw_split;
-        a.part = reinterpret_cast<float *>(ws + p.sums);
-        a.out = dw; a.ldo = l.in_f; a.out_dt = dw_dtype;
-        SOL_TRY(launch_linear_gemm(a, l.dtype, GEMM_DW, st));
-        if (p.dw_split > 1) SOL_TRY(launch_sum_parts(a.part, p.dw_split, (long)l.out_f * l.in_f, dw, dw_dtype, st));
+        aw.M = l.out_f; aw.N = l.in_f; aw.K = l.m; aw.plan = p.dw;
+        aw.part = reinterpret_cast<float *>(ws + p.dw_sums);
+        aw.out = dw; aw.ldo = l.in_f; aw.out_dt = dw_dtype;
+        if (p.dw.split > 1) sums.add(aw.part, p.dw.split, (long)l.out_f * l.in_f, dw, dw_dtype);
     }
-    return SOL_OK;
+    if (dx && dw) SOL_TRY(launch_linear_pair(ax, aw, l.dtype, st));
+    else if (dx) SOL_TRY(launch_linear_gemm(ax, l.dtype, GEMM_DX, st));
+    else if (dw) SOL_TRY(launch_linear_gemm(aw, l.dtype, GEMM_DW, st));
+    return launch_sums(sums, st);
 }
 
 sol_status sol_dropout(int rows, int cols, sol_dtype dt, const void *x, const sol_dropout_desc *drop, const void *residual, void *y, void *stream) {

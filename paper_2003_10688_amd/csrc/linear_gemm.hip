@@ -133,10 +133,10 @@ template <typename T, bool ACROSS, int BR, int N> struct Places {
 
 // Tile order.  Workgroups go to the eight XCDs in turn; each XCD takes a contiguous run of a sequence that walks the columns of eight rows of
 // tiles, so that what runs on it at one time is a block of about eight by four tiles and shares its operands in that L2.
-__device__ __forceinline__ bool pick_tile(const GemmArgs &a, int &split, int &tp, int &tc) {
+__device__ __forceinline__ bool pick_tile(const GemmArgs &a, int block, int &split, int &tp, int &tc) {
     const int ntiles = a.ntp * a.ntc, per = (ntiles + 7) >> 3;
-    split = (int)blockIdx.x / (per * 8);
-    const int bid = (int)blockIdx.x - split * per * 8, t = (bid & 7) * per + (bid >> 3);
+    split = block / (per * 8);
+    const int bid = block - split * per * 8, t = (bid & 7) * per + (bid >> 3);
     if (t >= ntiles) return false;
     const int g = t / (8 * a.ntc), in = t - g * 8 * a.ntc, rows = min(8, a.ntp - g * 8);
     // divisions run on the vector units: back to scalars, or every resource derived from them would be taken for different ones per lane
@@ -160,7 +160,7 @@ template <typename T, GemmKind KIND, int RP, int RC>
 __device__ __forceinline__ void write_results(const GemmArgs &a, int split, const f32x4_t (&acc)[RP][RC], int p0, int c0, int lane) {
     static_assert(RP % 2 == 0 && RC % 2 == 0, "two blocks at a time");
     const int lrow = lane & 15, lcol = (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
-    if (KIND == GEMM_FORWARD && a.nsplit <= 1) {
+    if (KIND == GEMM_FORWARD && a.plan.split <= 1) {
         const uint32_t step = drop_step(a.epi.drop);
 #pragma unroll 1
         for (int u = 0; u < RP * RC / 4; u++) {                 // one copy of the epilogue's code: 32 rows x 32 columns at a time
@@ -185,7 +185,7 @@ __device__ __forceinline__ void write_results(const GemmArgs &a, int split, cons
             float v[8];
             rows8(acc[j][i], acc[j][i + 1], v);
             if (m >= a.M || nv <= 0) return;
-            if (a.nsplit > 1) store8_any<float>(a.part + ((size_t)split * a.M + m) * a.N + n, v, nv);
+            if (a.plan.split > 1) store8_any<float>(a.part + ((size_t)split * a.M + m) * a.N + n, v, nv);
             else if (a.out_dt == SOL_F32) store8_any<float>(static_cast<float *>(a.out) + (size_t)m * a.ldo + n, v, nv);
             else store8_any<T>(static_cast<T *>(a.out) + (size_t)m * a.ldo + n, v, nv);
         });
@@ -234,24 +234,26 @@ template <int BK> struct Cursor<true, BK> {
     }
 };
 
-// KIND: GEMM_FORWARD (A, B along k), GEMM_DX (B across), GEMM_DW (both across).  WP x WC = 4 waves of RP x RC blocks of 16 x 16.
-template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int PERCU>
-__global__ void __launch_bounds__(256, PERCU) linear_tile_kernel(const GemmArgs a) {
+// KIND: GEMM_FORWARD (A, B along k), GEMM_DX (B across), GEMM_DW (both across).  WP x WC waves of RP x RC blocks of 16 x 16, a ring of NS stages.
+template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS> struct TileShape {
+    static constexpr int THREADS = WP * WC * 64, LDS_BYTES = NS * (WP * RP + WC * RC) * 16 * ROWB;
+};
+template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS>
+__device__ __forceinline__ void linear_tile(const GemmArgs &a, int block, unsigned char *lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool AX = KIND == GEMM_DW, BX = KIND != GEMM_FORWARD;
-    constexpr int NW = 4, ES = (int)sizeof(T), BP = WP * RP * 16, BC = WC * RC * 16, BK = ROWB / ES;
+    constexpr int NW = WP * WC, ES = (int)sizeof(T), BP = WP * RP * 16, BC = WC * RC * 16, BK = ROWB / ES;
     using TA = Tile<T, AX, BP>;
     using TB = Tile<T, BX, BC>;
     constexpr int STAGE = TA::BYTES + TB::BYTES, XL = TA::SEGS / NW, WL = TB::SEGS / NW, L = XL + WL;
     constexpr int READS = RP * Frag<T, AX>::READS + RC * Frag<T, BX>::READS;       // LDS instructions of half a stage
-    static_assert(WP * WC == NW && TA::SEGS % (2 * NW) == 0 && TB::SEGS % NW == 0 && BP <= 128, "waves; rows that a cursor covers");
-    static_assert(NS >= 2 && (NS - 1) * L < 64 && NS * STAGE <= 160 * 1024 / PERCU, "vmcnt; LDS");
-    __shared__ __align__(1024) unsigned char lds[NS * STAGE];
+    static_assert(TA::SEGS % (2 * NW) == 0 && TB::SEGS % NW == 0 && BP <= 128, "waves; rows that a cursor covers");
+    static_assert(NS >= 2 && (NS - 1) * L < 64 && NS * STAGE == TileShape<T, KIND, WP, WC, RP, RC, NS>::LDS_BYTES, "vmcnt; LDS");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wc = wave / WP;
     int split, tp, tc;
-    if (!pick_tile(a, split, tp, tc)) return;
+    if (!pick_tile(a, block, split, tp, tc)) return;
     const int p0 = tp * BP, c0 = tc * BC;
     const int nk = (a.K + BK - 1) / BK, s0 = split * a.steps, s1 = min(nk, s0 + a.steps);   // this part's stages
 
@@ -358,6 +360,21 @@ __global__ void __launch_bounds__(256, PERCU) linear_tile_kernel(const GemmArgs 
 #endif
 }
 
+template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int PERCU>
+__global__ void __launch_bounds__(WP * WC * 64, PERCU * WP * WC / 4) linear_tile_kernel(const GemmArgs a) {
+    using S = TileShape<T, KIND, WP, WC, RP, RC, NS>;
+    static_assert(S::LDS_BYTES <= 160 * 1024 / PERCU, "LDS");
+    __shared__ __align__(1024) unsigned char lds[S::LDS_BYTES];
+    linear_tile<T, KIND, WP, WC, RP, RC, NS>(a, (int)blockIdx.x, lds);
+}
+
+// dx and dW of a small layer in one launch: the first `first` workgroups have tiles of dx, the others of dW.
+template <typename T> __global__ void __launch_bounds__(256, 3) linear_pair_kernel(const GemmArgs dx, const GemmArgs dw, int first) {
+    __shared__ __align__(1024) unsigned char lds[TileShape<T, GEMM_DX, 2, 2, 2, 2, 3>::LDS_BYTES];
+    if ((int)blockIdx.x < first) linear_tile<T, GEMM_DX, 2, 2, 2, 2, 3>(dx, (int)blockIdx.x, lds);
+    else linear_tile<T, GEMM_DW, 2, 2, 2, 2, 3>(dw, (int)blockIdx.x - first, lds);
+}
+
 // ---- tiles of 256 x 256 ----------------------------------------------------------------------------------------------------------
 // One workgroup of eight waves per CU: a row or column fetched once serves 256 of the other operand, 32 bytes a clock at the full rate of the matrix units, where the path
 // from L2 to LDS gives 58.  A stage is four units of 16 KB: B0, B1 (columns 0 .. 127, 128 .. 255), A0, A1 (rows).  A wave has 64 rows of each half of A and 64 columns: it takes
@@ -374,9 +391,10 @@ __device__ __forceinline__ unsigned unit_bytes(bool across, int es, int first, i
     return rows > 0 ? (unsigned)(rows - 1) * pitch + (unsigned)row_bytes : 0u;
 }
 
-template <typename T, GemmKind KIND>
+template <GemmKind KIND>
 __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
 #if defined(__HIP_DEVICE_COMPILE__)
+    using T = bf16_t;
     constexpr bool AX = KIND == GEMM_DW, BX = KIND != GEMM_FORWARD;
     constexpr int NW = 8, ES = (int)sizeof(T), BK = ROWB / ES, UNIT = 16384, UL = UNIT / 1024 / NW, NU = 10;
     using TA = Tile<T, AX, 128>;
@@ -388,7 +406,7 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave & 1, wc = wave >> 1;
     int split, tp, tc;
-    if (!pick_tile(a, split, tp, tc)) return;
+    if (!pick_tile(a, (int)blockIdx.x, split, tp, tc)) return;
     const int p0 = tp * 256, c0 = tc * 256, nk = (a.K + BK - 1) / BK;
 
     const unsigned apitch = (unsigned)(a.lda * ES), bpitch = (unsigned)(a.ldb * ES), astep = AX ? BK * apitch : ROWB, bstep = BX ? BK * bpitch : ROWB;
@@ -567,36 +585,69 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
 #endif
 }
 
-static long tiles_of(GemmArgs &a, int dt, int bp, int bc) {     // fills in the tile counts; workgroups of the launch
-    a.ntp = ceil_div(a.M, bp);
-    a.ntc = ceil_div(a.N, bc);
-    a.nsplit = a.nsplit < 1 ? 1 : a.nsplit;
-    a.steps = ceil_div(ceil_div(a.K, ROWB / (int)dtype_size(dt)), a.nsplit);
-    return (long)ceil_div(a.ntp * a.ntc, 8) * 8 * a.nsplit;
+// ---- which kernel ----------------------------------------------------------------------------------------------------------------
+// Times of the kernels in us as fitted to 270 products of 16 .. 8192 rows, columns and steps on 256 CUs, `s` the 128-byte stages of the reduction.  They put the fastest kernel
+// first, or one within 3 %, in 19 of 20.
+//   bf16   64 x 64 tiles (three workgroups a CU): 0.36 + 0.22 s for up to 256 of them, 0.69 + 0.166 s for every 256 beyond
+//          128 x 128 tiles: 3.3 + 0.39 s for up to 256 (one workgroup a CU, a ring of four stages), 3.3 + 0.76 s for every 512 beyond (two a CU, rings of two)
+//          256 x 256 tiles: 7.0 + 1.04 s for every 256
+//   fp32   64 x 64 tiles: 0.87 + 0.55 s for every 256; 128 x 128 tiles: 2.85 + 1.88 s for every 256; 256 x 256 tiles were never better by more than 3 %
+// For instance 2048 x 2048 with a reduction of 8192 in bf16: 256 tiles of 128 x 128 take 65 us (67 by the formula), 1024 of 64 x 64 83.
+// A reduction in p parts makes p times as many tiles of 1 / p of the stages, and costs one more launch and the parts' way to memory and back.
+static double tile_time(long tiles, double s, int tile, int dt) {
+    const double rounds = (double)((tiles + 255) / 256);
+    if (dt == SOL_F32) return tile == 64 ? rounds * (0.87 + 0.55 * s) : rounds * (2.85 + 1.88 * s);
+    if (tile == 64) return rounds <= 1 ? 0.36 + 0.22 * s : rounds * (0.69 + 0.166 * s);
+    if (tile == 128) return rounds <= 1 ? 3.3 + 0.39 * s : (double)((tiles + 511) / 512) * (3.3 + 0.76 * s);
+    return rounds * (7.0 + 1.04 * s);
 }
 
-template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int PERCU> static sol_status launch_tile(GemmArgs a, int dt, hipStream_t st) {
-    const long blocks = tiles_of(a, dt, WP * RP * 16, WC * RC * 16);
-    hipLaunchKernelGGL((linear_tile_kernel<T, KIND, WP, WC, RP, RC, NS, PERCU>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+GemmPlan plan_gemm(int M, int N, int K, int dt, bool may_split) {
+    const long stages = ceil_div(K, ROWB / (int)dtype_size(dt));
+    GemmPlan best{64, 1};
+    double least = 0;
+    for (int tile = 64; tile <= (dt == SOL_BF16 ? 256 : 128); tile *= 2) {
+        const long tiles = (long)ceil_div(M, tile) * ceil_div(N, tile), most = may_split && tile < 256 ? min(16l, stages / 2) : 1;
+        for (long p = 1; p <= max(1l, most); p++) {
+            const double t = tile_time(tiles * p, (double)((stages + p - 1) / p), tile, dt) + (p > 1 ? 4.0 + 8e-6 * p * M * N / 4.0 : 0.0);
+            if (least == 0 || t < least) {
+                least = t;
+                best = GemmPlan{tile, (int)p};
+            }
+        }
+    }
+    return best;
+}
+
+static long tiles_of(GemmArgs &a, int dt, int tile) {     // fills in the tile counts; workgroups of the launch
+    a.ntp = ceil_div(a.M, tile);
+    a.ntc = ceil_div(a.N, tile);
+    a.steps = ceil_div(ceil_div(a.K, ROWB / (int)dtype_size(dt)), a.plan.split);
+    return (long)ceil_div(a.ntp * a.ntc, 8) * 8 * a.plan.split;
+}
+
+template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int PERCU> static void launch_tile(const GemmArgs &a, long blocks, hipStream_t st) {
+    hipLaunchKernelGGL((linear_tile_kernel<T, KIND, WP, WC, RP, RC, NS, PERCU>), dim3((unsigned)blocks), dim3(WP * WC * 64), 0, st, a);
+}
+
+template <typename T, GemmKind KIND> static sol_status launch_kind(GemmArgs a, int dt, hipStream_t st) {
+    int tile = a.plan.tile;
+    if (tile == 256) {                       // its offsets along a reduction over rows have 32 bits, requests of whole tiles behind the last row included
+        const double rows = a.K + 256.0, abytes = (KIND == GEMM_DW ? rows : 256.0) * a.lda * sizeof(T), bbytes = (KIND != GEMM_FORWARD ? rows : 256.0) * a.ldb * sizeof(T);
+        if (abytes >= 4294967296.0 || bbytes >= 4294967296.0) tile = 128;
+    }
+    const long blocks = tiles_of(a, dt, tile);
+    if (tile == 64) launch_tile<T, KIND, 2, 2, 2, 2, 3, 3>(a, blocks, st);
+    else if constexpr (sizeof(T) == 2) {
+        if (tile == 256) hipLaunchKernelGGL((linear_huge_kernel<KIND>), dim3((unsigned)blocks), dim3(512), 0, st, a);
+        else if (blocks <= 256) launch_tile<T, KIND, 2, 4, 4, 2, 4, 1>(a, blocks, st);
+        else launch_tile<T, KIND, 2, 4, 4, 2, 2, 2>(a, blocks, st);
+    } else launch_tile<T, KIND, 2, 4, 4, 2, 2, 2>(a, blocks, st);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
 
-template <typename T, GemmKind KIND> static sol_status launch_kind(GemmArgs a, int dt, hipStream_t st) {
-    const long huge = (long)ceil_div(a.M, 256) * ceil_div(a.N, 256), mid = (long)ceil_div(a.M, 128) * ceil_div(a.N, 128) * (a.nsplit < 1 ? 1 : a.nsplit);
-    // 32-bit offsets along the reduction
-    const double abytes = (KIND == GEMM_DW ? a.K + 256.0 : 256.0) * a.lda * sizeof(T), bbytes = (KIND != GEMM_FORWARD ? a.K + 256.0 : 256.0) * a.ldb * sizeof(T);
-    if (huge >= 200 && a.nsplit <= 1 && abytes < 4294967296.0 && bbytes < 4294967296.0) {
-        const long blocks = tiles_of(a, dt, 256, 256);
-        hipLaunchKernelGGL((linear_huge_kernel<T, KIND>), dim3((unsigned)blocks), dim3(512), 0, st, a);
-        SOL_HIP(hipGetLastError());
-        return SOL_OK;
-    }
-    if (mid >= 200) return launch_tile<T, KIND, 2, 2, 4, 4, 2, 2>(a, dt, st);
-    return launch_tile<T, KIND, 2, 2, 2, 2, 3, 3>(a, dt, st);
-}
-
-sol_status launch_linear_gemm(GemmArgs a, int dt, GemmKind kind, hipStream_t st) {
+sol_status launch_linear_gemm(const GemmArgs &a, int dt, GemmKind kind, hipStream_t st) {
     if (dt == SOL_BF16) {
         switch (kind) {
             case GEMM_FORWARD: return launch_kind<bf16_t, GEMM_FORWARD>(a, dt, st);
@@ -609,6 +660,18 @@ sol_status launch_linear_gemm(GemmArgs a, int dt, GemmKind kind, hipStream_t st)
         case GEMM_DX: return launch_kind<float, GEMM_DX>(a, dt, st);
         default: return launch_kind<float, GEMM_DW>(a, dt, st);
     }
+}
+
+sol_status launch_linear_pair(GemmArgs dx, GemmArgs dw, int dt, hipStream_t st) {
+    if (dx.plan.tile != 64 || dw.plan.tile != 64) {
+        const sol_status s = launch_linear_gemm(dx, dt, GEMM_DX, st);
+        return s != SOL_OK ? s : launch_linear_gemm(dw, dt, GEMM_DW, st);
+    }
+    const long first = tiles_of(dx, dt, 64), blocks = first + tiles_of(dw, dt, 64);
+    if (dt == SOL_BF16) hipLaunchKernelGGL(linear_pair_kernel<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, st, dx, dw, (int)first);
+    else hipLaunchKernelGGL(linear_pair_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, dx, dw, (int)first);
+    SOL_HIP(hipGetLastError());
+    return SOL_OK;
 }
 
 }  // namespace sol

@@ -245,29 +245,48 @@ __device__ __forceinline__ void finish_rows(const LinearEpi &e, uint32_t step, i
 // D[p][c] = sum_k A(p, k) B(c, k) for p < M, c < N, k < K.  An operand is stored along k ([p][k], ld elements between its rows) or across
 // it ([k][p]).  Base addresses and pitches are multiples of 16 bytes; an operand stored along k ends its rows with zeros up to a multiple of
 // 128 bytes, or has K a multiple of 16 bytes' worth of elements and a_cut set.
+struct GemmPlan {
+    int tile;                   // 64, 128 or 256 rows and columns
+    int split;                  // > 1: the reduction in so many parts; part s goes to `part` + s * M * N (fp32, dense), nothing else is written
+};
 struct GemmArgs {
     const void *a, *b;
     long lda, ldb;
     int a_row, b_row;           // bytes of a row that may be read (the pitch where it is this library's own buffer)
     int a_cut;                  // A, stored along k: elements >= K of a row are not zeros and have to be masked
     int M, N, K;
-    int nsplit;                 // > 1: the reduction in so many parts; part s goes to `part` + s * M * N (fp32, dense), nothing else is written
+    GemmPlan plan;
     float *part;
     void *out; long ldo; int out_dt;    // plain result (no epilogue)
     LinearEpi epi;
     int ntp, ntc, steps;        // set by the launcher: tiles of rows and columns; stages of a part
 };
 enum GemmKind { GEMM_FORWARD, GEMM_DX, GEMM_DW };
-sol_status launch_linear_gemm(GemmArgs a, int dt, GemmKind kind, hipStream_t st);
+GemmPlan plan_gemm(int M, int N, int K, int dt, bool may_split);
+sol_status launch_linear_gemm(const GemmArgs &a, int dt, GemmKind kind, hipStream_t st);
+sol_status launch_linear_pair(GemmArgs dx, GemmArgs dw, int dt, hipStream_t st);       // both products of the backward pass
 bool linear_rows_applies(const GemmArgs &a, int dt);            // forward, up to 128 rows, weights streamed (linear.hip)
 sol_status launch_linear_rows(const GemmArgs &a, int dt, hipStream_t st);
 // copies [rows][cols] (pitch ld, any alignment) to dense rows of ldo elements, the rest of each row zeros
 sol_status launch_pad_rows(const void *x, long ld, void *out, long ldo, int rows, int cols, int dt, hipStream_t st);
 sol_status launch_dropout(const void *x, const void *res, void *y, int rows, int cols, int dt, const DropArgs &d, hipStream_t st);
-// dz = act'(z) * dropout(dy) into rows of ldz elements (zeros behind the columns) unless dz is NULL; column sums of dz into db through part unless db is NULL
-sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, float *db,
-                            hipStream_t st);
-int linear_dz_chunks(int rows, int cols);      // rows of `cols` floats that launch_linear_dz writes to part
-sol_status launch_sum_parts(const float *part, int nsplit, long n, void *out, int out_dt, hipStream_t st);
+// dz = act'(z) * dropout(dy) into rows of ldz elements (zeros behind the columns) unless dz is NULL; column sums of dz over every chunk of rows into part
+// [linear_dz_chunks][cols] unless that is NULL
+sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, hipStream_t st);
+int linear_dz_chunks(int rows, int cols);
+// Sums of parts: out[i] = part[0][i] + part[1][i] + ..., in this order; zeros where there are no parts.  Up to three of them in one launch.
+struct SumJobs {
+    struct Job {
+        const float *part;
+        int nsplit;
+        long n;
+        void *out;
+        int out_dt;
+    } job[3];
+    int first[4];               // set by the launcher: workgroups in front of each job
+    int count;
+    void add(const float *part, int nsplit, long n, void *out, int out_dt) { job[count++] = Job{part, nsplit, n, out, out_dt}; }
+};
+sol_status launch_sums(SumJobs jobs, hipStream_t st);
 
 }  // namespace sol
