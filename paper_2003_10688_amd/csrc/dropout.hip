@@ -38,10 +38,10 @@ sol_status launch_dropout(const void *x, const void *res, void *y, int rows, int
 
 // dz = act'(z) * dropout(dy), and sums of its columns in 32 bits before it is rounded.  A workgroup takes 256 columns of a chunk of rows: 32 groups of 8
 // columns x 8 rows at a time.
-constexpr int DZ_ROWS = 8;
+constexpr int DZ_ROWS = 32;
 template <typename T>
-__global__ void __launch_bounds__(256) linear_dz_kernel(const T *__restrict__ dy, long lddy, const T *__restrict__ z, T *__restrict__ dz, long ldz, int rows, int cols,
-                                                        int rows_per_chunk, int act, const DropArgs d, float *__restrict__ part) {
+__global__ void __launch_bounds__(32 * DZ_ROWS) linear_dz_kernel(const T *__restrict__ dy, long lddy, const T *__restrict__ z, T *__restrict__ dz, long ldz, int rows, int cols,
+                                                                 int rows_per_chunk, int act, const DropArgs d, float *__restrict__ part) {
     __shared__ float red[DZ_ROWS][256 + 4];
     const int gl = threadIdx.x & 31, rl = threadIdx.x >> 5, n = (blockIdx.x * 32 + gl) * 8, nv = min(8, cols - n);
     const int r0 = blockIdx.y * rows_per_chunk, r1 = min(rows, r0 + rows_per_chunk);
@@ -77,46 +77,73 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const T *__restrict__ dy
     for (int e = 0; e < 8; e++) red[rl][gl * 8 + e] = sum[e];
     __syncthreads();
     const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
+    if (threadIdx.x >= 256 || c >= cols) return;
     float t = 0.f;
 #pragma unroll
     for (int r = 0; r < DZ_ROWS; r++) t += red[r][threadIdx.x];
     part[(size_t)blockIdx.y * cols + c] = t;
 }
 
-// Four workgroups per CU, but 64 rows or more in each: up to 64 rows have one chunk, whose sums are db themselves.
+// Two workgroups per CU, each with 32 rows or more; up to 64 rows are one chunk, whose sums are db themselves.
 static int dz_rows_per_chunk(int rows, int cols) {
-    const int want = max(1, 1024 / ceil_div(cols, 256));
-    return (int)round_up((size_t)max(64, ceil_div(rows, want)), DZ_ROWS);
+    const int want = max(1, 512 / ceil_div(cols, 256));
+    return rows <= 64 ? 64 : (int)round_up((size_t)max(1, ceil_div(rows, want)), DZ_ROWS);
 }
 int linear_dz_chunks(int rows, int cols) { return rows > 0 ? ceil_div(rows, dz_rows_per_chunk(rows, cols)) : 0; }
 
 sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, hipStream_t st) {
     const int rpc = dz_rows_per_chunk(rows, cols);
-    const dim3 grid(ceil_div(dz ? (int)ldz : cols, 256), linear_dz_chunks(rows, cols));
+    const dim3 grid(ceil_div(dz ? (int)ldz : cols, 256), linear_dz_chunks(rows, cols)), block(32 * DZ_ROWS);
     if (dt == SOL_BF16)
-        hipLaunchKernelGGL(linear_dz_kernel<bf16_t>, grid, dim3(256), 0, st, (const bf16_t *)dy, lddy, (const bf16_t *)z, (bf16_t *)dz, ldz, rows, cols, rpc, act, d, part);
+        hipLaunchKernelGGL(linear_dz_kernel<bf16_t>, grid, block, 0, st, (const bf16_t *)dy, lddy, (const bf16_t *)z, (bf16_t *)dz, ldz, rows, cols, rpc, act, d, part);
     else
-        hipLaunchKernelGGL(linear_dz_kernel<float>, grid, dim3(256), 0, st, (const float *)dy, lddy, (const float *)z, (float *)dz, ldz, rows, cols, rpc, act, d, part);
+        hipLaunchKernelGGL(linear_dz_kernel<float>, grid, block, 0, st, (const float *)dy, lddy, (const float *)z, (float *)dz, ldz, rows, cols, rpc, act, d, part);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
 
+// A workgroup sums 256 elements, or, where there are more than 16 parts (column sums), 32 elements in eight groups that take the parts in turn.
 __global__ void __launch_bounds__(256) sums_kernel(const SumJobs jobs) {
+    __shared__ float red[8][32];
     const int b = (int)blockIdx.x, k = b >= jobs.first[2] ? 2 : b >= jobs.first[1] ? 1 : 0;
     const SumJobs::Job &j = jobs.job[k];
-    const long stride = (long)(jobs.first[k + 1] - jobs.first[k]) * 256;
-    for (long i = (b - jobs.first[k]) * 256l + threadIdx.x; i < j.n; i += stride) {
+    const int groups = j.nsplit > 16 ? 8 : 1, wide = 256 / groups, lane = threadIdx.x & (wide - 1), group = threadIdx.x / wide;
+    const long n = j.n;
+    for (long i0 = (long)(b - jobs.first[k]) * wide; i0 < n; i0 += (long)(jobs.first[k + 1] - jobs.first[k]) * wide) {
+        const long i = i0 + lane;
+        const float *p = j.part + i;
         float s = 0.f;
-        for (int p = 0; p < j.nsplit; p++) s += j.part[p * j.n + i];
-        if (j.out_dt == SOL_BF16) Elem<bf16_t>::store(static_cast<bf16_t *>(j.out) + i, s);
-        else static_cast<float *>(j.out)[i] = s;
+        if (i < n) {
+            int q = group;
+            for (; q + 3 * groups < j.nsplit; q += 4 * groups) {          // four loads under way at a time
+                const float v0 = p[q * n], v1 = p[(q + groups) * n], v2 = p[(q + 2 * groups) * n], v3 = p[(q + 3 * groups) * n];
+                s += v0;
+                s += v1;
+                s += v2;
+                s += v3;
+            }
+            for (; q < j.nsplit; q += groups) s += p[q * n];
+        }
+        if (groups > 1) {
+            red[group][lane] = s;
+            __syncthreads();
+            s = 0.f;
+            for (int g = 0; g < groups; g++) s += red[g][lane];
+            __syncthreads();
+        }
+        if (group == 0 && i < n) {
+            if (j.out_dt == SOL_BF16) Elem<bf16_t>::store(static_cast<bf16_t *>(j.out) + i, s);
+            else static_cast<float *>(j.out)[i] = s;
+        }
     }
 }
 
 sol_status launch_sums(SumJobs jobs, hipStream_t st) {
     jobs.first[0] = 0;
-    for (int k = 0; k < 3; k++) jobs.first[k + 1] = jobs.first[k] + (k < jobs.count ? (int)min((jobs.job[k].n + 255) / 256, 8192l) : 0);
+    for (int k = 0; k < 3; k++) {
+        const int wide = jobs.job[k].nsplit > 16 ? 32 : 256;
+        jobs.first[k + 1] = jobs.first[k] + (k < jobs.count ? (int)min((jobs.job[k].n + wide - 1) / wide, 8192l) : 0);
+    }
     if (jobs.first[3] == 0) return SOL_OK;
     hipLaunchKernelGGL(sums_kernel, dim3((unsigned)jobs.first[3]), dim3(256), 0, st, jobs);
     SOL_HIP(hipGetLastError());

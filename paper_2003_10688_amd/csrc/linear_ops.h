@@ -274,7 +274,7 @@ sol_status launch_dropout(const void *x, const void *res, void *y, int rows, int
 // [linear_dz_chunks][cols] unless that is NULL
 sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, hipStream_t st);
 int linear_dz_chunks(int rows, int cols);
-// Sums of parts: out[i] = part[0][i] + part[1][i] + ..., in this order; zeros where there are no parts.  Up to three of them in one launch.
+// Sums of parts: out[i] = part[0][i] + part[1][i] + ..., in an order that the shape alone fixes; zeros where there are no parts.  Up to three of them in one launch.
 struct SumJobs {
     struct Job {
         const float *part;

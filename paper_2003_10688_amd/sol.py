@@ -337,7 +337,7 @@ def _packed(w, in_f, out_f, x):
 
 def _scratch(workspace, need, x):
     if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+        return x.new_empty(need, dtype=torch.uint8) if need else None
     if workspace.device != x.device or not workspace.is_contiguous():
         raise ValueError("workspace: a contiguous tensor on the operands' device is wanted")
     return workspace
@@ -355,9 +355,9 @@ def sol_linear_fused(x, w_packed, out_f, bias=None, act=ACT_NONE, drop=None, res
     xa, ldx = _rows(x, in_f, "x")
     _on_current(x)
     ra, ldr = _rows(residual, out_f, "residual", x) if residual is not None else (0, 0)
-    y = torch.empty((m, out_f), dtype=x.dtype, device=x.device) if out is None else out
+    y = x.new_empty((m, out_f)) if out is None else out
     ya, ldy = _rows(y, out_f, "out", x)
-    z = torch.empty((m, out_f), dtype=x.dtype, device=x.device) if want_preact else None
+    z = x.new_empty((m, out_f)) if want_preact else None
     ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldy, ldr)
     need = lib().sol_linear_fused_workspace_bytes(ld)
     ws = _scratch(workspace, need, x)
@@ -379,9 +379,9 @@ def sol_linear_backward(dy, x, w_packed, preact=None, act=ACT_NONE, drop=None, n
     wdt = x.dtype if dw_dtype is None else dw_dtype
     if wdt not in (torch.float32, torch.bfloat16):
         raise ValueError(f"dw_dtype: float32 or the layer's type is wanted, not {wdt}")
-    dx = torch.empty((m, in_f), dtype=x.dtype, device=x.device) if need_dx else None
-    dw = torch.empty((out_f, in_f), dtype=wdt, device=x.device) if need_dw else None
-    db = torch.empty(out_f, dtype=torch.float32, device=x.device) if need_db else None
+    dx = x.new_empty((m, in_f)) if need_dx else None
+    dw = x.new_empty((out_f, in_f), dtype=wdt) if need_dw else None
+    db = x.new_empty(out_f, dtype=torch.float32) if need_db else None
     ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldg, 0)
     ws = _scratch(workspace, lib().sol_linear_backward_workspace_bytes(ld), x)
     _check(lib().sol_linear_backward(ld, ga, xa, _packed(w_packed, in_f, out_f, x), _dense(preact, (m, out_f), "preact", x), drop, _addr(dx), _addr(dw),
