@@ -138,9 +138,15 @@ template <typename T> __device__ __forceinline__ void load8_any(const T *p, floa
 #pragma unroll
             for (int e = 0; e < 4; e++) { v[e] = __uint_as_float(a[e]); v[4 + e] = __uint_as_float(b[e]); }
         }
-    } else {
+    } else {                                                   // no branch between the loads, so that they are under way together
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = e < nv ? Elem<T>::load(p + e) : 0.f;
+        for (int e = 0; e < 8; e++) v[e] = 0.f;
+        if (nv > 0) {
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = Elem<T>::load(p + min(e, nv - 1));
+#pragma unroll
+            for (int e = 1; e < 8; e++) v[e] = e < nv ? v[e] : 0.f;
+        }
     }
 }
 template <typename T> __device__ __forceinline__ void store8_any(T *p, const float v[8], int nv) {
