@@ -129,7 +129,8 @@ __global__ void __launch_bounds__(512) linear_stream_kernel(const ConvArgs a, co
     const int tid = threadIdx.x, lane = tid & 63, lr = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int lslot = lane & 7, lrow = lane >> 3;
-    const unsigned xbytes = ((unsigned)(a.P - 1) * a.ldx + a.C) * ES, wbytes = (unsigned)a.Cout * a.Kp * ES;
+    // rows of a length that 16 bytes do not divide lie in a padded copy: their last piece is read whole
+    const unsigned xbytes = (unsigned)(a.P - 1) * a.ldx * ES + (((unsigned)a.C * ES + 15u) & ~15u), wbytes = (unsigned)a.Cout * a.Kp * ES;
     const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.x), 0, (int)xbytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.w), 0, (int)wbytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t xnull = __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(a.x), 0, 0, 0x00020000);
@@ -304,12 +305,19 @@ bool linear_stream_applies(const ConvArgs &a, int dt) {
     return linear_kernel_applies(a, dt) && a.P <= 128 && !ring_kernel_is_better(a, dt) && a.C * (int)es >= (dt == SOL_BF16 ? 4096 : 2048) && (double)a.P * a.C * es < 2147483648.0 && (double)a.Cout * a.Kp * es < 2147483648.0;
 }
 
-template <typename T, bool FUSED> static sol_status launch_stream_typed(const ConvArgs &a, const LinearEpi &epi, hipStream_t st) {
-    const int pb = a.P <= 16 ? 1 : a.P <= 32 ? 2 : 4, nrt = ceil_div(a.P, pb * 16);
+struct StreamGrid { int pb, nrt, nft; bool wide; };
+static StreamGrid stream_grid(int rows, int features) {
+    const int pb = rows <= 16 ? 1 : rows <= 32 ? 2 : 4, nrt = ceil_div(rows, pb * 16);
     // 32 features per workgroup, or 16 when that takes fewer row loads in the rounds that 256 workgroups of one per CU make
-    const int n32 = ceil_div(a.Cout, 32), n16 = ceil_div(a.Cout, 16);
+    const int n32 = ceil_div(features, 32), n16 = ceil_div(features, 16);
     const bool wide = (long)ceil_div(n32 * nrt, 256) * (pb * 16 + 32) <= (long)ceil_div(n16 * nrt, 256) * (pb * 16 + 16);
-    const int nft = wide ? n32 : n16;
+    return StreamGrid{pb, nrt, wide ? n32 : n16, wide};
+}
+
+template <typename T, bool FUSED> static sol_status launch_stream_typed(const ConvArgs &a, const LinearEpi &epi, hipStream_t st) {
+    const StreamGrid sg = stream_grid(a.P, a.Cout);
+    const int pb = sg.pb, nrt = sg.nrt, nft = sg.nft;
+    const bool wide = sg.wide;
     const dim3 grid(ceil_div(nft, 8) * 8 * nrt), block(512);
 #define STREAM(PB, CB, NS) hipLaunchKernelGGL((linear_stream_kernel<T, PB, CB, NS, FUSED>), grid, block, 0, st, a, epi, nrt, nft)
     if (wide) {
@@ -331,9 +339,22 @@ sol_status launch_linear_stream(const ConvArgs &a, int dt, hipStream_t st) {
 }
 
 // The same with the epilogue of sol_linear_fused.  Rows of x and of the packed weights are whole fragments of 16 bytes.
-bool linear_rows_applies(const GemmArgs &g, int dt) {
+// The time in us that tells it from the tile kernels (plan_gemm's is made the same way), negative where its 32-bit offsets do not reach: every round of 256 workgroups
+// costs a start, a sum over the waves and the stages of the longest wave.  Fitted to 150 products of 1 .. 256 rows, 64 .. 8192 -> 32 .. 16384, and held against 170 more of up to
+// 1500 rows: the choice between the two kinds is 0.5 % slower than the better one on average and 35 % at worst.  Tile kernel against here, us: one row
+// bf16 512 -> 1632 4.4, 4.7; 1728 -> 1200 7.8, 4.7; 48 rows 1024 -> 10272 6.4, 13.8; 3904 -> 3856 17.2, 12.0; 256 rows fp32 896 -> 3856 20.8, 27.7;
+// 4544 -> 96 81, 25; 16 rows fp32 7040 -> 7552 125, 34.
+double linear_rows_time(const GemmArgs &g, int dt) {
     const double es = (double)dtype_size(dt);
-    return g.M <= 128 && g.K * (int)es >= 2048 && (double)g.M * g.lda * es < 2147483648.0 && (double)g.N * g.ldb * es < 2147483648.0;
+    if ((double)g.M * g.lda * es >= 2147483648.0 || (double)g.N * g.ldb * es >= 2147483648.0) return -1.0;
+    static const double cost[2][3][2][2] = {                   // [fp32][16, 32 or 64 rows][16 or 32 features] a round, a stage
+        {{{1.36, 0.28}, {1.65, 0.90}}, {{1.77, 0.38}, {2.07, 1.07}}, {{1.41, 0.70}, {2.53, 1.05}}},
+        {{{1.61, 0.33}, {2.55, 0.84}}, {{3.28, 0.54}, {5.06, 1.14}}, {{2.31, 1.15}, {4.65, 2.09}}},
+    };
+    const StreamGrid sg = stream_grid(g.M, g.N);
+    const double *c = cost[dt == SOL_F32][sg.pb >> 1][sg.wide];
+    const long rounds = ((long)sg.nft * sg.nrt + 255) / 256, stages = ceil_div(ceil_div(g.K * (int)es, 128), 8);
+    return rounds * (c[0] + c[1] * stages);
 }
 sol_status launch_linear_rows(const GemmArgs &g, int dt, hipStream_t st) {
     ConvArgs a{};

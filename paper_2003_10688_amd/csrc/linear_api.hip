@@ -137,7 +137,8 @@ sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void
     a.b = w_packed; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
     a.M = l.m; a.N = l.out_f; a.K = l.in_f; a.plan = plan_gemm(l.m, l.out_f, l.in_f, l.dtype, false);
     a.epi = LinearEpi{bias, residual, y, preact, l.ldr, l.ldy, l.act, d};
-    if (linear_rows_applies(a, l.dtype)) return launch_linear_rows(a, l.dtype, st);
+    const double us = linear_rows_time(a, l.dtype);
+    if (us >= 0.0 && us < a.plan.us) return launch_linear_rows(a, l.dtype, st);
     return launch_linear_gemm(a, l.dtype, GEMM_FORWARD, st);
 }
 

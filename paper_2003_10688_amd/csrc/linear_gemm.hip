@@ -604,16 +604,12 @@ static double tile_time(long tiles, double s, int tile, int dt) {
 
 GemmPlan plan_gemm(int M, int N, int K, int dt, bool may_split) {
     const long stages = ceil_div(K, ROWB / (int)dtype_size(dt));
-    GemmPlan best{64, 1};
-    double least = 0;
+    GemmPlan best{64, 1, 0.0};
     for (int tile = 64; tile <= (dt == SOL_BF16 ? 256 : 128); tile *= 2) {
         const long tiles = (long)ceil_div(M, tile) * ceil_div(N, tile), most = may_split && tile < 256 ? min(16l, stages / 2) : 1;
         for (long p = 1; p <= max(1l, most); p++) {
             const double t = tile_time(tiles * p, (double)((stages + p - 1) / p), tile, dt) + (p > 1 ? 4.0 + 8e-6 * p * M * N / 4.0 : 0.0);
-            if (least == 0 || t < least) {
-                least = t;
-                best = GemmPlan{tile, (int)p};
-            }
+            if (best.us == 0.0 || t < best.us) best = GemmPlan{tile, (int)p, t};
         }
     }
     return best;

@@ -63,6 +63,7 @@ __device__ __forceinline__ void drop8(const DropArgs &d, uint32_t step, uint32_t
 // ---- activations ---------------------------------------------------------------------------------------------------------------
 // Infinite z give the limits (silu(-inf) = -0, not NaN); a NaN stays one, except that ReLU maps it to 0 as in every other kernel here.
 __device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896341f); }
+__device__ __forceinline__ float half_exp(float s) { return __builtin_amdgcn_exp2f(s * -0.72134752044448170f); }     // exp(-s / 2)
 __device__ __forceinline__ float at_least(float z, float lo) { return z < lo ? lo : z; }          // keeps a NaN
 __device__ __forceinline__ float within(float z, float lim) { return z > lim ? lim : z < -lim ? -lim : z; }
 
@@ -88,10 +89,9 @@ constexpr float TANH_2C = 1.5957691216057308f, TANH_CUBE = 0.044715f;      // ge
 __device__ __forceinline__ float act_forward(int act, float z) {
     switch (act) {
         case SOL_ACT_RELU: return __builtin_fmaxf(z, 0.f);
-        case SOL_ACT_GELU: {
-            z = at_least(z, -100.f);
-            const float q = normal_tail(__builtin_fabsf(z), fast_exp(-0.5f * z * z));
-            return z * (z < 0.f ? q : 1.f - q);
+        case SOL_ACT_GELU: {                                                // max(z, 0) - |z| Q(|z|)
+            const float a = __builtin_fminf(__builtin_fabsf(z), 100.f);
+            return __builtin_fmaf(-a, normal_tail(a, half_exp(a * a)), at_least(z, 0.f));
         }
         case SOL_ACT_GELU_TANH: z = at_least(z, -100.f); return z * sigmoid(TANH_2C * (z + TANH_CUBE * z * z * z));
         case SOL_ACT_SILU: z = at_least(z, -100.f); return z * sigmoid(z);
@@ -105,7 +105,7 @@ __device__ __forceinline__ float act_slope(int act, float z) {
         case SOL_ACT_RELU: return z > 0.f ? 1.f : 0.f;
         case SOL_ACT_GELU: {
             z = within(z, 100.f);
-            const float e = fast_exp(-0.5f * z * z), q = normal_tail(__builtin_fabsf(z), e);
+            const float e = half_exp(z * z), q = normal_tail(__builtin_fabsf(z), e);
             return (z < 0.f ? q : 1.f - q) + z * e * 0.3989422804014327f;
         }
         case SOL_ACT_GELU_TANH: {
@@ -254,6 +254,7 @@ __device__ __forceinline__ void finish_rows(const LinearEpi &e, uint32_t step, i
 struct GemmPlan {
     int tile;                   // 64, 128 or 256 rows and columns
     int split;                  // > 1: the reduction in so many parts; part s goes to `part` + s * M * N (fp32, dense), nothing else is written
+    double us;                  // estimate of the time
 };
 struct GemmArgs {
     const void *a, *b;
@@ -271,7 +272,7 @@ enum GemmKind { GEMM_FORWARD, GEMM_DX, GEMM_DW };
 GemmPlan plan_gemm(int M, int N, int K, int dt, bool may_split);
 sol_status launch_linear_gemm(const GemmArgs &a, int dt, GemmKind kind, hipStream_t st);
 sol_status launch_linear_pair(GemmArgs dx, GemmArgs dw, int dt, hipStream_t st);       // both products of the backward pass
-bool linear_rows_applies(const GemmArgs &a, int dt);            // forward, up to 128 rows, weights streamed (linear.hip)
+double linear_rows_time(const GemmArgs &a, int dt);            // forward, weights streamed past few rows (linear.hip): estimate of its time, negative where it cannot run
 sol_status launch_linear_rows(const GemmArgs &a, int dt, hipStream_t st);
 // copies [rows][cols] (pitch ld, any alignment) to dense rows of ldo elements, the rest of each row zeros
 sol_status launch_pad_rows(const void *x, long ld, void *out, long ldo, int rows, int cols, int dt, hipStream_t st);

@@ -104,6 +104,16 @@ def test_whole_numbers(sol, dt, rows, n_in, n_out):
             assert np.array_equal(host(dw32), wdw)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [1, 3, 33, 200, 300])
+def test_every_element_of_a_row_counts(sol, dt, rows):
+    """Ones times ones: the sum is the number of elements, for lengths that end anywhere in a 16-byte piece and in a stage."""
+    for n_in in (*range(1, 18), *range(509, 530), 1531, 2045, 2049):
+        x = dev(np.ones((rows, n_in), np.float32), dt)
+        y, _ = sol.sol_linear_fused(x, pack(np.ones((40, n_in), np.float32), dt), 40)
+        assert np.array_equal(host(y), grid(np.full((rows, 40), float(n_in)), dt)), n_in
+
+
 def close(got, want, tol, what):
     bad = np.abs(got - want) - tol
     assert np.all(np.isfinite(got)) and bad.max() <= 0, f"{what}: off by {np.abs(got - want).flat[bad.argmax()]:.3g}, {tol.flat[bad.argmax()]:.3g} allowed, at {np.unravel_index(bad.argmax(), bad.shape)}"
