@@ -309,20 +309,22 @@ def sol_linear(x, w_packed, bias, out_f, act=ACT_NONE, stream=None):
 
 def _rows(t, cols, what, like=None):
     """Address and pitch of a [rows][cols] device tensor whose rows are contiguous; `like`: what it has to match in rows, type and device."""
-    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{what}: rows of {cols} neighbouring elements are wanted, not a tensor of shape {tuple(t.shape)} and strides {t.stride()}")
-    if not t.is_cuda or t.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"{what}: a float32 or bfloat16 GPU tensor is wanted, not {t.dtype} on {t.device}")
-    if like is not None and (t.shape[0] != like.shape[0] or t.dtype != like.dtype or t.device != like.device):
-        raise ValueError(f"{what}: {t.shape[0]} rows of {t.dtype} on {t.device} do not go with {like.shape[0]} of {like.dtype} on {like.device}")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else cols
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] != cols or (stride[1] != 1 and cols > 1):
+        raise ValueError(f"{what}: rows of {cols} neighbouring elements are wanted, not a tensor of shape {tuple(shape)} and strides {stride}")
+    if like is None:
+        if not t.is_cuda or t.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"{what}: a float32 or bfloat16 GPU tensor is wanted, not {t.dtype} on {t.device}")
+    elif shape[0] != like.shape[0] or t.dtype != like.dtype or t.get_device() != like.get_device():
+        raise ValueError(f"{what}: {shape[0]} rows of {t.dtype} on {t.device} do not go with {like.shape[0]} of {like.dtype} on {like.device}")
+    return t.data_ptr(), stride[0] if shape[0] > 1 else cols
 
 
 def _dense(t, shape, what, like, dtype=None):
     """Address of an optional dense device tensor of this shape, on `like`'s device and of its type (or dtype)."""
     if t is None:
         return 0
-    if tuple(t.shape) != shape or not t.is_contiguous() or t.dtype != (dtype or like.dtype) or t.device != like.device:
+    if t.shape != shape or not t.is_contiguous() or t.dtype != (dtype or like.dtype) or t.get_device() != like.get_device():
         raise ValueError(f"{what}: a contiguous {dtype or like.dtype} tensor of shape {shape} on {like.device} is wanted, not {tuple(t.shape)} of {t.dtype} on {t.device}")
     return t.data_ptr()
 
@@ -330,21 +332,24 @@ def _dense(t, shape, what, like, dtype=None):
 def _packed(w, in_f, out_f, x):
     """Address of packed linear weights, checked for their size."""
     block = 64 if x.dtype == torch.bfloat16 else 32
-    if w.device != x.device or not w.is_contiguous() or w.numel() * w.element_size() != out_f * ((in_f + block - 1) // block * block) * x.element_size():
+    if w.get_device() != x.get_device() or not w.is_contiguous() or w.nbytes != out_f * ((in_f + block - 1) // block * block) * x.element_size():
         raise ValueError(f"w_packed: [{out_f}][{in_f}] packed for {x.dtype} on {x.device} is wanted")
     return w.data_ptr()
 
 
 def _scratch(workspace, need, x):
+    """Address and bytes of the caller's workspace, or of one made here (the third result keeps it alive until the call is enqueued)."""
     if workspace is None:
-        return x.new_empty(need, dtype=torch.uint8) if need else None
-    if workspace.device != x.device or not workspace.is_contiguous():
+        if not need:
+            return 0, 0, None
+        workspace = x.new_empty(need, dtype=torch.uint8)
+    elif workspace.get_device() != x.get_device() or not workspace.is_contiguous():
         raise ValueError("workspace: a contiguous tensor on the operands' device is wanted")
-    return workspace
+    return workspace.data_ptr(), workspace.nbytes, workspace
 
 
 def _on_current(x):
-    if x.get_device() != torch.cuda.current_device():
+    if x.get_device() != torch._C._cuda_getDevice():
         raise ValueError(f"tensors on {x.device}, but the current device is cuda:{torch.cuda.current_device()}: call under torch.cuda.device({x.get_device()})")
 
 
@@ -360,9 +365,9 @@ def sol_linear_fused(x, w_packed, out_f, bias=None, act=ACT_NONE, drop=None, res
     z = x.new_empty((m, out_f)) if want_preact else None
     ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldy, ldr)
     need = lib().sol_linear_fused_workspace_bytes(ld)
-    ws = _scratch(workspace, need, x)
+    wa, wbytes, keep = _scratch(workspace, need, x)
     _check(lib().sol_linear_fused(ld, xa, _packed(w_packed, in_f, out_f, x), _dense(bias, (out_f,), "bias", x, torch.float32), drop, ra, ya,
-                                  _addr(z), _addr(ws), ws.numel() * ws.element_size() if ws is not None else 0, _stream_handle(stream)))
+                                  z.data_ptr() if want_preact else 0, wa, wbytes, _stream_handle(stream)))
     return y, z
 
 
@@ -383,9 +388,9 @@ def sol_linear_backward(dy, x, w_packed, preact=None, act=ACT_NONE, drop=None, n
     dw = x.new_empty((out_f, in_f), dtype=wdt) if need_dw else None
     db = x.new_empty(out_f, dtype=torch.float32) if need_db else None
     ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldg, 0)
-    ws = _scratch(workspace, lib().sol_linear_backward_workspace_bytes(ld), x)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_linear_backward_workspace_bytes(ld), x)
     _check(lib().sol_linear_backward(ld, ga, xa, _packed(w_packed, in_f, out_f, x), _dense(preact, (m, out_f), "preact", x), drop, _addr(dx), _addr(dw),
-                                     BF16 if wdt == torch.bfloat16 else F32, _addr(db), _addr(ws), ws.numel() * ws.element_size() if ws is not None else 0, _stream_handle(stream)))
+                                     BF16 if wdt == torch.bfloat16 else F32, _addr(db), wa, wbytes, _stream_handle(stream)))
     return dx, dw, db
 
 
