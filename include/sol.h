@@ -232,8 +232,8 @@ typedef struct {
                                    features or more, at most 2^21; elements between the rows are neither read into a result nor written */
 } sol_linear_desc;
 
-/* Device scratch that sol_linear_fused needs, often 0: a copy of x when its rows do not start at multiples of 16 bytes or do not end on one, and
- * partial sums when there are too few rows to fill the GPU.  sol_linear_backward: dz, partial sums of dW and db, and such a copy. */
+/* Device scratch that sol_linear_fused needs, mostly 0: a copy of x when its rows do not start at multiples of 16 bytes or do not end on one.
+ * sol_linear_backward: dz, partial sums of dx, dW and db, and such a copy.  Calls that may run at the same time need scratch of their own. */
 size_t sol_linear_fused_workspace_bytes(const sol_linear_desc *ld);
 size_t sol_linear_backward_workspace_bytes(const sol_linear_desc *ld);
 

@@ -417,6 +417,8 @@ static sol_status plan_network(sol_network *net, const sol_layer *layers, int n_
         lp.L = layers[i];
         const sol_layer &L = lp.L;
         SOL_REQUIRE(L.src >= -1 && L.src < i, SOL_ERR_SHAPE, "layer %d: src %d must name an earlier layer", i, L.src);
+        if (L.kind == SOL_LAYER_CONV || L.kind == SOL_LAYER_DWCONV || L.kind == SOL_LAYER_LINEAR)
+            SOL_REQUIRE(L.act == SOL_ACT_NONE || L.act == SOL_ACT_RELU, SOL_ERR_UNSUPPORTED, "layer %d: activation %d (networks have none or ReLU)", i, L.act);
         lp.src = L.src == -1 ? i - 1 : L.src;
         lp.res = -1;
         lp.concat_into = -1;

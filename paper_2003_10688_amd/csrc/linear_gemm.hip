@@ -593,7 +593,8 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
 //          256 x 256 tiles: 7.0 + 1.04 s for every 256
 //   fp32   64 x 64 tiles: 0.87 + 0.55 s for every 256; 128 x 128 tiles: 2.85 + 1.88 s for every 256; 256 x 256 tiles were never better by more than 3 %
 // For instance 2048 x 2048 with a reduction of 8192 in bf16: 256 tiles of 128 x 128 take 65 us (67 by the formula), 1024 of 64 x 64 83.
-// A reduction in p parts makes p times as many tiles of 1 / p of the stages, and costs one more launch and the parts' way to memory and back.
+// A reduction in p parts makes p times as many tiles of 1 / p of the stages, and costs one more launch and the parts' way to memory and back; up to
+// 1024 tiles, 64 MB of parts.
 static double tile_time(long tiles, double s, int tile, int dt) {
     const double rounds = (double)((tiles + 255) / 256);
     if (dt == SOL_F32) return tile == 64 ? rounds * (0.87 + 0.55 * s) : rounds * (2.85 + 1.88 * s);
@@ -606,7 +607,7 @@ GemmPlan plan_gemm(int M, int N, int K, int dt, bool may_split) {
     const long stages = ceil_div(K, ROWB / (int)dtype_size(dt));
     GemmPlan best{64, 1, 0.0};
     for (int tile = 64; tile <= (dt == SOL_BF16 ? 256 : 128); tile *= 2) {
-        const long tiles = (long)ceil_div(M, tile) * ceil_div(N, tile), most = may_split && tile < 256 ? min(16l, stages / 2) : 1;
+        const long tiles = (long)ceil_div(M, tile) * ceil_div(N, tile), most = may_split && tile < 256 ? min(min(16l, stages / 2), 1024 / tiles) : 1;
         for (long p = 1; p <= max(1l, most); p++) {
             const double t = tile_time(tiles * p, (double)((stages + p - 1) / p), tile, dt) + (p > 1 ? 4.0 + 8e-6 * p * M * N / 4.0 : 0.0);
             if (best.us == 0.0 || t < best.us) best = GemmPlan{tile, (int)p, t};
@@ -629,7 +630,7 @@ template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int
 template <typename T, GemmKind KIND> static sol_status launch_kind(GemmArgs a, int dt, hipStream_t st) {
     int tile = a.plan.tile;
     if (tile == 256) {                       // its offsets along a reduction over rows have 32 bits, requests of whole tiles behind the last row included
-        const double rows = a.K + 256.0, abytes = (KIND == GEMM_DW ? rows : 256.0) * a.lda * sizeof(T), bbytes = (KIND != GEMM_FORWARD ? rows : 256.0) * a.ldb * sizeof(T);
+        const double rows = a.K + 512.0, abytes = (KIND == GEMM_DW ? rows : 256.0) * a.lda * sizeof(T), bbytes = (KIND != GEMM_FORWARD ? rows : 256.0) * a.ldb * sizeof(T);
         if (abytes >= 4294967296.0 || bbytes >= 4294967296.0) tile = 128;
     }
     const long blocks = tiles_of(a, dt, tile);

@@ -146,6 +146,19 @@ def test_other_calls_refuse_the_new_activations(sol):
         assert sol.lib().sol_linear(4, 16, 8, 0, C.c_void_p(FAKE), C.c_void_p(FAKE), C.c_void_p(0), act, C.c_void_p(FAKE), C.c_void_p(0)) == 2
 
 
+@pytest.mark.parametrize("kind", ["conv", "dw", "linear"])
+def test_networks_refuse_the_new_activations(sol, kind):
+    layer = {"kind": "linear", "out": 5} if kind == "linear" else {"kind": "conv", "cout": 8, "kh": 1, "kw": 1, "sh": 1, "sw": 1, "ph": 0, "pw": 0, "bn": False, "dw": kind == "dw"}
+    for act, want in ((sol.ACT_NONE, 0), (sol.ACT_RELU, 0), (sol.ACT_GELU, 6), (sol.ACT_GELU_TANH, 6), (sol.ACT_SILU, 6), (-1, 6)):      # 6: SOL_ERR_UNSUPPORTED
+        arr = sol.make_layer_array([layer])
+        arr[0].act = act
+        h = C.c_void_p(0)
+        st = sol.lib().sol_network_create(arr, 1, C.byref(sol.TensorDesc(2, 1, 1, 8, sol.BF16)), 0, C.byref(h))
+        assert st == want, (act, sol.lib().sol_last_error())
+        if st == 0:
+            sol.lib().sol_network_destroy(h)
+
+
 def test_binding_refuses_what_is_not_on_the_gpu(sol):
     import torch
 
