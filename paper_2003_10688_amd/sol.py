@@ -348,9 +348,12 @@ def _scratch(workspace, need, x):
     return workspace.data_ptr(), workspace.nbytes, workspace
 
 
-def _on_current(x):
-    if x.get_device() != torch._C._cuda_getDevice():
-        raise ValueError(f"tensors on {x.device}, but the current device is cuda:{torch.cuda.current_device()}: call under torch.cuda.device({x.get_device()})")
+def _on_current(x, stream):
+    """Handle of the stream to run on; the operands' device has to be the current one."""
+    device = torch._C._cuda_getDevice()
+    if x.get_device() != device:
+        raise ValueError(f"tensors on {x.device}, but the current device is cuda:{device}: call under torch.cuda.device({x.get_device()})")
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
 def sol_linear_fused(x, w_packed, out_f, bias=None, act=ACT_NONE, drop=None, residual=None, want_preact=False, out=None, workspace=None, stream=None):
@@ -358,16 +361,19 @@ def sol_linear_fused(x, w_packed, out_f, bias=None, act=ACT_NONE, drop=None, res
     drop: a Dropout.  Returns (y, z or None)."""
     m, in_f = x.shape
     xa, ldx = _rows(x, in_f, "x")
-    _on_current(x)
+    handle = _on_current(x, stream)
     ra, ldr = _rows(residual, out_f, "residual", x) if residual is not None else (0, 0)
-    y = x.new_empty((m, out_f)) if out is None else out
-    ya, ldy = _rows(y, out_f, "out", x)
+    if out is None:
+        y, ldy = x.new_empty((m, out_f)), out_f
+        ya = y.data_ptr()
+    else:
+        y = out
+        ya, ldy = _rows(y, out_f, "out", x)
     z = x.new_empty((m, out_f)) if want_preact else None
     ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldy, ldr)
-    need = lib().sol_linear_fused_workspace_bytes(ld)
-    wa, wbytes, keep = _scratch(workspace, need, x)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_linear_fused_workspace_bytes(ld), x)
     _check(lib().sol_linear_fused(ld, xa, _packed(w_packed, in_f, out_f, x), _dense(bias, (out_f,), "bias", x, torch.float32), drop, ra, ya,
-                                  z.data_ptr() if want_preact else 0, wa, wbytes, _stream_handle(stream)))
+                                  z.data_ptr() if want_preact else 0, wa, wbytes, handle))
     return y, z
 
 
@@ -379,7 +385,7 @@ def sol_linear_backward(dy, x, w_packed, preact=None, act=ACT_NONE, drop=None, n
     m, in_f = x.shape
     out_f = dy.shape[1]
     xa, ldx = _rows(x, in_f, "x")
-    _on_current(x)
+    handle = _on_current(x, stream)
     ga, ldg = _rows(dy, out_f, "dy", x)
     wdt = x.dtype if dw_dtype is None else dw_dtype
     if wdt not in (torch.float32, torch.bfloat16):
@@ -389,8 +395,8 @@ def sol_linear_backward(dy, x, w_packed, preact=None, act=ACT_NONE, drop=None, n
     db = x.new_empty(out_f, dtype=torch.float32) if need_db else None
     ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldg, 0)
     wa, wbytes, keep = _scratch(workspace, lib().sol_linear_backward_workspace_bytes(ld), x)
-    _check(lib().sol_linear_backward(ld, ga, xa, _packed(w_packed, in_f, out_f, x), _dense(preact, (m, out_f), "preact", x), drop, _addr(dx), _addr(dw),
-                                     BF16 if wdt == torch.bfloat16 else F32, _addr(db), wa, wbytes, _stream_handle(stream)))
+    _check(lib().sol_linear_backward(ld, ga, xa, _packed(w_packed, in_f, out_f, x), _dense(preact, (m, out_f), "preact", x), drop, dx.data_ptr() if need_dx else 0, dw.data_ptr() if need_dw else 0,
+                                     BF16 if wdt == torch.bfloat16 else F32, db.data_ptr() if need_db else 0, wa, wbytes, handle))
     return dx, dw, db
 
 
@@ -399,10 +405,10 @@ def sol_dropout(x, drop, residual=None, out=None, stream=None):
     cols = x.shape[-1]
     if x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda or not x.is_contiguous():
         raise ValueError(f"x: a contiguous float32 or bfloat16 GPU tensor is wanted, not {x.dtype} on {x.device}")
-    _on_current(x)
+    handle = _on_current(x, stream)
     y = torch.empty_like(x) if out is None else out
-    _check(lib().sol_dropout(x.numel() // cols if cols else 0, cols, dtype_of(x), x.data_ptr(), drop, _dense(residual, tuple(x.shape), "residual", x),
-                             _dense(y, tuple(x.shape), "out", x), _stream_handle(stream)))
+    _check(lib().sol_dropout(x.numel() // cols if cols else 0, cols, dtype_of(x), x.data_ptr(), drop, _dense(residual, x.shape, "residual", x),
+                             y.data_ptr() if out is None else _dense(y, x.shape, "out", x), handle))
     return y
 
 
