@@ -109,7 +109,8 @@ sol_status launch_linear(const ConvArgs &a, int dt, hipStream_t st) {
 // rows 49.8 -> 30.2, 1 row 36.3 -> 18.2.  With 64 rows the rows of x are twice the bytes of the weights on the way into a CU.
 // Weights packed so that a workgroup's stream is one contiguous run: 28.1 instead of 30.2 us with 1 row, 38.4 instead of 35.6
 // with 64 (so the pitch of the rows is not what bounds it).
-// FUSED: the epilogue of sol_linear_fused (activation, dropout, residual, z) in the place of scale, shift and ReLU.
+// FUSED: the epilogue of sol_linear_fused (activation, dropout, residual, z) in the place of scale, shift and ReLU.  It costs nothing that shows: 8 rows, 8192 -> 8192 with GELU and a
+// residual 30.9 us (4.3 TB/s); 64 rows fp32 4096 -> 4096 with SiLU and a residual 24.5 us, where the products alone take 14.
 template <typename T, int PB, int CB, int NS, bool FUSED>
 __global__ void __launch_bounds__(512) linear_stream_kernel(const ConvArgs a, const LinearEpi epi, int nrt, int nft) {
 #if defined(__HIP_DEVICE_COMPILE__)
