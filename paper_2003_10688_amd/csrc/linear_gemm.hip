@@ -158,29 +158,31 @@ __device__ __forceinline__ void rows8(const f32x4_t &x, const f32x4_t &y, float 
 }
 template <typename T, GemmKind KIND, int RP, int RC>
 __device__ __forceinline__ void write_results(const GemmArgs &a, int split, const f32x4_t (&acc)[RP][RC], int p0, int c0, int lane) {
-    static_assert(RP % 2 == 0 && RC % 2 == 0, "two blocks at a time");
+    static_assert(RP % 2 == 0 && (RC == 2 || RC % 4 == 0), "two or four blocks at a time");
     const int lrow = lane & 15, lcol = (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
     if (KIND == GEMM_FORWARD && a.plan.split <= 1) {
+        constexpr bool BESIDE = RC >= 4;                        // 16 rows x 64 columns at a time, or 32 x 32
         const uint32_t step = drop_step(a.epi.drop);
 #pragma unroll 1
-        for (int u = 0; u < RP * RC / 4; u++) {                 // one copy of the epilogue's code: 32 rows x 32 columns at a time
+        for (int u = 0; u < RP * RC / 4; u++) {                 // one copy of the epilogue's code
             f32x4_t b[2][2];
             static_for<RP * RC / 4>([&](auto U) {
-                constexpr int j = decltype(U)::value % (RP / 2) * 2, i = decltype(U)::value / (RP / 2) * 2;
-                if (u == decltype(U)::value) {
-                    b[0][0] = acc[j][i]; b[0][1] = acc[j][i + 1]; b[1][0] = acc[j + 1][i]; b[1][1] = acc[j + 1][i + 1];
+                constexpr int w = decltype(U)::value, j = BESIDE ? w / (RC / 4) : w % (RP / 2) * 2, i = BESIDE ? w % (RC / 4) * 4 : w / (RP / 2) * 2;
+                if (u == w) {
+                    b[0][0] = acc[j][i]; b[0][1] = acc[j][i + 1];
+                    if constexpr (BESIDE) { b[1][0] = acc[j][i + 2]; b[1][1] = acc[j][i + 3]; }
+                    else { b[1][0] = acc[j + 1][i]; b[1][1] = acc[j + 1][i + 1]; }
                 }
             });
-            const int m = p0 + u % (RP / 2) * 32 + lrow, n = c0 + u / (RP / 2) * 32 + lcol, nv = min(8, a.N - n);
-            float v[2][8], bias8[8];
+            const int m = p0 + (BESIDE ? u / (RC / 4) * 16 : u % (RP / 2) * 32) + lrow, n = c0 + (BESIDE ? u % (RC / 4) * 64 : u / (RP / 2) * 32) + lcol;
+            float v[2][8];
             rows8(b[0][0], b[0][1], v[0]);
             rows8(b[1][0], b[1][1], v[1]);
-            load_bias8(a.epi.bias, n, nv, bias8);
-            finish_rows<T>(a.epi, step, m, n, a.M, a.N, nv, v, bias8);
+            finish_two<T, BESIDE>(a.epi, step, m, n, a.M, a.N, v);
         }
     } else {
-        static_for<RP * RC / 2>([&](auto U) {
-            constexpr int j = decltype(U)::value % RP, i = decltype(U)::value / RP * 2;
+        static_for<RP * RC / 2>([&](auto U) {                   // the columns of a row one behind the other
+            constexpr int j = decltype(U)::value / (RC / 2), i = decltype(U)::value % (RC / 2) * 2;
             const int m = p0 + j * 16 + lrow, n = c0 + i * 16 + lcol, nv = min(8, a.N - n);
             float v[8];
             rows8(acc[j][i], acc[j][i + 1], v);
@@ -387,7 +389,9 @@ template <typename T> __global__ void __launch_bounds__(256, 3) linear_pair_kern
 // The two waves of a SIMD issue one instruction each at a time, and everything that is not a product has to fit beside the products: resources and lane offsets are
 // constants of the loop (a scalar offset moves along the reduction, and the range check includes it), and the loop is unrolled over the five stages after which the ring repeats.
 // What bounds it: the card's power limit, and the starts and ends of tiles, which nothing overlaps.  8192 x 8192 x 8192 takes 775 us (1.42 PFLOP/s, a stage 2500 cycles of which
-// the products need 2048); 8192 x 16384, 4096 845 us (1.30), 95 more with GELU, dropout and z stored (the epilogue is bound by its arithmetic: some 300 instructions for 8 elements).
+// the products need 2048); 8192 x 16384, 4096 860 us (1.28), 55 more with GELU, dropout and z
+// stored (the epilogue is bound by its arithmetic, some 300 instructions for 8 elements; with the halves of a line stored apart, 32 rows x 32 columns at a time, half as much again
+// went to memory, 803 for 536 MB, and it took 40 us more).
 // Also measured on the former, us: two groups of waves that take turns at the matrix units 938; two workgroups a CU with tiles of 256 x 128 904; four waves of 128 x 128 with a ring
 // of two stages 770, but 869 against 845 on the latter and 63 against 58 for 2048 x 8192, 2048; starts staggered over a CU's neighbours 778; one barrier a stage, 2 % slower.
 

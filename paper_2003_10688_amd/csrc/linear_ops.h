@@ -210,16 +210,22 @@ __device__ __forceinline__ void load_bias8(const float *bias, int n, int nv, flo
     }
 }
 
-// The same for rows m and m + 16 at once: their arithmetic is independent and fills the waits of one another.
-template <typename T>
-__device__ __forceinline__ void finish_rows(const LinearEpi &e, uint32_t step, int m, int n, int M, int N, int nv, float (&v)[2][8], const float (&bias8)[8]) {
-    const int nv0 = m < M ? nv : 0, nv1 = m + 16 < M ? nv : 0;
-    const size_t zat = (size_t)m * N + n, yat = (size_t)m * e.ldy + n;
+// The same for two groups of one product's results at once, whose arithmetic is independent and fills the waits of one another: columns n .. n + 7 and n + 32 .. n + 39 of row m (BESIDE:
+// both halves of a 128-byte line of bf16 are stored one behind the other), or of rows m and m + 16.
+template <typename T, bool BESIDE>
+__device__ __forceinline__ void finish_two(const LinearEpi &e, uint32_t step, int m, int n, int M, int N, float (&v)[2][8]) {
+    const int m1 = BESIDE ? m : m + 16, n1 = BESIDE ? n + 32 : n;
+    const int nv0 = m < M ? min(8, N - n) : 0, nv1 = m1 < M ? min(8, N - n1) : 0;
+    const size_t zat = (size_t)m * N + n, yat = (size_t)m * e.ldy + n, rat = (size_t)m * e.ldr + n;
+    const size_t zto = BESIDE ? 32 : (size_t)16 * N, yto = BESIDE ? 32 : (size_t)16 * e.ldy, rto = BESIDE ? 32 : (size_t)16 * e.ldr;
+    float b[2][8];
+    load_bias8(e.bias, n, min(8, N - n), b[0]);
+    if constexpr (BESIDE) load_bias8(e.bias, n1, min(8, N - n1), b[1]);
 #pragma unroll
-    for (int c = 0; c < 8; c++) { v[0][c] += bias8[c]; v[1][c] += bias8[c]; }
+    for (int c = 0; c < 8; c++) { v[0][c] += b[0][c]; v[1][c] += b[BESIDE][c]; }
     if (e.pre) {
         if (nv0 > 0) store8_any<T>(static_cast<T *>(e.pre) + zat, v[0], nv0);
-        if (nv1 > 0) store8_any<T>(static_cast<T *>(e.pre) + zat + (size_t)16 * N, v[1], nv1);
+        if (nv1 > 0) store8_any<T>(static_cast<T *>(e.pre) + zat + zto, v[1], nv1);
     }
     if (e.act != SOL_ACT_NONE) {
         switch (e.act) {
@@ -233,18 +239,17 @@ __device__ __forceinline__ void finish_rows(const LinearEpi &e, uint32_t step, i
     }
     if (e.drop.t) {
         drop8(e.drop, step, (uint32_t)m, (uint32_t)n >> 3, v[0]);
-        drop8(e.drop, step, (uint32_t)m + 16, (uint32_t)n >> 3, v[1]);
+        drop8(e.drop, step, (uint32_t)m1, (uint32_t)n1 >> 3, v[1]);
     }
     if (e.res) {
-        const size_t rat = (size_t)m * e.ldr + n;
         float r[2][8];
         load8_any<T>(static_cast<const T *>(e.res) + rat, r[0], nv0);
-        load8_any<T>(static_cast<const T *>(e.res) + rat + 16 * e.ldr, r[1], nv1);
+        load8_any<T>(static_cast<const T *>(e.res) + rat + rto, r[1], nv1);
 #pragma unroll
         for (int c = 0; c < 8; c++) { v[0][c] += r[0][c]; v[1][c] += r[1][c]; }
     }
     if (nv0 > 0) store8_any<T>(static_cast<T *>(e.y) + yat, v[0], nv0);
-    if (nv1 > 0) store8_any<T>(static_cast<T *>(e.y) + yat + 16 * e.ldy, v[1], nv1);
+    if (nv1 > 0) store8_any<T>(static_cast<T *>(e.y) + yat + yto, v[1], nv1);
 }
 
 // ---- launchers --------------------------------------------------------------------------------------------------------------------
