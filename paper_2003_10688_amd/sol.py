@@ -58,6 +58,8 @@ class Dropout(C.Structure):
                 raise ValueError("dropout's step is a device int32 tensor of one element")
             self.step_tensor = step
             step = step.data_ptr()
+        else:
+            self.step_tensor = None
         super().__init__(p, seed & 0xFFFFFFFFFFFFFFFF, call, step)
 
 
@@ -310,7 +312,7 @@ def sol_linear(x, w_packed, bias, out_f, act=ACT_NONE, stream=None):
 def _rows(t, cols, what, like=None):
     """Address and pitch of a [rows][cols] device tensor whose rows are contiguous; `like`: what it has to match in rows, type and device."""
     shape, stride = t.shape, t.stride()
-    if len(shape) != 2 or shape[1] != cols or (stride[1] != 1 and cols > 1):
+    if len(shape) != 2 or shape[1] != cols or (stride[1] != 1 and cols > 1) or (stride[0] < cols and shape[0] > 1):     # rows of an expanded tensor lie on each other
         raise ValueError(f"{what}: rows of {cols} neighbouring elements are wanted, not a tensor of shape {tuple(shape)} and strides {stride}")
     if like is None:
         if not t.is_cuda or t.dtype not in (torch.float32, torch.bfloat16):
@@ -348,11 +350,13 @@ def _scratch(workspace, need, x):
     return workspace.data_ptr(), workspace.nbytes, workspace
 
 
-def _on_current(x, stream):
-    """Handle of the stream to run on; the operands' device has to be the current one."""
+def _on_current(x, drop, stream):
+    """Handle of the stream to run on; the operands' device has to be the current one, and that of dropout's step."""
     device = torch._C._cuda_getDevice()
     if x.get_device() != device:
         raise ValueError(f"tensors on {x.device}, but the current device is cuda:{device}: call under torch.cuda.device({x.get_device()})")
+    if drop is not None and drop.step_tensor is not None and drop.step_tensor.get_device() != device:
+        raise ValueError(f"dropout's step is on {drop.step_tensor.device}, the operands on {x.device}")
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
@@ -361,7 +365,7 @@ def sol_linear_fused(x, w_packed, out_f, bias=None, act=ACT_NONE, drop=None, res
     drop: a Dropout.  Returns (y, z or None)."""
     m, in_f = x.shape
     xa, ldx = _rows(x, in_f, "x")
-    handle = _on_current(x, stream)
+    handle = _on_current(x, drop, stream)
     ra, ldr = _rows(residual, out_f, "residual", x) if residual is not None else (0, 0)
     if out is None:
         y, ldy = x.new_empty((m, out_f)), out_f
@@ -385,7 +389,7 @@ def sol_linear_backward(dy, x, w_packed, preact=None, act=ACT_NONE, drop=None, n
     m, in_f = x.shape
     out_f = dy.shape[1]
     xa, ldx = _rows(x, in_f, "x")
-    handle = _on_current(x, stream)
+    handle = _on_current(x, drop, stream)
     ga, ldg = _rows(dy, out_f, "dy", x)
     wdt = x.dtype if dw_dtype is None else dw_dtype
     if wdt not in (torch.float32, torch.bfloat16):
@@ -405,7 +409,7 @@ def sol_dropout(x, drop, residual=None, out=None, stream=None):
     cols = x.shape[-1]
     if x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda or not x.is_contiguous():
         raise ValueError(f"x: a contiguous float32 or bfloat16 GPU tensor is wanted, not {x.dtype} on {x.device}")
-    handle = _on_current(x, stream)
+    handle = _on_current(x, drop, stream)
     y = torch.empty_like(x) if out is None else out
     _check(lib().sol_dropout(x.numel() // cols if cols else 0, cols, dtype_of(x), x.data_ptr(), drop, _dense(residual, x.shape, "residual", x),
                              y.data_ptr() if out is None else _dense(y, x.shape, "out", x), handle))

@@ -360,6 +360,79 @@ def test_no_rows(sol):
     assert sol.sol_dropout(torch.empty((0, 16), device="cuda:0"), sol.Dropout(0.5, 1)).shape == (0, 16)
 
 
+def test_expanded_rows_are_refused(sol):
+    """Rows that lie on each other have no pitch."""
+    x, w, row = torch.zeros((4, 32), device="cuda:0"), pack(np.ones((8, 32)), "f32"), torch.zeros((1, 8), device="cuda:0")
+    bad = [lambda: sol.sol_linear_fused(x[:1].expand(4, 32), w, 8), lambda: sol.sol_linear_fused(x, w, 8, residual=row.expand(4, 8)), lambda: sol.sol_linear_fused(x, w, 8, out=row.expand(4, 8)),
+           lambda: sol.sol_linear_backward(row.expand(4, 8), x, w), lambda: sol.sol_linear_fused(x.as_strided((4, 32), (16, 1)), w, 8)]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} was not refused")
+
+
+@pytest.mark.parametrize("dt,pitch", [("bf16", 30000), ("f32", 30000), ("bf16", 30002)])
+def test_rows_that_span_more_than_4_gb(sol, dt, pitch):
+    """Views of one wide tensor (4.2 and 8.4 GB) give the bits that dense tensors give; 30002: x and dy are copied to aligned rows."""
+    rows, n_in, n_out = 70000, 72, 264
+    gen = torch.Generator(device="cuda:0").manual_seed(3)
+    rnd = lambda *s: torch.randn(s, generator=gen, device="cuda:0").to(TDT[dt])  # noqa: E731
+    wide = torch.full((rows, pitch), float("nan"), dtype=TDT[dt], device="cuda:0")
+    x, g, r, out = (wide[:, at:at + n] for at, n in ((0, n_in), (1024, n_out), (4096, n_out), (8192, n_out)))
+    for t in (x, g, r):
+        t.copy_(rnd(rows, t.shape[1]))
+    w, d = rnd(n_out, 128 if dt == "bf16" else 96), sol.Dropout(0.25, 77, 2)
+    w[:, n_in:] = 0
+    for act in (sol.ACT_NONE, sol.ACT_SILU):
+        y, z = sol.sol_linear_fused(x, w, n_out, act=act, drop=d, residual=r, want_preact=True, out=out)
+        yd, zd = sol.sol_linear_fused(x.contiguous(), w, n_out, act=act, drop=d, residual=r.contiguous(), want_preact=True)
+        assert torch.equal(y, yd) and torch.equal(z, zd)
+        drop = None if act == sol.ACT_NONE else d                # without either, dy itself is what the products read
+        got = sol.sol_linear_backward(g, x, w, preact=z, act=act, drop=drop, need_db=act != sol.ACT_NONE)
+        want = sol.sol_linear_backward(g.contiguous(), x.contiguous(), w, preact=z, act=act, drop=drop, need_db=act != sol.ACT_NONE)
+        assert all(a is None and b is None or torch.equal(a, b) for a, b in zip(got, want))
+    assert torch.isnan(wide[:, n_in:1024]).all() and torch.isnan(wide[:, 8192 + n_out:]).all()
+
+
+def test_two_streams_at_once_and_graphs_that_share_a_workspace(sol):
+    """Layers of two sizes: run on two streams together, with a workspace each; captured into two graphs with one workspace, replayed in turn."""
+    rng = np.random.default_rng(12)
+    layers = []
+    for rows, n_in, n_out in ((300, 130, 700), (41, 900, 260)):
+        layers.append([dev(rng.standard_normal((rows, n_in)), "bf16", 3), pack(rng.standard_normal((n_out, n_in)) / 30, "bf16"), dev(rng.standard_normal((rows, n_out)), "bf16"), n_out])
+    d = sol.Dropout(0.1, 4, 1)
+
+    def run(k, **kw):
+        x, w, g, n_out = layers[k]
+        y, z = sol.sol_linear_fused(x, w, n_out, act=sol.ACT_GELU, drop=d, want_preact=True, **kw)
+        return (y, z) + sol.sol_linear_backward(g, x, w, preact=z, act=sol.ACT_GELU, drop=d, **kw)
+
+    want = [run(0), run(1)]
+    torch.cuda.synchronize()
+    spaces = [torch.empty(1 << 22, dtype=torch.uint8, device="cuda:0") for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    kept = [[] for _ in range(2)]
+    for _ in range(4):
+        for k in range(2):
+            with torch.cuda.stream(streams[k]):                  # the results belong to the stream that writes them
+                kept[k].append(run(k, workspace=spaces[k]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for k in range(2) for got in kept[k] for a, b in zip(got, want[k]))
+
+    graphs, outs = [], []
+    for k in range(2):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[k]):
+            outs.append(run(k, workspace=spaces[0]))
+    for i in range(3):
+        layers[i % 2][0].mul_(-1)
+        want = [[t.clone() for t in run(k)] for k in range(2)]
+        for k in (0, 1):
+            graphs[k].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for k in range(2) for a, b in zip(outs[k], want[k])), i
+
+
 def test_refusals_of_the_binding(sol):
     x, w = torch.zeros((4, 32), device="cuda:0"), pack(np.ones((8, 32)), "f32")
     bad = [lambda: sol.sol_linear_fused(x.t(), w, 8), lambda: sol.sol_linear_fused(x.double(), w, 8), lambda: sol.sol_linear_fused(x, w[:7], 8),
