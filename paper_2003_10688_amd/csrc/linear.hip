@@ -340,11 +340,11 @@ sol_status launch_linear_stream(const ConvArgs &a, int dt, hipStream_t st) {
 }
 
 // The same with the epilogue of sol_linear_fused.  Rows of x and of the packed weights are whole fragments of 16 bytes.
-// The time in us that tells it from the tile kernels (plan_gemm's is made the same way), negative where its 32-bit offsets do not reach: every round of 256 workgroups
-// costs a start, a sum over the waves and the stages of the longest wave.  Fitted to 150 products of 1 .. 256 rows, 64 .. 8192 -> 32 .. 16384, and held against 170 more of up to
-// 1500 rows: the choice between the two kinds is 0.5 % slower than the better one on average and 35 % at worst.  Tile kernel against here, us: one row
-// bf16 512 -> 1632 4.4, 4.7; 1728 -> 1200 7.8, 4.7; 48 rows 1024 -> 10272 6.4, 13.8; 3904 -> 3856 17.2, 12.0; 256 rows fp32 896 -> 3856 20.8, 27.7;
-// 4544 -> 96 81, 25; 16 rows fp32 7040 -> 7552 125, 34.
+// The time in us that tells it from the tile kernels (plan_gemm's is made the same way), negative where its 32-bit offsets do not reach: every round of 32 workgroups of an
+// XCD (which has every eighth tile of features) costs a start, a sum over the waves and the stages of the longest wave.  Fitted to 150 products of 1 .. 256 rows,
+// 64 .. 8192 -> 32 .. 16384, and held against 260 more of up to 4000 rows: the choice between the two kinds is 0.5 % slower than the better one on average and 35 % at worst
+// (1500 rows, 1792 -> 80, bf16: 11.1 for 8.2).  Tile kernel against here, us: one row bf16 512 -> 1632 4.4, 4.7; 1728 -> 1200 7.8, 4.7; 48 rows 1024 -> 10272 6.4, 13.8;
+// 3904 -> 3856 17.2, 12.0; 256 rows fp32 896 -> 3856 20.8, 27.7; 4544 -> 96 81, 25; 16 rows fp32 7040 -> 7552 125, 34.
 double linear_rows_time(const GemmArgs &g, int dt) {
     const double es = (double)dtype_size(dt);
     if ((double)g.M * g.lda * es >= 2147483648.0 || (double)g.N * g.ldb * es >= 2147483648.0) return -1.0;
@@ -354,7 +354,7 @@ double linear_rows_time(const GemmArgs &g, int dt) {
     };
     const StreamGrid sg = stream_grid(g.M, g.N);
     const double *c = cost[dt == SOL_F32][sg.pb >> 1][sg.wide];
-    const long rounds = ((long)sg.nft * sg.nrt + 255) / 256, stages = ceil_div(ceil_div(g.K * (int)es, 128), 8);
+    const long rounds = ((long)ceil_div(sg.nft, 8) * sg.nrt + 31) / 32, stages = ceil_div(ceil_div(g.K * (int)es, 128), 8);
     return rounds * (c[0] + c[1] * stages);
 }
 sol_status launch_linear_rows(const GemmArgs &g, int dt, hipStream_t st) {
