@@ -131,7 +131,7 @@ sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void
     GemmArgs a{};
     a.a = x; a.lda = l.ldx; a.a_row = row_bytes(l.in_f, l.dtype); a.a_cut = cut_needed(l.in_f, l.dtype);
     if (p.pad) {
-        SOL_TRY(launch_pad_rows(x, l.ldx, workspace, kp, l.m, l.in_f, l.dtype, st));
+        SOL_TRY(launch_pad_rows(PadRows{x, workspace, l.ldx, kp, l.m, l.in_f}, l.dtype, st));
         a.a = workspace; a.lda = kp; a.a_row = row_bytes(kp, l.dtype); a.a_cut = 0;
     }
     a.b = w_packed; a.ldb = kp; a.b_row = row_bytes(kp, l.dtype);
@@ -174,13 +174,16 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
     const long ldz = own_dz ? pack_pitch(l.out_f, l.dtype) : l.ldy;
     const void *dz = own_dz ? ws + p.dz : dy;
     const int dz_row = row_bytes(own_dz ? (int)ldz : l.out_f, l.dtype);
+    const int kp = pack_pitch(l.in_f, l.dtype);
+    const PadRows pad = dw && p.pad ? PadRows{x, ws + p.xpad, l.ldx, kp, l.m, l.in_f} : PadRows{nullptr, nullptr, 0, 8, 0, 0};
     if (own_dz || db) {
         const int chunks = linear_dz_chunks(l.m, l.out_f);
         float *part = !db ? nullptr : chunks == 1 ? db : reinterpret_cast<float *>(ws + p.part);
-        SOL_TRY(launch_linear_dz(dy, l.ldy, preact, own_dz ? ws + p.dz : nullptr, ldz, l.m, l.out_f, l.act, d, l.dtype, part, st));
+        SOL_TRY(launch_linear_dz(dy, l.ldy, preact, own_dz ? ws + p.dz : nullptr, ldz, l.m, l.out_f, l.act, d, l.dtype, part, pad, st));
         if (db && chunks > 1) sums.add(part, chunks, l.out_f, db, SOL_F32);
+    } else if (pad.x) {
+        SOL_TRY(launch_pad_rows(pad, l.dtype, st));
     }
-    const int kp = pack_pitch(l.in_f, l.dtype);
     GemmArgs ax{}, aw{};
     if (dx) {
         ax.a = dz; ax.lda = ldz; ax.a_row = dz_row; ax.a_cut = !own_dz && cut_needed(l.out_f, l.dtype);
@@ -194,7 +197,6 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
         aw.a = dz; aw.lda = ldz; aw.a_row = dz_row;
         aw.b = x; aw.ldb = l.ldx; aw.b_row = row_bytes(l.in_f, l.dtype);
         if (p.pad) {
-            SOL_TRY(launch_pad_rows(x, l.ldx, ws + p.xpad, kp, l.m, l.in_f, l.dtype, st));
             aw.b = ws + p.xpad; aw.ldb = kp; aw.b_row = row_bytes(kp, l.dtype);
         }
         aw.M = l.out_f; aw.N = l.in_f; aw.K = l.m; aw.plan = p.dw;

@@ -279,12 +279,19 @@ sol_status launch_linear_gemm(const GemmArgs &a, int dt, GemmKind kind, hipStrea
 sol_status launch_linear_pair(GemmArgs dx, GemmArgs dw, int dt, hipStream_t st);       // both products of the backward pass
 double linear_rows_time(const GemmArgs &a, int dt);            // forward, weights streamed past few rows (linear.hip): estimate of its time, negative where it cannot run
 sol_status launch_linear_rows(const GemmArgs &a, int dt, hipStream_t st);
-// copies [rows][cols] (pitch ld, any alignment) to dense rows of ldo elements, the rest of each row zeros
-sol_status launch_pad_rows(const void *x, long ld, void *out, long ldo, int rows, int cols, int dt, hipStream_t st);
+// A copy of [rows][cols] (pitch ld, any alignment) to dense rows of ldo elements, the rest of each row zeros
+struct PadRows {
+    const void *x;
+    void *out;
+    long ld, ldo;               // ldo: a multiple of 8
+    int rows, cols;
+};
+sol_status launch_pad_rows(const PadRows &p, int dt, hipStream_t st);
 sol_status launch_dropout(const void *x, const void *res, void *y, int rows, int cols, int dt, const DropArgs &d, hipStream_t st);
 // dz = act'(z) * dropout(dy) into rows of ldz elements (zeros behind the columns) unless dz is NULL; column sums of dz over every chunk of rows into part
-// [linear_dz_chunks][cols] unless that is NULL
-sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, hipStream_t st);
+// [linear_dz_chunks][cols] unless that is NULL; in the same launch the copy `pad` of as many rows, unless its x is NULL
+sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, long ldz, int rows, int cols, int act, const DropArgs &d, int dt, float *part, const PadRows &pad,
+                            hipStream_t st);
 int linear_dz_chunks(int rows, int cols);
 // Sums of parts: out[i] = part[0][i] + part[1][i] + ..., in an order that the shape alone fixes; zeros where there are no parts.  Up to three of them in one launch.
 struct SumJobs {
