@@ -135,48 +135,16 @@ sol_status launch_linear_dz(const void *dy, long lddy, const void *z, void *dz, 
     return SOL_OK;
 }
 
-// Parts are read once, coalesced.  A workgroup sums 256 elements, or, where there are more than 16 parts (column sums), 32 elements in eight groups that take the parts in turn
-// (8192 columns, 64 parts: 4.6 us, 10.8 with one thread per column).
 __global__ void __launch_bounds__(256) sums_kernel(const SumJobs jobs) {
-    __shared__ float red[8][32];
+    __shared__ float red[256];
     const int b = (int)blockIdx.x, k = b >= jobs.first[2] ? 2 : b >= jobs.first[1] ? 1 : 0;
-    const SumJobs::Job &j = jobs.job[k];
-    const int groups = j.nsplit > 16 ? 8 : 1, wide = 256 / groups, lane = threadIdx.x & (wide - 1), group = threadIdx.x / wide;
-    const long n = j.n;
-    for (long i0 = (long)(b - jobs.first[k]) * wide; i0 < n; i0 += (long)(jobs.first[k + 1] - jobs.first[k]) * wide) {
-        const long i = i0 + lane;
-        const float *p = j.part + i;
-        float s = 0.f;
-        if (i < n) {
-            int q = group;
-            for (; q + 3 * groups < j.nsplit; q += 4 * groups) {          // four loads under way at a time
-                const float v0 = p[q * n], v1 = p[(q + groups) * n], v2 = p[(q + 2 * groups) * n], v3 = p[(q + 3 * groups) * n];
-                s += v0;
-                s += v1;
-                s += v2;
-                s += v3;
-            }
-            for (; q < j.nsplit; q += groups) s += p[q * n];
-        }
-        if (groups > 1) {
-            red[group][lane] = s;
-            __syncthreads();
-            s = 0.f;
-            for (int g = 0; g < groups; g++) s += red[g][lane];
-            __syncthreads();
-        }
-        if (group == 0 && i < n) {
-            if (j.out_dt == SOL_BF16) Elem<bf16_t>::store(static_cast<bf16_t *>(j.out) + i, s);
-            else static_cast<float *>(j.out)[i] = s;
-        }
-    }
+    sum_parts(jobs.job[k], b - jobs.first[k], jobs.first[k + 1] - jobs.first[k], red);
 }
 
 sol_status launch_sums(SumJobs jobs, hipStream_t st) {
     jobs.first[0] = 0;
     for (int k = 0; k < 3; k++) {
-        const int wide = jobs.job[k].nsplit > 16 ? 32 : 256;
-        jobs.first[k + 1] = jobs.first[k] + (k < jobs.count ? (int)min((jobs.job[k].n + wide - 1) / wide, 8192l) : 0);
+        jobs.first[k + 1] = jobs.first[k] + (k < jobs.count ? sum_blocks(jobs.job[k]) : 0);
     }
     if (jobs.first[3] == 0) return SOL_OK;
     hipLaunchKernelGGL(sums_kernel, dim3((unsigned)jobs.first[3]), dim3(256), 0, st, jobs);

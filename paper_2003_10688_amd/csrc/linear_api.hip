@@ -176,11 +176,12 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
     const int dz_row = row_bytes(own_dz ? (int)ldz : l.out_f, l.dtype);
     const int kp = pack_pitch(l.in_f, l.dtype);
     const PadRows pad = dw && p.pad ? PadRows{x, ws + p.xpad, l.ldx, kp, l.m, l.in_f} : PadRows{nullptr, nullptr, 0, 8, 0, 0};
+    SumJob columns{};
     if (own_dz || db) {
         const int chunks = linear_dz_chunks(l.m, l.out_f);
         float *part = !db ? nullptr : chunks == 1 ? db : reinterpret_cast<float *>(ws + p.part);
         SOL_TRY(launch_linear_dz(dy, l.ldy, preact, own_dz ? ws + p.dz : nullptr, ldz, l.m, l.out_f, l.act, d, l.dtype, part, pad, st));
-        if (db && chunks > 1) sums.add(part, chunks, l.out_f, db, SOL_F32);
+        if (db && chunks > 1) columns = SumJob{part, chunks, l.out_f, db, SOL_F32};
     } else if (pad.x) {
         SOL_TRY(launch_pad_rows(pad, l.dtype, st));
     }
@@ -204,9 +205,13 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
         aw.out = dw; aw.ldo = l.in_f; aw.out_dt = dw_dtype;
         if (p.dw.split > 1) sums.add(aw.part, p.dw.split, (long)l.out_f * l.in_f, dw, dw_dtype);
     }
-    if (dx && dw) SOL_TRY(launch_linear_pair(ax, aw, l.dtype, st));
-    else if (dx) SOL_TRY(launch_linear_gemm(ax, l.dtype, GEMM_DX, st));
-    else if (dw) SOL_TRY(launch_linear_gemm(aw, l.dtype, GEMM_DW, st));
+    if (dx && dw && linear_pair_applies(ax, aw)) {
+        SOL_TRY(launch_linear_pair(ax, aw, columns, l.dtype, st));
+    } else {
+        if (dx) SOL_TRY(launch_linear_gemm(ax, l.dtype, GEMM_DX, st));
+        if (dw) SOL_TRY(launch_linear_gemm(aw, l.dtype, GEMM_DW, st));
+        if (columns.n > 0) sums.add(columns.part, columns.nsplit, columns.n, columns.out, columns.out_dt);
+    }
     return launch_sums(sums, st);
 }
 

@@ -373,11 +373,13 @@ __global__ void __launch_bounds__(WP * WC * 64, PERCU * WP * WC / 4) linear_tile
     linear_tile<T, KIND, WP, WC, RP, RC, NS>(a, (int)blockIdx.x, lds);
 }
 
-// dx and dW of a small layer in one launch: the first `first` workgroups have tiles of dx, the others of dW.
-template <typename T> __global__ void __launch_bounds__(256, 3) linear_pair_kernel(const GemmArgs dx, const GemmArgs dw, int first) {
+// dx and dW of a small layer in one launch, and the column sums that are db: workgroups below `first` have tiles of dx, below `second` of dW, the others sum.
+template <typename T> __global__ void __launch_bounds__(256, 3) linear_pair_kernel(const GemmArgs dx, const GemmArgs dw, int first, int second, const SumJob sum) {
     __shared__ __align__(1024) unsigned char lds[TileShape<T, GEMM_DX, 2, 2, 2, 2, 3>::LDS_BYTES];
-    if ((int)blockIdx.x < first) linear_tile<T, GEMM_DX, 2, 2, 2, 2, 3>(dx, (int)blockIdx.x, lds);
-    else linear_tile<T, GEMM_DW, 2, 2, 2, 2, 3>(dw, (int)blockIdx.x - first, lds);
+    const int b = (int)blockIdx.x;
+    if (b < first) linear_tile<T, GEMM_DX, 2, 2, 2, 2, 3>(dx, b, lds);
+    else if (b < second) linear_tile<T, GEMM_DW, 2, 2, 2, 2, 3>(dw, b - first, lds);
+    else sum_parts(sum, b - second, (int)gridDim.x - second, reinterpret_cast<float *>(lds));
 }
 
 // ---- tiles of 256 x 256 ----------------------------------------------------------------------------------------------------------
@@ -683,14 +685,12 @@ sol_status launch_linear_gemm(const GemmArgs &a, int dt, GemmKind kind, hipStrea
     }
 }
 
-sol_status launch_linear_pair(GemmArgs dx, GemmArgs dw, int dt, hipStream_t st) {
-    if (dx.plan.tile != 64 || dw.plan.tile != 64) {
-        const sol_status s = launch_linear_gemm(dx, dt, GEMM_DX, st);
-        return s != SOL_OK ? s : launch_linear_gemm(dw, dt, GEMM_DW, st);
-    }
-    const long first = tiles_of(dx, dt, 64), blocks = first + tiles_of(dw, dt, 64);
-    if (dt == SOL_BF16) hipLaunchKernelGGL(linear_pair_kernel<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, st, dx, dw, (int)first);
-    else hipLaunchKernelGGL(linear_pair_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, st, dx, dw, (int)first);
+bool linear_pair_applies(const GemmArgs &dx, const GemmArgs &dw) { return dx.plan.tile == 64 && dw.plan.tile == 64; }
+sol_status launch_linear_pair(GemmArgs dx, GemmArgs dw, const SumJob &sum, int dt, hipStream_t st) {
+    const long first = tiles_of(dx, dt, 64), second = first + tiles_of(dw, dt, 64);
+    const dim3 grid((unsigned)(second + (sum.n > 0 ? sum_blocks(sum) : 0)));
+    if (dt == SOL_BF16) hipLaunchKernelGGL(linear_pair_kernel<bf16_t>, grid, dim3(256), 0, st, dx, dw, (int)first, (int)second, sum);
+    else hipLaunchKernelGGL(linear_pair_kernel<float>, grid, dim3(256), 0, st, dx, dw, (int)first, (int)second, sum);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
