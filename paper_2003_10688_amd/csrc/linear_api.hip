@@ -64,8 +64,8 @@ ForwardPlan forward_plan(const sol_linear_desc &l) {
 
 struct BackwardPlan {
     size_t dz, part, xpad, dw_sums, dx_sums, bytes;     // offsets
-    bool pad;
-    GemmPlan dw, dx;
+    bool pad, pair;
+    GemmPlan dw, dx, pair_dw, pair_dx;      // one by one; in one launch (pair)
 };
 BackwardPlan backward_plan(const sol_linear_desc &l) {
     BackwardPlan p{};
@@ -78,8 +78,10 @@ BackwardPlan backward_plan(const sol_linear_desc &l) {
     p.xpad = take(p.pad ? (size_t)l.m * pack_pitch(l.in_f, l.dtype) * es : 0);
     p.dw = plan_gemm(l.out_f, l.in_f, l.m, l.dtype, true);
     p.dx = plan_gemm(l.m, l.in_f, l.out_f, l.dtype, true);
-    p.dw_sums = take(p.dw.split > 1 ? (size_t)p.dw.split * l.out_f * l.in_f * 4 : 0);
-    p.dx_sums = take(p.dx.split > 1 ? (size_t)p.dx.split * l.m * l.in_f * 4 : 0);
+    p.pair = plan_pair(l.m, l.in_f, l.out_f, l.dtype, p.dx, p.dw, &p.pair_dx, &p.pair_dw);
+    const int wparts = p.pair ? max(p.dw.split, p.pair_dw.split) : p.dw.split, xparts = p.pair ? max(p.dx.split, p.pair_dx.split) : p.dx.split;
+    p.dw_sums = take(wparts > 1 ? (size_t)wparts * l.out_f * l.in_f * 4 : 0);
+    p.dx_sums = take(xparts > 1 ? (size_t)xparts * l.m * l.in_f * 4 : 0);
     p.bytes = at;
     return p;
 }
@@ -185,14 +187,15 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
     } else if (pad.x) {
         SOL_TRY(launch_pad_rows(pad, l.dtype, st));
     }
+    const bool pair = p.pair && dx && dw;
     GemmArgs ax{}, aw{};
     if (dx) {
         ax.a = dz; ax.lda = ldz; ax.a_row = dz_row; ax.a_cut = !own_dz && cut_needed(l.out_f, l.dtype);
         ax.b = w_packed; ax.ldb = kp; ax.b_row = row_bytes(kp, l.dtype);
-        ax.M = l.m; ax.N = l.in_f; ax.K = l.out_f; ax.plan = p.dx;
+        ax.M = l.m; ax.N = l.in_f; ax.K = l.out_f; ax.plan = pair ? p.pair_dx : p.dx;
         ax.part = reinterpret_cast<float *>(ws + p.dx_sums);
         ax.out = dx; ax.ldo = l.in_f; ax.out_dt = l.dtype;
-        if (p.dx.split > 1) sums.add(ax.part, p.dx.split, (long)l.m * l.in_f, dx, l.dtype);
+        if (ax.plan.split > 1) sums.add(ax.part, ax.plan.split, (long)l.m * l.in_f, dx, l.dtype);
     }
     if (dw) {
         aw.a = dz; aw.lda = ldz; aw.a_row = dz_row;
@@ -200,12 +203,12 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
         if (p.pad) {
             aw.b = ws + p.xpad; aw.ldb = kp; aw.b_row = row_bytes(kp, l.dtype);
         }
-        aw.M = l.out_f; aw.N = l.in_f; aw.K = l.m; aw.plan = p.dw;
+        aw.M = l.out_f; aw.N = l.in_f; aw.K = l.m; aw.plan = pair ? p.pair_dw : p.dw;
         aw.part = reinterpret_cast<float *>(ws + p.dw_sums);
         aw.out = dw; aw.ldo = l.in_f; aw.out_dt = dw_dtype;
-        if (p.dw.split > 1) sums.add(aw.part, p.dw.split, (long)l.out_f * l.in_f, dw, dw_dtype);
+        if (aw.plan.split > 1) sums.add(aw.part, aw.plan.split, (long)l.out_f * l.in_f, dw, dw_dtype);
     }
-    if (dx && dw && linear_pair_applies(ax, aw)) {
+    if (pair) {
         SOL_TRY(launch_linear_pair(ax, aw, columns, l.dtype, st));
     } else {
         if (dx) SOL_TRY(launch_linear_gemm(ax, l.dtype, GEMM_DX, st));

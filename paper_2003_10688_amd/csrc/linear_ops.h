@@ -275,6 +275,8 @@ struct GemmArgs {
 };
 enum GemmKind { GEMM_FORWARD, GEMM_DX, GEMM_DW };
 GemmPlan plan_gemm(int M, int N, int K, int dt, bool may_split);
+// whether dx and dW are faster in one launch than as planned one by one; *px, *pw: their plans then
+bool plan_pair(int m, int in_f, int out_f, int dt, const GemmPlan &dx, const GemmPlan &dw, GemmPlan *px, GemmPlan *pw);
 sol_status launch_linear_gemm(const GemmArgs &a, int dt, GemmKind kind, hipStream_t st);
 double linear_rows_time(const GemmArgs &a, int dt);            // forward, weights streamed past few rows (linear.hip): estimate of its time, negative where it cannot run
 sol_status launch_linear_rows(const GemmArgs &a, int dt, hipStream_t st);
@@ -341,8 +343,7 @@ struct SumJobs {                // up to three of them in one launch
     void add(const float *part, int nsplit, long n, void *out, int out_dt) { job[count++] = SumJob{part, nsplit, n, out, out_dt}; }
 };
 sol_status launch_sums(SumJobs jobs, hipStream_t st);
-// dx and dW of a small layer, and sums whose parts are there already, in one launch; false: the layer is not small
-bool linear_pair_applies(const GemmArgs &dx, const GemmArgs &dw);
+// dx and dW as plan_pair has them, and a sum whose parts are there already, in one launch
 sol_status launch_linear_pair(GemmArgs dx, GemmArgs dw, const SumJob &sum, int dt, hipStream_t st);
 
 }  // namespace sol
