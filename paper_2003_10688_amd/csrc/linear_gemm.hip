@@ -394,8 +394,9 @@ template <typename T> __global__ void __launch_bounds__(256, 3) linear_pair_kern
 // the products need 2048); 8192 x 16384, 4096 860 us (1.28), 55 more with GELU, dropout and z
 // stored (the epilogue is bound by its arithmetic, some 300 instructions for 8 elements; with the halves of a line stored apart, 32 rows x 32 columns at a time, half as much again
 // went to memory, 803 for 536 MB, and it took 40 us more).
-// Also measured on the former, us: two groups of waves that take turns at the matrix units 938; two workgroups a CU with tiles of 256 x 128 904; four waves of 128 x 128 with a ring
-// of two stages 770, but 869 against 845 on the latter and 63 against 58 for 2048 x 8192, 2048; starts staggered over a CU's neighbours 778; one barrier a stage, 2 % slower.
+// Also measured on the former, us: two groups of waves that take turns at the matrix units 938; two workgroups a CU with tiles of 256 x 128 904; four waves of 128 x 128 with a
+// ring of five half stages 747 for 743 on one card, but 3 % behind on the latter, 12 % on 2048 x 8192, 2048 and 11 % as dx; starts staggered over a CU's neighbours 778; one barrier
+// a stage, 2 % slower.
 
 // Bytes from the corner of a unit (its first row, or column, is `first` of `limit`) to the end of what may be read
 __device__ __forceinline__ unsigned unit_bytes(bool across, int es, int first, int limit, int K, unsigned pitch, int row_bytes) {
