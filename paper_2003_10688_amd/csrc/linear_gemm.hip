@@ -160,7 +160,7 @@ template <typename T, GemmKind KIND, int RP, int RC>
 __device__ __forceinline__ void write_results(const GemmArgs &a, int split, const f32x4_t (&acc)[RP][RC], int p0, int c0, int lane) {
     static_assert(RP % 2 == 0 && (RC == 2 || RC % 4 == 0), "two or four blocks at a time");
     const int lrow = lane & 15, lcol = (lane >> 4 & 1) * 16 + (lane >> 5) * 8;
-    if (KIND == GEMM_FORWARD && a.plan.split <= 1) {
+    if constexpr (KIND == GEMM_FORWARD) {
         constexpr bool BESIDE = RC >= 4;                        // 16 rows x 64 columns at a time, or 32 x 32
         const uint32_t step = drop_step(a.epi.drop);
 #pragma unroll 1
@@ -240,9 +240,7 @@ template <int BK> struct Cursor<true, BK> {
 };
 
 // KIND: GEMM_FORWARD (A, B along k), GEMM_DX (B across), GEMM_DW (both across).  WP x WC waves of RP x RC blocks of 16 x 16, a ring of NS stages.
-template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS> struct TileShape {
-    static constexpr int THREADS = WP * WC * 64, LDS_BYTES = NS * (WP * RP + WC * RC) * 16 * ROWB;
-};
+constexpr int ring_bytes(int WP, int WC, int RP, int RC, int NS) { return NS * (WP * RP + WC * RC) * 16 * ROWB; }
 template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS>
 __device__ __forceinline__ void linear_tile(const GemmArgs &a, int block, unsigned char *lds) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -253,7 +251,7 @@ __device__ __forceinline__ void linear_tile(const GemmArgs &a, int block, unsign
     constexpr int STAGE = TA::BYTES + TB::BYTES, XL = TA::SEGS / NW, WL = TB::SEGS / NW, L = XL + WL;
     constexpr int READS = RP * Frag<T, AX>::READS + RC * Frag<T, BX>::READS;       // LDS instructions of half a stage
     static_assert(TA::SEGS % (2 * NW) == 0 && TB::SEGS % NW == 0 && BP <= 128, "waves; rows that a cursor covers");
-    static_assert(NS >= 2 && (NS - 1) * L < 64 && NS * STAGE == TileShape<T, KIND, WP, WC, RP, RC, NS>::LDS_BYTES, "vmcnt; LDS");
+    static_assert(NS >= 2 && (NS - 1) * L < 64 && NS * STAGE == ring_bytes(WP, WC, RP, RC, NS), "vmcnt; LDS");
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wp = wave % WP, wc = wave / WP;
@@ -367,15 +365,14 @@ __device__ __forceinline__ void linear_tile(const GemmArgs &a, int block, unsign
 
 template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int PERCU>
 __global__ void __launch_bounds__(WP * WC * 64, PERCU * WP * WC / 4) linear_tile_kernel(const GemmArgs a) {
-    using S = TileShape<T, KIND, WP, WC, RP, RC, NS>;
-    static_assert(S::LDS_BYTES <= 160 * 1024 / PERCU, "LDS");
-    __shared__ __align__(1024) unsigned char lds[S::LDS_BYTES];
+    static_assert(ring_bytes(WP, WC, RP, RC, NS) <= 160 * 1024 / PERCU, "LDS");
+    __shared__ __align__(1024) unsigned char lds[ring_bytes(WP, WC, RP, RC, NS)];
     linear_tile<T, KIND, WP, WC, RP, RC, NS>(a, (int)blockIdx.x, lds);
 }
 
 // dx and dW of a small layer in one launch, and the column sums that are db: workgroups below `first` have tiles of dx, below `second` of dW, the others sum.
 template <typename T> __global__ void __launch_bounds__(256, 3) linear_pair_kernel(const GemmArgs dx, const GemmArgs dw, int first, int second, const SumJob sum) {
-    __shared__ __align__(1024) unsigned char lds[TileShape<T, GEMM_DX, 2, 2, 2, 2, 3>::LDS_BYTES];
+    __shared__ __align__(1024) unsigned char lds[ring_bytes(2, 2, 2, 2, 3)];
     const int b = (int)blockIdx.x;
     if (b < first) linear_tile<T, GEMM_DX, 2, 2, 2, 2, 3>(dx, b, lds);
     else if (b < second) linear_tile<T, GEMM_DW, 2, 2, 2, 2, 3>(dw, b - first, lds);

@@ -394,6 +394,21 @@ def test_rows_that_span_more_than_4_gb(sol, dt, pitch):
     assert torch.isnan(wide[:, n_in:1024]).all() and torch.isnan(wide[:, 8192 + n_out:]).all()
 
 
+def test_large_tiles_at_the_end_of_32_bit_offsets(sol):
+    """dW over rows whose last lies 4.28 GB behind the first: whole numbers, so equal to the last bit to that of dense rows."""
+    rows, n, pitch = 21400, 4096, 100000
+    gen = torch.Generator(device="cuda:0").manual_seed(5)
+    ints = lambda: torch.randint(-1, 2, (rows, n), generator=gen, device="cuda:0").bfloat16()  # noqa: E731
+    x = torch.full((rows, pitch), float("nan"), dtype=torch.bfloat16, device="cuda:0")[:, :n]
+    x.copy_(ints())
+    g, w = ints(), torch.zeros((n, n), dtype=torch.bfloat16, device="cuda:0")
+    kw = dict(need_dx=False, need_db=False, dw_dtype=torch.float32)
+    _, dw, _ = sol.sol_linear_backward(g, x, w, **kw)
+    assert torch.equal(dw, sol.sol_linear_backward(g, x.contiguous(), w, **kw)[1])
+    want = g[:, :64].float().t() @ x[:, :64].float()
+    assert torch.equal(dw[:64, :64], want)
+
+
 def test_two_streams_at_once_and_graphs_that_share_a_workspace(sol):
     """Layers of two sizes: run on two streams together, with a workspace each; captured into two graphs with one workspace, replayed in turn."""
     rng = np.random.default_rng(12)
