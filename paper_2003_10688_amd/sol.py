@@ -51,6 +51,7 @@ class Dropout(C.Structure):
     """p: probability of dropping an element; seed: 64 bits; call: which dropout of the model this is; step: None, or a device int32
     tensor of one element that the kernels read when they run (a captured graph draws a new mask when it has changed)."""
     _fields_ = [("p", C.c_float), ("seed", C.c_uint64), ("call", C.c_uint32), ("step", C.c_void_p)]
+    step_tensor = None
 
     def __init__(self, p, seed, call=0, step=None):
         if step is not None:
@@ -58,8 +59,6 @@ class Dropout(C.Structure):
                 raise ValueError("dropout's step is a device int32 tensor of one element")
             self.step_tensor = step
             step = step.data_ptr()
-        else:
-            self.step_tensor = None
         super().__init__(p, seed & 0xFFFFFFFFFFFFFFFF, call, step)
 
 
