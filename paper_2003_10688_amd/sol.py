@@ -338,43 +338,64 @@ def _packed(w, in_f, out_f, x):
     return w.data_ptr()
 
 
-def _scratch(workspace, need, x):
-    """Address and bytes of the caller's workspace, or of one made here (the third result keeps it alive until the call is enqueued)."""
+def _new(x, shape, dtype, side):
+    """A tensor on x's device that a call on the stream `side` writes (None: the current stream).  Memory of a freed tensor belongs to the stream that it was allocated on and is handed
+    out again in that stream's order alone, so it has to come from `side`: from the current stream it could still be read by what that stream has to do, and be handed out there before
+    the call has run."""
+    if side is None:
+        return x.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(side):
+        return x.new_empty(shape, dtype=dtype)
+
+
+def _result(x, shape, dtype, side):
+    """Likewise, for the caller, who will use it on the current stream too: once freed, it also waits for what that stream does with it."""
+    t = _new(x, shape, dtype, side)
+    if side is not None:
+        t.record_stream(torch.cuda.current_stream())
+    return t
+
+
+def _scratch(workspace, need, x, side):
+    """Address and bytes of the caller's workspace, or of one made here, and what keeps it: it is freed when the call is enqueued, and only calls behind it on its stream can get its memory."""
     if workspace is None:
         if not need:
             return 0, 0, None
-        workspace = x.new_empty(need, dtype=torch.uint8)
+        workspace = _new(x, need, torch.uint8, side)
     elif workspace.get_device() != x.get_device() or not workspace.is_contiguous():
         raise ValueError("workspace: a contiguous tensor on the operands' device is wanted")
     return workspace.data_ptr(), workspace.nbytes, workspace
 
 
 def _on_current(x, drop, stream):
-    """Handle of the stream to run on; the operands' device has to be the current one, and that of dropout's step."""
+    """Handle of the stream to run on, and the stream itself unless it is the current one; the operands' device has to be the current one, and that of dropout's step."""
     device = torch._C._cuda_getDevice()
     if x.get_device() != device:
         raise ValueError(f"tensors on {x.device}, but the current device is cuda:{device}: call under torch.cuda.device({x.get_device()})")
     if drop is not None and drop.step_tensor is not None and drop.step_tensor.get_device() != device:
         raise ValueError(f"dropout's step is on {drop.step_tensor.device}, the operands on {x.device}")
-    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    current = torch._C._cuda_getCurrentRawStream(device)
+    return (current, None) if stream is None or stream.cuda_stream == current else (stream.cuda_stream, stream)
 
 
+# These calls run on the current stream, or on `stream`: it has to wait for what its operands still wait for, they have to live until the call has run, and another stream
+# has to wait for it before it uses the results; results and scratch are the call's own concern.
 def sol_linear_fused(x, w_packed, out_f, bias=None, act=ACT_NONE, drop=None, residual=None, want_preact=False, out=None, workspace=None, stream=None):
     """y = dropout(act(z)) + residual, z = x W^T + bias.  x [m][in] with rows of any pitch; residual, out: [m][out_f] likewise (out may be residual);
     drop: a Dropout.  Returns (y, z or None)."""
     m, in_f = x.shape
     xa, ldx = _rows(x, in_f, "x")
-    handle = _on_current(x, drop, stream)
+    handle, side = _on_current(x, drop, stream)
     ra, ldr = _rows(residual, out_f, "residual", x) if residual is not None else (0, 0)
     if out is None:
-        y, ldy = x.new_empty((m, out_f)), out_f
+        y, ldy = _result(x, (m, out_f), x.dtype, side), out_f
         ya = y.data_ptr()
     else:
         y = out
         ya, ldy = _rows(y, out_f, "out", x)
-    z = x.new_empty((m, out_f)) if want_preact else None
+    z = _result(x, (m, out_f), x.dtype, side) if want_preact else None
     ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldy, ldr)
-    wa, wbytes, keep = _scratch(workspace, lib().sol_linear_fused_workspace_bytes(ld), x)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_linear_fused_workspace_bytes(ld), x, side)
     _check(lib().sol_linear_fused(ld, xa, _packed(w_packed, in_f, out_f, x), _dense(bias, (out_f,), "bias", x, torch.float32), drop, ra, ya,
                                   z.data_ptr() if want_preact else 0, wa, wbytes, handle))
     return y, z
@@ -388,16 +409,16 @@ def sol_linear_backward(dy, x, w_packed, preact=None, act=ACT_NONE, drop=None, n
     m, in_f = x.shape
     out_f = dy.shape[1]
     xa, ldx = _rows(x, in_f, "x")
-    handle = _on_current(x, drop, stream)
+    handle, side = _on_current(x, drop, stream)
     ga, ldg = _rows(dy, out_f, "dy", x)
     wdt = x.dtype if dw_dtype is None else dw_dtype
     if wdt not in (torch.float32, torch.bfloat16):
         raise ValueError(f"dw_dtype: float32 or the layer's type is wanted, not {wdt}")
-    dx = x.new_empty((m, in_f)) if need_dx else None
-    dw = x.new_empty((out_f, in_f), dtype=wdt) if need_dw else None
-    db = x.new_empty(out_f, dtype=torch.float32) if need_db else None
+    dx = _result(x, (m, in_f), x.dtype, side) if need_dx else None
+    dw = _result(x, (out_f, in_f), wdt, side) if need_dw else None
+    db = _result(x, out_f, torch.float32, side) if need_db else None
     ld = LinearDesc(m, in_f, out_f, dtype_of(x), act, ldx, ldg, 0)
-    wa, wbytes, keep = _scratch(workspace, lib().sol_linear_backward_workspace_bytes(ld), x)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_linear_backward_workspace_bytes(ld), x, side)
     _check(lib().sol_linear_backward(ld, ga, xa, _packed(w_packed, in_f, out_f, x), _dense(preact, (m, out_f), "preact", x), drop, dx.data_ptr() if need_dx else 0, dw.data_ptr() if need_dw else 0,
                                      BF16 if wdt == torch.bfloat16 else F32, db.data_ptr() if need_db else 0, wa, wbytes, handle))
     return dx, dw, db
@@ -408,8 +429,8 @@ def sol_dropout(x, drop, residual=None, out=None, stream=None):
     cols = x.shape[-1]
     if x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda or not x.is_contiguous():
         raise ValueError(f"x: a contiguous float32 or bfloat16 GPU tensor is wanted, not {x.dtype} on {x.device}")
-    handle = _on_current(x, drop, stream)
-    y = torch.empty_like(x) if out is None else out
+    handle, side = _on_current(x, drop, stream)
+    y = _result(x, x.shape, x.dtype, side) if out is None else out
     _check(lib().sol_dropout(x.numel() // cols if cols else 0, cols, dtype_of(x), x.data_ptr(), drop, _dense(residual, x.shape, "residual", x),
                              y.data_ptr() if out is None else _dense(y, x.shape, "out", x), handle))
     return y

@@ -322,6 +322,47 @@ def test_another_stream_and_caller_workspace(sol):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_calls_on_other_streams_without_a_workspace(sol, dt):
+    """Two streams that have work in front of the calls, each with a forward and a backward pass of its own, while the current stream frees and allocates tensors of the sizes that
+    the calls take: neither stream's scratch or results are the other's or the current stream's, nor what the current stream still reads."""
+    rng = np.random.default_rng(21)
+    rows, n_in, n_out = 700, 333, 520                             # dz, a copy of x, column sums and parts are scratch
+    data = [(dev(rng.standard_normal((rows, n_in)), dt), pack(rng.standard_normal((n_out, n_in)) / 18, dt), dev(rng.standard_normal((rows, n_out)), dt)) for _ in range(2)]
+    d = sol.Dropout(0.1, 8)
+
+    def run(k, **kw):
+        x, w, g = data[k]
+        y, z = sol.sol_linear_fused(x, w, n_out, act=sol.ACT_GELU, drop=d, want_preact=True, **kw)
+        return (y, z) + sol.sol_linear_backward(g, x, w, preact=z, act=sol.ACT_GELU, drop=d, **kw) + (sol.sol_dropout(g, d, **kw),)
+
+    want = [run(0), run(1)]
+    big = torch.randn((4096, 4096), device="cuda:0")
+
+    def wait_a_while():                                           # milliseconds of the current stream
+        for _ in range(4):
+            big @ big
+
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        read = torch.randn((rows, n_out), device="cuda:0").to(TDT[dt])
+        copy = read.clone()
+        torch.cuda.synchronize()
+        for st in streams:
+            with torch.cuda.stream(st):
+                wait_a_while()
+        wait_a_while()
+        late = read + 0                                           # the current stream reads it behind that, but its memory is free at once
+        del read
+        got = [run(k, stream=streams[k]) for k in range(2)]
+        sizes = (rows * n_out, rows * n_out // 2, n_out * n_in, n_out * n_in // 2, rows * 512, rows * 192, rows * n_in, n_out, 1 << 20, 1 << 22)
+        junk = [torch.full((n,), float("nan"), device="cuda:0") for n in sizes for _ in range(3)]
+        torch.cuda.synchronize()
+        assert torch.equal(late, copy)
+        assert all(torch.equal(a, b) for k in range(2) for a, b in zip(got[k], want[k]))
+        del junk, got, late
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 def test_captured_and_replayed(sol, dt):
     """A captured training step of the block; the step word changes between the replays, and so do the masks."""
     a = block_inputs(dt, 130, 72, 288, seed=5)

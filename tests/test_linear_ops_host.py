@@ -171,3 +171,40 @@ def test_binding_refuses_what_is_not_on_the_gpu(sol):
         sol.sol_dropout(x, sol.Dropout(0.5, 1))
     with pytest.raises(ValueError):
         sol.Dropout(0.5, 1, step=torch.zeros(1, dtype=torch.int32))
+
+
+def test_scratch_and_results_come_from_the_stream_that_the_call_runs_on(sol, monkeypatch):
+    """Memory from the current stream could be handed out there again while the kernels on another stream still use it."""
+    import contextlib
+
+    import torch
+
+    log, side = [], object()
+
+    class Operand(torch.Tensor):
+        def new_empty(self, *a, **k):
+            log.append("alloc")
+            return torch.empty(4)
+
+        def record_stream(self, s):
+            log.append(s)
+
+    @contextlib.contextmanager
+    def stream(s):
+        assert s is side
+        log.append("enter")
+        yield
+        log.append("leave")
+
+    monkeypatch.setattr(torch.cuda, "stream", stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: "current")
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, s: log.append(s))
+    x = torch.zeros(4).as_subclass(Operand)
+    sol._scratch(None, 4, x, side)
+    assert log == ["enter", "alloc", "leave"]                  # freed behind the call, for that stream alone
+    log.clear()
+    sol._result(x, (4,), torch.float32, side)
+    assert log == ["enter", "alloc", "leave", "current"]       # freed by the caller, behind the uses on its stream
+    log.clear()
+    sol._scratch(None, 4, x, None), sol._result(x, (4,), torch.float32, None)
+    assert log == ["alloc", "alloc"]
