@@ -232,7 +232,8 @@ typedef struct {
                                    features or more, at most 2^21; elements between the rows are neither read into a result nor written */
 } sol_linear_desc;
 
-/* Device scratch that sol_linear_fused needs, mostly 0: a copy of x when its rows do not start at multiples of 16 bytes or do not end on one.
+/* Device scratch that sol_linear_fused needs, mostly 0: a copy of x when its rows do not start at multiples of 16 bytes or do not end on one (in rows of a
+ * multiple of 64 elements in bf16, 32 in fp32; at most 2^35 - 2^24 elements in all, which only half a billion rows of a few features exceed).
  * sol_linear_backward: dz, partial sums of dx, dW and db, and such a copy.  Calls that may run at the same time need scratch of their own. */
 size_t sol_linear_fused_workspace_bytes(const sol_linear_desc *ld);
 size_t sol_linear_backward_workspace_bytes(const sol_linear_desc *ld);

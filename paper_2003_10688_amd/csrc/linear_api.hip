@@ -32,6 +32,10 @@ sol_status check_pitch(const char *what, int rows, int cols, int *ld) {
     return SOL_OK;
 }
 
+int pack_pitch(int n, int dt) { return (int)round_up((size_t)n, dt == SOL_BF16 ? 64 : 32); }
+// rows that DMA can take as they are: they start and end at multiples of 16 bytes
+bool rows_aligned(int ld, int cols, int dt) { return (ld * dtype_size(dt)) % 16 == 0 && (cols * dtype_size(dt)) % 16 == 0; }
+
 // *l: the description with every pitch filled in
 sol_status check_linear(const sol_linear_desc *ld, sol_linear_desc *l) {
     SOL_REQUIRE(ld, SOL_ERR_NULL, "linear descriptor is NULL");
@@ -43,12 +47,15 @@ sol_status check_linear(const sol_linear_desc *ld, sol_linear_desc *l) {
     SOL_REQUIRE(l->act >= SOL_ACT_NONE && l->act <= SOL_ACT_SILU, SOL_ERR_SHAPE, "bad activation %d", l->act);
     SOL_TRY(check_pitch("x", l->m, l->in_f, &l->ldx));
     SOL_TRY(check_pitch("y", l->m, l->out_f, &l->ldy));
-    return check_pitch("residual", l->m, l->out_f, &l->ldr);
+    SOL_TRY(check_pitch("residual", l->m, l->out_f, &l->ldr));
+    // The copy of x to aligned rows counts its groups of 8 elements, and the step of its grid (2^21 threads at most) beyond the last of them, in 32 bits.  A few features
+    // make much more of a copy than of x: the element count of x does not bound it.
+    if (!rows_aligned(l->ldx, l->in_f, l->dtype))
+        SOL_REQUIRE((size_t)l->m * (pack_pitch(l->in_f, l->dtype) / 8) <= MAX_PAD_GROUPS, SOL_ERR_UNSUPPORTED, "%d rows of x to be copied to rows of %d elements: more than 2^35 - 2^24",
+                    l->m, pack_pitch(l->in_f, l->dtype));
+    return SOL_OK;
 }
 
-int pack_pitch(int n, int dt) { return (int)round_up((size_t)n, dt == SOL_BF16 ? 64 : 32); }
-// rows that DMA can take as they are: they start and end at multiples of 16 bytes
-bool rows_aligned(int ld, int cols, int dt) { return (ld * dtype_size(dt)) % 16 == 0 && (cols * dtype_size(dt)) % 16 == 0; }
 bool cut_needed(int k, int dt) { return (k * dtype_size(dt)) % 128 != 0; }
 
 struct ForwardPlan {

@@ -287,6 +287,7 @@ struct PadRows {
     long ld, ldo;               // ldo: a multiple of 8
     int rows, cols;
 };
+constexpr size_t MAX_PAD_GROUPS = 0x100000000ull - 0x200000ull;         // rows * (ldo / 8) at most: counted in 32 bits, and a grid has 2^21 threads at most
 sol_status launch_pad_rows(const PadRows &p, int dt, hipStream_t st);
 sol_status launch_dropout(const void *x, const void *res, void *y, int rows, int cols, int dt, const DropArgs &d, hipStream_t st);
 // dz = act'(z) * dropout(dy) into rows of ldz elements (zeros behind the columns) unless dz is NULL; column sums of dz over every chunk of rows into part

@@ -435,6 +435,25 @@ def test_rows_that_span_more_than_4_gb(sol, dt, pitch):
     assert torch.isnan(wide[:, n_in:1024]).all() and torch.isnan(wide[:, 8192 + n_out:]).all()
 
 
+def test_as_many_rows_as_are_copied(sol):
+    """The largest copy of x that is not refused (68.7 GB): every row of y, and dW, whose copy runs beside dz.  Whole numbers, so equal to the last bit."""
+    rows = (1 << 29) - (1 << 18)
+    if torch.cuda.mem_get_info()[0] < 170e9:
+        pytest.skip("needs 170 GB of free memory")
+    gen = torch.Generator(device="cuda:0").manual_seed(9)
+    x = torch.empty((rows, 3), dtype=torch.bfloat16, device="cuda:0")
+    for part in x.split(1 << 26):
+        part.copy_(torch.randint(-1, 2, part.shape, generator=gen, device="cuda:0", dtype=torch.int8))
+    w = pack(np.array([[1, 2, -3]]), "bf16")
+    y, _ = sol.sol_linear_fused(x, w, 1)
+    assert all(torch.equal(b[:, 0], a[:, 0] + 2 * a[:, 1] - 3 * a[:, 2]) for a, b in zip(x.split(1 << 26), y.split(1 << 26)))
+    g = torch.randint(-1, 2, (rows, 1), generator=gen, device="cuda:0", dtype=torch.int8).bfloat16()      # independent of x: sums of some ten thousand, exact in any order
+    _, dw, _ = sol.sol_linear_backward(g, x, w, need_dx=False, need_db=False, dw_dtype=torch.float32)
+    assert torch.equal(dw[0].double(), sum((b.double() * a.double()).sum(0) for a, b in zip(x.split(1 << 26), g.split(1 << 26))))
+    del x, y, g, dw
+    torch.cuda.empty_cache()
+
+
 def test_large_tiles_at_the_end_of_32_bit_offsets(sol):
     """dW over rows whose last lies 4.28 GB behind the first: whole numbers, so equal to the last bit to that of dense rows."""
     rows, n, pitch = 21400, 4096, 100000

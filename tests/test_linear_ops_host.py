@@ -208,3 +208,17 @@ def test_scratch_and_results_come_from_the_stream_that_the_call_runs_on(sol, mon
     log.clear()
     sol._scratch(None, 4, x, None), sol._result(x, (4,), torch.float32, None)
     assert log == ["alloc", "alloc"]
+
+
+@pytest.mark.parametrize("dtype,i,per_row", [(1, 1, 8), (1, 2, 8), (1, 3, 8), (0, 1, 4)])
+def test_rows_whose_copy_passes_32_bits(sol, dtype, i, per_row):
+    """x of few features has fewer than 2^31 elements where its copy to aligned rows has more groups of eight than 32 bits count, with a step of the grid beyond the last."""
+    L = sol.lib()
+    most = ((1 << 32) - (1 << 21)) // per_row
+    for m, want in ((1 << 24, 5), (most, 5), (most + 1, 6), (1 << 29, 5 if per_row == 4 else 6), ((1 << 31) // i - 1, 6)):       # 5: the workspace is too small, 6: refused
+        ld = desc(sol, m=m, i=i, o=1, dtype=dtype)
+        assert forward(sol, ld, ws=0xB000, nbytes=1) == want and backward(sol, ld, nbytes=1) == want, m
+        bytes_ = (L.sol_linear_fused_workspace_bytes(ld), L.sol_linear_backward_workspace_bytes(ld))
+        assert bytes_[0] == (m * per_row * 8 * (2 if dtype else 4) if want == 5 else 0) and (bytes_[1] > bytes_[0] or want == 6), m
+    ld = desc(sol, m=(1 << 28) - 1, i=8, o=1, dtype=dtype)                  # rows that are not copied
+    assert L.sol_linear_fused_workspace_bytes(ld) == 0 and backward(sol, ld, nbytes=1) == 5
