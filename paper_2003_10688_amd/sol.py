@@ -374,6 +374,8 @@ def _on_current(x, drop, stream):
         raise ValueError(f"tensors on {x.device}, but the current device is cuda:{device}: call under torch.cuda.device({x.get_device()})")
     if drop is not None and drop.step_tensor is not None and drop.step_tensor.get_device() != device:
         raise ValueError(f"dropout's step is on {drop.step_tensor.device}, the operands on {x.device}")
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"a stream of cuda:{stream.device_index} cannot run a call on {x.device}")
     current = torch._C._cuda_getCurrentRawStream(device)
     return (current, None) if stream is None or stream.cuda_stream == current else (stream.cuda_stream, stream)
 

@@ -222,3 +222,17 @@ def test_rows_whose_copy_passes_32_bits(sol, dtype, i, per_row):
         assert bytes_[0] == (m * per_row * 8 * (2 if dtype else 4) if want == 5 else 0) and (bytes_[1] > bytes_[0] or want == 6), m
     ld = desc(sol, m=(1 << 28) - 1, i=8, o=1, dtype=dtype)                  # rows that are not copied
     assert L.sol_linear_fused_workspace_bytes(ld) == 0 and backward(sol, ld, nbytes=1) == 5
+
+
+def test_a_stream_of_another_device_is_refused(sol, monkeypatch):
+    """Kernels on the current device's tensors cannot be launched on it."""
+    import torch
+    from types import SimpleNamespace
+
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda device: 500 + device, raising=False)
+    x = SimpleNamespace(get_device=lambda: 1, device="cuda:1")
+    mine, current, other = (SimpleNamespace(device_index=d, cuda_stream=h) for d, h in ((1, 77), (1, 501), (0, 78)))
+    assert sol._on_current(x, None, None) == (501, None) and sol._on_current(x, None, current) == (501, None) and sol._on_current(x, None, mine) == (77, mine)
+    with pytest.raises(ValueError, match="stream of cuda:0"):
+        sol._on_current(x, None, other)
