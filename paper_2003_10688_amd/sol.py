@@ -318,7 +318,10 @@ def _rows(t, cols, what, like=None):
             raise ValueError(f"{what}: a float32 or bfloat16 GPU tensor is wanted, not {t.dtype} on {t.device}")
     elif shape[0] != like.shape[0] or t.dtype != like.dtype or t.get_device() != like.get_device():
         raise ValueError(f"{what}: {shape[0]} rows of {t.dtype} on {t.device} do not go with {like.shape[0]} of {like.dtype} on {like.device}")
-    return t.data_ptr(), stride[0] if shape[0] > 1 else cols
+    pitch = stride[0] if shape[0] > 1 else cols
+    if shape[0] >= 1 << 31 or pitch >= 1 << 31:
+        raise SolError(6, f"{what}: {shape[0]} rows at a pitch of {pitch}: 2^31 or more")      # a C int would get their low 32 bits
+    return t.data_ptr(), pitch
 
 
 def _dense(t, shape, what, like, dtype=None):
@@ -431,6 +434,8 @@ def sol_dropout(x, drop, residual=None, out=None, stream=None):
     cols = x.shape[-1]
     if x.dtype not in (torch.float32, torch.bfloat16) or not x.is_cuda or not x.is_contiguous():
         raise ValueError(f"x: a contiguous float32 or bfloat16 GPU tensor is wanted, not {x.dtype} on {x.device}")
+    if x.numel() >= 1 << 31:
+        raise SolError(6, f"x: {x.numel()} elements: 2^31 or more")                            # a C int would get the low 32 bits of its rows
     handle, side = _on_current(x, drop, stream)
     y = _result(x, x.shape, x.dtype, side) if out is None else out
     _check(lib().sol_dropout(x.numel() // cols if cols else 0, cols, dtype_of(x), x.data_ptr(), drop, _dense(residual, x.shape, "residual", x),

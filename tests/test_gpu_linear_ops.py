@@ -508,6 +508,19 @@ def test_two_streams_at_once_and_graphs_that_share_a_workspace(sol):
         assert all(torch.equal(a, b) for k in range(2) for a, b in zip(outs[k], want[k])), i
 
 
+def test_sizes_that_a_c_int_does_not_hold_are_refused(sol):
+    """2^32 + 8 rows, whose low 32 bits are 8."""
+    x = torch.empty((2**32 + 8, 1), dtype=torch.bfloat16, device="cuda:0")
+    w = pack(np.ones((1, 1)), "bf16")
+    for f in (lambda: sol.sol_dropout(x, sol.Dropout(0.5, 1), out=x), lambda: sol.sol_dropout(x.view(8, -1), sol.Dropout(0.5, 1), out=x.view(8, -1)),
+              lambda: sol.sol_linear_fused(x, w, 1, out=x), lambda: sol.sol_linear_backward(x, x, w)):
+        with pytest.raises(sol.SolError) as e:
+            f()
+        assert e.value.status == 6
+    del x
+    torch.cuda.empty_cache()
+
+
 def test_refusals_of_the_binding(sol):
     x, w = torch.zeros((4, 32), device="cuda:0"), pack(np.ones((8, 32)), "f32")
     bad = [lambda: sol.sol_linear_fused(x.t(), w, 8), lambda: sol.sol_linear_fused(x.double(), w, 8), lambda: sol.sol_linear_fused(x, w[:7], 8),

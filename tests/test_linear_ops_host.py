@@ -236,3 +236,16 @@ def test_a_stream_of_another_device_is_refused(sol, monkeypatch):
     assert sol._on_current(x, None, None) == (501, None) and sol._on_current(x, None, current) == (501, None) and sol._on_current(x, None, mine) == (77, mine)
     with pytest.raises(ValueError, match="stream of cuda:0"):
         sol._on_current(x, None, other)
+
+
+def test_sizes_that_a_c_int_does_not_hold_are_refused(sol):
+    """2^32 + 8 rows are not 8 rows."""
+    import torch
+
+    for shape, stride in (((2**32 + 8, 1), (1, 1)), ((2**31, 1), (1, 1)), ((8, 16), (2**32 + 64, 1)), ((1, 2**32 + 64), (1, 1))):
+        t = torch.empty_strided(shape, stride, device="meta")
+        with pytest.raises(sol.SolError) as e:
+            sol._rows(t, shape[1], "x", t)
+        assert e.value.status == 6
+    t = torch.empty_strided((1, 16), (2**32 + 64, 1), device="meta")      # the pitch of a single row does not matter
+    assert sol._rows(t, 16, "x", t)[1] == 16
