@@ -334,6 +334,10 @@ const char *sol_debug_conv_kernel(void);
 sol_status sol_debug_choose_conv_tile(const sol_tensor_desc *x, const sol_conv_desc *conv, int residual, const sol_pool_desc *pool, int gradient,
                                       int *tile);
 
+/* Rows and columns of the tiles (64, 128 or 256) that the last forward product (0), dx (1) or dW (2) of a sol_linear_fused or sol_linear_backward
+ * call of the CALLING THREAD ran on; 0: none ran, or the weights were streamed past the rows of the last forward product (test aid). */
+int sol_debug_linear_tile(int product);
+
 /* Measured ceilings for the roofline report (benchmark aid; no layer arithmetic).
  *   sol_debug_probe_copy   a plain device-to-device copy of `bytes` (multiple of 16; 16-byte aligned, non-overlapping
  *                          device buffers) by a simple kernel: what HBM delivers, 2 * bytes of traffic per call;

@@ -358,6 +358,7 @@ double linear_rows_time(const GemmArgs &g, int dt) {
     return rounds * (c[0] + c[1] * stages);
 }
 sol_status launch_linear_rows(const GemmArgs &g, int dt, hipStream_t st) {
+    linear_tile_of_thread(GEMM_FORWARD) = 0;
     ConvArgs a{};
     a.x = g.a; a.w = g.b;
     a.P = g.M; a.C = g.K; a.ldx = (int)g.lda; a.Cout = g.N; a.Kp = (int)g.ldb;

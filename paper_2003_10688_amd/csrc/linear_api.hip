@@ -225,6 +225,8 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
     return launch_sums(sums, st);
 }
 
+int sol_debug_linear_tile(int product) { return product >= GEMM_FORWARD && product <= GEMM_DW ? linear_tile_of_thread((GemmKind)product) : 0; }
+
 sol_status sol_dropout(int rows, int cols, sol_dtype dt, const void *x, const sol_dropout_desc *drop, const void *residual, void *y, void *stream) {
     SOL_REQUIRE(dt == SOL_F32 || dt == SOL_BF16, SOL_ERR_DTYPE, "dropout: unknown dtype %d", (int)dt);
     SOL_REQUIRE(rows >= 0 && cols > 0, SOL_ERR_SHAPE, "bad dropout shape [%d,%d]", rows, cols);

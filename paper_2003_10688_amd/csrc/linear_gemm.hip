@@ -664,12 +664,16 @@ template <typename T, GemmKind KIND, int WP, int WC, int RP, int RC, int NS, int
     hipLaunchKernelGGL((linear_tile_kernel<T, KIND, WP, WC, RP, RC, NS, PERCU>), dim3((unsigned)blocks), dim3(WP * WC * 64), 0, st, a);
 }
 
+static thread_local int t_tile[3];             // see sol_debug_linear_tile
+int &linear_tile_of_thread(GemmKind kind) { return t_tile[kind]; }
+
 template <typename T, GemmKind KIND> static sol_status launch_kind(GemmArgs a, int dt, hipStream_t st) {
     int tile = a.plan.tile;
     if (tile == 256) {                       // its offsets along a reduction over rows have 32 bits, requests of whole tiles behind the last row included
         const double rows = a.K + 512.0, abytes = (KIND == GEMM_DW ? rows : 256.0) * a.lda * sizeof(T), bbytes = (KIND != GEMM_FORWARD ? rows : 256.0) * a.ldb * sizeof(T);
         if (abytes >= 4294967296.0 || bbytes >= 4294967296.0) tile = 128;
     }
+    t_tile[KIND] = tile;
     const long blocks = tiles_of(a, dt, tile);
     if constexpr (sizeof(T) == 2 && KIND == GEMM_FORWARD) {
         // One workgroup a CU or fewer: a longer ring in the place of neighbours (3123 x 128, 7488: 31.0 -> 25.8 us; 469 x 384, 6080: 25.6 -> 21.2).  With 270 .. 350 tiles it loses
@@ -710,6 +714,7 @@ sol_status launch_linear_gemm(const GemmArgs &a, int dt, GemmKind kind, hipStrea
 }
 
 sol_status launch_linear_pair(GemmArgs dx, GemmArgs dw, const SumJob &sum, int dt, hipStream_t st) {
+    t_tile[GEMM_DX] = t_tile[GEMM_DW] = 64;
     const long first = tiles_of(dx, dt, 64), second = first + tiles_of(dw, dt, 64);
     const dim3 grid((unsigned)(second + (sum.n > 0 ? sum_blocks(sum) : 0)));
     if (dt == SOL_BF16) hipLaunchKernelGGL(linear_pair_kernel<bf16_t>, grid, dim3(256), 0, st, dx, dw, (int)first, (int)second, sum);

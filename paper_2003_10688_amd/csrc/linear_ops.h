@@ -278,6 +278,7 @@ GemmPlan plan_gemm(int M, int N, int K, int dt, bool may_split);
 // whether dx and dW are faster in one launch than as planned one by one; *px, *pw: their plans then
 bool plan_pair(int m, int in_f, int out_f, int dt, const GemmPlan &dx, const GemmPlan &dw, GemmPlan *px, GemmPlan *pw);
 sol_status launch_linear_gemm(const GemmArgs &a, int dt, GemmKind kind, hipStream_t st);
+int &linear_tile_of_thread(GemmKind kind);                     // sol_debug_linear_tile
 double linear_rows_time(const GemmArgs &a, int dt);            // forward, weights streamed past few rows (linear.hip): estimate of its time, negative where it cannot run
 sol_status launch_linear_rows(const GemmArgs &a, int dt, hipStream_t st);
 // A copy of [rows][cols] (pitch ld, any alignment) to dense rows of ldo elements, the rest of each row zeros

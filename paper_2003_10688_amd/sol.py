@@ -429,6 +429,11 @@ def sol_linear_backward(dy, x, w_packed, preact=None, act=ACT_NONE, drop=None, n
     return dx, dw, db
 
 
+def sol_debug_linear_tile(product):
+    """Rows and columns of the tiles that the last forward product (0), dx (1) or dW (2) of this thread ran on; 0: streamed weights, or none ran."""
+    return lib().sol_debug_linear_tile(product)
+
+
 def sol_dropout(x, drop, residual=None, out=None, stream=None):
     """y = dropout(x) + residual; x: contiguous, its last dimension the columns, all before it the rows; out may be x or residual.  Returns y."""
     cols = x.shape[-1]

@@ -114,6 +114,82 @@ def test_every_element_of_a_row_counts(sol, dt, rows):
         assert np.array_equal(host(y), grid(np.full((rows, 40), float(n_in)), dt)), n_in
 
 
+# ---- the tile kernels, one product at a time, on reductions longer than their rings: whole numbers against torch's fp32 product of the same whole numbers
+KINDS = ("forward", "dx", "dw")
+
+
+def ints_on_gpu(gen, rows, cols, dt, gap=0):
+    """Whole numbers -2 .. 2 in rows that `gap` columns of NaN lie between."""
+    t = torch.full((rows, cols + gap), float("nan"), dtype=TDT[dt], device="cuda:0")[:, :cols]
+    return t.copy_(torch.randint(-2, 3, (rows, cols), generator=gen, device="cuda:0", dtype=torch.int8))
+
+
+def packed_on_gpu(w):
+    block = 64 if w.dtype == torch.bfloat16 else 32
+    p = torch.zeros((w.shape[0], -(-w.shape[1] // block) * block), dtype=w.dtype, device="cuda:0")
+    p[:, :w.shape[1]] = w
+    return p
+
+
+def check_product(sol, kind, dt, n, c, k, tiles, plain):
+    """A product of n rows and c columns over k has to run on a tile in `tiles` (0: streamed weights) and be right to the last bit.  plain: no activation and no dropout, so that the backward products read dy itself
+    where its rows are aligned."""
+    gen = torch.Generator(device="cuda:0").manual_seed(n * 31 + c * 7 + k)
+    ints = lambda rows, cols, gap=0: ints_on_gpu(gen, rows, cols, dt, gap)  # noqa: E731
+    act, d = (sol.ACT_NONE, None) if plain else (sol.ACT_RELU, sol.Dropout(0.5, 7, 3))
+    if kind == "forward":
+        x, w, b, r = ints(n, k, 8), ints(c, k), torch.randint(-2, 3, (c,), generator=gen, device="cuda:0").float(), ints(n, c, 5)
+        y, z = sol.sol_linear_fused(x, packed_on_gpu(w), c, bias=b, act=act, drop=d, residual=r, want_preact=True)
+        assert sol.sol_debug_linear_tile(0) in tiles
+        wz = x.float() @ w.float().t() + b
+        v = wz if plain else sol.sol_dropout(wz.clamp(min=0), d)
+        assert torch.equal(z, wz.to(TDT[dt])) and torch.equal(y, (v + r.float()).to(TDT[dt]))
+        return
+    m, n_in, n_out = (n, c, k) if kind == "dx" else (k, c, n)
+    x, w, g = ints(m, n_in, 8), ints(n_out, n_in), ints(m, n_out, 8)
+    z = None if plain else ints(m, n_out)
+    dx, dw, _ = sol.sol_linear_backward(g, x, packed_on_gpu(w), preact=z, act=act, drop=d, need_dx=kind == "dx", need_dw=kind == "dw", need_db=False)
+    assert sol.sol_debug_linear_tile(KINDS.index(kind)) in tiles
+    dz = g.float() if plain else sol.sol_dropout(g.float().contiguous(), d) * (z > 0)
+    if kind == "dx":
+        assert torch.equal(dx, (dz @ w.float()).to(TDT[dt]))
+    else:
+        assert torch.equal(dw, (dz.t() @ x.float()).to(TDT[dt]))
+
+
+# stages of 64 products and the length of the last: the ring of the 256-tile kernel has ten units, four a stage, and repeats after five stages
+HUGE = [(1, 40), (2, 56), (3, 8), (4, 64), (4, 8), (5, 24), (5, 64), (6, 40), (7, 13), (8, 61), (9, 56), (10, 8), (11, 64), (11, 48), (12, 1), (13, 31), (16, 16), (21, 40)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("stages,last", HUGE)
+def test_largest_tiles_over_every_turn_of_their_ring(sol, kind, stages, last):
+    """Rows and columns end inside a tile, the reduction inside a 16-byte piece (odd: rows are copied), inside a stage or on its end."""
+    k = (stages - 1) * 64 + last
+    check_product(sol, kind, "bf16", 3904, 4000, k, (256,), True)
+    check_product(sol, kind, "bf16", 3900, 4001, k, (256,), False)
+
+
+RINGS = [       # type, rows, columns, the tile
+    ("bf16", 950, 1000, 64),        # up to 256 tiles: a ring of five stages forward, three backward
+    ("bf16", 500, 900, 64),         # the same, with streamed weights for the longest reductions forward
+    ("bf16", 1100, 1304, 64),       # more
+    ("bf16", 2000, 1992, 128),      # up to 256: a ring of four
+    ("bf16", 2900, 2801, 128),      # more: rings of two
+    ("f32", 500, 900, 64),
+    ("f32", 2000, 1990, 128),
+]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dt,n,c,tile", RINGS)
+def test_smaller_tiles_over_every_turn_of_their_rings(sol, kind, dt, n, c, tile):
+    stage = 64 if dt == "bf16" else 32
+    for stages, last in ((8, 8), (9, 16), (10, stage), (11, 12), (12, 31), (13, 5), (17, 24), (30, 8)):
+        k = (stages - 1) * stage + last
+        check_product(sol, kind, dt, n, c, k, (tile, 0) if n == 500 and kind == "forward" else (tile,), stages % 2 == 0)
+
+
 def close(got, want, tol, what):
     bad = np.abs(got - want) - tol
     assert np.all(np.isfinite(got)) and bad.max() <= 0, f"{what}: off by {np.abs(got - want).flat[bad.argmax()]:.3g}, {tol.flat[bad.argmax()]:.3g} allowed, at {np.unravel_index(bad.argmax(), bad.shape)}"
