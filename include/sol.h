@@ -252,7 +252,9 @@ sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void
  *   dx         NULL, or dense [m][in_f];  db: NULL, or device fp32 [out_f]
  *   dw         NULL, or dense [out_f][in_f] (not packed) of dw_dtype: the layer's dtype or SOL_F32
  * For bf16, dz is rounded to bf16 before it is multiplied (both products run on the bf16 matrix instructions); db sums it unrounded.
- * With m = 0, dw and db become zeros.  Every sum runs in an order that depends on the sizes alone. */
+ * With m = 0, dw and db become zeros.
+ * The order of every sum here and in sol_linear_fused is fixed by the description (sizes, dtype, pitches), that of dx and dw also by whether both are
+ * asked for, and by nothing else: a call repeated gives the same bits, but dw asked for alone may differ in its roundings from dw beside dx. */
 sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const void *x, const void *w_packed, const void *preact,
                                const sol_dropout_desc *drop, void *dx, void *dw, int dw_dtype, float *db, void *workspace,
                                size_t workspace_bytes, void *hip_stream);

@@ -316,6 +316,40 @@ def test_equal_rows_equal_bits_and_repeats(sol, dt):
         first = got
 
 
+@pytest.mark.parametrize("dt,rows,n_in,n_out", [("bf16", 1, 2048, 1000), ("bf16", 16, 4096, 520), ("bf16", 77, 2056, 300), ("f32", 130, 1100, 90), ("f32", 20, 2000, 1000),
+                                                ("bf16", 500, 700, 900), ("bf16", 2000, 1000, 1992), ("bf16", 2900, 700, 2801), ("bf16", 3900, 500, 4001), ("f32", 500, 333, 900),
+                                                ("f32", 2000, 500, 1990)])
+def test_equal_rows_give_equal_bits(sol, dt, rows, n_in, n_out):
+    """Copies of one row: every row of y, z and dx has the bits of the first, wherever in a tile it lies."""
+    rng = np.random.default_rng([rows, n_in])
+    same = lambda n: dev(rng.standard_normal((1, n)), dt).expand(rows, n).contiguous()  # noqa: E731
+    x, w, g = same(n_in), pack(rng.standard_normal((n_out, n_in)) / np.sqrt(n_in), dt), same(n_out)
+    y, z = sol.sol_linear_fused(x, w, n_out, act=sol.ACT_SILU, residual=g, want_preact=True)
+    dx, _, _ = sol.sol_linear_backward(g, x, w, preact=z, act=sol.ACT_SILU, need_dw=False)
+    for t in (y, z, dx):
+        assert torch.equal(t, t[:1].expand_as(t).contiguous())
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n_in,n_out", [(300, 128, 2048), (512, 256, 512), (40, 2048, 1000), (2600, 72, 5130)])
+def test_what_bits_do_not_depend_on(sol, dt, rows, n_in, n_out):
+    """Neither the outputs without a product (z, db) nor where anything lies in memory changes the order of a sum; asking for dx or dW alone may."""
+    rng = np.random.default_rng([rows, n_out])
+    x, w, g = dev(rng.standard_normal((rows, n_in)), dt), pack(rng.standard_normal((n_out, n_in)) / np.sqrt(n_in), dt), dev(rng.standard_normal((rows, n_out)), dt)
+    y, z = sol.sol_linear_fused(x, w, n_out, act=sol.ACT_SILU, want_preact=True)
+    bw = lambda x_=x, w_=w, g_=g, **kw: sol.sol_linear_backward(g_, x_, w_, preact=z, act=sol.ACT_SILU, **kw)  # noqa: E731
+    want, one = bw(), (bw(need_dw=False)[0], bw(need_dx=False)[1])
+    keep, room = [], torch.empty(1 << 27, dtype=torch.uint8, device="cuda:0")
+    for i in range(3):
+        x2, w2, g2 = x.clone(), w.clone(), g.clone()
+        keep.append((x2, w2, g2))
+        assert torch.equal(sol.sol_linear_fused(x2, w2, n_out, act=sol.ACT_SILU)[0], y)
+        assert all(torch.equal(a, b) for a, b in zip(bw(x2, w2, g2, workspace=room[i * 4096:]), want))
+        got = bw(x2, w2, g2, need_db=False)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        assert torch.equal(bw(need_dw=False, need_db=False)[0], one[0]) and torch.equal(bw(need_dx=False, need_db=False)[1], one[1]) and torch.equal(bw(need_dx=False, need_dw=False)[2], want[2])
+
+
 def block_forward(sol, x, w1, b1, w2, b2, hidden, d1, d2):
     """A feed-forward block with a residual: x + dropout(W2 dropout(gelu(W1 x + b1)) + b2)."""
     h, z = sol.sol_linear_fused(x, w1, hidden, bias=b1, act=sol.ACT_GELU, drop=d1, want_preact=True)
