@@ -30,6 +30,10 @@ template <> struct Mma<float> {
     }
 };
 
+// The range check of a raw buffer (loads to registers and to LDS alike) compares the sum of the lane's and the scalar offset, which does not wrap at 2^32, with the resource's size; what is
+// out of range is not read and arrives as zeros.  Measured with every address in bounds of one allocation: a scalar offset alone at the size, behind it and up to 2^32 - 4096;
+// a lane's offset of all ones with and without a scalar one; size 0 with either; sizes and offsets beyond 2^31.
+
 // Hand-ordered LDS pipeline pieces shared by the DMA-ring kernels.  The compiler cannot tell which ring stage an
 // LDS read touches and would make every fragment read wait for all outstanding DMA; the reads are therefore opaque
 // volatile statements ordered by hand (ds_read -> s_waitcnt lgkmcnt -> landed() -> use).

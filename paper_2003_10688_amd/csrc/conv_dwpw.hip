@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(WP *WC * 64, 2) conv_dwpw_kernel(const DwPwArg
         const unsigned soff = isoff;
 #pragma unroll
         for (int i = 0; i < WL; i++) {
-            const unsigned off = wo[i] + soff;                         // the whole offset in the lane's part: the range check is on it
+            const unsigned off = wo[i] + soff;                         // (the range check is on the sum of the lane's and the scalar offset)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (__attribute__((address_space(3))) void *)(ring + slot * STAGE + (wave * WL + i) * 1024), 16,
                                                      is < nst ? off : 0xffffffffu, 0, 0, 0);
         }

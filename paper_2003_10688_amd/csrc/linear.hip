@@ -98,7 +98,7 @@ sol_status launch_linear(const ConvArgs &a, int dt, hipStream_t st) {
 }
 
 // ---- weight streaming ---------------------------------------------------------------------------------------------
-//   y[m][o] as above, for up to 128 rows.  PB x CB blocks of 16 rows x 16 features per workgroup; eight waves split the
+//   y[m][o] as above, for up to 128 rows (FUSED: for as many as the times at linear_rows_time say).  PB x CB blocks of 16 rows x 16 features per workgroup; eight waves split the
 // reduction.  The job is to stream the weights at the rate of HBM, so their loads must be whole lines and many of them must be
 // in flight: a wave loads 128 bytes of 8 weight rows per instruction into REGISTERS, NS stages ahead (with the rows of x in
 // the LDS ring as well, LDS would hold one stage of both), turns them into MFMA fragments through a strip of LDS of its own, and

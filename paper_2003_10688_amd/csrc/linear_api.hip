@@ -59,7 +59,7 @@ sol_status check_linear(const sol_linear_desc *ld, sol_linear_desc *l) {
 bool cut_needed(int k, int dt) { return (k * dtype_size(dt)) % 128 != 0; }
 
 struct ForwardPlan {
-    size_t xpad, bytes;
+    size_t bytes;
     bool pad;
 };
 ForwardPlan forward_plan(const sol_linear_desc &l) {

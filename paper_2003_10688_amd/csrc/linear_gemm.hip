@@ -197,7 +197,7 @@ __device__ __forceinline__ void write_results(const GemmArgs &a, int split, cons
 // ---- tiles of 64 x 64 to 128 x 128: a ring of NS whole stages --------------------------------------------------------------------
 // Products whose tiles of 256 x 256 would leave CUs idle.  A stage's first half is multiplied while the second is read from LDS, and the other way round; a slot is requested again as soon as
 // every wave has read it.  One workgroup on a CU is bound by the way of the data (0.2 us a stage of 64 x 64 tiles, 0.39 of 128 x 128 where the products need 0.06 and 0.23), several by
-// the matrix units: 2048 x 2048, 8192 bf16 66 us (1.05 PFLOP/s); 1021 x 2304, 1536 16 us; fp32, where the products are sixteen times as long, reaches 122 of 150 TFLOP/s.
+// the matrix units: 2048 x 2048, 8192 bf16 66 us (1.05 PFLOP/s); 1021 x 2304, 1536 16 us; fp32, where the products are sixteen times as long, reaches 122 to 145 of 150 TFLOP/s (4096 x 4096, 4096 950 us).
 // An operand's corner moves along the reduction as a scalar; what lies behind the tensor, or behind the part's last stage, is out of range of the resource and
 // arrives as zeros.  Along k: rows from `limit` on.  Across k: rows of k from `left` on, and what lies behind row_bytes of the last one.
 template <bool ACROSS, int BK> struct Cursor;
@@ -386,7 +386,7 @@ template <typename T> __global__ void __launch_bounds__(256, 3) linear_pair_kern
 // units; A0, A1 of stage s + 2 and B0 of s + 3 take the places of B0, B1 and A0 of stage s, and B1 of s + 3 that of A1, so every unit is requested one and a half stages (96 matrix
 // instructions of a wave) before it is needed.
 // The two waves of a SIMD issue one instruction each at a time, and everything that is not a product has to fit beside the products: resources and lane offsets are
-// constants of the loop (a scalar offset moves along the reduction, and the range check includes it), and the loop is unrolled over the five stages after which the ring repeats.
+// constants of the loop (a scalar offset moves along the reduction; the range check includes it, also where a unit behind the last stage is requested), and the loop is unrolled over the five stages after which the ring repeats.
 // What bounds it: the card's power limit, and the starts and ends of tiles, which nothing overlaps.  8192 x 8192 x 8192 takes 775 us (1.42 PFLOP/s, a stage 2500 cycles of which
 // the products need 2048); 8192 x 16384, 4096 860 us (1.28), 55 more with GELU, dropout and z
 // stored (the epilogue is bound by its arithmetic, some 300 instructions for 8 elements; with the halves of a line stored apart, 32 rows x 32 columns at a time, half as much again
@@ -598,12 +598,14 @@ __global__ void __launch_bounds__(512, 2) linear_huge_kernel(const GemmArgs a) {
 
 // ---- which kernel ----------------------------------------------------------------------------------------------------------------
 // Times of the kernels in us as fitted to 270 products of 16 .. 8192 rows, columns and steps on 256 CUs, `s` the 128-byte stages of the reduction.  They put the fastest kernel
-// first, or one within 3 %, in 19 of 20.
+// first, or one within 3 %, in 19 of 20.  They are there to be compared with one another: the epilogue is not in them, and long bf16 products, which run at the power limit, take 20 to 35 %
+// longer (us, these times and measured: 256-tiles 4096 x 4096, 4096 74, 100; 8192 x 8192, 8192 560, 754; 8192 x 16384, 4096 589, 798; 128-tiles 2048 x 2048, 8192 53, 66; fp32 within 4 %:
+// 4096 x 4096, 4096 974, 950).
 //   bf16   64 x 64 tiles (three workgroups a CU): 0.36 + 0.22 s for up to 256 of them, 0.69 + 0.166 s for every 256 beyond
 //          128 x 128 tiles: 3.3 + 0.39 s for up to 256 (one workgroup a CU, a ring of four stages), 3.3 + 0.76 s for every 512 beyond (two a CU, rings of two)
 //          256 x 256 tiles: 7.0 + 1.04 s for every 256
 //   fp32   64 x 64 tiles: 0.87 + 0.55 s for every 256; 128 x 128 tiles: 2.85 + 1.88 s for every 256; 256 x 256 tiles were never better by more than 3 %
-// For instance 2048 x 2048 with a reduction of 8192 in bf16: 256 tiles of 128 x 128 take 65 us (67 by the formula), 1024 of 64 x 64 83.
+// For instance 2048 x 2048 with a reduction of 8192 in bf16: 256 tiles of 128 x 128 take 66 us, 1024 of 64 x 64 83 (88 by the formula).
 // A reduction in p parts makes p times as many tiles of 1 / p of the stages, and costs one more launch and the parts' way to memory and back; up to
 // 1024 tiles, 64 MB of parts.
 static double tile_time(long tiles, double s, int tile, int dt) {
