@@ -501,6 +501,33 @@ def test_captured_and_replayed(sol, dt):
         last = (i, want[0])
 
 
+def test_captured_on_a_second_stream(sol):
+    """Two branches of one graph, the second on a stream given to the calls, both with scratch of their own; replayed with other work between."""
+    rng = np.random.default_rng(31)
+    data = [(dev(rng.standard_normal((260, 333)), "bf16"), pack(rng.standard_normal((520, 333)) / 18, "bf16"), dev(rng.standard_normal((260, 520)), "bf16")) for _ in range(2)]
+    step = torch.zeros(1, dtype=torch.int32, device="cuda:0")
+    d = sol.Dropout(0.1, 8, 0, step)
+
+    def run(k, **kw):
+        x, w, g = data[k]
+        y, z = sol.sol_linear_fused(x, w, 520, act=sol.ACT_GELU, drop=d, want_preact=True, **kw)
+        return (y, z) + sol.sol_linear_backward(g, x, w, preact=z, act=sol.ACT_GELU, drop=d, **kw) + (sol.sol_dropout(g, d, **kw),)
+
+    run(0), run(1)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        out = [run(0), run(1, stream=side)]
+        torch.cuda.current_stream().wait_stream(side)
+    for i in (0, 2, 2, 7):
+        step.fill_(i)
+        want = [[t.clone() for t in run(k)] for k in range(2)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for k in range(2) for a, b in zip(out[k], want[k])), i
+
+
 def test_no_rows(sol):
     x = torch.empty((0, 24), device="cuda:0")
     w = pack(np.ones((16, 24)), "f32")
