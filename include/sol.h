@@ -21,7 +21,8 @@
  *    documentation and pooling argmax use logical (n,c,h,w) indices;
  *  - arguments are validated before anything is launched; on error nothing was
  *    enqueued, a status code is returned and sol_last_error() holds the text;
- *  - device buffers must be 16-byte aligned; tensors hold fewer than 2^31 elements.
+ *  - device buffers must be 16-byte aligned; tensors hold fewer than 2^31 elements, where a call does not
+ *    say otherwise.
  */
 #ifndef SOL_MI355_H
 #define SOL_MI355_H
@@ -258,6 +259,89 @@ sol_status sol_linear_fused(const sol_linear_desc *ld, const void *x, const void
 sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const void *x, const void *w_packed, const void *preact,
                                const sol_dropout_desc *drop, void *dx, void *dw, int dw_dtype, float *db, void *workspace,
                                size_t workspace_bytes, void *hip_stream);
+
+/* Layer norm over the rows of x [rows][cols], and its backward pass:
+ *   forward   mean, rstd = 1 / sqrt(variance + eps) of each row (the variance about the mean, divided by cols)
+ *             y = (x - mean) * rstd * gamma + beta
+ *   backward  h = (x - mean) * rstd,  g = dy * gamma
+ *             dx = rstd * (g - mean(g) - h * mean(g * h)) + residual      dgamma = sum over the rows of dy * h     dbeta = sum over the rows of dy
+ * Every sum, mean and rstd are fp32 for both dtypes.  An infinity or a NaN in a row makes that row of y, and of dx, NaN, and no other.  A row whose squared deviations
+ * add up to more than fp32 holds has rstd 0. */
+typedef struct {
+    int rows, cols;             /* at most 2^20 columns */
+    int dtype;                  /* sol_dtype of x, y, dy, residual and dx */
+    int ldx, ldy;               /* elements between consecutive rows of x and of y (backward: of dy): 0 = dense, or cols or more, at most 2^21; elements between
+                                   the rows are neither read into a result nor written.  Rows may span 2^31 elements and more. */
+    float eps;                  /* at least 2^-126; not used by the backward pass */
+} sol_layer_norm_desc;
+
+/*   gamma, beta  device fp32 [cols] or NULL (1 / 0)
+ *   y            may be x itself (same pitch); otherwise outputs must not overlap inputs
+ *   mean, rstd   NULL, or device fp32 [rows] each, which the backward pass needs
+ * rows = 0 does nothing. */
+sol_status sol_layer_norm(const sol_layer_norm_desc *nd, const void *x, const float *gamma, const float *beta, void *y, float *mean, float *rstd,
+                          void *hip_stream);
+
+/* Device scratch that sol_layer_norm_backward needs (partial sums of dgamma and dbeta).  Calls that may run at the same time need scratch of their own. */
+size_t sol_layer_norm_backward_workspace_bytes(const sol_layer_norm_desc *nd);
+
+/*   dy           [rows][cols] with pitch ldy;  x, gamma: those of the forward call;  mean, rstd: as it stored them
+ *   residual     NULL, or dense [rows][cols]: the gradient that reaches x past the layer
+ *   dx           NULL, or dense [rows][cols]; may be residual itself
+ *   dgamma,dbeta NULL, or device fp32 [cols] each
+ * With rows = 0, dgamma and dbeta become zeros.  The order of every sum is fixed by the description and by which of dx and of (dgamma, dbeta) are asked for: a call repeated gives the
+ * same bits. */
+sol_status sol_layer_norm_backward(const sol_layer_norm_desc *nd, const void *dy, const void *x, const float *gamma, const float *mean,
+                                   const float *rstd, const void *residual, void *dx, float *dgamma, float *dbeta, void *workspace,
+                                   size_t workspace_bytes, void *hip_stream);
+
+/* Embedding, and the gradient of its table:
+ *   forward   y[i] = scale * table[tokens[i]]            (the product is fp32, then rounded to dtype)
+ *   backward  dtable[v] = scale * sum of the dy[i] with tokens[i] = v, in the order of i
+ * A token equal to pad gives a row of zeros and no gradient, whether the table has such a row or not.  Any other token outside 0 .. vocab - 1 gives a row of NaN and no gradient. */
+typedef struct {
+    int tokens, vocab, cols;    /* at most 2^30 tokens, 2^24 rows of the table, 2^20 columns */
+    int dtype;                  /* sol_dtype of table, y and dy */
+    int token_bits;             /* 32 or 64: tokens are int32_t or int64_t */
+    int ldt, ldy;               /* elements between consecutive rows of table (forward only) and of y (backward: of dy): 0 = dense, or cols or more, at most 2^21; elements
+                                   between the rows are neither read into a result nor written.  Rows may span 2^31 elements and more. */
+    float scale;
+    int pad;                    /* -1, which is no row of the table, where there is no padding token */
+} sol_embedding_desc;
+
+/* tokens: device [tokens];  table: [vocab][cols] with pitch ldt;  y: [tokens][cols] with pitch ldy, must not overlap the table.  tokens = 0 does nothing. */
+sol_status sol_embedding(const sol_embedding_desc *ed, const void *tokens, const void *table, void *y, void *hip_stream);
+
+/* Device scratch that sol_embedding_backward needs: the tokens' positions sorted by token, and sums of parts of the longest runs.  Calls that may run at the same time need
+ * scratch of their own. */
+size_t sol_embedding_backward_workspace_bytes(const sol_embedding_desc *ed);
+
+/*   dy         [tokens][cols] with pitch ldy
+ *   dtable     dense [vocab][cols] of dtable_dtype: the table's dtype or SOL_F32
+ *   accumulate 0: every row of dtable is written (zeros where no token is); else the sums are added to the rows whose tokens occur, rounded once, and no other row is touched
+ *              (a table that is also the weight of the last layer; gradients of several batches)
+ * Sums are fp32.  Their order is fixed by the description and the tokens: a call repeated gives the same bits. */
+sol_status sol_embedding_backward(const sol_embedding_desc *ed, const void *tokens, const void *dy, void *dtable, int dtable_dtype, int accumulate,
+                                  void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The norm of all gradients together, and clipping by it:
+ *   norm = sqrt of the sum of the squares of all elements of all tensors        out = grad * (max_norm / norm)   if norm is finite and above max_norm, else grad
+ * A norm that is not finite leaves the gradients as they are: the caller sees it in *norm. */
+typedef struct {
+    const void *grad;           /* device, aligned to its elements (a slice of a flat buffer will do) */
+    void *out;                  /* device, like grad; may be grad itself; not used by sol_grad_norm */
+    size_t count;               /* elements; with 0 the pointers are not looked at */
+    int dtype;                  /* sol_dtype of grad and out; tensors of both types may be mixed */
+} sol_grad;
+
+/* Device scratch of sol_grad_norm and sol_grad_clip for these tensors (their counts are what matters).  Calls that may run at the same time need scratch of their own. */
+size_t sol_grad_workspace_bytes(const sol_grad *grads, int tensors);
+
+/* grads: host array of `tensors` entries, read during the call.  norm: device fp32.  Squares are summed in 64 bits, in an order that the counts fix.
+ * No two entries of sol_grad_clip may share memory, but for an entry's out in place of its grad.  No tensors: norm 0. */
+sol_status sol_grad_norm(const sol_grad *grads, int tensors, float *norm, void *workspace, size_t workspace_bytes, void *hip_stream);
+sol_status sol_grad_clip(const sol_grad *grads, int tensors, float max_norm, float *norm, void *workspace, size_t workspace_bytes,
+                         void *hip_stream);
 
 /* Stand-alone pooling over NHWC x (max with optional int32 argmax as above, or average).
  * Padding acts as -inf for max and as 0 for average.  Requires pad < kernel. */
@@ -499,6 +583,11 @@ sol_status sol_network_layer_output(const sol_network *net, int layer, void *wor
  * SOL_ERR_UNSUPPORTED for inference networks. */
 sol_status sol_network_backward(sol_network *net, const void *x, const int32_t *labels, float *loss,
                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* sol_grad_clip on every gradient of the last sol_network_backward, in place, in front of sol_network_sgd_step.  norm: device float. */
+size_t sol_network_clip_workspace_bytes(const sol_network *net);
+sol_status sol_network_clip_gradients(sol_network *net, float max_norm, float *norm, void *workspace, size_t workspace_bytes,
+                                      void *hip_stream);
 
 /* v <- momentum * v + g ;  p <- p - lr * v  on every fp32 master parameter that received a gradient,
  * then re-packs the weights the kernels read. */

@@ -1,6 +1,7 @@
 // C ABI of the library: argument validation, the single fused-layer entry points, and the network
 // object (planner + executor).  Host code only; all device work is in conv_igemm.hip / fusion.hip.
 #include <stdarg.h>
+#include <stdlib.h>
 
 #include <algorithm>
 #include <mutex>
@@ -2043,6 +2044,51 @@ sol_status sol_network_sgd_step(sol_network *net, float lr, float momentum, void
             SOL_TRY(add(vec_ptr(net, lp, VEC_BIAS), vec_ptr(net, lp, VEC_V_BIAS), vec_ptr(net, lp, VEC_G_BIAS), nullptr, nullptr, 1, K, 1, 0, 0));
     }
     return flush();
+}
+
+// The gradients that sol_network_sgd_step takes, into `list` (NULL: they are counted only)
+static int gradient_list(const sol_network *net, sol_grad *list) {
+    int n = 0;
+    auto add = [&](float *g, size_t count) {
+        if (list) list[n] = sol_grad{g, g, count, SOL_F32};
+        n++;
+    };
+    for (const auto &lp : net->layers) {
+        if (!(lp.L.kind == SOL_LAYER_CONV || lp.L.kind == SOL_LAYER_LINEAR) || !lp.has_grad) continue;
+        add(reinterpret_cast<float *>(net->params + lp.grad_off), (size_t)lp.cd.cout * lp.cd.cin * lp.cd.kh * lp.cd.kw);
+        if (lp.L.kind == SOL_LAYER_CONV && lp.L.has_bn) {
+            add(vec_ptr(net, lp, VEC_G_GAMMA), lp.cd.cout);
+            add(vec_ptr(net, lp, VEC_G_BETA), lp.cd.cout);
+        } else {
+            add(vec_ptr(net, lp, VEC_G_BIAS), lp.cd.cout);
+        }
+    }
+    return n;
+}
+
+size_t sol_network_clip_workspace_bytes(const sol_network *net) {
+    if (!net || !net->training) return 0;
+    const int n = gradient_list(net, nullptr);
+    sol_grad *list = static_cast<sol_grad *>(malloc(((size_t)n + 1) * sizeof(sol_grad)));
+    if (!list) return 0;
+    gradient_list(net, list);
+    for (int i = 0; i < n; i++) list[i].grad = list[i].out = list;      // sizes are what counts; the buffer may not be bound yet
+    const size_t bytes = sol_grad_workspace_bytes(list, n);
+    free(list);
+    return bytes;
+}
+
+sol_status sol_network_clip_gradients(sol_network *net, float max_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream) {
+    SOL_REQUIRE(net, SOL_ERR_NULL, "net is NULL");
+    SOL_REQUIRE(net->training, SOL_ERR_UNSUPPORTED, "network was not created with SOL_NET_TRAINING");
+    SOL_REQUIRE(net->params, SOL_ERR_WORKSPACE, "no parameter buffer bound (sol_network_bind_params)");
+    const int n = gradient_list(net, nullptr);
+    sol_grad *list = static_cast<sol_grad *>(malloc(((size_t)n + 1) * sizeof(sol_grad)));
+    SOL_REQUIRE(list, SOL_ERR_UNSUPPORTED, "no memory for a list of %d gradients", n);
+    gradient_list(net, list);
+    const sol_status r = sol_grad_clip(list, n, max_norm, norm, workspace, workspace_bytes, stream);
+    free(list);
+    return r;
 }
 
 sol_status sol_network_tensor(const sol_network *net, int layer, int which, float **ptr, size_t *count) {

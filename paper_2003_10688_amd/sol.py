@@ -47,6 +47,18 @@ class LinearDesc(C.Structure):
     _fields_ = [(n, C.c_int) for n in ("m", "in_f", "out_f", "dtype", "act", "ldx", "ldy", "ldr")]
 
 
+class LayerNormDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("rows", "cols", "dtype", "ldx", "ldy")] + [("eps", C.c_float)]
+
+
+class EmbeddingDesc(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("tokens", "vocab", "cols", "dtype", "token_bits", "ldt", "ldy")] + [("scale", C.c_float), ("pad", C.c_int)]
+
+
+class Grad(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("count", C.c_size_t), ("dtype", C.c_int)]
+
+
 class Dropout(C.Structure):
     """p: probability of dropping an element; seed: 64 bits; call: which dropout of the model this is; step: None, or a device int32
     tensor of one element that the kernels read when they run (a captured graph draws a new mask when it has changed)."""
@@ -107,6 +119,17 @@ def lib():
         L.sol_linear_fused.argtypes = [C.POINTER(LinearDesc), vp, vp, vp, C.POINTER(Dropout), vp, vp, vp, vp, sz, vp]
         L.sol_linear_backward.argtypes = [C.POINTER(LinearDesc), vp, vp, vp, vp, C.POINTER(Dropout), vp, vp, i, vp, vp, sz, vp]
         L.sol_dropout.argtypes = [i, i, i, vp, C.POINTER(Dropout), vp, vp, vp]
+        L.sol_layer_norm.argtypes = [C.POINTER(LayerNormDesc), vp, vp, vp, vp, vp, vp, vp]
+        L.sol_layer_norm_backward.argtypes = [C.POINTER(LayerNormDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.sol_layer_norm_backward_workspace_bytes.restype, L.sol_layer_norm_backward_workspace_bytes.argtypes = sz, [C.POINTER(LayerNormDesc)]
+        L.sol_embedding.argtypes = [C.POINTER(EmbeddingDesc), vp, vp, vp, vp]
+        L.sol_embedding_backward.argtypes = [C.POINTER(EmbeddingDesc), vp, vp, vp, i, i, vp, sz, vp]
+        L.sol_embedding_backward_workspace_bytes.restype, L.sol_embedding_backward_workspace_bytes.argtypes = sz, [C.POINTER(EmbeddingDesc)]
+        L.sol_grad_workspace_bytes.restype, L.sol_grad_workspace_bytes.argtypes = sz, [vp, i]
+        L.sol_grad_norm.argtypes = [vp, i, vp, vp, sz, vp]
+        L.sol_grad_clip.argtypes = [vp, i, C.c_float, vp, vp, sz, vp]
+        L.sol_network_clip_workspace_bytes.restype, L.sol_network_clip_workspace_bytes.argtypes = sz, [vp]
+        L.sol_network_clip_gradients.argtypes = [vp, C.c_float, vp, vp, sz, vp]
         L.sol_network_forward.argtypes = [vp, vp, vp, vp, sz, vp]
         L.sol_network_backward.argtypes = [vp, vp, vp, vp, vp, sz, vp]
         L.sol_network_sgd_step.argtypes = [vp, C.c_float, C.c_float, vp]
@@ -448,6 +471,137 @@ def sol_dropout(x, drop, residual=None, out=None, stream=None):
     return y
 
 
+def sol_layer_norm(x, gamma=None, beta=None, eps=1e-5, want_stats=False, out=None, stream=None):
+    """y = (x - mean) * rstd * gamma + beta over the rows of x [rows][cols] of any pitch; gamma, beta: fp32 [cols] or None (1 / 0); out: [rows][cols] of any pitch
+    (may be x).  Returns (y, mean, rstd), the last two fp32 [rows], or None without want_stats; the backward pass needs them."""
+    rows, cols = x.shape
+    xa, ldx = _rows(x, cols, "x")
+    handle, side = _on_current(x, None, stream)
+    ga, ba = _dense(gamma, (cols,), "gamma", x, torch.float32), _dense(beta, (cols,), "beta", x, torch.float32)
+    if out is None:
+        y, ldy = _result(x, (rows, cols), x.dtype, side), cols
+        ya = y.data_ptr()
+    else:
+        y = out
+        ya, ldy = _rows(y, cols, "out", x)
+    mean, rstd = (_result(x, rows, torch.float32, side), _result(x, rows, torch.float32, side)) if want_stats else (None, None)
+    _check(lib().sol_layer_norm(LayerNormDesc(rows, cols, dtype_of(x), ldx, ldy, eps), xa, ga, ba, ya, mean.data_ptr() if want_stats else 0, rstd.data_ptr() if want_stats else 0, handle))
+    return y, mean, rstd
+
+
+def sol_layer_norm_backward(dy, x, mean, rstd, gamma=None, residual=None, need_dx=True, need_dgamma=True, need_dbeta=True, workspace=None, stream=None):
+    """Gradients of sol_layer_norm: dy and x [rows][cols] with rows of any pitch; mean, rstd: as the forward call returned them; residual: dense [rows][cols] that is
+    added to dx (the gradient that reaches x past the layer).  Returns (dx, dgamma, dbeta), the last two fp32, None for what is not needed."""
+    rows, cols = x.shape
+    xa, ldx = _rows(x, cols, "x")
+    handle, side = _on_current(x, None, stream)
+    ga, ldg = _rows(dy, cols, "dy", x)
+    wa, ma, sa = _dense(gamma, (cols,), "gamma", x, torch.float32), _dense(mean, (rows,), "mean", x, torch.float32), _dense(rstd, (rows,), "rstd", x, torch.float32)
+    ra = _dense(residual, (rows, cols), "residual", x)
+    dx = _result(x, (rows, cols), x.dtype, side) if need_dx else None
+    dgamma = _result(x, cols, torch.float32, side) if need_dgamma else None
+    dbeta = _result(x, cols, torch.float32, side) if need_dbeta else None
+    nd = LayerNormDesc(rows, cols, dtype_of(x), ldx, ldg, 0.0)
+    sa_, sbytes, keep = _scratch(workspace, lib().sol_layer_norm_backward_workspace_bytes(nd), x, side)
+    _check(lib().sol_layer_norm_backward(nd, ga, xa, wa, ma, sa, ra, dx.data_ptr() if need_dx else 0, dgamma.data_ptr() if need_dgamma else 0, dbeta.data_ptr() if need_dbeta else 0,
+                                         sa_, sbytes, handle))
+    return dx, dgamma, dbeta
+
+
+def _tokens(tokens, pad, like):
+    """Address, number and bits of a tensor of tokens."""
+    if not -(1 << 31) <= pad < 1 << 31:
+        raise ValueError(f"pad: {pad} is no 32-bit number")
+    if tokens.dtype not in (torch.int32, torch.int64) or not tokens.is_contiguous() or tokens.get_device() != like.get_device():
+        raise ValueError(f"tokens: a contiguous int32 or int64 tensor on {like.device} is wanted, not {tokens.dtype} on {tokens.device}")
+    n = tokens.numel()
+    if n >= 1 << 31:
+        raise SolError(6, f"tokens: {n} of them: 2^31 or more")                                # a C int would get the low 32 bits
+    return tokens.data_ptr(), n, 64 if tokens.dtype == torch.int64 else 32
+
+
+def sol_embedding(tokens, table, scale=1.0, pad=-1, out=None, stream=None):
+    """y[i] = scale * table[tokens[i]]: tokens int32 or int64 of any shape, table [vocab][cols] with rows of any pitch; the rows of tokens equal to pad are zeros, those of
+    other tokens outside the table NaN.  out: [number of tokens][cols] with rows of any pitch.  Returns y [*tokens.shape][cols], or out."""
+    vocab, cols = table.shape
+    ta, ldt = _rows(table, cols, "table")
+    handle, side = _on_current(table, None, stream)
+    ka, n, bits = _tokens(tokens, pad, table)
+    if out is None:
+        y, ldy = _result(table, (*tokens.shape, cols), table.dtype, side), cols
+        ya = y.data_ptr()
+    else:
+        y = out
+        ya, ldy = _rows(y, cols, "out")
+        if y.shape[0] != n or y.dtype != table.dtype or y.get_device() != table.get_device():
+            raise ValueError(f"out: {n} rows of {table.dtype} on {table.device} are wanted, not {y.shape[0]} of {y.dtype} on {y.device}")
+    _check(lib().sol_embedding(EmbeddingDesc(n, vocab, cols, dtype_of(table), bits, ldt, ldy, scale, pad), ka, ta, ya, handle))
+    return y
+
+
+def sol_embedding_backward(dy, tokens, vocab, scale=1.0, pad=-1, dtable_dtype=None, add_to=None, workspace=None, stream=None):
+    """Gradient of sol_embedding's table: dy [number of tokens][cols] with rows of any pitch, or contiguous [*tokens.shape][cols].  Returns dtable [vocab][cols] of dy's type or
+    dtable_dtype, zeros where no token is; add_to: a contiguous tensor like that, to which the sums are added, and which is returned."""
+    cols = dy.shape[-1]
+    if dy.dim() != 2:
+        if dy.shape[:-1] != tokens.shape or not dy.is_contiguous():
+            raise ValueError(f"dy: contiguous [*{tuple(tokens.shape)}][cols] is wanted, not a tensor of shape {tuple(dy.shape)} and strides {dy.stride()}")
+        dy = dy.view(tokens.numel(), cols)
+    ga, ldg = _rows(dy, cols, "dy")
+    handle, side = _on_current(dy, None, stream)
+    ka, n, bits = _tokens(tokens, pad, dy)
+    if dy.shape[0] != n:
+        raise ValueError(f"dy: {dy.shape[0]} rows do not go with {n} tokens")
+    wdt = add_to.dtype if add_to is not None else dy.dtype if dtable_dtype is None else dtable_dtype
+    if wdt not in (torch.float32, torch.bfloat16) or (dtable_dtype is not None and wdt != dtable_dtype):
+        raise ValueError(f"dtable_dtype: float32 or dy's type is wanted, not {wdt if dtable_dtype is None else dtable_dtype}")
+    if not 0 < vocab < 1 << 31:
+        raise ValueError(f"vocab: {vocab}")
+    dtable = _result(dy, (vocab, cols), wdt, side) if add_to is None else add_to
+    da = dtable.data_ptr() if add_to is None else _dense(add_to, (vocab, cols), "add_to", dy, wdt)
+    ed = EmbeddingDesc(n, vocab, cols, dtype_of(dy), bits, 0, ldg, scale, pad)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_embedding_backward_workspace_bytes(ed), dy, side)
+    _check(lib().sol_embedding_backward(ed, ka, ga, da, BF16 if wdt == torch.bfloat16 else F32, int(add_to is not None), wa, wbytes, handle))
+    return dtable
+
+
+def _grad_list(grads, out):
+    """The list as the library takes it (entries as Grad has them), from tensors of one device; out: None, or where each result goes."""
+    device = grads[0].get_device() if len(grads) else -1
+    flat = []
+    for g, o in zip(grads, grads if out is None else out, strict=True):
+        dt = g.dtype
+        if not g.is_cuda or dt not in (torch.float32, torch.bfloat16) or not g.is_contiguous() or g.get_device() != device:
+            raise ValueError(f"gradients: contiguous float32 or bfloat16 tensors of one GPU are wanted, not {dt} of strides {g.stride()} on {g.device}")
+        if o is not g and (o.dtype != dt or o.shape != g.shape or not o.is_contiguous() or o.get_device() != device):
+            raise ValueError(f"out: a contiguous {dt} tensor of shape {tuple(g.shape)} on {g.device} is wanted, not {tuple(o.shape)} of {o.dtype} on {o.device}")
+        flat += (g.data_ptr(), o.data_ptr(), g.numel(), BF16 if dt == torch.bfloat16 else F32)
+    if not flat:
+        raise ValueError("gradients: one tensor at least is wanted")
+    return (C.c_int64 * len(flat))(*flat)
+
+
+def sol_grad_norm(grads, workspace=None, stream=None):
+    """The norm of all tensors of the list together, as an fp32 tensor without dimensions."""
+    arr = _grad_list(grads, None)
+    handle, side = _on_current(grads[0], None, stream)
+    norm = _result(grads[0], (), torch.float32, side)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_grad_workspace_bytes(arr, len(grads)), grads[0], side)
+    _check(lib().sol_grad_norm(arr, len(grads), norm.data_ptr(), wa, wbytes, handle))
+    return norm
+
+
+def sol_grad_clip(grads, max_norm, out=None, workspace=None, stream=None):
+    """Multiplies all tensors of the list by max_norm / norm if their norm is finite and above max_norm, in place, or into the tensors of the list `out`.  Returns the norm, as
+    sol_grad_norm does."""
+    arr = _grad_list(grads, out)
+    handle, side = _on_current(grads[0], None, stream)
+    norm = _result(grads[0], (), torch.float32, side)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_grad_workspace_bytes(arr, len(grads)), grads[0], side)
+    _check(lib().sol_grad_clip(arr, len(grads), max_norm, norm.data_ptr(), wa, wbytes, handle))
+    return norm
+
+
 def sol_pool(x, pd, want_argmax=False, stream=None):
     pd = pd if isinstance(pd, PoolDesc) else pool_desc(pd)
     n, h, w, c = x.shape
@@ -718,6 +872,14 @@ class Network:
         _check(lib().sol_network_backward(self._h, _addr(x), _addr(labels), _addr(self.loss), _addr(self.workspace), self.workspace.numel(),
                                           _stream_handle(stream)))
         return self.loss[:1]
+
+    def clip_gradients(self, max_norm, stream=None):
+        """sol_grad_clip on every gradient of the last backward; returns the device scalar holding their norm."""
+        if not hasattr(self, "grad_norm"):
+            self.grad_norm = torch.zeros(4, dtype=torch.float32, device=self.device)
+            self.clip_space = torch.empty(max(lib().sol_network_clip_workspace_bytes(self._h), 16), dtype=torch.uint8, device=self.device)
+        _check(lib().sol_network_clip_gradients(self._h, max_norm, _addr(self.grad_norm), _addr(self.clip_space), self.clip_space.numel(), _stream_handle(stream)))
+        return self.grad_norm[:1]
 
     def sgd_step(self, lr, momentum, stream=None):
         _check(lib().sol_network_sgd_step(self._h, lr, momentum, _stream_handle(stream)))

@@ -1,0 +1,699 @@
+"""Layer norm, embedding and gradient clipping through the public entry points, against the 64-bit oracle.
+
+Tolerances are counted in roundings: `half` = half a step of the output type, U = 2^-24 for an fp32 operation.  Where every sum is a whole number below 2^24 it is exact in
+fp32 whatever its order, and the outputs have to be EQUAL (for bf16 after one rounding of the exact value).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import linear_ops as lo
+from oracle import train_ops as to
+
+pytestmark = pytest.mark.gpu
+
+HALF = {"f32": 2.0**-24, "bf16": 2.0**-8}      # half a step, relative
+U = 2.0**-24
+TDT = {"f32": torch.float32, "bf16": torch.bfloat16}
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def sol():
+    from paper_2003_10688_amd import sol as s
+
+    s.lib()
+    return s
+
+
+def dev(a, dt="f32", pitch=0, fill=float("nan")):
+    """Device tensor of an array; pitch: so many more columns per row, which hold `fill`."""
+    t = torch.from_numpy(np.ascontiguousarray(a, np.float32)).to(DEV, TDT[dt])
+    if not pitch:
+        return t
+    wide = torch.full((a.shape[0], a.shape[1] + pitch), fill, dtype=TDT[dt], device=DEV)
+    wide[:, :a.shape[1]] = t
+    return wide[:, :a.shape[1]]
+
+
+def host(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+def grid(a, dt):
+    """Values that dt holds exactly."""
+    return host(torch.from_numpy(np.asarray(a, np.float32)).to(TDT[dt]))
+
+
+def close(got, want, tol, what):
+    bad = np.abs(got - want) - tol
+    assert np.all(np.isfinite(got)) and bad.max() <= 0, f"{what}: off by {np.abs(got - want).flat[bad.argmax()]:.3g}, {tol.flat[bad.argmax()]:.3g} allowed, at {np.unravel_index(bad.argmax(), bad.shape)}"
+
+
+# ---- layer norm -------------------------------------------------------------------------------------------------
+# rows, columns: one of each, ends inside a group of 8, inside a wave, at and around the borders between the kernels, rows that registers do not hold
+SHAPES = [(1, 1), (3, 2), (5, 7), (2, 8), (1, 9), (70, 64), (33, 500), (4, 511), (4, 512), (4, 513), (9, 1000), (9, 1024), (5, 1025), (1, 2048), (67, 2047), (5, 2049), (130, 1531), (3, 4095), (3, 4096), (3, 4097),
+          (2, 8191), (2, 8192), (2, 8193), (3, 10001), (2, 16384), (2, 16385), (2, 40000), (1, 1 << 20), (700, 33), (5000, 16), (3000, 257), (1100, 1024), (600, 4096), (2100, 2056), (1030, 8190)]
+
+
+def norm_inputs(rows, cols, dt, shift=0.0):
+    rng = np.random.default_rng([rows, cols])
+    x = grid(rng.standard_normal((rows, cols)) * np.exp(0.3 * rng.standard_normal(cols)) + shift, dt)
+    return x, (1 + 0.3 * rng.standard_normal(cols)).astype(np.float32), rng.standard_normal(cols).astype(np.float32), grid(rng.standard_normal((rows, cols)), dt), grid(rng.standard_normal((rows, cols)), dt)
+
+
+def norm_tolerances(x, mean, rstd, cols):
+    """How far mean, rstd (relative) may be off.  N additions at most lie one behind the other in a sum: 8 per group of a thread, then those over the wave, the workgroup."""
+    n = 8 * (cols // 8192 + 2) + 48
+    em = (n + 3) * U * np.abs(x).mean(1)                          # a sum's additions, its scale, the waves' means put together
+    sd = 1 / rstd                                                  # with eps inside, which only makes the terms below larger than they have to be where the deviation is small
+    # deviations off by the mean's error enter the sum of squares to first order only through the waves' own means (each differs from the row's by at most 8 deviations: 64 lanes and more
+    # of 8 columns against the row), then n additions, the scale, eps and the reciprocal root's 1 ulp
+    er = (n / 2 + 6) * U + 8 * em / sd + (em / sd) ** 2
+    return em, er
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_layer_norm(sol, dt, rows, cols):
+    x, gamma, beta, _, _ = norm_inputs(rows, cols, dt, shift=0.5)
+    for pitch, weights in ((0, True), (3, True), (8, False)):
+        gm, bt = (gamma, beta) if weights else (None, None)
+        y, mean, rstd = sol.sol_layer_norm(dev(x, dt, pitch), *(None if w is None else dev(w) for w in (gm, bt)), eps=1e-3, want_stats=True)
+        wy, wm, wr = to.layer_norm(x, gm, bt, 1e-3)
+        em, er = norm_tolerances(x, wm, wr, cols)
+        close(host(mean), wm, em + U * np.abs(wm), "mean")
+        close(host(rstd), wr, er * wr, "rstd")
+        g = np.ones(cols) if gm is None else np.abs(gamma.astype(np.float64))
+        b = np.zeros(cols) if bt is None else np.abs(beta.astype(np.float64))
+        h = np.abs(wy - (0 if bt is None else beta))               # |(x - mean) rstd gamma|
+        tol = (em + 2 * U * np.abs(x - wm[:, None]).max(1))[:, None] * wr[:, None] * g * 1.01 + (er[:, None] + 4 * U) * h + 2 * U * b + HALF[dt] * np.abs(wy) * 1.02
+        close(host(y), wy, tol, "y")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_layer_norm_backward(sol, dt, rows, cols):
+    x, gamma, _, dy, res = norm_inputs(rows, cols, dt)
+    _, mean, rstd = to.layer_norm(x)
+    mean, rstd = mean.astype(np.float32), rstd.astype(np.float32)
+    n = 8 * (cols // 8192 + 2) + 48
+    for pitch, gm, r in ((0, gamma, None), (5, gamma, res), (8, None, res)):
+        dx, dg, db = sol.sol_layer_norm_backward(dev(dy, dt, pitch), dev(x, dt, pitch), dev(mean), dev(rstd), None if gm is None else dev(gm), residual=None if r is None else dev(r, dt))
+        wx, wg, wb = to.layer_norm_bwd(dy, x, mean, rstd, gm, r)
+        rs = rstd.astype(np.float64)[:, None]
+        h = np.abs(x - mean.astype(np.float64)[:, None]) * rs      # two roundings
+        g = np.abs(dy) * (1 if gm is None else np.abs(gm.astype(np.float64)))      # one
+        c1, c2 = g.mean(1, keepdims=True), (g * h).mean(1, keepdims=True)           # of magnitudes: a sum is off by its additions' share of them
+        inner = 5 * U * (g + c1 + h * c2) + (n + 4) * U * c1 + h * (n + 8) * U * c2
+        close(host(dx), wx, rs * inner * 1.01 + U * (0 if r is None else np.abs(r) + np.abs(wx)) + HALF[dt] * np.abs(wx) * 1.02, "dx")
+        close(host(dg), wg, (rows + 48) * U * (np.abs(dy) * h).sum(0), "dgamma")
+        close(host(db), wb, (rows + 48) * U * np.abs(dy).sum(0), "dbeta")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(1, 8), (5, 77), (64, 2048), (65, 2048), (600, 1000), (3000, 4096), (70, 9000), (2500, 24)])
+def test_column_sums_of_whole_numbers(sol, dt, rows, cols):
+    """mean 0, rstd 1 and whole x and dy: dgamma = sum of dy x and dbeta = sum of dy to the last bit, whatever is asked for beside them."""
+    rng = np.random.default_rng([cols, rows])
+    x, dy = rng.integers(-3, 4, (rows, cols)), rng.integers(-3, 4, (rows, cols))
+    args = (dev(dy, dt, 3), dev(x, dt, 3), torch.zeros(rows, device=DEV), torch.ones(rows, device=DEV))
+    wg, wb = (x * dy).sum(0), dy.sum(0)
+    for need in ((True, True, True), (False, True, True), (True, False, True), (False, True, False), (True, True, False), (False, False, True)):
+        dx, dg, db = sol.sol_layer_norm_backward(*args, need_dx=need[0], need_dgamma=need[1], need_dbeta=need[2])
+        assert (dx is not None, dg is not None, db is not None) == need
+        assert dg is None or np.array_equal(host(dg), wg)
+        assert db is None or np.array_equal(host(db), wb)
+    alone = sol.sol_layer_norm_backward(*args, need_dgamma=False, need_dbeta=False)
+    assert alone[1] is None and alone[2] is None and torch.isfinite(alone[0]).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_rows_far_from_zero(sol, dt):
+    """Deviations of 1 about a mean of 4096, and rows without any deviation: the variance is that about the mean, not a difference of large sums."""
+    rng = np.random.default_rng(5)
+    for cols in (100, 1000, 3000, 6000, 20000):
+        x = 4096 + rng.integers(-1, 2, (6, cols)) * (16.0 if dt == "bf16" else 1.0)      # bf16 has steps of 32 there; 16 rounds to even and so to multiples of 32
+        x = grid(x, dt)
+        x[2] = 4096
+        y, mean, rstd = sol.sol_layer_norm(dev(x, dt), eps=1e-5, want_stats=True)
+        wy, wm, wr = to.layer_norm(x)
+        # x - mean: the mean is off by half a step at 4096 (2^-12) and a few additions' share; relative to deviations of about 1
+        assert np.abs(host(mean) - wm).max() <= 2.0**-9
+        flat = np.arange(6) == 2
+        assert np.all(host(y)[flat] == 0) and np.allclose(host(rstd)[flat], wr[flat], rtol=1e-6)      # all sums of equal terms 4096: exact for these counts' partial sums
+        assert np.abs(host(rstd) / wr - 1)[~flat].max() <= 1e-4 and np.abs(host(y) - wy)[~flat].max() <= 2.0**-7 * np.abs(wy).max() + 2.0**-8
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(9, 40), (9, 900), (9, 2048), (9, 4001), (9, 20000), (300, 2048)])
+def test_rows_that_are_not_finite(sol, dt, rows, cols):
+    """An infinity or a NaN stays in its row of y and dx; what it does to dgamma and dbeta, it does in every column it meets."""
+    x, gamma, beta, dy, _ = norm_inputs(rows, cols, dt)
+    x[2, 3], x[4, 0], x[5, cols - 1] = np.inf, np.nan, -np.inf
+    y, mean, rstd = sol.sol_layer_norm(dev(x, dt), dev(gamma), dev(beta), want_stats=True)
+    fine = np.delete(np.arange(rows), [2, 4, 5])
+    assert np.all(np.isnan(host(y)[[2, 4, 5]])) and np.all(np.isnan(host(rstd)[[2, 4, 5]])) and not np.any(np.isfinite(host(mean)[[2, 4, 5]]))
+    assert np.all(np.isfinite(host(y)[fine]))
+    clean = sol.sol_layer_norm(dev(np.where(np.isfinite(x), x, 0), dt), dev(gamma), dev(beta))[0]
+    assert np.array_equal(host(y)[fine], host(clean)[fine])
+    dx, dg, db = sol.sol_layer_norm_backward(dev(dy, dt), dev(x, dt), mean, rstd, dev(gamma))
+    assert np.all(np.isnan(host(dx)[[2, 4, 5]])) and np.all(np.isfinite(host(dx)[fine])) and np.all(np.isnan(host(dg))) and np.all(np.isfinite(host(db)))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(1, 5), (37, 100), (37, 1030), (37, 3000), (37, 8192), (5, 17000), (500, 2048)])
+def test_what_lies_between_rows_and_in_place(sol, dt, rows, cols):
+    """Gaps of NaN beside x and dy do not reach a result, gaps of the outputs stay as they were; y may take x's place, dx the residual's."""
+    x, gamma, beta, dy, res = norm_inputs(rows, cols, dt)
+    want, mean, rstd = sol.sol_layer_norm(dev(x, dt), dev(gamma), dev(beta), want_stats=True)
+    for pitch in (1, 8, 64):
+        out = torch.full((rows, cols + pitch), 7.0, dtype=TDT[dt], device=DEV)
+        sol.sol_layer_norm(dev(x, dt, pitch), dev(gamma), dev(beta), out=out[:, :cols])
+        assert torch.equal(out[:, :cols], want) and torch.all(out[:, cols:] == 7)
+        place = dev(x, dt, pitch)
+        assert sol.sol_layer_norm(place, dev(gamma), dev(beta), out=place)[0] is place and torch.equal(place, want)
+    grads = sol.sol_layer_norm_backward(dev(dy, dt), dev(x, dt), mean, rstd, dev(gamma), residual=dev(res, dt))
+    for pitch in (1, 8, 64):
+        got = sol.sol_layer_norm_backward(dev(dy, dt, pitch), dev(x, dt, pitch), mean, rstd, dev(gamma), residual=dev(res, dt))
+        assert all(torch.equal(a, b) for a, b in zip(got, grads))
+    # dx in the residual's place, through the C entry point: the binding makes its results
+    place, xd, dyd, gm = dev(res, dt), dev(x, dt), dev(dy, dt), dev(gamma)
+    nd = sol.LayerNormDesc(rows, cols, sol.dtype_of(xd), 0, 0, 0.0)
+    ws = torch.empty(max(16, sol.lib().sol_layer_norm_backward_workspace_bytes(nd)), dtype=torch.uint8, device=DEV).fill_(255)
+    dg, db = torch.empty(cols, device=DEV), torch.empty(cols, device=DEV)
+    assert sol.lib().sol_layer_norm_backward(nd, dyd.data_ptr(), xd.data_ptr(), gm.data_ptr(), mean.data_ptr(), rstd.data_ptr(), place.data_ptr(), place.data_ptr(), dg.data_ptr(), db.data_ptr(),
+                                             ws.data_ptr(), ws.nbytes, sol._stream_handle()) == 0
+    assert torch.equal(place, grads[0]) and torch.equal(dg, grads[1]) and torch.equal(db, grads[2])
+
+
+def test_layer_norm_gradients_are_differences(sol):
+    rng = np.random.default_rng(4)
+    for rows, cols in ((11, 37), (4, 2500)):
+        x, gamma, beta, g = rng.standard_normal((rows, cols)), 1 + 0.2 * rng.standard_normal(cols), rng.standard_normal(cols), rng.standard_normal((rows, cols))
+        out = lambda x_, gm, bt: host(sol.sol_layer_norm(dev(x_), dev(gm), dev(bt))[0])  # noqa: E731
+        _, mean, rstd = sol.sol_layer_norm(dev(x), want_stats=True)
+        grads = [host(t) for t in sol.sol_layer_norm_backward(dev(g), dev(x), mean, rstd, dev(gamma))]
+        for i, t in enumerate((x, gamma, beta)):
+            u = rng.standard_normal(t.shape)
+            h = 2.0**-7
+            up, down = [x, gamma, beta], [x, gamma, beta]
+            up[i], down[i] = t + h * u, t - h * u
+            slope = float(((out(*up) - out(*down)) * g).sum()) / (2 * h)
+            # h^2 / 6 of a third derivative of order one along a step of unit size per element, and fp32 roundings over 2h
+            assert abs(slope - float((grads[i] * u).sum())) <= 1e-3 * np.linalg.norm(grads[i]) * np.linalg.norm(u), (i, slope)
+
+
+def test_no_rows(sol):
+    x = torch.empty((0, 24), device=DEV)
+    y, mean, rstd = sol.sol_layer_norm(x, want_stats=True)
+    assert y.shape == (0, 24) and mean.shape == (0,) and rstd.shape == (0,)
+    dx, dg, db = sol.sol_layer_norm_backward(x, x, mean, rstd)
+    assert dx.shape == (0, 24) and dg.shape == (24,) and not dg.any() and not db.any()
+    table = torch.ones((5, 24), device=DEV)
+    none = torch.empty(0, dtype=torch.int64, device=DEV)
+    assert sol.sol_embedding(none, table).shape == (0, 24)
+    d = sol.sol_embedding_backward(x, none, 5)
+    assert d.shape == (5, 24) and not d.any()
+    assert sol.sol_embedding_backward(x, none, 5, add_to=table) is table and torch.all(table == 1)
+
+
+# ---- embedding --------------------------------------------------------------------------------------------------
+def some_tokens(rng, n, vocab, kind):
+    if kind == "one":                                             # all the same
+        return np.full(n, vocab // 2)
+    if kind == "few":                                             # a few frequent ones: runs that end anywhere
+        return np.minimum(rng.geometric(0.3, n) - 1, vocab - 1)
+    t = rng.integers(0, vocab, n)
+    if kind == "rest":                                            # padding, and outside the table on both sides
+        t[::3] = -1
+        t[1::5] = vocab + rng.integers(0, 3, len(t[1::5]))
+        t[2::7] = -2 - rng.integers(0, 3, len(t[2::7]))
+    return t
+
+
+EMBED = [(1, 1, 1), (1, 10, 8), (3, 5, 7), (17, 100, 64), (8, 3, 520), (64, 40, 100), (65, 40, 33), (129, 7, 65), (500, 1000, 201), (300, 30000, 16), (2049, 50, 130), (5000, 300, 72), (16384, 257, 24), (16385, 9000, 40),
+         (40000, 4, 9), (100, 60, 2050), (3000, 2500, 1031)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n,vocab,cols", EMBED)
+def test_embedding(sol, dt, n, vocab, cols):
+    rng = np.random.default_rng([n, vocab, cols])
+    table = grid(rng.standard_normal((vocab, cols)), dt)
+    for kind, bits, pitch in (("any", torch.int64, 0), ("rest", torch.int32, 3)):
+        tok = some_tokens(rng, n, vocab, kind)
+        tokens = torch.from_numpy(tok).to(DEV, bits)
+        out = torch.full((n, cols + 8 + pitch), 7.0, dtype=TDT[dt], device=DEV)
+        for scale in (1.0, -0.5, 1.7):
+            want = to.embedding(tok, table, scale)
+            y = sol.sol_embedding(tokens, dev(table, dt, pitch), scale)
+            sol.sol_embedding(tokens, dev(table, dt, pitch), scale, out=out[:, :cols])
+            assert torch.equal(out[:, :cols].nan_to_num(9e9), y.nan_to_num(9e9)) and torch.all(out[:, cols:] == 7)
+            nan = np.isnan(want)
+            assert np.array_equal(np.isnan(host(y)), nan)
+            if scale == 1.7:                                      # the product rounds once, and once more to bf16
+                close(np.where(nan, 0, host(y)), np.where(nan, 0, want), (HALF[dt] * 1.01 + U) * np.where(nan, 0, np.abs(want)), "y")
+            else:
+                assert np.array_equal(np.where(nan, 0, host(y)), np.where(nan, 0, want))
+    shaped = torch.from_numpy(some_tokens(rng, 2 * 3 * n, vocab, "any")).to(DEV).view(2, 3 * n)
+    y = sol.sol_embedding(shaped, dev(table, dt))
+    assert y.shape == (2, 3 * n, cols) and torch.equal(y, dev(table, dt)[shaped])
+
+
+@pytest.mark.parametrize("dt,grad", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("n,vocab,cols", EMBED)
+def test_embedding_backward_of_whole_numbers(sol, dt, grad, n, vocab, cols):
+    """Equal to the last bit, into a new tensor, and added to one (whose rows without tokens keep their bits)."""
+    rng = np.random.default_rng([n, vocab, cols])
+    dy = rng.integers(-2, 3, (n, cols)).astype(np.float32)
+    for kind, bits, pitch in (("any", torch.int32, 0), ("one", torch.int64, 3), ("few", torch.int64, 8), ("rest", torch.int32, 1)):
+        tok = some_tokens(rng, n, vocab, kind)
+        tokens = torch.from_numpy(tok).to(DEV, bits)
+        got = sol.sol_embedding_backward(dev(dy, dt, pitch), tokens, vocab, 2.0, dtable_dtype=TDT[grad])
+        want = to.embedding_bwd(dy, tok, vocab, 2.0)
+        assert got.dtype == TDT[grad] and np.array_equal(host(got), grid(want, grad)), kind
+        start = rng.integers(-2, 3, (vocab, cols)).astype(np.float32)
+        unused = ~np.isin(np.arange(vocab), tok)
+        first = dev(start, grad)
+        first[torch.from_numpy(unused).to(DEV)] = float("nan")
+        assert sol.sol_embedding_backward(dev(dy, dt, pitch), tokens, vocab, 2.0, add_to=first) is first
+        assert np.array_equal(host(first)[~unused], grid(want + start, grad)[~unused]) and np.all(np.isnan(host(first)[unused])), kind
+
+
+@pytest.mark.parametrize("dt,grad", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("n,vocab,cols", [(700, 90, 40), (20000, 3000, 100), (9000, 2, 520)])
+def test_embedding_backward_of_real_numbers(sol, dt, grad, n, vocab, cols):
+    rng = np.random.default_rng([vocab, n])
+    tok = some_tokens(rng, n, vocab, "few" if vocab > 100 else "any")
+    dy = grid(rng.standard_normal((n, cols)), dt)
+    got = host(sol.sol_embedding_backward(dev(dy, dt), torch.from_numpy(tok).to(DEV), vocab, 1.3, dtable_dtype=TDT[grad]))
+    want, size = to.embedding_bwd(dy, tok, vocab, 1.3), to.embedding_bwd(np.abs(dy), tok, vocab, 1.3)
+    count = np.bincount(tok, minlength=vocab)[:, None]
+    close(got, want, (count + 3) * U * size + HALF[grad] * np.abs(want) * 1.01, "dtable")      # at most count additions, and the factor
+
+
+def test_embedding_padding_token_of_the_table(sol):
+    """pad may be a row of the table: it reads as zeros and gets no gradient."""
+    table = torch.arange(1.0, 41.0, device=DEV).view(5, 8)
+    tokens = torch.tensor([3, 0, 3, 4, 1], device=DEV)
+    y = sol.sol_embedding(tokens, table, pad=3)
+    assert not y[[0, 2]].any() and torch.equal(y[[1, 3, 4]], table[[0, 4, 1]])
+    d = sol.sol_embedding_backward(torch.ones((5, 8), device=DEV), tokens, 5, pad=3)
+    assert torch.equal(d[:, 0], torch.tensor([1.0, 1, 0, 0, 1], device=DEV))
+    wide = torch.tensor([2**32, 2**32 + 3, -(2**32) - 1, 2**63 - 1, 1], device=DEV)      # tokens whose low 32 bits are others'
+    y = sol.sol_embedding(wide, table)
+    assert torch.isnan(y[:4]).all() and torch.equal(y[4], table[1])
+    assert torch.equal(sol.sol_embedding_backward(torch.ones((5, 8), device=DEV), wide, 5)[:, 0], torch.tensor([0.0, 1, 0, 0, 0], device=DEV))
+
+
+# ---- clipping ---------------------------------------------------------------------------------------------------
+def clip_tensors(rng, sizes, dts, apart):
+    """Slices of one flat buffer, `apart` elements between them (their addresses are aligned to nothing but themselves), or tensors of their own."""
+    out = []
+    for i, n in enumerate(sizes):
+        a = grid(rng.standard_normal(n) * 0.01 * (1 + i % 5), dts[i % len(dts)])
+        t = dev(a, dts[i % len(dts)])
+        if apart is not None:
+            room = torch.full((n + 2 * apart + 16,), 7.0, dtype=t.dtype, device=DEV)
+            at = apart + i % 9
+            room[at:at + n] = t
+            t = room[at:at + n]
+        out.append((a, t))
+    return out
+
+
+CLIP = [[1], [0], [0, 5, 0], [8192], [8191, 8193, 1], [100, 3, 1, 17] * 5, [2048, 2047, 2049], [1] * 113, [7] * 112, [30] * 400, [1000003], [40000] * 130, [3000000, 5, 12345]]
+
+
+@pytest.mark.parametrize("dts", [("f32",), ("bf16",), ("bf16", "f32")])
+@pytest.mark.parametrize("at", range(len(CLIP)))
+def test_clip(sol, at, dts):
+    rng = np.random.default_rng(at)
+    for apart in (None, 3):
+        ts = clip_tensors(rng, CLIP[at], dts, apart)
+        norm, _, _ = to.grad_clip([a for a, _ in ts], 1.0)
+        got = sol.sol_grad_norm([t for _, t in ts])
+        assert got.shape == () and got.dtype == torch.float32
+        assert abs(float(got) - norm) <= 1.01 * U * norm          # one rounding: squares are summed in 64 bits
+        for share in (0.25, 0.99, 1.01, 100.0, float("inf")):
+            limit = share * max(norm, 1e-30)
+            wn, factor, want = to.grad_clip([a for a, _ in ts], limit)
+            out = [torch.full_like(t, 5.0) for _, t in ts]
+            assert torch.equal(sol.sol_grad_clip([t for _, t in ts], limit, out=out), got)
+            for (a, t), o, w in zip(ts, out, want):
+                if factor == 1.0:
+                    assert torch.equal(o, t)
+                else:                                             # norm, quotient, product, then the type
+                    assert a.size == 0 or np.all(np.abs(host(o) - w) <= (4 * U + HALF[dts[0] if len(dts) == 1 else "bf16"]) * np.abs(w))
+            place = [t.clone() for _, t in ts]
+            assert torch.equal(sol.sol_grad_clip(place, limit), got) and all(torch.equal(p, o) for p, o in zip(place, out))
+        if apart is not None:                                     # in place in a buffer that others use too
+            sol.sol_grad_clip([t for _, t in ts], max(norm / 2, 1e-30))
+            for i, (_, t) in enumerate(ts):
+                room = t._base
+                assert torch.all(room[:apart + i % 9] == 7) and torch.all(room[apart + i % 9 + t.numel():] == 7)
+
+
+def test_clip_leaves_what_is_not_finite(sol):
+    for bad, want in ((float("inf"), float("inf")), (float("-inf"), float("inf")), (float("nan"), float("nan"))):
+        ts = [torch.ones(5000, device=DEV), torch.ones(77, device=DEV, dtype=torch.bfloat16)]
+        ts[1][76] = bad
+        before = [t.clone() for t in ts]
+        n = float(sol.sol_grad_clip(ts, 0.5))
+        assert (n == want or (np.isnan(n) and np.isnan(want))) and all(torch.equal(a.nan_to_num(3), b.nan_to_num(3)) for a, b in zip(ts, before))
+        out = [torch.zeros_like(t) for t in ts]
+        sol.sol_grad_clip(ts, 0.5, out=out)
+        assert all(torch.equal(a.nan_to_num(3), b.nan_to_num(3)) for a, b in zip(ts, out))
+
+
+def test_clip_of_very_large_and_very_small_values(sol):
+    """Squares that fp32 does not hold: 1e30 and 1e-30, summed in 64 bits."""
+    for size in (1e30, 1e-30, 3e38):
+        t = torch.full((4,), size, device=DEV)
+        n = float(sol.sol_grad_norm([t]))
+        want = 2 * float(t[0])
+        assert n == want if want < 3.4e38 else n == float("inf")
+        if want < 3.4e38:
+            sol.sol_grad_clip([t], want / 4)
+            assert torch.allclose(t, torch.full_like(t, size / 4), rtol=1e-6, atol=0)
+    z = torch.zeros(100, device=DEV)
+    assert float(sol.sol_grad_clip([z], 1.0)) == 0 and not z.any()
+
+
+def test_clip_network_gradients(sol, oracle_mod):
+    """sol_network_clip_gradients is sol_grad_clip on every gradient of the network."""
+    from paper_2003_10688_amd import workloads as wl
+
+    wk = wl.config(1, batch=4)
+    layers = [dict(l, pool=None) if l["kind"] == "conv" else l for l in wk.layers]
+    net = sol.Network(layers, wk.in_shape, sol.F32, flags=sol.NET_TRAINING)
+    net.set_params(wk.params)
+    x = sol.to_device_nhwc(wk.x, sol.F32)
+    labels = torch.tensor([1, 0, 3, 2], dtype=torch.int32, device=DEV)
+
+    def gradients():
+        out = []
+        for i, l in enumerate(layers):
+            if l["kind"] in ("conv", "linear"):
+                out += [net.tensor(i, k) for k in ([sol.NT_GRAD_W] + ([sol.NT_GRAD_GAMMA, sol.NT_GRAD_BETA] if l["kind"] == "conv" and l["bn"] else [sol.NT_GRAD_BIAS]))]
+        return out
+
+    net.forward(x)
+    net.backward(x, labels)
+    before = [g.clone() for g in gradients()]
+    norm, factor, want = to.grad_clip([host(g) for g in before], 0.0)
+    assert norm > 0 and abs(float(net.clip_gradients(2 * norm)) - norm) <= 1.01 * U * norm and all(torch.equal(a, b) for a, b in zip(before, gradients()))
+    limit = norm / 3
+    _, factor, want = to.grad_clip([host(g) for g in before], limit)
+    net.clip_gradients(limit)
+    assert all(np.all(np.abs(host(g) - w) <= 5 * U * np.abs(w)) for g, w in zip(gradients(), want))
+    w0 = net.tensor(0, sol.NT_W).clone()
+    net.sgd_step(0.5, 0.0)
+    assert torch.allclose(net.tensor(0, sol.NT_W), w0 - 0.5 * gradients()[0], rtol=1e-6, atol=1e-7)
+
+
+# ---- streams, graphs, repeats ------------------------------------------------------------------------------------
+def everything(sol, d, **kw):
+    y, mean, rstd = sol.sol_layer_norm(d["x"], d["gamma"], d["beta"], want_stats=True, stream=kw.get("stream"))
+    out = (y, mean, rstd) + sol.sol_layer_norm_backward(d["dy"], d["x"], mean, rstd, d["gamma"], residual=d["res"], **kw)
+    e = sol.sol_embedding(d["tokens"], d["table"], 1.5, stream=kw.get("stream"))
+    t = sol.sol_embedding_backward(d["de"], d["tokens"], d["table"].shape[0], 1.5, **kw)
+    n = sol.sol_grad_norm(d["grads"], **kw)
+    c = sol.sol_grad_clip(d["grads"], 0.1, out=d["out"], **kw)
+    return out + (e, t, n, c, *d["out"])
+
+
+def data_for(dt, rows, cols, n, vocab, seed):
+    gen = torch.Generator(device=DEV).manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, generator=gen, device=DEV)  # noqa: E731
+    d = {"x": rnd(rows, cols).to(TDT[dt]), "dy": rnd(rows, cols).to(TDT[dt]), "res": rnd(rows, cols).to(TDT[dt]), "gamma": rnd(cols), "beta": rnd(cols), "table": rnd(vocab, cols).to(TDT[dt]),
+         "de": rnd(n, cols).to(TDT[dt]), "tokens": (torch.rand(n, generator=gen, device=DEV) ** 4 * vocab).long(), "grads": [rnd(k).to(TDT[dt]) for k in (5, 30000, 1, 9001, 400000)]}
+    d["out"] = [torch.empty_like(g) for g in d["grads"]]
+    return d
+
+
+SETS = [("bf16", 700, 520, 3000, 333), ("f32", 41, 2049, 60, 900), ("bf16", 3000, 1024, 20000, 70)]
+
+
+@pytest.mark.parametrize("dt,rows,cols,n,vocab", SETS)
+def test_repeats_and_workspaces(sol, dt, rows, cols, n, vocab):
+    """A call repeated gives the same bits, wherever its workspace lies and whatever it holds; one that is too small is refused."""
+    d = data_for(dt, rows, cols, n, vocab, 1)
+    want = [t.clone() for t in everything(sol, d)]
+    room = torch.empty(1 << 28, dtype=torch.uint8, device=DEV)
+    for i in range(3):
+        room.fill_((255, 0, 77)[i])
+        d = {k: [t.clone() for t in v] if isinstance(v, list) else v.clone() for k, v in d.items()}
+        assert all(torch.equal(a, b) for a, b in zip(want, everything(sol, d, workspace=room[i * 4096:])))
+    for f in (lambda: sol.sol_embedding_backward(d["de"], d["tokens"], vocab, workspace=room[:64]), lambda: sol.sol_grad_norm(d["grads"], workspace=room[:0])):
+        with pytest.raises(sol.SolError) as e:
+            f()
+        assert e.value.status == 5
+
+
+def test_calls_on_other_streams_without_a_workspace(sol):
+    """Two streams with work in front of the calls, while the current stream frees and allocates tensors: neither stream's scratch or results are the other's."""
+    sets = [data_for(*s, seed=k) for k, s in enumerate(SETS[:2])]
+    want = [[t.clone() for t in everything(sol, d)] for d in sets]
+    big = torch.randn((4096, 4096), device=DEV)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for d in sets:
+            for o in d["out"]:
+                o.zero_()
+        torch.cuda.synchronize()
+        for st in streams:
+            with torch.cuda.stream(st):
+                big @ big
+        big @ big
+        got = [everything(sol, sets[k], stream=streams[k]) for k in range(2)]
+        junk = [torch.full((m,), float("nan"), device=DEV) for m in (64, 700, 2049, 20000, 333 * 520, 900 * 2049, 1 << 20, 1 << 22) for _ in range(3)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for k in range(2) for a, b in zip(got[k], want[k]))
+        del junk, got
+
+
+def test_graphs_that_share_a_workspace(sol):
+    """Two graphs with one workspace, replayed in turn, inputs changing between."""
+    sets = [data_for(*s, seed=k) for k, s in enumerate(SETS)]
+    for d in sets:
+        everything(sol, d)
+    torch.cuda.synchronize()
+    ws = torch.empty(1 << 28, dtype=torch.uint8, device=DEV)
+    graphs, outs = [], []
+    for d in sets:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(everything(sol, d, workspace=ws))
+    for i in range(4):
+        for d in sets:
+            d["x"].mul_(-1.5)
+            d["tokens"].add_(1).remainder_(d["table"].shape[0])
+            d["grads"][1].mul_(1.25)
+        want = [[t.clone() for t in everything(sol, d)] for d in sets]
+        ws.fill_(i * 50)
+        for d in sets:
+            for o in d["out"]:
+                o.zero_()
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for k in range(len(sets)) for a, b in zip(outs[k], want[k])), i
+
+
+def test_captured_on_a_second_stream(sol):
+    sets = [data_for(*s, seed=k) for k, s in enumerate(SETS[:2])]
+    for d in sets:
+        everything(sol, d)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        outs = [everything(sol, sets[0]), everything(sol, sets[1], stream=side)]
+        torch.cuda.current_stream().wait_stream(side)
+    for i in range(3):
+        for d in sets:
+            d["x"].mul_(-1.5)
+        want = [[t.clone() for t in everything(sol, d)] for d in sets]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for k in range(2) for a, b in zip(outs[k], want[k])), i
+
+
+# ---- the operators together: a language model of one block ---------------------------------------------------------
+VOCAB, WIDTH, HIDDEN = 211, 72, 288
+
+
+def model_weights(seed):
+    rng = np.random.default_rng(seed)
+    return {"table": rng.standard_normal((VOCAB, WIDTH)) / np.sqrt(WIDTH), "g1": 1 + 0.2 * rng.standard_normal(WIDTH), "b1": 0.2 * rng.standard_normal(WIDTH),
+            "w1": rng.standard_normal((HIDDEN, WIDTH)) / np.sqrt(WIDTH), "c1": 0.1 * rng.standard_normal(HIDDEN), "w2": rng.standard_normal((WIDTH, HIDDEN)) / np.sqrt(HIDDEN),
+            "c2": 0.1 * rng.standard_normal(WIDTH), "g2": 1 + 0.2 * rng.standard_normal(WIDTH), "b2": 0.2 * rng.standard_normal(WIDTH)}
+
+
+SCALE = float(np.sqrt(WIDTH))
+DROPS = ((0.1, 77, 0, 6), (0.2, 77, 1, 6))
+
+
+def oracle_step(w, tokens, dlogits):
+    """x = embed; x += mlp(norm(x)); logits = norm(x) table^T; the table is the last layer's weight too."""
+    x0 = to.embedding(tokens, w["table"], SCALE)
+    n1, m1, r1 = to.layer_norm(x0, w["g1"], w["b1"])
+    h, z = lo.linear_fused(n1, w["w1"], w["c1"], "gelu", DROPS[0])
+    x1, _ = lo.linear_fused(h, w["w2"], w["c2"], "none", DROPS[1], x0)
+    n2, m2, r2 = to.layer_norm(x1, w["g2"], w["b2"])
+    logits, _ = lo.linear_fused(n2, w["table"])
+    g = {}
+    dn2, dtable, _, _ = lo.linear_fused_bwd(dlogits, n2, w["table"], None)
+    dx1, g["g2"], g["b2"] = to.layer_norm_bwd(dn2, x1, m2, r2, w["g2"])
+    dh, g["w2"], g["c2"], _ = lo.linear_fused_bwd(dx1, h, w["w2"], None, "none", DROPS[1])
+    dn1, g["w1"], g["c1"], _ = lo.linear_fused_bwd(dh, n1, w["w1"], z, "gelu", DROPS[0])
+    dx0, g["g1"], g["b1"] = to.layer_norm_bwd(dn1, x0, m1, r1, w["g1"], dx1)
+    g["table"] = to.embedding_bwd(dx0, tokens, VOCAB, SCALE, start=dtable)
+    return logits, g
+
+
+def pack(w, dt):
+    block = 64 if dt == "bf16" else 32
+    p = torch.zeros((w.shape[0], -(-w.shape[1] // block) * block), dtype=TDT[dt], device=DEV)
+    p[:, :w.shape[1]] = dev(w, dt)
+    return p
+
+
+class Model:
+    def __init__(self, sol, w, dt, step):
+        self.sol, self.dt = sol, dt
+        self.table = dev(w["table"], dt)
+        self.p = {k: pack(w[k], dt) for k in ("table", "w1", "w2")}
+        self.v = {k: dev(w[k]) for k in ("g1", "b1", "c1", "c2", "g2", "b2")}
+        self.d1, self.d2 = (sol.Dropout(p, seed, call, step) for p, seed, call, _ in DROPS)
+
+    def step(self, tokens, dlogits, max_norm):
+        s, v, p = self.sol, self.v, self.p
+        f32 = torch.float32
+        x0 = s.sol_embedding(tokens, self.table, SCALE)
+        n1, m1, r1 = s.sol_layer_norm(x0, v["g1"], v["b1"], want_stats=True)
+        h, z = s.sol_linear_fused(n1, p["w1"], HIDDEN, bias=v["c1"], act=s.ACT_GELU, drop=self.d1, want_preact=True)
+        x1, _ = s.sol_linear_fused(h, p["w2"], WIDTH, bias=v["c2"], drop=self.d2, residual=x0)
+        n2, m2, r2 = s.sol_layer_norm(x1, v["g2"], v["b2"], want_stats=True)
+        logits, _ = s.sol_linear_fused(n2, p["table"], VOCAB)
+        g = {}
+        dn2, dtable, _ = s.sol_linear_backward(dlogits, n2, p["table"], dw_dtype=f32, need_db=False)
+        dx1, g["g2"], g["b2"] = s.sol_layer_norm_backward(dn2, x1, m2, r2, v["g2"])
+        dh, g["w2"], g["c2"] = s.sol_linear_backward(dx1, h, p["w2"], drop=self.d2, dw_dtype=f32)
+        dn1, g["w1"], g["c1"] = s.sol_linear_backward(dh, n1, p["w1"], preact=z, act=s.ACT_GELU, drop=self.d1, dw_dtype=f32)
+        dx0, g["g1"], g["b1"] = s.sol_layer_norm_backward(dn1, x0, m1, r1, v["g1"], residual=dx1)
+        g["table"] = s.sol_embedding_backward(dx0, tokens, VOCAB, SCALE, add_to=dtable)
+        names = sorted(g)
+        norm = s.sol_grad_clip([g[k] for k in names], max_norm)
+        return (logits, norm) + tuple(g[k] for k in names)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [5, 190, 1500])
+def test_a_training_step_against_the_oracle(sol, dt, n):
+    """Relative 2-norms.  bf16 rounds the table, ten tensors on the way (2^-8 / sqrt(3) at most each, added up) and what norms divide by; fp32 sums of a thousand terms."""
+    w = {k: (grid(a, dt) if k in ("table", "w1", "w2") else grid(a, "f32")) for k, a in model_weights(1).items()}
+    rng = np.random.default_rng(n)
+    tok = np.minimum(rng.geometric(0.05, n) - 1, VOCAB - 1)
+    dlogits = grid(rng.standard_normal((n, VOCAB)) / n, dt)
+    logits, g = oracle_step(w, tok, dlogits)
+    names = sorted(g)
+    norm, factor, want = to.grad_clip([g[k] for k in names], 0.3 * float(np.sqrt(sum((v**2).sum() for v in g.values()))))
+    step = torch.tensor([DROPS[0][3]], dtype=torch.int32, device=DEV)
+    got = Model(sol, w, dt, step).step(torch.from_numpy(tok).to(DEV), dev(dlogits, dt), 0.3 * norm)
+    tol = 10 * HALF["bf16"] / np.sqrt(3) if dt == "bf16" else 2e-5
+    assert abs(float(got[1]) / norm - 1) <= tol
+    for name, v, t in zip(["logits"] + names, (got[0],) + got[2:], [logits] + want):
+        assert np.linalg.norm(host(v) - t) <= tol * np.linalg.norm(t), name
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_a_captured_training_step(sol, dt):
+    """The whole step in a graph: tokens, gradients and dropout's step change between the replays."""
+    rng = np.random.default_rng(2)
+    step = torch.zeros(1, dtype=torch.int32, device=DEV)
+    m = Model(sol, model_weights(2), dt, step)
+    tokens = torch.from_numpy(rng.integers(0, VOCAB, 300)).to(DEV)
+    dlogits = dev(rng.standard_normal((300, VOCAB)) / 300, dt)
+    m.step(tokens, dlogits, 0.01)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = m.step(tokens, dlogits, 0.01)
+    for i in (0, 3, 3, 9):
+        step.fill_(i)
+        tokens.add_(i).remainder_(VOCAB)
+        want = [t.clone() for t in m.step(tokens, dlogits, 0.01)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, out)), i
+
+
+# ---- sizes that 32 bits do not hold --------------------------------------------------------------------------------
+def test_rows_behind_2_31_elements(sol):
+    """Views of one wide tensor of 2.3e9 elements give the bits that dense tensors give."""
+    rows, pitch, cols = 70000, 32768, 600
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    wide = torch.full((rows, pitch), float("nan"), dtype=torch.bfloat16, device=DEV)
+    x, dy, out = (wide[:, at:at + cols] for at in (0, 1024, 32000))
+    for t in (x, dy):
+        t.copy_(torch.randn((rows, cols), generator=gen, device=DEV))
+    gamma = torch.randn(cols, generator=gen, device=DEV)
+    y, mean, rstd = sol.sol_layer_norm(x, gamma, want_stats=True, out=out)
+    want, wm, wr = sol.sol_layer_norm(x.contiguous(), gamma, want_stats=True)
+    assert torch.equal(y, want) and torch.equal(mean, wm) and torch.equal(rstd, wr)
+    got = sol.sol_layer_norm_backward(dy, x, mean, rstd, gamma)
+    assert all(torch.equal(a, b) for a, b in zip(got, sol.sol_layer_norm_backward(dy.contiguous(), x.contiguous(), mean, rstd, gamma)))
+    assert torch.isnan(wide[:, 1024 + cols:32000]).all()
+    # a table with rows behind 2^31 elements: read, and its gradient of a dense 2^31 and more
+    tokens = torch.randint(0, rows, (500,), generator=gen, device=DEV)
+    tokens[:3] = rows - 1
+    assert torch.equal(sol.sol_embedding(tokens, out, out=x[:500]), want[tokens])
+    del wide, x, dy, out, y, got
+    torch.cuda.empty_cache()
+    g = torch.randint(-2, 3, (500, pitch), generator=gen, device=DEV).bfloat16()
+    d = sol.sol_embedding_backward(g, tokens, rows)
+    used = torch.unique(tokens)
+    want = torch.zeros((rows, pitch), device=DEV).index_add_(0, tokens, g.float())
+    assert torch.equal(d[used].float(), want[used]) and int(torch.count_nonzero(d)) == int(torch.count_nonzero(want))
+    del d, want
+    torch.cuda.empty_cache()
+
+
+def test_a_gradient_of_more_than_2_32_elements(sol):
+    n = 2**32 + 4099
+    t = torch.ones(n, dtype=torch.bfloat16, device=DEV)
+    t[-1] = 3
+    norm = float(np.sqrt(n + 8.0))
+    assert abs(float(sol.sol_grad_clip([t, torch.zeros(3, device=DEV)], norm / 2)) - norm) <= U * norm * 1.01
+    assert float(t[-1]) == 1.5 and int((t[:-1] == 0.5).sum()) == n - 1
+    del t
+    torch.cuda.empty_cache()
+
+
+# ---- refusals of the binding ---------------------------------------------------------------------------------------
+def test_refusals_of_the_binding(sol):
+    x, v, r = torch.zeros((4, 32), device=DEV), torch.zeros(32, device=DEV), torch.ones(4, device=DEV)
+    tok = torch.zeros(4, dtype=torch.int64, device=DEV)
+    bad = [lambda: sol.sol_layer_norm(x.t()[:, ::2], v), lambda: sol.sol_layer_norm(x.double(), v), lambda: sol.sol_layer_norm(x, v[:31]), lambda: sol.sol_layer_norm(x, v.bfloat16()), lambda: sol.sol_layer_norm(x, v, v[::1].cpu()),
+           lambda: sol.sol_layer_norm(x[:1].expand(4, 32), v), lambda: sol.sol_layer_norm(x, v, out=x[:3]), lambda: sol.sol_layer_norm(x, v, out=x.bfloat16()),
+           lambda: sol.sol_layer_norm_backward(x[:3], x, r, r), lambda: sol.sol_layer_norm_backward(x, x, r[:3], r), lambda: sol.sol_layer_norm_backward(x, x, r, r.double()), lambda: sol.sol_layer_norm_backward(x, x, r, r, residual=x[:, :31]),
+           lambda: sol.sol_layer_norm_backward(x.bfloat16(), x, r, r),
+           lambda: sol.sol_embedding(tok.float(), x), lambda: sol.sol_embedding(tok.cpu(), x), lambda: sol.sol_embedding(tok.expand(3, 4).t(), x), lambda: sol.sol_embedding(tok, x.half()), lambda: sol.sol_embedding(tok, x, out=x[:3].clone()),
+           lambda: sol.sol_embedding(tok, x, pad=2**32), lambda: sol.sol_embedding(tok, x, out=x.bfloat16()),
+           lambda: sol.sol_embedding_backward(x[:3], tok, 9), lambda: sol.sol_embedding_backward(x, tok, 9, dtable_dtype=torch.float16), lambda: sol.sol_embedding_backward(x, tok, 9, add_to=torch.zeros((8, 32), device=DEV)),
+           lambda: sol.sol_embedding_backward(x, tok, 0), lambda: sol.sol_embedding_backward(x, tok, 2**32 + 5), lambda: sol.sol_embedding_backward(x.view(2, 2, 32), tok, 9),
+           lambda: sol.sol_embedding_backward(x, tok, 9, dtable_dtype=torch.bfloat16, add_to=torch.zeros((9, 32), device=DEV)),
+           lambda: sol.sol_grad_norm([x, x.cpu()]), lambda: sol.sol_grad_norm([x.double()]), lambda: sol.sol_grad_norm([x.t()]), lambda: sol.sol_grad_clip([x], 1.0, out=[]), lambda: sol.sol_grad_clip([x], 1.0, out=[v]),
+           lambda: sol.sol_grad_clip([], 1.0)]
+    for i, f in enumerate(bad):
+        with pytest.raises(ValueError):
+            f()
+            pytest.fail(f"call {i} was not refused")
+    for f, status in ((lambda: sol.sol_layer_norm(x, eps=0.0), 2), (lambda: sol.sol_embedding_backward(x, tok, 9, dtable_dtype=torch.bfloat16), 3), (lambda: sol.sol_grad_clip([x], -1.0), 2),
+                      (lambda: sol.sol_grad_clip([x, x], 1.0), 6), (lambda: sol.sol_grad_clip([x, v], 1.0, out=[x, x[0]]), 6), (lambda: sol.sol_embedding(tok, x, scale=float("nan")), 2)):
+        with pytest.raises(sol.SolError) as e:
+            f()
+        assert e.value.status == status
