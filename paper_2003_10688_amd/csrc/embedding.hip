@@ -26,9 +26,9 @@ struct EmbedArgs {
 };
 template <typename T, typename I> __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a) {
     const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1), slot = threadIdx.x >> a.lanes_log2;
-    const int c = ((int)blockIdx.y * 64 + lane) * 8, nv = min(8, a.cols - c);
+    const int c = ((int)blockIdx.x * 64 + lane) * 8, nv = min(8, a.cols - c);
     if (nv <= 0) return;
-    for (long i = (long)blockIdx.x * (256 >> a.lanes_log2) + slot; i < a.n; i += (long)gridDim.x * (256 >> a.lanes_log2)) {
+    for (long i = (long)blockIdx.y * (256 >> a.lanes_log2) + slot; i < a.n; i += (long)gridDim.y * (256 >> a.lanes_log2)) {
         const I tok = static_cast<const I *>(a.tokens)[i];
         float v[8];
         if (tok != (I)a.pad && tok >= 0 && tok < (I)a.vocab) {
@@ -45,134 +45,221 @@ template <typename T, typename I> __global__ void __launch_bounds__(256) embed_k
 }
 
 // ---- the gradient's first half: positions sorted by token --------------------------------------------------------------------
-// Every workgroup owns a range of the table's rows and reads all tokens, twice: once to count those of its rows and those in front of them, once to write the positions of
-// its rows' tokens, in order, behind each other.  So it takes one launch, without a word between the workgroups.  The tokens are read from L2.
-constexpr int INDEX_THREADS = 1024, INDEX_EACH = 16, INDEX_TILE = INDEX_THREADS * INDEX_EACH, INDEX_ROWS = 8192, INDEX_GROUPS = 256;
+// The tokens' order is that of (v mod G, v / G) for G workgroups: each owns the rows of one residue, so that neighbouring rows, which frequent tokens often are, fall to different
+// ones, and reads all tokens.  It counts those of each of its rows and those of the residues in front, keeps what is its own in a list, in order, and writes the positions
+// of its rows' tokens behind each other.  So it takes one launch, without a word between the workgroups.  The tokens are read from L2, a second time where the list does not hold
+// a workgroup's share.
+constexpr int INDEX_THREADS = 1024, INDEX_EACH = 16, INDEX_TILE = INDEX_THREADS * INDEX_EACH, INDEX_ROWS = 1024, INDEX_GROUPS = 256, INDEX_WAVES = INDEX_THREADS / 64;
+constexpr int LIST_BITS = 22;   // of a position in a list's entry, the row's 10 above them
 constexpr int RUN = 64;         // longer runs of one token are summed in parts of the sorted order, RUN positions each
 
 struct IndexArgs {
     const void *tokens;
-    int n, vocab, pad, rows;    // rows: of the table, per workgroup
-    int *start, *order, *sorted;    // [vocab + 1], [n], [n]
+    int n, vocab, pad, rows, log2;  // 2^log2 workgroups, `rows` of the table each
+    int *start, *order, *sorted;    // [places + 1], [n], [n]: a row's place is (v mod G) * rows + v / G
 };
 
-// 16 neighbouring tokens; -1 where there is none or it has no row
-template <typename I> __device__ __forceinline__ void load_tokens(const IndexArgs &a, int at, int t[INDEX_EACH]) {
-    const I *p = static_cast<const I *>(a.tokens) + at;
-    constexpr int PER = 16 / sizeof(I);
-    if (at + INDEX_EACH <= a.n) {
-        uint4 raw[INDEX_EACH / PER];
+// A tile is PIECES pieces of 4 neighbouring tokens a thread: lanes next to each other read next to each other.  t: the tokens, where[j]: the lanes of the wave whose token j is this workgroup's own.
+// Returns how many of the wave's belong to the residues in front.  What a token costs here is what the launch costs, since every workgroup looks at every token: six vector instructions,
+// counts and prefixes come from the masks.
+constexpr int PIECES = INDEX_EACH / 4;
+typedef unsigned long long lanes_t;
+template <typename I> __device__ __forceinline__ int look_at_tokens(const IndexArgs &a, int base, uint32_t t[INDEX_EACH], lanes_t where[INDEX_EACH]) {
+    const I *p = static_cast<const I *>(a.tokens);
+    I raw[INDEX_EACH];
 #pragma unroll
-        for (int q = 0; q < INDEX_EACH / PER; q++) raw[q] = reinterpret_cast<const uint4 *>(p)[q];
+    for (int q = 0; q < PIECES; q++) {
+        const int at = base + q * (INDEX_THREADS * 4) + (int)threadIdx.x * 4;
+        if (at + 4 <= a.n) {
 #pragma unroll
-        for (int j = 0; j < INDEX_EACH; j++) {
-            const I tok = reinterpret_cast<const I *>(raw)[j];
-            t[j] = tok != (I)a.pad && tok >= 0 && tok < (I)a.vocab ? (int)tok : -1;
-        }
-    } else {
+            for (int k = 0; k < (int)sizeof(I) / 4; k++) reinterpret_cast<uint4 *>(raw + q * 4)[k] = reinterpret_cast<const uint4 *>(p + at)[k];
+        } else {
 #pragma unroll
-        for (int j = 0; j < INDEX_EACH; j++) {
-            const I tok = at + j < a.n ? p[j] : (I)-1;
-            t[j] = tok != (I)a.pad && tok >= 0 && tok < (I)a.vocab ? (int)tok : -1;
+            for (int j = 0; j < 4; j++) raw[q * 4 + j] = at + j < a.n ? p[at + j] : (I)-1;
         }
     }
+    int less = 0;
+    const uint32_t mine = blockIdx.x, mask = (1u << a.log2) - 1, vocab = (uint32_t)a.vocab, pad = (uint32_t)a.pad;
+#pragma unroll
+    for (int j = 0; j < INDEX_EACH; j++) {
+        t[j] = (uint32_t)raw[j];
+        bool row = t[j] < vocab && t[j] != pad;         // a negative one is not: vocab has 25 bits at most
+        if constexpr (sizeof(I) == 8) row = row && (raw[j] >> 32) == 0;
+        const uint32_t res = row ? t[j] & mask : 0xffffffffu;
+        where[j] = __ballot(res == mine);
+        less += __popcll(__ballot(res < mine));
+    }
+    return less;
 }
+__device__ __forceinline__ int place_in_tile(int j) { return (j >> 2) * (INDEX_THREADS * 4) + (int)threadIdx.x * 4 + (j & 3); }
 
-__device__ __forceinline__ int wave_scan(int v) {       // sum over the lanes up to this one
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(v, d);
-        v += lane >= d ? o : 0;
-    }
+// Sum over the lanes up to this one: rows of 16 by shifts, then the rows in front through their last lanes
+__device__ __forceinline__ uint32_t wave_scan(uint32_t v) {
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xf, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xa, 0xf, false);
+    v += (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xc, 0xf, false);
     return v;
 }
-// Sum over the threads in front of this one; *total: over all.  One set of slots: a barrier in front and one behind the writing.
-__device__ __forceinline__ int block_scan(int v, int *slots, int *total) {
-    const int inc = wave_scan(v), w = threadIdx.x >> 6;
+// Two sums over the waves in front of this one of what each wave has; *total: over all.  One set of slots: a barrier in front and one behind the writing.
+__device__ __forceinline__ uint2 sum_waves(uint2 v, uint2 *slots, uint2 *total) {
+    const int w = threadIdx.x >> 6;
     __syncthreads();
-    if ((threadIdx.x & 63) == 63) slots[w] = inc;
+    if ((threadIdx.x & 63) == 63) slots[w] = v;
     __syncthreads();
-    int before = 0, all = 0;
+    uint2 before = make_uint2(0, 0), all = make_uint2(0, 0);
 #pragma unroll
-    for (int q = 0; q < INDEX_THREADS / 64; q++) {
-        const int s = slots[q];
-        before += q < w ? s : 0;
-        all += s;
+    for (int q = 0; q < INDEX_WAVES; q++) {
+        const uint2 s = slots[q];
+        before.x += q < w ? s.x : 0;
+        before.y += q < w ? s.y : 0;
+        all.x += s.x;
+        all.y += s.y;
     }
     *total = all;
-    return before + inc - v;
+    return before;
+}
+
+struct IndexShared {
+    uint32_t list[INDEX_TILE];                      // this residue's tokens, in order: row << LIST_BITS | position behind the list's base
+    uint32_t count[INDEX_WAVES][INDEX_ROWS];        // of the rows in each wave's part of the list; then where each wave's next position of a row goes
+    uint32_t next[INDEX_ROWS];                      // of all rows so far; then where the next position of each row goes
+    uint2 slots[INDEX_WAVES];
+};
+
+// Appends a tile's tokens of this residue to the list, which has `have` entries, unless it would not hold them.  Returns how many there are then.
+__device__ __forceinline__ int index_append(const IndexArgs &a, IndexShared &s, int behind, const uint32_t t[INDEX_EACH], const lanes_t where[INDEX_EACH], int have) {
+    static_assert(PIECES == 4, "two counts in a word, two words");
+    uint32_t found[2];                  // the pieces' counts, two in a word: a piece has 4096 tokens
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        int n[2] = {0, 0};
+#pragma unroll
+        for (int j = 0; j < 8; j++) n[j >> 2] += __popcll(where[8 * k + j]);
+        found[k] = (uint32_t)n[0] | (uint32_t)n[1] << 16;
+    }
+    uint2 all;
+    const uint2 before = sum_waves(make_uint2(found[0], found[1]), s.slots, &all);      // behind its first barrier the list's last readers are through
+    const int many = (int)((all.x & 0xffff) + (all.x >> 16) + (all.y & 0xffff) + (all.y >> 16));
+    if ((found[0] | found[1]) && have + many <= INDEX_TILE) {
+        const uint32_t piece[PIECES] = {all.x & 0xffff, all.x >> 16, all.y & 0xffff, 0};
+        const uint32_t wave[PIECES] = {before.x & 0xffff, before.x >> 16, before.y & 0xffff, before.y >> 16};
+        uint32_t first = (uint32_t)have;
+#pragma unroll
+        for (int q = 0; q < PIECES; q++) {
+            if (where[4 * q] | where[4 * q + 1] | where[4 * q + 2] | where[4 * q + 3]) {
+                uint32_t to = first + wave[q];          // + those of the lanes in front
+#pragma unroll
+                for (int j = 0; j < 4; j++) to = __builtin_amdgcn_mbcnt_hi((uint32_t)(where[4 * q + j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)where[4 * q + j], to));
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    if (where[4 * q + j] >> (threadIdx.x & 63) & 1) s.list[to++] = (t[4 * q + j] >> a.log2) << LIST_BITS | (uint32_t)(behind + place_in_tile(4 * q + j));
+            }
+            first += piece[q];
+        }
+    }
+    return have + many;
+}
+
+// The lanes whose row is this lane's, of those that have one
+__device__ __forceinline__ lanes_t same_row(uint32_t row, bool has, int bits) {
+    lanes_t same = __ballot(has);
+    if (__ballot(has && row != (uint32_t)__builtin_amdgcn_readfirstlane((int)row)) == 0) return same;       // a frequent token's; lane 0 has one
+    for (int b = 0; b < bits; b++) {
+        const lanes_t one = __ballot(has && (row >> b & 1));
+        same &= row >> b & 1 ? one : ~one;
+    }
+    return same;
+}
+// Each wave takes a part of the list, 64 entries at a time, in order
+template <typename F> __device__ __forceinline__ void index_part(const IndexShared &s, int total, int bits, F f) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, per = (total + INDEX_THREADS - 1) / INDEX_THREADS * 64, end = min(total, (w + 1) * per);
+    for (int i = w * per; i < end; i += 64) {
+        const bool has = i + lane < end;
+        const uint32_t e = has ? s.list[i + lane] : 0u;
+        f(w, e, has, same_row(e >> LIST_BITS, has, bits));
+    }
+}
+// count[w][r]: how many entries of row r wave w's part has.  Ends with a barrier.
+__device__ __forceinline__ void index_count(const IndexArgs &a, IndexShared &s, int total, int bits) {
+    if ((int)threadIdx.x < a.rows)
+        for (int w = 0; w < INDEX_WAVES; w++) s.count[w][threadIdx.x] = 0;
+    __syncthreads();
+    index_part(s, total, bits, [&](int w, uint32_t e, bool has, lanes_t same) {
+        if (has && (int)__ffsll(same) - 1 == (int)(threadIdx.x & 63)) s.count[w][e >> LIST_BITS] += (uint32_t)__popcll(same);
+    });
+    __syncthreads();
+}
+// Writes the positions of the list, whose counts are there, from next[] on, which moves behind them
+__device__ __forceinline__ void index_place(const IndexArgs &a, IndexShared &s, int total, int bits, int base) {
+    const int r = threadIdx.x;
+    if (r < a.rows) {
+        uint32_t at = s.next[r];
+        for (int w = 0; w < INDEX_WAVES; w++) {
+            const uint32_t k = s.count[w][r];
+            s.count[w][r] = at;
+            at += k;
+        }
+        s.next[r] = at;
+    }
+    __syncthreads();
+    index_part(s, total, bits, [&](int w, uint32_t e, bool has, lanes_t same) {
+        const uint32_t row = e >> LIST_BITS, lane = threadIdx.x & 63;
+        const uint32_t first = has ? s.count[w][row] : 0u;
+        if (has) {
+            const uint32_t dst = first + (uint32_t)__popcll(same & ((1ull << lane) - 1));
+            a.order[dst] = base + (int)(e & ((1u << LIST_BITS) - 1));
+            a.sorted[dst] = (int)blockIdx.x * a.rows + (int)row;
+            if ((uint32_t)__ffsll(same) - 1 == lane) s.count[w][row] = first + (uint32_t)__popcll(same);
+        }
+    });
 }
 
 template <typename I> __global__ void __launch_bounds__(INDEX_THREADS) embed_index_kernel(const IndexArgs a) {
-    __shared__ uint32_t next[INDEX_ROWS];               // counts, then where the next position of each row goes
-    __shared__ uint32_t list[INDEX_TILE];               // a tile's tokens of this range: row << 14 | place in the tile
-    __shared__ int slots[INDEX_THREADS / 64];
-    const int lo = (int)blockIdx.x * a.rows, hi = min(a.vocab, lo + a.rows), mine = hi - lo;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    for (int r = threadIdx.x; r < a.rows; r += INDEX_THREADS) next[r] = 0;
+    __shared__ IndexShared s;
+    const int r = (int)threadIdx.x, bits = 32 - __clz(a.rows - 1);      // 0 for one row
+    s.next[r] = 0;
+    uint32_t t[INDEX_EACH], less = 0;
+    lanes_t where[INDEX_EACH];
+    int have = 0;
+    bool whole = a.n <= 1 << LIST_BITS;                 // the list has all of this residue, positions from the first token on
+    auto add_counts = [&]() {
+        index_count(a, s, have, bits);
+        if (r < a.rows)
+            for (int w = 0; w < INDEX_WAVES; w++) s.next[r] += s.count[w][r];
+    };
+    for (int base = 0; base < a.n; base += INDEX_TILE) {
+        less += (uint32_t)look_at_tokens<I>(a, base, t, where);
+        const int then = index_append(a, s, whole ? base : 0, t, where, have);
+        if (then <= INDEX_TILE) {
+            have = then;
+            continue;
+        }
+        whole = false;
+        add_counts();
+        have = index_append(a, s, 0, t, where, 0);      // its barrier is behind the last reading of the list
+    }
     __syncthreads();
-    int t[INDEX_EACH], less = 0;
-    for (int base = 0; base < a.n; base += INDEX_TILE) {
-        const int at = base + threadIdx.x * INDEX_EACH;
-        if (at >= a.n) continue;
-        load_tokens<I>(a, at, t);
-#pragma unroll
-        for (int j = 0; j < INDEX_EACH; j++) {
-            less += t[j] >= 0 && t[j] < lo ? 1 : 0;
-            if (t[j] >= lo && t[j] < hi) atomicAdd(&next[t[j] - lo], 1u);
-        }
+    add_counts();
+    uint2 all;
+    const uint32_t count = s.next[r], up_to = wave_scan(count);      // next[r] is this thread's own
+    const uint2 before = sum_waves(make_uint2((uint32_t)__builtin_amdgcn_readlane((int)up_to, 63), less), s.slots, &all);
+    const uint32_t at = all.y + before.x + up_to - count;
+    s.next[r] = at;
+    if (r < a.rows) a.start[(int)blockIdx.x * a.rows + r] = (int)at;
+    if (blockIdx.x == gridDim.x - 1 && r == 0) a.start[(int)gridDim.x * a.rows] = (int)(all.x + all.y);
+    if (whole) {
+        index_place(a, s, have, bits, 0);
+        return;
     }
-    int before;
-    block_scan(less, slots, &before);                   // its barriers are behind the counts too
-    const int each = (a.rows + INDEX_THREADS - 1) / INDEX_THREADS, r0 = threadIdx.x * each, r1 = min(mine, r0 + each);
-    int sum = 0, here;
-    for (int r = r0; r < r1; r++) sum += (int)next[r];
-    int at = before + block_scan(sum, slots, &here);
-    for (int r = r0; r < r1; r++) {
-        const int k = (int)next[r];
-        next[r] = (uint32_t)at;
-        a.start[lo + r] = at;
-        at += k;
-    }
-    if (hi == a.vocab && threadIdx.x == 0) a.start[a.vocab] = before + here;
-    if (here == 0) return;
     for (int base = 0; base < a.n; base += INDEX_TILE) {
-        const int at0 = base + threadIdx.x * INDEX_EACH;
-        int found = 0;
-        if (at0 < a.n) {
-            load_tokens<I>(a, at0, t);
-#pragma unroll
-            for (int j = 0; j < INDEX_EACH; j++) found += t[j] >= lo && t[j] < hi ? 1 : 0;
-        }
-        int total;
-        int to = block_scan(found, slots, &total);      // its first barrier: next[] is there, and the list's last readers are through
-        if (found) {
-#pragma unroll
-            for (int j = 0; j < INDEX_EACH; j++)
-                if (t[j] >= lo && t[j] < hi) list[to++] = (uint32_t)(t[j] - lo) << 14 | (uint32_t)(threadIdx.x * INDEX_EACH + j);
-        }
+        look_at_tokens<I>(a, base, t, where);
+        have = index_append(a, s, 0, t, where, 0);
         __syncthreads();
-        // each wave takes the rows of one residue, 64 entries at a time; equal rows among them by one ballot per different row
-        for (int i = 0; i < total; i += 64) {
-            const uint32_t e = i + lane < total ? list[i + lane] : 0xffffffffu;
-            const int row = (int)(e >> 14);
-            const bool own = e != 0xffffffffu && (row & 15) == w;
-            unsigned long long left = __ballot(own);
-            while (left) {
-                const int first = __ffsll((unsigned long long)left) - 1, r = __builtin_amdgcn_readlane(row, first);
-                const unsigned long long same = __ballot(own && row == r);
-                uint32_t dst = 0;
-                if (lane == first) dst = atomicAdd(&next[r], (uint32_t)__popcll(same));
-                dst = (uint32_t)__builtin_amdgcn_readlane((int)dst, first);
-                if (own && row == r) {
-                    dst += (uint32_t)__popcll(same & ((1ull << lane) - 1));
-                    a.order[dst] = base + (int)(e & 16383u);
-                    a.sorted[dst] = lo + r;
-                }
-                left &= ~same;
-            }
-        }
+        index_count(a, s, have, bits);
+        index_place(a, s, have, bits, base);
     }
 }
 
@@ -183,17 +270,53 @@ struct GatherArgs {
     const int *start, *order, *sorted;
     float *part;                // [windows][2][cols]: sums of the parts of long runs that a window of RUN positions holds, of the run that reaches in first, of the one that leaves it second
     long ldy;
-    int n, vocab, cols, windows, accumulate, lanes_log2;
+    int vocab, cols, windows, accumulate, lanes_log2;
+    int rows, log2, places;         // as the index has them
     float scale;
+    FastDiv by_rows;
+};
+__device__ __forceinline__ int row_of_place(const GatherArgs &a, int place) {
+    uint32_t q, r;
+    a.by_rows.divmod((uint32_t)place, q, r);
+    return (int)(r << a.log2 | q);
+}
+
+// A lane's 8 columns of a slab of 8 * lanes: two quads half a slab apart where fp32 is written, so that a wave's store covers whole lines, else 8 neighbours.
+template <typename T, typename TO> struct Columns {
+    static constexpr bool QUADS = sizeof(TO) == 4;
+    int c, apart, nv0, nv1;
+    __device__ __forceinline__ Columns(int slab, int lane, int lanes, int cols) {
+        c = slab * 512 + lane * (QUADS ? 4 : 8);
+        apart = QUADS ? lanes * 4 : 0;
+        nv0 = cols - c;
+        nv1 = cols - c - apart;
+    }
+    __device__ __forceinline__ bool none() const { return nv0 <= 0; }
+    template <typename X> __device__ __forceinline__ void load(const X *p, float v[8]) const {
+        if constexpr (QUADS) {
+            load4_any<X>(p + c, v, nv0);
+            load4_any<X>(p + c + apart, v + 4, nv1);
+        } else {
+            load8_any<X>(p + c, v, nv0);
+        }
+    }
+    template <typename X> __device__ __forceinline__ void store(X *p, const float v[8]) const {
+        if constexpr (QUADS) {
+            store4_any<X>(p + c, v, nv0);
+            store4_any<X>(p + c + apart, v + 4, nv1);
+        } else {
+            store8_any<X>(p + c, v, nv0);
+        }
+    }
 };
 
 // acc += the rows order[b .. e), in that order; eight loads under way at a time
-template <typename T> __device__ __forceinline__ void sum_rows(const GatherArgs &a, int b, int e, int c, int nv, float acc[8]) {
-    const T *dy = static_cast<const T *>(a.dy) + c;
+template <typename T, typename C> __device__ __forceinline__ void sum_rows(const GatherArgs &a, const C &cl, int b, int e, float acc[8]) {
+    const T *dy = static_cast<const T *>(a.dy);
     for (; b + 8 <= e; b += 8) {
         float v[8][8];
 #pragma unroll
-        for (int u = 0; u < 8; u++) load8_any<T>(dy + (long)a.order[b + u] * a.ldy, v[u], nv);
+        for (int u = 0; u < 8; u++) cl.load(dy + (long)a.order[b + u] * a.ldy, v[u]);
 #pragma unroll
         for (int u = 0; u < 8; u++)
 #pragma unroll
@@ -201,64 +324,148 @@ template <typename T> __device__ __forceinline__ void sum_rows(const GatherArgs 
     }
     for (; b < e; b++) {
         float v[8];
-        load8_any<T>(dy + (long)a.order[b] * a.ldy, v, nv);
+        cl.load(dy + (long)a.order[b] * a.ldy, v);
 #pragma unroll
         for (int k = 0; k < 8; k++) acc[k] += v[k];
     }
 }
 
-template <typename TO> __device__ __forceinline__ void put_row(const GatherArgs &a, int v, int c, int nv, float acc[8]) {
-    TO *out = static_cast<TO *>(a.out) + (size_t)v * a.cols + c;
+template <typename TO, typename C> __device__ __forceinline__ void put_row(const GatherArgs &a, const C &cl, int v, float acc[8]) {
+    TO *out = static_cast<TO *>(a.out) + (size_t)v * a.cols;
     float old[8];
-    if (a.accumulate) load8_any<TO>(out, old, nv);
+    if (a.accumulate) cl.load(out, old);
 #pragma unroll
     for (int k = 0; k < 8; k++) acc[k] = a.accumulate ? acc[k] * a.scale + old[k] : acc[k] * a.scale;
-    store8_any<TO>(out, acc, nv);
+    cl.store(out, acc);
 }
 
-// Items: the parts of long runs in each window, two a window, then the table's rows
+// Items: the parts of long runs in each window, two a window, then the table's rows.  A part of a long run:
+struct Part { int place, b, e; };
+__device__ __forceinline__ bool window_part(const GatherArgs &a, int item, Part *q) {
+    const int used = a.start[a.places], w0 = (item >> 1) * RUN, w1 = min(used, w0 + RUN);
+    if (w0 >= w1) return false;
+    const int first = a.sorted[w0], last = a.sorted[w1 - 1];
+    if ((item & 1) && last == first) return false;
+    const int p = item & 1 ? last : first, b = a.start[p], e = a.start[p + 1];
+    if (e - b <= RUN) return false;
+    *q = Part{p, max(b, w0), min(e, w1)};
+    return true;
+}
+__device__ __forceinline__ int place_of_row(const GatherArgs &a, int v) { return (v & ((1 << a.log2) - 1)) * a.rows + (v >> a.log2); }
+
+// Narrow tables: a row of the table for 8 to 32 lanes
 template <typename T, typename TO> __global__ void __launch_bounds__(256) embed_gather_kernel(const GatherArgs a) {
-    const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1), slot = threadIdx.x >> a.lanes_log2;
-    const long item = (long)blockIdx.x * (256 >> a.lanes_log2) + slot;
-    const int c = ((int)blockIdx.y * 64 + lane) * 8, nv = min(8, a.cols - c);
-    if (item >= (long)a.vocab + 2 * a.windows || nv <= 0) return;
+    const int log2 = a.lanes_log2, lane = threadIdx.x & ((1 << log2) - 1);
+    const long item = (long)blockIdx.x * (256 >> log2) + (threadIdx.x >> log2);
+    const Columns<T, TO> cl(0, lane, 1 << log2, a.cols);
+    if (cl.none()) return;
     float acc[8];
 #pragma unroll
     for (int k = 0; k < 8; k++) acc[k] = 0.f;
-    if (item >= 2 * a.windows) {
-        const int v = (int)(item - 2 * a.windows), b = a.start[v], e = a.start[v + 1];
-        if (e - b > RUN || (a.accumulate && e == b)) return;
-        sum_rows<T>(a, b, e, c, nv, acc);
-        put_row<TO>(a, v, c, nv, acc);
+    if (item < 2 * a.windows) {
+        Part q;
+        if (!window_part(a, (int)item, &q)) return;
+        sum_rows<T>(a, cl, q.b, q.e, acc);
+        cl.store(a.part + (size_t)item * a.cols, acc);
         return;
     }
-    const int win = (int)(item >> 1), used = a.start[a.vocab], w0 = win * RUN, w1 = min(used, w0 + RUN);
-    if (w0 >= w1) return;
-    const int first = a.sorted[w0], last = a.sorted[w1 - 1];
-    if ((item & 1) && last == first) return;
-    const int v = item & 1 ? last : first, b = a.start[v], e = a.start[v + 1];
-    if (e - b <= RUN) return;
-    sum_rows<T>(a, max(b, w0), min(e, w1), c, nv, acc);
-    store8_any<float>(a.part + (size_t)item * a.cols + c, acc, nv);
+    if (item - 2 * a.windows >= a.vocab) return;
+    const int v = (int)(item - 2 * a.windows), p = place_of_row(a, v), b = a.start[p], e = a.start[p + 1];
+    if (e - b > RUN || (a.accumulate && e == b)) return;
+    sum_rows<T>(a, cl, b, e, acc);
+    put_row<TO>(a, cl, v, acc);
+}
+
+// Wider ones: a wave takes PIECES * 64 * W columns of a row.  Three round trips to memory: where its run is, the positions in it (a lane each), and FLIGHT of the gradient's rows at a time.
+template <typename T, typename TO, int W, int PIECES> __device__ __forceinline__ void wide_item(const GatherArgs &a, int item, int c0) {
+    constexpr int FLIGHT = 64 / (W * PIECES);
+    const int lane = threadIdx.x & 63;
+    const bool window = item < 2 * a.windows;
+    Part q;
+    if (window) {
+        if (!window_part(a, item, &q)) return;
+    } else {
+        const int p = place_of_row(a, item - 2 * a.windows);
+        q = Part{p, a.start[p], a.start[p + 1]};
+        if (q.e - q.b > RUN || (a.accumulate && q.e == q.b)) return;
+    }
+    const T *dy = static_cast<const T *>(a.dy) + c0;
+    const int nv = a.cols - c0, many = q.e - q.b, order = lane < many ? a.order[q.b + lane] : 0;        // RUN of them at most
+    float acc[PIECES][W];
+#pragma unroll
+    for (int i = 0; i < PIECES; i++)
+#pragma unroll
+        for (int k = 0; k < W; k++) acc[i][k] = 0.f;
+    for (int j = 0; j < many; j += FLIGHT) {
+        RawPiece<T, W> raw[FLIGHT][PIECES];
+#pragma unroll
+        for (int u = 0; u < FLIGHT; u++) {
+            if (j + u < many) {
+                const T *p = dy + (long)__builtin_amdgcn_readlane(order, j + u) * a.ldy;
+#pragma unroll
+                for (int i = 0; i < PIECES; i++) raw[u][i].load(p + i * 64 * W, nv - i * 64 * W);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < FLIGHT; u++) {
+            if (j + u < many) {
+#pragma unroll
+                for (int i = 0; i < PIECES; i++)
+#pragma unroll
+                    for (int k = 0; k < W; k++) acc[i][k] += raw[u][i].get(k);
+            }
+        }
+    }
+    if (window) {
+        float *part = a.part + (size_t)item * a.cols + c0;
+#pragma unroll
+        for (int i = 0; i < PIECES; i++) store_piece<float, W>(part + i * 64 * W, acc[i], nv - i * 64 * W);
+        return;
+    }
+    TO *out = static_cast<TO *>(a.out) + (size_t)(item - 2 * a.windows) * a.cols + c0;
+#pragma unroll
+    for (int i = 0; i < PIECES; i++) {
+        RawPiece<TO, W> old;
+        if (a.accumulate) old.load(out + i * 64 * W, nv - i * 64 * W);
+#pragma unroll
+        for (int k = 0; k < W; k++) acc[i][k] = a.accumulate ? acc[i][k] * a.scale + old.get(k) : acc[i][k] * a.scale;
+        store_piece<TO, W>(out + i * 64 * W, acc[i], nv - i * 64 * W);
+    }
+}
+// Slabs of columns vary fastest: workgroups that run together then write whole rows, not the same part of every row, whose addresses would fall on a few of the memory's channels.
+template <typename T, typename TO, int W, int PIECES> __global__ void __launch_bounds__(256) embed_wide_kernel(const GatherArgs a, int items) {
+    const int c0 = (int)blockIdx.x * (PIECES * 64 * W) + (threadIdx.x & 63) * W;
+    for (int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += (int)gridDim.y * 4) wide_item<T, TO, W, PIECES>(a, item, c0);
 }
 
 // A long run ends behind the window that it starts in: at most one starts in each
-template <typename TO> __global__ void __launch_bounds__(256) embed_join_kernel(const GatherArgs a) {
+template <typename T, typename TO> __global__ void __launch_bounds__(256) embed_join_kernel(const GatherArgs a) {
     const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1), slot = threadIdx.x >> a.lanes_log2;
     const long win = (long)blockIdx.x * (256 >> a.lanes_log2) + slot;
-    const int c = ((int)blockIdx.y * 64 + lane) * 8, nv = min(8, a.cols - c), used = a.start[a.vocab];
-    if (win >= a.windows || nv <= 0 || win * RUN >= used) return;
-    const int v = a.sorted[min(used, (int)win * RUN + RUN) - 1], b = a.start[v], e = a.start[v + 1];
+    const int used = a.start[a.places];
+    const Columns<T, TO> cl((int)blockIdx.y, lane, 1 << a.lanes_log2, a.cols);
+    if (win >= a.windows || cl.none() || win * RUN >= used) return;
+    const int p = a.sorted[min(used, (int)win * RUN + RUN) - 1], b = a.start[p], e = a.start[p + 1];
     if (e - b <= RUN || b / RUN != win) return;
-    float acc[8], p[8];
+    float acc[8], v[8];
+    const int last = (e - 1) / RUN;
+    cl.load(a.part + (size_t)(2 * win + (b % RUN ? 1 : 0)) * a.cols, acc);
+    int w = (int)win + 1;
+    for (; w + 7 <= last; w += 8) {
+        float u[8][8];
 #pragma unroll
-    for (int k = 0; k < 8; k++) acc[k] = 0.f;
-    for (int w = (int)win; w * RUN < e; w++) {
-        load8_any<float>(a.part + (size_t)(2 * w + (w == win && b % RUN ? 1 : 0)) * a.cols + c, p, nv);
+        for (int q = 0; q < 8; q++) cl.load(a.part + (size_t)2 * (w + q) * a.cols, u[q]);
 #pragma unroll
-        for (int k = 0; k < 8; k++) acc[k] += p[k];
+        for (int q = 0; q < 8; q++)
+#pragma unroll
+            for (int k = 0; k < 8; k++) acc[k] += u[q][k];
     }
-    put_row<TO>(a, v, c, nv, acc);
+    for (; w <= last; w++) {
+        cl.load(a.part + (size_t)2 * w * a.cols, v);
+#pragma unroll
+        for (int k = 0; k < 8; k++) acc[k] += v[k];
+    }
+    put_row<TO>(a, cl, row_of_place(a, p), acc);
 }
 
 sol_status check_embed(const sol_embedding_desc *ed, sol_embedding_desc *d) {
@@ -277,14 +484,17 @@ sol_status check_embed(const sol_embedding_desc *ed, sol_embedding_desc *d) {
 
 struct EmbedPlan {
     size_t start, order, sorted, part, bytes;
-    int windows;
+    int windows, rows, log2, places;
 };
 EmbedPlan embed_plan(const sol_embedding_desc &d) {
     EmbedPlan p{};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at = round_up(at + bytes, 256); return here; };
+    while ((1 << p.log2) < d.vocab && ((1 << p.log2) < INDEX_GROUPS || (size_t)INDEX_ROWS << p.log2 < (size_t)d.vocab)) p.log2++;
+    p.rows = ceil_div(d.vocab, 1 << p.log2);
+    p.places = p.rows << p.log2;
     p.windows = d.tokens > RUN ? ceil_div(d.tokens, RUN) : 0;       // no run is longer than the tokens are
-    p.start = take(((size_t)d.vocab + 1) * 4);
+    p.start = take(((size_t)p.places + 1) * 4);
     p.order = take((size_t)d.tokens * 4);
     p.sorted = take((size_t)d.tokens * 4);
     p.part = take((size_t)p.windows * 2 * d.cols * 4);
@@ -292,13 +502,19 @@ EmbedPlan embed_plan(const sol_embedding_desc &d) {
     return p;
 }
 
+template <typename T, typename TO, int PIECES> void launch_wide(const GatherArgs &g, hipStream_t st) {
+    constexpr int W = sizeof(TO) == 4 ? 4 : 8;      // 16 bytes of the table's gradient
+    const int items = g.vocab + 2 * g.windows;
+    hipLaunchKernelGGL((embed_wide_kernel<T, TO, W, PIECES * 8 / W>), dim3((unsigned)ceil_div(g.cols, PIECES * 512), (unsigned)min(ceil_div(items, 4), 65535)), dim3(256), 0, st, g, items);
+}
 template <typename T, typename TO> sol_status launch_gather(const GatherArgs &g, hipStream_t st) {
     const int per = 256 >> g.lanes_log2, slabs = row_slabs(g.cols);
-    const long items = (long)g.vocab + 2 * g.windows;
-    hipLaunchKernelGGL((embed_gather_kernel<T, TO>), dim3((unsigned)((items + per - 1) / per), (unsigned)slabs), dim3(256), 0, st, g);
+    if (g.lanes_log2 < 6) hipLaunchKernelGGL((embed_gather_kernel<T, TO>), dim3((unsigned)ceil_div(g.vocab + 2 * g.windows, per)), dim3(256), 0, st, g);
+    else if (g.cols <= 512) launch_wide<T, TO, 1>(g, st);
+    else launch_wide<T, TO, 2>(g, st);
     SOL_HIP(hipGetLastError());
     if (g.windows) {
-        hipLaunchKernelGGL(embed_join_kernel<TO>, dim3((unsigned)ceil_div(g.windows, per), (unsigned)slabs), dim3(256), 0, st, g);
+        hipLaunchKernelGGL((embed_join_kernel<T, TO>), dim3((unsigned)ceil_div(g.windows, per), (unsigned)slabs), dim3(256), 0, st, g);
         SOL_HIP(hipGetLastError());
     }
     return SOL_OK;
@@ -321,7 +537,7 @@ sol_status sol_embedding(const sol_embedding_desc *ed, const void *tokens, const
     hipStream_t st = (hipStream_t)stream;
     const EmbedArgs a{tokens, table, y, d.ldt, d.ldy, d.tokens, d.vocab, d.cols, d.pad, row_lanes_log2(d.cols), d.scale};
     const int per = 256 >> a.lanes_log2;
-    const dim3 grid((unsigned)min(ceil_div(d.tokens, per), 1 << 16), (unsigned)row_slabs(d.cols));
+    const dim3 grid((unsigned)row_slabs(d.cols), (unsigned)min(ceil_div(d.tokens, per), 1 << 15));
     if (d.dtype == SOL_BF16) {
         if (d.token_bits == 64) hipLaunchKernelGGL((embed_kernel<bf16_t, int64_t>), grid, dim3(256), 0, st, a);
         else hipLaunchKernelGGL((embed_kernel<bf16_t, int32_t>), grid, dim3(256), 0, st, a);
@@ -351,13 +567,13 @@ sol_status sol_embedding_backward(const sol_embedding_desc *ed, const void *toke
     hipStream_t st = (hipStream_t)stream;
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     int *start = reinterpret_cast<int *>(ws + p.start), *order = reinterpret_cast<int *>(ws + p.order), *sorted = reinterpret_cast<int *>(ws + p.sorted);
-    const int rows = min(INDEX_ROWS, max(1, ceil_div(d.vocab, INDEX_GROUPS)));
-    const IndexArgs x{tokens, d.tokens, d.vocab, d.pad, rows, start, order, sorted};
-    const dim3 grid((unsigned)ceil_div(d.vocab, rows));
+    const IndexArgs x{tokens, d.tokens, d.vocab, d.pad, p.rows, p.log2, start, order, sorted};
+    const dim3 grid(1u << p.log2);
     if (d.token_bits == 64) hipLaunchKernelGGL(embed_index_kernel<int64_t>, grid, dim3(INDEX_THREADS), 0, st, x);
     else hipLaunchKernelGGL(embed_index_kernel<int32_t>, grid, dim3(INDEX_THREADS), 0, st, x);
     SOL_HIP(hipGetLastError());
-    const GatherArgs g{dy, dtable, start, order, sorted, reinterpret_cast<float *>(ws + p.part), d.ldy, d.tokens, d.vocab, d.cols, p.windows, accumulate ? 1 : 0, row_lanes_log2(d.cols), d.scale};
+    const GatherArgs g{dy, dtable, start, order, sorted, reinterpret_cast<float *>(ws + p.part), d.ldy, d.vocab, d.cols, p.windows, accumulate ? 1 : 0, row_lanes_log2(d.cols),
+                 p.rows, p.log2, p.places, d.scale, FastDiv((uint32_t)p.rows)};
     if (d.dtype == SOL_F32) return launch_gather<float, float>(g, st);
     return dtable_dtype == SOL_F32 ? launch_gather<bf16_t, float>(g, st) : launch_gather<bf16_t, bf16_t>(g, st);
 }

@@ -24,6 +24,77 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
+// 4 neighbouring elements of a row, of which nv exist, at any element's address
+typedef __attribute__((ext_vector_type(2), aligned(2))) uint32_t u32x2_any;
+template <typename T> __device__ __forceinline__ void load4_any(const T *p, float v[4], int nv) {
+    if (nv >= 4) {
+        if constexpr (sizeof(T) == 2) {
+            const u32x2_any w = *reinterpret_cast<const u32x2_any *>(p);
+            v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u); v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
+        } else {
+            const lds_pipe::u32x4_t w = *reinterpret_cast<const u32x4_any *>(p);
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[e] = __uint_as_float(w[e]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++) v[e] = nv > 0 ? Elem<T>::load(p + min(e, nv - 1)) : 0.f;
+#pragma unroll
+        for (int e = 1; e < 4; e++) v[e] = e < nv ? v[e] : 0.f;
+    }
+}
+template <typename T> __device__ __forceinline__ void store4_any(T *p, const float v[4], int nv) {
+    if (nv >= 4) {
+        if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any *>(p) = u32x2_any{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        else *reinterpret_cast<u32x4_any *>(p) = lds_pipe::u32x4_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+            if (e < nv) Elem<T>::store(p + e, v[e]);
+    }
+}
+
+// The same as they lie in memory, W = 4 or 8 of them, so that loads under way take no more registers than that
+template <typename T, int W> struct RawPiece {
+    uint32_t w[W * sizeof(T) / 4];
+    __device__ __forceinline__ void load(const T *p, int nv) {
+        if (nv >= W) {
+            if constexpr (sizeof(w) == 8) {
+                const u32x2_any v = *reinterpret_cast<const u32x2_any *>(p);
+                w[0] = v.x; w[1] = v.y;
+            } else {
+#pragma unroll
+                for (int i = 0; i < (int)sizeof(w) / 16; i++) {
+                    const lds_pipe::u32x4_t v = reinterpret_cast<const u32x4_any *>(p)[i];
+#pragma unroll
+                    for (int e = 0; e < 4; e++) w[4 * i + e] = v[e];
+                }
+            }
+        } else {
+            float v[W];
+#pragma unroll
+            for (int e = 0; e < W; e++) v[e] = nv > 0 ? Elem<T>::load(p + min(e, nv - 1)) : 0.f;
+#pragma unroll
+            for (int e = 1; e < W; e++) v[e] = e < nv ? v[e] : 0.f;
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int e = 0; e < W / 2; e++) w[e] = __float_as_uint(v[2 * e]) >> 16 | (__float_as_uint(v[2 * e + 1]) & 0xffff0000u);
+            } else {
+#pragma unroll
+                for (int e = 0; e < W; e++) w[e] = __float_as_uint(v[e]);
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int e) const {
+        if constexpr (sizeof(T) == 2) return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16);
+        else return __uint_as_float(w[e]);
+    }
+};
+template <typename T, int W> __device__ __forceinline__ void store_piece(T *p, const float *v, int nv) {
+    if constexpr (W == 4) store4_any<T>(p, v, nv);
+    else store8_any<T>(p, v, nv);
+}
+
 constexpr int MAX_COLS = 1 << 20, MAX_ROW_PITCH = 1 << 21;
 
 inline sol_status check_row_pitch(const char *what, int cols, int *ld) {
