@@ -3,6 +3,8 @@
 //   backward  h = (x - mean) * rstd,  g = dy * gamma;  dx = rstd * (g - mean(g) - h * mean(g h)) + residual;  dgamma = column sums of dy h, dbeta of dy
 #include <float.h>
 
+#include <utility>
+
 #include "row_ops.h"
 
 namespace sol {
@@ -26,6 +28,20 @@ __device__ __forceinline__ void load_weight8(const float *w, int c, int nv, floa
         for (int e = 0; e < 8; e++) v[e] = none;
     }
 }
+// of a span; 0 in the places that are not the thread's own
+__device__ __forceinline__ void load_weight8(const float *w, const Span<8> &sp, float none, float v[8]) {
+    load_weight8(w, sp.c, sp.some() ? sp.end : 0, none, v);
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = sp.has(e) ? v[e] : 0.f;
+}
+// A row for TPR threads: four rows a workgroup where one wave takes a row and none waits for another, else one
+template <int TPR> constexpr int ROW_BLOCK = TPR == 64 ? 256 : TPR;
+template <int TPR, int G> struct Spans {
+    Span<8> of[G];
+    template <int... K> __device__ __forceinline__ Spans(int lane, int cols, std::integer_sequence<int, K...>) : of{Span<8>((lane + K * TPR) * 8, cols)...} {}
+    __device__ __forceinline__ Spans(int lane, int cols) : Spans(lane, cols, std::make_integer_sequence<int, G>()) {}
+    __device__ __forceinline__ const Span<8> &operator[](int k) const { return of[k]; }
+};
 
 // sum / n with the reciprocal and one correction, so that equal elements whose sum is exact have their own value for a mean
 __device__ __forceinline__ float mean_of(float sum, float n, float inv) {
@@ -35,19 +51,18 @@ __device__ __forceinline__ float mean_of(float sum, float n, float inv) {
 
 // Means and squared deviations of the waves, put together: mean = sum n_w mean_w / n, deviations = sum (d_w + n_w (mean_w - mean)^2) (Chan, Golub, LeVeque).
 // One barrier a row; two sets of slots in turn, so that the next row's values do not meet readers of this one's.
-template <int TPR, int G, typename T>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(const NormArgs a) {
-    constexpr int BLOCK = TPR < 256 ? 256 : TPR, RPB = BLOCK / TPR, WAVES = TPR / 64;
+template <int TPR, int G, bool WHOLE, typename T>
+__global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) {
+    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64;
     __shared__ float4 red[2][WAVES];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const Spans<TPR, G> sp(lane, a.cols);
     float gm[G][8], bt[G][8];
-    int nv[G], n_wave = 0;
+    int n_wave = 0;
 #pragma unroll
     for (int k = 0; k < G; k++) {
-        const int c = (lane + k * TPR) * 8;
-        nv[k] = min(8, a.cols - c);
-        load_weight8(a.gamma, c, nv[k], 1.f, gm[k]);
-        load_weight8(a.beta, c, nv[k], 0.f, bt[k]);
+        load_weight8(a.gamma, sp[k], 1.f, gm[k]);
+        load_weight8(a.beta, sp[k], 0.f, bt[k]);
         n_wave += max(0, min(512, a.cols - (lane / 64 * 64 + k * TPR) * 8));
     }
     const float inv_wave = n_wave ? 1.f / (float)n_wave : 0.f;
@@ -57,16 +72,20 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(const NormA
         float v[G][8], s = 0.f;
 #pragma unroll
         for (int k = 0; k < G; k++) {
-            load8_any<T>(x + (lane + k * TPR) * 8, v[k], nv[k]);
+            RawPiece<T, 8> raw;
+            sp[k].template load<WHOLE>(x, raw);
 #pragma unroll
-            for (int e = 0; e < 8; e++) s += v[k][e];
+            for (int e = 0; e < 8; e++) {
+                v[k][e] = raw.get(e);
+                s += WHOLE || sp[k].has(e) ? v[k][e] : 0.f;     // zeros where there is nothing
+            }
         }
         float mean = mean_of(wave_sum(s), (float)n_wave, inv_wave), m2 = 0.f;
 #pragma unroll
         for (int k = 0; k < G; k++)
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const float d = e < nv[k] ? v[k][e] - mean : 0.f;
+                const float d = (WHOLE ? sp[k].some() : sp[k].has(e)) ? v[k][e] - mean : 0.f;
                 m2 += d * d;
             }
         m2 = wave_sum(m2);
@@ -91,7 +110,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_kernel(const NormA
         for (int k = 0; k < G; k++) {
 #pragma unroll
             for (int e = 0; e < 8; e++) v[k][e] = (v[k][e] - mean) * rstd * gm[k][e] + bt[k][e];
-            store8_any<T>(y + (lane + k * TPR) * 8, v[k], nv[k]);
+            sp[k].template store<WHOLE>(y, v[k]);
         }
         if (lane == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -152,59 +171,248 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_long_kernel(c
     }
 }
 
-template <int TPR, int G, typename T>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) norm_dx_kernel(const NormArgs a) {
-    constexpr int BLOCK = TPR < 256 ? 256 : TPR, RPB = BLOCK / TPR, WAVES = TPR / 64;
-    __shared__ float2 red[2][WAVES];
-    const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    float gm[G][8];
-    int nv[G];
+// Column sums of a chunk of rows, by the workgroup `block` of tiles * chunks.
+struct NormColumns {
+    const void *dy, *x;
+    const float *mean, *rstd;
+    long ldy, ldx;
+    int rows, cols, per_chunk, tiles, blocks;
+    float *dgamma, *dbeta;      // parts [chunk][cols], or the sums themselves; NULL: not wanted
+};
+// GROUPS groups of 8 columns x LANES rows at a time, four rows of a thread under way
+template <int GROUPS, int LANES, typename T> __device__ __forceinline__ void column_sums(const NormColumns &a, int block, float (*red)[LANES][GROUPS * 8 + 4]) {
+    const int tile = block % a.tiles, chunk = block / a.tiles;
+    const int gl = threadIdx.x % GROUPS, rl = threadIdx.x / GROUPS, first = (tile * GROUPS + gl) * 8;
+    const int r0 = chunk * a.per_chunk, r1 = min(a.rows, r0 + a.per_chunk);
+    const Span<8> sp(first, a.cols);
+    float sg[8], sb[8];
 #pragma unroll
-    for (int k = 0; k < G; k++) {
-        const int c = (lane + k * TPR) * 8;
-        nv[k] = min(8, a.cols - c);
-        load_weight8(a.gamma, c, nv[k], 1.f, gm[k]);
+    for (int e = 0; e < 8; e++) sg[e] = sb[e] = 0.f;
+    if (sp.some()) {
+        for (int r = r0 + rl; r < r1; r += 4 * LANES) {
+            RawPiece<T, 8> h[4], g[4];
+            float mean[4], rstd[4];
+#pragma unroll
+            for (int u = 0; u < 4; u++) {
+                const int q = min(r + u * LANES, r1 - 1);
+                sp.template load<false>(static_cast<const T *>(a.x) + q * a.ldx, h[u]);
+                sp.template load<false>(static_cast<const T *>(a.dy) + q * a.ldy, g[u]);
+                mean[u] = a.mean[q];
+                rstd[u] = a.rstd[q];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; u++)
+                if (r + u * LANES < r1) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        sg[e] += g[u].get(e) * ((h[u].get(e) - mean[u]) * rstd[u]);
+                        sb[e] += g[u].get(e);
+                    }
+                }
+        }
     }
+#pragma unroll
+    for (int e = 0; e < 8; e++)
+        if (sp.has(e)) {
+            const int lc = sp.c + e - tile * GROUPS * 8;
+            red[0][rl][lc] = sg[e];
+            red[1][rl][lc] = sb[e];
+        }
+    __syncthreads();
+    const int which = threadIdx.x / (GROUPS * 8), lc = threadIdx.x % (GROUPS * 8), col = tile * GROUPS * 8 + lc;
+    float *out = which == 0 ? a.dgamma : a.dbeta;
+    if (which > 1 || col >= a.cols || !out) return;
+    float s = 0.f;
+#pragma unroll
+    for (int r = 0; r < LANES; r++) s += red[which][r][lc];
+    out[(size_t)chunk * a.cols + col] = s;
+}
+template <typename T> __global__ void __launch_bounds__(1024) norm_columns_kernel(const NormColumns a) {
+    __shared__ float red[2][32][256 + 4];
+    column_sums<32, 32, T>(a, (int)blockIdx.x, red);
+}
+
+// The row's part of the backward pass, from g = dy gamma and h: gamma, and so g, is 0 in places that are not the thread's own
+template <int G> __device__ __forceinline__ void row_products(const float (&g)[G][8], const float (&h)[G][8], float &s1, float &s2) {
+    s1 = s2 = 0.f;
+#pragma unroll
+    for (int k = 0; k < G; k++)
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            s1 += g[k][e];
+            s2 += g[k][e] * h[k][e];
+        }
+}
+
+// dx, a row for TPR threads; the workgroups in front sum the columns where there are few rows, so that both take one launch: the data is read twice, but the second time from the caches
+template <int TPR, int G, bool WHOLE, typename T>
+__global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs a, const NormColumns cols) {
+    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64;
+    __shared__ union {
+        float columns[2][BLOCK / 8][64 + 4];
+        float2 red[2][WAVES];
+    } s;
+    if ((int)blockIdx.x < cols.blocks) {
+        column_sums<8, BLOCK / 8, T>(cols, (int)blockIdx.x, s.columns);
+        return;
+    }
+    const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const Spans<TPR, G> sp(lane, a.cols);
+    float gm[G][8];
+#pragma unroll
+    for (int k = 0; k < G; k++) load_weight8(a.gamma, sp[k], 1.f, gm[k]);
     int phase = 0;
-    for (long row = (long)blockIdx.x * RPB + slot; row < a.rows; row += (long)gridDim.x * RPB) {
+    for (long row = (long)(blockIdx.x - cols.blocks) * RPB + slot; row < a.rows; row += (long)(gridDim.x - cols.blocks) * RPB) {
         const T *x = static_cast<const T *>(a.x) + row * a.ldx, *dy = static_cast<const T *>(a.dy) + row * a.ldy;
         const float mean = a.mean_in[row], rstd = a.rstd_in[row];
-        float h[G][8], g[G][8], s1 = 0.f, s2 = 0.f;
+        float h[G][8], g[G][8], s1, s2;
 #pragma unroll
         for (int k = 0; k < G; k++) {
-            load8_any<T>(x + (lane + k * TPR) * 8, h[k], nv[k]);
-            load8_any<T>(dy + (lane + k * TPR) * 8, g[k], nv[k]);
+            RawPiece<T, 8> rx, ry;
+            sp[k].template load<WHOLE>(x, rx);
+            sp[k].template load<WHOLE>(dy, ry);
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                h[k][e] = e < nv[k] ? (h[k][e] - mean) * rstd : 0.f;
-                g[k][e] *= gm[k][e];
-                s1 += g[k][e];
-                s2 += g[k][e] * h[k][e];
+                h[k][e] = (rx.get(e) - mean) * rstd;
+                g[k][e] = ry.get(e) * gm[k][e];
             }
         }
+        row_products<G>(g, h, s1, s2);
         s1 = wave_sum(s1);
         s2 = wave_sum(s2);
         if constexpr (WAVES > 1) {
-            if ((threadIdx.x & 63) == 0) red[phase][lane / 64] = make_float2(s1, s2);
+            if ((threadIdx.x & 63) == 0) s.red[phase][lane / 64] = make_float2(s1, s2);
             __syncthreads();
             s1 = s2 = 0.f;
 #pragma unroll
-            for (int w = 0; w < WAVES; w++) { s1 += red[phase][w].x; s2 += red[phase][w].y; }
+            for (int w = 0; w < WAVES; w++) { s1 += s.red[phase][w].x; s2 += s.red[phase][w].y; }
             phase ^= 1;
         }
         const float c1 = s1 * a.inv_cols, c2 = s2 * a.inv_cols;
         const size_t out = (size_t)row * a.cols;
 #pragma unroll
         for (int k = 0; k < G; k++) {
-            const int c = (lane + k * TPR) * 8;
 #pragma unroll
             for (int e = 0; e < 8; e++) g[k][e] = rstd * (g[k][e] - c1 - h[k][e] * c2);
-            if (a.residual) {
-                load8_any<T>(static_cast<const T *>(a.residual) + out + c, h[k], nv[k]);
+            if (a.residual) {       // dx may be in its place: a thread uses its own elements alone
+                RawPiece<T, 8> res;
+                sp[k].template load<WHOLE>(static_cast<const T *>(a.residual) + out, res);
 #pragma unroll
-                for (int e = 0; e < 8; e++) g[k][e] += h[k][e];
+                for (int e = 0; e < 8; e++) g[k][e] += res.get(e);
             }
-            store8_any<T>(static_cast<T *>(a.y) + out + c, g[k], nv[k]);
+            sp[k].template store<WHOLE>(static_cast<T *>(a.y) + out, g[k]);
+        }
+    }
+}
+
+// dx and the columns' sums in one pass over the data: workgroups stay, take SLOTS rows at a time, with the next ones' loads under way, and keep the sums of their rows' columns in
+// registers; parts [workgroup][cols] at the end.
+template <int TPR> constexpr int GRAD_BLOCK = TPR < 512 ? 512 : TPR;
+template <int TPR, int G, bool WHOLE, typename T>
+__global__ void __launch_bounds__(GRAD_BLOCK<TPR>) norm_grad_kernel(const NormArgs a, float *dgamma, float *dbeta) {
+    constexpr int SLOTS = GRAD_BLOCK<TPR> / TPR, WAVES = TPR / 64;
+    __shared__ float2 red[2][GRAD_BLOCK<TPR> / 64];
+    __shared__ float sums[SLOTS > 1 ? SLOTS - 1 : 1][TPR * G * 8];
+    const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
+    const Spans<TPR, G> sp(lane, a.cols);
+    float gm[G][8], sg[G][8], sb[G][8];
+#pragma unroll
+    for (int k = 0; k < G; k++) {
+        load_weight8(a.gamma, sp[k], 1.f, gm[k]);
+#pragma unroll
+        for (int e = 0; e < 8; e++) sg[k][e] = sb[k][e] = 0.f;
+    }
+    RawPiece<T, 8> xr[G], yr[G];
+    float mean = 0.f, rstd = 0.f;
+    auto fetch = [&](long row) {
+        if (row >= a.rows) return;
+#pragma unroll
+        for (int k = 0; k < G; k++) {
+            sp[k].template load<WHOLE>(static_cast<const T *>(a.x) + row * a.ldx, xr[k]);
+            sp[k].template load<WHOLE>(static_cast<const T *>(a.dy) + row * a.ldy, yr[k]);
+        }
+        mean = a.mean_in[row];
+        rstd = a.rstd_in[row];
+    };
+    int phase = 0;
+    long row = (long)blockIdx.x * SLOTS + slot;
+    fetch(row);
+    for (long first = (long)blockIdx.x * SLOTS; first < a.rows; first += (long)gridDim.x * SLOTS) {      // the same for every thread: each meets every barrier
+        const bool there = row < a.rows;
+        float h[G][8], g[G][8], s1 = 0.f, s2 = 0.f;
+        const float r = rstd;
+        if (there) {
+#pragma unroll
+            for (int k = 0; k < G; k++)
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    h[k][e] = (xr[k].get(e) - mean) * rstd;
+                    const float d = yr[k].get(e);
+                    sb[k][e] += d;
+                    sg[k][e] += d * h[k][e];
+                    g[k][e] = d * gm[k][e];
+                }
+        }
+        RawPiece<T, 8> res[G];
+        const size_t out = (size_t)row * a.cols;
+        if (there && a.residual) {
+#pragma unroll
+            for (int k = 0; k < G; k++) sp[k].template load<WHOLE>(static_cast<const T *>(a.residual) + out, res[k]);
+        }
+        row += (long)gridDim.x * SLOTS;
+        fetch(row);
+        if (a.y) {
+            if (there) row_products<G>(g, h, s1, s2);
+            s1 = wave_sum(s1);
+            s2 = wave_sum(s2);
+            if constexpr (WAVES > 1) {
+                if ((threadIdx.x & 63) == 0) red[phase][threadIdx.x / 64] = make_float2(s1, s2);
+                __syncthreads();
+                s1 = s2 = 0.f;
+#pragma unroll
+                for (int w = 0; w < WAVES; w++) { s1 += red[phase][slot * WAVES + w].x; s2 += red[phase][slot * WAVES + w].y; }
+                phase ^= 1;
+            }
+            const float c1 = s1 * a.inv_cols, c2 = s2 * a.inv_cols;
+            if (there) {
+#pragma unroll
+                for (int k = 0; k < G; k++) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        g[k][e] = r * (g[k][e] - c1 - h[k][e] * c2);
+                        if (a.residual) g[k][e] += res[k].get(e);
+                    }
+                    sp[k].template store<WHOLE>(static_cast<T *>(a.y) + out, g[k]);
+                }
+            }
+        }
+    }
+    // the slots' sums, in their order
+#pragma unroll
+    for (int which = 0; which < 2; which++) {
+        float (&s)[G][8] = which == 0 ? sg : sb;
+        float *part = which == 0 ? dgamma : dbeta;
+        if (!part) continue;
+        if constexpr (SLOTS > 1) {
+            __syncthreads();
+            if (slot > 0) {
+#pragma unroll
+                for (int k = 0; k < G; k++)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) sums[slot - 1][(k * 8 + e) * TPR + lane] = s[k][e];
+            }
+            __syncthreads();
+        }
+        if (slot == 0) {
+#pragma unroll
+            for (int k = 0; k < G; k++) {
+                if constexpr (SLOTS > 1) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++)
+                        for (int q = 0; q < SLOTS - 1; q++) s[k][e] += sums[q][(k * 8 + e) * TPR + lane];
+                }
+                sp[k].template store<WHOLE>(part + (size_t)blockIdx.x * a.cols, s[k]);
+            }
         }
     }
 }
@@ -246,47 +454,6 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_dx_long_kerne
     }
 }
 
-// Column sums of a chunk of rows: 32 groups of 8 columns x 32 rows at a time.
-struct NormColumns {
-    const void *dy, *x;
-    const float *mean, *rstd;
-    long ldy, ldx;
-    int rows, cols, per_chunk, tiles;
-    float *dgamma, *dbeta;      // parts [chunk][cols], or the sums themselves; NULL: not wanted
-};
-template <typename T> __global__ void __launch_bounds__(1024) norm_columns_kernel(const NormColumns a) {
-    __shared__ float red[2][32][256 + 4];
-    const int tile = (int)blockIdx.x % a.tiles, chunk = (int)blockIdx.x / a.tiles;
-    const int gl = threadIdx.x & 31, rl = threadIdx.x >> 5, c = (tile * 32 + gl) * 8, nv = min(8, a.cols - c);
-    const int r0 = chunk * a.per_chunk, r1 = min(a.rows, r0 + a.per_chunk);
-    float sg[8], sb[8];
-#pragma unroll
-    for (int e = 0; e < 8; e++) sg[e] = sb[e] = 0.f;
-    if (nv > 0) {
-        for (int r = r0 + rl; r < r1; r += 32) {
-            float h[8], g[8];
-            load8_any<T>(static_cast<const T *>(a.x) + r * a.ldx + c, h, nv);
-            load8_any<T>(static_cast<const T *>(a.dy) + r * a.ldy + c, g, nv);
-            const float mean = a.mean[r], rstd = a.rstd[r];
-#pragma unroll
-            for (int e = 0; e < 8; e++) {
-                sg[e] += g[e] * ((h[e] - mean) * rstd);
-                sb[e] += g[e];
-            }
-        }
-    }
-#pragma unroll
-    for (int e = 0; e < 8; e++) { red[0][rl][gl * 8 + e] = sg[e]; red[1][rl][gl * 8 + e] = sb[e]; }
-    __syncthreads();
-    const int which = threadIdx.x >> 8, col = tile * 256 + (threadIdx.x & 255);
-    float *out = which == 0 ? a.dgamma : a.dbeta;
-    if (which > 1 || col >= a.cols || !out) return;
-    float s = 0.f;
-#pragma unroll
-    for (int r = 0; r < 32; r++) s += red[which][r][threadIdx.x & 255];
-    out[(size_t)chunk * a.cols + col] = s;
-}
-
 // Two workgroups per CU, each with 32 rows or more
 int rows_per_chunk(int rows, int cols) {
     const int want = max(1, 512 / ceil_div(cols, 256));
@@ -305,27 +472,51 @@ sol_status check_norm(const sol_layer_norm_desc *nd, sol_layer_norm_desc *n) {
     return SOL_OK;
 }
 
-enum { NORM_FORWARD, NORM_DX };
-template <int TPR, int G, typename T> void launch_rows(int kind, const NormArgs &a, hipStream_t st) {
-    constexpr int BLOCK = TPR < 256 ? 256 : TPR, RPB = BLOCK / TPR;
-    const dim3 grid((unsigned)min(((long)a.rows + RPB - 1) / RPB, 2048l));
-    if (kind == NORM_FORWARD) hipLaunchKernelGGL((norm_kernel<TPR, G, T>), grid, dim3(BLOCK), 0, st, a);
-    else hipLaunchKernelGGL((norm_dx_kernel<TPR, G, T>), grid, dim3(BLOCK), 0, st, a);
+enum { NORM_FORWARD, NORM_DX, NORM_GRAD };
+constexpr int MAX_REGISTER_GROUPS = 1024, FEW_ROWS = 512;
+
+struct NormLaunch {
+    int kind;
+    NormArgs a;
+    NormColumns cols;           // NORM_DX: what the workgroups in front sum
+    int groups;                 // NORM_GRAD: workgroups
+    float *dgamma, *dbeta;      // and their parts
+};
+template <int TPR, int G, bool WHOLE, typename T> void launch_rows_of(const NormLaunch &l, hipStream_t st) {
+    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR;
+    const int rows = (int)min(((long)l.a.rows + RPB - 1) / RPB, 2048l);
+    if (l.kind == NORM_FORWARD) hipLaunchKernelGGL((norm_kernel<TPR, G, WHOLE, T>), dim3((unsigned)rows), dim3(BLOCK), 0, st, l.a);
+    else if (l.kind == NORM_DX) hipLaunchKernelGGL((norm_dx_kernel<TPR, G, WHOLE, T>), dim3((unsigned)(l.cols.blocks + (l.a.y ? rows : 0))), dim3(BLOCK), 0, st, l.a, l.cols);
+    else hipLaunchKernelGGL((norm_grad_kernel<TPR, G, WHOLE, T>), dim3((unsigned)l.groups), dim3(GRAD_BLOCK<TPR>), 0, st, l.a, l.dgamma, l.dbeta);
 }
-template <typename T> sol_status launch_norm(int kind, const NormArgs &a, hipStream_t st) {
-    const int groups = ceil_div(a.cols, 8);
-    if (groups <= 64) launch_rows<64, 1, T>(kind, a, st);
-    else if (groups <= 128) launch_rows<64, 2, T>(kind, a, st);
-    else if (groups <= 256) launch_rows<256, 1, T>(kind, a, st);
-    else if (groups <= 512) launch_rows<256, 2, T>(kind, a, st);
-    else if (groups <= 1024) launch_rows<512, 2, T>(kind, a, st);
+template <int TPR, int G, typename T> void launch_rows(const NormLaunch &l, hipStream_t st) {
+    if (l.a.cols % 8 == 0) launch_rows_of<TPR, G, true, T>(l, st);
+    else launch_rows_of<TPR, G, false, T>(l, st);
+}
+template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st) {
+    const int groups = ceil_div(l.a.cols, 8);
+    if (groups <= 64) launch_rows<64, 1, T>(l, st);
+    else if (groups <= 128) launch_rows<128, 1, T>(l, st);
+    else if (groups <= 256) launch_rows<256, 1, T>(l, st);
+    else if (groups <= 512) launch_rows<256, 2, T>(l, st);
+    else if (groups <= MAX_REGISTER_GROUPS) launch_rows<512, 2, T>(l, st);
     else {
-        const dim3 grid((unsigned)min(a.rows, 1024));
-        if (kind == NORM_FORWARD) hipLaunchKernelGGL(norm_long_kernel<T>, grid, dim3(1024), 0, st, a);
-        else hipLaunchKernelGGL(norm_dx_long_kernel<T>, grid, dim3(1024), 0, st, a);
+        const dim3 grid((unsigned)min(l.a.rows, 1024));
+        if (l.kind == NORM_FORWARD) hipLaunchKernelGGL(norm_long_kernel<T>, grid, dim3(1024), 0, st, l.a);
+        else hipLaunchKernelGGL(norm_dx_long_kernel<T>, grid, dim3(1024), 0, st, l.a);
     }
     SOL_HIP(hipGetLastError());
     return SOL_OK;
+}
+sol_status launch_norm(const NormLaunch &l, int dt, hipStream_t st) { return dt == SOL_BF16 ? launch_norm<bf16_t>(l, st) : launch_norm<float>(l, st); }
+
+// Parts that dgamma and dbeta are summed in: 1 where workgroups beside the rows' sum whole columns
+int norm_parts(int rows, int cols) {
+    const int groups = ceil_div(cols, 8);
+    if (groups > MAX_REGISTER_GROUPS) return norm_chunks(rows, cols);
+    if (rows <= FEW_ROWS) return 1;
+    const int slots = groups <= 64 ? 8 : groups <= 128 ? 4 : groups <= 512 ? 2 : 1;
+    return (int)min(((long)rows + slots - 1) / slots, groups <= 256 ? 512l : 256l);
 }
 
 }  // namespace
@@ -348,17 +539,19 @@ sol_status sol_layer_norm(const sol_layer_norm_desc *nd, const void *x, const fl
         for (int j = 0; j < (i ? 3 : 2); j++) SOL_REQUIRE(!outs[i] || outs[i] != ins[j], SOL_ERR_UNSUPPORTED, "layer norm: outputs must not alias inputs");
         for (int j = 0; j < i; j++) SOL_REQUIRE(!outs[i] || outs[i] != outs[j], SOL_ERR_UNSUPPORTED, "layer norm: outputs must not alias each other");
     }
-    NormArgs a{};
+    NormLaunch l{};
+    l.kind = NORM_FORWARD;
+    NormArgs &a = l.a;
     a.x = x; a.gamma = gamma; a.beta = beta; a.y = y; a.mean = mean; a.rstd = rstd;
     a.ldx = n.ldx; a.ldy = n.ldy; a.rows = n.rows; a.cols = n.cols; a.eps = n.eps; a.inv_cols = 1.f / (float)n.cols;
-    return n.dtype == SOL_BF16 ? launch_norm<bf16_t>(NORM_FORWARD, a, (hipStream_t)stream) : launch_norm<float>(NORM_FORWARD, a, (hipStream_t)stream);
+    return launch_norm(l, n.dtype, (hipStream_t)stream);
 }
 
 size_t sol_layer_norm_backward_workspace_bytes(const sol_layer_norm_desc *nd) {
     sol_layer_norm_desc n;
     if (check_norm(nd, &n) != SOL_OK) return 0;
-    const int chunks = norm_chunks(n.rows, n.cols);
-    return chunks > 1 ? (size_t)2 * chunks * n.cols * 4 : 0;
+    const int parts = norm_parts(n.rows, n.cols);
+    return parts > 1 ? (size_t)2 * parts * n.cols * 4 : 0;
 }
 
 sol_status sol_layer_norm_backward(const sol_layer_norm_desc *nd, const void *dy, const void *x, const float *gamma, const float *mean, const float *rstd, const void *residual, void *dx,
@@ -381,24 +574,38 @@ sol_status sol_layer_norm_backward(const sol_layer_norm_desc *nd, const void *dy
         for (int j = 0; j < i; j++) SOL_REQUIRE(!outs[i] || outs[i] != outs[j], SOL_ERR_UNSUPPORTED, "layer norm backward: outputs must not alias each other");
     }
     SOL_TRY(check_scratch(workspace, workspace_bytes, sol_layer_norm_backward_workspace_bytes(&n)));
-    if (dgamma || dbeta) {
-        const int chunks = norm_chunks(n.rows, n.cols);
-        float *pg = static_cast<float *>(workspace), *pb = pg + (size_t)chunks * n.cols;
-        NormColumns c{dy, x, mean, rstd, n.ldy, n.ldx, n.rows, n.cols, rows_per_chunk(n.rows, n.cols), ceil_div(n.cols, 256), dgamma, dbeta};
-        if (chunks > 1) {
-            if (dgamma) { c.dgamma = pg; sums.add(pg, chunks, n.cols, dgamma, SOL_F32); }
-            if (dbeta) { c.dbeta = pb; sums.add(pb, chunks, n.cols, dbeta, SOL_F32); }
-        }
-        const dim3 grid((unsigned)(c.tiles * chunks));
-        if (n.dtype == SOL_BF16) hipLaunchKernelGGL(norm_columns_kernel<bf16_t>, grid, dim3(1024), 0, st, c);
-        else hipLaunchKernelGGL(norm_columns_kernel<float>, grid, dim3(1024), 0, st, c);
-        SOL_HIP(hipGetLastError());
+    NormLaunch l{};
+    NormArgs &a = l.a;
+    a.x = x; a.dy = dy; a.residual = residual; a.gamma = gamma; a.mean_in = mean; a.rstd_in = rstd; a.y = dx;
+    a.ldx = n.ldx; a.ldy = n.ldy; a.rows = n.rows; a.cols = n.cols; a.inv_cols = 1.f / (float)n.cols;
+    const bool columns = dgamma || dbeta, wide = ceil_div(n.cols, 8) > MAX_REGISTER_GROUPS;
+    if (!columns && !dx) return SOL_OK;
+    // where the columns' sums go: parts, which a launch behind puts together, or their own place
+    const int parts = norm_parts(n.rows, n.cols);
+    float *pg = dgamma, *pb = dbeta;
+    if (parts > 1) {
+        float *ws = static_cast<float *>(workspace);
+        if (dgamma) { pg = ws; sums.add(pg, parts, n.cols, dgamma, SOL_F32); }
+        if (dbeta) { pb = ws + (size_t)parts * n.cols; sums.add(pb, parts, n.cols, dbeta, SOL_F32); }
     }
-    if (dx) {
-        NormArgs a{};
-        a.x = x; a.dy = dy; a.residual = residual; a.gamma = gamma; a.mean_in = mean; a.rstd_in = rstd; a.y = dx;
-        a.ldx = n.ldx; a.ldy = n.ldy; a.rows = n.rows; a.cols = n.cols; a.inv_cols = 1.f / (float)n.cols;
-        SOL_TRY(n.dtype == SOL_BF16 ? launch_norm<bf16_t>(NORM_DX, a, st) : launch_norm<float>(NORM_DX, a, st));
+    if (columns) l.cols = NormColumns{dy, x, mean, rstd, n.ldy, n.ldx, n.rows, n.cols, n.rows, ceil_div(n.cols, 64), ceil_div(n.cols, 64), pg, pb};
+    if (wide) {
+        if (columns) {
+            l.cols.per_chunk = rows_per_chunk(n.rows, n.cols);
+            l.cols.tiles = ceil_div(n.cols, 256);
+            const dim3 grid((unsigned)(l.cols.tiles * parts));
+            if (n.dtype == SOL_BF16) hipLaunchKernelGGL(norm_columns_kernel<bf16_t>, grid, dim3(1024), 0, st, l.cols);
+            else hipLaunchKernelGGL(norm_columns_kernel<float>, grid, dim3(1024), 0, st, l.cols);
+            SOL_HIP(hipGetLastError());
+        }
+        l.kind = NORM_DX;
+        if (dx) SOL_TRY(launch_norm(l, n.dtype, st));
+    } else {
+        l.kind = columns && n.rows > FEW_ROWS ? NORM_GRAD : NORM_DX;
+        l.groups = parts;
+        l.dgamma = pg;
+        l.dbeta = pb;
+        SOL_TRY(launch_norm(l, n.dtype, st));
     }
     return launch_sums(sums, st);
 }

@@ -56,7 +56,7 @@ template <typename T> __device__ __forceinline__ void store4_any(T *p, const flo
 
 // The same as they lie in memory, W = 4 or 8 of them, so that loads under way take no more registers than that
 template <typename T, int W> struct RawPiece {
-    uint32_t w[W * sizeof(T) / 4];
+    uint32_t w[W * sizeof(T) / 4] = {};
     __device__ __forceinline__ void load(const T *p, int nv) {
         if (nv >= W) {
             if constexpr (sizeof(w) == 8) {
@@ -90,10 +90,36 @@ template <typename T, int W> struct RawPiece {
         else return __uint_as_float(w[e]);
     }
 };
-template <typename T, int W> __device__ __forceinline__ void store_piece(T *p, const float *v, int nv) {
-    if constexpr (W == 4) store4_any<T>(p, v, nv);
-    else store8_any<T>(p, v, nv);
-}
+// W neighbouring columns of a row for one thread.  The last thread of a row whose length is no multiple of W takes the row's last W columns, of which it leaves the first `skip` to the
+// thread in front: a load of one piece like the others', which is waited for where it is used and not where it is asked for, as pieces put together of elements are.
+// Only rows shorter than W end early.
+template <int W> struct Span {
+    int c, skip, end;               // columns c + skip .. c + end - 1 are this thread's; skip = W: none
+    __device__ __forceinline__ Span(int at, int cols) : c(at), skip(0), end(W) {
+        if (at >= cols) { c = 0; skip = W; }
+        else if (cols < W) end = cols;
+        else if (at + W > cols) { c = cols - W; skip = at - c; }
+    }
+    __device__ __forceinline__ bool some() const { return skip < W; }
+    __device__ __forceinline__ bool has(int e) const { return e >= skip && e < end; }
+    // WHOLE: the row's length is a multiple of W
+    template <bool WHOLE, typename T> __device__ __forceinline__ void load(const T *row, RawPiece<T, W> &r) const {
+        if (!some()) return;
+        if (WHOLE || end == W) r.load(row + c, W);
+        else r.load(row + c, end);
+    }
+    template <bool WHOLE, typename T> __device__ __forceinline__ void store(T *row, const float *v) const {
+        if (!some()) return;
+        if (WHOLE || (skip == 0 && end == W)) {
+            if constexpr (W == 4) store4_any<T>(row + c, v, W);
+            else store8_any<T>(row + c, v, W);
+        } else {
+#pragma unroll
+            for (int e = 0; e < W; e++)
+                if (has(e)) Elem<T>::store(row + c + e, v[e]);
+        }
+    }
+};
 
 constexpr int MAX_COLS = 1 << 20, MAX_ROW_PITCH = 1 << 21;
 
