@@ -307,11 +307,12 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
 
 // dx and the columns' sums in one pass over the data: workgroups stay, take SLOTS rows at a time, with the next ones' loads under way, and keep the sums of their rows' columns in
 // registers; parts [workgroup][cols] at the end.
-template <int TPR> constexpr int GRAD_BLOCK = TPR < 512 ? 512 : TPR;
+// Threads of a workgroup: 1024 where 128 registers hold a thread's share, so that fewer workgroups fill the GPU and fewer parts are left
+template <int G, bool WHOLE> constexpr int GRAD_BLOCK = G == 1 && WHOLE ? 1024 : 512;
 template <int TPR, int G, bool WHOLE, typename T>
-__global__ void __launch_bounds__(GRAD_BLOCK<TPR>) norm_grad_kernel(const NormArgs a, float *dgamma, float *dbeta) {
-    constexpr int SLOTS = GRAD_BLOCK<TPR> / TPR, WAVES = TPR / 64;
-    __shared__ float2 red[2][GRAD_BLOCK<TPR> / 64];
+__global__ void __launch_bounds__((GRAD_BLOCK<G, WHOLE>)) norm_grad_kernel(const NormArgs a, float *dgamma, float *dbeta) {
+    constexpr int SLOTS = GRAD_BLOCK<G, WHOLE> / TPR, WAVES = TPR / 64;
+    __shared__ float2 red[2][GRAD_BLOCK<G, WHOLE> / 64];
     __shared__ float sums[SLOTS > 1 ? SLOTS - 1 : 1][TPR * G * 8];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
     const Spans<TPR, G> sp(lane, a.cols);
@@ -473,7 +474,11 @@ sol_status check_norm(const sol_layer_norm_desc *nd, sol_layer_norm_desc *n) {
 }
 
 enum { NORM_FORWARD, NORM_DX, NORM_GRAD };
-constexpr int MAX_REGISTER_GROUPS = 1024, FEW_ROWS = 512;
+constexpr int MAX_REGISTER_GROUPS = 1024;
+// Few rows: columns are summed by workgroups of their own, beside the rows', in the same launch.  us, one launch against one pass and a launch for its parts: 512 rows of 2048 bf16 6.0 and 8.6,
+// 1024 rows 9.6 and 10.3, 1536 rows 17.2 and 11.7; 512 rows of 1531 fp32 6.6 and 9.4, 1024 rows 14.1 and 11.9.
+bool few_rows(int rows, int dt) { return (size_t)rows * dtype_size(dt) <= 2048; }
+
 
 struct NormLaunch {
     int kind;
@@ -487,7 +492,7 @@ template <int TPR, int G, bool WHOLE, typename T> void launch_rows_of(const Norm
     const int rows = (int)min(((long)l.a.rows + RPB - 1) / RPB, 2048l);
     if (l.kind == NORM_FORWARD) hipLaunchKernelGGL((norm_kernel<TPR, G, WHOLE, T>), dim3((unsigned)rows), dim3(BLOCK), 0, st, l.a);
     else if (l.kind == NORM_DX) hipLaunchKernelGGL((norm_dx_kernel<TPR, G, WHOLE, T>), dim3((unsigned)(l.cols.blocks + (l.a.y ? rows : 0))), dim3(BLOCK), 0, st, l.a, l.cols);
-    else hipLaunchKernelGGL((norm_grad_kernel<TPR, G, WHOLE, T>), dim3((unsigned)l.groups), dim3(GRAD_BLOCK<TPR>), 0, st, l.a, l.dgamma, l.dbeta);
+    else hipLaunchKernelGGL((norm_grad_kernel<TPR, G, WHOLE, T>), dim3((unsigned)l.groups), dim3(GRAD_BLOCK<G, WHOLE>), 0, st, l.a, l.dgamma, l.dbeta);
 }
 template <int TPR, int G, typename T> void launch_rows(const NormLaunch &l, hipStream_t st) {
     if (l.a.cols % 8 == 0) launch_rows_of<TPR, G, true, T>(l, st);
@@ -511,12 +516,17 @@ template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st
 sol_status launch_norm(const NormLaunch &l, int dt, hipStream_t st) { return dt == SOL_BF16 ? launch_norm<bf16_t>(l, st) : launch_norm<float>(l, st); }
 
 // Parts that dgamma and dbeta are summed in: 1 where workgroups beside the rows' sum whole columns
-int norm_parts(int rows, int cols) {
+int norm_parts(int rows, int cols, int dt) {
     const int groups = ceil_div(cols, 8);
     if (groups > MAX_REGISTER_GROUPS) return norm_chunks(rows, cols);
-    if (rows <= FEW_ROWS) return 1;
-    const int slots = groups <= 64 ? 8 : groups <= 128 ? 4 : groups <= 512 ? 2 : 1;
-    return (int)min(((long)rows + slots - 1) / slots, groups <= 256 ? 512l : 256l);
+    if (few_rows(rows, dt)) return 1;
+    const bool large = groups <= 256 && cols % 8 == 0;      // workgroups of 1024 threads
+    const int slots = (large ? 1024 : 512) / (groups <= 64 ? 64 : groups <= 128 ? 128 : groups <= 512 ? 256 : 512);
+    const long rounds = ((long)rows + slots - 1) / slots;
+    // A round of rows costs a workgroup about what 32 more parts cost the launch that sums them: 32 rounds = parts^2 makes the sum of both least.  Up to a GPU full of workgroups.
+    long parts = 1;
+    while (parts * parts < 32 * rounds && parts < min(rounds, groups <= 256 && !large ? 512l : 256l)) parts++;
+    return (int)parts;
 }
 
 }  // namespace
@@ -550,7 +560,7 @@ sol_status sol_layer_norm(const sol_layer_norm_desc *nd, const void *x, const fl
 size_t sol_layer_norm_backward_workspace_bytes(const sol_layer_norm_desc *nd) {
     sol_layer_norm_desc n;
     if (check_norm(nd, &n) != SOL_OK) return 0;
-    const int parts = norm_parts(n.rows, n.cols);
+    const int parts = norm_parts(n.rows, n.cols, n.dtype);
     return parts > 1 ? (size_t)2 * parts * n.cols * 4 : 0;
 }
 
@@ -581,7 +591,7 @@ sol_status sol_layer_norm_backward(const sol_layer_norm_desc *nd, const void *dy
     const bool columns = dgamma || dbeta, wide = ceil_div(n.cols, 8) > MAX_REGISTER_GROUPS;
     if (!columns && !dx) return SOL_OK;
     // where the columns' sums go: parts, which a launch behind puts together, or their own place
-    const int parts = norm_parts(n.rows, n.cols);
+    const int parts = norm_parts(n.rows, n.cols, n.dtype);
     float *pg = dgamma, *pb = dbeta;
     if (parts > 1) {
         float *ws = static_cast<float *>(workspace);
@@ -601,7 +611,7 @@ sol_status sol_layer_norm_backward(const sol_layer_norm_desc *nd, const void *dy
         l.kind = NORM_DX;
         if (dx) SOL_TRY(launch_norm(l, n.dtype, st));
     } else {
-        l.kind = columns && n.rows > FEW_ROWS ? NORM_GRAD : NORM_DX;
+        l.kind = columns && !few_rows(n.rows, n.dtype) ? NORM_GRAD : NORM_DX;
         l.groups = parts;
         l.dgamma = pg;
         l.dbeta = pb;
