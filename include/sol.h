@@ -337,7 +337,7 @@ typedef struct {
 /* Device scratch of sol_grad_norm and sol_grad_clip for these tensors (their counts are what matters).  Calls that may run at the same time need scratch of their own. */
 size_t sol_grad_workspace_bytes(const sol_grad *grads, int tensors);
 
-/* grads: host array of `tensors` entries, read during the call.  norm: device fp32.  Squares are summed in 64 bits, in an order that the counts fix.
+/* grads: host array of `tensors` entries, at most 2^15, read during the call.  norm: device fp32.  Squares are summed in 64 bits, in an order that the counts fix.
  * No two entries of sol_grad_clip may share memory, but for an entry's out in place of its grad.  No tensors: norm 0. */
 sol_status sol_grad_norm(const sol_grad *grads, int tensors, float *norm, void *workspace, size_t workspace_bytes, void *hip_stream);
 sol_status sol_grad_clip(const sol_grad *grads, int tensors, float max_norm, float *norm, void *workspace, size_t workspace_bytes,

@@ -8,11 +8,11 @@
 namespace sol {
 namespace {
 
-// Lanes that a row takes: up to a wave's 64, 8 columns each; wider rows are cut into slabs of 512 columns.
-int row_lanes_log2(int cols) {
-    const int groups = ceil_div(cols, 8);
+// Lanes that a row takes: 8 to a wave's 64, so many columns each
+int row_lanes_log2(int cols, int each) {
+    const int pieces = ceil_div(cols, each);
     int l = 3;
-    while (l < 6 && (1 << l) < groups) l++;
+    while (l < 6 && (1 << l) < pieces) l++;
     return l;
 }
 int row_slabs(int cols) { return ceil_div(cols, 512); }
@@ -24,23 +24,31 @@ struct EmbedArgs {
     int n, vocab, cols, pad, lanes_log2;
     float scale;
 };
-template <typename T, typename I> __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a) {
-    const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1), slot = threadIdx.x >> a.lanes_log2;
-    const int c = ((int)blockIdx.x * 64 + lane) * 8, nv = min(8, a.cols - c);
-    if (nv <= 0) return;
-    for (long i = (long)blockIdx.y * (256 >> a.lanes_log2) + slot; i < a.n; i += (long)gridDim.y * (256 >> a.lanes_log2)) {
-        const I tok = static_cast<const I *>(a.tokens)[i];
-        float v[8];
-        if (tok != (I)a.pad && tok >= 0 && tok < (I)a.vocab) {
-            load8_any<T>(static_cast<const T *>(a.table) + (long)tok * a.ldt + c, v, nv);
+// 16 bytes of a row for a lane: 2^lanes_log2 lanes, or slabs of 64, which vary fastest (see embed_wide_kernel); KEEP tokens of a lane under way at a time.  65536 tokens of 2048 bf16: one token 99 us,
+// two 96, four 90 with ordinary stores, 54 to 57 with two to eight past the caches; 8 tokens of 4096 4.2, 4.5 and 5.2 us.
+constexpr int KEEP = 2;
+template <typename T, typename I, bool STREAM> __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a) {
+    constexpr int W = 16 / sizeof(T);
+    const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1), slot = threadIdx.x >> a.lanes_log2, per = 256 >> a.lanes_log2;
+    const Span<W> sp(((int)blockIdx.x * 64 + lane) * W, a.cols);
+    for (long i0 = (long)blockIdx.y * (per * KEEP) + slot; i0 < a.n; i0 += (long)gridDim.y * (per * KEEP)) {
+        I tok[KEEP];
+        RawPiece<T, W> raw[KEEP];
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[e] *= a.scale;
-        } else {
-            const float none = tok == (I)a.pad ? 0.f : __uint_as_float(0x7fc00000u);
+        for (int k = 0; k < KEEP; k++) tok[k] = static_cast<const I *>(a.tokens)[min(i0 + k * per, (long)a.n - 1)];
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[e] = none;
+        for (int k = 0; k < KEEP; k++)
+            if (tok[k] != (I)a.pad && tok[k] >= 0 && tok[k] < (I)a.vocab) sp.template load<false>(static_cast<const T *>(a.table) + (long)tok[k] * a.ldt, raw[k]);
+#pragma unroll
+        for (int k = 0; k < KEEP; k++) {
+            if (i0 + k * per >= a.n) break;
+            const bool row = tok[k] != (I)a.pad && tok[k] >= 0 && tok[k] < (I)a.vocab;
+            const float none = tok[k] == (I)a.pad ? 0.f : __uint_as_float(0x7fc00000u);
+            float v[W];
+#pragma unroll
+            for (int e = 0; e < W; e++) v[e] = row ? raw[k].get(e) * a.scale : none;
+            sp.template store<false, STREAM>(static_cast<T *>(a.y) + (i0 + k * per) * a.ldy, v);
         }
-        store8_any<T>(static_cast<T *>(a.y) + i * a.ldy + c, v, nv);
     }
 }
 
@@ -377,7 +385,7 @@ template <typename T, typename TO> __global__ void __launch_bounds__(256) embed_
 }
 
 // Wider ones: a wave takes PIECES * 64 * W columns of a row.  Three round trips to memory: where its run is, the positions in it (a lane each), and FLIGHT of the gradient's rows at a time.
-template <typename T, typename TO, int W, int PIECES> __device__ __forceinline__ void wide_item(const GatherArgs &a, int item, int c0) {
+template <typename T, typename TO, int W, int PIECES, bool STREAM> __device__ __forceinline__ void wide_item(const GatherArgs &a, int item, int c0) {
     constexpr int FLIGHT = 64 / (W * PIECES);
     const int lane = threadIdx.x & 63;
     const bool window = item < 2 * a.windows;
@@ -389,8 +397,9 @@ template <typename T, typename TO, int W, int PIECES> __device__ __forceinline__
         q = Part{p, a.start[p], a.start[p + 1]};
         if (q.e - q.b > RUN || (a.accumulate && q.e == q.b)) return;
     }
-    const T *dy = static_cast<const T *>(a.dy) + c0;
-    const int nv = a.cols - c0, many = q.e - q.b, order = lane < many ? a.order[q.b + lane] : 0;        // RUN of them at most
+    const T *dy = static_cast<const T *>(a.dy);
+    const Spans<W, PIECES> sp(c0, 64 * W, a.cols);
+    const int many = q.e - q.b, order = lane < many ? a.order[q.b + lane] : 0;        // RUN of them at most
     float acc[PIECES][W];
 #pragma unroll
     for (int i = 0; i < PIECES; i++)
@@ -403,7 +412,7 @@ template <typename T, typename TO, int W, int PIECES> __device__ __forceinline__
             if (j + u < many) {
                 const T *p = dy + (long)__builtin_amdgcn_readlane(order, j + u) * a.ldy;
 #pragma unroll
-                for (int i = 0; i < PIECES; i++) raw[u][i].load(p + i * 64 * W, nv - i * 64 * W);
+                for (int i = 0; i < PIECES; i++) sp[i].template load<false>(p, raw[u][i]);
             }
         }
 #pragma unroll
@@ -417,25 +426,25 @@ template <typename T, typename TO, int W, int PIECES> __device__ __forceinline__
         }
     }
     if (window) {
-        float *part = a.part + (size_t)item * a.cols + c0;
+        float *part = a.part + (size_t)item * a.cols;
 #pragma unroll
-        for (int i = 0; i < PIECES; i++) store_piece<float, W>(part + i * 64 * W, acc[i], nv - i * 64 * W);
+        for (int i = 0; i < PIECES; i++) sp[i].template store<false>(part, acc[i]);
         return;
     }
-    TO *out = static_cast<TO *>(a.out) + (size_t)(item - 2 * a.windows) * a.cols + c0;
+    TO *out = static_cast<TO *>(a.out) + (size_t)(item - 2 * a.windows) * a.cols;
 #pragma unroll
     for (int i = 0; i < PIECES; i++) {
         RawPiece<TO, W> old;
-        if (a.accumulate) old.load(out + i * 64 * W, nv - i * 64 * W);
+        if (a.accumulate) sp[i].template load<false>(out, old);
 #pragma unroll
         for (int k = 0; k < W; k++) acc[i][k] = a.accumulate ? acc[i][k] * a.scale + old.get(k) : acc[i][k] * a.scale;
-        store_piece<TO, W>(out + i * 64 * W, acc[i], nv - i * 64 * W);
+        sp[i].template store<false, STREAM>(out, acc[i]);
     }
 }
 // Slabs of columns vary fastest: workgroups that run together then write whole rows, not the same part of every row, whose addresses would fall on a few of the memory's channels.
-template <typename T, typename TO, int W, int PIECES> __global__ void __launch_bounds__(256) embed_wide_kernel(const GatherArgs a, int items) {
+template <typename T, typename TO, int W, int PIECES, bool STREAM> __global__ void __launch_bounds__(256) embed_wide_kernel(const GatherArgs a, int items) {
     const int c0 = (int)blockIdx.x * (PIECES * 64 * W) + (threadIdx.x & 63) * W;
-    for (int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += (int)gridDim.y * 4) wide_item<T, TO, W, PIECES>(a, item, c0);
+    for (int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += (int)gridDim.y * 4) wide_item<T, TO, W, PIECES, STREAM>(a, item, c0);
 }
 
 // A long run ends behind the window that it starts in: at most one starts in each
@@ -482,6 +491,18 @@ sol_status check_embed(const sol_embedding_desc *ed, sol_embedding_desc *d) {
     return SOL_OK;
 }
 
+template <typename T, typename I> sol_status launch_embed_of(const EmbedArgs &a, hipStream_t st) {
+    const int per = (256 >> a.lanes_log2) * KEEP;
+    const dim3 grid((unsigned)ceil_div(a.cols, 64 * 16 / (int)sizeof(T)), (unsigned)min(ceil_div(a.n, per), 65535));
+    if ((size_t)a.n * a.cols * sizeof(T) >= STREAM_BYTES) hipLaunchKernelGGL((embed_kernel<T, I, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((embed_kernel<T, I, false>), grid, dim3(256), 0, st, a);
+    SOL_HIP(hipGetLastError());
+    return SOL_OK;
+}
+template <typename T> sol_status launch_embed(const EmbedArgs &a, int bits, hipStream_t st) {
+    return bits == 64 ? launch_embed_of<T, int64_t>(a, st) : launch_embed_of<T, int32_t>(a, st);
+}
+
 struct EmbedPlan {
     size_t start, order, sorted, part, bytes;
     int windows, rows, log2, places;
@@ -505,7 +526,9 @@ EmbedPlan embed_plan(const sol_embedding_desc &d) {
 template <typename T, typename TO, int PIECES> void launch_wide(const GatherArgs &g, hipStream_t st) {
     constexpr int W = sizeof(TO) == 4 ? 4 : 8;      // 16 bytes of the table's gradient
     const int items = g.vocab + 2 * g.windows;
-    hipLaunchKernelGGL((embed_wide_kernel<T, TO, W, PIECES * 8 / W>), dim3((unsigned)ceil_div(g.cols, PIECES * 512), (unsigned)min(ceil_div(items, 4), 65535)), dim3(256), 0, st, g, items);
+    const dim3 grid((unsigned)ceil_div(g.cols, PIECES * 512), (unsigned)min(ceil_div(items, 4), 65535));
+    if ((size_t)g.vocab * g.cols * sizeof(TO) >= STREAM_BYTES) hipLaunchKernelGGL((embed_wide_kernel<T, TO, W, PIECES * 8 / W, true>), grid, dim3(256), 0, st, g, items);
+    else hipLaunchKernelGGL((embed_wide_kernel<T, TO, W, PIECES * 8 / W, false>), grid, dim3(256), 0, st, g, items);
 }
 template <typename T, typename TO> sol_status launch_gather(const GatherArgs &g, hipStream_t st) {
     const int per = 256 >> g.lanes_log2, slabs = row_slabs(g.cols);
@@ -535,18 +558,8 @@ sol_status sol_embedding(const sol_embedding_desc *ed, const void *tokens, const
     SOL_REQUIRE(aligned16(tokens) && aligned16(table) && aligned16(y), SOL_ERR_ALIGN, "device pointers must be 16-byte aligned");
     SOL_REQUIRE(y != table && y != tokens, SOL_ERR_UNSUPPORTED, "embedding: y must not alias the table or the tokens");
     hipStream_t st = (hipStream_t)stream;
-    const EmbedArgs a{tokens, table, y, d.ldt, d.ldy, d.tokens, d.vocab, d.cols, d.pad, row_lanes_log2(d.cols), d.scale};
-    const int per = 256 >> a.lanes_log2;
-    const dim3 grid((unsigned)row_slabs(d.cols), (unsigned)min(ceil_div(d.tokens, per), 1 << 15));
-    if (d.dtype == SOL_BF16) {
-        if (d.token_bits == 64) hipLaunchKernelGGL((embed_kernel<bf16_t, int64_t>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((embed_kernel<bf16_t, int32_t>), grid, dim3(256), 0, st, a);
-    } else {
-        if (d.token_bits == 64) hipLaunchKernelGGL((embed_kernel<float, int64_t>), grid, dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((embed_kernel<float, int32_t>), grid, dim3(256), 0, st, a);
-    }
-    SOL_HIP(hipGetLastError());
-    return SOL_OK;
+    const EmbedArgs a{tokens, table, y, d.ldt, d.ldy, d.tokens, d.vocab, d.cols, d.pad, row_lanes_log2(d.cols, 16 / (int)dtype_size(d.dtype)), d.scale};
+    return d.dtype == SOL_BF16 ? launch_embed<bf16_t>(a, d.token_bits, st) : launch_embed<float>(a, d.token_bits, st);
 }
 
 size_t sol_embedding_backward_workspace_bytes(const sol_embedding_desc *ed) {
@@ -572,7 +585,7 @@ sol_status sol_embedding_backward(const sol_embedding_desc *ed, const void *toke
     if (d.token_bits == 64) hipLaunchKernelGGL(embed_index_kernel<int64_t>, grid, dim3(INDEX_THREADS), 0, st, x);
     else hipLaunchKernelGGL(embed_index_kernel<int32_t>, grid, dim3(INDEX_THREADS), 0, st, x);
     SOL_HIP(hipGetLastError());
-    const GatherArgs g{dy, dtable, start, order, sorted, reinterpret_cast<float *>(ws + p.part), d.ldy, d.vocab, d.cols, p.windows, accumulate ? 1 : 0, row_lanes_log2(d.cols),
+    const GatherArgs g{dy, dtable, start, order, sorted, reinterpret_cast<float *>(ws + p.part), d.ldy, d.vocab, d.cols, p.windows, accumulate ? 1 : 0, row_lanes_log2(d.cols, 8),
                  p.rows, p.log2, p.places, d.scale, FastDiv((uint32_t)p.rows)};
     if (d.dtype == SOL_F32) return launch_gather<float, float>(g, st);
     return dtable_dtype == SOL_F32 ? launch_gather<bf16_t, float>(g, st) : launch_gather<bf16_t, bf16_t>(g, st);

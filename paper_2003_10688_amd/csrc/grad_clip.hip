@@ -3,21 +3,29 @@
 #include <float.h>
 #include <stdlib.h>
 
+#include <algorithm>
+
 #include "row_ops.h"
 
 namespace sol {
 namespace {
 
 // The tensors of one launch, by value: no copy to the device, nothing to keep alive, and a captured graph holds them.  A tensor is cut into chunks, so that a workgroup's share is even.
-constexpr int TABLE = 112, CHUNK = 8192, MAX_GROUPS = 1024;
+// 170 tensors fill the 4 KB of a kernel's arguments, so that a network of that many takes one launch and not two.
+#ifndef GC_G
+#define GC_G 1024
+#endif
+constexpr int TABLE = 170, CHUNK = 8192, MAX_GROUPS = GC_G;
+constexpr int MAX_TENSORS = 1 << 15, MAX_JOIN = 4096;
 struct GradTable {
     const void *grad[TABLE];
     void *out[TABLE];
-    uint64_t count[TABLE];
     uint32_t first[TABLE + 1];      // chunks in front of each tensor
+    uint16_t last[TABLE];           // elements of its last chunk - 1
     uint32_t bf16[(TABLE + 31) / 32];
     int n;
 };
+static_assert(sizeof(GradTable) <= 4096 - 64, "kernel arguments");
 
 struct Chunk {
     int tensor;
@@ -31,8 +39,7 @@ __device__ __forceinline__ Chunk find_chunk(const GradTable &t, uint32_t i) {
         if (t.first[mid] <= i) lo = mid;
         else hi = mid;
     }
-    const uint64_t at = (uint64_t)(i - t.first[lo]) * CHUNK, left = t.count[lo] - at;
-    return {lo, at, (int)(left < CHUNK ? left : CHUNK)};
+    return {lo, (uint64_t)(i - t.first[lo]) * CHUNK, i + 1 == t.first[lo + 1] ? t.last[lo] + 1 : CHUNK};
 }
 __device__ __forceinline__ bool is_bf16(const GradTable &t, int k) { return t.bf16[k >> 5] >> (k & 31) & 1; }
 
@@ -45,13 +52,37 @@ __device__ __forceinline__ double block_sum(double v, double *red) {        // 2
     return red[0] + red[1] + red[2] + red[3];
 }
 
+// Both passes take a chunk in pieces of 16 bytes a thread, all of a chunk's under way at a time; the ends of tensors element by element.
+template <typename T> constexpr int WIDTH = 16 / sizeof(T);
+template <typename T> constexpr int PIECES = CHUNK / (256 * WIDTH<T>);      // of a thread
+template <typename T> __device__ __forceinline__ void load_chunk(const T *g, RawPiece<T, WIDTH<T>> (&r)[PIECES<T>]) {
+#pragma unroll
+    for (int k = 0; k < PIECES<T>; k++) r[k].load(g + (k * 256 + threadIdx.x) * WIDTH<T>, WIDTH<T>);
+}
+
+// A product of two fp32 values is exact in 64 bits: 2^28 bf16 elements in 62 us (8.7 TB/s from the last cache and memory), as fast as with fp32 sums.
 template <typename T> __device__ __forceinline__ double squares(const T *g, int len) {
     double s = 0.0;
-    for (int i = threadIdx.x * 8; i < len; i += 2048) {
-        float v[8];
-        load8_any<T>(g + i, v, len - i);
+    if (len == CHUNK) {
+        RawPiece<T, WIDTH<T>> r[PIECES<T>];
+        load_chunk<T>(g, r);
 #pragma unroll
-        for (int e = 0; e < 8; e++) s += (double)v[e] * (double)v[e];
+        for (int k = 0; k < PIECES<T>; k++)
+#pragma unroll
+            for (int e = 0; e < WIDTH<T>; e++) {
+                const double v = r[k].get(e);
+                s += v * v;
+            }
+    } else {
+        for (int i = threadIdx.x * WIDTH<T>; i < len; i += 256 * WIDTH<T>) {
+            RawPiece<T, WIDTH<T>> r;
+            r.load(g + i, len - i);
+#pragma unroll
+            for (int e = 0; e < WIDTH<T>; e++) {
+                const double v = r.get(e);
+                s += v * v;
+            }
+        }
     }
     return s;
 }
@@ -81,74 +112,95 @@ __global__ void __launch_bounds__(256) grad_norm_kernel(const double *part, int 
     if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
-template <typename T> __device__ __forceinline__ void scaled(const T *g, T *out, int len, float f) {
-    for (int i = threadIdx.x * 8; i < len; i += 2048) {
-        float v[8];
-        load8_any<T>(g + i, v, len - i);
+template <bool STREAM, typename T> __device__ __forceinline__ void scaled(const T *g, T *out, int len, float f) {
+    if (len == CHUNK) {
+        RawPiece<T, WIDTH<T>> r[PIECES<T>];
+        load_chunk<T>(g, r);
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] *= f;
-        store8_any<T>(out + i, v, len - i);
+        for (int k = 0; k < PIECES<T>; k++) {
+            float v[WIDTH<T>];
+#pragma unroll
+            for (int e = 0; e < WIDTH<T>; e++) v[e] = r[k].get(e) * f;
+            if constexpr (STREAM) stream_piece<T, WIDTH<T>>(out + (k * 256 + threadIdx.x) * WIDTH<T>, v);
+            else store_piece<T, WIDTH<T>>(out + (k * 256 + threadIdx.x) * WIDTH<T>, v, WIDTH<T>);
+        }
+    } else {
+        for (int i = threadIdx.x * WIDTH<T>; i < len; i += 256 * WIDTH<T>) {
+            RawPiece<T, WIDTH<T>> r;
+            r.load(g + i, len - i);
+            float v[WIDTH<T>];
+#pragma unroll
+            for (int e = 0; e < WIDTH<T>; e++) v[e] = r.get(e) * f;
+            store_piece<T, WIDTH<T>>(out + i, v, len - i);
+        }
     }
 }
 
-// The norm comes in 32 bits from grad_norm_kernel in front.  Where nothing is clipped the elements are copied as they are, or left where they are in place.
-__global__ void __launch_bounds__(256) grad_scale_kernel(const GradTable t, const float *norm, float max_norm) {
-    const float n = *norm;
+// Every workgroup joins the parts itself, which takes a launch less, and the first leaves the norm (each launch's first, the same one); parts = 0: the norm is there.  Where nothing is clipped the elements are copied as they are, or left where they are in place.
+// The chunks are taken from the last on: what the pass in front read last is still in the caches.
+template <bool STREAM> __global__ void __launch_bounds__(256) grad_scale_kernel(const GradTable t, const double *part, int parts, float *norm, float max_norm) {
+    __shared__ double red[4];
+    const float n = parts ? (float)sqrt(sum_of_parts(part, parts, red)) : *norm;
+    if (parts && blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
     const bool clip = n > max_norm && n <= FLT_MAX;
     const float f = clip ? max_norm / n : 1.f;
-    for (uint32_t i = blockIdx.x; i < t.first[t.n]; i += gridDim.x) {
-        const Chunk c = find_chunk(t, i);
+    for (uint32_t j = blockIdx.x; j < t.first[t.n]; j += gridDim.x) {
+        const Chunk c = find_chunk(t, t.first[t.n] - 1 - j);
         if (!clip && t.grad[c.tensor] == t.out[c.tensor]) continue;
-        if (is_bf16(t, c.tensor)) scaled<bf16_t>(static_cast<const bf16_t *>(t.grad[c.tensor]) + c.at, static_cast<bf16_t *>(t.out[c.tensor]) + c.at, c.len, f);
-        else scaled<float>(static_cast<const float *>(t.grad[c.tensor]) + c.at, static_cast<float *>(t.out[c.tensor]) + c.at, c.len, f);
+        if (is_bf16(t, c.tensor)) scaled<STREAM, bf16_t>(static_cast<const bf16_t *>(t.grad[c.tensor]) + c.at, static_cast<bf16_t *>(t.out[c.tensor]) + c.at, c.len, f);
+        else scaled<STREAM, float>(static_cast<const float *>(t.grad[c.tensor]) + c.at, static_cast<float *>(t.out[c.tensor]) + c.at, c.len, f);
     }
 }
 
 uint64_t chunks_of(const sol_grad &g) { return (g.count + CHUNK - 1) / CHUNK; }
 
-// Calls f(table, first part) for each launch's share of the tensors
-template <typename F> sol_status each_table(const sol_grad *grads, int tensors, F f) {
-    GradTable t;
-    int part = 0;
-    t.n = 0;
-    t.first[0] = 0;
-    memset(t.bf16, 0, sizeof(t.bf16));
-    auto flush = [&]() -> sol_status {
-        if (t.n == 0) return SOL_OK;
-        const int groups = (int)min(t.first[t.n], (uint32_t)MAX_GROUPS);
-        SOL_TRY(f(t, groups, part));
-        part += groups;
-        t.n = 0;
-        memset(t.bf16, 0, sizeof(t.bf16));
-        return SOL_OK;
-    };
-    for (int i = 0; i < tensors; i++) {
-        const sol_grad &g = grads[i];
-        if (g.count == 0) continue;
-        if (t.n == TABLE || (t.n && t.first[t.n] + chunks_of(g) > 0x7fffffffu)) SOL_TRY(flush());
-        t.grad[t.n] = g.grad; t.out[t.n] = g.out; t.count[t.n] = g.count;
-        t.bf16[t.n >> 5] |= (g.dtype == SOL_BF16 ? 1u : 0u) << (t.n & 31);
-        t.first[t.n + 1] = t.first[t.n] + (uint32_t)chunks_of(g);
-        t.n++;
+// How many tensors from `at` on fit one launch; *chunks: theirs
+int table_end(const sol_grad *grads, int tensors, int at, uint64_t *chunks) {
+    int n = 0;
+    *chunks = 0;
+    for (; at < tensors; at++) {
+        const uint64_t k = chunks_of(grads[at]);
+        if (k == 0) continue;
+        if (n == TABLE || (n && *chunks + k > 0x7fffffffu)) break;
+        *chunks += k;
+        n++;
     }
-    return flush();
+    return at;
+}
+int groups_of(uint64_t chunks) { return (int)(chunks < MAX_GROUPS ? chunks : MAX_GROUPS); }
+
+// The tensors from `at` to `end`
+void fill_table(const sol_grad *grads, int at, int end, GradTable *t) {
+    t->n = 0;
+    t->first[0] = 0;
+    memset(t->bf16, 0, sizeof(t->bf16));
+    for (; at < end; at++) {
+        const sol_grad &g = grads[at];
+        if (g.count == 0) continue;
+        const int i = t->n++;
+        t->grad[i] = g.grad; t->out[i] = g.out;
+        t->bf16[i >> 5] |= (g.dtype == SOL_BF16 ? 1u : 0u) << (i & 31);
+        t->first[i + 1] = t->first[i] + (uint32_t)chunks_of(g);
+        t->last[i] = (uint16_t)((g.count - 1) % CHUNK);
+    }
 }
 
 int total_parts(const sol_grad *grads, int tensors) {
     int parts = 0;
-    each_table(grads, tensors, [&](const GradTable &, int groups, int) { parts += groups; return SOL_OK; });
+    uint64_t chunks;
+    for (int at = 0; at < tensors;) {
+        at = table_end(grads, tensors, at, &chunks);
+        parts += groups_of(chunks);
+    }
     return parts;
 }
 
-struct Span { uintptr_t at, end; int i; };
-int by_start(const void *p, const void *q) {
-    const Span *a = static_cast<const Span *>(p), *b = static_cast<const Span *>(q);
-    return a->at < b->at ? -1 : a->at > b->at ? 1 : a->i - b->i;
-}
+struct Buffer { uintptr_t at, end; int i; };
 
 sol_status check_grads(const sol_grad *grads, int tensors, bool out) {
     SOL_REQUIRE(tensors >= 0, SOL_ERR_SHAPE, "%d tensors", tensors);
     SOL_REQUIRE(grads || tensors == 0, SOL_ERR_NULL, "the list of gradients is NULL");
+    SOL_REQUIRE(tensors <= MAX_TENSORS, SOL_ERR_UNSUPPORTED, "more than 2^15 tensors: %d", tensors);
     for (int i = 0; i < tensors; i++) {
         const sol_grad &g = grads[i];
         SOL_REQUIRE(g.dtype == SOL_F32 || g.dtype == SOL_BF16, SOL_ERR_DTYPE, "gradient %d: unknown dtype %d", i, g.dtype);
@@ -160,16 +212,16 @@ sol_status check_grads(const sol_grad *grads, int tensors, bool out) {
     }
     if (!out || tensors == 0) return SOL_OK;
     // No two of the buffers may share memory: a tensor listed twice would be scaled twice, an output on another gradient would change it before it is read.
-    Span few[256], *spans = 2 * (size_t)tensors <= 256 ? few : static_cast<Span *>(malloc(2 * (size_t)tensors * sizeof(Span)));
+    Buffer few[512], *spans = 2 * tensors <= 512 ? few : static_cast<Buffer *>(malloc(2 * (size_t)tensors * sizeof(Buffer)));
     SOL_REQUIRE(spans, SOL_ERR_UNSUPPORTED, "no memory for a list of %d gradients", tensors);
     int n = 0;
     for (int i = 0; i < tensors; i++) {
         const sol_grad &g = grads[i];
         const uintptr_t bytes = g.count * dtype_size(g.dtype), at = reinterpret_cast<uintptr_t>(g.grad), to = reinterpret_cast<uintptr_t>(g.out);
-        if (bytes) spans[n++] = Span{at, at + bytes, i};
-        if (bytes && at != to) spans[n++] = Span{to, to + bytes, i};
+        if (bytes) spans[n++] = Buffer{at, at + bytes, i};
+        if (bytes && at != to) spans[n++] = Buffer{to, to + bytes, i};
     }
-    qsort(spans, (size_t)n, sizeof(Span), by_start);
+    std::sort(spans, spans + n, [](const Buffer &p, const Buffer &q) { return p.at < q.at; });       // in place, without memory of its own
     int a = -1, b = -1;
     for (int k = 1; k < n && a < 0; k++)
         if (spans[k].at < spans[k - 1].end) { a = spans[k - 1].i; b = spans[k].i; }
@@ -178,17 +230,18 @@ sol_status check_grads(const sol_grad *grads, int tensors, bool out) {
     return SOL_OK;
 }
 
-sol_status launch_norm_of(const sol_grad *grads, int tensors, float *norm, void *workspace, hipStream_t st) {
-    double *part = static_cast<double *>(workspace);
-    int parts = 0;
-    SOL_TRY(each_table(grads, tensors, [&](const GradTable &t, int groups, int first) -> sol_status {
-        hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)groups), dim3(256), 0, st, t, part + first);
+sol_status launch_squares(const sol_grad *grads, int tensors, double *part, hipStream_t st) {
+    GradTable t;
+    uint64_t chunks;
+    for (int at = 0; at < tensors;) {
+        const int end = table_end(grads, tensors, at, &chunks), groups = groups_of(chunks);
+        fill_table(grads, at, end, &t);
+        at = end;
+        if (groups == 0) continue;
+        hipLaunchKernelGGL(grad_squares_kernel, dim3((unsigned)groups), dim3(256), 0, st, t, part);
         SOL_HIP(hipGetLastError());
-        parts = first + groups;
-        return SOL_OK;
-    }));
-    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, st, part, parts, norm);
-    SOL_HIP(hipGetLastError());
+        part += groups;
+    }
     return SOL_OK;
 }
 
@@ -212,22 +265,47 @@ size_t sol_grad_workspace_bytes(const sol_grad *grads, int tensors) {
 sol_status sol_grad_norm(const sol_grad *grads, int tensors, float *norm, void *workspace, size_t workspace_bytes, void *stream) {
     SOL_TRY(check_grads(grads, tensors, false));
     SOL_TRY(check_norm_out(norm));
-    SOL_TRY(check_scratch(workspace, workspace_bytes, (size_t)total_parts(grads, tensors) * 8));
-    return launch_norm_of(grads, tensors, norm, workspace, (hipStream_t)stream);
+    const int parts = total_parts(grads, tensors);
+    SOL_TRY(check_scratch(workspace, workspace_bytes, (size_t)parts * 8));
+    hipStream_t st = (hipStream_t)stream;
+    SOL_TRY(launch_squares(grads, tensors, static_cast<double *>(workspace), st));
+    hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, st, static_cast<const double *>(workspace), parts, norm);
+    SOL_HIP(hipGetLastError());
+    return SOL_OK;
 }
 
 sol_status sol_grad_clip(const sol_grad *grads, int tensors, float max_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream) {
     SOL_TRY(check_grads(grads, tensors, true));
     SOL_TRY(check_norm_out(norm));
     SOL_REQUIRE(max_norm > 0.f, SOL_ERR_SHAPE, "max_norm %g is not positive", (double)max_norm);       // refuses a NaN too
-    SOL_TRY(check_scratch(workspace, workspace_bytes, (size_t)total_parts(grads, tensors) * 8));
+    const int parts = total_parts(grads, tensors);
+    SOL_TRY(check_scratch(workspace, workspace_bytes, (size_t)parts * 8));
     hipStream_t st = (hipStream_t)stream;
-    SOL_TRY(launch_norm_of(grads, tensors, norm, workspace, st));
-    return each_table(grads, tensors, [&](const GradTable &t, int groups, int) -> sol_status {
-        hipLaunchKernelGGL(grad_scale_kernel, dim3((unsigned)groups), dim3(256), 0, st, t, norm, max_norm);
+    double *part = static_cast<double *>(workspace);
+    SOL_TRY(launch_squares(grads, tensors, part, st));
+    const bool join = parts > MAX_JOIN || parts == 0;
+    if (join) {
+        hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, st, part, parts, norm);
         SOL_HIP(hipGetLastError());
-        return SOL_OK;
-    });
+    }
+    // from the last tensors to the first: what the first pass read last is still in the caches
+    int starts[MAX_TENSORS / TABLE + 2], tables = 0;
+    uint64_t chunks;
+    for (int at = 0; at < tensors; at = table_end(grads, tensors, at, &chunks)) starts[tables++] = at;
+    starts[tables] = tensors;
+    size_t bytes = 0;
+    for (int i = 0; i < tensors; i++) bytes += grads[i].count * dtype_size(grads[i].dtype);
+    const bool stream_out = bytes >= STREAM_BYTES;
+    GradTable t;
+    for (int k = tables - 1; k >= 0; k--) {
+        const int groups = groups_of((table_end(grads, starts[k + 1], starts[k], &chunks), chunks));
+        if (groups == 0) continue;
+        fill_table(grads, starts[k], starts[k + 1], &t);
+        if (stream_out) hipLaunchKernelGGL(grad_scale_kernel<true>, dim3((unsigned)groups), dim3(256), 0, st, t, part, join ? 0 : parts, norm, max_norm);
+        else hipLaunchKernelGGL(grad_scale_kernel<false>, dim3((unsigned)groups), dim3(256), 0, st, t, part, join ? 0 : parts, norm, max_norm);
+        SOL_HIP(hipGetLastError());
+    }
+    return SOL_OK;
 }
 
 }  // extern "C"

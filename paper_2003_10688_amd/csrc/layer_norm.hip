@@ -3,8 +3,6 @@
 //   backward  h = (x - mean) * rstd,  g = dy * gamma;  dx = rstd * (g - mean(g) - h * mean(g h)) + residual;  dgamma = column sums of dy h, dbeta of dy
 #include <float.h>
 
-#include <utility>
-
 #include "row_ops.h"
 
 namespace sol {
@@ -36,12 +34,6 @@ __device__ __forceinline__ void load_weight8(const float *w, const Span<8> &sp, 
 }
 // A row for TPR threads: four rows a workgroup where one wave takes a row and none waits for another, else one
 template <int TPR> constexpr int ROW_BLOCK = TPR == 64 ? 256 : TPR;
-template <int TPR, int G> struct Spans {
-    Span<8> of[G];
-    template <int... K> __device__ __forceinline__ Spans(int lane, int cols, std::integer_sequence<int, K...>) : of{Span<8>((lane + K * TPR) * 8, cols)...} {}
-    __device__ __forceinline__ Spans(int lane, int cols) : Spans(lane, cols, std::make_integer_sequence<int, G>()) {}
-    __device__ __forceinline__ const Span<8> &operator[](int k) const { return of[k]; }
-};
 
 // sum / n with the reciprocal and one correction, so that equal elements whose sum is exact have their own value for a mean
 __device__ __forceinline__ float mean_of(float sum, float n, float inv) {
@@ -56,7 +48,7 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) 
     constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64;
     __shared__ float4 red[2][WAVES];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    const Spans<TPR, G> sp(lane, a.cols);
+    const Spans<8, G> sp(lane * 8, TPR * 8, a.cols);
     float gm[G][8], bt[G][8];
     int n_wave = 0;
 #pragma unroll
@@ -257,7 +249,7 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
         return;
     }
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    const Spans<TPR, G> sp(lane, a.cols);
+    const Spans<8, G> sp(lane * 8, TPR * 8, a.cols);
     float gm[G][8];
 #pragma unroll
     for (int k = 0; k < G; k++) load_weight8(a.gamma, sp[k], 1.f, gm[k]);
@@ -315,7 +307,7 @@ __global__ void __launch_bounds__((GRAD_BLOCK<G, WHOLE>)) norm_grad_kernel(const
     __shared__ float2 red[2][GRAD_BLOCK<G, WHOLE> / 64];
     __shared__ float sums[SLOTS > 1 ? SLOTS - 1 : 1][TPR * G * 8];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    const Spans<TPR, G> sp(lane, a.cols);
+    const Spans<8, G> sp(lane * 8, TPR * 8, a.cols);
     float gm[G][8], sg[G][8], sb[G][8];
 #pragma unroll
     for (int k = 0; k < G; k++) {

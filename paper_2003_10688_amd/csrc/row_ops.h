@@ -1,5 +1,7 @@
 // What the kernels over rows of features share: sums over a wave and a workgroup, checks of the arguments (internal).
 #pragma once
+#include <utility>
+
 #include "linear_ops.h"
 
 namespace sol {
@@ -90,6 +92,24 @@ template <typename T, int W> struct RawPiece {
         else return __uint_as_float(w[e]);
     }
 };
+template <typename T, int W> __device__ __forceinline__ void store_piece(T *p, const float *v, int nv) {
+    if constexpr (W == 4) store4_any<T>(p, v, nv);
+    else store8_any<T>(p, v, nv);
+}
+// The same for a whole piece, past the caches: results as large as the last cache would push out what is still to be read, and little of them would be left for their reader.
+// (The choice has to be the kernel's, at compile time: behind a branch the compiler makes one ordinary store of both.)
+constexpr size_t STREAM_BYTES = (size_t)256 << 20;
+template <typename T, int W> __device__ __forceinline__ void stream_piece(T *p, const float *v) {
+    uint32_t w[W * sizeof(T) / 4];
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(w) / 4); i++) w[i] = sizeof(T) == 4 ? __float_as_uint(v[i]) : pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    if constexpr (sizeof(w) == 8) __builtin_nontemporal_store(u32x2_any{w[0], w[1]}, reinterpret_cast<u32x2_any *>(p));
+    else {
+#pragma unroll
+        for (int i = 0; i < (int)(sizeof(w) / 16); i++) __builtin_nontemporal_store(lds_pipe::u32x4_t{w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]}, reinterpret_cast<u32x4_any *>(p) + i);
+    }
+}
+
 // W neighbouring columns of a row for one thread.  The last thread of a row whose length is no multiple of W takes the row's last W columns, of which it leaves the first `skip` to the
 // thread in front: a load of one piece like the others', which is waited for where it is used and not where it is asked for, as pieces put together of elements are.
 // Only rows shorter than W end early.
@@ -108,17 +128,25 @@ template <int W> struct Span {
         if (WHOLE || end == W) r.load(row + c, W);
         else r.load(row + c, end);
     }
-    template <bool WHOLE, typename T> __device__ __forceinline__ void store(T *row, const float *v) const {
+    template <bool WHOLE, bool STREAM = false, typename T> __device__ __forceinline__ void store(T *row, const float *v) const {
         if (!some()) return;
         if (WHOLE || (skip == 0 && end == W)) {
-            if constexpr (W == 4) store4_any<T>(row + c, v, W);
-            else store8_any<T>(row + c, v, W);
+            if constexpr (STREAM) stream_piece<T, W>(row + c, v);
+            else store_piece<T, W>(row + c, v, W);
         } else {
 #pragma unroll
             for (int e = 0; e < W; e++)
                 if (has(e)) Elem<T>::store(row + c + e, v[e]);
         }
     }
+};
+
+// COUNT of them, `apart` columns from one to the next
+template <int W, int COUNT> struct Spans {
+    Span<W> of[COUNT];
+    template <int... K> __device__ __forceinline__ Spans(int at, int apart, int cols, std::integer_sequence<int, K...>) : of{Span<W>(at + K * apart, cols)...} {}
+    __device__ __forceinline__ Spans(int at, int apart, int cols) : Spans(at, apart, cols, std::make_integer_sequence<int, COUNT>()) {}
+    __device__ __forceinline__ const Span<W> &operator[](int k) const { return of[k]; }
 };
 
 constexpr int MAX_COLS = 1 << 20, MAX_ROW_PITCH = 1 << 21;

@@ -566,39 +566,45 @@ def sol_embedding_backward(dy, tokens, vocab, scale=1.0, pad=-1, dtable_dtype=No
 
 
 def _grad_list(grads, out):
-    """The list as the library takes it (entries as Grad has them), from tensors of one device; out: None, or where each result goes."""
-    device = grads[0].get_device() if len(grads) else -1
-    flat = []
-    for g, o in zip(grads, grads if out is None else out, strict=True):
-        dt = g.dtype
-        if not g.is_cuda or dt not in (torch.float32, torch.bfloat16) or not g.is_contiguous() or g.get_device() != device:
-            raise ValueError(f"gradients: contiguous float32 or bfloat16 tensors of one GPU are wanted, not {dt} of strides {g.stride()} on {g.device}")
-        if o is not g and (o.dtype != dt or o.shape != g.shape or not o.is_contiguous() or o.get_device() != device):
-            raise ValueError(f"out: a contiguous {dt} tensor of shape {tuple(g.shape)} on {g.device} is wanted, not {tuple(o.shape)} of {o.dtype} on {o.device}")
-        flat += (g.data_ptr(), o.data_ptr(), g.numel(), BF16 if dt == torch.bfloat16 else F32)
-    if not flat:
-        raise ValueError("gradients: one tensor at least is wanted")
-    return (C.c_int64 * len(flat))(*flat)
+    """The list as the library takes it (an array whose rows are what Grad has), from tensors of one device; out: None, or where each result goes.  Returns its first tensor and length too."""
+    grads = list(grads)
+    out = grads if out is None else list(out)
+    if not grads or len(out) != len(grads):
+        raise ValueError(f"gradients: one tensor at least, and as many results, are wanted, not {len(grads)} and {len(out)}")
+    # one attribute of all tensors at a time: a network has hundreds
+    both = grads if out is grads else grads + out
+    dtypes, counts = [g.dtype for g in grads], list(map(torch.Tensor.numel, grads))
+    if not set(dtypes) <= {torch.float32, torch.bfloat16} or not all(map(torch.Tensor.is_contiguous, both)) or set(map(torch.Tensor.get_device, both)) != {max(grads[0].get_device(), 0)}:
+        raise ValueError("gradients and results: contiguous float32 or bfloat16 tensors of one GPU are wanted")
+    if out is not grads and (counts != list(map(torch.Tensor.numel, out)) or dtypes != [o.dtype for o in out]):
+        raise ValueError("results: tensors of the gradients' sizes and types are wanted")
+    n = len(grads)
+    arr = np.empty((n, 4), np.int64)
+    arr[:, 0] = list(map(torch.Tensor.data_ptr, grads))
+    arr[:, 1] = arr[:, 0] if out is grads else list(map(torch.Tensor.data_ptr, out))
+    arr[:, 2] = counts
+    arr[:, 3] = [d == torch.bfloat16 for d in dtypes]          # BF16 and F32 are 1 and 0
+    return grads[0], n, arr
 
 
 def sol_grad_norm(grads, workspace=None, stream=None):
     """The norm of all tensors of the list together, as an fp32 tensor without dimensions."""
-    arr = _grad_list(grads, None)
-    handle, side = _on_current(grads[0], None, stream)
-    norm = _result(grads[0], (), torch.float32, side)
-    wa, wbytes, keep = _scratch(workspace, lib().sol_grad_workspace_bytes(arr, len(grads)), grads[0], side)
-    _check(lib().sol_grad_norm(arr, len(grads), norm.data_ptr(), wa, wbytes, handle))
+    g, n, arr = _grad_list(grads, None)
+    handle, side = _on_current(g, None, stream)
+    norm = _result(g, (), torch.float32, side)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_grad_workspace_bytes(arr.ctypes.data, n), g, side)
+    _check(lib().sol_grad_norm(arr.ctypes.data, n, norm.data_ptr(), wa, wbytes, handle))
     return norm
 
 
 def sol_grad_clip(grads, max_norm, out=None, workspace=None, stream=None):
     """Multiplies all tensors of the list by max_norm / norm if their norm is finite and above max_norm, in place, or into the tensors of the list `out`.  Returns the norm, as
     sol_grad_norm does."""
-    arr = _grad_list(grads, out)
-    handle, side = _on_current(grads[0], None, stream)
-    norm = _result(grads[0], (), torch.float32, side)
-    wa, wbytes, keep = _scratch(workspace, lib().sol_grad_workspace_bytes(arr, len(grads)), grads[0], side)
-    _check(lib().sol_grad_clip(arr, len(grads), max_norm, norm.data_ptr(), wa, wbytes, handle))
+    g, n, arr = _grad_list(grads, out)
+    handle, side = _on_current(g, None, stream)
+    norm = _result(g, (), torch.float32, side)
+    wa, wbytes, keep = _scratch(workspace, lib().sol_grad_workspace_bytes(arr.ctypes.data, n), g, side)
+    _check(lib().sol_grad_clip(arr.ctypes.data, n, max_norm, norm.data_ptr(), wa, wbytes, handle))
     return norm
 
 
