@@ -27,10 +27,11 @@ __device__ __forceinline__ void load_weight8(const float *w, int c, int nv, floa
     }
 }
 // of a span; 0 in the places that are not the thread's own
-__device__ __forceinline__ void load_weight8(const float *w, const Span<8> &sp, float none, float v[8]) {
-    load_weight8(w, sp.c, sp.some() ? sp.end : 0, none, v);
+template <int W> __device__ __forceinline__ void load_weight(const float *w, const Span<W> &sp, float none, float v[W]) {
+    RawPiece<float, W> raw;
+    if (w) sp.template load<false>(w, raw);
 #pragma unroll
-    for (int e = 0; e < 8; e++) v[e] = sp.has(e) ? v[e] : 0.f;
+    for (int e = 0; e < W; e++) v[e] = !sp.has(e) ? 0.f : w ? raw.get(e) : none;
 }
 // A row for TPR threads: four rows a workgroup where one wave takes a row and none waits for another, else one
 template <int TPR> constexpr int ROW_BLOCK = TPR == 64 ? 256 : TPR;
@@ -43,40 +44,40 @@ __device__ __forceinline__ float mean_of(float sum, float n, float inv) {
 
 // Means and squared deviations of the waves, put together: mean = sum n_w mean_w / n, deviations = sum (d_w + n_w (mean_w - mean)^2) (Chan, Golub, LeVeque).
 // One barrier a row; two sets of slots in turn, so that the next row's values do not meet readers of this one's.
-template <int TPR, int G, bool WHOLE, typename T>
+template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
 __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) {
-    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64;
+    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64, W = 16 / sizeof(T), P = G * 8 / W;
     __shared__ float4 red[2][WAVES];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    const Spans<8, G> sp(lane * 8, TPR * 8, a.cols);
-    float gm[G][8], bt[G][8];
+    const Spans<W, P> sp(lane * W, TPR * W, a.cols);
+    float gm[P][W], bt[P][W];
     int n_wave = 0;
 #pragma unroll
-    for (int k = 0; k < G; k++) {
-        load_weight8(a.gamma, sp[k], 1.f, gm[k]);
-        load_weight8(a.beta, sp[k], 0.f, bt[k]);
-        n_wave += max(0, min(512, a.cols - (lane / 64 * 64 + k * TPR) * 8));
+    for (int k = 0; k < P; k++) {
+        load_weight(a.gamma, sp[k], 1.f, gm[k]);
+        load_weight(a.beta, sp[k], 0.f, bt[k]);
+        n_wave += max(0, min(64 * W, a.cols - (lane / 64 * 64 + k * TPR) * W));
     }
     const float inv_wave = n_wave ? 1.f / (float)n_wave : 0.f;
     int phase = 0;
     for (long row = (long)blockIdx.x * RPB + slot; row < a.rows; row += (long)gridDim.x * RPB) {      // with TPR > 64 a workgroup has one row at a time: every thread meets every barrier
         const T *x = static_cast<const T *>(a.x) + row * a.ldx;
-        float v[G][8], s = 0.f;
+        float v[P][W], s = 0.f;
 #pragma unroll
-        for (int k = 0; k < G; k++) {
-            RawPiece<T, 8> raw;
+        for (int k = 0; k < P; k++) {
+            RawPiece<T, W> raw;
             sp[k].template load<WHOLE>(x, raw);
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
+            for (int e = 0; e < W; e++) {
                 v[k][e] = raw.get(e);
                 s += WHOLE || sp[k].has(e) ? v[k][e] : 0.f;     // zeros where there is nothing
             }
         }
         float mean = mean_of(wave_sum(s), (float)n_wave, inv_wave), m2 = 0.f;
 #pragma unroll
-        for (int k = 0; k < G; k++)
+        for (int k = 0; k < P; k++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
+            for (int e = 0; e < W; e++) {
                 const float d = (WHOLE ? sp[k].some() : sp[k].has(e)) ? v[k][e] - mean : 0.f;
                 m2 += d * d;
             }
@@ -99,10 +100,10 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) 
         const float rstd = __builtin_amdgcn_rsqf(m2 * a.inv_cols + a.eps);
         T *y = static_cast<T *>(a.y) + row * a.ldy;
 #pragma unroll
-        for (int k = 0; k < G; k++) {
+        for (int k = 0; k < P; k++) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[k][e] = (v[k][e] - mean) * rstd * gm[k][e] + bt[k][e];
-            sp[k].template store<WHOLE>(y, v[k]);
+            for (int e = 0; e < W; e++) v[k][e] = (v[k][e] - mean) * rstd * gm[k][e] + bt[k][e];
+            sp[k].template store<WHOLE, STREAM>(y, v[k]);
         }
         if (lane == 0) {
             if (a.mean) a.mean[row] = mean;
@@ -225,21 +226,21 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_columns_kerne
 }
 
 // The row's part of the backward pass, from g = dy gamma and h: gamma, and so g, is 0 in places that are not the thread's own
-template <int G> __device__ __forceinline__ void row_products(const float (&g)[G][8], const float (&h)[G][8], float &s1, float &s2) {
+template <int P, int W> __device__ __forceinline__ void row_products(const float (&g)[P][W], const float (&h)[P][W], float &s1, float &s2) {
     s1 = s2 = 0.f;
 #pragma unroll
-    for (int k = 0; k < G; k++)
+    for (int k = 0; k < P; k++)
 #pragma unroll
-        for (int e = 0; e < 8; e++) {
+        for (int e = 0; e < W; e++) {
             s1 += g[k][e];
             s2 += g[k][e] * h[k][e];
         }
 }
 
 // dx, a row for TPR threads; the workgroups in front sum the columns where there are few rows, so that both take one launch: the data is read twice, but the second time from the caches
-template <int TPR, int G, bool WHOLE, typename T>
+template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
 __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs a, const NormColumns cols) {
-    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64;
+    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64, W = 16 / sizeof(T), P = G * 8 / W;
     __shared__ union {
         float columns[2][BLOCK / 8][64 + 4];
         float2 red[2][WAVES];
@@ -249,27 +250,27 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
         return;
     }
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    const Spans<8, G> sp(lane * 8, TPR * 8, a.cols);
-    float gm[G][8];
+    const Spans<W, P> sp(lane * W, TPR * W, a.cols);
+    float gm[P][W];
 #pragma unroll
-    for (int k = 0; k < G; k++) load_weight8(a.gamma, sp[k], 1.f, gm[k]);
+    for (int k = 0; k < P; k++) load_weight(a.gamma, sp[k], 1.f, gm[k]);
     int phase = 0;
     for (long row = (long)(blockIdx.x - cols.blocks) * RPB + slot; row < a.rows; row += (long)(gridDim.x - cols.blocks) * RPB) {
         const T *x = static_cast<const T *>(a.x) + row * a.ldx, *dy = static_cast<const T *>(a.dy) + row * a.ldy;
         const float mean = a.mean_in[row], rstd = a.rstd_in[row];
-        float h[G][8], g[G][8], s1, s2;
+        float h[P][W], g[P][W], s1, s2;
 #pragma unroll
-        for (int k = 0; k < G; k++) {
-            RawPiece<T, 8> rx, ry;
+        for (int k = 0; k < P; k++) {
+            RawPiece<T, W> rx, ry;
             sp[k].template load<WHOLE>(x, rx);
             sp[k].template load<WHOLE>(dy, ry);
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
+            for (int e = 0; e < W; e++) {
                 h[k][e] = (rx.get(e) - mean) * rstd;
                 g[k][e] = ry.get(e) * gm[k][e];
             }
         }
-        row_products<G>(g, h, s1, s2);
+        row_products(g, h, s1, s2);
         s1 = wave_sum(s1);
         s2 = wave_sum(s2);
         if constexpr (WAVES > 1) {
@@ -283,16 +284,16 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
         const float c1 = s1 * a.inv_cols, c2 = s2 * a.inv_cols;
         const size_t out = (size_t)row * a.cols;
 #pragma unroll
-        for (int k = 0; k < G; k++) {
+        for (int k = 0; k < P; k++) {
 #pragma unroll
-            for (int e = 0; e < 8; e++) g[k][e] = rstd * (g[k][e] - c1 - h[k][e] * c2);
+            for (int e = 0; e < W; e++) g[k][e] = rstd * (g[k][e] - c1 - h[k][e] * c2);
             if (a.residual) {       // dx may be in its place: a thread uses its own elements alone
-                RawPiece<T, 8> res;
+                RawPiece<T, W> res;
                 sp[k].template load<WHOLE>(static_cast<const T *>(a.residual) + out, res);
 #pragma unroll
-                for (int e = 0; e < 8; e++) g[k][e] += res.get(e);
+                for (int e = 0; e < W; e++) g[k][e] += res.get(e);
             }
-            sp[k].template store<WHOLE>(static_cast<T *>(a.y) + out, g[k]);
+            sp[k].template store<WHOLE, STREAM>(static_cast<T *>(a.y) + out, g[k]);
         }
     }
 }
@@ -301,26 +302,26 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
 // registers; parts [workgroup][cols] at the end.
 // Threads of a workgroup: 1024 where 128 registers hold a thread's share, so that fewer workgroups fill the GPU and fewer parts are left
 template <int G, bool WHOLE> constexpr int GRAD_BLOCK = G == 1 && WHOLE ? 1024 : 512;
-template <int TPR, int G, bool WHOLE, typename T>
+template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
 __global__ void __launch_bounds__((GRAD_BLOCK<G, WHOLE>)) norm_grad_kernel(const NormArgs a, float *dgamma, float *dbeta) {
-    constexpr int SLOTS = GRAD_BLOCK<G, WHOLE> / TPR, WAVES = TPR / 64;
+    constexpr int SLOTS = GRAD_BLOCK<G, WHOLE> / TPR, WAVES = TPR / 64, W = 16 / sizeof(T), P = G * 8 / W;
     __shared__ float2 red[2][GRAD_BLOCK<G, WHOLE> / 64];
     __shared__ float sums[SLOTS > 1 ? SLOTS - 1 : 1][TPR * G * 8];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
-    const Spans<8, G> sp(lane * 8, TPR * 8, a.cols);
-    float gm[G][8], sg[G][8], sb[G][8];
+    const Spans<W, P> sp(lane * W, TPR * W, a.cols);
+    float gm[P][W], sg[P][W], sb[P][W];
 #pragma unroll
-    for (int k = 0; k < G; k++) {
-        load_weight8(a.gamma, sp[k], 1.f, gm[k]);
+    for (int k = 0; k < P; k++) {
+        load_weight(a.gamma, sp[k], 1.f, gm[k]);
 #pragma unroll
-        for (int e = 0; e < 8; e++) sg[k][e] = sb[k][e] = 0.f;
+        for (int e = 0; e < W; e++) sg[k][e] = sb[k][e] = 0.f;
     }
-    RawPiece<T, 8> xr[G], yr[G];
+    RawPiece<T, W> xr[P], yr[P];
     float mean = 0.f, rstd = 0.f;
     auto fetch = [&](long row) {
         if (row >= a.rows) return;
 #pragma unroll
-        for (int k = 0; k < G; k++) {
+        for (int k = 0; k < P; k++) {
             sp[k].template load<WHOLE>(static_cast<const T *>(a.x) + row * a.ldx, xr[k]);
             sp[k].template load<WHOLE>(static_cast<const T *>(a.dy) + row * a.ldy, yr[k]);
         }
@@ -332,13 +333,13 @@ __global__ void __launch_bounds__((GRAD_BLOCK<G, WHOLE>)) norm_grad_kernel(const
     fetch(row);
     for (long first = (long)blockIdx.x * SLOTS; first < a.rows; first += (long)gridDim.x * SLOTS) {      // the same for every thread: each meets every barrier
         const bool there = row < a.rows;
-        float h[G][8], g[G][8], s1 = 0.f, s2 = 0.f;
+        float h[P][W], g[P][W], s1 = 0.f, s2 = 0.f;
         const float r = rstd;
         if (there) {
 #pragma unroll
-            for (int k = 0; k < G; k++)
+            for (int k = 0; k < P; k++)
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
+                for (int e = 0; e < W; e++) {
                     h[k][e] = (xr[k].get(e) - mean) * rstd;
                     const float d = yr[k].get(e);
                     sb[k][e] += d;
@@ -346,16 +347,16 @@ __global__ void __launch_bounds__((GRAD_BLOCK<G, WHOLE>)) norm_grad_kernel(const
                     g[k][e] = d * gm[k][e];
                 }
         }
-        RawPiece<T, 8> res[G];
+        RawPiece<T, W> res[P];
         const size_t out = (size_t)row * a.cols;
         if (there && a.residual) {
 #pragma unroll
-            for (int k = 0; k < G; k++) sp[k].template load<WHOLE>(static_cast<const T *>(a.residual) + out, res[k]);
+            for (int k = 0; k < P; k++) sp[k].template load<WHOLE>(static_cast<const T *>(a.residual) + out, res[k]);
         }
         row += (long)gridDim.x * SLOTS;
         fetch(row);
         if (a.y) {
-            if (there) row_products<G>(g, h, s1, s2);
+            if (there) row_products(g, h, s1, s2);
             s1 = wave_sum(s1);
             s2 = wave_sum(s2);
             if constexpr (WAVES > 1) {
@@ -369,13 +370,13 @@ __global__ void __launch_bounds__((GRAD_BLOCK<G, WHOLE>)) norm_grad_kernel(const
             const float c1 = s1 * a.inv_cols, c2 = s2 * a.inv_cols;
             if (there) {
 #pragma unroll
-                for (int k = 0; k < G; k++) {
+                for (int k = 0; k < P; k++) {
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
+                    for (int e = 0; e < W; e++) {
                         g[k][e] = r * (g[k][e] - c1 - h[k][e] * c2);
                         if (a.residual) g[k][e] += res[k].get(e);
                     }
-                    sp[k].template store<WHOLE>(static_cast<T *>(a.y) + out, g[k]);
+                    sp[k].template store<WHOLE, STREAM>(static_cast<T *>(a.y) + out, g[k]);
                 }
             }
         }
@@ -383,26 +384,26 @@ __global__ void __launch_bounds__((GRAD_BLOCK<G, WHOLE>)) norm_grad_kernel(const
     // the slots' sums, in their order
 #pragma unroll
     for (int which = 0; which < 2; which++) {
-        float (&s)[G][8] = which == 0 ? sg : sb;
+        float (&s)[P][W] = which == 0 ? sg : sb;
         float *part = which == 0 ? dgamma : dbeta;
         if (!part) continue;
         if constexpr (SLOTS > 1) {
             __syncthreads();
             if (slot > 0) {
 #pragma unroll
-                for (int k = 0; k < G; k++)
+                for (int k = 0; k < P; k++)
 #pragma unroll
-                    for (int e = 0; e < 8; e++) sums[slot - 1][(k * 8 + e) * TPR + lane] = s[k][e];
+                    for (int e = 0; e < W; e++) sums[slot - 1][(k * W + e) * TPR + lane] = s[k][e];
             }
             __syncthreads();
         }
         if (slot == 0) {
 #pragma unroll
-            for (int k = 0; k < G; k++) {
+            for (int k = 0; k < P; k++) {
                 if constexpr (SLOTS > 1) {
 #pragma unroll
-                    for (int e = 0; e < 8; e++)
-                        for (int q = 0; q < SLOTS - 1; q++) s[k][e] += sums[q][(k * 8 + e) * TPR + lane];
+                    for (int e = 0; e < W; e++)
+                        for (int q = 0; q < SLOTS - 1; q++) s[k][e] += sums[q][(k * W + e) * TPR + lane];
                 }
                 sp[k].template store<WHOLE>(part + (size_t)blockIdx.x * a.cols, s[k]);
             }
@@ -479,16 +480,18 @@ struct NormLaunch {
     int groups;                 // NORM_GRAD: workgroups
     float *dgamma, *dbeta;      // and their parts
 };
-template <int TPR, int G, bool WHOLE, typename T> void launch_rows_of(const NormLaunch &l, hipStream_t st) {
+template <int TPR, int G, bool WHOLE, bool STREAM, typename T> void launch_rows_of(const NormLaunch &l, hipStream_t st) {
     constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR;
     const int rows = (int)min(((long)l.a.rows + RPB - 1) / RPB, 2048l);
-    if (l.kind == NORM_FORWARD) hipLaunchKernelGGL((norm_kernel<TPR, G, WHOLE, T>), dim3((unsigned)rows), dim3(BLOCK), 0, st, l.a);
-    else if (l.kind == NORM_DX) hipLaunchKernelGGL((norm_dx_kernel<TPR, G, WHOLE, T>), dim3((unsigned)(l.cols.blocks + (l.a.y ? rows : 0))), dim3(BLOCK), 0, st, l.a, l.cols);
-    else hipLaunchKernelGGL((norm_grad_kernel<TPR, G, WHOLE, T>), dim3((unsigned)l.groups), dim3(GRAD_BLOCK<G, WHOLE>), 0, st, l.a, l.dgamma, l.dbeta);
+    if (l.kind == NORM_FORWARD) hipLaunchKernelGGL((norm_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)rows), dim3(BLOCK), 0, st, l.a);
+    else if (l.kind == NORM_DX) hipLaunchKernelGGL((norm_dx_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)(l.cols.blocks + (l.a.y ? rows : 0))), dim3(BLOCK), 0, st, l.a, l.cols);
+    else hipLaunchKernelGGL((norm_grad_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)l.groups), dim3(GRAD_BLOCK<G, WHOLE>), 0, st, l.a, l.dgamma, l.dbeta);
 }
 template <int TPR, int G, typename T> void launch_rows(const NormLaunch &l, hipStream_t st) {
-    if (l.a.cols % 8 == 0) launch_rows_of<TPR, G, true, T>(l, st);
-    else launch_rows_of<TPR, G, false, T>(l, st);
+    const bool whole = l.a.cols % (16 / sizeof(T)) == 0;
+    if (whole && (size_t)l.a.rows * l.a.cols * sizeof(T) >= STREAM_BYTES) launch_rows_of<TPR, G, true, true, T>(l, st);
+    else if (whole) launch_rows_of<TPR, G, true, false, T>(l, st);
+    else launch_rows_of<TPR, G, false, false, T>(l, st);
 }
 template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st) {
     const int groups = ceil_div(l.a.cols, 8);
@@ -512,7 +515,7 @@ int norm_parts(int rows, int cols, int dt) {
     const int groups = ceil_div(cols, 8);
     if (groups > MAX_REGISTER_GROUPS) return norm_chunks(rows, cols);
     if (few_rows(rows, dt)) return 1;
-    const bool large = groups <= 256 && cols % 8 == 0;      // workgroups of 1024 threads
+    const bool large = groups <= 256 && cols % (16 / (int)dtype_size(dt)) == 0;      // workgroups of 1024 threads
     const int slots = (large ? 1024 : 512) / (groups <= 64 ? 64 : groups <= 128 ? 128 : groups <= 512 ? 256 : 512);
     const long rounds = ((long)rows + slots - 1) / slots;
     // A round of rows costs a workgroup about what 32 more parts cost the launch that sums them: 32 rounds = parts^2 makes the sum of both least.  Up to a GPU full of workgroups.
