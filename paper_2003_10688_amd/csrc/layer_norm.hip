@@ -300,12 +300,13 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
 
 // dx and the columns' sums in one pass over the data: workgroups stay, take SLOTS rows at a time, with the next ones' loads under way, and keep the sums of their rows' columns in
 // registers; parts [workgroup][cols] at the end.
-// Threads of a workgroup: 1024 where 128 registers hold a thread's share, so that fewer workgroups fill the GPU and fewer parts are left
-template <int G, bool WHOLE> constexpr int GRAD_BLOCK = G == 1 && WHOLE ? 1024 : 512;
+// Threads of a workgroup: 1024 with one piece each where rows are whole pieces, which 128 registers hold, so that one workgroup a CU is enough and fewer parts are left (16384 x 4096 bf16 104 us; 512
+// threads with two pieces each 111).  Ends of rows take more registers.
+template <bool WHOLE> constexpr int GRAD_BLOCK = WHOLE ? 1024 : 512;
 template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
-__global__ void __launch_bounds__((GRAD_BLOCK<G, WHOLE>)) norm_grad_kernel(const NormArgs a, float *dgamma, float *dbeta) {
-    constexpr int SLOTS = GRAD_BLOCK<G, WHOLE> / TPR, WAVES = TPR / 64, W = 16 / sizeof(T), P = G * 8 / W;
-    __shared__ float2 red[2][GRAD_BLOCK<G, WHOLE> / 64];
+__global__ void __launch_bounds__(GRAD_BLOCK<WHOLE>) norm_grad_kernel(const NormArgs a, float *dgamma, float *dbeta) {
+    constexpr int SLOTS = GRAD_BLOCK<WHOLE> / TPR, WAVES = TPR / 64, W = 16 / sizeof(T), P = G * 8 / W;
+    __shared__ float2 red[2][GRAD_BLOCK<WHOLE> / 64];
     __shared__ float sums[SLOTS > 1 ? SLOTS - 1 : 1][TPR * G * 8];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
     const Spans<W, P> sp(lane * W, TPR * W, a.cols);
@@ -484,26 +485,48 @@ template <int TPR, int G, bool WHOLE, bool STREAM, typename T> void launch_rows_
     constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR;
     const int rows = (int)min(((long)l.a.rows + RPB - 1) / RPB, 2048l);
     if (l.kind == NORM_FORWARD) hipLaunchKernelGGL((norm_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)rows), dim3(BLOCK), 0, st, l.a);
-    else if (l.kind == NORM_DX) hipLaunchKernelGGL((norm_dx_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)(l.cols.blocks + (l.a.y ? rows : 0))), dim3(BLOCK), 0, st, l.a, l.cols);
-    else hipLaunchKernelGGL((norm_grad_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)l.groups), dim3(GRAD_BLOCK<G, WHOLE>), 0, st, l.a, l.dgamma, l.dbeta);
+    else hipLaunchKernelGGL((norm_dx_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)(l.cols.blocks + (l.a.y ? rows : 0))), dim3(BLOCK), 0, st, l.a, l.cols);
 }
+template <typename T> bool whole_rows(int cols) { return cols % (16 / sizeof(T)) == 0; }
+template <typename T> bool streamed(const NormArgs &a) { return (size_t)a.rows * a.cols * sizeof(T) >= STREAM_BYTES; }
 template <int TPR, int G, typename T> void launch_rows(const NormLaunch &l, hipStream_t st) {
-    const bool whole = l.a.cols % (16 / sizeof(T)) == 0;
-    if (whole && (size_t)l.a.rows * l.a.cols * sizeof(T) >= STREAM_BYTES) launch_rows_of<TPR, G, true, true, T>(l, st);
-    else if (whole) launch_rows_of<TPR, G, true, false, T>(l, st);
-    else launch_rows_of<TPR, G, false, false, T>(l, st);
+    if (!whole_rows<T>(l.a.cols)) launch_rows_of<TPR, G, false, false, T>(l, st);
+    else if (streamed<T>(l.a)) launch_rows_of<TPR, G, true, true, T>(l, st);
+    else launch_rows_of<TPR, G, true, false, T>(l, st);
+}
+template <int TPR, int G, bool WHOLE, typename T> void launch_grad(const NormLaunch &l, hipStream_t st) {
+    const dim3 grid((unsigned)l.groups), block(GRAD_BLOCK<WHOLE>);
+    if constexpr (WHOLE) {
+        if (streamed<T>(l.a)) hipLaunchKernelGGL((norm_grad_kernel<TPR, G, true, true, T>), grid, block, 0, st, l.a, l.dgamma, l.dbeta);
+        else hipLaunchKernelGGL((norm_grad_kernel<TPR, G, true, false, T>), grid, block, 0, st, l.a, l.dgamma, l.dbeta);
+    } else {
+        hipLaunchKernelGGL((norm_grad_kernel<TPR, G, false, false, T>), grid, block, 0, st, l.a, l.dgamma, l.dbeta);
+    }
 }
 template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st) {
     const int groups = ceil_div(l.a.cols, 8);
-    if (groups <= 64) launch_rows<64, 1, T>(l, st);
-    else if (groups <= 128) launch_rows<128, 1, T>(l, st);
-    else if (groups <= 256) launch_rows<256, 1, T>(l, st);
-    else if (groups <= 512) launch_rows<256, 2, T>(l, st);
-    else if (groups <= MAX_REGISTER_GROUPS) launch_rows<512, 2, T>(l, st);
-    else {
+    if (groups > MAX_REGISTER_GROUPS) {
         const dim3 grid((unsigned)min(l.a.rows, 1024));
         if (l.kind == NORM_FORWARD) hipLaunchKernelGGL(norm_long_kernel<T>, grid, dim3(1024), 0, st, l.a);
         else hipLaunchKernelGGL(norm_dx_long_kernel<T>, grid, dim3(1024), 0, st, l.a);
+    } else if (l.kind != NORM_GRAD) {
+        if (groups <= 64) launch_rows<64, 1, T>(l, st);
+        else if (groups <= 128) launch_rows<128, 1, T>(l, st);
+        else if (groups <= 256) launch_rows<256, 1, T>(l, st);
+        else if (groups <= 512) launch_rows<256, 2, T>(l, st);
+        else launch_rows<512, 2, T>(l, st);
+    } else if (whole_rows<T>(l.a.cols)) {
+        if (groups <= 64) launch_grad<64, 1, true, T>(l, st);
+        else if (groups <= 128) launch_grad<128, 1, true, T>(l, st);
+        else if (groups <= 256) launch_grad<256, 1, true, T>(l, st);
+        else if (groups <= 512) launch_grad<512, 1, true, T>(l, st);
+        else launch_grad<1024, 1, true, T>(l, st);
+    } else {
+        if (groups <= 64) launch_grad<64, 1, false, T>(l, st);
+        else if (groups <= 128) launch_grad<128, 1, false, T>(l, st);
+        else if (groups <= 256) launch_grad<256, 1, false, T>(l, st);
+        else if (groups <= 512) launch_grad<256, 2, false, T>(l, st);
+        else launch_grad<512, 2, false, T>(l, st);
     }
     SOL_HIP(hipGetLastError());
     return SOL_OK;
@@ -515,12 +538,13 @@ int norm_parts(int rows, int cols, int dt) {
     const int groups = ceil_div(cols, 8);
     if (groups > MAX_REGISTER_GROUPS) return norm_chunks(rows, cols);
     if (few_rows(rows, dt)) return 1;
-    const bool large = groups <= 256 && cols % (16 / (int)dtype_size(dt)) == 0;      // workgroups of 1024 threads
-    const int slots = (large ? 1024 : 512) / (groups <= 64 ? 64 : groups <= 128 ? 128 : groups <= 512 ? 256 : 512);
-    const long rounds = ((long)rows + slots - 1) / slots;
+    const bool whole = cols % (16 / (int)dtype_size(dt)) == 0;
+    const int threads = groups <= 64 ? 64 : groups <= 128 ? 128 : groups <= 256 ? 256 : !whole ? (groups <= 512 ? 256 : 512) : groups <= 512 ? 512 : 1024;
+    const int slots = (whole ? GRAD_BLOCK<true> : GRAD_BLOCK<false>) / threads;
+    const long rounds = ((long)rows + slots - 1) / slots, most = min(rounds, groups <= 256 && !whole ? 512l : 256l);
     // A round of rows costs a workgroup about what 32 more parts cost the launch that sums them: 32 rounds = parts^2 makes the sum of both least.  Up to a GPU full of workgroups.
     long parts = 1;
-    while (parts * parts < 32 * rounds && parts < min(rounds, groups <= 256 && !large ? 512l : 256l)) parts++;
+    while (parts * parts < 32 * rounds && parts < most) parts++;
     return (int)parts;
 }
 
