@@ -384,6 +384,40 @@ template <typename T, typename TO> __global__ void __launch_bounds__(256) embed_
     put_row<TO>(a, cl, v, acc);
 }
 
+// acc += `many` rows (FLIGHT at most, all of them with FULL: no branch between the loads, which are then under way together); next() gives them one by one
+template <int FLIGHT, bool FULL, typename T, int W, int PIECES, typename F>
+__device__ __forceinline__ void add_rows(const T *dy, long ldy, const Spans<W, PIECES> &sp, int many, float (&acc)[PIECES][W], F next) {
+    RawPiece<T, W> raw[FLIGHT][PIECES];
+#pragma unroll
+    for (int u = 0; u < FLIGHT; u++)
+        if (FULL || u < many) {
+            const T *p = dy + (long)next() * ldy;
+#pragma unroll
+            for (int i = 0; i < PIECES; i++) sp[i].template load<false>(p, raw[u][i]);
+        }
+#pragma unroll
+    for (int u = 0; u < FLIGHT; u++)
+        if (FULL || u < many) {
+#pragma unroll
+            for (int i = 0; i < PIECES; i++)
+#pragma unroll
+                for (int k = 0; k < W; k++) acc[i][k] += raw[u][i].get(k);
+        }
+}
+
+// scale * acc into a row, or onto it
+template <typename TO, int W, int PIECES, bool STREAM>
+__device__ __forceinline__ void write_row(TO *out, const Spans<W, PIECES> &sp, float (&acc)[PIECES][W], float scale, int accumulate) {
+#pragma unroll
+    for (int i = 0; i < PIECES; i++) {
+        RawPiece<TO, W> old;
+        if (accumulate) sp[i].template load<false>(out, old);
+#pragma unroll
+        for (int k = 0; k < W; k++) acc[i][k] = accumulate ? acc[i][k] * scale + old.get(k) : acc[i][k] * scale;
+        sp[i].template store<false, STREAM>(out, acc[i]);
+    }
+}
+
 // Wider ones: a wave takes PIECES * 64 * W columns of a row.  Three round trips to memory: where its run is, the positions in it (a lane each), and FLIGHT of the gradient's rows at a time.
 template <typename T, typename TO, int W, int PIECES, bool STREAM> __device__ __forceinline__ void wide_item(const GatherArgs &a, int item, int c0) {
     constexpr int FLIGHT = 64 / (W * PIECES);
@@ -405,41 +439,17 @@ template <typename T, typename TO, int W, int PIECES, bool STREAM> __device__ __
     for (int i = 0; i < PIECES; i++)
 #pragma unroll
         for (int k = 0; k < W; k++) acc[i][k] = 0.f;
-    for (int j = 0; j < many; j += FLIGHT) {
-        RawPiece<T, W> raw[FLIGHT][PIECES];
-#pragma unroll
-        for (int u = 0; u < FLIGHT; u++) {
-            if (j + u < many) {
-                const T *p = dy + (long)__builtin_amdgcn_readlane(order, j + u) * a.ldy;
-#pragma unroll
-                for (int i = 0; i < PIECES; i++) sp[i].template load<false>(p, raw[u][i]);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < FLIGHT; u++) {
-            if (j + u < many) {
-#pragma unroll
-                for (int i = 0; i < PIECES; i++)
-#pragma unroll
-                    for (int k = 0; k < W; k++) acc[i][k] += raw[u][i].get(k);
-            }
-        }
-    }
+    int j = 0;
+    auto next = [&]() { return __builtin_amdgcn_readlane(order, j++); };
+    while (j + FLIGHT <= many) add_rows<FLIGHT, true>(dy, a.ldy, sp, FLIGHT, acc, next);
+    if (j < many) add_rows<FLIGHT, false>(dy, a.ldy, sp, many - j, acc, next);
     if (window) {
         float *part = a.part + (size_t)item * a.cols;
 #pragma unroll
         for (int i = 0; i < PIECES; i++) sp[i].template store<false>(part, acc[i]);
         return;
     }
-    TO *out = static_cast<TO *>(a.out) + (size_t)(item - 2 * a.windows) * a.cols;
-#pragma unroll
-    for (int i = 0; i < PIECES; i++) {
-        RawPiece<TO, W> old;
-        if (a.accumulate) sp[i].template load<false>(out, old);
-#pragma unroll
-        for (int k = 0; k < W; k++) acc[i][k] = a.accumulate ? acc[i][k] * a.scale + old.get(k) : acc[i][k] * a.scale;
-        sp[i].template store<false, STREAM>(out, acc[i]);
-    }
+    write_row<TO, W, PIECES, STREAM>(static_cast<TO *>(a.out) + (size_t)(item - 2 * a.windows) * a.cols, sp, acc, a.scale, a.accumulate);
 }
 // Slabs of columns vary fastest: workgroups that run together then write whole rows, not the same part of every row, whose addresses would fall on a few of the memory's channels.
 template <typename T, typename TO, int W, int PIECES, bool STREAM> __global__ void __launch_bounds__(256) embed_wide_kernel(const GatherArgs a, int items) {
@@ -477,6 +487,117 @@ template <typename T, typename TO> __global__ void __launch_bounds__(256) embed_
     put_row<TO>(a, cl, row_of_place(a, p), acc);
 }
 
+// ---- the gradient of few tokens, in one launch ----------------------------------------------------------------------------------
+// A workgroup looks at all tokens, lists those of its `block` rows in order, and sums and writes its rows, a wave each.  One row's tokens are added one behind the other, so
+// there can only be few; the rows without tokens, nearly all of them, are what the time goes into.
+constexpr int DIRECT = 512, CROWD = 32;
+struct DirectArgs {
+    const void *tokens, *dy;
+    void *out;
+    long ldy;
+    int n, vocab, cols, pad, block, accumulate;
+    float scale;
+};
+template <typename T, typename TO, typename I, int W, int PIECES, bool STREAM> __global__ void __launch_bounds__(256) embed_direct_kernel(const DirectArgs a) {
+    constexpr int FLIGHT = 64 / (W * PIECES);
+    __shared__ uint32_t list[DIRECT];                   // row in the block << 16 | position
+    __shared__ int counts[4];
+    __shared__ float sums[3][PIECES * W][64];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Spans<W, PIECES> sp((int)blockIdx.x * (PIECES * 64 * W) + lane * W, 64 * W, a.cols);
+    const T *dy = static_cast<const T *>(a.dy);
+    int tok[2];
+#pragma unroll
+    for (int j = 0; j < 2; j++) {
+        const int i = (int)threadIdx.x * 2 + j;
+        const I t = i < a.n ? static_cast<const I *>(a.tokens)[i] : (I)-1;
+        tok[j] = i < a.n && t != (I)a.pad && t >= 0 && t < (I)a.vocab ? (int)t : -1;
+    }
+    for (int v0 = (int)blockIdx.y * a.block; v0 < a.vocab; v0 += (int)gridDim.y * a.block) {
+        const int v1 = min(a.vocab, v0 + a.block);
+        const bool own0 = tok[0] >= v0 && tok[0] < v1, own1 = tok[1] >= v0 && tok[1] < v1;
+        const lanes_t m0 = __ballot(own0), m1 = __ballot(own1);
+        if (lane == 0) counts[w] = __popcll(m0) + __popcll(m1);
+        __syncthreads();
+        int at = 0, total = 0;
+#pragma unroll
+        for (int q = 0; q < 4; q++) {
+            at += q < w ? counts[q] : 0;
+            total += counts[q];
+        }
+        at = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m0 >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m0, (uint32_t)at));
+        at = (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(m1 >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m1, (uint32_t)at));
+        if (own0) list[at++] = (uint32_t)(tok[0] - v0) << 16 | threadIdx.x * 2;
+        if (own1) list[at] = (uint32_t)(tok[1] - v0) << 16 | (threadIdx.x * 2 + 1);
+        __syncthreads();
+        // With a crowded list every wave looks at every row; one of more than CROWD tokens is summed by all four, 64 entries of the list in turn.  Else the waves take the rows in turn.
+        const bool crowded = total > CROWD;
+        uint32_t rows[DIRECT / 64];                     // the list's rows, 64 entries a lane each
+#pragma unroll
+        for (int c = 0; c < DIRECT / 64; c++) rows[c] = c * 64 + lane < total ? list[c * 64 + lane] >> 16 : 0xffffu;
+        for (int r = crowded ? 0 : w; v0 + r < v1; r += crowded ? 1 : 4) {
+            int many = 0;
+#pragma unroll
+            for (int c = 0; c < DIRECT / 64; c++)
+                if (c * 64 < total) many += __popcll(__ballot((int)rows[c] == r));
+            const bool shared = many > CROWD;
+            if (crowded && !shared && (r & 3) != w) continue;
+            float acc[PIECES][W];
+#pragma unroll
+            for (int i = 0; i < PIECES; i++)
+#pragma unroll
+                for (int k = 0; k < W; k++) acc[i][k] = 0.f;
+            for (int c = many == 0 ? total : shared ? w * 64 : 0; c < total; c += shared ? 256 : 64) {
+                const uint32_t e = c + lane < total ? list[c + lane] : 0xffffffffu;
+                lanes_t left = __ballot((int)(e >> 16) == r);       // r < 2^15
+                auto next = [&]() {
+                    const int p = __builtin_amdgcn_readlane((int)(e & 0xffffu), __ffsll(left) - 1);
+                    left &= left - 1;
+                    return p;
+                };
+                while (__popcll(left) >= FLIGHT) add_rows<FLIGHT, true>(dy, a.ldy, sp, FLIGHT, acc, next);
+                if (left) add_rows<FLIGHT, false>(dy, a.ldy, sp, __popcll(left), acc, next);
+            }
+            if (shared) {                               // the same for all four waves: the list says so
+                __syncthreads();                        // the sums of a shared row in front are read
+#pragma unroll
+                for (int i = 0; i < PIECES; i++)
+#pragma unroll
+                    for (int k = 0; k < W; k++)
+                        if (w > 0) sums[w - 1][i * W + k][lane] = acc[i][k];
+                __syncthreads();
+                if (w > 0) continue;
+#pragma unroll
+                for (int i = 0; i < PIECES; i++)
+#pragma unroll
+                    for (int k = 0; k < W; k++) acc[i][k] += sums[0][i * W + k][lane] + sums[1][i * W + k][lane] + sums[2][i * W + k][lane];
+            } else if (a.accumulate && many == 0) continue;
+            write_row<TO, W, PIECES, STREAM>(static_cast<TO *>(a.out) + (size_t)(v0 + r) * a.cols, sp, acc, a.scale, a.accumulate);
+        }
+        __syncthreads();                                // the list's readers are through
+    }
+}
+
+template <typename T, typename TO, typename I, int PIECES> void launch_direct_of(const DirectArgs &a, hipStream_t st) {
+    constexpr int W = sizeof(TO) == 4 ? 4 : 8;
+    const dim3 grid((unsigned)ceil_div(a.cols, PIECES * 64 * W), (unsigned)min(ceil_div(a.vocab, a.block), 65535));
+    if ((size_t)a.vocab * a.cols * sizeof(TO) >= STREAM_BYTES) hipLaunchKernelGGL((embed_direct_kernel<T, TO, I, W, PIECES, true>), grid, dim3(256), 0, st, a);
+    else hipLaunchKernelGGL((embed_direct_kernel<T, TO, I, W, PIECES, false>), grid, dim3(256), 0, st, a);
+}
+template <typename T, typename TO, typename I> sol_status launch_direct_of(DirectArgs a, hipStream_t st) {
+    constexpr int W = sizeof(TO) == 4 ? 4 : 8;
+    const int pieces = ceil_div(a.cols, 64 * W), slabs = pieces <= 1 ? 1 : ceil_div(pieces, 2);
+    // rows enough for a workgroup to make up for its look at the tokens, workgroups enough to fill the GPU
+    a.block = max(4, min(32, (int)((long)a.vocab * slabs / 1024) & ~3));
+    if (pieces <= 1) launch_direct_of<T, TO, I, 1>(a, st);
+    else launch_direct_of<T, TO, I, 2>(a, st);
+    SOL_HIP(hipGetLastError());
+    return SOL_OK;
+}
+template <typename T, typename TO> sol_status launch_direct(const DirectArgs &a, int bits, hipStream_t st) {
+    return bits == 64 ? launch_direct_of<T, TO, int64_t>(a, st) : launch_direct_of<T, TO, int32_t>(a, st);
+}
+
 sol_status check_embed(const sol_embedding_desc *ed, sol_embedding_desc *d) {
     SOL_REQUIRE(ed, SOL_ERR_NULL, "embedding descriptor is NULL");
     *d = *ed;
@@ -509,12 +630,13 @@ struct EmbedPlan {
 };
 EmbedPlan embed_plan(const sol_embedding_desc &d) {
     EmbedPlan p{};
+    if (d.tokens <= DIRECT) return p;       // no scratch
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at = round_up(at + bytes, 256); return here; };
     while ((1 << p.log2) < d.vocab && ((1 << p.log2) < INDEX_GROUPS || (size_t)INDEX_ROWS << p.log2 < (size_t)d.vocab)) p.log2++;
     p.rows = ceil_div(d.vocab, 1 << p.log2);
     p.places = p.rows << p.log2;
-    p.windows = d.tokens > RUN ? ceil_div(d.tokens, RUN) : 0;       // no run is longer than the tokens are
+    p.windows = ceil_div(d.tokens, RUN);
     p.start = take(((size_t)p.places + 1) * 4);
     p.order = take((size_t)d.tokens * 4);
     p.sorted = take((size_t)d.tokens * 4);
@@ -536,10 +658,8 @@ template <typename T, typename TO> sol_status launch_gather(const GatherArgs &g,
     else if (g.cols <= 512) launch_wide<T, TO, 1>(g, st);
     else launch_wide<T, TO, 2>(g, st);
     SOL_HIP(hipGetLastError());
-    if (g.windows) {
-        hipLaunchKernelGGL((embed_join_kernel<T, TO>), dim3((unsigned)ceil_div(g.windows, per), (unsigned)slabs), dim3(256), 0, st, g);
-        SOL_HIP(hipGetLastError());
-    }
+    hipLaunchKernelGGL((embed_join_kernel<T, TO>), dim3((unsigned)ceil_div(g.windows, per), (unsigned)slabs), dim3(256), 0, st, g);
+    SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
 
@@ -578,6 +698,11 @@ sol_status sol_embedding_backward(const sol_embedding_desc *ed, const void *toke
     const EmbedPlan p = embed_plan(d);
     SOL_TRY(check_scratch(workspace, workspace_bytes, p.bytes));
     hipStream_t st = (hipStream_t)stream;
+    if (d.tokens <= DIRECT) {
+        const DirectArgs a{tokens, dy, dtable, d.ldy, d.tokens, d.vocab, d.cols, d.pad, 0, accumulate ? 1 : 0, d.scale};
+        if (d.dtype == SOL_F32) return launch_direct<float, float>(a, d.token_bits, st);
+        return dtable_dtype == SOL_F32 ? launch_direct<bf16_t, float>(a, d.token_bits, st) : launch_direct<bf16_t, bf16_t>(a, d.token_bits, st);
+    }
     unsigned char *ws = static_cast<unsigned char *>(workspace);
     int *start = reinterpret_cast<int *>(ws + p.start), *order = reinterpret_cast<int *>(ws + p.order), *sorted = reinterpret_cast<int *>(ws + p.sorted);
     const IndexArgs x{tokens, d.tokens, d.vocab, d.pad, p.rows, p.log2, start, order, sorted};

@@ -12,10 +12,7 @@ namespace {
 
 // The tensors of one launch, by value: no copy to the device, nothing to keep alive, and a captured graph holds them.  A tensor is cut into chunks, so that a workgroup's share is even.
 // 170 tensors fill the 4 KB of a kernel's arguments, so that a network of that many takes one launch and not two.
-#ifndef GC_G
-#define GC_G 1024
-#endif
-constexpr int TABLE = 170, CHUNK = 8192, MAX_GROUPS = GC_G;
+constexpr int TABLE = 170, CHUNK = 8192, MAX_GROUPS = 1024;
 constexpr int MAX_TENSORS = 1 << 15, MAX_JOIN = 4096;
 struct GradTable {
     const void *grad[TABLE];

