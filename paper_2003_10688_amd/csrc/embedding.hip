@@ -3,6 +3,8 @@
 //   backward  dtable[v] = scale * sum of the dy[i] with tokens[i] = v, in the order of i
 #include <float.h>
 
+#include <type_traits>
+
 #include "row_ops.h"
 
 namespace sol {
@@ -68,11 +70,11 @@ struct IndexArgs {
 };
 
 // A tile is PIECES pieces of 4 neighbouring tokens a thread: lanes next to each other read next to each other.  t: the tokens, where[j]: the lanes of the wave whose token j is this workgroup's own.
-// Returns how many of the wave's belong to the residues in front.  What a token costs here is what the launch costs, since every workgroup looks at every token: six vector instructions,
-// counts and prefixes come from the masks.
+// Returns how many of this thread's belong to the residues in front.  What a token costs here is what the launch costs, since every workgroup looks at every token: six vector instructions, and as few
+// scalar ones as can be, which all waves of a CU share one unit for.  PAD: the padding token is a row of the table.
 constexpr int PIECES = INDEX_EACH / 4;
 typedef unsigned long long lanes_t;
-template <typename I> __device__ __forceinline__ int look_at_tokens(const IndexArgs &a, int base, uint32_t t[INDEX_EACH], lanes_t where[INDEX_EACH]) {
+template <typename I, bool PAD> __device__ __forceinline__ uint32_t look_at_tokens(const IndexArgs &a, int base, uint32_t t[INDEX_EACH], lanes_t where[INDEX_EACH]) {
     const I *p = static_cast<const I *>(a.tokens);
     I raw[INDEX_EACH];
 #pragma unroll
@@ -86,16 +88,16 @@ template <typename I> __device__ __forceinline__ int look_at_tokens(const IndexA
             for (int j = 0; j < 4; j++) raw[q * 4 + j] = at + j < a.n ? p[at + j] : (I)-1;
         }
     }
-    int less = 0;
-    const uint32_t mine = blockIdx.x, mask = (1u << a.log2) - 1, vocab = (uint32_t)a.vocab, pad = (uint32_t)a.pad;
+    uint32_t less = 0;
+    const uint32_t mine = blockIdx.x, mask = (1u << a.log2) - 1, vocab = (uint32_t)a.vocab;
 #pragma unroll
     for (int j = 0; j < INDEX_EACH; j++) {
+        typedef typename std::conditional<sizeof(I) == 8, uint64_t, uint32_t>::type U;
         t[j] = (uint32_t)raw[j];
-        bool row = t[j] < vocab && t[j] != pad;         // a negative one is not: vocab has 25 bits at most
-        if constexpr (sizeof(I) == 8) row = row && (raw[j] >> 32) == 0;
-        const uint32_t res = row ? t[j] & mask : 0xffffffffu;
+        uint32_t res = (U)raw[j] < (U)vocab ? t[j] & mask : 0xffffffffu;       // a negative one is not below it
+        if (PAD) res = raw[j] == (I)a.pad ? 0xffffffffu : res;
         where[j] = __ballot(res == mine);
-        less += __popcll(__ballot(res < mine));
+        less += res < mine ? 1u : 0u;
     }
     return less;
 }
@@ -225,7 +227,7 @@ __device__ __forceinline__ void index_place(const IndexArgs &a, IndexShared &s, 
     });
 }
 
-template <typename I> __global__ void __launch_bounds__(INDEX_THREADS) embed_index_kernel(const IndexArgs a) {
+template <typename I, bool PAD> __global__ void __launch_bounds__(INDEX_THREADS) embed_index_kernel(const IndexArgs a) {
     __shared__ IndexShared s;
     const int r = (int)threadIdx.x, bits = 32 - __clz(a.rows - 1);      // 0 for one row
     s.next[r] = 0;
@@ -239,7 +241,7 @@ template <typename I> __global__ void __launch_bounds__(INDEX_THREADS) embed_ind
             for (int w = 0; w < INDEX_WAVES; w++) s.next[r] += s.count[w][r];
     };
     for (int base = 0; base < a.n; base += INDEX_TILE) {
-        less += (uint32_t)look_at_tokens<I>(a, base, t, where);
+        less += look_at_tokens<I, PAD>(a, base, t, where);
         const int then = index_append(a, s, whole ? base : 0, t, where, have);
         if (then <= INDEX_TILE) {
             have = then;
@@ -253,7 +255,7 @@ template <typename I> __global__ void __launch_bounds__(INDEX_THREADS) embed_ind
     add_counts();
     uint2 all;
     const uint32_t count = s.next[r], up_to = wave_scan(count);      // next[r] is this thread's own
-    const uint2 before = sum_waves(make_uint2((uint32_t)__builtin_amdgcn_readlane((int)up_to, 63), less), s.slots, &all);
+    const uint2 before = sum_waves(make_uint2((uint32_t)__builtin_amdgcn_readlane((int)up_to, 63), (uint32_t)__builtin_amdgcn_readlane((int)wave_scan(less), 63)), s.slots, &all);
     const uint32_t at = all.y + before.x + up_to - count;
     s.next[r] = at;
     if (r < a.rows) a.start[(int)blockIdx.x * a.rows + r] = (int)at;
@@ -263,7 +265,7 @@ template <typename I> __global__ void __launch_bounds__(INDEX_THREADS) embed_ind
         return;
     }
     for (int base = 0; base < a.n; base += INDEX_TILE) {
-        look_at_tokens<I>(a, base, t, where);
+        look_at_tokens<I, PAD>(a, base, t, where);
         have = index_append(a, s, 0, t, where, 0);
         __syncthreads();
         index_count(a, s, have, bits);
@@ -457,34 +459,46 @@ template <typename T, typename TO, int W, int PIECES, bool STREAM> __global__ vo
     for (int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += (int)gridDim.y * 4) wide_item<T, TO, W, PIECES, STREAM>(a, item, c0);
 }
 
-// A long run ends behind the window that it starts in: at most one starts in each
+// A long run ends behind the window that it starts in: at most one starts in each.  A workgroup joins its parts in a slab of columns, a wave a quarter of them, one behind the other.
 template <typename T, typename TO> __global__ void __launch_bounds__(256) embed_join_kernel(const GatherArgs a) {
-    const int lane = threadIdx.x & ((1 << a.lanes_log2) - 1), slot = threadIdx.x >> a.lanes_log2;
-    const long win = (long)blockIdx.x * (256 >> a.lanes_log2) + slot;
-    const int used = a.start[a.places];
-    const Columns<T, TO> cl((int)blockIdx.y, lane, 1 << a.lanes_log2, a.cols);
-    if (win >= a.windows || cl.none() || win * RUN >= used) return;
-    const int p = a.sorted[min(used, (int)win * RUN + RUN) - 1], b = a.start[p], e = a.start[p + 1];
-    if (e - b <= RUN || b / RUN != win) return;
-    float acc[8], v[8];
-    const int last = (e - 1) / RUN;
-    cl.load(a.part + (size_t)(2 * win + (b % RUN ? 1 : 0)) * a.cols, acc);
-    int w = (int)win + 1;
-    for (; w + 7 <= last; w += 8) {
-        float u[8][8];
+    __shared__ float sums[3][8][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, used = a.start[a.places];
+    const Columns<T, TO> cl((int)blockIdx.x, lane, 64, a.cols);
+    for (long win = blockIdx.y; win < a.windows && win * RUN < used; win += gridDim.y) {
+        const int p = a.sorted[min(used, (int)win * RUN + RUN) - 1], b = a.start[p], e = a.start[p + 1];
+        if (e - b <= RUN || b / RUN != win) continue;       // the same for all threads
+        const int last = (e - 1) / RUN, per = (last - (int)win + 4) / 4, w0 = (int)win + wave * per, w1 = min(last + 1, w0 + per);
+        auto part = [&](int w) { return a.part + (size_t)(2 * (long)w + (w == (int)win && b % RUN ? 1 : 0)) * a.cols; };
+        float acc[8];
 #pragma unroll
-        for (int q = 0; q < 8; q++) cl.load(a.part + (size_t)2 * (w + q) * a.cols, u[q]);
+        for (int k = 0; k < 8; k++) acc[k] = 0.f;
+        int w = w0;
+        for (; w + 8 <= w1; w += 8) {
+            float u[8][8];
 #pragma unroll
-        for (int q = 0; q < 8; q++)
+            for (int q = 0; q < 8; q++) cl.load(part(w + q), u[q]);
 #pragma unroll
-            for (int k = 0; k < 8; k++) acc[k] += u[q][k];
+            for (int q = 0; q < 8; q++)
+#pragma unroll
+                for (int k = 0; k < 8; k++) acc[k] += u[q][k];
+        }
+        for (; w < w1; w++) {
+            float u[8];
+            cl.load(part(w), u);
+#pragma unroll
+            for (int k = 0; k < 8; k++) acc[k] += u[k];
+        }
+        __syncthreads();                                    // the sums of a run in front are read
+        if (wave > 0) {
+#pragma unroll
+            for (int k = 0; k < 8; k++) sums[wave - 1][k][lane] = acc[k];
+        }
+        __syncthreads();
+        if (wave > 0 || cl.none()) continue;
+#pragma unroll
+        for (int k = 0; k < 8; k++) acc[k] += sums[0][k][lane] + sums[1][k][lane] + sums[2][k][lane];
+        put_row<TO>(a, cl, row_of_place(a, p), acc);
     }
-    for (; w <= last; w++) {
-        cl.load(a.part + (size_t)2 * w * a.cols, v);
-#pragma unroll
-        for (int k = 0; k < 8; k++) acc[k] += v[k];
-    }
-    put_row<TO>(a, cl, row_of_place(a, p), acc);
 }
 
 // ---- the gradient of few tokens, in one launch ----------------------------------------------------------------------------------
@@ -653,12 +667,12 @@ template <typename T, typename TO, int PIECES> void launch_wide(const GatherArgs
     else hipLaunchKernelGGL((embed_wide_kernel<T, TO, W, PIECES * 8 / W, false>), grid, dim3(256), 0, st, g, items);
 }
 template <typename T, typename TO> sol_status launch_gather(const GatherArgs &g, hipStream_t st) {
-    const int per = 256 >> g.lanes_log2, slabs = row_slabs(g.cols);
+    const int per = 256 >> g.lanes_log2;
     if (g.lanes_log2 < 6) hipLaunchKernelGGL((embed_gather_kernel<T, TO>), dim3((unsigned)ceil_div(g.vocab + 2 * g.windows, per)), dim3(256), 0, st, g);
     else if (g.cols <= 512) launch_wide<T, TO, 1>(g, st);
     else launch_wide<T, TO, 2>(g, st);
     SOL_HIP(hipGetLastError());
-    hipLaunchKernelGGL((embed_join_kernel<T, TO>), dim3((unsigned)ceil_div(g.windows, per), (unsigned)slabs), dim3(256), 0, st, g);
+    hipLaunchKernelGGL((embed_join_kernel<T, TO>), dim3((unsigned)row_slabs(g.cols), (unsigned)min(g.windows, 65535)), dim3(256), 0, st, g);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
@@ -707,8 +721,14 @@ sol_status sol_embedding_backward(const sol_embedding_desc *ed, const void *toke
     int *start = reinterpret_cast<int *>(ws + p.start), *order = reinterpret_cast<int *>(ws + p.order), *sorted = reinterpret_cast<int *>(ws + p.sorted);
     const IndexArgs x{tokens, d.tokens, d.vocab, d.pad, p.rows, p.log2, start, order, sorted};
     const dim3 grid(1u << p.log2);
-    if (d.token_bits == 64) hipLaunchKernelGGL(embed_index_kernel<int64_t>, grid, dim3(INDEX_THREADS), 0, st, x);
-    else hipLaunchKernelGGL(embed_index_kernel<int32_t>, grid, dim3(INDEX_THREADS), 0, st, x);
+    const bool pad = d.pad >= 0 && d.pad < d.vocab;
+    if (d.token_bits == 64) {
+        if (pad) hipLaunchKernelGGL((embed_index_kernel<int64_t, true>), grid, dim3(INDEX_THREADS), 0, st, x);
+        else hipLaunchKernelGGL((embed_index_kernel<int64_t, false>), grid, dim3(INDEX_THREADS), 0, st, x);
+    } else {
+        if (pad) hipLaunchKernelGGL((embed_index_kernel<int32_t, true>), grid, dim3(INDEX_THREADS), 0, st, x);
+        else hipLaunchKernelGGL((embed_index_kernel<int32_t, false>), grid, dim3(INDEX_THREADS), 0, st, x);
+    }
     SOL_HIP(hipGetLastError());
     const GatherArgs g{dy, dtable, start, order, sorted, reinterpret_cast<float *>(ws + p.part), d.ldy, d.vocab, d.cols, p.windows, accumulate ? 1 : 0, row_lanes_log2(d.cols, 8),
                  p.rows, p.log2, p.places, d.scale, FastDiv((uint32_t)p.rows)};
