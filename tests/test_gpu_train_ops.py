@@ -698,3 +698,136 @@ def test_refusals_of_the_binding(sol):
         with pytest.raises(sol.SolError) as e:
             f()
         assert e.value.status == status
+
+
+# ---- borders between the kernels: rows, parts, lists, tables ---------------------------------------------------------
+@pytest.mark.parametrize("dt,rows,cols", [("bf16", 1024, 264), ("bf16", 1025, 264), ("f32", 512, 129), ("f32", 513, 129), ("bf16", 1500, 5000), ("bf16", 1100, 8192), ("f32", 600, 8188), ("f32", 600, 4100),
+                                          ("f32", 515, 700), ("f32", 515, 701), ("bf16", 9000, 96), ("bf16", 1030, 16), ("bf16", 1500, 3), ("f32", 1500, 7), ("bf16", 20, 9000), ("f32", 3000, 12000)])
+def test_backward_of_whole_numbers_at_the_borders(sol, dt, rows, cols):
+    """dgamma and dbeta to the last bit; dx against 64 bits, where mean 0, rstd 1 and whole numbers leave the two means and four operations to round."""
+    rng = np.random.default_rng([cols, rows, 3])
+    x, dy, res = rng.integers(-2, 3, (rows, cols)), rng.integers(-2, 3, (rows, cols)), rng.integers(-2, 3, (rows, cols))
+    zeros, ones = torch.zeros(rows, device=DEV), torch.ones(rows, device=DEV)
+    for pitch in (0, 1):
+        dx, dg, db = sol.sol_layer_norm_backward(dev(dy, dt, pitch), dev(x, dt, pitch), zeros, ones, residual=dev(res, dt))
+        wx, wg, wb = to.layer_norm_bwd(dy, x, np.zeros(rows), np.ones(rows), None, res)
+        assert np.array_equal(host(dg), wg) and np.array_equal(host(db), wb)
+        c1, c2 = np.abs(dy.mean(1, keepdims=True)), np.abs((dy * x).mean(1, keepdims=True))      # whole sums: exact, then 1 / cols and a product
+        close(host(dx), wx, 4 * U * (np.abs(dy) + c1 + np.abs(x) * c2 * 2) + 2 * U * (np.abs(res) + np.abs(wx)) + HALF[dt] * np.abs(wx) * 1.02, "dx")
+
+
+@pytest.mark.parametrize("dt,rows,cols", [("bf16", 16400, 8192), ("f32", 16400, 4096), ("f32", 70000, 1000), ("bf16", 140001, 960), ("bf16", 270000, 512)])
+def test_norms_larger_than_the_last_cache(sol, dt, rows, cols):
+    """Such results are written past the caches: the bits are those of the same rows in calls that are not."""
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    x, dy = (torch.randn((rows, cols), generator=gen, device=DEV).to(TDT[dt]) for _ in range(2))
+    gamma, beta = torch.randn(cols, generator=gen, device=DEV), torch.randn(cols, generator=gen, device=DEV)
+    assert x.nbytes >= 1 << 28
+    y, mean, rstd = sol.sol_layer_norm(x, gamma, beta, want_stats=True)
+    dx, dg, db = sol.sol_layer_norm_backward(dy, x, mean, rstd, gamma, residual=y)
+    alone = sol.sol_layer_norm_backward(dy, x, mean, rstd, gamma, residual=y, need_dgamma=False, need_dbeta=False)[0]
+    cut = rows // 3
+    sums = [torch.zeros(cols, device=DEV, dtype=torch.float64) for _ in range(2)]
+    for a, b in ((0, cut), (cut, 2 * cut), (2 * cut, rows)):
+        ya, ma, ra = sol.sol_layer_norm(x[a:b], gamma, beta, want_stats=True)
+        assert torch.equal(ya, y[a:b]) and torch.equal(ma, mean[a:b]) and torch.equal(ra, rstd[a:b])
+        da, ga, ba = sol.sol_layer_norm_backward(dy[a:b], x[a:b], ma.clone(), ra.clone(), gamma, residual=y[a:b])
+        assert torch.equal(alone[a:b], sol.sol_layer_norm_backward(dy[a:b], x[a:b], ma.clone(), ra.clone(), gamma, residual=y[a:b], need_dgamma=False, need_dbeta=False)[0])
+        assert torch.equal(da, dx[a:b])
+        sums[0] += ga
+        sums[1] += ba
+    # both sides: additions of a part of the rows one behind the other, then the parts; of sums of about the root of their number
+    for got, want, terms in ((dg, sums[0], dy.double() * ((x.double() - mean[:, None]) * rstd[:, None])), (db, sums[1], dy.double())):
+        size = terms.abs().sum(0)
+        assert torch.all((got.double() - want).abs() <= 400 * U * size)
+    del x, dy, y, dx, alone
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dt,grad", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("n,vocab,cols", [(400, 140000, 1000), (3000, 70000, 2056)])
+def test_tables_larger_than_the_last_cache(sol, dt, grad, n, vocab, cols):
+    """Whole numbers, so equal to the last bit to torch's sums; the embedding of so many tokens that its result is as large too."""
+    gen = torch.Generator(device=DEV).manual_seed(n)
+    tokens = (torch.rand(n, generator=gen, device=DEV) ** 3 * vocab).long()
+    dy = torch.randint(-2, 3, (n, cols), generator=gen, device=DEV).to(TDT[dt])
+    got = sol.sol_embedding_backward(dy, tokens, vocab, dtable_dtype=TDT[grad])
+    assert got.nbytes >= 1 << 28
+    want = torch.zeros((vocab, cols), device=DEV).index_add_(0, tokens, dy.float()).to(TDT[grad])
+    assert torch.equal(got, want)
+    assert torch.equal(sol.sol_embedding_backward(dy, tokens, vocab, add_to=got), (want.float() + want.float()).to(TDT[grad]))
+    many = torch.randint(0, vocab, ((1 << 28) // (cols * dy.element_size()) + 5,), generator=gen, device=DEV)
+    assert torch.equal(sol.sol_embedding(many, want.to(TDT[dt])), want.to(TDT[dt])[many])
+    del got, want, many
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n", [511, 512, 513, 576, 1025])
+@pytest.mark.parametrize("cols", [1, 30, 256, 300, 513, 1100])
+@pytest.mark.parametrize("dt,grad", [("bf16", "f32"), ("bf16", "bf16"), ("f32", "f32")])
+def test_few_and_more_tokens(sol, dt, grad, n, cols):
+    """On both sides of the border between one launch and three; rows of 1, 31 to 33 and 63 to 65 tokens, in one block of rows or spread."""
+    rng = np.random.default_rng([n, cols])
+    dy = rng.integers(-2, 3, (n, cols)).astype(np.float32)
+    sizes = [1, 31, 32, 33, 63, 64, 65, 3, 90]
+    for vocab, spread in ((40, 1), (9000, 997)):
+        tok = np.concatenate([np.full(k, (i * spread) % vocab) for i, k in enumerate(sizes)])
+        tok = np.concatenate([tok, rng.integers(0, vocab, n - len(tok))])
+        rng.shuffle(tok)
+        for bits in (torch.int32, torch.int64):
+            got = sol.sol_embedding_backward(dev(dy, dt, 5), torch.from_numpy(tok).to(DEV, bits), vocab, dtable_dtype=TDT[grad])
+            assert np.array_equal(host(got), grid(to.embedding_bwd(dy, tok, vocab), grad))
+
+
+@pytest.mark.parametrize("n,vocab,cols,kind", [(2000, 300001, 24, "any"), (40000, 1 << 24, 8, "any"), (70000, 70000, 16, "one"), (50000, 260, 8, "residue"), (33000, 5, 40, "any"), ((1 << 22) + 5000, 50, 8, "any"),
+                                               ((1 << 22) + 5000, 300000, 8, "one"), ((1 << 22), 1000, 8, "residue")])
+def test_sorting_of_tokens(sol, n, vocab, cols, kind):
+    """More rows than 256 workgroups hold, lists that overflow (all tokens of one workgroup's residue), more positions than a list's entry holds."""
+    gen = torch.Generator(device=DEV).manual_seed(n % 1000)
+    tokens = {"any": lambda: torch.randint(0, vocab, (n,), generator=gen, device=DEV), "one": lambda: torch.full((n,), vocab - 1, device=DEV),
+              "residue": lambda: torch.randint(0, (vocab + 255) // 256, (n,), generator=gen, device=DEV) * 256 % vocab}[kind]()
+    if kind == "one":
+        tokens[::7] = torch.randint(-3, vocab + 3, tokens[::7].shape, generator=gen, device=DEV)
+    dy = torch.randint(-1, 2, (n, cols), generator=gen, device=DEV).bfloat16()
+    kept = (tokens >= 0) & (tokens < vocab)
+    want = torch.zeros((vocab, cols), device=DEV).index_add_(0, torch.where(kept, tokens, 0), dy.float() * kept[:, None])
+    assert float(want.abs().max()) < 2**24
+    for t in (tokens, tokens.int()):
+        assert torch.equal(sol.sol_embedding_backward(dy, t, vocab, dtable_dtype=torch.float32), want)
+    pad = int(tokens[n // 2])                                     # a row of the table as padding
+    other = torch.where(tokens == pad, -1, tokens)
+    assert torch.equal(sol.sol_embedding_backward(dy, tokens, vocab, pad=pad, dtable_dtype=torch.float32), sol.sol_embedding_backward(dy, other, vocab, dtable_dtype=torch.float32))
+    del dy, want
+    torch.cuda.empty_cache()
+
+
+def test_sums_in_the_order_of_tokens(sol):
+    """fp32 sums of runs up to 64 tokens are those of the tokens' order, one addition behind the other."""
+    rng = np.random.default_rng(8)
+    for n, vocab, cols in ((3000, 100, 1000), (3000, 100, 24)):
+        tok = rng.permutation(np.concatenate([np.full(k % 64 + 1, k) for k in range(vocab)])[:n])
+        dy = rng.standard_normal((len(tok), cols)).astype(np.float32)
+        want = np.zeros((vocab, cols), np.float32)
+        for i, t in enumerate(tok):
+            want[t] = want[t] + dy[i]
+        got = sol.sol_embedding_backward(dev(dy), torch.from_numpy(tok).to(DEV), vocab)
+        assert len(tok) > 512 and np.array_equal(got.cpu().numpy(), want)
+
+
+def test_clip_of_more_tensors_than_tables_hold(sol):
+    """Six launches a pass, and more partial sums than every workgroup joins itself."""
+    gen = torch.Generator(device=DEV).manual_seed(4)
+    grads = [torch.randn(65536 + i, generator=gen, device=DEV) for i in range(900)]
+    grads[17] = torch.empty(0, device=DEV)
+    want = float(np.sqrt(sum(float((g.double() ** 2).sum()) for g in grads)))
+    out = [torch.zeros_like(g) for g in grads]
+    assert abs(float(sol.sol_grad_norm(grads)) - want) <= 1.01 * U * want
+    norm = float(sol.sol_grad_clip(grads, want / 3, out=out))
+    assert abs(norm - want) <= 1.01 * U * want
+    f = torch.tensor(want / 3, dtype=torch.float32).item() / np.float32(norm)
+    assert all(torch.allclose(o, g * float(f), rtol=3 * U, atol=0) for o, g in zip(out, grads))
+    before = [g.clone() for g in grads]
+    assert float(sol.sol_grad_clip(grads, 2 * want)) == norm and all(torch.equal(a, b) for a, b in zip(before, grads))
+    with pytest.raises(sol.SolError) as e:
+        sol.sol_grad_norm([grads[0]] * 32769)
+    assert e.value.status == 6
