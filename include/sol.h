@@ -309,7 +309,7 @@ typedef struct {
     int pad;                    /* -1, which is no row of the table, where there is no padding token */
 } sol_embedding_desc;
 
-/* tokens: device [tokens];  table: [vocab][cols] with pitch ldt;  y: [tokens][cols] with pitch ldy, must not overlap the table.  tokens = 0 does nothing. */
+/* tokens: device [tokens], aligned to their own size (a slice of a stream of tokens will do);  table: [vocab][cols] with pitch ldt;  y: [tokens][cols] with pitch ldy, must not overlap the table.  tokens = 0 does nothing. */
 sol_status sol_embedding(const sol_embedding_desc *ed, const void *tokens, const void *table, void *y, void *hip_stream);
 
 /* Device scratch that sol_embedding_backward needs: the tokens' positions sorted by token, and sums of parts of the longest runs.  Calls that may run at the same time need
@@ -337,7 +337,7 @@ typedef struct {
 /* Device scratch of sol_grad_norm and sol_grad_clip for these tensors (their counts are what matters).  Calls that may run at the same time need scratch of their own. */
 size_t sol_grad_workspace_bytes(const sol_grad *grads, int tensors);
 
-/* grads: host array of `tensors` entries, at most 2^15, read during the call.  norm: device fp32.  Squares are summed in 64 bits, in an order that the counts fix.
+/* grads: host array of `tensors` entries, at most 2^15 with fewer than 2^40 elements in all, read during the call.  norm: device fp32.  Squares are summed in 64 bits, in an order that the counts fix.
  * No two entries of sol_grad_clip may share memory, but for an entry's out in place of its grad.  No tensors: norm 0. */
 sol_status sol_grad_norm(const sol_grad *grads, int tensors, float *norm, void *workspace, size_t workspace_bytes, void *hip_stream);
 sol_status sol_grad_clip(const sol_grad *grads, int tensors, float max_norm, float *norm, void *workspace, size_t workspace_bytes,

@@ -82,7 +82,7 @@ template <typename I, bool PAD> __device__ __forceinline__ uint32_t look_at_toke
         const int at = base + q * (INDEX_THREADS * 4) + (int)threadIdx.x * 4;
         if (at + 4 <= a.n) {
 #pragma unroll
-            for (int k = 0; k < (int)sizeof(I) / 4; k++) reinterpret_cast<uint4 *>(raw + q * 4)[k] = reinterpret_cast<const uint4 *>(p + at)[k];
+            for (int k = 0; k < (int)sizeof(I) / 4; k++) reinterpret_cast<lds_pipe::u32x4_t *>(raw + q * 4)[k] = reinterpret_cast<const u32x4_any *>(p + at)[k];
         } else {
 #pragma unroll
             for (int j = 0; j < 4; j++) raw[q * 4 + j] = at + j < a.n ? p[at + j] : (I)-1;
@@ -626,6 +626,11 @@ sol_status check_embed(const sol_embedding_desc *ed, sol_embedding_desc *d) {
     return SOL_OK;
 }
 
+sol_status check_tokens(const void *tokens, int bits) {
+    SOL_REQUIRE((reinterpret_cast<uintptr_t>(tokens) & (bits / 8 - 1)) == 0, SOL_ERR_ALIGN, "tokens of %d bits must be aligned to them", bits);
+    return SOL_OK;
+}
+
 template <typename T, typename I> sol_status launch_embed_of(const EmbedArgs &a, hipStream_t st) {
     const int per = (256 >> a.lanes_log2) * KEEP;
     const dim3 grid((unsigned)ceil_div(a.cols, 64 * 16 / (int)sizeof(T)), (unsigned)min(ceil_div(a.n, per), 65535));
@@ -689,7 +694,8 @@ sol_status sol_embedding(const sol_embedding_desc *ed, const void *tokens, const
     SOL_TRY(check_embed(ed, &d));
     if (d.tokens == 0) return SOL_OK;
     SOL_REQUIRE(tokens && table && y, SOL_ERR_NULL, "tokens, table and y must not be NULL");
-    SOL_REQUIRE(aligned16(tokens) && aligned16(table) && aligned16(y), SOL_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    SOL_TRY(check_tokens(tokens, d.token_bits));
+    SOL_REQUIRE(aligned16(table) && aligned16(y), SOL_ERR_ALIGN, "device pointers must be 16-byte aligned");
     SOL_REQUIRE(y != table && y != tokens, SOL_ERR_UNSUPPORTED, "embedding: y must not alias the table or the tokens");
     hipStream_t st = (hipStream_t)stream;
     const EmbedArgs a{tokens, table, y, d.ldt, d.ldy, d.tokens, d.vocab, d.cols, d.pad, row_lanes_log2(d.cols, 16 / (int)dtype_size(d.dtype)), d.scale};
@@ -707,7 +713,8 @@ sol_status sol_embedding_backward(const sol_embedding_desc *ed, const void *toke
     SOL_TRY(check_embed(ed, &d));
     SOL_REQUIRE(dtable_dtype == d.dtype || dtable_dtype == SOL_F32, SOL_ERR_DTYPE, "dtable is of the table's dtype or fp32, not %d", dtable_dtype);
     SOL_REQUIRE(dtable && (d.tokens == 0 || (tokens && dy)), SOL_ERR_NULL, "tokens, dy and dtable must not be NULL");
-    SOL_REQUIRE(aligned16(tokens) && aligned16(dy) && aligned16(dtable), SOL_ERR_ALIGN, "device pointers must be 16-byte aligned");
+    SOL_TRY(check_tokens(tokens, d.token_bits));
+    SOL_REQUIRE(aligned16(dy) && aligned16(dtable), SOL_ERR_ALIGN, "device pointers must be 16-byte aligned");
     SOL_REQUIRE(dtable != dy && dtable != tokens, SOL_ERR_UNSUPPORTED, "embedding backward: dtable must not alias dy or the tokens");
     const EmbedPlan p = embed_plan(d);
     SOL_TRY(check_scratch(workspace, workspace_bytes, p.bytes));

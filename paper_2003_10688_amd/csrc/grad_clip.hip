@@ -151,14 +151,14 @@ template <bool STREAM> __global__ void __launch_bounds__(256) grad_scale_kernel(
 
 uint64_t chunks_of(const sol_grad &g) { return (g.count + CHUNK - 1) / CHUNK; }
 
-// How many tensors from `at` on fit one launch; *chunks: theirs
+// How many tensors from `at` on fit one launch; *chunks: theirs (2^27 at most, from fewer than 2^40 elements)
 int table_end(const sol_grad *grads, int tensors, int at, uint64_t *chunks) {
     int n = 0;
     *chunks = 0;
     for (; at < tensors; at++) {
         const uint64_t k = chunks_of(grads[at]);
         if (k == 0) continue;
-        if (n == TABLE || (n && *chunks + k > 0x7fffffffu)) break;
+        if (n == TABLE) break;
         *chunks += k;
         n++;
     }
@@ -198,11 +198,12 @@ sol_status check_grads(const sol_grad *grads, int tensors, bool out) {
     SOL_REQUIRE(tensors >= 0, SOL_ERR_SHAPE, "%d tensors", tensors);
     SOL_REQUIRE(grads || tensors == 0, SOL_ERR_NULL, "the list of gradients is NULL");
     SOL_REQUIRE(tensors <= MAX_TENSORS, SOL_ERR_UNSUPPORTED, "more than 2^15 tensors: %d", tensors);
+    uint64_t total = 0;
     for (int i = 0; i < tensors; i++) {
         const sol_grad &g = grads[i];
         SOL_REQUIRE(g.dtype == SOL_F32 || g.dtype == SOL_BF16, SOL_ERR_DTYPE, "gradient %d: unknown dtype %d", i, g.dtype);
         if (g.count == 0) continue;
-        SOL_REQUIRE(g.count < (1ull << 40), SOL_ERR_UNSUPPORTED, "gradient %d: 2^40 elements or more", i);
+        SOL_REQUIRE(g.count < (1ull << 40) && (total += g.count) < (1ull << 40), SOL_ERR_UNSUPPORTED, "gradients up to %d: 2^40 elements or more", i);
         SOL_REQUIRE(g.grad && (g.out || !out), SOL_ERR_NULL, "gradient %d: a pointer is NULL", i);
         const uintptr_t mask = dtype_size(g.dtype) - 1;
         SOL_REQUIRE(!(reinterpret_cast<uintptr_t>(g.grad) & mask) && (!out || !(reinterpret_cast<uintptr_t>(g.out) & mask)), SOL_ERR_ALIGN, "gradient %d is not aligned to its elements", i);

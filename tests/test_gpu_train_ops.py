@@ -831,3 +831,16 @@ def test_clip_of_more_tensors_than_tables_hold(sol):
     with pytest.raises(sol.SolError) as e:
         sol.sol_grad_norm([grads[0]] * 32769)
     assert e.value.status == 6
+
+
+@pytest.mark.parametrize("bits", [torch.int32, torch.int64])
+@pytest.mark.parametrize("n", [300, 5000, 40001])
+def test_tokens_are_a_slice_of_a_stream(sol, bits, n):
+    """Inputs start at any token of a stream, whose neighbours are other tokens."""
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    stream = torch.randint(0, 700, (n + 16,), generator=gen, device=DEV).to(bits)
+    table, dy = torch.randn((700, 40), generator=gen, device=DEV), torch.randint(-2, 3, (n, 40), generator=gen, device=DEV).float()
+    for at in (1, 2, 3, 5):
+        t = stream[at:at + n]
+        assert torch.equal(sol.sol_embedding(t, table), table[t.long()])
+        assert torch.equal(sol.sol_embedding_backward(dy, t, 700), torch.zeros((700, 40), device=DEV).index_add_(0, t.long(), dy))

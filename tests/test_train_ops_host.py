@@ -117,7 +117,7 @@ def test_embedding_refusals(sol):
             assert call(sol, embed_desc(sol, **bad)) == 3, bad
         for bad in (dict(cols=(1 << 20) + 1), dict(ldt=(1 << 21) + 1), dict(vocab=(1 << 24) + 1), dict(tokens=(1 << 30) + 1)):
             assert call(sol, embed_desc(sol, **bad)) == 6, bad
-        assert call(sol, embed_desc(sol), tokens=FAKE + 8) == 4
+        assert call(sol, embed_desc(sol), tokens=FAKE + 2) == 4 and call(sol, embed_desc(sol, bits=64), tokens=FAKE + 4) == 4
     assert embed(sol, embed_desc(sol), table=NULL) == 1 and embed(sol, embed_desc(sol), y=NULL) == 1
     assert embed(sol, embed_desc(sol), table=0x2004) == 4 and embed(sol, embed_desc(sol), y=0x3004) == 4
     assert embed(sol, embed_desc(sol), y=0x2000) == 6 and embed(sol, embed_desc(sol), y=FAKE) == 6
@@ -153,6 +153,8 @@ def test_grad_refusals(sol):
     for e, want in (((NULL, 0x2000, 4, 0), 1), ((0x1000, NULL, 4, 0), 1), ((0x1002, 0x2000, 4, 0), 4), ((0x1000, 0x2002, 4, 0), 4), ((0x1001, 0x2000, 4, 1), 4), ((0x1000, 0x2000, 4, 2), 3),
                     ((0x1000, 0x2000, 1 << 40, 0), 6)):
         assert clip(grads(sol, e)) == want, e
+    assert clip(grads(sol, (0x1000, 0x2000, 1 << 39, 0), (1 << 50, 1 << 51, 1 << 39, 1))) == 6          # together
+    assert clip(grads(sol, *[(0x1000, 0x1000, 0, 0)] * 32769)) == 6
     # memory that two entries share: the same tensor twice, an output on another gradient, overlapping ends, an output that starts inside its own gradient
     for entries in (((0x1000, 0x1000, 4, 0), (0x1000, 0x1000, 4, 0)), ((0x1000, 0x2000, 4, 0), (0x2000, 0x3000, 4, 0)), ((0x1000, 0x5000, 8, 0), (0x3000, 0x5010, 8, 0)),
                     ((0x1000, 0x1004, 8, 0),), ((0x1000, 0x1000, 8, 1), (0x100e, 0x100e, 8, 1)),
