@@ -42,7 +42,7 @@ __device__ __forceinline__ float mean_of(float sum, float n, float inv) {
     return fmaf(fmaf(-m, n, sum), inv, m);
 }
 
-// Means and squared deviations of the waves, put together: mean = sum n_w mean_w / n, deviations = sum (d_w + n_w (mean_w - mean)^2) (Chan, Golub, LeVeque).
+// Sums and squared deviations of the waves, put together: mean = sum s_w / n, deviations = sum (d_w + n_w (mean_w - mean)^2) (Chan, Golub, LeVeque).
 // One barrier a row; two sets of slots in turn, so that the next row's values do not meet readers of this one's.
 template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
 __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) {
@@ -73,7 +73,8 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) 
                 s += WHOLE || sp[k].has(e) ? v[k][e] : 0.f;     // zeros where there is nothing
             }
         }
-        float mean = mean_of(wave_sum(s), (float)n_wave, inv_wave), m2 = 0.f;
+        s = wave_sum(s);
+        float mean = mean_of(s, (float)n_wave, inv_wave), m2 = 0.f;
 #pragma unroll
         for (int k = 0; k < P; k++)
 #pragma unroll
@@ -83,11 +84,11 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) 
             }
         m2 = wave_sum(m2);
         if constexpr (WAVES > 1) {
-            if ((threadIdx.x & 63) == 0) red[phase][lane / 64] = make_float4(mean, m2, (float)n_wave, 0.f);
+            if ((threadIdx.x & 63) == 0) red[phase][lane / 64] = make_float4(mean, m2, (float)n_wave, s);
             __syncthreads();
             float sum = 0.f;
 #pragma unroll
-            for (int w = 0; w < WAVES; w++) sum += red[phase][w].x * red[phase][w].z;
+            for (int w = 0; w < WAVES; w++) sum += red[phase][w].w;
             mean = mean_of(sum, (float)a.cols, a.inv_cols);
             m2 = 0.f;
 #pragma unroll
@@ -468,7 +469,8 @@ sol_status check_norm(const sol_layer_norm_desc *nd, sol_layer_norm_desc *n) {
 }
 
 enum { NORM_FORWARD, NORM_DX, NORM_GRAD };
-constexpr int MAX_REGISTER_GROUPS = 1024;
+// Groups of 8 columns that a row may have in registers: where dx alone is computed, and where gamma and beta or the columns' sums are kept beside it
+constexpr int MAX_DX_GROUPS = 2048, MAX_GROUPS = 1024;
 // Few rows: columns are summed by workgroups of their own, beside the rows', in the same launch.  us, one launch against one pass and a launch for its parts: 512 rows of 2048 bf16 6.0 and 8.6,
 // 1024 rows 9.6 and 10.3, 1536 rows 17.2 and 11.7; 512 rows of 1531 fp32 6.6 and 9.4, 1024 rows 14.1 and 11.9.
 bool few_rows(int rows, int dt) { return (size_t)rows * dtype_size(dt) <= 2048; }
@@ -484,8 +486,13 @@ struct NormLaunch {
 template <int TPR, int G, bool WHOLE, bool STREAM, typename T> void launch_rows_of(const NormLaunch &l, hipStream_t st) {
     constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR;
     const int rows = (int)min(((long)l.a.rows + RPB - 1) / RPB, 2048l);
-    if (l.kind == NORM_FORWARD) hipLaunchKernelGGL((norm_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)rows), dim3(BLOCK), 0, st, l.a);
-    else hipLaunchKernelGGL((norm_dx_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)(l.cols.blocks + (l.a.y ? rows : 0))), dim3(BLOCK), 0, st, l.a, l.cols);
+    if constexpr (TPR * G <= MAX_GROUPS) {
+        if (l.kind == NORM_FORWARD) {
+            hipLaunchKernelGGL((norm_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)rows), dim3(BLOCK), 0, st, l.a);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((norm_dx_kernel<TPR, G, WHOLE, STREAM, T>), dim3((unsigned)(l.cols.blocks + (l.a.y ? rows : 0))), dim3(BLOCK), 0, st, l.a, l.cols);
 }
 template <typename T> bool whole_rows(int cols) { return cols % (16 / sizeof(T)) == 0; }
 template <typename T> bool streamed(const NormArgs &a) { return (size_t)a.rows * a.cols * sizeof(T) >= STREAM_BYTES; }
@@ -505,7 +512,7 @@ template <int TPR, int G, bool WHOLE, typename T> void launch_grad(const NormLau
 }
 template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st) {
     const int groups = ceil_div(l.a.cols, 8);
-    if (groups > MAX_REGISTER_GROUPS) {
+    if (groups > (l.kind == NORM_DX ? MAX_DX_GROUPS : MAX_GROUPS)) {
         const dim3 grid((unsigned)min(l.a.rows, 1024));
         if (l.kind == NORM_FORWARD) hipLaunchKernelGGL(norm_long_kernel<T>, grid, dim3(1024), 0, st, l.a);
         else hipLaunchKernelGGL(norm_dx_long_kernel<T>, grid, dim3(1024), 0, st, l.a);
@@ -514,7 +521,8 @@ template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st
         else if (groups <= 128) launch_rows<128, 1, T>(l, st);
         else if (groups <= 256) launch_rows<256, 1, T>(l, st);
         else if (groups <= 512) launch_rows<256, 2, T>(l, st);
-        else launch_rows<512, 2, T>(l, st);
+        else if (groups <= 1024) launch_rows<512, 2, T>(l, st);
+        else launch_rows<1024, 2, T>(l, st);
     } else if (whole_rows<T>(l.a.cols)) {
         if (groups <= 64) launch_grad<64, 1, true, T>(l, st);
         else if (groups <= 128) launch_grad<128, 1, true, T>(l, st);
@@ -536,8 +544,8 @@ sol_status launch_norm(const NormLaunch &l, int dt, hipStream_t st) { return dt 
 // Parts that dgamma and dbeta are summed in: 1 where workgroups beside the rows' sum whole columns
 int norm_parts(int rows, int cols, int dt) {
     const int groups = ceil_div(cols, 8);
-    if (groups > MAX_REGISTER_GROUPS) return norm_chunks(rows, cols);
-    if (few_rows(rows, dt)) return 1;
+    if (groups <= MAX_DX_GROUPS && few_rows(rows, dt)) return 1;
+    if (groups > MAX_GROUPS) return norm_chunks(rows, cols);
     const bool whole = cols % (16 / (int)dtype_size(dt)) == 0;
     const int threads = groups <= 64 ? 64 : groups <= 128 ? 128 : groups <= 256 ? 256 : !whole ? (groups <= 512 ? 256 : 512) : groups <= 512 ? 512 : 1024;
     const int slots = (whole ? GRAD_BLOCK<true> : GRAD_BLOCK<false>) / threads;
@@ -607,7 +615,7 @@ sol_status sol_layer_norm_backward(const sol_layer_norm_desc *nd, const void *dy
     NormArgs &a = l.a;
     a.x = x; a.dy = dy; a.residual = residual; a.gamma = gamma; a.mean_in = mean; a.rstd_in = rstd; a.y = dx;
     a.ldx = n.ldx; a.ldy = n.ldy; a.rows = n.rows; a.cols = n.cols; a.inv_cols = 1.f / (float)n.cols;
-    const bool columns = dgamma || dbeta, wide = ceil_div(n.cols, 8) > MAX_REGISTER_GROUPS;
+    const bool columns = dgamma || dbeta, few = ceil_div(n.cols, 8) <= MAX_DX_GROUPS && few_rows(n.rows, n.dtype), wide = ceil_div(n.cols, 8) > MAX_GROUPS && !few;
     if (!columns && !dx) return SOL_OK;
     // where the columns' sums go: parts, which a launch behind puts together, or their own place
     const int parts = norm_parts(n.rows, n.cols, n.dtype);
@@ -626,11 +634,12 @@ sol_status sol_layer_norm_backward(const sol_layer_norm_desc *nd, const void *dy
             if (n.dtype == SOL_BF16) hipLaunchKernelGGL(norm_columns_kernel<bf16_t>, grid, dim3(1024), 0, st, l.cols);
             else hipLaunchKernelGGL(norm_columns_kernel<float>, grid, dim3(1024), 0, st, l.cols);
             SOL_HIP(hipGetLastError());
+            l.cols = NormColumns{};
         }
         l.kind = NORM_DX;
         if (dx) SOL_TRY(launch_norm(l, n.dtype, st));
     } else {
-        l.kind = columns && !few_rows(n.rows, n.dtype) ? NORM_GRAD : NORM_DX;
+        l.kind = columns && !few ? NORM_GRAD : NORM_DX;
         l.groups = parts;
         l.dgamma = pg;
         l.dbeta = pb;

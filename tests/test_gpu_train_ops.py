@@ -844,3 +844,26 @@ def test_tokens_are_a_slice_of_a_stream(sol, bits, n):
         t = stream[at:at + n]
         assert torch.equal(sol.sol_embedding(t, table), table[t.long()])
         assert torch.equal(sol.sol_embedding_backward(dy, t, 700), torch.zeros((700, 40), device=DEV).index_add_(0, t.long(), dy))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(3, 8193), (600, 8200), (1100, 16384), (5, 16384), (1100, 16380), (4, 16385), (1100, 16392), (513, 12289)])
+def test_wide_rows(sol, dt, rows, cols):
+    """Between the rows that all kernels hold in registers and those that none does: columns' sums of whole numbers to the last bit, y and dx against 64 bits."""
+    rng = np.random.default_rng([cols, rows])
+    x, dy = rng.integers(-2, 3, (rows, cols)), rng.integers(-2, 3, (rows, cols))
+    args = (dev(dy, dt, 1), dev(x, dt, 1), torch.zeros(rows, device=DEV), torch.ones(rows, device=DEV))
+    dx, dg, db = sol.sol_layer_norm_backward(*args)
+    assert np.array_equal(host(dg), (x * dy).sum(0)) and np.array_equal(host(db), dy.sum(0))
+    alone = sol.sol_layer_norm_backward(*args, need_dgamma=False, need_dbeta=False)[0]
+    wx, _, _ = to.layer_norm_bwd(dy, x, np.zeros(rows), np.ones(rows))
+    c1, c2 = np.abs(dy.mean(1, keepdims=True)), np.abs((dy * x).mean(1, keepdims=True))
+    for got in (dx, alone):
+        close(host(got), wx, 4 * U * (np.abs(dy) + c1 + 2 * np.abs(x) * c2) + 2 * U * np.abs(wx) + HALF[dt] * np.abs(wx) * 1.02, "dx")
+    y, mean, rstd = sol.sol_layer_norm(dev(x, dt, 1), want_stats=True)
+    wy, wm, wr = to.layer_norm(x)
+    # a whole sum: exact, so the mean is off by its division alone, deviations by a rounding, their squares' sum by 8 * (cols / 8192 + 2) + 48 additions at most
+    close(host(mean), wm, 2 * U * np.abs(wm), "mean")
+    er = (4 * (cols // 8192 + 2) + 30) * U + 8 * 2 * U
+    close(host(rstd), wr, er * wr, "rstd")
+    close(host(y), wy, (er + 4 * U) * np.abs(wy) + 4 * U * wr[:, None] + HALF[dt] * np.abs(wy) * 1.02, "y")
