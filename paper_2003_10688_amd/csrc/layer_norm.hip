@@ -33,8 +33,9 @@ template <int W> __device__ __forceinline__ void load_weight(const float *w, con
 #pragma unroll
     for (int e = 0; e < W; e++) v[e] = !sp.has(e) ? 0.f : w ? raw.get(e) : none;
 }
-// A row for TPR threads: four rows a workgroup where one wave takes a row and none waits for another, else one
-template <int TPR> constexpr int ROW_BLOCK = TPR == 64 ? 256 : TPR;
+// A row for TPR threads, 8 to 1024: workgroups of 256 where a row's threads are in one wave and none waits for another, else one row a workgroup
+template <int TPR> constexpr int ROW_BLOCK = TPR <= 64 ? 256 : TPR;
+template <int TPR> constexpr int ROW_WAVES = TPR <= 64 ? 1 : TPR / 64;
 
 // sum / n with the reciprocal and one correction, so that equal elements whose sum is exact have their own value for a mean
 __device__ __forceinline__ float mean_of(float sum, float n, float inv) {
@@ -46,7 +47,7 @@ __device__ __forceinline__ float mean_of(float sum, float n, float inv) {
 // One barrier a row; two sets of slots in turn, so that the next row's values do not meet readers of this one's.
 template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
 __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) {
-    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64, W = 16 / sizeof(T), P = G * 8 / W;
+    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = ROW_WAVES<TPR>, W = 16 / sizeof(T), P = G * 8 / W;
     __shared__ float4 red[2][WAVES];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
     const Spans<W, P> sp(lane * W, TPR * W, a.cols);
@@ -56,11 +57,11 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) 
     for (int k = 0; k < P; k++) {
         load_weight(a.gamma, sp[k], 1.f, gm[k]);
         load_weight(a.beta, sp[k], 0.f, bt[k]);
-        n_wave += max(0, min(64 * W, a.cols - (lane / 64 * 64 + k * TPR) * W));
+        n_wave += max(0, min((TPR < 64 ? TPR : 64) * W, a.cols - (lane / 64 * 64 + k * TPR) * W));
     }
     const float inv_wave = n_wave ? 1.f / (float)n_wave : 0.f;
     int phase = 0;
-    for (long row = (long)blockIdx.x * RPB + slot; row < a.rows; row += (long)gridDim.x * RPB) {      // with TPR > 64 a workgroup has one row at a time: every thread meets every barrier
+    for (long row = (long)blockIdx.x * RPB + slot; row < a.rows; row += (long)gridDim.x * RPB) {      // above 64 threads a row a workgroup has one at a time: every thread meets every barrier
         const T *x = static_cast<const T *>(a.x) + row * a.ldx;
         float v[P][W], s = 0.f;
 #pragma unroll
@@ -73,7 +74,7 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) 
                 s += WHOLE || sp[k].has(e) ? v[k][e] : 0.f;     // zeros where there is nothing
             }
         }
-        s = wave_sum(s);
+        s = group_sum<TPR>(s);
         float mean = mean_of(s, (float)n_wave, inv_wave), m2 = 0.f;
 #pragma unroll
         for (int k = 0; k < P; k++)
@@ -82,7 +83,7 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) 
                 const float d = (WHOLE ? sp[k].some() : sp[k].has(e)) ? v[k][e] - mean : 0.f;
                 m2 += d * d;
             }
-        m2 = wave_sum(m2);
+        m2 = group_sum<TPR>(m2);
         if constexpr (WAVES > 1) {
             if ((threadIdx.x & 63) == 0) red[phase][lane / 64] = make_float4(mean, m2, (float)n_wave, s);
             __syncthreads();
@@ -241,7 +242,7 @@ template <int P, int W> __device__ __forceinline__ void row_products(const float
 // dx, a row for TPR threads; the workgroups in front sum the columns where there are few rows, so that both take one launch: the data is read twice, but the second time from the caches
 template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
 __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs a, const NormColumns cols) {
-    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = TPR / 64, W = 16 / sizeof(T), P = G * 8 / W;
+    constexpr int BLOCK = ROW_BLOCK<TPR>, RPB = BLOCK / TPR, WAVES = ROW_WAVES<TPR>, W = 16 / sizeof(T), P = G * 8 / W;
     __shared__ union {
         float columns[2][BLOCK / 8][64 + 4];
         float2 red[2][WAVES];
@@ -272,8 +273,8 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
             }
         }
         row_products(g, h, s1, s2);
-        s1 = wave_sum(s1);
-        s2 = wave_sum(s2);
+        s1 = group_sum<TPR>(s1);
+        s2 = group_sum<TPR>(s2);
         if constexpr (WAVES > 1) {
             if ((threadIdx.x & 63) == 0) s.red[phase][lane / 64] = make_float2(s1, s2);
             __syncthreads();
@@ -306,9 +307,9 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
 template <bool WHOLE> constexpr int GRAD_BLOCK = WHOLE ? 1024 : 512;
 template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
 __global__ void __launch_bounds__(GRAD_BLOCK<WHOLE>) norm_grad_kernel(const NormArgs a, float *dgamma, float *dbeta) {
-    constexpr int SLOTS = GRAD_BLOCK<WHOLE> / TPR, WAVES = TPR / 64, W = 16 / sizeof(T), P = G * 8 / W;
+    constexpr int SLOTS = GRAD_BLOCK<WHOLE> / TPR, WAVES = ROW_WAVES<TPR>, W = 16 / sizeof(T), P = G * 8 / W;
     __shared__ float2 red[2][GRAD_BLOCK<WHOLE> / 64];
-    __shared__ float sums[SLOTS > 1 ? SLOTS - 1 : 1][TPR * G * 8];
+    __shared__ float sums[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? TPR * G * 8 : 1];
     const int lane = threadIdx.x % TPR, slot = threadIdx.x / TPR;
     const Spans<W, P> sp(lane * W, TPR * W, a.cols);
     float gm[P][W], sg[P][W], sb[P][W];
@@ -359,8 +360,8 @@ __global__ void __launch_bounds__(GRAD_BLOCK<WHOLE>) norm_grad_kernel(const Norm
         fetch(row);
         if (a.y) {
             if (there) row_products(g, h, s1, s2);
-            s1 = wave_sum(s1);
-            s2 = wave_sum(s2);
+            s1 = group_sum<TPR>(s1);
+            s2 = group_sum<TPR>(s2);
             if constexpr (WAVES > 1) {
                 if ((threadIdx.x & 63) == 0) red[phase][threadIdx.x / 64] = make_float2(s1, s2);
                 __syncthreads();
@@ -383,31 +384,29 @@ __global__ void __launch_bounds__(GRAD_BLOCK<WHOLE>) norm_grad_kernel(const Norm
             }
         }
     }
-    // the slots' sums, in their order
+    // the slots' sums, in their order, a column a thread
 #pragma unroll
     for (int which = 0; which < 2; which++) {
         float (&s)[P][W] = which == 0 ? sg : sb;
         float *part = which == 0 ? dgamma : dbeta;
         if (!part) continue;
-        if constexpr (SLOTS > 1) {
+        part += (size_t)blockIdx.x * a.cols;
+        if constexpr (SLOTS == 1) {
+#pragma unroll
+            for (int k = 0; k < P; k++) sp[k].template store<WHOLE>(part, s[k]);
+        } else {
             __syncthreads();
-            if (slot > 0) {
 #pragma unroll
-                for (int k = 0; k < P; k++)
+            for (int k = 0; k < P; k++)
 #pragma unroll
-                    for (int e = 0; e < W; e++) sums[slot - 1][(k * W + e) * TPR + lane] = s[k][e];
-            }
+                for (int e = 0; e < W; e++)
+                    if (sp[k].has(e)) sums[slot][sp[k].c + e] = s[k][e];
             __syncthreads();
-        }
-        if (slot == 0) {
+            for (int c = threadIdx.x; c < a.cols; c += GRAD_BLOCK<WHOLE>) {
+                float v = 0.f;
 #pragma unroll
-            for (int k = 0; k < P; k++) {
-                if constexpr (SLOTS > 1) {
-#pragma unroll
-                    for (int e = 0; e < W; e++)
-                        for (int q = 0; q < SLOTS - 1; q++) s[k][e] += sums[q][(k * W + e) * TPR + lane];
-                }
-                sp[k].template store<WHOLE>(part + (size_t)blockIdx.x * a.cols, s[k]);
+                for (int q = 0; q < SLOTS; q++) v += sums[q][c];
+                part[c] = v;
             }
         }
     }
@@ -517,20 +516,29 @@ template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st
         if (l.kind == NORM_FORWARD) hipLaunchKernelGGL(norm_long_kernel<T>, grid, dim3(1024), 0, st, l.a);
         else hipLaunchKernelGGL(norm_dx_long_kernel<T>, grid, dim3(1024), 0, st, l.a);
     } else if (l.kind != NORM_GRAD) {
-        if (groups <= 64) launch_rows<64, 1, T>(l, st);
+        if (groups <= 8) launch_rows<8, 1, T>(l, st);
+        else if (groups <= 16) launch_rows<16, 1, T>(l, st);
+        else if (groups <= 32) launch_rows<32, 1, T>(l, st);
+        else if (groups <= 64) launch_rows<64, 1, T>(l, st);
         else if (groups <= 128) launch_rows<128, 1, T>(l, st);
         else if (groups <= 256) launch_rows<256, 1, T>(l, st);
         else if (groups <= 512) launch_rows<256, 2, T>(l, st);
         else if (groups <= 1024) launch_rows<512, 2, T>(l, st);
         else launch_rows<1024, 2, T>(l, st);
     } else if (whole_rows<T>(l.a.cols)) {
-        if (groups <= 64) launch_grad<64, 1, true, T>(l, st);
+        if (groups <= 8) launch_grad<8, 1, true, T>(l, st);
+        else if (groups <= 16) launch_grad<16, 1, true, T>(l, st);
+        else if (groups <= 32) launch_grad<32, 1, true, T>(l, st);
+        else if (groups <= 64) launch_grad<64, 1, true, T>(l, st);
         else if (groups <= 128) launch_grad<128, 1, true, T>(l, st);
         else if (groups <= 256) launch_grad<256, 1, true, T>(l, st);
         else if (groups <= 512) launch_grad<512, 1, true, T>(l, st);
         else launch_grad<1024, 1, true, T>(l, st);
     } else {
-        if (groups <= 64) launch_grad<64, 1, false, T>(l, st);
+        if (groups <= 8) launch_grad<8, 1, false, T>(l, st);
+        else if (groups <= 16) launch_grad<16, 1, false, T>(l, st);
+        else if (groups <= 32) launch_grad<32, 1, false, T>(l, st);
+        else if (groups <= 64) launch_grad<64, 1, false, T>(l, st);
         else if (groups <= 128) launch_grad<128, 1, false, T>(l, st);
         else if (groups <= 256) launch_grad<256, 1, false, T>(l, st);
         else if (groups <= 512) launch_grad<256, 2, false, T>(l, st);
@@ -547,7 +555,7 @@ int norm_parts(int rows, int cols, int dt) {
     if (groups <= MAX_DX_GROUPS && few_rows(rows, dt)) return 1;
     if (groups > MAX_GROUPS) return norm_chunks(rows, cols);
     const bool whole = cols % (16 / (int)dtype_size(dt)) == 0;
-    const int threads = groups <= 64 ? 64 : groups <= 128 ? 128 : groups <= 256 ? 256 : !whole ? (groups <= 512 ? 256 : 512) : groups <= 512 ? 512 : 1024;
+    const int threads = groups <= 8 ? 8 : groups <= 16 ? 16 : groups <= 32 ? 32 : groups <= 64 ? 64 : groups <= 128 ? 128 : groups <= 256 ? 256 : !whole ? (groups <= 512 ? 256 : 512) : groups <= 512 ? 512 : 1024;
     const int slots = (whole ? GRAD_BLOCK<true> : GRAD_BLOCK<false>) / threads;
     const long rounds = ((long)rows + slots - 1) / slots, most = min(rounds, groups <= 256 && !whole ? 512l : 256l);
     // A round of rows costs a workgroup about what 32 more parts cost the launch that sums them: 32 rounds = parts^2 makes the sum of both least.  Up to a GPU full of workgroups.

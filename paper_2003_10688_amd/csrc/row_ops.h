@@ -149,6 +149,17 @@ template <int W, int COUNT> struct Spans {
     __device__ __forceinline__ const Span<W> &operator[](int k) const { return of[k]; }
 };
 
+// The sum over groups of LANES lanes (8, 16, 32 or the wave's 64), in all of a group's lanes
+template <int LANES> __device__ __forceinline__ float group_sum(float v) {
+    if constexpr (LANES >= 64) return wave_sum(v);
+    v += dpp_from<0xB1, 0xf>(v);
+    v += dpp_from<0x4E, 0xf>(v);
+    v += dpp_from<0x141, 0xf>(v);
+    if constexpr (LANES >= 16) v += dpp_from<0x140, 0xf>(v);
+    if constexpr (LANES >= 32) v += __uint_as_float((uint32_t)__builtin_amdgcn_ds_swizzle((int)__float_as_uint(v), 0x401f));      // lane ^ 16
+    return v;
+}
+
 constexpr int MAX_COLS = 1 << 20, MAX_ROW_PITCH = 1 << 21;
 
 inline sol_status check_row_pitch(const char *what, int cols, int *ld) {

@@ -867,3 +867,26 @@ def test_wide_rows(sol, dt, rows, cols):
     er = (4 * (cols // 8192 + 2) + 30) * U + 8 * 2 * U
     close(host(rstd), wr, er * wr, "rstd")
     close(host(y), wy, (er + 4 * U) * np.abs(wy) + 4 * U * wr[:, None] + HALF[dt] * np.abs(wy) * 1.02, "y")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [1, 2, 3, 4, 5, 7, 8, 9, 12, 60, 63, 64, 65, 100, 127, 128, 129, 200, 255, 256, 257, 260])
+def test_narrow_rows(sol, dt, cols):
+    """8 to 64 threads a row: rows that fill a wave's groups and that do not, in one launch and in two, with stored statistics that each row has of its own."""
+    for rows in (1, 31, 1000, 4099):
+        rng = np.random.default_rng([cols, rows])
+        x = grid(rng.standard_normal((rows, cols)) * 2.0 ** rng.integers(-3, 4, (rows, 1)) + rng.integers(-2, 3, (rows, 1)), dt)
+        y, mean, rstd = sol.sol_layer_norm(dev(x, dt, 3), eps=1e-2, want_stats=True)
+        wy, wm, wr = to.layer_norm(x, eps=1e-2)
+        em, er = norm_tolerances(x, wm, wr, cols)
+        close(host(mean), wm, em + U * np.abs(wm), "mean")
+        close(host(rstd), wr, er * wr, "rstd")
+        close(host(y), wy, (em + 2 * U * np.abs(x - wm[:, None]).max(1))[:, None] * wr[:, None] * 1.01 + (er[:, None] + 4 * U) * np.abs(wy) + HALF[dt] * np.abs(wy) * 1.02, "y")
+        whole, dy, res = rng.integers(-2, 3, (rows, cols)), rng.integers(-2, 3, (rows, cols)), rng.integers(-2, 3, (rows, cols))
+        m, r = rng.integers(-1, 2, rows), 2.0 ** rng.integers(-1, 2, rows)      # (x - mean) rstd and its products are whole halves
+        dx, dg, db = sol.sol_layer_norm_backward(dev(dy, dt, 1), dev(whole, dt), dev(m), dev(r), residual=dev(res, dt))
+        wx, wg, wb = to.layer_norm_bwd(dy, whole, m, r, None, res)
+        assert np.array_equal(host(dg), wg) and np.array_equal(host(db), wb)
+        h = np.abs(whole - m[:, None]) * r[:, None]
+        c1, c2 = np.abs(dy.mean(1, keepdims=True)), np.abs((dy * (whole - m[:, None]) * r[:, None]).mean(1, keepdims=True))
+        close(host(dx), wx, r[:, None] * 4 * U * (np.abs(dy) + c1 + 2 * h * c2) + 2 * U * (np.abs(res) + np.abs(wx)) + HALF[dt] * np.abs(wx) * 1.02, "dx")
