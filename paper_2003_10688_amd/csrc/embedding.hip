@@ -17,7 +17,6 @@ int row_lanes_log2(int cols, int each) {
     while (l < 6 && (1 << l) < pieces) l++;
     return l;
 }
-int row_slabs(int cols) { return ceil_div(cols, 512); }
 
 struct EmbedArgs {
     const void *tokens, *table;
@@ -26,7 +25,7 @@ struct EmbedArgs {
     int n, vocab, cols, pad, lanes_log2;
     float scale;
 };
-// 16 bytes of a row for a lane: 2^lanes_log2 lanes, or slabs of 64, which vary fastest (see embed_wide_kernel); KEEP tokens of a lane under way at a time.  65536 tokens of 2048 bf16: one token 99 us,
+// 16 bytes of a row for a lane: 2^lanes_log2 lanes, or slabs of 64, which vary fastest (see embed_sum_kernel); KEEP tokens of a lane under way at a time.  65536 tokens of 2048 bf16: one token 99 us,
 // two 96, four 90 with ordinary stores, 54 to 57 with two to eight past the caches; 8 tokens of 4096 4.2, 4.5 and 5.2 us.
 constexpr int KEEP = 2;
 template <typename T, typename I, bool STREAM> __global__ void __launch_bounds__(256) embed_kernel(const EmbedArgs a) {
@@ -280,7 +279,7 @@ struct GatherArgs {
     const int *start, *order, *sorted;
     float *part;                // [windows][2][cols]: sums of the parts of long runs that a window of RUN positions holds, of the run that reaches in first, of the one that leaves it second
     long ldy;
-    int vocab, cols, windows, accumulate, lanes_log2;
+    int vocab, cols, windows, accumulate;
     int rows, log2, places;         // as the index has them
     float scale;
     FastDiv by_rows;
@@ -289,64 +288,6 @@ __device__ __forceinline__ int row_of_place(const GatherArgs &a, int place) {
     uint32_t q, r;
     a.by_rows.divmod((uint32_t)place, q, r);
     return (int)(r << a.log2 | q);
-}
-
-// A lane's 8 columns of a slab of 8 * lanes: two quads half a slab apart where fp32 is written, so that a wave's store covers whole lines, else 8 neighbours.
-template <typename T, typename TO> struct Columns {
-    static constexpr bool QUADS = sizeof(TO) == 4;
-    int c, apart, nv0, nv1;
-    __device__ __forceinline__ Columns(int slab, int lane, int lanes, int cols) {
-        c = slab * 512 + lane * (QUADS ? 4 : 8);
-        apart = QUADS ? lanes * 4 : 0;
-        nv0 = cols - c;
-        nv1 = cols - c - apart;
-    }
-    __device__ __forceinline__ bool none() const { return nv0 <= 0; }
-    template <typename X> __device__ __forceinline__ void load(const X *p, float v[8]) const {
-        if constexpr (QUADS) {
-            load4_any<X>(p + c, v, nv0);
-            load4_any<X>(p + c + apart, v + 4, nv1);
-        } else {
-            load8_any<X>(p + c, v, nv0);
-        }
-    }
-    template <typename X> __device__ __forceinline__ void store(X *p, const float v[8]) const {
-        if constexpr (QUADS) {
-            store4_any<X>(p + c, v, nv0);
-            store4_any<X>(p + c + apart, v + 4, nv1);
-        } else {
-            store8_any<X>(p + c, v, nv0);
-        }
-    }
-};
-
-// acc += the rows order[b .. e), in that order; eight loads under way at a time
-template <typename T, typename C> __device__ __forceinline__ void sum_rows(const GatherArgs &a, const C &cl, int b, int e, float acc[8]) {
-    const T *dy = static_cast<const T *>(a.dy);
-    for (; b + 8 <= e; b += 8) {
-        float v[8][8];
-#pragma unroll
-        for (int u = 0; u < 8; u++) cl.load(dy + (long)a.order[b + u] * a.ldy, v[u]);
-#pragma unroll
-        for (int u = 0; u < 8; u++)
-#pragma unroll
-            for (int k = 0; k < 8; k++) acc[k] += v[u][k];
-    }
-    for (; b < e; b++) {
-        float v[8];
-        cl.load(dy + (long)a.order[b] * a.ldy, v);
-#pragma unroll
-        for (int k = 0; k < 8; k++) acc[k] += v[k];
-    }
-}
-
-template <typename TO, typename C> __device__ __forceinline__ void put_row(const GatherArgs &a, const C &cl, int v, float acc[8]) {
-    TO *out = static_cast<TO *>(a.out) + (size_t)v * a.cols;
-    float old[8];
-    if (a.accumulate) cl.load(out, old);
-#pragma unroll
-    for (int k = 0; k < 8; k++) acc[k] = a.accumulate ? acc[k] * a.scale + old[k] : acc[k] * a.scale;
-    cl.store(out, acc);
 }
 
 // Items: the parts of long runs in each window, two a window, then the table's rows.  A part of a long run:
@@ -362,29 +303,6 @@ __device__ __forceinline__ bool window_part(const GatherArgs &a, int item, Part 
     return true;
 }
 __device__ __forceinline__ int place_of_row(const GatherArgs &a, int v) { return (v & ((1 << a.log2) - 1)) * a.rows + (v >> a.log2); }
-
-// Narrow tables: a row of the table for 8 to 32 lanes
-template <typename T, typename TO> __global__ void __launch_bounds__(256) embed_gather_kernel(const GatherArgs a) {
-    const int log2 = a.lanes_log2, lane = threadIdx.x & ((1 << log2) - 1);
-    const long item = (long)blockIdx.x * (256 >> log2) + (threadIdx.x >> log2);
-    const Columns<T, TO> cl(0, lane, 1 << log2, a.cols);
-    if (cl.none()) return;
-    float acc[8];
-#pragma unroll
-    for (int k = 0; k < 8; k++) acc[k] = 0.f;
-    if (item < 2 * a.windows) {
-        Part q;
-        if (!window_part(a, (int)item, &q)) return;
-        sum_rows<T>(a, cl, q.b, q.e, acc);
-        cl.store(a.part + (size_t)item * a.cols, acc);
-        return;
-    }
-    if (item - 2 * a.windows >= a.vocab) return;
-    const int v = (int)(item - 2 * a.windows), p = place_of_row(a, v), b = a.start[p], e = a.start[p + 1];
-    if (e - b > RUN || (a.accumulate && e == b)) return;
-    sum_rows<T>(a, cl, b, e, acc);
-    put_row<TO>(a, cl, v, acc);
-}
 
 // acc += `many` rows (FLIGHT at most, all of them with FULL: no branch between the loads, which are then under way together); next() gives them one by one
 template <int FLIGHT, bool FULL, typename T, int W, int PIECES, typename F>
@@ -420,8 +338,8 @@ __device__ __forceinline__ void write_row(TO *out, const Spans<W, PIECES> &sp, f
     }
 }
 
-// Wider ones: a wave takes PIECES * 64 * W columns of a row.  Three round trips to memory: where its run is, the positions in it (a lane each), and FLIGHT of the gradient's rows at a time.
-template <typename T, typename TO, int W, int PIECES, bool STREAM> __device__ __forceinline__ void wide_item(const GatherArgs &a, int item, int c0) {
+// A wave takes PIECES * 64 * W columns of a row.  Three round trips to memory: where its run is, the positions in it (a lane each), and FLIGHT of the gradient's rows at a time.
+template <typename T, typename TO, int W, int PIECES, bool STREAM> __device__ __forceinline__ void sum_item(const GatherArgs &a, int item, int c0) {
     constexpr int FLIGHT = 64 / (W * PIECES);
     const int lane = threadIdx.x & 63;
     const bool window = item < 2 * a.windows;
@@ -454,50 +372,48 @@ template <typename T, typename TO, int W, int PIECES, bool STREAM> __device__ __
     write_row<TO, W, PIECES, STREAM>(static_cast<TO *>(a.out) + (size_t)(item - 2 * a.windows) * a.cols, sp, acc, a.scale, a.accumulate);
 }
 // Slabs of columns vary fastest: workgroups that run together then write whole rows, not the same part of every row, whose addresses would fall on a few of the memory's channels.
-template <typename T, typename TO, int W, int PIECES, bool STREAM> __global__ void __launch_bounds__(256) embed_wide_kernel(const GatherArgs a, int items) {
+template <typename T, typename TO, int W, int PIECES, bool STREAM> __global__ void __launch_bounds__(256) embed_sum_kernel(const GatherArgs a, int items) {
     const int c0 = (int)blockIdx.x * (PIECES * 64 * W) + (threadIdx.x & 63) * W;
-    for (int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += (int)gridDim.y * 4) wide_item<T, TO, W, PIECES, STREAM>(a, item, c0);
+    for (int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += (int)gridDim.y * 4) sum_item<T, TO, W, PIECES, STREAM>(a, item, c0);
 }
 
 // A long run ends behind the window that it starts in: at most one starts in each.  A workgroup joins its parts in a slab of columns, a wave a quarter of them, one behind the other.
-template <typename T, typename TO> __global__ void __launch_bounds__(256) embed_join_kernel(const GatherArgs a) {
-    __shared__ float sums[3][8][64];
+template <typename TO, int W, int PIECES> __global__ void __launch_bounds__(256) embed_join_kernel(const GatherArgs a) {
+    constexpr int FLIGHT = 64 / (W * PIECES);
+    __shared__ float sums[3][PIECES * W][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, used = a.start[a.places];
-    const Columns<T, TO> cl((int)blockIdx.x, lane, 64, a.cols);
+    const Spans<W, PIECES> sp((int)blockIdx.x * (PIECES * 64 * W) + lane * W, 64 * W, a.cols);
     for (long win = blockIdx.y; win < a.windows && win * RUN < used; win += gridDim.y) {
         const int p = a.sorted[min(used, (int)win * RUN + RUN) - 1], b = a.start[p], e = a.start[p + 1];
         if (e - b <= RUN || b / RUN != win) continue;       // the same for all threads
-        const int last = (e - 1) / RUN, per = (last - (int)win + 4) / 4, w0 = (int)win + wave * per, w1 = min(last + 1, w0 + per);
-        auto part = [&](int w) { return a.part + (size_t)(2 * (long)w + (w == (int)win && b % RUN ? 1 : 0)) * a.cols; };
-        float acc[8];
+        const int last = (e - 1) / RUN, per = (last - (int)win + 4) / 4, w0 = (int)win + wave * per, many = min(last + 1, w0 + per) - w0;
+        float acc[PIECES][W];
 #pragma unroll
-        for (int k = 0; k < 8; k++) acc[k] = 0.f;
+        for (int i = 0; i < PIECES; i++)
+#pragma unroll
+            for (int k = 0; k < W; k++) acc[i][k] = 0.f;
         int w = w0;
-        for (; w + 8 <= w1; w += 8) {
-            float u[8][8];
-#pragma unroll
-            for (int q = 0; q < 8; q++) cl.load(part(w + q), u[q]);
-#pragma unroll
-            for (int q = 0; q < 8; q++)
-#pragma unroll
-                for (int k = 0; k < 8; k++) acc[k] += u[q][k];
-        }
-        for (; w < w1; w++) {
-            float u[8];
-            cl.load(part(w), u);
-#pragma unroll
-            for (int k = 0; k < 8; k++) acc[k] += u[k];
-        }
+        auto next = [&]() {                                 // the parts' rows
+            const long row = 2 * (long)w + (w == (int)win && b % RUN ? 1 : 0);
+            w++;
+            return row;
+        };
+        while (w + FLIGHT <= w0 + many) add_rows<FLIGHT, true>(a.part, a.cols, sp, FLIGHT, acc, next);
+        if (w < w0 + many) add_rows<FLIGHT, false>(a.part, a.cols, sp, w0 + many - w, acc, next);
         __syncthreads();                                    // the sums of a run in front are read
         if (wave > 0) {
 #pragma unroll
-            for (int k = 0; k < 8; k++) sums[wave - 1][k][lane] = acc[k];
+            for (int i = 0; i < PIECES; i++)
+#pragma unroll
+                for (int k = 0; k < W; k++) sums[wave - 1][i * W + k][lane] = acc[i][k];
         }
         __syncthreads();
-        if (wave > 0 || cl.none()) continue;
+        if (wave > 0) continue;
 #pragma unroll
-        for (int k = 0; k < 8; k++) acc[k] += sums[0][k][lane] + sums[1][k][lane] + sums[2][k][lane];
-        put_row<TO>(a, cl, row_of_place(a, p), acc);
+        for (int i = 0; i < PIECES; i++)
+#pragma unroll
+            for (int k = 0; k < W; k++) acc[i][k] += sums[0][i * W + k][lane] + sums[1][i * W + k][lane] + sums[2][i * W + k][lane];
+        write_row<TO, W, PIECES, false>(static_cast<TO *>(a.out) + (size_t)row_of_place(a, p) * a.cols, sp, acc, a.scale, a.accumulate);
     }
 }
 
@@ -664,20 +580,22 @@ EmbedPlan embed_plan(const sol_embedding_desc &d) {
     return p;
 }
 
-template <typename T, typename TO, int PIECES> void launch_wide(const GatherArgs &g, hipStream_t st) {
-    constexpr int W = sizeof(TO) == 4 ? 4 : 8;      // 16 bytes of the table's gradient
+template <typename T, typename TO, int PIECES> void launch_sums_of_rows(const GatherArgs &g, hipStream_t st) {
+    constexpr int W = 16 / sizeof(TO);
     const int items = g.vocab + 2 * g.windows;
-    const dim3 grid((unsigned)ceil_div(g.cols, PIECES * 512), (unsigned)min(ceil_div(items, 4), 65535));
-    if ((size_t)g.vocab * g.cols * sizeof(TO) >= STREAM_BYTES) hipLaunchKernelGGL((embed_wide_kernel<T, TO, W, PIECES * 8 / W, true>), grid, dim3(256), 0, st, g, items);
-    else hipLaunchKernelGGL((embed_wide_kernel<T, TO, W, PIECES * 8 / W, false>), grid, dim3(256), 0, st, g, items);
+    const dim3 grid((unsigned)ceil_div(g.cols, PIECES * 64 * W), (unsigned)min(ceil_div(items, 4), 65535));
+    if ((size_t)g.vocab * g.cols * sizeof(TO) >= STREAM_BYTES) hipLaunchKernelGGL((embed_sum_kernel<T, TO, W, PIECES, true>), grid, dim3(256), 0, st, g, items);
+    else hipLaunchKernelGGL((embed_sum_kernel<T, TO, W, PIECES, false>), grid, dim3(256), 0, st, g, items);
 }
+// 1024 columns a wave where there are as many: see embed_sum_kernel
 template <typename T, typename TO> sol_status launch_gather(const GatherArgs &g, hipStream_t st) {
-    const int per = 256 >> g.lanes_log2;
-    if (g.lanes_log2 < 6) hipLaunchKernelGGL((embed_gather_kernel<T, TO>), dim3((unsigned)ceil_div(g.vocab + 2 * g.windows, per)), dim3(256), 0, st, g);
-    else if (g.cols <= 512) launch_wide<T, TO, 1>(g, st);
-    else launch_wide<T, TO, 2>(g, st);
+    constexpr int W = 16 / sizeof(TO), PIECES = 16 / W;
+    const int pieces = ceil_div(g.cols, 64 * W);
+    if (pieces == 1) launch_sums_of_rows<T, TO, 1>(g, st);
+    else if (pieces == 2 || PIECES == 2) launch_sums_of_rows<T, TO, 2>(g, st);
+    else launch_sums_of_rows<T, TO, PIECES>(g, st);
     SOL_HIP(hipGetLastError());
-    hipLaunchKernelGGL((embed_join_kernel<T, TO>), dim3((unsigned)row_slabs(g.cols), (unsigned)min(g.windows, 65535)), dim3(256), 0, st, g);
+    hipLaunchKernelGGL((embed_join_kernel<TO, W, PIECES / 2>), dim3((unsigned)ceil_div(g.cols, 512), (unsigned)min(g.windows, 65535)), dim3(256), 0, st, g);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
@@ -737,7 +655,7 @@ sol_status sol_embedding_backward(const sol_embedding_desc *ed, const void *toke
         else hipLaunchKernelGGL((embed_index_kernel<int32_t, false>), grid, dim3(INDEX_THREADS), 0, st, x);
     }
     SOL_HIP(hipGetLastError());
-    const GatherArgs g{dy, dtable, start, order, sorted, reinterpret_cast<float *>(ws + p.part), d.ldy, d.vocab, d.cols, p.windows, accumulate ? 1 : 0, row_lanes_log2(d.cols, 8),
+    const GatherArgs g{dy, dtable, start, order, sorted, reinterpret_cast<float *>(ws + p.part), d.ldy, d.vocab, d.cols, p.windows, accumulate ? 1 : 0,
                  p.rows, p.log2, p.places, d.scale, FastDiv((uint32_t)p.rows)};
     if (d.dtype == SOL_F32) return launch_gather<float, float>(g, st);
     return dtable_dtype == SOL_F32 ? launch_gather<bf16_t, float>(g, st) : launch_gather<bf16_t, bf16_t>(g, st);

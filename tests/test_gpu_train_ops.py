@@ -890,3 +890,23 @@ def test_narrow_rows(sol, dt, cols):
         h = np.abs(whole - m[:, None]) * r[:, None]
         c1, c2 = np.abs(dy.mean(1, keepdims=True)), np.abs((dy * (whole - m[:, None]) * r[:, None]).mean(1, keepdims=True))
         close(host(dx), wx, r[:, None] * 4 * U * (np.abs(dy) + c1 + 2 * h * c2) + 2 * U * (np.abs(res) + np.abs(wx)) + HALF[dt] * np.abs(wx) * 1.02, "dx")
+
+
+@pytest.mark.parametrize("n", [7, 3000, 70000])
+def test_padding_alone(sol, n):
+    """A batch without a single token: zeros, and a table that is added to keeps its bits."""
+    tokens = torch.full((n,), -1, device=DEV)
+    dy = torch.full((n, 40), float("nan"), device=DEV)
+    table = torch.randn((500, 40), device=DEV)
+    assert not sol.sol_embedding(tokens, table).any() and not sol.sol_embedding_backward(dy, tokens, 500).any()
+    before = table.clone()
+    assert torch.equal(sol.sol_embedding_backward(dy, tokens, 500, add_to=table), before)
+
+
+def test_tokens_of_any_shape(sol):
+    gen = torch.Generator(device=DEV).manual_seed(1)
+    for shape in ((3, 400), (2, 5, 7), ()):
+        tokens = torch.randint(0, 90, shape, generator=gen, device=DEV)
+        table, dy = torch.randn((90, 24), generator=gen, device=DEV), torch.randint(-2, 3, (*shape, 24), generator=gen, device=DEV).float()
+        assert torch.equal(sol.sol_embedding(tokens, table), table[tokens])
+        assert torch.equal(sol.sol_embedding_backward(dy, tokens, 90), torch.zeros((90, 24), device=DEV).index_add_(0, tokens.reshape(-1), dy.reshape(-1, 24)))
