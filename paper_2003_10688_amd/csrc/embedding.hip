@@ -57,7 +57,8 @@ template <typename T, typename I, bool STREAM> __global__ void __launch_bounds__
 // The tokens' order is that of (v mod G, v / G) for G workgroups: each owns the rows of one residue, so that neighbouring rows, which frequent tokens often are, fall to different
 // ones, and reads all tokens.  It counts those of each of its rows and those of the residues in front, keeps what is its own in a list, in order, and writes the positions
 // of its rows' tokens behind each other.  So it takes one launch, without a word between the workgroups.  The tokens are read from L2, a second time where the list does not hold
-// a workgroup's share.
+// a workgroup's share.  65536 tokens of text 22 us (358 with neighbouring rows in one workgroup, which then has half of all tokens), 4096 9 us; every 16384 more take 4 us,
+// 3 where tokens are spread evenly.
 constexpr int INDEX_THREADS = 1024, INDEX_EACH = 16, INDEX_TILE = INDEX_THREADS * INDEX_EACH, INDEX_ROWS = 1024, INDEX_GROUPS = 256, INDEX_WAVES = INDEX_THREADS / 64;
 constexpr int LIST_BITS = 22;   // of a position in a list's entry, the row's 10 above them
 constexpr int RUN = 64;         // longer runs of one token are summed in parts of the sorted order, RUN positions each
@@ -182,9 +183,11 @@ __device__ __forceinline__ lanes_t same_row(uint32_t row, bool has, int bits) {
     }
     return same;
 }
-// Each wave takes a part of the list, 64 entries at a time, in order
+// Each wave takes a part of the list, 64 entries at a time, in order; short lists have parts for a few waves only
+__device__ __forceinline__ int part_length(int total) { return (total + INDEX_THREADS - 1) / INDEX_THREADS * 64; }
+__device__ __forceinline__ int parts_of(int total) { return total ? (total + part_length(total) - 1) / part_length(total) : 0; }
 template <typename F> __device__ __forceinline__ void index_part(const IndexShared &s, int total, int bits, F f) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, per = (total + INDEX_THREADS - 1) / INDEX_THREADS * 64, end = min(total, (w + 1) * per);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, per = part_length(total), end = min(total, (w + 1) * per);
     for (int i = w * per; i < end; i += 64) {
         const bool has = i + lane < end;
         const uint32_t e = has ? s.list[i + lane] : 0u;
@@ -193,8 +196,9 @@ template <typename F> __device__ __forceinline__ void index_part(const IndexShar
 }
 // count[w][r]: how many entries of row r wave w's part has.  Ends with a barrier.
 __device__ __forceinline__ void index_count(const IndexArgs &a, IndexShared &s, int total, int bits) {
+    const int parts = parts_of(total);
     if ((int)threadIdx.x < a.rows)
-        for (int w = 0; w < INDEX_WAVES; w++) s.count[w][threadIdx.x] = 0;
+        for (int w = 0; w < parts; w++) s.count[w][threadIdx.x] = 0;
     __syncthreads();
     index_part(s, total, bits, [&](int w, uint32_t e, bool has, lanes_t same) {
         if (has && (int)__ffsll(same) - 1 == (int)(threadIdx.x & 63)) s.count[w][e >> LIST_BITS] += (uint32_t)__popcll(same);
@@ -203,10 +207,10 @@ __device__ __forceinline__ void index_count(const IndexArgs &a, IndexShared &s, 
 }
 // Writes the positions of the list, whose counts are there, from next[] on, which moves behind them
 __device__ __forceinline__ void index_place(const IndexArgs &a, IndexShared &s, int total, int bits, int base) {
-    const int r = threadIdx.x;
+    const int r = threadIdx.x, parts = parts_of(total);
     if (r < a.rows) {
         uint32_t at = s.next[r];
-        for (int w = 0; w < INDEX_WAVES; w++) {
+        for (int w = 0; w < parts; w++) {
             const uint32_t k = s.count[w][r];
             s.count[w][r] = at;
             at += k;
@@ -236,8 +240,9 @@ template <typename I, bool PAD> __global__ void __launch_bounds__(INDEX_THREADS)
     bool whole = a.n <= 1 << LIST_BITS;                 // the list has all of this residue, positions from the first token on
     auto add_counts = [&]() {
         index_count(a, s, have, bits);
+        const int parts = parts_of(have);
         if (r < a.rows)
-            for (int w = 0; w < INDEX_WAVES; w++) s.next[r] += s.count[w][r];
+            for (int w = 0; w < parts; w++) s.next[r] += s.count[w][r];
     };
     for (int base = 0; base < a.n; base += INDEX_TILE) {
         less += look_at_tokens<I, PAD>(a, base, t, where);
@@ -338,7 +343,9 @@ __device__ __forceinline__ void write_row(TO *out, const Spans<W, PIECES> &sp, f
     }
 }
 
-// A wave takes PIECES * 64 * W columns of a row.  Three round trips to memory: where its run is, the positions in it (a lane each), and FLIGHT of the gradient's rows at a time.
+// A wave takes PIECES * 64 * W columns of a row, up to 1024.  Three round trips to memory: where its run is, the positions in it (a lane each), and FLIGHT of the gradient's rows at a time.
+// Bound by memory where it is large: 65536 tokens of text, table 65536 x 2048, bf16 to fp32 125 us (6.3 TB/s, a part of the gradient from the last cache; 165 to 190 with results that go through
+// the caches).  A row to a wave: the rows of frequent tokens are neighbours, and two rows a wave took 274 us in place of 224 for the whole gradient.
 template <typename T, typename TO, int W, int PIECES, bool STREAM> __device__ __forceinline__ void sum_item(const GatherArgs &a, int item, int c0) {
     constexpr int FLIGHT = 64 / (W * PIECES);
     const int lane = threadIdx.x & 63;
@@ -371,7 +378,8 @@ template <typename T, typename TO, int W, int PIECES, bool STREAM> __device__ __
     }
     write_row<TO, W, PIECES, STREAM>(static_cast<TO *>(a.out) + (size_t)(item - 2 * a.windows) * a.cols, sp, acc, a.scale, a.accumulate);
 }
-// Slabs of columns vary fastest: workgroups that run together then write whole rows, not the same part of every row, whose addresses would fall on a few of the memory's channels.
+// Slabs of columns vary fastest: workgroups that run together then write whole rows, not the same part of every row, whose addresses would fall on a few of the memory's channels
+// (326 us in place of 258 then; rows in the order of their places, 2 MB apart, 938).
 template <typename T, typename TO, int W, int PIECES, bool STREAM> __global__ void __launch_bounds__(256) embed_sum_kernel(const GatherArgs a, int items) {
     const int c0 = (int)blockIdx.x * (PIECES * 64 * W) + (threadIdx.x & 63) * W;
     for (int item = (int)blockIdx.y * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items; item += (int)gridDim.y * 4) sum_item<T, TO, W, PIECES, STREAM>(a, item, c0);
@@ -419,7 +427,7 @@ template <typename TO, int W, int PIECES> __global__ void __launch_bounds__(256)
 
 // ---- the gradient of few tokens, in one launch ----------------------------------------------------------------------------------
 // A workgroup looks at all tokens, lists those of its `block` rows in order, and sums and writes its rows, a wave each.  One row's tokens are added one behind the other, so
-// there can only be few; the rows without tokens, nearly all of them, are what the time goes into.
+// there can only be few; the rows without tokens, nearly all of them, are what the time goes into.  509 tokens, table 10007 x 201 fp32: 9 us, 20 in three launches; 512 equal tokens 18 and 36.
 constexpr int DIRECT = 512, CROWD = 32;
 struct DirectArgs {
     const void *tokens, *dy;

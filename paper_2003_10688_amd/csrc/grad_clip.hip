@@ -57,7 +57,8 @@ template <typename T> __device__ __forceinline__ void load_chunk(const T *g, Raw
     for (int k = 0; k < PIECES<T>; k++) r[k].load(g + (k * 256 + threadIdx.x) * WIDTH<T>, WIDTH<T>);
 }
 
-// A product of two fp32 values is exact in 64 bits: 2^28 bf16 elements in 62 us (8.7 TB/s from the last cache and memory), as fast as with fp32 sums.
+// A product of two fp32 values is exact in 64 bits, and sums of them neither overflow nor lose small terms.  It costs nothing beside the memory: 2^28 bf16 elements 112 us (4.8 TB/s), 110 with fp32
+// sums; 2^26 fp32 elements 44 us (6.1 TB/s) either way.
 template <typename T> __device__ __forceinline__ double squares(const T *g, int len) {
     double s = 0.0;
     if (len == CHUNK) {
@@ -134,7 +135,8 @@ template <bool STREAM, typename T> __device__ __forceinline__ void scaled(const 
 }
 
 // Every workgroup joins the parts itself, which takes a launch less, and the first leaves the norm (each launch's first, the same one); parts = 0: the norm is there.  Where nothing is clipped the elements are copied as they are, or left where they are in place.
-// The chunks are taken from the last on: what the pass in front read last is still in the caches.
+// The chunks are taken from the last on: what the pass in front read last is still in the caches, and stays there where the results are written past them (STREAM): 2^28 bf16 elements
+// 300 us, both passes together, 333 with ordinary stores; 2^26 fp32 elements 123 and 147.  The 102 MB of a ResNet-50-shaped network's gradients 57 us.
 template <bool STREAM> __global__ void __launch_bounds__(256) grad_scale_kernel(const GradTable t, const double *part, int parts, float *norm, float max_norm) {
     __shared__ double red[4];
     const float n = parts ? (float)sqrt(sum_of_parts(part, parts, red)) : *norm;
