@@ -194,9 +194,10 @@ int total_parts(const sol_grad *grads, int tensors) {
     return parts;
 }
 
-struct Buffer { uintptr_t at, end; int i; };
+struct Buffer { uintptr_t at, end; int i; };      // i = -1: the norm
 
-sol_status check_grads(const sol_grad *grads, int tensors, bool out) {
+// out: the results and the norm are looked at too
+sol_status check_grads(const sol_grad *grads, int tensors, bool out, const float *norm = nullptr) {
     SOL_REQUIRE(tensors >= 0, SOL_ERR_SHAPE, "%d tensors", tensors);
     SOL_REQUIRE(grads || tensors == 0, SOL_ERR_NULL, "the list of gradients is NULL");
     SOL_REQUIRE(tensors <= MAX_TENSORS, SOL_ERR_UNSUPPORTED, "more than 2^15 tensors: %d", tensors);
@@ -211,10 +212,11 @@ sol_status check_grads(const sol_grad *grads, int tensors, bool out) {
         SOL_REQUIRE(!(reinterpret_cast<uintptr_t>(g.grad) & mask) && (!out || !(reinterpret_cast<uintptr_t>(g.out) & mask)), SOL_ERR_ALIGN, "gradient %d is not aligned to its elements", i);
     }
     if (!out || tensors == 0) return SOL_OK;
-    // No two of the buffers may share memory: a tensor listed twice would be scaled twice, an output on another gradient would change it before it is read.
-    Buffer few[512], *spans = 2 * tensors <= 512 ? few : static_cast<Buffer *>(malloc(2 * (size_t)tensors * sizeof(Buffer)));
+    // No two of the buffers may share memory: a tensor listed twice would be scaled twice, an output on another gradient would change it before it is read, and so would the norm.
+    Buffer few[513], *spans = 2 * tensors <= 512 ? few : static_cast<Buffer *>(malloc((2 * (size_t)tensors + 1) * sizeof(Buffer)));
     SOL_REQUIRE(spans, SOL_ERR_UNSUPPORTED, "no memory for a list of %d gradients", tensors);
     int n = 0;
+    if (norm) spans[n++] = Buffer{reinterpret_cast<uintptr_t>(norm), reinterpret_cast<uintptr_t>(norm + 1), -1};
     for (int i = 0; i < tensors; i++) {
         const sol_grad &g = grads[i];
         const uintptr_t bytes = g.count * dtype_size(g.dtype), at = reinterpret_cast<uintptr_t>(g.grad), to = reinterpret_cast<uintptr_t>(g.out);
@@ -222,11 +224,13 @@ sol_status check_grads(const sol_grad *grads, int tensors, bool out) {
         if (bytes && at != to) spans[n++] = Buffer{to, to + bytes, i};
     }
     std::sort(spans, spans + n, [](const Buffer &p, const Buffer &q) { return p.at < q.at; });       // in place, without memory of its own
-    int a = -1, b = -1;
-    for (int k = 1; k < n && a < 0; k++)
-        if (spans[k].at < spans[k - 1].end) { a = spans[k - 1].i; b = spans[k].i; }
+    int a = 0, b = 0;
+    bool shared = false;
+    for (int k = 1; k < n && !shared; k++)
+        if (spans[k].at < spans[k - 1].end) { a = spans[k - 1].i; b = spans[k].i; shared = true; }
     if (spans != few) free(spans);
-    SOL_REQUIRE(a < 0, SOL_ERR_UNSUPPORTED, "gradients %d and %d, or what is written for them, share memory", a, b);
+    SOL_REQUIRE(!shared || (a >= 0 && b >= 0), SOL_ERR_UNSUPPORTED, "the norm and gradient %d, or what is written for it, share memory", max(a, b));
+    SOL_REQUIRE(!shared, SOL_ERR_UNSUPPORTED, "gradients %d and %d, or what is written for them, share memory", a, b);
     return SOL_OK;
 }
 
@@ -275,8 +279,8 @@ sol_status sol_grad_norm(const sol_grad *grads, int tensors, float *norm, void *
 }
 
 sol_status sol_grad_clip(const sol_grad *grads, int tensors, float max_norm, float *norm, void *workspace, size_t workspace_bytes, void *stream) {
-    SOL_TRY(check_grads(grads, tensors, true));
     SOL_TRY(check_norm_out(norm));
+    SOL_TRY(check_grads(grads, tensors, true, norm));
     SOL_REQUIRE(max_norm > 0.f, SOL_ERR_SHAPE, "max_norm %g is not positive", (double)max_norm);       // refuses a NaN too
     const int parts = total_parts(grads, tensors);
     SOL_TRY(check_scratch(workspace, workspace_bytes, (size_t)parts * 8));

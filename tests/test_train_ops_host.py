@@ -163,6 +163,21 @@ def test_grad_refusals(sol):
     assert L.sol_grad_workspace_bytes(grads(sol, (0x1000, 0, 5, 9)), 1) == 0
 
 
+def test_clip_refuses_a_norm_inside_the_gradients(sol):
+    """The norm is written while gradients are scaled: it may not be a part of one, nor of what is written for it.  Behind the last element and in front of the first there is room."""
+    L = sol.lib()
+    clip = lambda arr, norm: L.sol_grad_clip(arr, len(arr), 1.0, norm, NULL, 0, NULL)  # noqa: E731  no workspace: 5 where everything else is right
+    for many in (1, 300):
+        arr = grads(sol, *[(0x10000 + 0x100 * i, 0x80000 + 0x100 * i, 4, 0) for i in range(many)])
+        last = 0x100 * (many - 1)
+        for at in (0x10000, 0x1000c, 0x80000, 0x8000c, 0x10000 + last, 0x8000c + last):
+            assert clip(arr, at) == 6, hex(at)
+        for at in (0xfffc, 0x10010, 0x7fffc, 0x80010, 0x10010 + last, 0x80010 + last):
+            assert clip(arr, at) == 5, hex(at)
+    half = grads(sol, (0x10002, 0x10002, 3, 1))         # bf16: the norm's 4 bytes reach over its first element, or begin on its last
+    assert clip(half, 0x10000) == 6 and clip(half, 0x10004) == 6 and clip(half, 0x10008) == 5
+
+
 def test_binding_refuses_what_is_not_on_the_gpu(sol):
     import torch
 
