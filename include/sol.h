@@ -265,8 +265,8 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
  *             y = (x - mean) * rstd * gamma + beta
  *   backward  h = (x - mean) * rstd,  g = dy * gamma
  *             dx = rstd * (g - mean(g) - h * mean(g * h)) + residual      dgamma = sum over the rows of dy * h     dbeta = sum over the rows of dy
- * Every sum, mean and rstd are fp32 for both dtypes.  An infinity or a NaN in a row makes that row of y, and of dx, NaN, and no other.  A row whose squared deviations
- * add up to more than fp32 holds has rstd 0. */
+ * Every sum, mean and rstd are fp32 for both dtypes.  An infinity or a NaN in a row, or a sum of its elements that fp32 does not hold, makes that row of y, and of dx,
+ * NaN, and no other.  A row whose squared deviations add up to more than fp32 holds has rstd 0. */
 typedef struct {
     int rows, cols;             /* at most 2^20 columns */
     int dtype;                  /* sol_dtype of x, y, dy, residual and dx */

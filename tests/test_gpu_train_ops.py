@@ -162,6 +162,24 @@ def test_rows_that_are_not_finite(sol, dt, rows, cols):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(9, 40), (9, 900), (9, 2048), (9, 4001), (9, 20000), (300, 2048)])
+def test_rows_whose_sums_do_not_fit(sol, dt, rows, cols):
+    """Finite rows: a sum above 2^128 makes its row NaN; deviations whose squares add up to more than that, about a mean that fits, make rstd 0, so y = beta to the last bit and dx = 0.
+    No other row takes notice."""
+    x, gamma, beta, dy, _ = norm_inputs(rows, cols, dt)
+    x[2], x[4] = 2.0**127, 2.0**100 * (1 - 2 * (np.arange(cols) % 2))
+    y, mean, rstd = sol.sol_layer_norm(dev(x, dt), dev(gamma), dev(beta), want_stats=True)
+    fine = np.delete(np.arange(rows), [2, 4])
+    assert np.all(np.isnan(host(y)[2])) and np.isnan(host(rstd)[2]) and np.isfinite(host(mean)[4]) and host(rstd)[4] == 0
+    assert np.array_equal(host(y)[4], host(dev(beta, dt)))
+    x[[2, 4]] = 0
+    assert np.array_equal(host(y)[fine], host(sol.sol_layer_norm(dev(x, dt), dev(gamma), dev(beta))[0])[fine])
+    x[2], x[4] = 2.0**127, 2.0**100 * (1 - 2 * (np.arange(cols) % 2))
+    dx = sol.sol_layer_norm_backward(dev(dy, dt), dev(x, dt), mean, rstd, dev(gamma), need_dgamma=False, need_dbeta=False)[0]
+    assert np.all(np.isnan(host(dx)[2])) and np.all(host(dx)[4] == 0) and np.all(np.isfinite(host(dx)[fine]))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,cols", [(1, 5), (37, 100), (37, 1030), (37, 3000), (37, 8192), (5, 17000), (500, 2048)])
 def test_what_lies_between_rows_and_in_place(sol, dt, rows, cols):
     """Gaps of NaN beside x and dy do not reach a result, gaps of the outputs stay as they were; y may take x's place, dx the residual's."""
