@@ -230,6 +230,10 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_columns_kerne
     column_sums<32, 32, T>(a, (int)blockIdx.x, red);
 }
 
+// x - mean, and 0 in places that hold no element of the row: (0 - mean) * rstd may be more than fp32 holds where the row's own h are not, and 0 * inf would make the row's sums NaN
+template <bool WHOLE, int W> __device__ __forceinline__ float deviation(const Span<W> &sp, int e, float x, float mean) {
+    return x - ((WHOLE ? sp.some() : sp.holds(e)) ? mean : 0.f);
+}
 // The row's part of the backward pass, from g = dy gamma and h: gamma, and so g, is 0 in places that are not the thread's own
 template <int P, int W> __device__ __forceinline__ void row_products(const float (&g)[P][W], const float (&h)[P][W], float &s1, float &s2) {
     s1 = s2 = 0.f;
@@ -272,7 +276,7 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_dx_kernel(const NormArgs 
             sp[k].template load<WHOLE>(dy, ry);
 #pragma unroll
             for (int e = 0; e < W; e++) {
-                h[k][e] = (rx.get(e) - mean) * rstd;
+                h[k][e] = deviation<WHOLE>(sp[k], e, rx.get(e), mean) * rstd;
                 g[k][e] = ry.get(e) * gm[k][e];
             }
         }
@@ -347,7 +351,7 @@ __global__ void __launch_bounds__(GRAD_BLOCK<WHOLE>) norm_grad_kernel(const Norm
             for (int k = 0; k < P; k++)
 #pragma unroll
                 for (int e = 0; e < W; e++) {
-                    h[k][e] = (xr[k].get(e) - mean) * rstd;
+                    h[k][e] = deviation<WHOLE>(sp[k], e, xr[k].get(e), mean) * rstd;
                     const float d = yr[k].get(e);
                     sb[k][e] += d;
                     sg[k][e] += d * h[k][e];

@@ -122,6 +122,7 @@ template <int W> struct Span {
     }
     __device__ __forceinline__ bool some() const { return skip < W; }
     __device__ __forceinline__ bool has(int e) const { return e >= skip && e < end; }
+    __device__ __forceinline__ bool holds(int e) const { return some() && e < end; }       // load() has put the row's element there, the thread's own or the one's in front
     // WHOLE: the row's length is a multiple of W
     template <bool WHOLE, typename T> __device__ __forceinline__ void load(const T *row, RawPiece<T, W> &r) const {
         if (!some()) return;

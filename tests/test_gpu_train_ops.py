@@ -180,6 +180,34 @@ def test_rows_whose_sums_do_not_fit(sol, dt, rows, cols):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [4, 1100])
+@pytest.mark.parametrize("cols", [1, 3, 7, 8, 24, 40, 64, 77, 200, 520, 1001, 2048, 2500, 4001, 8184, 9000, 16392])
+def test_backward_of_equal_elements_far_from_zero(sol, dt, rows, cols):
+    """Rows of equal elements whose mean times rstd is more than fp32 holds: h is 0 in all of them, whether a row fills its threads or leaves some without columns, so dx = rstd (g - mean(g)) + residual."""
+    x, gamma, _, dy, res = norm_inputs(rows, cols, dt)
+    for value, eps in ((2.0**66, 2.0**-126), (2.0**120, 1e-5)):
+        if value * cols >= 2.0**127:                              # the row's sum has to fit
+            continue
+        x[1], x[rows - 1] = value, -value
+        xd = dev(x, dt)
+        _, mean, rstd = sol.sol_layer_norm(xd, eps=eps, want_stats=True)
+        m, r = host(mean), host(rstd)
+        assert m[1] == value and m[rows - 1] == -value and value * r[1] >= 2.0**128
+        n = 8 * (cols // 8192 + 2) + 48                           # additions behind each other, as in test_layer_norm_backward
+        for gm, q, columns in ((gamma, res, True), (None, None, True), (gamma, None, False)):
+            dx, dg, db = sol.sol_layer_norm_backward(dev(dy, dt), xd, mean, rstd, None if gm is None else dev(gm), residual=None if q is None else dev(q, dt), need_dgamma=columns, need_dbeta=columns)
+            wx, wg, wb = to.layer_norm_bwd(dy, x, m, r, gm, q)
+            h = np.abs(x - m[:, None]) * r[:, None]
+            g = np.abs(dy) * (1 if gm is None else np.abs(gm.astype(np.float64)))
+            c1, c2 = g.mean(1, keepdims=True), (g * h).mean(1, keepdims=True)
+            inner = 5 * U * (g + c1 + h * c2) + (n + 4) * U * c1 + h * (n + 8) * U * c2
+            close(host(dx), wx, r[:, None] * inner * 1.01 + U * (0 if q is None else np.abs(q) + np.abs(wx)) + HALF[dt] * np.abs(wx) * 1.02, "dx")
+            if columns:
+                close(host(dg), wg, (rows + 48) * U * (np.abs(dy) * h).sum(0), "dgamma")
+                close(host(db), wb, (rows + 48) * U * np.abs(dy).sum(0), "dbeta")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,cols", [(1, 5), (37, 100), (37, 1030), (37, 3000), (37, 8192), (5, 17000), (500, 2048)])
 def test_what_lies_between_rows_and_in_place(sol, dt, rows, cols):
     """Gaps of NaN beside x and dy do not reach a result, gaps of the outputs stay as they were; y may take x's place, dx the residual's."""
