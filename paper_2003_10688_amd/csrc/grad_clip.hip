@@ -110,7 +110,19 @@ __global__ void __launch_bounds__(256) grad_norm_kernel(const double *part, int 
     if (threadIdx.x == 0) *norm = (float)sqrt(s);
 }
 
-template <bool STREAM, typename T> __device__ __forceinline__ void scaled(const T *g, T *out, int len, float f) {
+// max_norm / norm as the product of two factors.  Where fp32 holds the quotient with all its digits the second is 1, and so without effect; where the quotient lies below 2^-126 (an exploded norm of
+// 1e38 and a max_norm of 1e-3, whose results fp32 holds all the same), the first is the power of two that brings the norm into 2 .. 4, which rounds nothing, and the second max_norm over that.
+struct Factor { float first, then; };
+__device__ __forceinline__ Factor clip_factor(float max_norm, float norm) {
+    const float q = max_norm / norm;
+    if (q >= FLT_MIN) return {q, 1.f};
+    int k;
+    frexpf(norm, &k);
+    const float first = ldexpf(1.f, 2 - k);
+    return {first, max_norm / (norm * first)};
+}
+
+template <bool STREAM, typename T> __device__ __forceinline__ void scaled(const T *g, T *out, int len, Factor f) {
     if (len == CHUNK) {
         RawPiece<T, WIDTH<T>> r[PIECES<T>];
         load_chunk<T>(g, r);
@@ -118,7 +130,7 @@ template <bool STREAM, typename T> __device__ __forceinline__ void scaled(const 
         for (int k = 0; k < PIECES<T>; k++) {
             float v[WIDTH<T>];
 #pragma unroll
-            for (int e = 0; e < WIDTH<T>; e++) v[e] = r[k].get(e) * f;
+            for (int e = 0; e < WIDTH<T>; e++) v[e] = r[k].get(e) * f.first * f.then;
             if constexpr (STREAM) stream_piece<T, WIDTH<T>>(out + (k * 256 + threadIdx.x) * WIDTH<T>, v);
             else store_piece<T, WIDTH<T>>(out + (k * 256 + threadIdx.x) * WIDTH<T>, v, WIDTH<T>);
         }
@@ -128,7 +140,7 @@ template <bool STREAM, typename T> __device__ __forceinline__ void scaled(const 
             r.load(g + i, len - i);
             float v[WIDTH<T>];
 #pragma unroll
-            for (int e = 0; e < WIDTH<T>; e++) v[e] = r.get(e) * f;
+            for (int e = 0; e < WIDTH<T>; e++) v[e] = r.get(e) * f.first * f.then;
             store_piece<T, WIDTH<T>>(out + i, v, len - i);
         }
     }
@@ -142,7 +154,7 @@ template <bool STREAM> __global__ void __launch_bounds__(256) grad_scale_kernel(
     const float n = parts ? (float)sqrt(sum_of_parts(part, parts, red)) : *norm;
     if (parts && blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
     const bool clip = n > max_norm && n <= FLT_MAX;
-    const float f = clip ? max_norm / n : 1.f;
+    const Factor f = clip ? clip_factor(max_norm, n) : Factor{1.f, 1.f};
     for (uint32_t j = blockIdx.x; j < t.first[t.n]; j += gridDim.x) {
         const Chunk c = find_chunk(t, t.first[t.n] - 1 - j);
         if (!clip && t.grad[c.tensor] == t.out[c.tensor]) continue;

@@ -427,6 +427,25 @@ def test_clip_of_very_large_and_very_small_values(sol):
     assert float(sol.sol_grad_clip([z], 1.0)) == 0 and not z.any()
 
 
+@pytest.mark.parametrize("dts", [("f32",), ("bf16",), ("bf16", "f32")])
+def test_clip_to_a_factor_below_the_normal_range(sol, dts):
+    """max_norm / norm below 2^-126, where fp32 has few digits or none: the results, which fp32 does hold, are as exact as ever."""
+    rng = np.random.default_rng(12)
+    for top, limit in ((2.0**118, 1e-5), (2.0**118, 1e-20), (2.0**110, 2.5), (2.0**60, 1e-30), (2.0**-3, 2.0**-120), (2.0**120, 3e-39)):
+        ts = [(dev(grid(rng.uniform(0.5, 1.0, n) * top, dts[i % len(dts)]), dts[i % len(dts)]), dts[i % len(dts)]) for i, n in enumerate((9000, 1, 77, 8192, 3))]
+        norm, factor, want = to.grad_clip([host(t) for t, _ in ts], limit)
+        out = [torch.full_like(t, 7) for t, _ in ts]
+        got = float(sol.sol_grad_clip([t for t, _ in ts], limit, out=out))
+        assert abs(got - norm) <= 1.01 * U * norm and norm < 2.0**128
+        place = [t.clone() for t, _ in ts]
+        sol.sol_grad_clip(place, limit)
+        for o, p, w, (_, dt) in zip(out, place, want, ts):
+            # norm, quotient, product, and the rounding to the type, whose steps below its normal range are 2^-149 and 2^-133
+            tol = (4 * U + HALF[dt]) * 1.02 * np.abs(w) + (2.0**-148 if dt == "f32" else 2.0**-132)
+            close(host(o), w, tol, f"{top:g} {limit:g}")
+            assert torch.equal(o, p)
+
+
 def test_clip_network_gradients(sol, oracle_mod):
     """sol_network_clip_gradients is sol_grad_clip on every gradient of the network."""
     from paper_2003_10688_amd import workloads as wl
