@@ -702,6 +702,9 @@ class Network:
         _check(lib().sol_network_bind_params(self._h, _ptr(self.param_buf), C.c_size_t(self.param_buf.numel())))
         od = self.output_desc(-1)
         self.y = torch.empty((od.n, od.h, od.w, od.c), dtype=torch_dtype(dt), device=device)
+        if self.training:      # here and unfilled: made by the first call they would belong to the current stream, or to a graph that it is captured into, and be filled beside what the call's stream writes
+            self.grad_norm = torch.empty(4, dtype=torch.float32, device=device)
+            self.clip_space = torch.empty(max(lib().sol_network_clip_workspace_bytes(self._h), 16), dtype=torch.uint8, device=device)
 
     def output_desc(self, layer=-1):
         d = TensorDesc()
@@ -881,9 +884,8 @@ class Network:
 
     def clip_gradients(self, max_norm, stream=None):
         """sol_grad_clip on every gradient of the last backward; returns the device scalar holding their norm."""
-        if not hasattr(self, "grad_norm"):
-            self.grad_norm = torch.zeros(4, dtype=torch.float32, device=self.device)
-            self.clip_space = torch.empty(max(lib().sol_network_clip_workspace_bytes(self._h), 16), dtype=torch.uint8, device=self.device)
+        if not self.training:
+            raise SolError(6, "network was not created with SOL_NET_TRAINING")
         _check(lib().sol_network_clip_gradients(self._h, max_norm, _addr(self.grad_norm), _addr(self.clip_space), self.clip_space.numel(), _stream_handle(stream)))
         return self.grad_norm[:1]
 

@@ -198,3 +198,49 @@ def test_networks_clip_only_when_they_train(sol):
         assert (sol.lib().sol_network_clip_workspace_bytes(h) > 0) == bool(flags)
         sol.lib().sol_network_destroy(h)
     assert sol.lib().sol_network_clip_gradients(None, 1.0, 0x100, 0x200, 1 << 20, NULL) == 1 and sol.lib().sol_network_clip_workspace_bytes(None) == 0
+
+
+class Recorder:
+    """The library, but for the calls that would launch kernels: those are noted down with their arguments and return 0."""
+
+    def __init__(self, real, names):
+        self.real, self.names, self.calls = real, names, []
+
+    def __getattr__(self, name):
+        if name in self.names:
+            return lambda *args: self.calls.append((name, args)) or 0
+        return getattr(self.real, name)
+
+
+@pytest.fixture
+def host_network(sol, monkeypatch):
+    """A training network in host memory, whose device calls are noted down only, and which may make no tensor once it is there."""
+    import torch
+
+    rec = Recorder(sol.lib(), ("sol_network_clip_gradients", "sol_network_backward"))
+    monkeypatch.setattr(sol, "lib", lambda: rec)
+    monkeypatch.setattr(sol, "_addr", lambda t: 0 if t is None else t.data_ptr() if isinstance(t, torch.Tensor) else int(t))
+    net = sol.Network([{"kind": "linear", "out": 8}], (2, 8, 1, 1), sol.F32, device="cpu", flags=sol.NET_TRAINING)
+
+    def none(*args, **kw):
+        raise AssertionError("a tensor made by the call belongs to the current stream, not to the call's")
+
+    for name in ("zeros", "empty"):
+        monkeypatch.setattr(torch, name, none)
+    return net, rec
+
+
+class OtherStream:
+    cuda_stream = 0x77
+
+
+def test_network_clipping_makes_nothing_on_the_current_stream(sol, host_network):
+    """Its norm and its scratch, which the call's stream writes, are there before the first call."""
+    net, rec = host_network
+    norm = net.clip_gradients(0.5, stream=OtherStream)
+    (name, args), = rec.calls
+    assert name == "sol_network_clip_gradients" and args[1] == 0.5 and args[2] == norm.data_ptr() and args[5] == 0x77
+    need = rec.sol_network_clip_workspace_bytes(net._h)
+    assert need > 0 and args[4] >= need and args[3] == net.clip_space.data_ptr()
+    net.clip_gradients(0.25, stream=OtherStream)
+    assert rec.calls[1][1][2:] == args[2:]
