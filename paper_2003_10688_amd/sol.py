@@ -703,6 +703,7 @@ class Network:
         od = self.output_desc(-1)
         self.y = torch.empty((od.n, od.h, od.w, od.c), dtype=torch_dtype(dt), device=device)
         if self.training:      # here and unfilled: made by the first call they would belong to the current stream, or to a graph that it is captured into, and be filled beside what the call's stream writes
+            self.loss = torch.empty(4, dtype=torch.float32, device=device)
             self.grad_norm = torch.empty(4, dtype=torch.float32, device=device)
             self.clip_space = torch.empty(max(lib().sol_network_clip_workspace_bytes(self._h), 16), dtype=torch.uint8, device=device)
 
@@ -876,8 +877,8 @@ class Network:
     def backward(self, x, labels, stream=None):
         """Loss + full backward on what the last forward left; labels: int32 device tensor [n].
         Returns the device scalar holding the mean cross-entropy."""
-        if not hasattr(self, "loss"):
-            self.loss = torch.zeros(4, dtype=torch.float32, device=self.device)
+        if not self.training:
+            raise SolError(6, "network was not created with SOL_NET_TRAINING")
         _check(lib().sol_network_backward(self._h, _addr(x), _addr(labels), _addr(self.loss), _addr(self.workspace), self.workspace.numel(),
                                           _stream_handle(stream)))
         return self.loss[:1]

@@ -523,6 +523,46 @@ def test_first_clip_of_a_network_on_another_stream(sol, oracle_mod):
     del graph
 
 
+def test_first_backward_of_a_network_on_another_stream(sol, oracle_mod):
+    """The loss of a network's first backward pass, on a second stream while the current one is busy, and captured."""
+    from paper_2003_10688_amd import workloads as wl
+
+    wk = wl.config(1, batch=4)
+    layers = [dict(l, pool=None) if l["kind"] == "conv" else l for l in wk.layers]
+    x, labels = sol.to_device_nhwc(wk.x, sol.F32), torch.tensor([1, 0, 3, 2], dtype=torch.int32, device=DEV)
+    big = torch.randn((8192, 8192), device=DEV)
+
+    def network():
+        net = sol.Network(layers, wk.in_shape, sol.F32, flags=sol.NET_TRAINING)
+        net.set_params(wk.params)
+        net.forward(x)
+        torch.cuda.synchronize()
+        return net
+
+    net, side = network(), torch.cuda.Stream()
+    want = float(net.backward(x, labels))
+    grad = net.tensor(0, sol.NT_GRAD_W).clone()
+    assert want > 0
+    for _ in range(3):
+        net = network()
+        for _ in range(4):
+            big @ big
+        loss = net.backward(x, labels, stream=side)
+        torch.cuda.synchronize()
+        assert float(loss) == want and torch.equal(net.tensor(0, sol.NT_GRAD_W), grad)
+    net, graph = network(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        loss = net.backward(x, labels)
+    for _ in range(3):
+        net.loss.fill_(-1)
+        net.tensor(0, sol.NT_GRAD_W).zero_()
+        net.forward(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert float(loss) == want and torch.equal(net.tensor(0, sol.NT_GRAD_W), grad)
+    del graph
+
+
 # ---- streams, graphs, repeats ------------------------------------------------------------------------------------
 def everything(sol, d, **kw):
     y, mean, rstd = sol.sol_layer_norm(d["x"], d["gamma"], d["beta"], want_stats=True, stream=kw.get("stream"))

@@ -244,3 +244,14 @@ def test_network_clipping_makes_nothing_on_the_current_stream(sol, host_network)
     assert need > 0 and args[4] >= need and args[3] == net.clip_space.data_ptr()
     net.clip_gradients(0.25, stream=OtherStream)
     assert rec.calls[1][1][2:] == args[2:]
+
+
+def test_network_backward_makes_nothing_on_the_current_stream(sol, host_network):
+    """Likewise the loss."""
+    import ctypes
+
+    net, rec = host_network
+    x, labels = ctypes.addressof(ctypes.create_string_buffer(64)), 0x40
+    loss = net.backward(x, labels, stream=OtherStream)
+    (name, args), = rec.calls
+    assert name == "sol_network_backward" and args[1:4] == (x, labels, loss.data_ptr()) and args[-1] == 0x77 and loss.data_ptr() == net.loss.data_ptr()
