@@ -338,7 +338,8 @@ typedef struct {
 size_t sol_grad_workspace_bytes(const sol_grad *grads, int tensors);
 
 /* grads: host array of `tensors` entries, at most 2^15 with fewer than 2^40 elements in all, read during the call.  norm: device fp32.  Squares are summed in 64 bits, in an order that the counts fix.
- * No two entries of sol_grad_clip may share memory, but for an entry's out in place of its grad, nor may an entry and norm.  No tensors: norm 0. */
+ * No two entries of sol_grad_clip may share memory, but for an entry's out in place of its grad, nor may an entry and norm.
+ * The bytes of the workspace that are needed may share memory with neither an entry (of sol_grad_norm: its grad) nor norm.  No tensors: norm 0. */
 sol_status sol_grad_norm(const sol_grad *grads, int tensors, float *norm, void *workspace, size_t workspace_bytes, void *hip_stream);
 sol_status sol_grad_clip(const sol_grad *grads, int tensors, float max_norm, float *norm, void *workspace, size_t workspace_bytes,
                          void *hip_stream);

@@ -261,6 +261,18 @@ sol_status launch_squares(const sol_grad *grads, int tensors, double *part, hipS
     return SOL_OK;
 }
 
+// The sums that a call writes into its scratch may lie on no gradient, on no result and not on the norm, which others of its workgroups read or write meanwhile.
+sol_status check_parts(const sol_grad *grads, int tensors, bool out, const float *norm, const void *workspace, size_t bytes) {
+    const uintptr_t at = reinterpret_cast<uintptr_t>(workspace), end = at + bytes;
+    auto meets = [&](const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) < end && at < reinterpret_cast<uintptr_t>(p) + n; };
+    SOL_REQUIRE(bytes == 0 || !meets(norm, sizeof(*norm)), SOL_ERR_UNSUPPORTED, "the workspace and the norm share memory");
+    for (int i = 0; i < tensors && bytes; i++) {
+        const size_t n = grads[i].count * dtype_size(grads[i].dtype);
+        SOL_REQUIRE(n == 0 || (!meets(grads[i].grad, n) && (!out || !meets(grads[i].out, n))), SOL_ERR_UNSUPPORTED, "the workspace and gradient %d, or what is written for it, share memory", i);
+    }
+    return SOL_OK;
+}
+
 sol_status check_norm_out(const float *norm) {
     SOL_REQUIRE(norm, SOL_ERR_NULL, "norm must not be NULL");
     SOL_REQUIRE((reinterpret_cast<uintptr_t>(norm) & 3u) == 0, SOL_ERR_ALIGN, "norm must be 4-byte aligned");
@@ -283,6 +295,7 @@ sol_status sol_grad_norm(const sol_grad *grads, int tensors, float *norm, void *
     SOL_TRY(check_norm_out(norm));
     const int parts = total_parts(grads, tensors);
     SOL_TRY(check_scratch(workspace, workspace_bytes, (size_t)parts * 8));
+    SOL_TRY(check_parts(grads, tensors, false, norm, workspace, (size_t)parts * 8));
     hipStream_t st = (hipStream_t)stream;
     SOL_TRY(launch_squares(grads, tensors, static_cast<double *>(workspace), st));
     hipLaunchKernelGGL(grad_norm_kernel, dim3(1), dim3(256), 0, st, static_cast<const double *>(workspace), parts, norm);
@@ -296,6 +309,7 @@ sol_status sol_grad_clip(const sol_grad *grads, int tensors, float max_norm, flo
     SOL_REQUIRE(max_norm > 0.f, SOL_ERR_SHAPE, "max_norm %g is not positive", (double)max_norm);       // refuses a NaN too
     const int parts = total_parts(grads, tensors);
     SOL_TRY(check_scratch(workspace, workspace_bytes, (size_t)parts * 8));
+    SOL_TRY(check_parts(grads, tensors, true, norm, workspace, (size_t)parts * 8));
     hipStream_t st = (hipStream_t)stream;
     double *part = static_cast<double *>(workspace);
     SOL_TRY(launch_squares(grads, tensors, part, st));

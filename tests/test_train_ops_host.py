@@ -255,3 +255,23 @@ def test_network_backward_makes_nothing_on_the_current_stream(sol, host_network)
     loss = net.backward(x, labels, stream=OtherStream)
     (name, args), = rec.calls
     assert name == "sol_network_backward" and args[1:4] == (x, labels, loss.data_ptr()) and args[-1] == 0x77 and loss.data_ptr() == net.loss.data_ptr()
+
+
+def test_clip_refuses_a_workspace_inside_what_it_reads_or_writes(sol):
+    """The partial sums lie there while gradients are read and results and the norm written.  Only the bytes that are needed count; each call here is refused, so that nothing is launched."""
+    L = sol.lib()
+    for many in (1, 300):
+        arr = grads(sol, *[(0x100000 + 0x100 * i, 0x800000 + 0x100 * i, 4, 0) for i in range(many)])
+        need, last = L.sol_grad_workspace_bytes(arr, many), 0x100 * (many - 1)
+        assert need == 8 * many
+        for call in (lambda ws, norm, n=need: L.sol_grad_norm(arr, many, norm, ws, n, NULL), lambda ws, norm, n=need: L.sol_grad_clip(arr, many, 1.0, norm, ws, n, NULL)):
+            for ws in (0x100000, 0x100000 + last, 0x100000 - need + 16 & ~15):
+                assert call(ws, 0x40) == 6 and b"workspace" in L.sol_last_error(), hex(ws)
+            ws = 0x4000000
+            for norm in (ws, ws + need - 4):
+                assert call(ws, norm) == 6 and b"workspace" in L.sol_last_error()
+                assert call(ws, norm, 1 << 20) == 6
+        for ws in (0x800000, 0x800000 + last):                    # where clipping writes
+            assert L.sol_grad_clip(arr, many, 1.0, 0x40, ws, need, NULL) == 6 and b"workspace" in L.sol_last_error()
+    half = grads(sol, (0x10010, 0x20010, 3, 1))
+    assert L.sol_grad_norm(half, 1, 0x40, 0x10010, 8, NULL) == 6 and L.sol_grad_clip(half, 1, 1.0, 0x40, 0x20010, 8, NULL) == 6
