@@ -297,7 +297,7 @@ sol_status sol_layer_norm_backward(const sol_layer_norm_desc *nd, const void *dy
 
 /* Embedding, and the gradient of its table:
  *   forward   y[i] = scale * table[tokens[i]]            (the product is fp32, then rounded to dtype)
- *   backward  dtable[v] = scale * sum of the dy[i] with tokens[i] = v, in the order of i
+ *   backward  dtable[v] = scale * sum of the dy[i] with tokens[i] = v
  * A token equal to pad gives a row of zeros and no gradient, whether the table has such a row or not.  Any other token outside 0 .. vocab - 1 gives a row of NaN and no gradient. */
 typedef struct {
     int tokens, vocab, cols;    /* at most 2^30 tokens, 2^24 rows of the table, 2^20 columns */
@@ -320,7 +320,8 @@ size_t sol_embedding_backward_workspace_bytes(const sol_embedding_desc *ed);
  *   dtable     dense [vocab][cols] of dtable_dtype: the table's dtype or SOL_F32
  *   accumulate 0: every row of dtable is written (zeros where no token is); else the sums are added to the rows whose tokens occur, rounded once, and no other row is touched
  *              (a table that is also the weight of the last layer; gradients of several batches)
- * Sums are fp32.  Their order is fixed by the description and the tokens: a call repeated gives the same bits. */
+ * Sums are fp32.  Their order is fixed by the description and the tokens: a call repeated gives the same bits.  A row of up to 32 tokens (up to 64 where there are more than 512 in all)
+ * has them added one behind the other in the order of i; of more tokens stretches are summed so, and then their sums. */
 sol_status sol_embedding_backward(const sol_embedding_desc *ed, const void *tokens, const void *dy, void *dtable, int dtable_dtype, int accumulate,
                                   void *workspace, size_t workspace_bytes, void *hip_stream);
 

@@ -1,6 +1,7 @@
 // Embedding and the gradient of its table.
 //   forward   y[i] = scale * table[tokens[i]];  a padding token: zeros;  any other token outside the table: NaN
-//   backward  dtable[v] = scale * sum of the dy[i] with tokens[i] = v, in the order of i
+//   backward  dtable[v] = scale * sum of the dy[i] with tokens[i] = v.  Rows of up to CROWD tokens (up to RUN of more than DIRECT in all) have them added in the order of i; longer ones in
+//             stretches, which are summed by the waves that have them and then put together: an order that the tokens alone fix.
 #include <float.h>
 
 #include <type_traits>
@@ -426,8 +427,8 @@ template <typename TO, int W, int PIECES> __global__ void __launch_bounds__(256)
 }
 
 // ---- the gradient of few tokens, in one launch ----------------------------------------------------------------------------------
-// A workgroup looks at all tokens, lists those of its `block` rows in order, and sums and writes its rows, a wave each.  One row's tokens are added one behind the other, so
-// there can only be few; the rows without tokens, nearly all of them, are what the time goes into.  509 tokens, table 10007 x 201 fp32: 9 us, 20 in three launches; 512 equal tokens 18 and 36.
+// A workgroup looks at all tokens, lists those of its `block` rows in order, and sums and writes its rows, a wave each, or all four where a row has more than CROWD tokens.  A wave's tokens are added
+// one behind the other, so there can only be few; the rows without tokens, nearly all of them, are what the time goes into.  509 tokens, table 10007 x 201 fp32: 9 us, 20 in three launches; 512 equal tokens 18 and 36.
 constexpr int DIRECT = 512, CROWD = 32;
 struct DirectArgs {
     const void *tokens, *dy;

@@ -964,6 +964,26 @@ def test_sums_in_the_order_of_tokens(sol):
         assert len(tok) > 512 and np.array_equal(got.cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("n", [40, 300, 512])
+@pytest.mark.parametrize("cols", [24, 300, 1000])
+def test_sums_of_few_tokens_in_their_order(sol, n, cols):
+    """Up to 512 tokens: fp32 sums of rows of up to 32 tokens are those of the tokens' order, one addition behind the other, in crowded blocks of rows and elsewhere; longer ones give the same bits again."""
+    rng = np.random.default_rng([n, cols])
+    for vocab, spread in ((40, 1), (9000, 997)):
+        tok = np.concatenate([np.full(k, (i * spread) % vocab) for i, k in enumerate([1, 32, 7, 31, 60, 2, 32])])[:n]
+        tok = rng.permutation(np.concatenate([tok, np.where(rng.random(n - len(tok)) < 0.5, -1, vocab - 1 - rng.integers(0, min(vocab // 2, 20), n - len(tok)))]))
+        dy = rng.standard_normal((n, cols)).astype(np.float32)
+        want = np.zeros((vocab, cols), np.float32)
+        for i, t in enumerate(tok):
+            if t >= 0:
+                want[t] = want[t] + dy[i]
+        few = np.bincount(tok[tok >= 0], minlength=vocab) <= 32
+        assert few.sum() < vocab or n == 40
+        got = sol.sol_embedding_backward(dev(dy), torch.from_numpy(tok).to(DEV), vocab)
+        assert np.array_equal(got.cpu().numpy()[few], want[few])
+        assert torch.equal(got, sol.sol_embedding_backward(dev(dy), torch.from_numpy(tok).to(DEV), vocab))
+
+
 def test_clip_of_more_tensors_than_tables_hold(sol):
     """Six launches a pass, and more partial sums than every workgroup joins itself."""
     gen = torch.Generator(device=DEV).manual_seed(4)
