@@ -266,7 +266,8 @@ sol_status sol_linear_backward(const sol_linear_desc *ld, const void *dy, const 
  *   backward  h = (x - mean) * rstd,  g = dy * gamma
  *             dx = rstd * (g - mean(g) - h * mean(g * h)) + residual      dgamma = sum over the rows of dy * h     dbeta = sum over the rows of dy
  * Every sum, mean and rstd are fp32 for both dtypes.  An infinity or a NaN in a row, or a sum of its elements that fp32 does not hold, makes that row of y, and of dx,
- * NaN, and no other.  A row whose squared deviations add up to more than fp32 holds has rstd 0. */
+ * NaN, and no other.  A row whose squared deviations add up to more than fp32 holds has rstd 0, so that y is beta there, and NaN where
+ * a deviation itself is more than that (which makes its row of dx NaN). */
 typedef struct {
     int rows, cols;             /* at most 2^20 columns */
     int dtype;                  /* sol_dtype of x, y, dy, residual and dx */

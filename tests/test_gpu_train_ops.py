@@ -180,6 +180,18 @@ def test_rows_whose_sums_do_not_fit(sol, dt, rows, cols):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_deviations_that_do_not_fit(sol, dt):
+    """A finite row with a mean that fits and a deviation that does not: rstd is 0, the element with that deviation NaN, the others of y are beta; its row of dx is NaN, no other row takes notice."""
+    x = grid([[1, 2, 4], [3e38, -3e38, -1.5e38], [5, 3, 3]], dt)
+    beta = np.array([1.0, -2.0, 0.5], np.float32)
+    y, mean, rstd = sol.sol_layer_norm(dev(x, dt), None, dev(beta), want_stats=True)
+    assert abs(host(mean)[1] / x[1].mean() - 1) <= 4 * U and host(rstd)[1] == 0
+    assert np.isnan(host(y)[1, 0]) and np.array_equal(host(y)[1, 1:], beta[1:])
+    dx, dg, db = sol.sol_layer_norm_backward(dev(np.ones((3, 3)), dt), dev(x, dt), mean, rstd)
+    assert np.all(np.isnan(host(dx)[1])) and np.all(np.isfinite(host(dx)[[0, 2]])) and np.isnan(host(dg)[0]) and np.array_equal(host(db), np.full(3, 3.0))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("rows", [4, 1100])
 @pytest.mark.parametrize("cols", [1, 3, 7, 8, 24, 40, 64, 77, 200, 520, 1001, 2048, 2500, 4001, 8184, 9000, 16392])
 def test_backward_of_equal_elements_far_from_zero(sol, dt, rows, cols):
