@@ -1,4 +1,4 @@
-// What the kernels over rows of features share: sums over a wave and a workgroup, checks of the arguments (internal).
+// What the kernels over rows of features share: sums over a wave and over groups of its lanes, loads and stores of pieces and ends of rows, checks of the arguments (internal).
 #pragma once
 #include <utility>
 
@@ -26,25 +26,8 @@ __device__ __forceinline__ float wave_sum(float v) {
     return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63));
 }
 
-// 4 neighbouring elements of a row, of which nv exist, at any element's address
+// Stores 4 neighbouring elements of a row, of which nv exist, at any element's address
 typedef __attribute__((ext_vector_type(2), aligned(2))) uint32_t u32x2_any;
-template <typename T> __device__ __forceinline__ void load4_any(const T *p, float v[4], int nv) {
-    if (nv >= 4) {
-        if constexpr (sizeof(T) == 2) {
-            const u32x2_any w = *reinterpret_cast<const u32x2_any *>(p);
-            v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xffff0000u); v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xffff0000u);
-        } else {
-            const lds_pipe::u32x4_t w = *reinterpret_cast<const u32x4_any *>(p);
-#pragma unroll
-            for (int e = 0; e < 4; e++) v[e] = __uint_as_float(w[e]);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; e++) v[e] = nv > 0 ? Elem<T>::load(p + min(e, nv - 1)) : 0.f;
-#pragma unroll
-        for (int e = 1; e < 4; e++) v[e] = e < nv ? v[e] : 0.f;
-    }
-}
 template <typename T> __device__ __forceinline__ void store4_any(T *p, const float v[4], int nv) {
     if (nv >= 4) {
         if constexpr (sizeof(T) == 2) *reinterpret_cast<u32x2_any *>(p) = u32x2_any{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -56,7 +39,7 @@ template <typename T> __device__ __forceinline__ void store4_any(T *p, const flo
     }
 }
 
-// The same as they lie in memory, W = 4 or 8 of them, so that loads under way take no more registers than that
+// W = 4 or 8 neighbouring elements, of which nv exist, as they lie in memory, so that loads under way take no more registers than that
 template <typename T, int W> struct RawPiece {
     uint32_t w[W * sizeof(T) / 4] = {};
     __device__ __forceinline__ void load(const T *p, int nv) {
