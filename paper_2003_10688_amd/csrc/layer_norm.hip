@@ -478,10 +478,23 @@ sol_status check_norm(const sol_layer_norm_desc *nd, sol_layer_norm_desc *n) {
 enum { NORM_FORWARD, NORM_DX, NORM_GRAD };
 // Groups of 8 columns that a row may have in registers: where dx alone is computed, and where gamma and beta or the columns' sums are kept beside it
 constexpr int MAX_DX_GROUPS = 2048, MAX_GROUPS = 1024;
-// Few rows: columns are summed by workgroups of their own, beside the rows', in the same launch.  us, one launch against one pass and a launch for its parts: 512 rows of 2048 bf16 6.0 and 8.6,
-// 1024 rows 9.6 and 10.3, 1536 rows 17.2 and 11.7; 512 rows of 1531 fp32 6.6 and 9.4, 1024 rows 14.1 and 11.9.
+// Few rows: columns are summed by workgroups of their own, beside the rows', in the same launch.  us, that launch against one pass and a launch for its parts, calls of a graph with a residual and
+// changing inputs:     64 columns        512             2048            8192
+//   bf16   512 rows    5.8 and  8.3     6.3 and  8.1    8.2 and 11.0   11.6 and 16.2
+//         1024         9.1 and  8.5    11.7 and  9.9   13.7 and 14.2   20.2 and 24.8
+//         1536        13.1 and  9.1    17.1 and 11.1   18.7 and 15.7   29.0 and 30.2
+//   fp32   512         5.6 and  8.9     7.3 and  7.6    9.1 and 11.6   19.5 and 21.2
+//          768         8.3 and  9.4    10.0 and 10.1   12.2 and 13.8   27.5 and 28.7
+//         1024        10.6 and  9.2    12.4 and 10.7   15.2 and 14.9   34.3 and 34.7
+// One border for all widths: at it narrow bf16 rows lose 1 to 2 us, and behind it wide ones would gain as much.
 bool few_rows(int rows, int dt) { return (size_t)rows * dtype_size(dt) <= 2048; }
 
+// Threads that a row takes in norm_grad_kernel: one for each group of 8 columns, or two groups a thread for long rows that are no whole pieces (see GRAD_BLOCK)
+int grad_threads(int groups, bool whole) {
+    int t = 8;
+    while (t < groups) t *= 2;
+    return !whole && t > 256 ? t / 2 : t;
+}
 
 struct NormLaunch {
     int kind;
@@ -517,6 +530,22 @@ template <int TPR, int G, bool WHOLE, typename T> void launch_grad(const NormLau
         hipLaunchKernelGGL((norm_grad_kernel<TPR, G, false, false, T>), grid, block, 0, st, l.a, l.dgamma, l.dbeta);
     }
 }
+template <bool WHOLE, typename T> void launch_grad_rows(const NormLaunch &l, int groups, hipStream_t st) {
+    switch (grad_threads(groups, WHOLE)) {
+    case 8: return launch_grad<8, 1, WHOLE, T>(l, st);
+    case 16: return launch_grad<16, 1, WHOLE, T>(l, st);
+    case 32: return launch_grad<32, 1, WHOLE, T>(l, st);
+    case 64: return launch_grad<64, 1, WHOLE, T>(l, st);
+    case 128: return launch_grad<128, 1, WHOLE, T>(l, st);
+    case 256:
+        if constexpr (!WHOLE)
+            if (groups > 256) return launch_grad<256, 2, false, T>(l, st);
+        return launch_grad<256, 1, WHOLE, T>(l, st);
+    case 512: return launch_grad<512, WHOLE ? 1 : 2, WHOLE, T>(l, st);
+    default:
+        if constexpr (WHOLE) launch_grad<1024, 1, true, T>(l, st);
+    }
+}
 template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st) {
     const int groups = ceil_div(l.a.cols, 8);
     if (groups > (l.kind == NORM_DX ? MAX_DX_GROUPS : MAX_GROUPS)) {
@@ -533,25 +562,8 @@ template <typename T> sol_status launch_norm(const NormLaunch &l, hipStream_t st
         else if (groups <= 512) launch_rows<256, 2, T>(l, st);
         else if (groups <= 1024) launch_rows<512, 2, T>(l, st);
         else launch_rows<1024, 2, T>(l, st);
-    } else if (whole_rows<T>(l.a.cols)) {
-        if (groups <= 8) launch_grad<8, 1, true, T>(l, st);
-        else if (groups <= 16) launch_grad<16, 1, true, T>(l, st);
-        else if (groups <= 32) launch_grad<32, 1, true, T>(l, st);
-        else if (groups <= 64) launch_grad<64, 1, true, T>(l, st);
-        else if (groups <= 128) launch_grad<128, 1, true, T>(l, st);
-        else if (groups <= 256) launch_grad<256, 1, true, T>(l, st);
-        else if (groups <= 512) launch_grad<512, 1, true, T>(l, st);
-        else launch_grad<1024, 1, true, T>(l, st);
-    } else {
-        if (groups <= 8) launch_grad<8, 1, false, T>(l, st);
-        else if (groups <= 16) launch_grad<16, 1, false, T>(l, st);
-        else if (groups <= 32) launch_grad<32, 1, false, T>(l, st);
-        else if (groups <= 64) launch_grad<64, 1, false, T>(l, st);
-        else if (groups <= 128) launch_grad<128, 1, false, T>(l, st);
-        else if (groups <= 256) launch_grad<256, 1, false, T>(l, st);
-        else if (groups <= 512) launch_grad<256, 2, false, T>(l, st);
-        else launch_grad<512, 2, false, T>(l, st);
-    }
+    } else if (whole_rows<T>(l.a.cols)) launch_grad_rows<true, T>(l, groups, st);
+    else launch_grad_rows<false, T>(l, groups, st);
     SOL_HIP(hipGetLastError());
     return SOL_OK;
 }
@@ -563,10 +575,11 @@ int norm_parts(int rows, int cols, int dt) {
     if (groups <= MAX_DX_GROUPS && few_rows(rows, dt)) return 1;
     if (groups > MAX_GROUPS) return norm_chunks(rows, cols);
     const bool whole = cols % (16 / (int)dtype_size(dt)) == 0;
-    const int threads = groups <= 8 ? 8 : groups <= 16 ? 16 : groups <= 32 ? 32 : groups <= 64 ? 64 : groups <= 128 ? 128 : groups <= 256 ? 256 : !whole ? (groups <= 512 ? 256 : 512) : groups <= 512 ? 512 : 1024;
-    const int slots = (whole ? GRAD_BLOCK<true> : GRAD_BLOCK<false>) / threads;
+    const int slots = (whole ? GRAD_BLOCK<true> : GRAD_BLOCK<false>) / grad_threads(groups, whole);
     const long rounds = ((long)rows + slots - 1) / slots, most = min(rounds, groups <= 256 && !whole ? 512l : 256l);
     // A round of rows costs a workgroup about what 32 more parts cost the launch that sums them: 32 rounds = parts^2 makes the sum of both least.  Up to a GPU full of workgroups.
+    // us for both launches with 4, 16, 32, 64 and 512 in place of 32: 1021 x 1531 fp32 19.9, 15.6, 13.8, 14.6, 19.6 (46 to 511 parts); 2048 x 2048 bf16 24.8, 18.5, 16.2, 16.4, 16.5 (46 to 256);
+    // 4096 x 512 bf16 17.7, 13.5, 13.6, 12.3, 13.0; 4096 x 1024 fp32 37.8, 25.9, 21.2, 21.2, 20.3; 4096 x 4096 bf16 56.3, 39.0, 34.3, 34.2, 34.2; 20000 x 1001 fp32 77.6, 81.9, 69.7, 68.3, 68.4.
     long parts = 1;
     while (parts * parts < 32 * rounds && parts < most) parts++;
     return (int)parts;
