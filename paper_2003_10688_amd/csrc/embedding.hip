@@ -59,7 +59,9 @@ template <typename T, typename I, bool STREAM> __global__ void __launch_bounds__
 // ones, and reads all tokens.  It counts those of each of its rows and those of the residues in front, keeps what is its own in a list, in order, and writes the positions
 // of its rows' tokens behind each other.  So it takes one launch, without a word between the workgroups.  The tokens are read from L2, a second time where the list does not hold
 // a workgroup's share.  65536 tokens of text 22 us (358 with neighbouring rows in one workgroup, which then has half of all tokens), 4096 9 us; every 16384 more take 4 us,
-// 3 where tokens are spread evenly.
+// 3 where tokens are spread evenly.  That is for tables of up to 2^18 rows, 1024 for each of 256 workgroups.  A longer table takes as many more workgroups, each of which looks at all tokens, one to a CU:
+// 65536 tokens 33 to 36 us for 2^18 + 1 rows, 61 to 63 for 2^20, 211 to 217 for 2^22, 800 to 814 for 2^24 (the sums of 8 columns fp32 then take 52, 93, 255 and 1124).  Where all tokens are the same, one
+// workgroup has them all: 4096 10 us, 16384 18, 65536 88, 262144 339, and the launch that joins the run's parts 4, 11, 38 and 143.
 constexpr int INDEX_THREADS = 1024, INDEX_EACH = 16, INDEX_TILE = INDEX_THREADS * INDEX_EACH, INDEX_ROWS = 1024, INDEX_GROUPS = 256, INDEX_WAVES = INDEX_THREADS / 64;
 constexpr int LIST_BITS = 22;   // of a position in a list's entry, the row's 10 above them
 constexpr int RUN = 64;         // longer runs of one token are summed in parts of the sorted order, RUN positions each

@@ -45,7 +45,7 @@ __device__ __forceinline__ float mean_of(float sum, float n, float inv) {
 
 // Sums and squared deviations of the waves, put together: mean = sum s_w / n, deviations = sum (d_w + n_w (mean_w - mean)^2) (Chan, Golub, LeVeque).
 // One barrier a row; two sets of slots in turn, so that the next row's values do not meet readers of this one's.
-// A row stays in registers between its only reading and its writing, gamma and beta for all rows of a workgroup.  Bound by memory: 16384 x 4096 bf16 43 us (6.2 TB/s), 2^20 x 64 43 us with 8 threads a
+// A row stays in registers between its only reading and its writing, gamma and beta for all rows of a workgroup.  Bound by memory: 16384 x 4096 bf16 43 us (6.2 TB/s; 52, 5.2 TB/s, with inputs that the last cache does not hold), 2^20 x 64 43 us with 8 threads a
 // row (162 with a wave's 64), 16384 x 8192 84 us with results past the caches (100 without); one row of 2048 2.2 us, a launch and one round trip.
 template <int TPR, int G, bool WHOLE, bool STREAM, typename T>
 __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) {
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(ROW_BLOCK<TPR>) norm_kernel(const NormArgs a) 
             }
             phase ^= 1;
         }
-        const float rstd = __builtin_amdgcn_rsqf(m2 * a.inv_cols + a.eps);
+        const float rstd = __builtin_amdgcn_rsqf(m2 * a.inv_cols + a.eps);      // within 1 ulp: half an ulp more than a rounded root, beside sums over a row
         T *y = static_cast<T *>(a.y) + row * a.ldy;
 #pragma unroll
         for (int k = 0; k < P; k++) {
@@ -151,7 +151,7 @@ template <typename T> __global__ void __launch_bounds__(1024) norm_long_kernel(c
                 s += d * d;
             }
         }
-        const float rstd = __builtin_amdgcn_rsqf(block_sum(s, red) * a.inv_cols + a.eps);
+        const float rstd = __builtin_amdgcn_rsqf(block_sum(s, red) * a.inv_cols + a.eps);       // within 1 ulp, as above
         for (int c = threadIdx.x * 8; c < a.cols; c += 8192) {
             const int nv = min(8, a.cols - c);
             float g[8], b[8];

@@ -1,4 +1,6 @@
 // What the kernels over rows of features share: sums over a wave and over groups of its lanes, loads and stores of pieces and ends of rows, checks of the arguments (internal).
+// Times in the comments of these kernels are a kernel's own, called again on the same inputs, of which the last cache (256 MB) holds a part or all, where they name nothing else: 6 TB/s and more are
+// its doing.  With inputs that it does not hold, copies of 256 MB to 1 GB reach 5.05 to 5.40 TB/s.
 #pragma once
 #include <utility>
 
