@@ -1092,3 +1092,53 @@ def test_tokens_of_any_shape(sol):
         table, dy = torch.randn((90, 24), generator=gen, device=DEV), torch.randint(-2, 3, (*shape, 24), generator=gen, device=DEV).float()
         assert torch.equal(sol.sol_embedding(tokens, table), table[tokens])
         assert torch.equal(sol.sol_embedding_backward(dy, tokens, 90), torch.zeros((90, 24), device=DEV).index_add_(0, tokens.reshape(-1), dy.reshape(-1, 24)))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_large_results_at_odd_addresses(sol, dt):
+    """What is written past the caches, in rows of odd length or odd pitch, whose pieces start at any element: whole numbers, and the bits of calls on fewer rows."""
+    gen = torch.Generator(device=DEV).manual_seed(3)
+    cols, size = 961, 2 if dt == "bf16" else 4
+    many = (1 << 28) // (cols * size) + 5
+    dy = torch.randint(-2, 3, (3000, cols + 2), generator=gen, device=DEV).to(TDT[dt])[:, :cols]
+    for n in (400, 3000):
+        tokens = torch.randint(0, many, (n,), generator=gen, device=DEV)
+        got = sol.sol_embedding_backward(dy[:n], tokens, many)
+        assert got.nbytes >= 1 << 28 and torch.equal(got, torch.zeros((many, cols), device=DEV).index_add_(0, tokens, dy[:n].float()).to(TDT[dt]))
+    tokens, out = torch.randint(0, 3000, (many,), generator=gen, device=DEV), torch.full((many, cols + 2), 7, dtype=TDT[dt], device=DEV)
+    sol.sol_embedding(tokens, dy, out=out[:, :cols])
+    assert torch.equal(out[:, :cols], dy[tokens]) and torch.all(out[:, cols:] == 7)
+    del got, out
+    cols = 8192
+    rows = (1 << 28) // (cols * size) + 3
+    x, gamma = torch.randn((rows, cols + 1), generator=gen, device=DEV).to(TDT[dt])[:, :cols], torch.randn(cols, generator=gen, device=DEV)
+    out = torch.full((rows, cols + 1), 7, dtype=TDT[dt], device=DEV)
+    sol.sol_layer_norm(x, gamma, out=out[:, :cols])
+    assert torch.all(out[:, cols:] == 7)
+    for a in range(0, rows, 8 * 500):                               # rows of a 16-byte border each
+        assert torch.equal(out[a:a + 4000, :cols], sol.sol_layer_norm(x[a:a + 4000], gamma)[0])
+    del x, out
+    torch.cuda.empty_cache()
+
+
+def test_clip_gradients_of_a_bf16_network(sol):
+    """Convolutions with batch norm: the norm of the fp32 gradients of all layers, each scaled once, whatever the network's type."""
+    from paper_2003_10688_amd import workloads as wl
+
+    wk = wl.config(4, batch=4, hw=32)
+    net = sol.Network(wk.layers, wk.in_shape, sol.BF16, flags=sol.NET_TRAINING)
+    net.set_params(wk.params)
+    x, labels = sol.to_device_nhwc(wk.x, sol.BF16), torch.tensor([1, 0, 3, 2], dtype=torch.int32, device=DEV)
+    net.forward(x)
+    net.backward(x, labels)
+    kinds = [(i, k) for i, l in enumerate(wk.layers) if l["kind"] in ("conv", "linear")
+             for k in [sol.NT_GRAD_W] + ([sol.NT_GRAD_GAMMA, sol.NT_GRAD_BETA] if l["kind"] == "conv" and l["bn"] else [sol.NT_GRAD_BIAS])]
+    before = [net.tensor(i, k).clone() for i, k in kinds]
+    want = float(sum((g.double() ** 2).sum() for g in before).sqrt())
+    limit = float(np.float32(want / 5))
+    got = float(net.clip_gradients(limit))
+    assert want > 0 and abs(got - want) <= 1.01 * U * want
+    for (i, k), g in zip(kinds, before):
+        # norm, quotient and product are rounded
+        exact = g.double() * (limit / want)
+        assert torch.all((net.tensor(i, k).double() - exact).abs() <= 4 * U * exact.abs() + 2.0**-149), (i, k)
