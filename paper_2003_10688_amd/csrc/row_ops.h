@@ -44,7 +44,8 @@ template <typename T> __device__ __forceinline__ void store4_any(T *p, const flo
 // W = 4 or 8 neighbouring elements, of which nv exist, as they lie in memory, so that loads under way take no more registers than that
 template <typename T, int W> struct RawPiece {
     uint32_t w[W * sizeof(T) / 4] = {};
-    __device__ __forceinline__ void load(const T *p, int nv) {
+    // REPEAT: places behind the nv elements hold the last of them instead of 0
+    template <bool REPEAT = false> __device__ __forceinline__ void load(const T *p, int nv) {
         if (nv >= W) {
             if constexpr (sizeof(w) == 8) {
                 const u32x2_any v = *reinterpret_cast<const u32x2_any *>(p);
@@ -62,7 +63,7 @@ template <typename T, int W> struct RawPiece {
 #pragma unroll
             for (int e = 0; e < W; e++) v[e] = nv > 0 ? Elem<T>::load(p + min(e, nv - 1)) : 0.f;
 #pragma unroll
-            for (int e = 1; e < W; e++) v[e] = e < nv ? v[e] : 0.f;
+            for (int e = 1; e < W; e++) v[e] = REPEAT || e < nv ? v[e] : 0.f;
             if constexpr (sizeof(T) == 2) {
 #pragma unroll
                 for (int e = 0; e < W / 2; e++) w[e] = __float_as_uint(v[2 * e]) >> 16 | (__float_as_uint(v[2 * e + 1]) & 0xffff0000u);
@@ -107,12 +108,11 @@ template <int W> struct Span {
     }
     __device__ __forceinline__ bool some() const { return skip < W; }
     __device__ __forceinline__ bool has(int e) const { return e >= skip && e < end; }
-    __device__ __forceinline__ bool holds(int e) const { return some() && e < end; }       // load() has put the row's element there, the thread's own or the one's in front
     // WHOLE: the row's length is a multiple of W
-    template <bool WHOLE, typename T> __device__ __forceinline__ void load(const T *row, RawPiece<T, W> &r) const {
+    template <bool WHOLE, bool REPEAT = false, typename T> __device__ __forceinline__ void load(const T *row, RawPiece<T, W> &r) const {
         if (!some()) return;
         if (WHOLE || end == W) r.load(row + c, W);
-        else r.load(row + c, end);
+        else r.template load<REPEAT>(row + c, end);
     }
     template <bool WHOLE, bool STREAM = false, typename T> __device__ __forceinline__ void store(T *row, const float *v) const {
         if (!some()) return;
